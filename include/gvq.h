@@ -465,6 +465,68 @@ gvq_status gvq_compress_quantize_aggregate(gvq_ctx *ctx, const float *const *g_n
                                            const float *mu, int levels, uint64_t seed, float *s_sum,
                                            int8_t *const *q_nodes_opt, float *const *norms_nodes_opt);
 
+/* ---- microscaled 4-bit floating point ------------------------------------------------------------------
+   The paper's iterations without the compressor send 4 bits an entry (Section 3); gvq_quantize_raw4 does that with one
+   norm per slice.  Here a block of 32 entries has a scale of its own, so that a slice's small entries survive beside
+   its large ones, and the tensor cores multiply the format as it is.
+
+   Format.  A matrix [rows][cols] is quantized along its rows: a block is 32 consecutive entries of a row (the last one
+   of a row may be shorter and is continued by zeros).  scale = 2^(s - 127), s the smallest integer >= 0 with
+   max |x| <= 6 * scale; an entry is one of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} times the scale (code = sign << 3 | index).
+   A block that holds a NaN or an infinity has s = 255 and codes 0 and stands for 32 NaN.
+     nearest:     the nearest of those values, ties to the even index;
+     stochastic:  with r = |x| / scale and step = 0.5 (r < 2), 1 (r < 4), 2:   ((floor(65536 r / step) + u) >> 16) steps,
+                  u = a 16-bit number: with h and x of gvq_quantize's hash24 for (seed, node, i = row, j = column / 2), the
+                  low half of x for an even column, the high half for an odd one.  max |x| <= 6 * scale makes it unbiased
+                  (to 2^-16 of a step).
+   codes:  device bytes [rows][16 * ceil(cols / 32)], two codes a byte, the even column in the low half.
+   scales: device bytes, tiles of 128 rows x 4 blocks, tile (row / 128, block / 4) in row-major order of tiles, and in a
+           tile byte (row % 32) * 16 + (row % 128) / 32 * 4 + block % 4; bytes outside the matrix are 0.
+   "Along the columns" means the same of the transposed matrix [cols][rows], its rows and columns being those of the
+   hash: what the call would give for a transposed copy of the input.
+   Sizes: rows, cols >= 1; ceil(rows / 128) * ceil(cols / 128) < 2^31. */
+typedef enum { GVQ_F32 = 0, GVQ_BF16 = 1, GVQ_F16 = 2 } gvq_dtype;
+enum { GVQ_ROUND_NEAREST = 0, GVQ_ROUND_STOCHASTIC = 1 };
+
+/* Bytes of the two arrays of a quantized matrix [rows][cols]; -1 on bad sizes. */
+int64_t gvq_mx4_codes_bytes(int64_t rows, int64_t cols);
+int64_t gvq_mx4_scales_bytes(int64_t rows, int64_t cols);
+
+/* Quantizes a matrix along its rows (codes, scales) and / or along its columns (codes_t, scales_t), reading it once.
+   A pair may be NULL, not both.  x: device, entries of type dtype, rows ld entries apart (ld >= cols; x aligned to its
+   entries' size only -- rows that start at 16-byte boundaries are read faster).  seed and node matter for stochastic
+   rounding only. */
+gvq_status gvq_mx4_quantize(gvq_ctx *ctx, const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, int rounding,
+                            uint64_t seed, uint32_t node, uint8_t *codes, uint8_t *scales, uint8_t *codes_t,
+                            uint8_t *scales_t);
+/* What a quantized matrix stands for.  out: device fp32, rows ld floats apart. */
+gvq_status gvq_mx4_dequantize(gvq_ctx *ctx, const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols,
+                              float *out, int64_t ld);
+
+/* The product of two quantized matrices, both quantized along the contraction:
+     out[m][n] = sum over k < K of a[m][k] * b[n][k]        (products exact, summed in fp32, rounded once to dtype)
+   a: [M][K], b: [N][K] as gvq_mx4_quantize lays them out; out: device, dtype entries, rows ld entries apart (ld >= N),
+   aligned to its entries' size.  A linear layer y = x W^T takes x and W along their rows; its gradients
+   dx = dy W take dy along its rows and W along its columns, dW = dy^T x both along their columns.
+   Few rows of a (M <= 64, a token or a small batch against kept weights) have a form of their own. */
+gvq_status gvq_mx4_matmul(gvq_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *b_codes,
+                          const uint8_t *b_scales, int64_t M, int64_t N, int64_t K, void *out, int dtype, int64_t ld);
+
+/* The exchange of an iteration without the compressor, in this format: the context's full slices are the rows of a
+   matrix [S][d] (row = global slice index), the tails are not quantized.
+   gvq_mx4_quantize_aggregate quantizes the slices of N nodes, whose indices are node0 .. node0 + N - 1, and sums what
+   the codes stand for:  g_sum = sum_{n<N} value_n  (fp32, n ascending), tails summed as they are; every gradient is read
+   once.  g_sum: device [M] or NULL; codes_nodes_opt, scales_nodes_opt: both NULL, or host arrays of N device pointers that
+   receive what each node would send ([S] x [d], sizes as above).  One node's share of an exchange: N = 1, node0 = its
+   index, g_sum = NULL.
+   gvq_mx4_dequantize_aggregate is the receiver's side: the same sum from codes (bit-identical). */
+gvq_status gvq_mx4_quantize_aggregate(gvq_ctx *ctx, const float *const *g_nodes, int N, uint32_t node0, int rounding,
+                                      uint64_t seed, float *g_sum, uint8_t *const *codes_nodes_opt,
+                                      uint8_t *const *scales_nodes_opt);
+gvq_status gvq_mx4_dequantize_aggregate(gvq_ctx *ctx, const uint8_t *const *codes_nodes,
+                                        const uint8_t *const *scales_nodes, const float *const *g_nodes_for_tails, int N,
+                                        float *g_sum);
+
 /* The whole path for callers whose gradients live in HOST memory (Eq. 3 + Eq. 4 + Eq. 5):
    copies the N gradients to the device scratch, runs gvq_compress_aggregate and
    gvq_decompress there, copies g_hat back and waits for it.

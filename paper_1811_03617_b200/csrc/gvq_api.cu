@@ -4,6 +4,7 @@
 #include <cstring>
 #include <new>
 
+#include "api_util.h"
 #include "gvq_internal.h"
 
 using namespace gvq;
@@ -11,8 +12,6 @@ using namespace gvq;
 namespace {
 
 constexpr size_t kMaxSmem = 227 * 1024;
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 gvq_status check_layout(const gvq_layout *l)
 {
@@ -42,38 +41,6 @@ int count_tiles(const gvq_layout *l, int rows)
     for (int i = 0; i < l->n_layers; ++i) n += (l->layer_len[i] / l->d + rows - 1) / rows;
     return (int)n;
 }
-
-gvq_status cuda_fail(gvq_ctx *ctx, cudaError_t e)
-{
-    if (ctx) ctx->last_cuda_error = (int)e;
-    (void)cudaGetLastError();
-    // tmap_slot's refusal to upload tensor maps while the stream is being captured
-    return e == cudaErrorStreamCaptureUnsupported ? GVQ_ERR_CAPTURE : GVQ_ERR_CUDA;
-}
-
-#define GVQ_CUDA(ctx, call)                                    \
-    do {                                                       \
-        cudaError_t e__ = (call);                              \
-        if (e__ != cudaSuccess) return cuda_fail((ctx), e__);  \
-    } while (0)
-
-template <typename T>
-gvq_status gather_nodes(const T *const *src, int N, NodePtrs<const T> &dst, bool need_align = true)
-{
-    if (!src) return GVQ_ERR_NULL;
-    if (N < 1 || N > GVQ_MAX_NODES) return GVQ_ERR_SHAPE;
-    for (int n = 0; n < GVQ_MAX_NODES; ++n) dst.p[n] = nullptr;
-    for (int n = 0; n < N; ++n) {
-        if (!src[n]) return GVQ_ERR_NULL;
-        if (need_align && !aligned16(src[n])) return GVQ_ERR_ALIGN;
-        dst.p[n] = src[n];
-    }
-    return GVQ_OK;
-}
-
-using EncodeTiledFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                   const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 // Finds (or makes) the slot that holds the tensor maps of gradient buffer `ptr`: one 2-D map per layer,
 // inner dimension = the d entries of a slice, outer = the layer's S_l slices, box = 32 entries x 128
@@ -259,19 +226,6 @@ cudaError_t clear_device_fault(gvq_ctx *ctx)
                             ctx->stream);
     return e;
 }
-
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = false;
-    explicit DeviceGuard(int dev)
-    {
-        if (cudaGetDevice(&prev) == cudaSuccess) ok = cudaSetDevice(dev) == cudaSuccess;
-    }
-    ~DeviceGuard()
-    {
-        if (ok && prev >= 0) cudaSetDevice(prev);
-    }
-};
 
 }  // namespace
 

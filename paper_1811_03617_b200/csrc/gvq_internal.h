@@ -47,6 +47,10 @@ struct LayerTables {
     int64_t *tail_pos = nullptr;  // [n_tails] offset of the tail in the tail part of an exchange buffer
 };
 
+using EncodeTiledFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                   const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);   // cuTensorMapEncodeTiled
+
 // Node pointers travel to the kernels by value.
 template <typename T>
 struct NodePtrs {
@@ -146,6 +150,24 @@ cudaError_t launch_quantize_aggregate(cudaStream_t st, int num_sms, int k, int64
 cudaError_t launch_dequantize_aggregate(cudaStream_t st, int num_sms, int k, int64_t S,
                                         const NodePtrs<const int8_t> &q, const NodePtrs<const float> &norms,
                                         int n_nodes, int levels, float *s_sum);
+
+// Microscaled 4-bit floating point (mx4_quantize.cu, mx4_matmul.cu).  dtype: gvq_dtype.  A null pair of outputs is not
+// written; at least one pair is given.
+cudaError_t launch_mx4_quantize(cudaStream_t st, const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld,
+                                bool stochastic, uint64_t seed, uint32_t node, uint8_t *codes, uint8_t *scales,
+                                uint8_t *codes_t, uint8_t *scales_t);
+// All nodes' full slices (tiles of kDecompressRows slices) and the sum of what their codes stand for; out may be null.
+cudaError_t launch_mx4_quantize_aggregate(cudaStream_t st, int d, int64_t S, const TileTable &tiles, const LayerTables &lt,
+                                          const NodePtrs<const float> &g, int n_nodes, uint32_t node0, bool stochastic,
+                                          uint64_t seed, float *out, const NodePtrs<uint8_t> *codes,
+                                          const NodePtrs<uint8_t> *scales);
+// Codes back to values, summed over the nodes: a matrix (rows ld apart), or with lt the slices of a layout.
+cudaError_t launch_mx4_dequantize(cudaStream_t st, int num_sms, const NodePtrs<const uint8_t> &codes,
+                                  const NodePtrs<const uint8_t> &scales, int n_nodes, int64_t rows, int64_t cols, float *out,
+                                  int64_t ld, const LayerTables *lt, int n_layers);
+cudaError_t launch_mx4_matmul(cudaStream_t st, int num_sms, EncodeTiledFn enc, const uint8_t *a, const uint8_t *sa, const uint8_t *b,
+                              const uint8_t *sb, int64_t M, int64_t N, int64_t K, void *out, int dtype, int64_t ld,
+                              int32_t *error_word, int wait_kcycles, int test_drop);
 
 // Basis fit.  Workspace layout is private to fit_basis.cu.
 size_t fit_workspace_bytes(int d, int n_layers, int n_fit_tiles);

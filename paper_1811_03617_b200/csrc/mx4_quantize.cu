@@ -1,0 +1,420 @@
+// Quantization to microscaled 4-bit floating point, and back (gvq.h, "microscaled 4-bit").
+//
+//  mx4_quantize_kernel            a matrix, along its rows and / or along its columns (the transposed operand), read once
+//  mx4_quantize_aggregate_kernel  every node's slices, and the sum over the nodes of what the codes stand for
+//  mx4_dequantize_kernel          codes back to values, summed over the nodes
+#include "gvq_internal.h"
+#include "mx4.cuh"
+
+namespace gvq {
+namespace {
+
+using namespace mx4;
+
+template <typename T> __device__ __forceinline__ float to_f(T x);
+template <> __device__ __forceinline__ float to_f(float x) { return x; }
+template <> __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <> __device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
+
+// Eight consecutive entries as they lie in memory.
+template <typename T> struct Raw8 { uint4 q[sizeof(T) / 2]; };
+
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8(const T *p, int n, bool vec)
+{
+    Raw8<T> r;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.q[i] = make_uint4(0, 0, 0, 0);
+    if (n >= 8 && vec) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.q[i] = __ldcs(reinterpret_cast<const uint4 *>(p) + i);
+    } else if (n > 0) {
+        T e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = i < n ? p[i] : T(0.0f);
+        memcpy(&r, e, sizeof(r));
+    }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void unpack8(const Raw8<T> &r, float (&v)[8])
+{
+    T e[8];
+    memcpy(e, &r, sizeof(r));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = to_f(e[i]);
+}
+
+struct QuantParams {
+    const void *x;
+    int64_t rows, cols, ld;
+    uint64_t seed_w;            // mix64 of (seed, node)
+    uint8_t *codes, *scales;    // along the rows; null: not wanted
+    uint8_t *codes_t, *scales_t;   // along the columns
+    int vec;                    // rows start at 16-byte boundaries
+    int ct;                     // tiles along the columns
+};
+
+// One CTA: a tile of 128 x 128 entries, which is one tile of scale bytes of either form.  Rows: 16 lanes hold a row's
+// 128 entries (eight each, 16- or 32-byte loads), a quad holds a block.  Columns: the same entries go through shared
+// memory in their own type, and a thread takes 32 entries of a column (two columns of a 16-bit type at a time, so that
+// a word is read once).  The columns' blocks are skewed by eight words per 32 rows, so that the four blocks of eight
+// columns that a warp works on lie in different banks, and a warp's four lanes write 64 bytes of one output row.
+template <typename T, bool SR, bool ROWS, bool COLS>
+__global__ void __launch_bounds__(256) mx4_quantize_kernel(const QuantParams prm)
+{
+    constexpr int W = 128 * (int)sizeof(T) / 4;    // words of a row of the tile
+    extern __shared__ uint4 smem_q[];
+    uint32_t *tile = reinterpret_cast<uint32_t *>(smem_q);          // [128][W] + skew, when COLS
+    __shared__ __align__(16) uint8_t sc[2][kTileBytes];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rtile = blockIdx.x / prm.ct, ctile = blockIdx.x - rtile * prm.ct;
+    const int64_t r0 = (int64_t)rtile * 128, c0 = (int64_t)ctile * 128;
+    const T *x = static_cast<const T *>(prm.x);
+    const int64_t pitch = 16 * blocks(prm.cols), pitch_t = 16 * blocks(prm.rows);
+
+    // warp w, iteration it: rows 16 w + 2 it + (lane >> 4)
+    const int cl = (lane & 15) * 8;
+    const int ncol = (int)min((int64_t)8, prm.cols - (c0 + cl));    // this lane's valid entries (<= 0: none)
+    uint64_t h_own = 0;
+    if (ROWS && SR) h_own = row_word(prm.seed_w, r0 + 16 * warp + (lane & 15));
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        Raw8<T> raw[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t r = r0 + 16 * warp + 2 * (4 * half + i) + (lane >> 4);
+            raw[i] = load8(x + r * prm.ld + c0 + cl, r < prm.rows ? ncol : 0, prm.vec);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int rl = 16 * warp + 2 * (4 * half + i) + (lane >> 4);
+            if (COLS) {
+#pragma unroll
+                for (int q = 0; q < (int)sizeof(T) / 2; ++q)
+                    *reinterpret_cast<uint4 *>(tile + rl * W + (rl >> 5) * 8 + (lane & 15) * (int)sizeof(T) * 2 + q * 4) = raw[i].q[q];
+            }
+            if (ROWS) {
+                float v[8];
+                unpack8(raw[i], v);
+                const float amax = quad_max(amax8(v));
+                const uint32_t s = scale_byte(amax);
+                uint64_t h = 0;
+                if (SR) h = __shfl_sync(0xffffffffu, h_own, rl & 15);
+                if (s == 255u) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+                }
+                grid8<SR>(v, inv_scale(min(s, 253u)), h, (uint32_t)((c0 + cl) >> 1));
+                const int64_t r = r0 + rl, b = (c0 + cl) >> 5;
+                if (r < prm.rows && b < blocks(prm.cols))
+                    *reinterpret_cast<uint32_t *>(prm.codes + r * pitch + ((c0 + cl) >> 1)) = codes8(v);
+                if ((lane & 3) == 0) sc[0][(rl & 31) * 16 + (rl >> 5) * 4 + ((lane & 15) >> 2)] = (uint8_t)s;
+            }
+        }
+    }
+    __syncthreads();
+    if (COLS) {
+        constexpr int PER = 4 / (int)sizeof(T);                 // columns of a word: 1 or 2
+        const int blk = lane & 3;
+#pragma unroll 1
+        for (int cw = warp * 8 + (lane >> 2); cw < W; cw += 64) {
+            uint32_t w[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) w[i] = tile[(blk * 32 + i) * W + blk * 8 + cw];
+#pragma unroll
+            for (int part = 0; part < PER; ++part) {
+                const int cl2 = cw * PER + part;
+                const int64_t c = c0 + cl2, b = (r0 >> 5) + blk;
+                auto entry = [&](int i) -> float {
+                    if (sizeof(T) == 4) return __uint_as_float(w[i]);
+                    T e;
+                    const uint16_t u = (uint16_t)(part ? w[i] >> 16 : w[i] & 0xFFFFu);
+                    memcpy(&e, &u, sizeof(e) < 2 ? sizeof(e) : 2);
+                    return to_f(e);
+                };
+                float amax = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) amax = max_nan(amax, fabsf(entry(i)));
+                const uint32_t s = scale_byte(amax);
+                const float inv = inv_scale(min(s, 253u));
+                uint64_t h = 0;
+                if (SR) h = row_word(prm.seed_w, c);
+                uint32_t code[4];
+#pragma unroll
+                for (int o = 0; o < 4; ++o) {
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = s == 255u ? 0.0f : entry(8 * o + e);
+                    grid8<SR>(v, inv, h, (uint32_t)((r0 + blk * 32 + 8 * o) >> 1));
+                    code[o] = codes8(v);
+                }
+                if (c < prm.cols && b < blocks(prm.rows))
+                    *reinterpret_cast<uint4 *>(prm.codes_t + c * pitch_t + b * 16) = make_uint4(code[0], code[1], code[2], code[3]);
+                sc[1][(cl2 & 31) * 16 + (cl2 >> 5) * 4 + blk] = (uint8_t)s;
+            }
+        }
+        __syncthreads();
+    }
+    // the tile's scale bytes, whole (entries past the matrix are zeros, whose scale byte is 0)
+    if (ROWS && tid < 32)
+        reinterpret_cast<uint4 *>(prm.scales + ((int64_t)rtile * prm.ct + ctile) * kTileBytes)[tid] =
+            reinterpret_cast<const uint4 *>(sc[0])[tid];
+    if (COLS && tid >= 32 && tid < 64)
+        reinterpret_cast<uint4 *>(prm.scales_t + ((int64_t)ctile * tiles_of(prm.rows, 128) + rtile) * kTileBytes)[tid - 32] =
+            reinterpret_cast<const uint4 *>(sc[1])[tid - 32];
+}
+
+struct AggParams {
+    int d, n_nodes;
+    uint64_t seed_w[GVQ_MAX_NODES];
+    const int32_t *tile_layer, *tile_row0, *layer_S;
+    const int64_t *layer_off, *layer_soff;
+    NodePtrs<const float> g;
+    NodePtrs<uint8_t> codes, scales;
+    float *out;                 // may be null
+};
+
+// A quad of lanes takes a block of a slice and goes through the nodes: eight entries a lane, read once, quantized, and
+// what the codes stand for added (fp32, n ascending; code times power of two is exact, so the only rounding is the
+// sum's).  OUT: the codes and scale bytes are wanted.
+template <bool SR, bool OUT>
+__global__ void __launch_bounds__(256) mx4_quantize_aggregate_kernel(const __grid_constant__ AggParams prm)
+{
+    const int t = blockIdx.x, layer = prm.tile_layer[t], row0 = prm.tile_row0[t];
+    const int rows = min(kDecompressRows, prm.layer_S[layer] - row0);
+    const int d = prm.d, nb = (d + kBlock - 1) / kBlock;
+    const int64_t base = prm.layer_off[layer] + (int64_t)row0 * d, slice0 = prm.layer_soff[layer] + row0;
+    const int64_t kt = tiles_of(nb, kTileBlocks);
+    const int lane4 = threadIdx.x & 3;
+    // every thread of a warp makes the same number of rounds: the shuffles below need the whole quad
+    const int n_items = rows * nb, rounds = (n_items + 63) / 64;
+    for (int it = 0; it < rounds; ++it) {
+        const int item = it * 64 + (threadIdx.x >> 2);
+        const bool in = item < n_items;
+        const int row = in ? item / nb : 0, b = in ? item - row * nb : 0;
+        const int j = b * kBlock + lane4 * 8;                    // first entry of this lane in the slice
+        const bool in0 = in && j < d, in1 = in && j + 4 < d;     // d is a multiple of 4
+        const int64_t at = base + (int64_t)row * d + j;
+        const int64_t slice = slice0 + row;
+        float acc[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+        constexpr int U = 4;                                     // nodes whose loads are in flight together
+        for (int n0 = 0; n0 < prm.n_nodes; n0 += U) {
+            float4 x[U][2];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                x[u][0] = x[u][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (n0 + u < prm.n_nodes) {
+                    const float4 *src = reinterpret_cast<const float4 *>(prm.g.p[n0 + u] + at);
+                    if (in0) x[u][0] = __ldcs(src);
+                    if (in1) x[u][1] = __ldcs(src + 1);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (n0 + u >= prm.n_nodes) break;
+                const int n = n0 + u;
+                float v[8] = {x[u][0].x, x[u][0].y, x[u][0].z, x[u][0].w, x[u][1].x, x[u][1].y, x[u][1].z, x[u][1].w};
+                const uint32_t s = scale_byte(quad_max(amax8(v)));
+                if (s == 255u) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+                }
+                const uint64_t h = SR ? row_word(prm.seed_w[n], slice) : 0;
+                grid8<SR>(v, inv_scale(min(s, 253u)), h, (uint32_t)(j >> 1));
+                if (OUT || !SR) {
+                    const uint32_t code = codes8(v);
+                    if (OUT && in && prm.codes.p[n]) {
+                        *reinterpret_cast<uint32_t *>(prm.codes.p[n] + (slice * nb + b) * 16 + lane4 * 4) = code;
+                        if (lane4 == 0) prm.scales.p[n][scale_at(slice, b, kt)] = (uint8_t)s;
+                    }
+                    if (!SR) {   // nearest: the grid value is what the code stands for
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const uint32_t c = code >> (4 * e);
+                            const uint32_t m = c & 7u;
+                            const float mag = m < 2u ? 0.5f * (float)m : __uint_as_float((m + 252u) << 22);
+                            v[e] = with_sign(mag, __uint_as_float(c << 28));
+                        }
+                    }
+                }
+                const float sv = scale_value(s);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[e] = fmaf(v[e], sv, acc[e]);
+            }
+        }
+        if (prm.out) {
+            float4 *dst = reinterpret_cast<float4 *>(prm.out + at);
+            if (in0) dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+            if (in1) dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+        }
+    }
+}
+
+// Scale bytes past the last slice or block of an operand that the kernel above writes entry by entry: zeros.
+__global__ void mx4_clear_scale_padding_kernel(NodePtrs<uint8_t> scales, int64_t S, int nb)
+{
+    const int64_t kt = tiles_of(nb, kTileBlocks), rt = tiles_of(S, kTileRows);
+    uint8_t *s = scales.p[blockIdx.y];
+    if (!s) return;
+    const int64_t total = rt * kt * kTileBytes;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t tile = i / kTileBytes;
+        const int in = (int)(i - tile * kTileBytes);
+        const int64_t row = (tile / kt) * kTileRows + ((in >> 2) & 3) * 32 + (in >> 4), b = (tile % kt) * kTileBlocks + (in & 3);
+        if (row >= S || b >= nb) s[i] = 0;
+    }
+}
+
+struct DeqParams {
+    int n_nodes;
+    int64_t rows, cols;         // of the quantized matrix
+    int64_t ld;                 // of the output; ignored when a layout gives the rows' places
+    int d;
+    int n_layers;
+    const int64_t *layer_off, *layer_soff;
+    const int32_t *layer_S;
+    NodePtrs<const uint8_t> codes, scales;
+    float *out;
+    int vec;
+};
+
+// A lane takes eight entries of a row, one after the other every node's: four code bytes and the block's scale byte.
+template <bool LAYOUT>
+__global__ void __launch_bounds__(256) mx4_dequantize_kernel(const __grid_constant__ DeqParams prm)
+{
+    const int64_t nb = blocks(prm.cols), kt = tiles_of(nb, kTileBlocks);
+    const int64_t total = prm.rows * nb * 4;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / (nb * 4), piece = i - row * (nb * 4), b = piece >> 2;
+        const int64_t sc = scale_at(row, b, kt);
+        float acc[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+        for (int n = 0; n < prm.n_nodes; ++n) {
+            const uint32_t code = __ldcs(reinterpret_cast<const uint32_t *>(prm.codes.p[n]) + i);
+            const float sv = scale_value(prm.scales.p[n][sc]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t c = code >> (4 * e), m = c & 7u;
+                const float mag = m < 2u ? 0.5f * (float)m : __uint_as_float((m + 252u) << 22);
+                acc[e] = fmaf(with_sign(mag, __uint_as_float(c << 28)), sv, acc[e]);
+            }
+        }
+        const int64_t col = piece * 8;
+        float *dst;
+        if (LAYOUT) {
+            int lo = 0, hi = prm.n_layers - 1;   // the layer of this slice: the last one that starts at or before it
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (prm.layer_soff[mid] <= row) lo = mid; else hi = mid - 1;
+            }
+            dst = prm.out + prm.layer_off[lo] + (row - prm.layer_soff[lo]) * prm.d + col;
+        } else {
+            dst = prm.out + row * prm.ld + col;
+        }
+        if (prm.vec && col + 8 <= prm.cols) {
+            reinterpret_cast<float4 *>(dst)[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+            reinterpret_cast<float4 *>(dst)[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (col + e < prm.cols) dst[e] = acc[e];
+        }
+    }
+}
+
+template <typename T, bool SR, bool ROWS, bool COLS>
+cudaError_t launch_quantize_as(cudaStream_t st, const QuantParams &prm)
+{
+    const unsigned grid = (unsigned)(prm.ct * tiles_of(prm.rows, 128));
+    const size_t smem = COLS ? 128 * 128 * sizeof(T) + 128 : 0;
+    auto kernel = mx4_quantize_kernel<T, SR, ROWS, COLS>;
+    if (smem > 48 * 1024) {
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    kernel<<<grid, 256, smem, st>>>(prm);
+    return cudaGetLastError();
+}
+template <typename T, bool SR>
+cudaError_t launch_quantize_forms(cudaStream_t st, const QuantParams &prm)
+{
+    if (prm.codes && prm.codes_t) return launch_quantize_as<T, SR, true, true>(st, prm);
+    if (prm.codes) return launch_quantize_as<T, SR, true, false>(st, prm);
+    return launch_quantize_as<T, SR, false, true>(st, prm);
+}
+template <typename T>
+cudaError_t launch_quantize_rounding(cudaStream_t st, const QuantParams &prm, bool stochastic)
+{
+    return stochastic ? launch_quantize_forms<T, true>(st, prm) : launch_quantize_forms<T, false>(st, prm);
+}
+
+}  // namespace
+
+cudaError_t launch_mx4_quantize(cudaStream_t st, const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld,
+                                bool stochastic, uint64_t seed, uint32_t node, uint8_t *codes, uint8_t *scales,
+                                uint8_t *codes_t, uint8_t *scales_t)
+{
+    QuantParams prm;
+    prm.ct = (int)tiles_of(cols, 128);
+    prm.x = x; prm.rows = rows; prm.cols = cols; prm.ld = ld;
+    prm.seed_w = seed_word(seed, node);
+    prm.codes = codes; prm.scales = scales; prm.codes_t = codes_t; prm.scales_t = scales_t;
+    const size_t size = dtype == GVQ_F32 ? 4 : 2;
+    prm.vec = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && (rows == 1 || (ld * size) % 16 == 0);
+    if (dtype == GVQ_F32) return launch_quantize_rounding<float>(st, prm, stochastic);
+    if (dtype == GVQ_BF16) return launch_quantize_rounding<__nv_bfloat16>(st, prm, stochastic);
+    return launch_quantize_rounding<__half>(st, prm, stochastic);
+}
+
+cudaError_t launch_mx4_quantize_aggregate(cudaStream_t st, int d, int64_t S, const TileTable &tiles, const LayerTables &lt,
+                                          const NodePtrs<const float> &g, int n_nodes, uint32_t node0, bool stochastic,
+                                          uint64_t seed, float *out, const NodePtrs<uint8_t> *codes,
+                                          const NodePtrs<uint8_t> *scales)
+{
+    if (tiles.n_tiles == 0) return cudaSuccess;
+    AggParams prm;
+    prm.d = d; prm.n_nodes = n_nodes;
+    for (int n = 0; n < GVQ_MAX_NODES; ++n) {
+        prm.seed_w[n] = seed_word(seed, node0 + (uint32_t)n);
+        prm.codes.p[n] = codes ? codes->p[n] : nullptr;
+        prm.scales.p[n] = scales ? scales->p[n] : nullptr;
+    }
+    prm.tile_layer = tiles.layer; prm.tile_row0 = tiles.row0; prm.layer_S = lt.S;
+    prm.layer_off = lt.off; prm.layer_soff = lt.soff;
+    prm.g = g; prm.out = out;
+    if (codes) {
+        mx4_clear_scale_padding_kernel<<<dim3(32, n_nodes), 256, 0, st>>>(prm.scales, S, (d + kBlock - 1) / kBlock);
+        cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+    }
+    auto launch = [&](auto kernel) {
+        kernel<<<tiles.n_tiles, 256, 0, st>>>(prm);
+        return cudaGetLastError();
+    };
+    if (stochastic) return codes ? launch(mx4_quantize_aggregate_kernel<true, true>) : launch(mx4_quantize_aggregate_kernel<true, false>);
+    return codes ? launch(mx4_quantize_aggregate_kernel<false, true>) : launch(mx4_quantize_aggregate_kernel<false, false>);
+}
+
+cudaError_t launch_mx4_dequantize(cudaStream_t st, int num_sms, const NodePtrs<const uint8_t> &codes,
+                                  const NodePtrs<const uint8_t> &scales, int n_nodes, int64_t rows, int64_t cols, float *out,
+                                  int64_t ld, const LayerTables *lt, int n_layers)
+{
+    if (rows == 0 || cols == 0) return cudaSuccess;
+    DeqParams prm;
+    prm.n_nodes = n_nodes; prm.rows = rows; prm.cols = cols; prm.ld = ld; prm.d = (int)cols;
+    prm.n_layers = n_layers;
+    prm.layer_off = lt ? lt->off : nullptr; prm.layer_soff = lt ? lt->soff : nullptr; prm.layer_S = lt ? lt->S : nullptr;
+    prm.codes = codes; prm.scales = scales; prm.out = out;
+    prm.vec = (reinterpret_cast<uintptr_t>(out) & 15u) == 0 && (lt ? cols % 4 == 0 : (rows == 1 || ld % 4 == 0));
+    const int64_t items = rows * blocks(cols) * 4;
+    const int grid = (int)min((int64_t)num_sms * 16, (items + 255) / 256);
+    if (lt) mx4_dequantize_kernel<true><<<grid, 256, 0, st>>>(prm);
+    else mx4_dequantize_kernel<false><<<grid, 256, 0, st>>>(prm);
+    return cudaGetLastError();
+}
+
+}  // namespace gvq

@@ -94,6 +94,15 @@ def lib() -> ctypes.CDLL:
         L.gvq_dequantize_raw4_aggregate.argtypes = [vp, vp, vp, vp, i32, i32, vp]
         L.gvq_flatten_layer.argtypes = [vp, vp, vp, i32, i32, i32]
         L.gvq_unflatten_layer.argtypes = [vp, vp, vp, i32, i32, i32]
+        L.gvq_mx4_codes_bytes.restype = i64
+        L.gvq_mx4_codes_bytes.argtypes = [i64, i64]
+        L.gvq_mx4_scales_bytes.restype = i64
+        L.gvq_mx4_scales_bytes.argtypes = [i64, i64]
+        L.gvq_mx4_quantize.argtypes = [vp, vp, i32, i64, i64, i64, i32, u64, u32, vp, vp, vp, vp]
+        L.gvq_mx4_dequantize.argtypes = [vp, vp, vp, i64, i64, vp, i64]
+        L.gvq_mx4_matmul.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, vp, i32, i64]
+        L.gvq_mx4_quantize_aggregate.argtypes = [vp, vp, i32, u32, i32, u64, vp, vp, vp]
+        L.gvq_mx4_dequantize_aggregate.argtypes = [vp, vp, vp, vp, i32, vp]
         L.gvq_exchange_floats.argtypes = [LP]
         L.gvq_exchange_floats.restype = i64
         L.gvq_segment_layout.argtypes = [LP, i32, i32, ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32),
@@ -248,6 +257,41 @@ class Schedule:
         return {"iteration": a.value, "refreshes": b.value, "early_stops": c.value}
 
 
+DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _dtype(t: torch.Tensor) -> int:
+    if t.dtype not in DTYPE:
+        raise TypeError(f"gvq takes float32, bfloat16 and float16 here, not {t.dtype}")
+    return DTYPE[t.dtype]
+
+
+def _rows(t: torch.Tensor, what: str):
+    """(rows, cols, leading dimension) of a 2-D tensor whose rows are contiguous."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{what}: a 2-D CUDA tensor is wanted")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: the entries of a row have to be contiguous")
+    return t.shape[0], t.shape[1], t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+class Mx4:
+    """A matrix [rows][cols] in microscaled 4-bit floating point: device bytes `codes` and `scales` (see gvq.h)."""
+
+    def __init__(self, rows: int, cols: int, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                 device=None):
+        self.rows, self.cols = int(rows), int(cols)
+        nc = lib().gvq_mx4_codes_bytes(self.rows, self.cols)
+        ns = lib().gvq_mx4_scales_bytes(self.rows, self.cols)
+        if nc < 0:
+            raise ValueError(f"no 4-bit matrix of {rows} x {cols}")
+        self.codes = torch.empty(nc, dtype=torch.uint8, device=device or "cuda") if codes is None else codes
+        self.scales = torch.empty(ns, dtype=torch.uint8, device=device or "cuda") if scales is None else scales
+        for t, n in ((self.codes, nc), (self.scales, ns)):
+            if t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous() or t.numel() < n:
+                raise ValueError(f"a 4-bit matrix of {rows} x {cols} has {nc} bytes of codes and {ns} of scales, contiguous")
+
+
 class Context:
     """gvq_ctx for one layout on one CUDA device."""
 
@@ -358,6 +402,80 @@ class Context:
         gp = _ptr_array(g_nodes_for_tails) if g_nodes_for_tails is not None else None
         _check(lib().gvq_dequantize_raw4_aggregate(self._h, _ptr_array(q4_nodes), _ptr_array(norms_nodes), gp, levels,
                                                    len(q4_nodes), g_sum.data_ptr()), "gvq_dequantize_raw4_aggregate")
+
+    # ---- microscaled 4-bit floating point ---------------------------------------------------
+    def _mx4(self, x, by_rows, by_cols, stochastic, seed, node, out=None, out_t=None):
+        rows, cols, ld = _rows(x, "mx4_quantize")
+        if by_rows and out is None:
+            out = Mx4(rows, cols, device=x.device)
+        if by_cols and out_t is None:
+            out_t = Mx4(cols, rows, device=x.device)
+        if (out is not None and (out.rows, out.cols) != (rows, cols)) or \
+                (out_t is not None and (out_t.rows, out_t.cols) != (cols, rows)):
+            raise ValueError("mx4_quantize: the output is of another size")
+        self._sync_stream()
+        _check(lib().gvq_mx4_quantize(self._h, x.data_ptr(), _dtype(x), rows, cols, ld, 1 if stochastic else 0, seed, node,
+                                      out.codes.data_ptr() if out else None, out.scales.data_ptr() if out else None,
+                                      out_t.codes.data_ptr() if out_t else None, out_t.scales.data_ptr() if out_t else None),
+               "gvq_mx4_quantize")
+        return out, out_t
+
+    def mx4_quantize(self, x, stochastic=False, seed=0, node=0, out: Optional[Mx4] = None) -> Mx4:
+        """gvq_mx4_quantize along the rows of x [rows, cols]."""
+        return self._mx4(x, True, False, stochastic, seed, node, out=out)[0]
+
+    def mx4_quantize_transposed(self, x, stochastic=False, seed=0, node=0, out: Optional[Mx4] = None) -> Mx4:
+        """gvq_mx4_quantize along the columns of x: the quantized [cols, rows] matrix."""
+        return self._mx4(x, False, True, stochastic, seed, node, out_t=out)[1]
+
+    def mx4_quantize_both(self, x, stochastic=False, seed=0, node=0, out: Optional[Mx4] = None,
+                          out_t: Optional[Mx4] = None):
+        """gvq_mx4_quantize along the rows and along the columns, reading x once: (by rows, by columns)."""
+        return self._mx4(x, True, True, stochastic, seed, node, out, out_t)
+
+    def mx4_dequantize(self, q: Mx4, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """gvq_mx4_dequantize: what q stands for, float32 [rows, cols]."""
+        if out is None:
+            out = torch.empty((q.rows, q.cols), device=q.codes.device)
+        rows, cols, ld = _rows(out, "mx4_dequantize")
+        if (rows, cols) != (q.rows, q.cols) or out.dtype != torch.float32:
+            raise ValueError("mx4_dequantize: a float32 output of the matrix's size is wanted")
+        self._sync_stream()
+        _check(lib().gvq_mx4_dequantize(self._h, q.codes.data_ptr(), q.scales.data_ptr(), rows, cols, out.data_ptr(), ld),
+               "gvq_mx4_dequantize")
+        return out
+
+    def mx4_matmul(self, a: Mx4, b: Mx4, out: torch.Tensor) -> torch.Tensor:
+        """gvq_mx4_matmul: out [a.rows, b.rows] = a b^T; out is float32, bfloat16 or float16."""
+        rows, cols, ld = _rows(out, "mx4_matmul")
+        if a.cols != b.cols or (rows, cols) != (a.rows, b.rows):
+            raise ValueError(f"mx4_matmul: [{a.rows}, {a.cols}] x [{b.rows}, {b.cols}]^T does not give [{rows}, {cols}]")
+        self._sync_stream()
+        _check(lib().gvq_mx4_matmul(self._h, a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(),
+                                    b.scales.data_ptr(), rows, cols, a.cols, out.data_ptr(), _dtype(out), ld),
+               "gvq_mx4_matmul")
+        return out
+
+    def mx4_slices(self) -> Mx4:
+        """Room for one node's quantized slices, a matrix [S][d]."""
+        return Mx4(self.S, self.d, device=f"cuda:{self.device}")
+
+    def mx4_quantize_aggregate(self, g_nodes, g_sum, stochastic=True, seed=0, node0=0,
+                               out: Optional[Sequence[Mx4]] = None):
+        """gvq_mx4_quantize_aggregate; out: one mx4_slices() per node that receives what it would send."""
+        self._sync_stream()
+        cp = _ptr_array([q.codes for q in out]) if out is not None else None
+        sp = _ptr_array([q.scales for q in out]) if out is not None else None
+        _check(lib().gvq_mx4_quantize_aggregate(self._h, _ptr_array(g_nodes), len(g_nodes), node0, 1 if stochastic else 0,
+                                                seed, g_sum.data_ptr() if g_sum is not None else None, cp, sp),
+               "gvq_mx4_quantize_aggregate")
+
+    def mx4_dequantize_aggregate(self, q_nodes: Sequence[Mx4], g_nodes_for_tails, g_sum):
+        self._sync_stream()
+        gp = _ptr_array(g_nodes_for_tails) if g_nodes_for_tails is not None else None
+        _check(lib().gvq_mx4_dequantize_aggregate(self._h, _ptr_array([q.codes for q in q_nodes]),
+                                                  _ptr_array([q.scales for q in q_nodes]), gp, len(q_nodes), g_sum.data_ptr()),
+               "gvq_mx4_dequantize_aggregate")
 
     def flatten_layer(self, framework, flat, F, D, X):
         self._sync_stream()
