@@ -465,7 +465,7 @@ gvq_status gvq_create(gvq_ctx **out, const gvq_layout *layout, int device, void 
         return GVQ_ERR_CUDA;
     }
     const int tt_n_tiles = (int)tt.layer.size();
-    if (project_sum_tc_supported(ctx->d, ctx->k) || cov_tc_supported(ctx->d)) {
+    {
         cudaDriverEntryPointQueryResult qres;
         void *fn = nullptr;
         if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) == cudaSuccess &&
