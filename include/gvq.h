@@ -527,6 +527,35 @@ gvq_status gvq_mx4_dequantize_aggregate(gvq_ctx *ctx, const uint8_t *const *code
                                         const uint8_t *const *scales_nodes, const float *const *g_nodes_for_tails, int N,
                                         float *g_sum);
 
+/* ---- the orthogonalised update ------------------------------------------------------------------------
+   What an aggregated gradient is for.  A plan holds the layers of the context's layout that are matrices (row-major
+   [rows][cols] where the layer lies in a flat buffer) and updates all of them in one call:
+     momentum = beta * momentum + g;    u = g + beta * momentum (nesterov != 0) or momentum
+     X = u / (|u|_F + 1e-7);            five times, on the shorter side:  A = X X^T,  X = a X + (b A + c A^2) X
+     w = (1 - lr * weight_decay) w - lr * scale * X          (a, b, c) = (3.4445, -4.7750, 2.0315)
+   (the update of the Muon optimiser: every singular value of u is moved to about 1; scale = sqrt(max(1, rows / cols))
+   unless given).  The products run on the tensor cores with half-precision operands and fp32 accumulation: X is within
+   about 2e-3 (relative, rms) of its value in exact arithmetic.  Momentum, norms and the weights' sum are fp32, each
+   rounding to w's type once.  A matrix that is zero moves nothing (X = 0); one that holds a NaN or an infinity gives NaN
+   or zero for its own layer, as the formula does, and touches no other.
+   rows, cols: HOST arrays [n_layers], rows[l] * cols[l] = layer_len[l], or both 0: the layer is left alone; the shorter
+   side is at most 32768.  scales_opt: NULL or HOST [n_layers].  workspace: device, 256-byte aligned,
+   gvq_ortho_workspace_bytes() bytes (-1 on bad sizes), owned by the caller and kept while the plan lives; its contents
+   carry nothing from one call to the next.  The plan keeps tables in device memory of its own (one allocation at create).
+   It must not outlive its context, whose stream its calls use; they allocate nothing and can be captured. */
+typedef struct gvq_ortho gvq_ortho;
+int64_t gvq_ortho_workspace_bytes(const gvq_layout *layout, const int32_t *rows, const int32_t *cols);
+gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, const int32_t *cols,
+                            const float *scales_opt, void *workspace, size_t workspace_bytes);
+gvq_status gvq_ortho_destroy(gvq_ortho *plan);
+/* One update.  g: device fp32 [M] (for instance gvq_decompress' g_hat); momentum: device fp32 [M], updated; w: device [M]
+   entries of type dtype, updated.  Entries outside the plan's matrices are neither read nor written.  The three buffers
+   are distinct, 0 <= beta < 1. */
+gvq_status gvq_ortho_step(gvq_ortho *plan, const float *g, float *momentum, float beta, int nesterov, void *w, int dtype,
+                          float lr, float weight_decay);
+/* The orthogonalisation alone: out = X of u = g, [M] entries of type dtype, written inside the plan's matrices only. */
+gvq_status gvq_orthogonalize(gvq_ortho *plan, const float *g, void *out, int dtype);
+
 /* The whole path for callers whose gradients live in HOST memory (Eq. 3 + Eq. 4 + Eq. 5):
    copies the N gradients to the device scratch, runs gvq_compress_aggregate and
    gvq_decompress there, copies g_hat back and waits for it.

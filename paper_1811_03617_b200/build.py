@@ -13,7 +13,7 @@ CSRC = PKG / "csrc"
 LIB = PKG / "libgvq.so"
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-shared"]
+              "-Xcompiler", "-fPIC", "-shared", "--threads", "8"]
 
 
 def sources():

@@ -14,6 +14,7 @@
 // Accumulators alternate between two column ranges.  Every mbarrier wait is bounded.
 #include "gvq_internal.h"
 #include "mx4.cuh"
+#include "row32.cuh"
 #include "sm100_ptx.cuh"
 
 namespace gvq {
@@ -78,33 +79,6 @@ __host__ __device__ constexpr uint32_t idesc_mxf4(int n, int half)
 {
     return ((uint32_t)(2 * half) << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) |
            ((uint32_t)(128 >> 4) << 24) | ((uint32_t)(2 * half) << 29);
-}
-
-template <typename T> __device__ __forceinline__ T from_f(float x);
-template <> __device__ __forceinline__ float from_f(float x) { return x; }
-template <> __device__ __forceinline__ __nv_bfloat16 from_f(float x) { return __float2bfloat16_rn(x); }
-template <> __device__ __forceinline__ __half from_f(float x) { return __float2half_rn(x); }
-
-// 32 consecutive columns of one row, as many as lie inside
-template <typename T>
-__device__ __forceinline__ void store_row32(T *dst, const float (&v)[32], int n)
-{
-    constexpr int PER = 16 / (int)sizeof(T);
-    T e[32];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) e[i] = from_f<T>(v[i]);
-    if (n >= 32 && (reinterpret_cast<uintptr_t>(dst) & 15u) == 0) {
-#pragma unroll
-        for (int i = 0; i < 32 / PER; ++i) {
-            uint4 q;
-            memcpy(&q, e + i * PER, 16);
-            reinterpret_cast<uint4 *>(dst)[i] = q;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (i < n) dst[i] = e[i];
-    }
 }
 
 template <typename T, int BN>

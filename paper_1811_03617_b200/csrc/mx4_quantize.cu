@@ -5,16 +5,12 @@
 //  mx4_dequantize_kernel          codes back to values, summed over the nodes
 #include "gvq_internal.h"
 #include "mx4.cuh"
+#include "row32.cuh"
 
 namespace gvq {
 namespace {
 
 using namespace mx4;
-
-template <typename T> __device__ __forceinline__ float to_f(T x);
-template <> __device__ __forceinline__ float to_f(float x) { return x; }
-template <> __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <> __device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
 
 // Eight consecutive entries as they lie in memory.
 template <typename T> struct Raw8 { uint4 q[sizeof(T) / 2]; };

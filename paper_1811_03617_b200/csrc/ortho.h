@@ -1,0 +1,69 @@
+// The plan of an orthogonalised update (gvq.h, gvq_ortho_*): what the host builds once and the kernels read.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "gvq_internal.h"
+
+namespace gvq {
+namespace ortho {
+
+constexpr int kSteps = 5;
+// The quintic step  X <- a X + (b A + c A^2) X,  A = X X^T: its coefficients push every singular value of (0, 1] to about 1 in
+// five steps (Jordan's choice for the Muon optimiser: slope 3.44 at zero, values end in [0.7, 1.2]).
+constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
+constexpr float kEps = 1e-7f;
+// Steps whose X is kept as a sum of two halves (ortho.cu's header has the reason).
+constexpr int kExactSteps = 3;
+// Scale of A and B in half precision: entries of both are of order 1 at most (|b| 1.2 + |c| 1.44 = 8.7), those off the
+// diagonal far smaller.
+constexpr float kGramScale = 256.0f;
+
+constexpr int kTileM = 128, kTileN = 256;
+constexpr int kChunk = 8192;     // entries of a chunk of the element-wise passes
+
+// One matrix [rows][cols] of the flat gradient.  r <= c its shorter and longer side.
+struct Matrix {
+    int32_t rows, cols, r, c, tall, ldx, ldr;
+    int32_t chunk0, n_chunks;        // its chunks in the element-wise passes
+    int64_t off;                     // in the flat buffers
+    __half *x[2], *lo, *gram, *poly; // X (two buffers, in turn), X's low halves, A, B; rows ldx or ldr entries apart
+    float sx;                        // scale of X in half precision
+    float scale;                     // of the update
+};
+struct Tile { int32_t matrix, tm, tn; };
+struct Chunk { int32_t matrix, index; };
+
+enum Phase { kGram = 0, kPoly = 1, kApply = 2 };
+enum Map { kX0 = 0, kX1 = 1, kGramMap = 2, kPolyMap = 3, kMaps = 4 };
+
+struct Device {
+    const Matrix *mats;
+    const CUtensorMap *maps;         // [matrices][kMaps]
+    const Tile *sym_tiles, *apply_tiles;
+    int n_sym, n_apply;
+    const Chunk *chunks;
+    int n_chunks;
+    float *partial;                  // [n_chunks] sums of squares
+};
+
+// momentum = beta * momentum + g (momentum may be null), u = g + beta * momentum (nesterov) or momentum, sums of squares;
+// then X = u / (|u| + eps) in half precision.
+struct ElementArgs {
+    const float *g;
+    float *momentum;
+    float beta;
+    int nesterov;
+};
+// What the last product's result is for: w <- decay w - step * scale * O, or out = O.
+struct OutputArgs {
+    void *ptr;
+    int dtype, update;
+    float decay, step;
+};
+
+cudaError_t launch_start(cudaStream_t st, const Device &dev, const ElementArgs &a);
+cudaError_t launch_product(cudaStream_t st, int num_sms, const Device &dev, Phase phase, int step, const OutputArgs *out,
+                           int32_t *error_word, int wait_kcycles, int test_drop);
+
+}  // namespace ortho
+}  // namespace gvq

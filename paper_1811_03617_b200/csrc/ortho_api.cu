@@ -1,0 +1,207 @@
+// C entry points of the orthogonalised update: the plan (sizes, tables, tensor maps) and its two calls.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+
+#include "api_util.h"
+#include "ortho.h"
+
+using namespace gvq;
+using namespace gvq::ortho;
+
+struct gvq_ortho {
+    gvq_ctx *ctx = nullptr;
+    Device dev{};
+    void *tables = nullptr;      // one device allocation: matrices, tensor maps, tiles, chunks, partial sums
+};
+
+namespace {
+
+constexpr size_t kAlign = 256;
+size_t up(size_t n) { return (n + kAlign - 1) & ~(kAlign - 1); }
+int up8(int n) { return (n + 7) & ~7; }
+
+struct Sizes {
+    std::vector<Matrix> mats;
+    size_t bytes = 0;            // of the workspace
+};
+
+// The matrices of a layout and the workspace they take, laid out from `base` (null: sizes only).
+gvq_status lay_out(int n_layers, const int64_t *off, const int64_t *len, const int32_t *rows, const int32_t *cols,
+                   const float *scales, unsigned char *base, Sizes &out)
+{
+    for (int l = 0; l < n_layers; ++l) {
+        if (rows[l] == 0 && cols[l] == 0) continue;               // not a matrix: left alone
+        if (rows[l] < 1 || cols[l] < 1 || (int64_t)rows[l] * cols[l] != len[l]) return GVQ_ERR_SHAPE;
+        if (rows[l] > INT32_MAX - 512 || cols[l] > INT32_MAX - 512) return GVQ_ERR_SHAPE;
+        Matrix m{};
+        m.rows = rows[l]; m.cols = cols[l];
+        m.r = std::min(m.rows, m.cols); m.c = std::max(m.rows, m.cols);
+        if (m.r > 32768) return GVQ_ERR_SHAPE;                    // r x r products beyond any layer
+        m.tall = m.rows > m.cols;
+        m.ldx = up8(m.cols); m.ldr = up8(m.r);
+        m.off = off[l];
+        // entries of X have an rms of 1 / sqrt(r c) at first and 1 / sqrt(c) at last: about 1 / sqrt(r) to 1 when scaled
+        m.sx = std::exp2(std::round(0.5f * std::log2((float)m.c)));
+        m.scale = scales ? scales[l] : std::sqrt(std::max(1.0f, (float)m.rows / (float)m.cols));
+        auto take = [&](size_t entries) {
+            __half *p = reinterpret_cast<__half *>(base ? base + out.bytes : nullptr);
+            out.bytes += up(entries * sizeof(__half));
+            return p;
+        };
+        const size_t nx = (size_t)m.rows * m.ldx, nr = (size_t)m.r * m.ldr;
+        m.x[0] = take(nx); m.x[1] = take(nx); m.lo = take(nx); m.gram = take(nr); m.poly = take(nr);
+        out.mats.push_back(m);
+    }
+    return GVQ_OK;
+}
+
+bool encode(EncodeTiledFn enc, CUtensorMap *map, void *p, int rows, int cols, int ld)
+{
+    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)ld * sizeof(__half)};
+    cuuint32_t box[2] = {64, 64};
+    cuuint32_t estr[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, p, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The five steps from X to the result.
+gvq_status products(gvq_ortho *p, const OutputArgs &out)
+{
+    gvq_ctx *ctx = p->ctx;
+    for (int s = 0; s < kSteps; ++s)
+        for (Phase ph : {kGram, kPoly, kApply})
+            GVQ_CUDA(ctx, launch_product(ctx->stream, ctx->num_sms, p->dev, ph, s, &out, ctx->error_word, ctx->wait_kcycles,
+                                         ctx->drop_last_load));
+    return GVQ_OK;
+}
+
+bool finite(float x) { return std::isfinite(x); }
+
+}  // namespace
+
+extern "C" {
+
+int64_t gvq_ortho_workspace_bytes(const gvq_layout *layout, const int32_t *rows, const int32_t *cols)
+{
+    if (!rows || !cols || gvq_layout_check(layout) != GVQ_OK) return -1;
+    Sizes s;
+    if (lay_out(layout->n_layers, layout->layer_off, layout->layer_len, rows, cols, nullptr, nullptr, s) != GVQ_OK) return -1;
+    return (int64_t)s.bytes;
+}
+
+gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, const int32_t *cols, const float *scales_opt,
+                            void *workspace, size_t workspace_bytes)
+{
+    if (!out) return GVQ_ERR_NULL;
+    *out = nullptr;
+    if (!ctx || !rows || !cols) return GVQ_ERR_NULL;
+    if (!ctx->encode_fn) return GVQ_ERR_UNSUPPORTED;
+    try {
+        Sizes sz;
+        gvq_status st = lay_out(ctx->n_layers, ctx->layer_off.data(), ctx->layer_len.data(), rows, cols, scales_opt,
+                                static_cast<unsigned char *>(workspace), sz);
+        if (st != GVQ_OK) return st;
+        if (scales_opt)
+            for (int l = 0; l < ctx->n_layers; ++l)
+                if (!finite(scales_opt[l])) return GVQ_ERR_SHAPE;
+        if (sz.bytes > 0 && (!workspace || workspace_bytes < sz.bytes)) return GVQ_ERR_WORKSPACE;
+        if ((reinterpret_cast<uintptr_t>(workspace) & (kAlign - 1)) != 0) return GVQ_ERR_ALIGN;
+
+        const int n = (int)sz.mats.size();
+        std::vector<CUtensorMap> maps((size_t)n * kMaps);
+        std::vector<Tile> sym, apply;
+        std::vector<Chunk> chunks;
+        for (int i = 0; i < n; ++i) {
+            Matrix &m = sz.mats[i];
+            CUtensorMap *mp = &maps[(size_t)i * kMaps];
+            EncodeTiledFn enc = (EncodeTiledFn)ctx->encode_fn;
+            if (!encode(enc, mp + kX0, m.x[0], m.rows, m.cols, m.ldx) || !encode(enc, mp + kX1, m.x[1], m.rows, m.cols, m.ldx) ||
+                !encode(enc, mp + kGramMap, m.gram, m.r, m.r, m.ldr) || !encode(enc, mp + kPolyMap, m.poly, m.r, m.r, m.ldr))
+                return GVQ_ERR_CUDA;
+            // tiles of a symmetric product: those whose 256 columns reach the diagonal block of their rows
+            for (int tm = 0; tm * kTileM < m.r; ++tm)
+                for (int tn = tm / 2; tn * kTileN < m.r; ++tn) sym.push_back({i, tm, tn});
+            for (int tm = 0; (int64_t)tm * kTileM < m.rows; ++tm)
+                for (int tn = 0; (int64_t)tn * kTileN < m.cols; ++tn) apply.push_back({i, tm, tn});
+            m.chunk0 = (int)chunks.size();
+            m.n_chunks = (int)(((int64_t)m.rows * m.cols + kChunk - 1) / kChunk);
+            for (int k = 0; k < m.n_chunks; ++k) chunks.push_back({i, k});
+        }
+        // longest contraction first: the CTAs take the tiles in turn, and the short ones level the end
+        std::stable_sort(sym.begin(), sym.end(), [&](const Tile &a, const Tile &b) { return sz.mats[a.matrix].c > sz.mats[b.matrix].c; });
+        std::stable_sort(apply.begin(), apply.end(), [&](const Tile &a, const Tile &b) { return sz.mats[a.matrix].r > sz.mats[b.matrix].r; });
+
+        gvq_ortho *p = new gvq_ortho();
+        p->ctx = ctx;
+        const size_t b_m = up(sizeof(Matrix) * n), b_t = up(sizeof(CUtensorMap) * maps.size()), b_s = up(sizeof(Tile) * sym.size()),
+                     b_a = up(sizeof(Tile) * apply.size()), b_c = up(sizeof(Chunk) * chunks.size()), b_p = up(sizeof(float) * chunks.size());
+        std::vector<unsigned char> image(b_m + b_t + b_s + b_a + b_c);
+        auto put = [&](size_t at, const void *src, size_t bytes) { if (bytes) std::memcpy(image.data() + at, src, bytes); };
+        put(0, sz.mats.data(), sizeof(Matrix) * n);
+        put(b_m, maps.data(), sizeof(CUtensorMap) * maps.size());
+        put(b_m + b_t, sym.data(), sizeof(Tile) * sym.size());
+        put(b_m + b_t + b_s, apply.data(), sizeof(Tile) * apply.size());
+        put(b_m + b_t + b_s + b_a, chunks.data(), sizeof(Chunk) * chunks.size());
+        DeviceGuard guard(ctx->device);
+        cudaError_t e = cudaMalloc(&p->tables, image.size() + b_p + kAlign);
+        if (e == cudaSuccess) e = cudaMemcpy(p->tables, image.data(), image.size(), cudaMemcpyHostToDevice);
+        if (e != cudaSuccess) {
+            if (p->tables) cudaFree(p->tables);
+            delete p;
+            return cuda_fail(ctx, e);
+        }
+        unsigned char *t = static_cast<unsigned char *>(p->tables);
+        Device &d = p->dev;
+        d.mats = reinterpret_cast<Matrix *>(t);
+        d.maps = reinterpret_cast<CUtensorMap *>(t + b_m);
+        d.sym_tiles = reinterpret_cast<Tile *>(t + b_m + b_t);
+        d.apply_tiles = reinterpret_cast<Tile *>(t + b_m + b_t + b_s);
+        d.chunks = reinterpret_cast<Chunk *>(t + b_m + b_t + b_s + b_a);
+        d.partial = reinterpret_cast<float *>(t + image.size());
+        d.n_sym = (int)sym.size(); d.n_apply = (int)apply.size(); d.n_chunks = (int)chunks.size();
+        *out = p;
+        return GVQ_OK;
+    } catch (const std::bad_alloc &) {
+        return GVQ_ERR_CUDA;
+    }
+}
+
+gvq_status gvq_ortho_destroy(gvq_ortho *p)
+{
+    if (!p) return GVQ_OK;
+    DeviceGuard guard(p->ctx->device);
+    if (p->tables) cudaFree(p->tables);
+    delete p;
+    return GVQ_OK;
+}
+
+gvq_status gvq_orthogonalize(gvq_ortho *p, const float *g, void *out, int dtype)
+{
+    if (!p || !g || !out) return GVQ_ERR_NULL;
+    if (dtype != GVQ_F32 && dtype != GVQ_BF16 && dtype != GVQ_F16) return GVQ_ERR_SHAPE;
+    if (static_cast<const void *>(g) == out) return GVQ_ERR_SHAPE;
+    if (!aligned16(g) || !aligned16(out)) return GVQ_ERR_ALIGN;
+    if (p->dev.n_chunks == 0) return GVQ_OK;
+    DeviceGuard guard(p->ctx->device);
+    GVQ_CUDA(p->ctx, launch_start(p->ctx->stream, p->dev, {g, nullptr, 0.0f, 0}));
+    return products(p, {out, dtype, 0, 0.0f, 0.0f});
+}
+
+gvq_status gvq_ortho_step(gvq_ortho *p, const float *g, float *momentum, float beta, int nesterov, void *w, int dtype, float lr,
+                          float weight_decay)
+{
+    if (!p || !g || !momentum || !w) return GVQ_ERR_NULL;
+    if (dtype != GVQ_F32 && dtype != GVQ_BF16 && dtype != GVQ_F16) return GVQ_ERR_SHAPE;
+    if (!(beta >= 0.0f && beta < 1.0f) || !finite(lr) || !finite(weight_decay)) return GVQ_ERR_SHAPE;
+    if (g == momentum || static_cast<const void *>(g) == w || static_cast<void *>(momentum) == w) return GVQ_ERR_SHAPE;
+    if (!aligned16(g) || !aligned16(momentum) || !aligned16(w)) return GVQ_ERR_ALIGN;
+    if (p->dev.n_chunks == 0) return GVQ_OK;
+    DeviceGuard guard(p->ctx->device);
+    GVQ_CUDA(p->ctx, launch_start(p->ctx->stream, p->dev, {g, momentum, beta, nesterov}));
+    return products(p, {w, dtype, 1, 1.0f - lr * weight_decay, lr});
+}
+
+}  // extern "C"

@@ -172,6 +172,25 @@ __host__ __device__ constexpr uint32_t make_idesc(int n)
     return (1u << 4) | (2u << 7) | (2u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
 
+// kind::f16 with both operands in shared memory: F16 x F16 -> FP32, M = 128.  An operand is K-major (rows of the
+// contraction) or MN-major (`mn`: rows of 64 entries across it, one row per step of the contraction).
+__device__ __forceinline__ void tc_mma_f16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__host__ __device__ constexpr uint32_t make_idesc_f16(int n, bool a_mn, bool b_mn)
+{
+    return (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+// MN-major, 128-byte swizzle: 64 entries (128 bytes) a row, 8-row groups 1024 bytes apart along the contraction, the
+// next 64 entries `chunk` bytes on.
+__device__ __forceinline__ uint64_t make_mn_desc(uint32_t smem_addr, uint32_t chunk)
+{
+    return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | ((uint64_t)(chunk >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+           ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
 
 // Tiled TMA store of a (32 entries x 128 slices) box from shared memory; rows / columns outside the
 // tensor are dropped.  Completion is tracked by the bulk async-group of the issuing thread.

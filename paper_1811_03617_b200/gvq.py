@@ -103,6 +103,13 @@ def lib() -> ctypes.CDLL:
         L.gvq_mx4_matmul.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, vp, i32, i64]
         L.gvq_mx4_quantize_aggregate.argtypes = [vp, vp, i32, u32, i32, u64, vp, vp, vp]
         L.gvq_mx4_dequantize_aggregate.argtypes = [vp, vp, vp, vp, i32, vp]
+        i32p = ctypes.POINTER(ctypes.c_int32)
+        L.gvq_ortho_workspace_bytes.restype = i64
+        L.gvq_ortho_workspace_bytes.argtypes = [LP, i32p, i32p]
+        L.gvq_ortho_create.argtypes = [ctypes.POINTER(vp), vp, i32p, i32p, ctypes.POINTER(ctypes.c_float), vp, ctypes.c_size_t]
+        L.gvq_ortho_destroy.argtypes = [vp]
+        L.gvq_ortho_step.argtypes = [vp, vp, vp, ctypes.c_float, i32, vp, i32, ctypes.c_float, ctypes.c_float]
+        L.gvq_orthogonalize.argtypes = [vp, vp, vp, i32]
         L.gvq_exchange_floats.argtypes = [LP]
         L.gvq_exchange_floats.restype = i64
         L.gvq_segment_layout.argtypes = [LP, i32, i32, ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32),
@@ -614,3 +621,54 @@ class Context:
         else:
             _check(lib().gvq_allreduce_host(self._h, _ptr_array(g_nodes_host), len(g_nodes_host), Ut.data_ptr(),
                                             mu.data_ptr(), g_hat_host.data_ptr()), "gvq_allreduce_host")
+
+
+class OrthoPlan:
+    """gvq_ortho: the orthogonalised update of a context's layers that are matrices, rows[l] x cols[l] (0, 0: not one)."""
+
+    def __init__(self, ctx: Context, rows: Sequence[int], cols: Sequence[int], scales: Optional[Sequence[float]] = None):
+        self._h = ctypes.c_void_p()
+        n = ctx.n_layers
+        if len(rows) != n or len(cols) != n or (scales is not None and len(scales) != n):
+            raise ValueError(f"OrthoPlan: one entry per layer is wanted ({n})")
+        self.ctx = ctx                       # the plan uses its stream and must not outlive it
+        r, c = (ctypes.c_int32 * n)(*[int(v) for v in rows]), (ctypes.c_int32 * n)(*[int(v) for v in cols])
+        nbytes = lib().gvq_ortho_workspace_bytes(ctypes.byref(ctx.layout.c), r, c)
+        if nbytes < 0:
+            raise GvqError(2, "gvq_ortho_workspace_bytes")
+        self._ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=f"cuda:{ctx.device}")
+        s = None if scales is None else (ctypes.c_float * n)(*[float(v) for v in scales])
+        _check(lib().gvq_ortho_create(ctypes.byref(self._h), ctx._h, r, c, s, self._ws.data_ptr(), self._ws.numel()),
+               "gvq_ortho_create")
+
+    def close(self):
+        if self._h:
+            lib().gvq_ortho_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _flat(self, t: torch.Tensor, what: str):
+        if not t.is_cuda or not t.is_contiguous() or t.numel() < self.ctx.M:
+            raise ValueError(f"{what}: a contiguous CUDA tensor of {self.ctx.M} entries is wanted")
+        return t.data_ptr()
+
+    def _fp32(self, t: torch.Tensor, what: str):
+        if t.dtype != torch.float32:
+            raise TypeError(f"{what}: float32 is wanted, not {t.dtype}")
+        return self._flat(t, what)
+
+    def step(self, g, momentum, w, lr: float, weight_decay: float = 0.0, beta: float = 0.95, nesterov: bool = True):
+        """gvq_ortho_step on flat buffers: momentum and w are updated in place."""
+        self.ctx._sync_stream()
+        _check(lib().gvq_ortho_step(self._h, self._fp32(g, "g"), self._fp32(momentum, "momentum"), beta, 1 if nesterov else 0,
+                                    self._flat(w, "w"), _dtype(w), lr, weight_decay), "gvq_ortho_step")
+
+    def orthogonalize(self, g, out):
+        """gvq_orthogonalize: the plan's matrices of the flat buffer g, orthogonalised, into `out`."""
+        self.ctx._sync_stream()
+        _check(lib().gvq_orthogonalize(self._h, self._fp32(g, "g"), self._flat(out, "out"), _dtype(out)), "gvq_orthogonalize")
