@@ -15,7 +15,7 @@
 // adds noise to every direction alike, and the first steps amplify the small singular directions, noise included, by
 // 3.4 each (an rms error of 5e-3 in the result for a low-rank gradient over noise, against 1e-3 for a Gaussian one).
 // The a X term carries X forward, so X is kept as a sum of two halves (22 bits) for the first kExactSteps steps; the
-// products take the high half.  After that the steps contract the noise of the large directions, and carrying it exactly
+// products take the high half,  X' = (a I + b A + c A^2) X_hi + a X_lo.  After that the steps contract the noise of the large directions, and carrying it exactly
 // would not help.  Measured on the CPU, relative to 64 bits: 0.4e-3 to 1.4e-3 for sides of 256 and more.
 #include "ortho.h"
 #include "row32.cuh"
@@ -57,6 +57,8 @@ struct StartParams {
 __global__ void __launch_bounds__(256) momentum_kernel(const StartParams prm)
 {
     __shared__ float scratch[8];
+    ptx::launch_dependents();
+    ptx::grid_dependency_wait();
     const Chunk ch = prm.dev.chunks[blockIdx.x];
     const Matrix &mx = prm.dev.mats[ch.matrix];
     const int64_t total = (int64_t)mx.rows * mx.cols, begin = (int64_t)ch.index * kChunk;
@@ -107,6 +109,8 @@ __global__ void __launch_bounds__(256) momentum_kernel(const StartParams prm)
 __global__ void __launch_bounds__(256) normalise_kernel(const StartParams prm)
 {
     __shared__ double norm_s[8];
+    ptx::launch_dependents();
+    ptx::grid_dependency_wait();
     const Chunk ch = prm.dev.chunks[blockIdx.x];
     const Matrix mx = prm.dev.mats[ch.matrix];
     double s = 0.0;
@@ -168,14 +172,27 @@ __global__ void __launch_bounds__(256) normalise_kernel(const StartParams prm)
 }
 
 // ---- the products ------------------------------------------------------------------------------------
-// One persistent CTA per SM, tiles of 128 x 256, 64 steps of the contraction a stage.  Every operand comes in boxes of
-// 64 x 64 entries (8 KB, 128-byte swizzle, zero fill outside), the same tensor map for either major:
+// Persistent CTAs (or pairs of CTAs), 64 steps of the contraction a stage.  Every operand comes in boxes of 64 x 64 entries
+// (8 KB, 128-byte swizzle, zero fill outside), the same tensor map for either major:
 //   K-major   box = 64 steps x 64 rows     MN-major   box = 64 entries across x 64 steps
-// two boxes for A, four for B.
 //   warp 0      producer      warp 1  MMA      warps 2-9  epilogue (lane quarter warp % 4, half the columns each)
-constexpr int KS = 64, STAGES = 4, NTHREADS = 320, NEPI = 8;
-constexpr uint32_t BOX = 64 * 128, A_BYTES = 2 * BOX, B_BYTES = 4 * BOX, STAGE = A_BYTES + B_BYTES;
-constexpr size_t PRODUCT_SMEM = (size_t)STAGES * STAGE + 256 + 1024;
+// Two tilings:
+//   CG = 2  a pair of CTAs on two SMs, tile 256 x 256: each loads and holds its own 128 rows of A and half of B's rows, the
+//           even one issues MMAs that read both.  32 KB a stage and SM for 512 clocks of MMAs; a CTA alone on 128 x 256
+//           would load 48 KB, more than L2 delivers to all SMs at that rate.
+//   CG = 1  one CTA, tile 128 x 64, for plans without enough large tiles to fill the GPU: four times the CTAs at work, a
+//           quarter of the time a stage, and two CTAs fit an SM, so that a launch's first tiles overlap the last one's end.
+constexpr int KS = 64, NTHREADS = 320, NEPI = 8;
+constexpr uint32_t BOX = 64 * 128;
+
+template <int CG> struct Shape {
+    static constexpr int BN = CG == 2 ? kPairN : kSoloN;                     // columns of a tile
+    static constexpr int NB = CG == 2 ? 2 : BN / 64;                        // boxes of B a CTA loads
+    static constexpr uint32_t A_BYTES = 2 * BOX, STAGE = A_BYTES + NB * BOX;
+    static constexpr int STAGES = CG == 2 ? 5 : 3;
+    static constexpr uint32_t TMEM = 2 * BN;                                 // two accumulators
+    static constexpr size_t SMEM = (size_t)STAGES * STAGE + NEPI * kPieceBytes + 256 + 1024;
+};
 
 struct ProductParams {
     Device dev;
@@ -200,111 +217,143 @@ __device__ __forceinline__ Work work_of(const Matrix &m, int step)
     return m.tall ? Work{m.rows, m.cols, m.r, x, kPolyMap, false, false} : Work{m.rows, m.cols, m.r, kPolyMap, x, false, true};
 }
 
-// The last step's result of 32 columns of a row.
+// The last step's result, a staged piece of rows x cols entries: out = X, or w = decay w - step scale X.
 template <typename T>
-__device__ __forceinline__ void write_result(const OutputArgs &o, const Matrix &mx, int m, int col0, int n, float (&v)[32])
+__device__ __forceinline__ void write_result(const OutputArgs &o, const Matrix &mx, const float *buf, int lane, int m, int n, int rows,
+                                             int cols)
 {
-    T *dst = static_cast<T *>(o.ptr) + mx.off + (int64_t)m * mx.cols + col0;
-    if (o.update) {
-        float w[32];
-        load_row32(dst, w, n);
-        const float k = o.step * mx.scale;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = __fmaf_rn(-k, v[i], o.decay * w[i]);
+    T *dst = static_cast<T *>(o.ptr) + mx.off + (int64_t)m * mx.cols + n;
+    const float f = 1.0f / (kGramScale * mx.sx), k = o.step * mx.scale;
+    if (sizeof(T) == 2 && (mx.cols & 1) == 0 && (reinterpret_cast<uintptr_t>(dst) & 3u) == 0) {
+        const int c = (lane & 15) * 2;        // mx.cols is even, and so is every count of columns
+        if (c >= cols) return;
+#pragma unroll 4
+        for (int r = lane >> 4; r < rows; r += 2) {
+            float2 x = *reinterpret_cast<const float2 *>(buf + r * kPiecePitch + c);
+            uint32_t *d = reinterpret_cast<uint32_t *>(dst + (int64_t)r * mx.cols + c);
+            T e[2];
+            x.x *= f;
+            x.y *= f;
+            if (o.update) {
+                const uint32_t w = *d;
+                memcpy(e, &w, 4);
+                x.x = __fmaf_rn(-k, x.x, o.decay * to_f(e[0]));
+                x.y = __fmaf_rn(-k, x.y, o.decay * to_f(e[1]));
+            }
+            e[0] = from_f<T>(x.x);
+            e[1] = from_f<T>(x.y);
+            uint32_t w;
+            memcpy(&w, e, 4);
+            *d = w;
+        }
+    } else if (lane < cols) {
+#pragma unroll 4
+        for (int r = 0; r < rows; ++r) {
+            float x = buf[r * kPiecePitch + lane] * f;
+            T *d = dst + (int64_t)r * mx.cols + lane;
+            if (o.update) x = __fmaf_rn(-k, x, o.decay * to_f(*d));
+            *d = from_f<T>(x);
+        }
     }
-    store_row32(dst, v, n);
 }
 
-template <int PHASE>
-__global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_constant__ ProductParams prm)
+template <int PHASE, int CG>
+__global__ void __launch_bounds__(NTHREADS, CG == 1 ? 2 : 1) product_kernel(const __grid_constant__ ProductParams prm)
 {
+    using S = Shape<CG>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + (size_t)STAGES * STAGE);
-    uint64_t *full = bars, *empty = full + STAGES, *d_full = empty + STAGES, *d_empty = d_full + 2;
+    float *staging = reinterpret_cast<float *>(smem + (size_t)S::STAGES * S::STAGE);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + (size_t)S::STAGES * S::STAGE + NEPI * kPieceBytes);
+    uint64_t *full = bars, *empty = full + S::STAGES, *d_full = empty + S::STAGES, *d_empty = d_full + 2;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(d_empty + 2);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = CG == 2 ? (int)cluster_rank() : 0;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < STAGES; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(d_full + i, 1); mbar_init(d_empty + i, NEPI); }
+        for (int i = 0; i < S::STAGES; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(d_full + i, 1); mbar_init(d_empty + i, CG * NEPI); }
         *abort_flag = 0;
         const_cast<int *>(abort_flag)[2] = prm.wait_kcycles;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                     ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
+    if (warp == 1) tmem_alloc<CG>(tmem_slot, S::TMEM);
     tc_fence_before();
-    __syncthreads();
+    if (CG == 2) cluster_sync(); else __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    launch_dependents();
+    grid_dependency_wait();      // what the previous launch wrote is visible from here on
     bool failed = false;
     const Tile *tiles = PHASE == kApply ? prm.dev.apply_tiles : prm.dev.sym_tiles;
     const int n_tiles = PHASE == kApply ? prm.dev.n_apply : prm.dev.n_sym;
+    const int first = blockIdx.x / CG, stride = gridDim.x / CG;
 
     if (warp == 0) {
         if (lane == 0) {
             uint32_t c = 0;
-            for (int t = blockIdx.x; t < n_tiles && !failed; t += gridDim.x) {
+            for (int t = first; t < n_tiles && !failed; t += stride) {
                 const Tile tile = tiles[t];
                 const Work w = work_of<PHASE>(prm.dev.mats[tile.matrix], prm.step);
                 const CUtensorMap *ma = prm.dev.maps + (size_t)tile.matrix * kMaps + w.a_map;
                 const CUtensorMap *mb = prm.dev.maps + (size_t)tile.matrix * kMaps + w.b_map;
-                const int m0 = tile.tm * kTileM, n0 = tile.tn * kTileN;
-                // boxes that hold anything of the product
-                const int na = min(2, (w.M - m0 + 63) / 64), nb = min(4, (w.N - n0 + 63) / 64);
+                // a pair's columns are split in halves of a multiple of 8 (the last tile's may be narrow)
+                const int half_n = CG == 2 ? min(S::BN, (w.N - tile.tn * S::BN + 15) / 16 * 16) / 2 : 0;
+                const int m0 = tile.tm * 128 * CG + 128 * rank, n0 = tile.tn * S::BN + half_n * rank;
                 const int n_stages = (w.K + KS - 1) / KS;
                 for (int st = 0; st < n_stages; ++st, ++c) {
-                    const uint32_t s = c % STAGES;
-                    if (!mbar_wait(empty + s, ((c / STAGES) & 1) ^ 1, abort_flag)) { failed = true; break; }
+                    const uint32_t s = c % S::STAGES;
+                    if (!mbar_poll(empty + s, ((c / S::STAGES) & 1) ^ 1, abort_flag)) { failed = true; break; }
                     if (prm.test_drop && blockIdx.x == 0 && c == 0) continue;   // test hook: this stage never arrives
-                    unsigned char *dst = smem + (size_t)s * STAGE;
-                    mbar_arrive_expect_tx(full + s, (na + nb) * BOX);
+                    unsigned char *dst = smem + (size_t)s * S::STAGE;
+                    if (rank == 0) mbar_arrive_expect_tx(full + s, CG * S::STAGE);
                     const int k = st * KS;
-                    for (int i = 0; i < na; ++i)
-                        tma_load_2d(dst + i * BOX, ma, w.a_mn ? m0 + 64 * i : k, w.a_mn ? k : m0 + 64 * i, full + s);
-                    for (int i = 0; i < nb; ++i)
-                        tma_load_2d(dst + A_BYTES + i * BOX, mb, w.b_mn ? n0 + 64 * i : k, w.b_mn ? k : n0 + 64 * i, full + s);
+                    const uint32_t bar = CG == 2 ? in_leader(full + s) : 0;
+                    auto load = [&](unsigned char *to, const CUtensorMap *map, bool mn, int at) {
+                        if (CG == 2) tma_load_2d_pair(to, map, mn ? at : k, mn ? k : at, bar);
+                        else tma_load_2d(to, map, mn ? at : k, mn ? k : at, full + s);
+                    };
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) load(dst + i * BOX, ma, w.a_mn, m0 + 64 * i);
+#pragma unroll
+                    for (int i = 0; i < S::NB; ++i) load(dst + S::A_BYTES + i * BOX, mb, w.b_mn, n0 + 64 * i);
                 }
             }
-            if (failed) {   // give the copies already in flight a bounded chance to land before the CTA exits
-                for (uint32_t i = c > STAGES ? c - STAGES : 0; i < c; ++i)
-                    for (int it = 0; it < 100000 && !mbar_try_wait(full + i % STAGES, (i / STAGES) & 1); ++it) {}
+            if (failed && rank == 0) {   // give the copies already in flight a bounded chance to land before the CTA exits
+                for (uint32_t i = c > S::STAGES ? c - S::STAGES : 0; i < c; ++i)
+                    for (int it = 0; it < 100000 && !mbar_try_wait(full + i % S::STAGES, (i / S::STAGES) & 1); ++it) {}
             }
         }
         failed = __shfl_sync(0xffffffffu, failed, 0);
     } else if (warp == 1) {
         uint32_t c = 0, u = 0;
-        for (int t = blockIdx.x; t < n_tiles && !failed; t += gridDim.x, ++u) {
+        for (int t = first; rank == 0 && t < n_tiles && !failed; t += stride, ++u) {
             const Tile tile = tiles[t];
             const Work w = work_of<PHASE>(prm.dev.mats[tile.matrix], prm.step);
-            const uint32_t buf = u & 1, d = tmem + buf * 256;
-            const int n = min(kTileN, (w.N - tile.tn * kTileN + 15) / 16 * 16);
-            const uint32_t idesc = make_idesc_f16(n, w.a_mn, w.b_mn);
+            const uint32_t buf = u & 1, d = tmem + buf * S::BN;
+            const int n = min(S::BN, (w.N - tile.tn * S::BN + 15) / 16 * 16);
+            const uint32_t idesc = make_idesc_f16(128 * CG, n, w.a_mn, w.b_mn);
             const int n_stages = (w.K + KS - 1) / KS;
-            bool ok = mbar_wait(d_empty + buf, ((u >> 1) & 1) ^ 1, abort_flag);
+            bool ok = mbar_poll(d_empty + buf, ((u >> 1) & 1) ^ 1, abort_flag);
             if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
             tc_fence_after();
             for (int st = 0; st < n_stages; ++st, ++c) {
-                const uint32_t s = c % STAGES;
-                ok = mbar_wait(full + s, (c / STAGES) & 1, abort_flag);
+                const uint32_t s = c % S::STAGES;
+                ok = mbar_poll(full + s, (c / S::STAGES) & 1, abort_flag);
                 if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
                 tc_fence_after();
-                const uint32_t base = smem_u32(smem + (size_t)s * STAGE);
+                const uint32_t base = smem_u32(smem + (size_t)s * S::STAGE);
                 const uint64_t da = w.a_mn ? make_mn_desc(base, BOX) : make_b_desc(base);
-                const uint64_t db = w.b_mn ? make_mn_desc(base + A_BYTES, BOX) : make_b_desc(base + A_BYTES);
+                const uint64_t db = w.b_mn ? make_mn_desc(base + S::A_BYTES, BOX) : make_b_desc(base + S::A_BYTES);
                 // 16 steps of the contraction: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major box
                 const uint32_t ia = w.a_mn ? 16 * 128 / 16 : 2, ib = w.b_mn ? 16 * 128 / 16 : 2;
                 const int n_mma = min(4, (w.K - st * KS + 15) / 16);
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        if (k < n_mma) tc_mma_f16(d, da + k * ia, db + k * ib, idesc, (st | k) != 0);
-                    tc_commit(empty + s);
-                    if (st == n_stages - 1) tc_commit(d_full + buf);
+                        if (k < n_mma) tc_mma_f16<CG>(d, da + k * ia, db + k * ib, idesc, (st | k) != 0);
+                    if (CG == 2) tc_commit_pair(empty + s); else tc_commit(empty + s);
+                    if (st == n_stages - 1) { if (CG == 2) tc_commit_pair(d_full + buf); else tc_commit(d_full + buf); }
                 }
                 __syncwarp();
             }
@@ -312,78 +361,91 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
     } else {
         const int q = warp & 3, half = (warp - 2) >> 2;
         const uint32_t lane_base = (uint32_t)(32 * q) << 16;
+        float *buf = staging + (warp - 2) * (kPieceBytes / 4);
+        constexpr int PIECES = S::BN / 2 / 32;      // of a warp
         uint32_t u = 0;
-        for (int t = blockIdx.x; t < n_tiles; t += gridDim.x, ++u) {
+        for (int t = first; t < n_tiles; t += stride, ++u) {
             const Tile tile = tiles[t];
             const Matrix mx = prm.dev.mats[tile.matrix];
             const Work w = work_of<PHASE>(mx, prm.step);
-            const uint32_t buf = u & 1;
-            bool ok = mbar_wait(d_full + buf, (u >> 1) & 1, abort_flag);
+            const uint32_t ab = u & 1;
+            bool ok = mbar_poll(d_full + ab, (u >> 1) & 1, abort_flag);
             if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
             tc_fence_after();
-            const int m = tile.tm * kTileM + 32 * q + lane;
-            // a tile right of the diagonal's 256 x 256 block stands for its mirror image too
-            const bool mirror = PHASE != kApply && tile.tn > tile.tm / 2;
+            const int m0 = tile.tm * 128 * CG + 128 * rank + 32 * q;       // first row of this warp's pieces
+            const int rows = min(32, w.M - m0);
+            // a tile wholly right of the diagonal stands for its mirror image too
+            const bool mirror = PHASE != kApply && tile.tn * S::BN >= (tile.tm + 1) * 128 * CG;
 #pragma unroll 1
-            for (int p = 0; p < 4; ++p) {
-                const int cl = half * 128 + p * 32, col0 = tile.tn * kTileN + cl;
-                if (col0 >= w.N) break;
+            for (int p = 0; p < PIECES; ++p) {
+                const int cl = half * (S::BN / 2) + p * 32, n0 = tile.tn * S::BN + cl;
+                if (n0 >= w.N) break;
                 float v[32];
-                tmem_ld32_wait(tmem + lane_base + buf * 256 + cl, v);
-                const int n = m < w.M ? min(32, w.N - col0) : 0;
-                if (n <= 0) continue;
+                tmem_ld32_wait(tmem + lane_base + ab * S::BN + cl, v);
+                if (rows <= 0) continue;
+                const int cols = min(32, w.N - n0);
                 if (PHASE == kApply) {
-                    const int64_t at = (int64_t)m * mx.ldx + col0;
-                    const int np = min(32, mx.ldx - col0);     // rows are padded: whole pieces of eight
-                    float x[32];
-                    load_row32(mx.x[prm.step & 1] + at, x, np);
-                    if (prm.step < kExactSteps) {
-                        float lo[32];
-                        load_row32(mx.lo + at, lo, np);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) x[i] += lo[i];
-                    }
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = __fmaf_rn(kA, x[i], v[i] * (1.0f / kGramScale));
+                    stage_piece(buf, lane, v);
                     if (prm.step < kSteps - 1) {
-                        store_row32(mx.x[(prm.step + 1) & 1] + at, v, np);
-                        if (prm.step + 1 < kExactSteps) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) v[i] -= __half2float(__float2half_rn(v[i]));
-                            store_row32(mx.lo + at, v, np);
+                        // rows are padded to whole pieces: every lane stores.  X' = P X_hi + a X_lo.
+                        const int c = (lane & 15) * 2;
+                        const int64_t at = (int64_t)m0 * mx.ldx + n0 + c;
+                        __half *lo = mx.lo + at, *hi = mx.x[(prm.step + 1) & 1] + at;
+                        const bool read_lo = prm.step < kExactSteps, write_lo = prm.step + 1 < kExactSteps;
+#pragma unroll 8
+                        for (int r = lane >> 4; r < rows; r += 2) {
+                            float2 x = *reinterpret_cast<const float2 *>(buf + r * kPiecePitch + c);
+                            x.x *= 1.0f / kGramScale;
+                            x.y *= 1.0f / kGramScale;
+                            const int64_t o = (int64_t)r * mx.ldx;
+                            if (read_lo) {
+                                const float2 l = __half22float2(*reinterpret_cast<const __half2 *>(lo + o));
+                                x.x = __fmaf_rn(kA, l.x, x.x);
+                                x.y = __fmaf_rn(kA, l.y, x.y);
+                            }
+                            const __half2 h = __floats2half2_rn(x.x, x.y);
+                            *reinterpret_cast<__half2 *>(hi + o) = h;
+                            if (write_lo) {
+                                const float2 f = __half22float2(h);
+                                *reinterpret_cast<__half2 *>(lo + o) = __floats2half2_rn(x.x - f.x, x.y - f.y);
+                            }
                         }
                     } else {
-                        const float f = 1.0f / mx.sx;
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] *= f;
-                        if (prm.out.dtype == GVQ_F32) write_result<float>(prm.out, mx, m, col0, n, v);
-                        else if (prm.out.dtype == GVQ_BF16) write_result<__nv_bfloat16>(prm.out, mx, m, col0, n, v);
-                        else write_result<__half>(prm.out, mx, m, col0, n, v);
+                        if (prm.out.dtype == GVQ_F32) write_result<float>(prm.out, mx, buf, lane, m0, n0, rows, cols);
+                        else if (prm.out.dtype == GVQ_BF16) write_result<__nv_bfloat16>(prm.out, mx, buf, lane, m0, n0, rows, cols);
+                        else write_result<__half>(prm.out, mx, buf, lane, m0, n0, rows, cols);
                     }
                 } else {
-                    const int64_t at = (int64_t)m * mx.ldr + col0;
+                    // A = X X^T, or P = a I + b A + c A^2 (so that the last product is all of the step).  A is symmetric:
+                    // its transposed entries are read, a column of them along the warp.
+                    __half *dst = PHASE == kGram ? mx.gram : mx.poly;
                     if (PHASE == kGram) {
                         const float f = kGramScale / (mx.sx * mx.sx);
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] *= f;
                     } else {
-                        float a[32];
-                        load_row32(mx.gram + at, a, min(32, mx.ldr - col0));
+                        const __half *a = mx.gram + (int64_t)n0 * mx.ldr + m0 + lane;
+                        __half av[32];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = __fmaf_rn(kB, a[i], v[i] * (kC / kGramScale));
+                        for (int i = 0; i < 32; ++i) av[i] = i < cols && lane < rows ? a[(int64_t)i * mx.ldr] : __half(0.0f);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            v[i] = __fmaf_rn(kB, __half2float(av[i]), v[i] * (kC / kGramScale));
+                            if (n0 + i == m0 + lane) v[i] += kA * kGramScale;
+                        }
                     }
-                    __half *dst = PHASE == kGram ? mx.gram : mx.poly;
-                    store_row32(dst + at, v, min(32, mx.ldr - col0));
                     if (mirror) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (i < n) dst[(int64_t)(col0 + i) * mx.ldr + m] = __float2half_rn(v[i]);
+                            if (i < cols && lane < rows) dst[(int64_t)(n0 + i) * mx.ldr + m0 + lane] = __float2half_rn(v[i]);
                     }
+                    stage_piece(buf, lane, v);
+                    store_piece(buf, lane, dst + (int64_t)m0 * mx.ldr + n0, mx.ldr, rows, cols);
                 }
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(d_empty + buf);
+            if (lane == 0) { if (CG == 2) mbar_arrive_cluster(in_leader(d_empty + ab)); else mbar_arrive(d_empty + ab); }
         }
     }
 
@@ -392,10 +454,33 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
         if (lane == 0) atomicExch(prm.error_word, 100 + warp);
     }
     tc_fence_before();
-    __syncthreads();
+    if (CG == 2) cluster_sync(); else __syncthreads();     // a pair: the other CTA's barriers and memory are in use until here
     tc_fence_after();
-    if (warp == 1)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    if (warp == 1) tmem_dealloc<CG>(tmem, S::TMEM);
+}
+
+template <typename K, typename P>
+cudaError_t launch_chained(K kernel, const P &prm, int grid, int threads, size_t smem, int cluster, cudaStream_t st)
+{
+    if (smem > 48 * 1024) {
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, prm);
 }
 
 }  // namespace
@@ -406,11 +491,9 @@ cudaError_t launch_start(cudaStream_t st, const Device &dev, const ElementArgs &
     prm.dev = dev;
     prm.a = a;
     prm.mode = !a.momentum ? 0 : a.nesterov ? 2 : 1;
-    momentum_kernel<<<dev.n_chunks, 256, 0, st>>>(prm);
-    cudaError_t e = cudaGetLastError();
+    cudaError_t e = launch_chained(momentum_kernel, prm, dev.n_chunks, 256, 0, 1, st);
     if (e != cudaSuccess) return e;
-    normalise_kernel<<<dev.n_chunks, 256, 0, st>>>(prm);
-    return cudaGetLastError();
+    return launch_chained(normalise_kernel, prm, dev.n_chunks, 256, 0, 1, st);
 }
 
 cudaError_t launch_product(cudaStream_t st, int num_sms, const Device &dev, Phase phase, int step, const OutputArgs *out,
@@ -424,16 +507,13 @@ cudaError_t launch_product(cudaStream_t st, int num_sms, const Device &dev, Phas
     prm.wait_kcycles = wait_kcycles > 0 ? wait_kcycles : WAIT_KCYCLES_DEFAULT;
     prm.test_drop = test_drop;
     const int n = phase == kApply ? dev.n_apply : dev.n_sym;
-    const int grid = n < num_sms ? n : num_sms;
-    auto launch = [&](auto kernel) {
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PRODUCT_SMEM);
-        if (e != cudaSuccess) return e;
-        kernel<<<grid, NTHREADS, PRODUCT_SMEM, st>>>(prm);
-        return cudaGetLastError();
+    auto launch = [&](auto pair, auto solo) {
+        return dev.pair ? launch_chained(pair, prm, 2 * min(n, num_sms / 2), NTHREADS, Shape<2>::SMEM, 2, st)
+                        : launch_chained(solo, prm, min(n, 2 * num_sms), NTHREADS, Shape<1>::SMEM, 1, st);
     };
-    if (phase == kGram) return launch(product_kernel<kGram>);
-    if (phase == kPoly) return launch(product_kernel<kPoly>);
-    return launch(product_kernel<kApply>);
+    if (phase == kGram) return launch(product_kernel<kGram, 2>, product_kernel<kGram, 1>);
+    if (phase == kPoly) return launch(product_kernel<kPoly, 2>, product_kernel<kPoly, 1>);
+    return launch(product_kernel<kApply, 2>, product_kernel<kApply, 1>);
 }
 
 }  // namespace ortho

@@ -14,11 +14,12 @@ constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr float kEps = 1e-7f;
 // Steps whose X is kept as a sum of two halves (ortho.cu's header has the reason).
 constexpr int kExactSteps = 3;
-// Scale of A and B in half precision: entries of both are of order 1 at most (|b| 1.2 + |c| 1.44 = 8.7), those off the
-// diagonal far smaller.
+// Scale of A and of a I + b A + c A^2 in half precision: entries of both are of order 1 (at most 3.5 + 1.2 |b| + 1.44 |c| = 12),
+// those off the diagonal far smaller.
 constexpr float kGramScale = 256.0f;
 
-constexpr int kTileM = 128, kTileN = 256;
+// Tiles of the products (ortho.cu): a pair of CTAs has 256 x kPairN, a CTA alone 128 x kSoloN.
+constexpr int kPairN = 256, kSoloN = 64;
 constexpr int kChunk = 8192;     // entries of a chunk of the element-wise passes
 
 // One matrix [rows][cols] of the flat gradient.  r <= c its shorter and longer side.
@@ -41,6 +42,7 @@ struct Device {
     const CUtensorMap *maps;         // [matrices][kMaps]
     const Tile *sym_tiles, *apply_tiles;
     int n_sym, n_apply;
+    int pair;                        // which tiling the tiles are of
     const Chunk *chunks;
     int n_chunks;
     float *partial;                  // [n_chunks] sums of squares

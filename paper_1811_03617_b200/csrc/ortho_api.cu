@@ -19,8 +19,9 @@ struct gvq_ortho {
 namespace {
 
 constexpr size_t kAlign = 256;
+constexpr int kPairTiles = 148;   // fewer 256 x 256 tiles than this: 128 x 64 tiles
 size_t up(size_t n) { return (n + kAlign - 1) & ~(kAlign - 1); }
-int up8(int n) { return (n + 7) & ~7; }
+int up32(int n) { return (n + 31) & ~31; }     // rows of the work arrays: whole pieces of 32 entries
 
 struct Sizes {
     std::vector<Matrix> mats;
@@ -40,7 +41,7 @@ gvq_status lay_out(int n_layers, const int64_t *off, const int64_t *len, const i
         m.r = std::min(m.rows, m.cols); m.c = std::max(m.rows, m.cols);
         if (m.r > 32768) return GVQ_ERR_SHAPE;                    // r x r products beyond any layer
         m.tall = m.rows > m.cols;
-        m.ldx = up8(m.cols); m.ldr = up8(m.r);
+        m.ldx = up32(m.cols); m.ldr = up32(m.r);
         m.off = off[l];
         // entries of X have an rms of 1 / sqrt(r c) at first and 1 / sqrt(c) at last: about 1 / sqrt(r) to 1 when scaled
         m.sx = std::exp2(std::round(0.5f * std::log2((float)m.c)));
@@ -121,14 +122,26 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
             if (!encode(enc, mp + kX0, m.x[0], m.rows, m.cols, m.ldx) || !encode(enc, mp + kX1, m.x[1], m.rows, m.cols, m.ldx) ||
                 !encode(enc, mp + kGramMap, m.gram, m.r, m.r, m.ldr) || !encode(enc, mp + kPolyMap, m.poly, m.r, m.r, m.ldr))
                 return GVQ_ERR_CUDA;
-            // tiles of a symmetric product: those whose 256 columns reach the diagonal block of their rows
-            for (int tm = 0; tm * kTileM < m.r; ++tm)
-                for (int tn = tm / 2; tn * kTileN < m.r; ++tn) sym.push_back({i, tm, tn});
-            for (int tm = 0; (int64_t)tm * kTileM < m.rows; ++tm)
-                for (int tn = 0; (int64_t)tn * kTileN < m.cols; ++tn) apply.push_back({i, tm, tn});
             m.chunk0 = (int)chunks.size();
             m.n_chunks = (int)(((int64_t)m.rows * m.cols + kChunk - 1) / kChunk);
             for (int k = 0; k < m.n_chunks; ++k) chunks.push_back({i, k});
+        }
+        // Which tiling: pairs of CTAs on 256 x 256 tiles where there are enough of them.
+        bool pair = false;
+        for (int attempt = 0; attempt < 2; ++attempt) {
+            pair = attempt == 0;
+            const int64_t bm = pair ? 256 : 128, bn = pair ? kPairN : kSoloN;
+            sym.clear();
+            apply.clear();
+            for (int i = 0; i < n; ++i) {
+                const Matrix &m = sz.mats[i];
+                // tiles of a symmetric product: those that reach the diagonal or lie right of it
+                for (int tm = 0; tm * bm < m.r; ++tm)
+                    for (int tn = (int)(tm * bm / bn); tn * bn < m.r; ++tn) sym.push_back({i, tm, tn});
+                for (int tm = 0; tm * bm < m.rows; ++tm)
+                    for (int tn = 0; tn * bn < m.cols; ++tn) apply.push_back({i, tm, tn});
+            }
+            if (pair && (int)apply.size() >= kPairTiles) break;
         }
         // longest contraction first: the CTAs take the tiles in turn, and the short ones level the end
         std::stable_sort(sym.begin(), sym.end(), [&](const Tile &a, const Tile &b) { return sz.mats[a.matrix].c > sz.mats[b.matrix].c; });
@@ -161,6 +174,7 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
         d.apply_tiles = reinterpret_cast<Tile *>(t + b_m + b_t + b_s);
         d.chunks = reinterpret_cast<Chunk *>(t + b_m + b_t + b_s + b_a);
         d.partial = reinterpret_cast<float *>(t + image.size());
+        d.pair = pair;
         d.n_sym = (int)sym.size(); d.n_apply = (int)apply.size(); d.n_chunks = (int)chunks.size();
         *out = p;
         return GVQ_OK;

@@ -1,4 +1,6 @@
-// What the epilogues of the product kernels share: 32 consecutive entries of a row, a thread's own, to and from memory.
+// What the epilogues of the product kernels share: a 32 x 32 piece of an accumulator goes from "a thread has a row"
+// (how tensor memory is read) to "a warp has a row" through shared memory, so that global memory is read and written
+// along rows: 64 or 128 bytes of one or two rows an instruction, where a thread's own row would touch 32 lines.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -15,45 +17,75 @@ template <typename T> __device__ __forceinline__ float to_f(T x);
 template <> __device__ __forceinline__ float to_f(float x) { return x; }
 template <> __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
 template <> __device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
-
-// The first n of 32 entries (n <= 0: none), in 16-byte pieces where they are aligned.
-template <typename T>
-__device__ __forceinline__ void store_row32(T *dst, const float (&v)[32], int n)
+__device__ __forceinline__ uint32_t pack2(__half a, __half b) { return (uint32_t)__half_as_ushort(a) | (uint32_t)__half_as_ushort(b) << 16; }
+__device__ __forceinline__ uint32_t pack2(__nv_bfloat16 a, __nv_bfloat16 b)
 {
-    constexpr int PER = 16 / (int)sizeof(T);
-    T e[32];
+    return (uint32_t)__bfloat16_as_ushort(a) | (uint32_t)__bfloat16_as_ushort(b) << 16;
+}
+
+constexpr int kPiecePitch = 36;                              // words: 16-byte stores of eight lanes hit all banks
+constexpr int kPieceBytes = 32 * kPiecePitch * 4;            // a warp's staging area
+
+// Thread `lane` holds row `lane` of the piece.
+__device__ __forceinline__ void stage_piece(float *buf, int lane, const float (&v)[32])
+{
+    __syncwarp();                                            // the last piece has been read
 #pragma unroll
-    for (int i = 0; i < 32; ++i) e[i] = from_f<T>(v[i]);
-    if (n >= 32 && (reinterpret_cast<uintptr_t>(dst) & 15u) == 0) {
+    for (int i = 0; i < 8; ++i)
+        *reinterpret_cast<float4 *>(buf + lane * kPiecePitch + 4 * i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+    __syncwarp();
+}
+
+// A piece as a TMA store reads it: 32 rows of 128 bytes, 16-byte chunk j of row r at place j ^ (r % 8).  Thread `lane` holds
+// row `lane`: 64 entries of a 16-bit type, or 32 floats.
+__device__ __forceinline__ void stage_swizzled(unsigned char *buf, int lane, const float (&v)[32])
+{
 #pragma unroll
-        for (int i = 0; i < 32 / PER; ++i) {
-            uint4 q;
-            memcpy(&q, e + i * PER, 16);
-            reinterpret_cast<uint4 *>(dst)[i] = q;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (i < n) dst[i] = e[i];
-    }
+    for (int j = 0; j < 8; ++j)
+        *reinterpret_cast<float4 *>(buf + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+            make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
 }
 template <typename T>
-__device__ __forceinline__ void load_row32(const T *src, float (&v)[32], int n)
+__device__ __forceinline__ void stage_swizzled16(unsigned char *buf, int lane, const float (&a)[32], const float (&b)[32])
 {
-    constexpr int PER = 16 / (int)sizeof(T);
-    T e[32];
-    if (n >= 32 && (reinterpret_cast<uintptr_t>(src) & 15u) == 0) {
 #pragma unroll
-        for (int i = 0; i < 32 / PER; ++i) {
-            const uint4 q = reinterpret_cast<const uint4 *>(src)[i];
-            memcpy(e + i * PER, &q, 16);
+    for (int j = 0; j < 8; ++j) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int e = (8 * j + 2 * i) & 31;
+            w[i] = j < 4 ? pack2(from_f<T>(a[e]), from_f<T>(a[e + 1])) : pack2(from_f<T>(b[e]), from_f<T>(b[e + 1]));
+        }
+        *reinterpret_cast<uint4 *>(buf + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// Writes the piece's rows x cols entries (both at most 32) at dst, rows ld entries apart.  PAIR: two entries a lane, for
+// 16-bit types whose rows start at 4-byte boundaries.
+template <typename T>
+__device__ __forceinline__ void store_piece(const float *buf, int lane, T *dst, int64_t ld, int rows, int cols)
+{
+    if (sizeof(T) == 2 && (ld & 1) == 0 && (reinterpret_cast<uintptr_t>(dst) & 3u) == 0) {
+        const int c = (lane & 15) * 2;
+#pragma unroll 4
+        for (int r = lane >> 4; r < rows; r += 2) {
+            const float2 x = *reinterpret_cast<const float2 *>(buf + r * kPiecePitch + c);
+            T *d = dst + (int64_t)r * ld + c;
+            const T a = from_f<T>(x.x), b = from_f<T>(x.y);
+            if (c + 1 < cols) {
+                uint32_t w;
+                T e[2] = {a, b};
+                memcpy(&w, e, 4);
+                *reinterpret_cast<uint32_t *>(d) = w;
+            } else if (c < cols) {
+                *d = a;
+            }
         }
     } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) e[i] = i < n ? src[i] : from_f<T>(0.0f);
+#pragma unroll 4
+        for (int r = 0; r < rows; ++r)
+            if (lane < cols) dst[(int64_t)r * ld + lane] = from_f<T>(buf[r * kPiecePitch + lane]);
     }
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = to_f(e[i]);
 }
 
 }  // namespace gvq

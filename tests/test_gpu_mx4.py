@@ -128,6 +128,34 @@ def test_product(ctx, m, n, k, dtype):
     assert (err <= bound[~near]).all(), float((err / bound[~near]).max())
 
 
+@pytest.mark.parametrize("m,n,k,dtype,pad", [
+    (1664, 1600, 256, "bf16", 0), (1601, 1611, 1300, "f32", 5), (1700, 1537, 96, "f16", 7), (2304, 2056, 640, "f32", 0),
+    (4100, 3000, 2048, "bf16", 8), (1537, 4000, 4128, "bf16", 0)])
+def test_large_product(ctx, m, n, k, dtype, pad):
+    """Enough 256 x 256 tiles for pairs of CTAs; codes and scales made on the GPU (tested bit for bit above), the product
+    against float64 of what they stand for."""
+    g = torch.Generator(device="cuda").manual_seed(m)
+    a = torch.randn(m, k, generator=g, device="cuda") * 2.0 ** torch.randint(-9, 10, (m, 1), generator=g, device="cuda")
+    b = torch.randn(n, k, generator=g, device="cuda")
+    for t in (a, b):
+        for j in range(0, k, 32):
+            t[:, j:j + 32] *= 2.0 ** torch.randint(-6, 7, (t.shape[0], 1), generator=g, device="cuda")
+    qa, qb = ctx.mx4_quantize(a), ctx.mx4_quantize(b)
+    va, vb = ctx.mx4_dequantize(qa).double(), ctx.mx4_dequantize(qb).double()
+    buf = torch.full((m, n + pad), 3.0, dtype=DT[dtype], device="cuda")
+    ctx.mx4_matmul(qa, qb, buf[:, :n])
+    ctx.device_status()
+    want, mag = va @ vb.T, va.abs() @ vb.abs().T
+    half_ulp = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}[DT[dtype]]
+    bound = mag * (-(-k // 64) + 2) * 2.0 ** -22 + want.abs() * half_ulp + (6e-8 if dtype == "f16" else 0)
+    near = want.abs() + bound < float(torch.finfo(DT[dtype]).max)
+    assert bool(((buf[:, :n].double() - want).abs() <= bound)[near].all())
+    assert bool((buf[:, n:] == 3.0).all())
+    again = torch.empty(m, n, dtype=DT[dtype], device="cuda")
+    ctx.mx4_matmul(qa, qb, again)
+    assert torch.equal(again, buf[:, :n])
+
+
 @pytest.mark.parametrize("m", [3, 150])
 def test_product_writes_inside_the_output_only_and_repeats_its_bits(ctx, m):
     n, k = 261, 513
