@@ -542,7 +542,8 @@ gvq_status gvq_mx4_dequantize_aggregate(gvq_ctx *ctx, const uint8_t *const *code
    side is at most 32768.  scales_opt: NULL or HOST [n_layers].  workspace: device, 256-byte aligned,
    gvq_ortho_workspace_bytes() bytes (-1 on bad sizes), owned by the caller and kept while the plan lives; its contents
    carry nothing from one call to the next.  The plan keeps tables in device memory of its own (one allocation at create).
-   It must not outlive its context, whose stream its calls use; they allocate nothing and can be captured. */
+   Its calls use its context's stream, allocate nothing and can be captured; after gvq_destroy(ctx) the plan can only be
+   destroyed. */
 typedef struct gvq_ortho gvq_ortho;
 int64_t gvq_ortho_workspace_bytes(const gvq_layout *layout, const int32_t *rows, const int32_t *cols);
 gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, const int32_t *cols,

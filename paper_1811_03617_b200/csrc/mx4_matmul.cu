@@ -133,6 +133,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) mx4_matmul_kernel(const __grid_co
     if (warp == 0) {
         // ------------------------------------------------------------------ producer
         if (lane == 0) {
+            fence_proxy_async_global();      // what plain stores of the previous launch wrote is read by TMA
             uint32_t c = 0;
             for (int tile = first; tile < n_tiles && !failed; tile += stride) {
                 const int tn = tile / prm.tiles_m, tm = tile - tn * prm.tiles_m;

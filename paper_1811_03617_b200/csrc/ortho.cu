@@ -175,23 +175,26 @@ __global__ void __launch_bounds__(256) normalise_kernel(const StartParams prm)
 // Persistent CTAs (or pairs of CTAs), 64 steps of the contraction a stage.  Every operand comes in boxes of 64 x 64 entries
 // (8 KB, 128-byte swizzle, zero fill outside), the same tensor map for either major:
 //   K-major   box = 64 steps x 64 rows     MN-major   box = 64 entries across x 64 steps
-//   warp 0      producer      warp 1  MMA      warps 2-9  epilogue (lane quarter warp % 4, half the columns each)
+//   warp 0      producer      warp 1  MMA      then the epilogue's warps (lane quarter warp % 4; a pair's CTA has eight, half
+//               the columns each): 64 columns at a time, staged in half precision and stored by TMA
 // Two tilings:
 //   CG = 2  a pair of CTAs on two SMs, tile 256 x 256: each loads and holds its own 128 rows of A and half of B's rows, the
 //           even one issues MMAs that read both.  32 KB a stage and SM for 512 clocks of MMAs; a CTA alone on 128 x 256
 //           would load 48 KB, more than L2 delivers to all SMs at that rate.
 //   CG = 1  one CTA, tile 128 x 64, for plans without enough large tiles to fill the GPU: four times the CTAs at work, a
 //           quarter of the time a stage, and two CTAs fit an SM, so that a launch's first tiles overlap the last one's end.
-constexpr int KS = 64, NTHREADS = 320, NEPI = 8;
+constexpr int KS = 64;
 constexpr uint32_t BOX = 64 * 128;
+constexpr uint32_t kStaging = 8192;      // of an epilogue warp: two pieces of 32 rows x 128 bytes
 
 template <int CG> struct Shape {
     static constexpr int BN = CG == 2 ? kPairN : kSoloN;                     // columns of a tile
     static constexpr int NB = CG == 2 ? 2 : BN / 64;                        // boxes of B a CTA loads
     static constexpr uint32_t A_BYTES = 2 * BOX, STAGE = A_BYTES + NB * BOX;
     static constexpr int STAGES = CG == 2 ? 5 : 3;
+    static constexpr int NEPI = CG == 2 ? 8 : 4, THREADS = 64 + 32 * NEPI;   // epilogue warps
     static constexpr uint32_t TMEM = 2 * BN;                                 // two accumulators
-    static constexpr size_t SMEM = (size_t)STAGES * STAGE + NEPI * kPieceBytes + 256 + 1024;
+    static constexpr size_t SMEM = (size_t)STAGES * STAGE + NEPI * kStaging + 256 + 1024;
 };
 
 struct ProductParams {
@@ -213,58 +216,102 @@ __device__ __forceinline__ Work work_of(const Matrix &m, int step)
 {
     const int x = step & 1;
     if (PHASE == kGram) return {m.r, m.r, m.c, x, x, m.tall != 0, m.tall != 0};
-    if (PHASE == kPoly) return {m.r, m.r, m.r, kGramMap, kGramMap, false, false};
+    if (PHASE == kPoly) return {m.r, m.r, m.r, kGramMap, kFactorMap, false, false};
     return m.tall ? Work{m.rows, m.cols, m.r, x, kPolyMap, false, false} : Work{m.rows, m.cols, m.r, kPolyMap, x, false, true};
 }
 
-// The last step's result, a staged piece of rows x cols entries: out = X, or w = decay w - step scale X.
-template <typename T>
-__device__ __forceinline__ void write_result(const OutputArgs &o, const Matrix &mx, const float *buf, int lane, int m, int n, int rows,
-                                             int cols)
-{
-    T *dst = static_cast<T *>(o.ptr) + mx.off + (int64_t)m * mx.cols + n;
-    const float f = 1.0f / (kGramScale * mx.sx), k = o.step * mx.scale;
-    if (sizeof(T) == 2 && (mx.cols & 1) == 0 && (reinterpret_cast<uintptr_t>(dst) & 3u) == 0) {
-        const int c = (lane & 15) * 2;        // mx.cols is even, and so is every count of columns
-        if (c >= cols) return;
-#pragma unroll 4
-        for (int r = lane >> 4; r < rows; r += 2) {
-            float2 x = *reinterpret_cast<const float2 *>(buf + r * kPiecePitch + c);
-            uint32_t *d = reinterpret_cast<uint32_t *>(dst + (int64_t)r * mx.cols + c);
-            T e[2];
-            x.x *= f;
-            x.y *= f;
-            if (o.update) {
-                const uint32_t w = *d;
-                memcpy(e, &w, 4);
-                x.x = __fmaf_rn(-k, x.x, o.decay * to_f(e[0]));
-                x.y = __fmaf_rn(-k, x.y, o.decay * to_f(e[1]));
+// The last step's result, 32 x 32 entries at a time: out = X, or w = decay w - step scale X.  A lane has a column, or two
+// neighbouring ones of a 16-bit type whose rows start at 4-byte boundaries, of every row or every other row; the weights
+// are fetched a piece ahead.
+template <typename T> struct Weights {
+    uint32_t w[32];
+    bool paired;
+    T *at;               // the piece's first entry
+    int rows, cols;
+
+    __device__ __forceinline__ void fetch(const OutputArgs &o, const Matrix &mx, int lane, int m, int n, int rows_, int cols_)
+    {
+        at = static_cast<T *>(o.ptr) + mx.off + (int64_t)m * mx.cols + n;
+        rows = rows_;
+        cols = cols_;
+        paired = sizeof(T) == 2 && (mx.cols & 1) == 0 && (reinterpret_cast<uintptr_t>(at) & 3u) == 0;
+        if (!o.update) return;
+        if (paired) {
+            const T *d = at + (int64_t)(lane >> 4) * mx.cols + (lane & 15) * 2;
+            const bool in = (lane & 15) * 2 < cols;      // cols is even: a layer's columns are, and 32
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (in && 2 * i + (lane >> 4) < rows) w[i] = *reinterpret_cast<const uint32_t *>(d + (int64_t)2 * i * mx.cols);
+        } else {
+            const T *d = at + lane;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                if (lane < cols && i < rows) {
+                    if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(d[(int64_t)i * mx.cols]);
+                    else w[i] = *reinterpret_cast<const uint16_t *>(d + (int64_t)i * mx.cols);
+                }
             }
-            e[0] = from_f<T>(x.x);
-            e[1] = from_f<T>(x.y);
-            uint32_t w;
-            memcpy(&w, e, 4);
-            *d = w;
-        }
-    } else if (lane < cols) {
-#pragma unroll 4
-        for (int r = 0; r < rows; ++r) {
-            float x = buf[r * kPiecePitch + lane] * f;
-            T *d = dst + (int64_t)r * mx.cols + lane;
-            if (o.update) x = __fmaf_rn(-k, x, o.decay * to_f(*d));
-            *d = from_f<T>(x);
         }
     }
+    static __device__ __forceinline__ T entry(uint32_t bits)
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(bits);
+        const uint16_t u = (uint16_t)bits;
+        T e;
+        memcpy(&e, &u, 2);
+        return e;
+    }
+    __device__ __forceinline__ void finish(const OutputArgs &o, const Matrix &mx, const float *buf, int lane)
+    {
+        const float f = 1.0f / (kGramScale * mx.sx), k = o.step * mx.scale;
+        if (paired) {
+            const int c = (lane & 15) * 2;
+            T *d = at + (int64_t)(lane >> 4) * mx.cols + c;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int r = 2 * i + (lane >> 4);
+                if (c < cols && r < rows) {
+                    float2 x = *reinterpret_cast<const float2 *>(buf + r * kPiecePitch + c);
+                    x.x *= f;
+                    x.y *= f;
+                    if (o.update) {
+                        x.x = __fmaf_rn(-k, x.x, o.decay * to_f(entry(w[i])));
+                        x.y = __fmaf_rn(-k, x.y, o.decay * to_f(entry(w[i] >> 16)));
+                    }
+                    if constexpr (sizeof(T) == 2)
+                        *reinterpret_cast<uint32_t *>(d + (int64_t)2 * i * mx.cols) = pack2(from_f<T>(x.x), from_f<T>(x.y));
+                }
+            }
+        } else if (lane < cols) {
+            T *d = at + lane;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                if (i < rows) {
+                    float x = buf[i * kPiecePitch + lane] * f;
+                    if (o.update) x = __fmaf_rn(-k, x, o.decay * to_f(entry(w[i])));
+                    d[(int64_t)i * mx.cols] = from_f<T>(x);
+                }
+            }
+        }
+    }
+};
+
+// 16 halves of a row (32 bytes, aligned)
+__device__ __forceinline__ void load16(const __half *p, uint32_t (&w)[8])
+{
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
 }
 
-template <int PHASE, int CG>
-__global__ void __launch_bounds__(NTHREADS, CG == 1 ? 2 : 1) product_kernel(const __grid_constant__ ProductParams prm)
+// T: the type of the last step's result (PHASE kLast).
+template <int PHASE, int CG, typename T = float>
+__global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_kernel(const __grid_constant__ ProductParams prm)
 {
     using S = Shape<CG>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    float *staging = reinterpret_cast<float *>(smem + (size_t)S::STAGES * S::STAGE);
-    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + (size_t)S::STAGES * S::STAGE + NEPI * kPieceBytes);
+    unsigned char *staging = smem + (size_t)S::STAGES * S::STAGE;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(staging + S::NEPI * kStaging);
     uint64_t *full = bars, *empty = full + S::STAGES, *d_full = empty + S::STAGES, *d_empty = d_full + 2;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(d_empty + 2);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
@@ -272,7 +319,7 @@ __global__ void __launch_bounds__(NTHREADS, CG == 1 ? 2 : 1) product_kernel(cons
     const int rank = CG == 2 ? (int)cluster_rank() : 0;
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::STAGES; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(d_full + i, 1); mbar_init(d_empty + i, CG * NEPI); }
+        for (int i = 0; i < 2; ++i) { mbar_init(d_full + i, 1); mbar_init(d_empty + i, CG * S::NEPI); }
         *abort_flag = 0;
         const_cast<int *>(abort_flag)[2] = prm.wait_kcycles;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -285,14 +332,17 @@ __global__ void __launch_bounds__(NTHREADS, CG == 1 ? 2 : 1) product_kernel(cons
     launch_dependents();
     grid_dependency_wait();      // what the previous launch wrote is visible from here on
     bool failed = false;
-    const Tile *tiles = PHASE == kApply ? prm.dev.apply_tiles : prm.dev.sym_tiles;
-    const int n_tiles = PHASE == kApply ? prm.dev.n_apply : prm.dev.n_sym;
-    const int first = blockIdx.x / CG, stride = gridDim.x / CG;
+    // this CTA's (pair's) run of tiles
+    constexpr bool APPLY = PHASE == kApply || PHASE == kLast;
+    const Tile *tiles = APPLY ? prm.dev.apply_tiles : prm.dev.sym_tiles;
+    const int32_t *starts = APPLY ? prm.dev.apply_start : prm.dev.sym_start;
+    const int t_begin = starts[blockIdx.x / CG], t_end = starts[blockIdx.x / CG + 1];
 
     if (warp == 0) {
         if (lane == 0) {
+            fence_proxy_async_global();      // what plain stores of the previous launch wrote is read by TMA
             uint32_t c = 0;
-            for (int t = first; t < n_tiles && !failed; t += stride) {
+            for (int t = t_begin; t < t_end && !failed; ++t) {
                 const Tile tile = tiles[t];
                 const Work w = work_of<PHASE>(prm.dev.mats[tile.matrix], prm.step);
                 const CUtensorMap *ma = prm.dev.maps + (size_t)tile.matrix * kMaps + w.a_map;
@@ -327,7 +377,7 @@ __global__ void __launch_bounds__(NTHREADS, CG == 1 ? 2 : 1) product_kernel(cons
         failed = __shfl_sync(0xffffffffu, failed, 0);
     } else if (warp == 1) {
         uint32_t c = 0, u = 0;
-        for (int t = first; rank == 0 && t < n_tiles && !failed; t += stride, ++u) {
+        for (int t = t_begin; rank == 0 && t < t_end && !failed; ++t, ++u) {
             const Tile tile = tiles[t];
             const Work w = work_of<PHASE>(prm.dev.mats[tile.matrix], prm.step);
             const uint32_t buf = u & 1, d = tmem + buf * S::BN;
@@ -361,92 +411,133 @@ __global__ void __launch_bounds__(NTHREADS, CG == 1 ? 2 : 1) product_kernel(cons
     } else {
         const int q = warp & 3, half = (warp - 2) >> 2;
         const uint32_t lane_base = (uint32_t)(32 * q) << 16;
-        float *buf = staging + (warp - 2) * (kPieceBytes / 4);
-        constexpr int PIECES = S::BN / 2 / 32;      // of a warp
-        uint32_t u = 0;
-        for (int t = first; t < n_tiles; t += stride, ++u) {
+        unsigned char *mine = staging + (warp - 2) * kStaging;
+        constexpr int COLS = S::BN / (S::NEPI / 4), PIECES = COLS / 64;      // of a warp
+        const bool read_lo = PHASE == kApply && prm.step < kExactSteps;
+        const bool write_lo = PHASE == kApply && prm.step + 1 < kExactSteps;
+        uint32_t u = 0, stores = 0;
+        for (int t = t_begin; t < t_end; ++t, ++u) {
             const Tile tile = tiles[t];
-            const Matrix mx = prm.dev.mats[tile.matrix];
+            const Matrix &mx = prm.dev.mats[tile.matrix];
             const Work w = work_of<PHASE>(mx, prm.step);
             const uint32_t ab = u & 1;
+            const int m0 = tile.tm * 128 * CG + 128 * rank + 32 * q;       // first row of this warp's pieces
+            const int c0 = tile.tn * S::BN + half * COLS;                  // and first column
+            const int rows = min(32, w.M - m0);
+            const CUtensorMap *maps = prm.dev.maps + (size_t)tile.matrix * kMaps;
+            // what the epilogue reads is on its way while the tile's MMAs run
+            uint32_t lo[4][8];
+            auto fetch_lo = [&](int n0) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) lo[i][e] = 0;
+                    if (lane < rows && n0 + 16 * i < mx.ldx) load16(mx.lo + (int64_t)(m0 + lane) * mx.ldx + n0 + 16 * i, lo[i]);
+                }
+            };
+            if (PHASE == kApply && read_lo) fetch_lo(c0);
+            Weights<T> weights;
+            if (PHASE == kLast && rows > 0 && c0 < w.N) weights.fetch(prm.out, mx, lane, m0, c0, rows, min(32, w.N - c0));
             bool ok = mbar_poll(d_full + ab, (u >> 1) & 1, abort_flag);
             if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
             tc_fence_after();
-            const int m0 = tile.tm * 128 * CG + 128 * rank + 32 * q;       // first row of this warp's pieces
-            const int rows = min(32, w.M - m0);
             // a tile wholly right of the diagonal stands for its mirror image too
-            const bool mirror = PHASE != kApply && tile.tn * S::BN >= (tile.tm + 1) * 128 * CG;
-#pragma unroll 1
+            const bool mirror = !APPLY && tile.tn * S::BN >= (tile.tm + 1) * 128 * CG;
+#pragma unroll
             for (int p = 0; p < PIECES; ++p) {
-                const int cl = half * (S::BN / 2) + p * 32, n0 = tile.tn * S::BN + cl;
-                if (n0 >= w.N) break;
-                float v[32];
-                tmem_ld32_wait(tmem + lane_base + ab * S::BN + cl, v);
-                if (rows <= 0) continue;
-                const int cols = min(32, w.N - n0);
-                if (PHASE == kApply) {
-                    stage_piece(buf, lane, v);
-                    if (prm.step < kSteps - 1) {
-                        // rows are padded to whole pieces: every lane stores.  X' = P X_hi + a X_lo.
-                        const int c = (lane & 15) * 2;
-                        const int64_t at = (int64_t)m0 * mx.ldx + n0 + c;
-                        __half *lo = mx.lo + at, *hi = mx.x[(prm.step + 1) & 1] + at;
-                        const bool read_lo = prm.step < kExactSteps, write_lo = prm.step + 1 < kExactSteps;
-#pragma unroll 8
-                        for (int r = lane >> 4; r < rows; r += 2) {
-                            float2 x = *reinterpret_cast<const float2 *>(buf + r * kPiecePitch + c);
-                            x.x *= 1.0f / kGramScale;
-                            x.y *= 1.0f / kGramScale;
-                            const int64_t o = (int64_t)r * mx.ldx;
-                            if (read_lo) {
-                                const float2 l = __half22float2(*reinterpret_cast<const __half2 *>(lo + o));
-                                x.x = __fmaf_rn(kA, l.x, x.x);
-                                x.y = __fmaf_rn(kA, l.y, x.y);
-                            }
-                            const __half2 h = __floats2half2_rn(x.x, x.y);
-                            *reinterpret_cast<__half2 *>(hi + o) = h;
-                            if (write_lo) {
-                                const float2 f = __half22float2(h);
-                                *reinterpret_cast<__half2 *>(lo + o) = __floats2half2_rn(x.x - f.x, x.y - f.y);
-                            }
+                const int n0 = c0 + p * 64;
+                float v[2][32];
+                tmem_ld32_wait(tmem + lane_base + ab * S::BN + half * COLS + p * 64, v[0]);
+                tmem_ld32_wait(tmem + lane_base + ab * S::BN + half * COLS + p * 64 + 32, v[1]);
+                if (p == PIECES - 1) {       // the accumulator is free
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) { if (CG == 2) mbar_arrive_cluster(in_leader(d_empty + ab)); else mbar_arrive(d_empty + ab); }
+                }
+                if (rows <= 0 || n0 >= w.N) continue;
+                if (PHASE == kLast) {
+                    float *buf = reinterpret_cast<float *>(mine);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int n = n0 + 32 * h;
+                        if (n < w.N) {
+                            stage_piece(buf, lane, v[h]);
+                            weights.finish(prm.out, mx, buf, lane);
+                            if (n + 32 < min(w.N, c0 + COLS)) weights.fetch(prm.out, mx, lane, m0, n + 32, rows, min(32, w.N - n - 32));
                         }
-                    } else {
-                        if (prm.out.dtype == GVQ_F32) write_result<float>(prm.out, mx, buf, lane, m0, n0, rows, cols);
-                        else if (prm.out.dtype == GVQ_BF16) write_result<__nv_bfloat16>(prm.out, mx, buf, lane, m0, n0, rows, cols);
-                        else write_result<__half>(prm.out, mx, buf, lane, m0, n0, rows, cols);
                     }
-                } else {
-                    // A = X X^T, or P = a I + b A + c A^2 (so that the last product is all of the step).  A is symmetric:
-                    // its transposed entries are read, a column of them along the warp.
-                    __half *dst = PHASE == kGram ? mx.gram : mx.poly;
-                    if (PHASE == kGram) {
-                        const float f = kGramScale / (mx.sx * mx.sx);
+                    continue;
+                }
+                auto store = [&](unsigned char *from, int map) {      // the staged piece, by one lane
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) {
+                        tma_store_2d(maps + map, n0, m0, from);
+                        bulk_commit_group();
+                    }
+                };
+                if (PHASE == kApply) {       // X' = P X_hi + a X_lo
+                    unsigned char *to = write_lo ? mine : mine + (stores++ & 1) * 4096;
+                    if (lane == 0) { if (write_lo) bulk_wait_group_read<0>(); else bulk_wait_group_read<1>(); }
+                    __syncwarp();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] *= f;
-                    } else {
-                        const __half *a = mx.gram + (int64_t)n0 * mx.ldr + m0 + lane;
-                        __half av[32];
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) av[i] = i < cols && lane < rows ? a[(int64_t)i * mx.ldr] : __half(0.0f);
+                    for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
-                            v[i] = __fmaf_rn(kB, __half2float(av[i]), v[i] * (kC / kGramScale));
-                            if (n0 + i == m0 + lane) v[i] += kA * kGramScale;
+                            v[h][i] *= 1.0f / kGramScale;
+                            if (read_lo) {
+                                const uint32_t two = lo[2 * h + (i >> 4)][(i & 15) >> 1];
+                                const __half l = __ushort_as_half((unsigned short)(i & 1 ? two >> 16 : two & 0xFFFFu));
+                                v[h][i] = __fmaf_rn(kA, __half2float(l), v[h][i]);
+                            }
                         }
+                    if (read_lo && p + 1 < PIECES) fetch_lo(n0 + 64);
+                    stage_swizzled16<__half>(to, lane, v[0], v[1]);
+                    store(to, kX0Out + ((prm.step + 1) & 1));
+                    if (write_lo) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) v[h][i] -= __half2float(__float2half_rn(v[h][i]));
+                        stage_swizzled16<__half>(mine + 4096, lane, v[0], v[1]);
+                        store(mine + 4096, kLoOut);
                     }
+                    continue;
+                }
+                // A = X X^T and b I + c A, whose product with A the next launch takes; then P = a I + A (b I + c A)
+                auto put = [&](__half *dst, int map) {
                     if (mirror) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (i < cols && lane < rows) dst[(int64_t)(n0 + i) * mx.ldr + m0 + lane] = __float2half_rn(v[i]);
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (n0 + 32 * h + i < w.N && lane < rows)
+                                    dst[(int64_t)(n0 + 32 * h + i) * mx.ldr + m0 + lane] = __float2half_rn(v[h][i]);
                     }
-                    stage_piece(buf, lane, v);
-                    store_piece(buf, lane, dst + (int64_t)m0 * mx.ldr + n0, mx.ldr, rows, cols);
-                }
+                    if (lane == 0) bulk_wait_group_read<1>();
+                    __syncwarp();
+                    unsigned char *to = mine + (stores++ & 1) * 4096;
+                    stage_swizzled16<__half>(to, lane, v[0], v[1]);
+                    store(to, map);
+                };
+                const float f = PHASE == kGram ? kGramScale / (mx.sx * mx.sx) : 1.0f / kGramScale;
+                const float diagonal = (PHASE == kGram ? kB : kA) * kGramScale;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[h][i] *= f;
+                if (PHASE == kGram) put(mx.gram, kGramOut);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        if (PHASE == kGram) v[h][i] *= kC;
+                        if (n0 + 32 * h + i == m0 + lane) v[h][i] += diagonal;
+                    }
+                if (PHASE == kGram) put(mx.factor, kFactorOut); else put(mx.poly, kPolyOut);
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) { if (CG == 2) mbar_arrive_cluster(in_leader(d_empty + ab)); else mbar_arrive(d_empty + ab); }
         }
+        if (lane == 0) bulk_wait_group_all();
     }
 
     if (failed) {
@@ -496,7 +587,7 @@ cudaError_t launch_start(cudaStream_t st, const Device &dev, const ElementArgs &
     return launch_chained(normalise_kernel, prm, dev.n_chunks, 256, 0, 1, st);
 }
 
-cudaError_t launch_product(cudaStream_t st, int num_sms, const Device &dev, Phase phase, int step, const OutputArgs *out,
+cudaError_t launch_product(cudaStream_t st, const Device &dev, Phase phase, int step, const OutputArgs *out,
                            int32_t *error_word, int wait_kcycles, int test_drop)
 {
     ProductParams prm;
@@ -506,14 +597,17 @@ cudaError_t launch_product(cudaStream_t st, int num_sms, const Device &dev, Phas
     prm.error_word = error_word;
     prm.wait_kcycles = wait_kcycles > 0 ? wait_kcycles : WAIT_KCYCLES_DEFAULT;
     prm.test_drop = test_drop;
-    const int n = phase == kApply ? dev.n_apply : dev.n_sym;
     auto launch = [&](auto pair, auto solo) {
-        return dev.pair ? launch_chained(pair, prm, 2 * min(n, num_sms / 2), NTHREADS, Shape<2>::SMEM, 2, st)
-                        : launch_chained(solo, prm, min(n, 2 * num_sms), NTHREADS, Shape<1>::SMEM, 1, st);
+        const int runs = phase == kApply ? dev.apply_runs : dev.sym_runs;
+        return dev.pair ? launch_chained(pair, prm, 2 * runs, Shape<2>::THREADS, Shape<2>::SMEM, 2, st)
+                        : launch_chained(solo, prm, runs, Shape<1>::THREADS, Shape<1>::SMEM, 1, st);
     };
     if (phase == kGram) return launch(product_kernel<kGram, 2>, product_kernel<kGram, 1>);
     if (phase == kPoly) return launch(product_kernel<kPoly, 2>, product_kernel<kPoly, 1>);
-    return launch(product_kernel<kApply, 2>, product_kernel<kApply, 1>);
+    if (step < kSteps - 1) return launch(product_kernel<kApply, 2>, product_kernel<kApply, 1>);
+    if (out->dtype == GVQ_F32) return launch(product_kernel<kLast, 2, float>, product_kernel<kLast, 1, float>);
+    if (out->dtype == GVQ_BF16) return launch(product_kernel<kLast, 2, __nv_bfloat16>, product_kernel<kLast, 1, __nv_bfloat16>);
+    return launch(product_kernel<kLast, 2, __half>, product_kernel<kLast, 1, __half>);
 }
 
 }  // namespace ortho

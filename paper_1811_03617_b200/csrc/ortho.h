@@ -27,21 +27,24 @@ struct Matrix {
     int32_t rows, cols, r, c, tall, ldx, ldr;
     int32_t chunk0, n_chunks;        // its chunks in the element-wise passes
     int64_t off;                     // in the flat buffers
-    __half *x[2], *lo, *gram, *poly; // X (two buffers, in turn), X's low halves, A, B; rows ldx or ldr entries apart
+    // X (two buffers, in turn), X's low halves; A, b I + c A, P; rows ldx or ldr entries apart
+    __half *x[2], *lo, *gram, *factor, *poly;
     float sx;                        // scale of X in half precision
     float scale;                     // of the update
 };
 struct Tile { int32_t matrix, tm, tn; };
 struct Chunk { int32_t matrix, index; };
 
-enum Phase { kGram = 0, kPoly = 1, kApply = 2 };
-enum Map { kX0 = 0, kX1 = 1, kGramMap = 2, kPolyMap = 3, kMaps = 4 };
+enum Phase { kGram = 0, kPoly = 1, kApply = 2, kLast = 3 };
+// Tensor maps of a matrix: operands (boxes of 64 x 64) and results (64 columns x 32 rows)
+enum Map { kX0 = 0, kX1, kGramMap, kFactorMap, kPolyMap, kX0Out, kX1Out, kLoOut, kGramOut, kFactorOut, kPolyOut, kMaps };
 
 struct Device {
     const Matrix *mats;
     const CUtensorMap *maps;         // [matrices][kMaps]
-    const Tile *sym_tiles, *apply_tiles;
-    int n_sym, n_apply;
+    const Tile *sym_tiles, *apply_tiles;         // in runs, one for each CTA (or pair)
+    const int32_t *sym_start, *apply_start;      // [runs + 1]
+    int sym_runs, apply_runs;
     int pair;                        // which tiling the tiles are of
     const Chunk *chunks;
     int n_chunks;
@@ -64,7 +67,7 @@ struct OutputArgs {
 };
 
 cudaError_t launch_start(cudaStream_t st, const Device &dev, const ElementArgs &a);
-cudaError_t launch_product(cudaStream_t st, int num_sms, const Device &dev, Phase phase, int step, const OutputArgs *out,
+cudaError_t launch_product(cudaStream_t st, const Device &dev, Phase phase, int step, const OutputArgs *out,
                            int32_t *error_word, int wait_kcycles, int test_drop);
 
 }  // namespace ortho

@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <functional>
 #include <new>
 
 #include "api_util.h"
@@ -12,6 +13,7 @@ using namespace gvq::ortho;
 
 struct gvq_ortho {
     gvq_ctx *ctx = nullptr;
+    int device = 0;              // (destroying the plan does not touch the context, which may be gone)
     Device dev{};
     void *tables = nullptr;      // one device allocation: matrices, tensor maps, tiles, chunks, partial sums
 };
@@ -19,6 +21,7 @@ struct gvq_ortho {
 namespace {
 
 constexpr size_t kAlign = 256;
+constexpr int kTileCost = 3;      // what a tile costs beyond its contraction, in stages of 64 steps
 constexpr int kPairTiles = 148;   // fewer 256 x 256 tiles than this: 128 x 64 tiles
 size_t up(size_t n) { return (n + kAlign - 1) & ~(kAlign - 1); }
 int up32(int n) { return (n + 31) & ~31; }     // rows of the work arrays: whole pieces of 32 entries
@@ -52,20 +55,47 @@ gvq_status lay_out(int n_layers, const int64_t *off, const int64_t *len, const i
             return p;
         };
         const size_t nx = (size_t)m.rows * m.ldx, nr = (size_t)m.r * m.ldr;
-        m.x[0] = take(nx); m.x[1] = take(nx); m.lo = take(nx); m.gram = take(nr); m.poly = take(nr);
+        m.x[0] = take(nx); m.x[1] = take(nx); m.lo = take(nx); m.gram = take(nr); m.factor = take(nr); m.poly = take(nr);
         out.mats.push_back(m);
     }
     return GVQ_OK;
 }
 
-bool encode(EncodeTiledFn enc, CUtensorMap *map, void *p, int rows, int cols, int ld)
+bool encode(EncodeTiledFn enc, CUtensorMap *map, void *p, int rows, int cols, int ld, int box_rows)
 {
     cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
     cuuint64_t strides[1] = {(cuuint64_t)ld * sizeof(__half)};
-    cuuint32_t box[2] = {64, 64};
+    cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
     cuuint32_t estr[2] = {1, 1};
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, p, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Deals tiles to at most `units` CTAs so that their costs come out even (longest first, to whoever has least), and puts
+// each one's tiles together, a matrix's next to each other.  Returns where the runs start.
+template <typename F>
+std::vector<int32_t> deal(std::vector<Tile> &tiles, int units, F contraction)
+{
+    auto cost = [&](const Tile &t) { return (contraction(t) + 63) / 64 + kTileCost; };
+    std::stable_sort(tiles.begin(), tiles.end(), [&](const Tile &a, const Tile &b) { return cost(a) > cost(b); });
+    const int runs = (int)std::min<size_t>(units, tiles.size());
+    std::vector<std::vector<Tile>> run(runs);
+    std::vector<std::pair<int64_t, int>> heap;       // (load, run), least on top
+    for (int i = 0; i < runs; ++i) heap.push_back({0, i});
+    const auto more = std::greater<std::pair<int64_t, int>>();
+    for (const Tile &t : tiles) {
+        std::pop_heap(heap.begin(), heap.end(), more);
+        run[heap.back().second].push_back(t);
+        heap.back().first += cost(t);
+        std::push_heap(heap.begin(), heap.end(), more);
+    }
+    std::vector<int32_t> start{0};
+    tiles.clear();
+    for (auto &r : run) {
+        tiles.insert(tiles.end(), r.begin(), r.end());
+        start.push_back((int32_t)tiles.size());
+    }
+    return start;
 }
 
 // The five steps from X to the result.
@@ -74,7 +104,7 @@ gvq_status products(gvq_ortho *p, const OutputArgs &out)
     gvq_ctx *ctx = p->ctx;
     for (int s = 0; s < kSteps; ++s)
         for (Phase ph : {kGram, kPoly, kApply})
-            GVQ_CUDA(ctx, launch_product(ctx->stream, ctx->num_sms, p->dev, ph, s, &out, ctx->error_word, ctx->wait_kcycles,
+            GVQ_CUDA(ctx, launch_product(ctx->stream, p->dev, ph, s, &out, ctx->error_word, ctx->wait_kcycles,
                                          ctx->drop_last_load));
     return GVQ_OK;
 }
@@ -118,9 +148,14 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
         for (int i = 0; i < n; ++i) {
             Matrix &m = sz.mats[i];
             CUtensorMap *mp = &maps[(size_t)i * kMaps];
-            EncodeTiledFn enc = (EncodeTiledFn)ctx->encode_fn;
-            if (!encode(enc, mp + kX0, m.x[0], m.rows, m.cols, m.ldx) || !encode(enc, mp + kX1, m.x[1], m.rows, m.cols, m.ldx) ||
-                !encode(enc, mp + kGramMap, m.gram, m.r, m.r, m.ldr) || !encode(enc, mp + kPolyMap, m.poly, m.r, m.r, m.ldr))
+            auto map = [&](int which, __half *p, int box_rows, bool square) {
+                return encode((EncodeTiledFn)ctx->encode_fn, mp + which, p, square ? m.r : m.rows, square ? m.r : m.cols,
+                              square ? m.ldr : m.ldx, box_rows);
+            };
+            if (!map(kX0, m.x[0], 64, false) || !map(kX1, m.x[1], 64, false) || !map(kGramMap, m.gram, 64, true) ||
+                !map(kFactorMap, m.factor, 64, true) || !map(kPolyMap, m.poly, 64, true) || !map(kX0Out, m.x[0], 32, false) ||
+                !map(kX1Out, m.x[1], 32, false) || !map(kLoOut, m.lo, 32, false) || !map(kGramOut, m.gram, 32, true) ||
+                !map(kFactorOut, m.factor, 32, true) || !map(kPolyOut, m.poly, 32, true))
                 return GVQ_ERR_CUDA;
             m.chunk0 = (int)chunks.size();
             m.n_chunks = (int)(((int64_t)m.rows * m.cols + kChunk - 1) / kChunk);
@@ -143,21 +178,26 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
             }
             if (pair && (int)apply.size() >= kPairTiles) break;
         }
-        // longest contraction first: the CTAs take the tiles in turn, and the short ones level the end
-        std::stable_sort(sym.begin(), sym.end(), [&](const Tile &a, const Tile &b) { return sz.mats[a.matrix].c > sz.mats[b.matrix].c; });
-        std::stable_sort(apply.begin(), apply.end(), [&](const Tile &a, const Tile &b) { return sz.mats[a.matrix].r > sz.mats[b.matrix].r; });
+        const int units = pair ? ctx->num_sms / 2 : 2 * ctx->num_sms;
+        // (A's contraction is c long, its polynomial's r: one order serves both)
+        const std::vector<int32_t> sym_start = deal(sym, units, [&](const Tile &t) { return sz.mats[t.matrix].c; });
+        const std::vector<int32_t> apply_start = deal(apply, units, [&](const Tile &t) { return sz.mats[t.matrix].r; });
 
         gvq_ortho *p = new gvq_ortho();
         p->ctx = ctx;
+        p->device = ctx->device;
         const size_t b_m = up(sizeof(Matrix) * n), b_t = up(sizeof(CUtensorMap) * maps.size()), b_s = up(sizeof(Tile) * sym.size()),
-                     b_a = up(sizeof(Tile) * apply.size()), b_c = up(sizeof(Chunk) * chunks.size()), b_p = up(sizeof(float) * chunks.size());
-        std::vector<unsigned char> image(b_m + b_t + b_s + b_a + b_c);
+                     b_a = up(sizeof(Tile) * apply.size()), b_c = up(sizeof(Chunk) * chunks.size()), b_ss = up(sizeof(int32_t) * sym_start.size()), b_as = up(sizeof(int32_t) * apply_start.size()),
+                     b_p = up(sizeof(float) * chunks.size());
+        std::vector<unsigned char> image(b_m + b_t + b_s + b_a + b_c + b_ss + b_as);
         auto put = [&](size_t at, const void *src, size_t bytes) { if (bytes) std::memcpy(image.data() + at, src, bytes); };
         put(0, sz.mats.data(), sizeof(Matrix) * n);
         put(b_m, maps.data(), sizeof(CUtensorMap) * maps.size());
         put(b_m + b_t, sym.data(), sizeof(Tile) * sym.size());
         put(b_m + b_t + b_s, apply.data(), sizeof(Tile) * apply.size());
         put(b_m + b_t + b_s + b_a, chunks.data(), sizeof(Chunk) * chunks.size());
+        put(b_m + b_t + b_s + b_a + b_c, sym_start.data(), sizeof(int32_t) * sym_start.size());
+        put(b_m + b_t + b_s + b_a + b_c + b_ss, apply_start.data(), sizeof(int32_t) * apply_start.size());
         DeviceGuard guard(ctx->device);
         cudaError_t e = cudaMalloc(&p->tables, image.size() + b_p + kAlign);
         if (e == cudaSuccess) e = cudaMemcpy(p->tables, image.data(), image.size(), cudaMemcpyHostToDevice);
@@ -175,7 +215,9 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
         d.chunks = reinterpret_cast<Chunk *>(t + b_m + b_t + b_s + b_a);
         d.partial = reinterpret_cast<float *>(t + image.size());
         d.pair = pair;
-        d.n_sym = (int)sym.size(); d.n_apply = (int)apply.size(); d.n_chunks = (int)chunks.size();
+        d.sym_start = reinterpret_cast<int32_t *>(t + b_m + b_t + b_s + b_a + b_c);
+        d.apply_start = reinterpret_cast<int32_t *>(t + b_m + b_t + b_s + b_a + b_c + b_ss);
+        d.sym_runs = (int)sym_start.size() - 1; d.apply_runs = (int)apply_start.size() - 1; d.n_chunks = (int)chunks.size();
         *out = p;
         return GVQ_OK;
     } catch (const std::bad_alloc &) {
@@ -186,7 +228,7 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
 gvq_status gvq_ortho_destroy(gvq_ortho *p)
 {
     if (!p) return GVQ_OK;
-    DeviceGuard guard(p->ctx->device);
+    DeviceGuard guard(p->device);
     if (p->tables) cudaFree(p->tables);
     delete p;
     return GVQ_OK;

@@ -89,6 +89,38 @@ def test_orthogonalize_all_shapes_in_one_call(kind):
         assert torch.equal(out[at], again[at])               # the same bits every time
 
 
+@pytest.mark.parametrize("dtype", list(DT))
+def test_many_large_matrices(dtype):
+    """Enough 256 x 256 tiles for pairs of CTAs: wide, tall and square matrices with ragged edges in one plan."""
+    shapes = [(1030, 2100)] * 2 + [(1500, 700)] * 2 + [(900, 900)] * 3 + [(24, 3000), (2999, 40), (257, 1030)]
+    shapes += [(1285, 1281)] * 2 + [(64, 576), (1024, 1024), (512, 4608)]
+    w, plan = make(shapes)
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    g = torch.randn(w.M, generator=gen, device="cuda")
+    for i, ((m, n), o) in enumerate(zip(shapes, w.layer_off)):
+        if i % 2:       # a few strong directions
+            g[o:o + m * n] = (torch.randn(m, 6, generator=gen, device="cuda") @ torch.randn(6, n, generator=gen, device="cuda")).view(-1) + 0.1 * g[o:o + m * n]
+    out = torch.full((w.M,), 7.0, dtype=DT[dtype], device="cuda")
+    plan.orthogonalize(g, out)
+    plan.ctx.device_status()
+    mo = torch.zeros(w.M, device="cuda")
+    wt = torch.full((w.M,), 2.0, dtype=DT[dtype], device="cuda")
+    plan.step(g, mo, wt, lr=0.5, weight_decay=0.5, beta=0.5, nesterov=False)
+    rest = torch.ones(w.M, dtype=torch.bool, device="cuda")
+    for (m, n), o in zip(shapes, w.layer_off):
+        sl = slice(o, o + m * n)
+        rest[sl] = False
+        want = exact(g[sl].view(m, n)).reshape(-1)
+        err = float((out[sl].double() - want).norm() / want.norm())
+        assert err <= bar(m, n) + 2 * HALF_ULP[DT[dtype]], (m, n, err)
+        s = math.sqrt(max(1.0, m / n))
+        new = 0.75 * 2.0 - 0.5 * s * want
+        err = float((wt[sl].double() - new).norm())
+        assert err <= 0.5 * s * float(want.norm()) * bar(m, n) + float(new.norm()) * (2 * HALF_ULP[DT[dtype]] + 2.0 ** -22), (m, n)
+    assert bool((out[rest] == 7.0).all()) and bool((wt[rest] == 2.0).all())
+    assert torch.equal(mo[~rest], g[~rest])
+
+
 def test_singular_values_end_near_one():
     shapes = [(192, 320), (700, 96)]
     w, plan = make(shapes)
@@ -218,6 +250,17 @@ def test_a_wait_that_runs_out_is_reported_and_the_plan_recovers():
     plan.orthogonalize(g, out)
     plan.ctx.device_status()
     assert torch.equal(out[:120000], good)
+
+
+def test_a_plan_can_be_destroyed_after_its_context():
+    """As garbage collection may order it."""
+    w, plan = make([(16, 32)])
+    plan.ctx.close()
+    plan.close()
+    _, plan = make([(16, 32)])
+    out = torch.empty(w.M, device="cuda")
+    plan.orthogonalize(torch.randn(w.M, device="cuda"), out)
+    plan.ctx.device_status()
 
 
 def test_refusals():
