@@ -8,7 +8,8 @@
 // with X^T X and X B; the tensor core reads an operand K-major or MN-major, so X is one row-major array for all of:
 //     wide   A = X X^T   both operands K-major       X' = B X   B K-major (symmetric), X MN-major
 //     tall   A = X^T X   both operands MN-major      X' = X B   both K-major
-// A and B are symmetric: only tiles that touch or lie above the diagonal are computed, and stored twice.
+// A, b I + c A and P are symmetric: only tiles that touch or lie right of the diagonal are computed and stored; an operand
+// tile left of it is read as the transposed tile, in the other major.
 //
 // Precision.  The products take half-precision operands (11 significant bits; bf16 would leave 8) and accumulate in
 // fp32.  Powers of two keep the operands in range.  X in half precision alone would lose what matters most: rounding X
@@ -189,6 +190,7 @@ constexpr uint32_t kStaging = 8192;      // of an epilogue warp: two pieces of 3
 
 template <int CG> struct Shape {
     static constexpr int BN = CG == 2 ? kPairN : kSoloN;                     // columns of a tile
+    static constexpr int BLOCK = 128 * CG;                                   // of the diagonal of a symmetric result
     static constexpr int NB = CG == 2 ? 2 : BN / 64;                        // boxes of B a CTA loads
     static constexpr uint32_t A_BYTES = 2 * BOX, STAGE = A_BYTES + NB * BOX;
     static constexpr int STAGES = CG == 2 ? 5 : 3;
@@ -209,15 +211,17 @@ struct ProductParams {
 struct Work {
     int M, N, K;         // extents of the whole product
     int a_map, b_map;
-    bool a_mn, b_mn;
+    bool a_mn, b_mn;     // MN-major operands
+    bool a_sym, b_sym;   // symmetric ones, stored on and right of the diagonal
 };
 template <int PHASE>
 __device__ __forceinline__ Work work_of(const Matrix &m, int step)
 {
     const int x = step & 1;
-    if (PHASE == kGram) return {m.r, m.r, m.c, x, x, m.tall != 0, m.tall != 0};
-    if (PHASE == kPoly) return {m.r, m.r, m.r, kGramMap, kFactorMap, false, false};
-    return m.tall ? Work{m.rows, m.cols, m.r, x, kPolyMap, false, false} : Work{m.rows, m.cols, m.r, kPolyMap, x, false, true};
+    if (PHASE == kGram) return {m.r, m.r, m.c, x, x, m.tall != 0, m.tall != 0, false, false};
+    if (PHASE == kPoly) return {m.r, m.r, m.r, kGramMap, kFactorMap, false, false, true, true};
+    return m.tall ? Work{m.rows, m.cols, m.r, x, kPolyMap, false, false, false, true}
+                  : Work{m.rows, m.cols, m.r, kPolyMap, x, false, true, true, false};
 }
 
 // The last step's result, 32 x 32 entries at a time: out = X, or w = decay w - step scale X.  A lane has a column, or two
@@ -296,6 +300,7 @@ template <typename T> struct Weights {
     }
 };
 
+__device__ __forceinline__ void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 // 16 halves of a row (32 bytes, aligned)
 __device__ __forceinline__ void load16(const __half *p, uint32_t (&w)[8])
 {
@@ -351,6 +356,8 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
                 const int half_n = CG == 2 ? min(S::BN, (w.N - tile.tn * S::BN + 15) / 16 * 16) / 2 : 0;
                 const int m0 = tile.tm * 128 * CG + 128 * rank, n0 = tile.tn * S::BN + half_n * rank;
                 const int n_stages = (w.K + KS - 1) / KS;
+                // steps of the contraction left of the diagonal's block of a symmetric operand's rows
+                const int a_left = w.a_sym ? m0 / S::BLOCK * S::BLOCK : 0, b_left = w.b_sym ? tile.tn * S::BN / S::BLOCK * S::BLOCK : 0;
                 for (int st = 0; st < n_stages; ++st, ++c) {
                     const uint32_t s = c % S::STAGES;
                     if (!mbar_poll(empty + s, ((c / S::STAGES) & 1) ^ 1, abort_flag)) { failed = true; break; }
@@ -364,9 +371,9 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
                         else tma_load_2d(to, map, mn ? at : k, mn ? k : at, full + s);
                     };
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) load(dst + i * BOX, ma, w.a_mn, m0 + 64 * i);
+                    for (int i = 0; i < 2; ++i) load(dst + i * BOX, ma, w.a_mn || k < a_left, m0 + 64 * i);
 #pragma unroll
-                    for (int i = 0; i < S::NB; ++i) load(dst + S::A_BYTES + i * BOX, mb, w.b_mn, n0 + 64 * i);
+                    for (int i = 0; i < S::NB; ++i) load(dst + S::A_BYTES + i * BOX, mb, w.b_mn || k < b_left, n0 + 64 * i);
                 }
             }
             if (failed && rank == 0) {   // give the copies already in flight a bounded chance to land before the CTA exits
@@ -382,7 +389,8 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
             const Work w = work_of<PHASE>(prm.dev.mats[tile.matrix], prm.step);
             const uint32_t buf = u & 1, d = tmem + buf * S::BN;
             const int n = min(S::BN, (w.N - tile.tn * S::BN + 15) / 16 * 16);
-            const uint32_t idesc = make_idesc_f16(128 * CG, n, w.a_mn, w.b_mn);
+            const int a_left = w.a_sym ? tile.tm * 128 * CG / S::BLOCK * S::BLOCK : 0;
+            const int b_left = w.b_sym ? tile.tn * S::BN / S::BLOCK * S::BLOCK : 0;
             const int n_stages = (w.K + KS - 1) / KS;
             bool ok = mbar_poll(d_empty + buf, ((u >> 1) & 1) ^ 1, abort_flag);
             if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
@@ -393,10 +401,12 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
                 if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
                 tc_fence_after();
                 const uint32_t base = smem_u32(smem + (size_t)s * S::STAGE);
-                const uint64_t da = w.a_mn ? make_mn_desc(base, BOX) : make_b_desc(base);
-                const uint64_t db = w.b_mn ? make_mn_desc(base + S::A_BYTES, BOX) : make_b_desc(base + S::A_BYTES);
+                const bool a_mn = w.a_mn || st * KS < a_left, b_mn = w.b_mn || st * KS < b_left;
+                const uint32_t idesc = make_idesc_f16(128 * CG, n, a_mn, b_mn);
+                const uint64_t da = a_mn ? make_mn_desc(base, BOX) : make_b_desc(base);
+                const uint64_t db = b_mn ? make_mn_desc(base + S::A_BYTES, BOX) : make_b_desc(base + S::A_BYTES);
                 // 16 steps of the contraction: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major box
-                const uint32_t ia = w.a_mn ? 16 * 128 / 16 : 2, ib = w.b_mn ? 16 * 128 / 16 : 2;
+                const uint32_t ia = a_mn ? 16 * 128 / 16 : 2, ib = b_mn ? 16 * 128 / 16 : 2;
                 const int n_mma = min(4, (w.K - st * KS + 15) / 16);
                 if (elect_one()) {
 #pragma unroll
@@ -435,14 +445,21 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
                     if (lane < rows && n0 + 16 * i < mx.ldx) load16(mx.lo + (int64_t)(m0 + lane) * mx.ldx + n0 + 16 * i, lo[i]);
                 }
             };
-            if (PHASE == kApply && read_lo) fetch_lo(c0);
+            if (PHASE == kApply && read_lo) {
+                fetch_lo(c0);
+                if (PIECES > 1 && lane < rows && c0 + 64 < mx.ldx) prefetch_l2(mx.lo + (int64_t)(m0 + lane) * mx.ldx + c0 + 64);
+            }
             Weights<T> weights;
+            if (PHASE == kLast && prm.out.update && lane < rows) {
+                const T *row = static_cast<const T *>(prm.out.ptr) + mx.off + (int64_t)(m0 + lane) * mx.cols;
+#pragma unroll
+                for (int c = 0; c < COLS; c += 128 / (int)sizeof(T))
+                    if (c0 + c < w.N) prefetch_l2(row + c0 + c);
+            }
             if (PHASE == kLast && rows > 0 && c0 < w.N) weights.fetch(prm.out, mx, lane, m0, c0, rows, min(32, w.N - c0));
             bool ok = mbar_poll(d_full + ab, (u >> 1) & 1, abort_flag);
             if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
             tc_fence_after();
-            // a tile wholly right of the diagonal stands for its mirror image too
-            const bool mirror = !APPLY && tile.tn * S::BN >= (tile.tm + 1) * 128 * CG;
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) {
                 const int n0 = c0 + p * 64;
@@ -505,15 +522,7 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
                     continue;
                 }
                 // A = X X^T and b I + c A, whose product with A the next launch takes; then P = a I + A (b I + c A)
-                auto put = [&](__half *dst, int map) {
-                    if (mirror) {
-#pragma unroll
-                        for (int h = 0; h < 2; ++h)
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (n0 + 32 * h + i < w.N && lane < rows)
-                                    dst[(int64_t)(n0 + 32 * h + i) * mx.ldr + m0 + lane] = __float2half_rn(v[h][i]);
-                    }
+                auto put = [&](int map) {
                     if (lane == 0) bulk_wait_group_read<1>();
                     __syncwarp();
                     unsigned char *to = mine + (stores++ & 1) * 4096;
@@ -526,7 +535,7 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[h][i] *= f;
-                if (PHASE == kGram) put(mx.gram, kGramOut);
+                if (PHASE == kGram) put(kGramOut);
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -534,7 +543,7 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
                         if (PHASE == kGram) v[h][i] *= kC;
                         if (n0 + 32 * h + i == m0 + lane) v[h][i] += diagonal;
                     }
-                if (PHASE == kGram) put(mx.factor, kFactorOut); else put(mx.poly, kPolyOut);
+                if (PHASE == kGram) put(kFactorOut); else put(kPolyOut);
             }
         }
         if (lane == 0) bulk_wait_group_all();
