@@ -283,7 +283,7 @@ template <typename T> struct Weights {
                         x.y = __fmaf_rn(-k, x.y, o.decay * to_f(entry(w[i] >> 16)));
                     }
                     if constexpr (sizeof(T) == 2)
-                        *reinterpret_cast<uint32_t *>(d + (int64_t)2 * i * mx.cols) = pack2(from_f<T>(x.x), from_f<T>(x.y));
+                        *reinterpret_cast<uint32_t *>(d + (int64_t)2 * i * mx.cols) = pack2<T>(x.x, x.y);
                 }
             }
         } else if (lane < cols) {
@@ -425,44 +425,66 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
         constexpr int COLS = S::BN / (S::NEPI / 4), PIECES = COLS / 64;      // of a warp
         const bool read_lo = PHASE == kApply && prm.step < kExactSteps;
         const bool write_lo = PHASE == kApply && prm.step + 1 < kExactSteps;
-        uint32_t u = 0, stores = 0;
-        for (int t = t_begin; t < t_end; ++t, ++u) {
+        // A tile as this warp sees it: its first row and column, its rows inside the product.
+        struct Place {
+            const Matrix *mx;
+            int m0, c0, rows, N;
+        };
+        auto place = [&](int t) {
             const Tile tile = tiles[t];
-            const Matrix &mx = prm.dev.mats[tile.matrix];
-            const Work w = work_of<PHASE>(mx, prm.step);
-            const uint32_t ab = u & 1;
-            const int m0 = tile.tm * 128 * CG + 128 * rank + 32 * q;       // first row of this warp's pieces
-            const int c0 = tile.tn * S::BN + half * COLS;                  // and first column
-            const int rows = min(32, w.M - m0);
-            const CUtensorMap *maps = prm.dev.maps + (size_t)tile.matrix * kMaps;
-            // what the epilogue reads is on its way while the tile's MMAs run
-            uint32_t lo[4][8];
-            auto fetch_lo = [&](int n0) {
+            const Matrix *mx = prm.dev.mats + tile.matrix;
+            const Work w = work_of<PHASE>(*mx, prm.step);
+            const int m0 = tile.tm * 128 * CG + 128 * rank + 32 * q;
+            return Place{mx, m0, tile.tn * S::BN + half * COLS, min(32, w.M - m0), w.N};
+        };
+        // What the epilogue reads besides the accumulator is asked for a piece ahead, across tiles, and a tile ahead into L2.
+        uint32_t lo[4][8];
+        auto fetch_lo = [&](const Place &at, int n0) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 4; ++i) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) lo[i][e] = 0;
-                    if (lane < rows && n0 + 16 * i < mx.ldx) load16(mx.lo + (int64_t)(m0 + lane) * mx.ldx + n0 + 16 * i, lo[i]);
-                }
-            };
-            if (PHASE == kApply && read_lo) {
-                fetch_lo(c0);
-                if (PIECES > 1 && lane < rows && c0 + 64 < mx.ldx) prefetch_l2(mx.lo + (int64_t)(m0 + lane) * mx.ldx + c0 + 64);
+                for (int e = 0; e < 8; ++e) lo[i][e] = 0;
+                if (lane < at.rows && n0 + 16 * i < at.mx->ldx)
+                    load16(at.mx->lo + (int64_t)(at.m0 + lane) * at.mx->ldx + n0 + 16 * i, lo[i]);
             }
-            Weights<T> weights;
-            if (PHASE == kLast && prm.out.update && lane < rows) {
-                const T *row = static_cast<const T *>(prm.out.ptr) + mx.off + (int64_t)(m0 + lane) * mx.cols;
+        };
+        Weights<T> weights;
+        auto fetch_weights = [&](const Place &at, int n) {
+            weights.fetch(prm.out, *at.mx, lane, at.m0, n, max(at.rows, 0), max(0, min(32, at.N - n)));
+        };
+        auto look_ahead = [&](const Place &at) {
+            if (lane >= at.rows) return;
+            if (PHASE == kApply && read_lo) {
+                const __half *row = at.mx->lo + (int64_t)(at.m0 + lane) * at.mx->ldx;
+#pragma unroll
+                for (int c = 0; c < COLS; c += 64)
+                    if (at.c0 + c < at.mx->ldx) prefetch_l2(row + at.c0 + c);
+            }
+            if (PHASE == kLast && prm.out.update) {
+                const T *row = static_cast<const T *>(prm.out.ptr) + at.mx->off + (int64_t)(at.m0 + lane) * at.mx->cols;
 #pragma unroll
                 for (int c = 0; c < COLS; c += 128 / (int)sizeof(T))
-                    if (c0 + c < w.N) prefetch_l2(row + c0 + c);
+                    if (at.c0 + c < at.N) prefetch_l2(row + at.c0 + c);
             }
-            if (PHASE == kLast && rows > 0 && c0 < w.N) weights.fetch(prm.out, mx, lane, m0, c0, rows, min(32, w.N - c0));
+        };
+        Place here = place(t_begin);
+        if (PHASE == kApply && read_lo) fetch_lo(here, here.c0);
+        if (PHASE == kLast) fetch_weights(here, here.c0);
+        uint32_t u = 0, stores = 0;
+        for (int t = t_begin; t < t_end; ++t, ++u) {
+            const Place next = place(min(t + 1, t_end - 1));
+            const Matrix &mx = *here.mx;
+            const int m0 = here.m0, c0 = here.c0, rows = here.rows;
+            const CUtensorMap *maps = prm.dev.maps + (size_t)tiles[t].matrix * kMaps;
+            const uint32_t ab = u & 1;
+            if (APPLY && t + 1 < t_end) look_ahead(next);
             bool ok = mbar_poll(d_full + ab, (u >> 1) & 1, abort_flag);
             if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
             tc_fence_after();
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) {
                 const int n0 = c0 + p * 64;
+                const bool live = rows > 0 && n0 < here.N;
                 float v[2][32];
                 tmem_ld32_wait(tmem + lane_base + ab * S::BN + half * COLS + p * 64, v[0]);
                 tmem_ld32_wait(tmem + lane_base + ab * S::BN + half * COLS + p * 64 + 32, v[1]);
@@ -471,20 +493,38 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
                     __syncwarp();
                     if (lane == 0) { if (CG == 2) mbar_arrive_cluster(in_leader(d_empty + ab)); else mbar_arrive(d_empty + ab); }
                 }
-                if (rows <= 0 || n0 >= w.N) continue;
                 if (PHASE == kLast) {
                     float *buf = reinterpret_cast<float *>(mine);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const int n = n0 + 32 * h;
-                        if (n < w.N) {
+                        if (live && n0 + 32 * h < here.N) {
                             stage_piece(buf, lane, v[h]);
                             weights.finish(prm.out, mx, buf, lane);
-                            if (n + 32 < min(w.N, c0 + COLS)) weights.fetch(prm.out, mx, lane, m0, n + 32, rows, min(32, w.N - n - 32));
                         }
+                        if (p * 64 + h * 32 + 32 < COLS) fetch_weights(here, n0 + 32 * h + 32);
+                        else if (t + 1 < t_end) fetch_weights(next, next.c0);
                     }
                     continue;
                 }
+                if (PHASE == kApply) {       // X' = P X_hi + a X_lo
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            v[h][i] *= 1.0f / kGramScale;
+                            v[h][i + 1] *= 1.0f / kGramScale;
+                            if (read_lo) {
+                                const float2 l = unpack_half2(lo[2 * h + (i >> 4)][(i & 15) >> 1]);
+                                v[h][i] = __fmaf_rn(kA, l.x, v[h][i]);
+                                v[h][i + 1] = __fmaf_rn(kA, l.y, v[h][i + 1]);
+                            }
+                        }
+                    if (read_lo) {
+                        if (p + 1 < PIECES) fetch_lo(here, n0 + 64);
+                        else if (t + 1 < t_end) fetch_lo(next, next.c0);
+                    }
+                }
+                if (!live) continue;
                 auto store = [&](unsigned char *from, int map) {      // the staged piece, by one lane
                     fence_proxy_async();
                     __syncwarp();
@@ -493,39 +533,33 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
                         bulk_commit_group();
                     }
                 };
-                if (PHASE == kApply) {       // X' = P X_hi + a X_lo
-                    unsigned char *to = write_lo ? mine : mine + (stores++ & 1) * 4096;
-                    if (lane == 0) { if (write_lo) bulk_wait_group_read<0>(); else bulk_wait_group_read<1>(); }
+                auto room = [&]() {      // one of the warp's two staging areas, once its last store has read it
+                    if (lane == 0) bulk_wait_group_read<1>();
                     __syncwarp();
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            v[h][i] *= 1.0f / kGramScale;
-                            if (read_lo) {
-                                const uint32_t two = lo[2 * h + (i >> 4)][(i & 15) >> 1];
-                                const __half l = __ushort_as_half((unsigned short)(i & 1 ? two >> 16 : two & 0xFFFFu));
-                                v[h][i] = __fmaf_rn(kA, __half2float(l), v[h][i]);
-                            }
-                        }
-                    if (read_lo && p + 1 < PIECES) fetch_lo(n0 + 64);
+                    return mine + (stores++ & 1) * 4096;
+                };
+                if (PHASE == kApply) {
+                    unsigned char *to = room();
                     stage_swizzled16<__half>(to, lane, v[0], v[1]);
                     store(to, kX0Out + ((prm.step + 1) & 1));
                     if (write_lo) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h)
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) v[h][i] -= __half2float(__float2half_rn(v[h][i]));
-                        stage_swizzled16<__half>(mine + 4096, lane, v[0], v[1]);
-                        store(mine + 4096, kLoOut);
+                            for (int i = 0; i < 32; i += 2) {
+                                const float2 f = unpack_half2(pack2<__half>(v[h][i], v[h][i + 1]));
+                                v[h][i] -= f.x;
+                                v[h][i + 1] -= f.y;
+                            }
+                        to = room();
+                        stage_swizzled16<__half>(to, lane, v[0], v[1]);
+                        store(to, kLoOut);
                     }
                     continue;
                 }
                 // A = X X^T and b I + c A, whose product with A the next launch takes; then P = a I + A (b I + c A)
                 auto put = [&](int map) {
-                    if (lane == 0) bulk_wait_group_read<1>();
-                    __syncwarp();
-                    unsigned char *to = mine + (stores++ & 1) * 4096;
+                    unsigned char *to = room();
                     stage_swizzled16<__half>(to, lane, v[0], v[1]);
                     store(to, map);
                 };
@@ -545,6 +579,7 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
                     }
                 if (PHASE == kGram) put(kFactorOut); else put(kPolyOut);
             }
+            here = next;
         }
         if (lane == 0) bulk_wait_group_all();
     }

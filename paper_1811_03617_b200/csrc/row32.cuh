@@ -17,10 +17,27 @@ template <typename T> __device__ __forceinline__ float to_f(T x);
 template <> __device__ __forceinline__ float to_f(float x) { return x; }
 template <> __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
 template <> __device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
-__device__ __forceinline__ uint32_t pack2(__half a, __half b) { return (uint32_t)__half_as_ushort(a) | (uint32_t)__half_as_ushort(b) << 16; }
-__device__ __forceinline__ uint32_t pack2(__nv_bfloat16 a, __nv_bfloat16 b)
+// Two entries of a 16-bit type in a word, rounded by one conversion; and back.
+template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b);
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b)
 {
-    return (uint32_t)__bfloat16_as_ushort(a) | (uint32_t)__bfloat16_as_ushort(b) << 16;
+    const __half2 h = __floats2half2_rn(a, b);
+    uint32_t w;
+    memcpy(&w, &h, 4);
+    return w;
+}
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    uint32_t w;
+    memcpy(&w, &h, 4);
+    return w;
+}
+__device__ __forceinline__ float2 unpack_half2(uint32_t w)
+{
+    __half2 h;
+    memcpy(&h, &w, 4);
+    return __half22float2(h);
 }
 
 constexpr int kPiecePitch = 36;                              // words: 16-byte stores of eight lanes hit all banks
@@ -54,7 +71,7 @@ __device__ __forceinline__ void stage_swizzled16(unsigned char *buf, int lane, c
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int e = (8 * j + 2 * i) & 31;
-            w[i] = j < 4 ? pack2(from_f<T>(a[e]), from_f<T>(a[e + 1])) : pack2(from_f<T>(b[e]), from_f<T>(b[e + 1]));
+            w[i] = j < 4 ? pack2<T>(a[e], a[e + 1]) : pack2<T>(b[e], b[e + 1]);
         }
         *reinterpret_cast<uint4 *>(buf + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
@@ -67,18 +84,13 @@ __device__ __forceinline__ void store_piece(const float *buf, int lane, T *dst, 
 {
     if (sizeof(T) == 2 && (ld & 1) == 0 && (reinterpret_cast<uintptr_t>(dst) & 3u) == 0) {
         const int c = (lane & 15) * 2;
-#pragma unroll 4
+#pragma unroll 8
         for (int r = lane >> 4; r < rows; r += 2) {
             const float2 x = *reinterpret_cast<const float2 *>(buf + r * kPiecePitch + c);
             T *d = dst + (int64_t)r * ld + c;
-            const T a = from_f<T>(x.x), b = from_f<T>(x.y);
-            if (c + 1 < cols) {
-                uint32_t w;
-                T e[2] = {a, b};
-                memcpy(&w, e, 4);
-                *reinterpret_cast<uint32_t *>(d) = w;
-            } else if (c < cols) {
-                *d = a;
+            if constexpr (sizeof(T) == 2) {
+                if (c + 1 < cols) *reinterpret_cast<uint32_t *>(d) = pack2<T>(x.x, x.y);
+                else if (c < cols) *d = from_f<T>(x.x);
             }
         }
     } else {
