@@ -224,23 +224,38 @@ __device__ __forceinline__ Work work_of(const Matrix &m, int step)
                   : Work{m.rows, m.cols, m.r, kPolyMap, x, false, true, true, false};
 }
 
-// The last step's result, 32 x 32 entries at a time: out = X, or w = decay w - step scale X.  A lane has a column, or two
-// neighbouring ones of a 16-bit type whose rows start at 4-byte boundaries, of every row or every other row; the weights
-// are fetched a piece ahead.
+// The last step's result: out = X, or w = decay w - step scale X, with the weights fetched a piece ahead.
+//   wide     rows start at 16-byte boundaries: a lane has a row, 128 bytes of it at a time, for the arithmetic (as tensor
+//            memory is read), and an eighth of four rows' 128 bytes for the stores
+//   others   32 x 32 entries at a time: a lane has a column, or two neighbouring ones of a 16-bit type whose rows start at
+//            4-byte boundaries, of every row or every other row
 template <typename T> struct Weights {
+    static constexpr int WIDE = 128 / (int)sizeof(T);     // columns of a wide piece
     uint32_t w[32];
-    bool paired;
-    T *at;               // the piece's first entry
-    int rows, cols;
 
-    __device__ __forceinline__ void fetch(const OutputArgs &o, const Matrix &mx, int lane, int m, int n, int rows_, int cols_)
+    static __device__ __forceinline__ bool wide(const OutputArgs &o, const Matrix &mx)
     {
-        at = static_cast<T *>(o.ptr) + mx.off + (int64_t)m * mx.cols + n;
-        rows = rows_;
-        cols = cols_;
-        paired = sizeof(T) == 2 && (mx.cols & 1) == 0 && (reinterpret_cast<uintptr_t>(at) & 3u) == 0;
+        return (mx.cols * (int64_t)sizeof(T)) % 16 == 0 && (reinterpret_cast<uintptr_t>(static_cast<T *>(o.ptr) + mx.off) & 15u) == 0;
+    }
+    static __device__ __forceinline__ bool paired(const OutputArgs &o, const Matrix &mx)
+    {
+        return sizeof(T) == 2 && (mx.cols & 1) == 0 && (reinterpret_cast<uintptr_t>(static_cast<T *>(o.ptr) + mx.off) & 3u) == 0;
+    }
+    // the piece at (m, n); rows, cols: what of the matrix begins there
+    __device__ __forceinline__ void fetch(const OutputArgs &o, const Matrix &mx, int lane, int m, int n, int rows, int cols)
+    {
         if (!o.update) return;
-        if (paired) {
+        const T *at = static_cast<const T *>(o.ptr) + mx.off + (int64_t)m * mx.cols + n;
+        if (wide(o, mx)) {
+            const T *d = at + (int64_t)lane * mx.cols;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (lane < rows && i * (16 / (int)sizeof(T)) < cols) {
+                    const uint4 q = *reinterpret_cast<const uint4 *>(d + i * (16 / (int)sizeof(T)));
+                    w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
+                }
+            }
+        } else if (paired(o, mx)) {
             const T *d = at + (int64_t)(lane >> 4) * mx.cols + (lane & 15) * 2;
             const bool in = (lane & 15) * 2 < cols;      // cols is even: a layer's columns are, and 32
 #pragma unroll
@@ -257,18 +272,56 @@ template <typename T> struct Weights {
             }
         }
     }
-    static __device__ __forceinline__ T entry(uint32_t bits)
+    static __device__ __forceinline__ float entry(uint32_t bits)      // of a 16-bit type: the low half
     {
         if constexpr (sizeof(T) == 4) return __uint_as_float(bits);
         const uint16_t u = (uint16_t)bits;
         T e;
         memcpy(&e, &u, 2);
-        return e;
+        return to_f(e);
     }
-    __device__ __forceinline__ void finish(const OutputArgs &o, const Matrix &mx, const float *buf, int lane)
+    // 64 columns of this lane's row (a 32-bit type: the first or last 32 of them), staged and stored
+    __device__ __forceinline__ void finish_wide(const OutputArgs &o, const Matrix &mx, unsigned char *buf, int lane, int m, int n, int rows,
+                                                int cols, float (&a)[32], float (&b)[32])
     {
-        const float f = 1.0f / (kGramScale * mx.sx), k = o.step * mx.scale;
-        if (paired) {
+        const float f = 1.0f / (kGramScale * mx.sx), k = o.update ? -o.step * mx.scale * f : f;
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float(&x)[32] = h ? b : a;
+                    const uint32_t two = w[16 * h + i / 2];
+                    x[i] = o.update ? __fmaf_rn(k, x[i], o.decay * entry(two)) : x[i] * k;
+                    x[i + 1] = o.update ? __fmaf_rn(k, x[i + 1], o.decay * entry(two >> 16)) : x[i + 1] * k;
+                }
+            }
+            __syncwarp();
+            stage_swizzled16<T>(buf, lane, a, b);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) a[i] = o.update ? __fmaf_rn(k, a[i], o.decay * entry(w[i])) : a[i] * k;
+            __syncwarp();
+            stage_swizzled(buf, lane, a);
+        }
+        __syncwarp();
+        const int c = (lane & 7) * (16 / (int)sizeof(T));
+        T *d = static_cast<T *>(o.ptr) + mx.off + (int64_t)m * mx.cols + n + c;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i + (lane >> 3);
+            if (r < rows && c < cols)
+                *reinterpret_cast<uint4 *>(d + (int64_t)r * mx.cols) =
+                    *reinterpret_cast<const uint4 *>(buf + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+        }
+    }
+    // a staged piece of 32 x 32
+    __device__ __forceinline__ void finish(const OutputArgs &o, const Matrix &mx, const float *buf, int lane, int m, int n, int rows,
+                                           int cols)
+    {
+        T *at = static_cast<T *>(o.ptr) + mx.off + (int64_t)m * mx.cols + n;
+        const float f = 1.0f / (kGramScale * mx.sx), k = o.update ? -o.step * mx.scale * f : f;
+        if (paired(o, mx)) {
             const int c = (lane & 15) * 2;
             T *d = at + (int64_t)(lane >> 4) * mx.cols + c;
 #pragma unroll
@@ -276,14 +329,9 @@ template <typename T> struct Weights {
                 const int r = 2 * i + (lane >> 4);
                 if (c < cols && r < rows) {
                     float2 x = *reinterpret_cast<const float2 *>(buf + r * kPiecePitch + c);
-                    x.x *= f;
-                    x.y *= f;
-                    if (o.update) {
-                        x.x = __fmaf_rn(-k, x.x, o.decay * to_f(entry(w[i])));
-                        x.y = __fmaf_rn(-k, x.y, o.decay * to_f(entry(w[i] >> 16)));
-                    }
-                    if constexpr (sizeof(T) == 2)
-                        *reinterpret_cast<uint32_t *>(d + (int64_t)2 * i * mx.cols) = pack2<T>(x.x, x.y);
+                    x.x = o.update ? __fmaf_rn(k, x.x, o.decay * entry(w[i])) : x.x * k;
+                    x.y = o.update ? __fmaf_rn(k, x.y, o.decay * entry(w[i] >> 16)) : x.y * k;
+                    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t *>(d + (int64_t)2 * i * mx.cols) = pack2<T>(x.x, x.y);
                 }
             }
         } else if (lane < cols) {
@@ -291,8 +339,8 @@ template <typename T> struct Weights {
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
                 if (i < rows) {
-                    float x = buf[i * kPiecePitch + lane] * f;
-                    if (o.update) x = __fmaf_rn(-k, x, o.decay * to_f(entry(w[i])));
+                    float x = buf[i * kPiecePitch + lane];
+                    x = o.update ? __fmaf_rn(k, x, o.decay * entry(w[i])) : x * k;
                     d[(int64_t)i * mx.cols] = from_f<T>(x);
                 }
             }
@@ -450,7 +498,8 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
         };
         Weights<T> weights;
         auto fetch_weights = [&](const Place &at, int n) {
-            weights.fetch(prm.out, *at.mx, lane, at.m0, n, max(at.rows, 0), max(0, min(32, at.N - n)));
+            const int most = Weights<T>::wide(prm.out, *at.mx) ? Weights<T>::WIDE : 32;
+            weights.fetch(prm.out, *at.mx, lane, at.m0, n, max(at.rows, 0), max(0, min(most, at.N - n)));
         };
         auto look_ahead = [&](const Place &at) {
             if (lane >= at.rows) return;
@@ -494,14 +543,21 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
                     if (lane == 0) { if (CG == 2) mbar_arrive_cluster(in_leader(d_empty + ab)); else mbar_arrive(d_empty + ab); }
                 }
                 if (PHASE == kLast) {
-                    float *buf = reinterpret_cast<float *>(mine);
+                    const bool wide = Weights<T>::wide(prm.out, mx);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        if (live && n0 + 32 * h < here.N) {
-                            stage_piece(buf, lane, v[h]);
-                            weights.finish(prm.out, mx, buf, lane);
+                        const int n = n0 + 32 * h;
+                        if (sizeof(T) == 2 && wide && h == 1) break;        // the first round took all 64 columns
+                        if (live && n < here.N) {
+                            if (wide) {
+                                weights.finish_wide(prm.out, mx, mine, lane, m0, n, rows, min(Weights<T>::WIDE, here.N - n), v[h], v[h ^ 1]);
+                            } else {
+                                stage_piece(reinterpret_cast<float *>(mine), lane, v[h]);
+                                weights.finish(prm.out, mx, reinterpret_cast<const float *>(mine), lane, m0, n, rows, min(32, here.N - n));
+                            }
                         }
-                        if (p * 64 + h * 32 + 32 < COLS) fetch_weights(here, n0 + 32 * h + 32);
+                        const int after = p * 64 + h * 32 + (wide ? Weights<T>::WIDE : 32);
+                        if (after < COLS) fetch_weights(here, c0 + after);
                         else if (t + 1 < t_end) fetch_weights(next, next.c0);
                     }
                     continue;
