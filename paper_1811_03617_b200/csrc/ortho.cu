@@ -183,7 +183,11 @@ __global__ void __launch_bounds__(256) normalise_kernel(const StartParams prm)
 //           even one issues MMAs that read both.  32 KB a stage and SM for 512 clocks of MMAs; a CTA alone on 128 x 256
 //           would load 48 KB, more than L2 delivers to all SMs at that rate.
 //   CG = 1  one CTA, tile 128 x 64, for plans without enough large tiles to fill the GPU: four times the CTAs at work, a
-//           quarter of the time a stage, and two CTAs fit an SM, so that a launch's first tiles overlap the last one's end.
+//           quarter of the time a stage.
+// A's contraction is the long side of the matrix and its tiles may be few: there the contraction is split between CTAs
+// (Tile::parts).  The sums of all parts go to scratch in fp32, a warp's piece by piece; of the warps that hold the same
+// piece of a tile the last to arrive adds the parts in their order and goes on with the epilogue, so the result does not
+// depend on who that is.
 constexpr int KS = 64;
 constexpr uint32_t BOX = 64 * 128;
 constexpr uint32_t kStaging = 8192;      // of an epilogue warp: two pieces of 32 rows x 128 bytes
@@ -193,7 +197,7 @@ template <int CG> struct Shape {
     static constexpr int BLOCK = 128 * CG;                                   // of the diagonal of a symmetric result
     static constexpr int NB = CG == 2 ? 2 : BN / 64;                        // boxes of B a CTA loads
     static constexpr uint32_t A_BYTES = 2 * BOX, STAGE = A_BYTES + NB * BOX;
-    static constexpr int STAGES = CG == 2 ? 5 : 3;
+    static constexpr int STAGES = 5;
     static constexpr int NEPI = CG == 2 ? 8 : 4, THREADS = 64 + 32 * NEPI;   // epilogue warps
     static constexpr uint32_t TMEM = 2 * BN;                                 // two accumulators
     static constexpr size_t SMEM = (size_t)STAGES * STAGE + NEPI * kStaging + 256 + 1024;
@@ -358,7 +362,7 @@ __device__ __forceinline__ void load16(const __half *p, uint32_t (&w)[8])
 
 // T: the type of the last step's result (PHASE kLast).
 template <int PHASE, int CG, typename T = float>
-__global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_kernel(const __grid_constant__ ProductParams prm)
+__global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __grid_constant__ ProductParams prm)
 {
     using S = Shape<CG>;
     extern __shared__ unsigned char smem_raw[];
@@ -387,9 +391,8 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
     bool failed = false;
     // this CTA's (pair's) run of tiles
     constexpr bool APPLY = PHASE == kApply || PHASE == kLast;
-    const Tile *tiles = APPLY ? prm.dev.apply_tiles : prm.dev.sym_tiles;
-    const int32_t *starts = APPLY ? prm.dev.apply_start : prm.dev.sym_start;
-    const int t_begin = starts[blockIdx.x / CG], t_end = starts[blockIdx.x / CG + 1];
+    const Tile *tiles = prm.dev.run[PHASE].tiles;
+    const int t_begin = prm.dev.run[PHASE].start[blockIdx.x / CG], t_end = prm.dev.run[PHASE].start[blockIdx.x / CG + 1];
 
     if (warp == 0) {
         if (lane == 0) {
@@ -403,10 +406,9 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
                 // a pair's columns are split in halves of a multiple of 8 (the last tile's may be narrow)
                 const int half_n = CG == 2 ? min(S::BN, (w.N - tile.tn * S::BN + 15) / 16 * 16) / 2 : 0;
                 const int m0 = tile.tm * 128 * CG + 128 * rank, n0 = tile.tn * S::BN + half_n * rank;
-                const int n_stages = (w.K + KS - 1) / KS;
                 // steps of the contraction left of the diagonal's block of a symmetric operand's rows
                 const int a_left = w.a_sym ? m0 / S::BLOCK * S::BLOCK : 0, b_left = w.b_sym ? tile.tn * S::BN / S::BLOCK * S::BLOCK : 0;
-                for (int st = 0; st < n_stages; ++st, ++c) {
+                for (int st = tile.k0; st < tile.k1; ++st, ++c) {
                     const uint32_t s = c % S::STAGES;
                     if (!mbar_poll(empty + s, ((c / S::STAGES) & 1) ^ 1, abort_flag)) { failed = true; break; }
                     if (prm.test_drop && blockIdx.x == 0 && c == 0) continue;   // test hook: this stage never arrives
@@ -439,11 +441,10 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
             const int n = min(S::BN, (w.N - tile.tn * S::BN + 15) / 16 * 16);
             const int a_left = w.a_sym ? tile.tm * 128 * CG / S::BLOCK * S::BLOCK : 0;
             const int b_left = w.b_sym ? tile.tn * S::BN / S::BLOCK * S::BLOCK : 0;
-            const int n_stages = (w.K + KS - 1) / KS;
             bool ok = mbar_poll(d_empty + buf, ((u >> 1) & 1) ^ 1, abort_flag);
             if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
             tc_fence_after();
-            for (int st = 0; st < n_stages; ++st, ++c) {
+            for (int st = tile.k0; st < tile.k1; ++st, ++c) {
                 const uint32_t s = c % S::STAGES;
                 ok = mbar_poll(full + s, (c / S::STAGES) & 1, abort_flag);
                 if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
@@ -459,9 +460,9 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        if (k < n_mma) tc_mma_f16<CG>(d, da + k * ia, db + k * ib, idesc, (st | k) != 0);
+                        if (k < n_mma) tc_mma_f16<CG>(d, da + k * ia, db + k * ib, idesc, st > tile.k0 || k > 0);
                     if (CG == 2) tc_commit_pair(empty + s); else tc_commit(empty + s);
-                    if (st == n_stages - 1) { if (CG == 2) tc_commit_pair(d_full + buf); else tc_commit(d_full + buf); }
+                    if (st == tile.k1 - 1) { if (CG == 2) tc_commit_pair(d_full + buf); else tc_commit(d_full + buf); }
                 }
                 __syncwarp();
             }
@@ -530,17 +531,62 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, CG == 1 ? 2 : 1) product_k
             bool ok = mbar_poll(d_full + ab, (u >> 1) & 1, abort_flag);
             if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
             tc_fence_after();
-#pragma unroll
-            for (int p = 0; p < PIECES; ++p) {
-                const int n0 = c0 + p * 64;
-                const bool live = rows > 0 && n0 < here.N;
-                float v[2][32];
+            auto read_accumulator = [&](int p, float (&v)[2][32]) {
                 tmem_ld32_wait(tmem + lane_base + ab * S::BN + half * COLS + p * 64, v[0]);
                 tmem_ld32_wait(tmem + lane_base + ab * S::BN + half * COLS + p * 64 + 32, v[1]);
                 if (p == PIECES - 1) {       // the accumulator is free
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) { if (CG == 2) mbar_arrive_cluster(in_leader(d_empty + ab)); else mbar_arrive(d_empty + ab); }
+                }
+            };
+            // a part of a contraction: this warp's pieces go to scratch, and the last warp to bring its part goes on
+            const int parts = PHASE == kGram ? tiles[t].parts : 1;
+            constexpr int PER_CTA = 4 * S::BN / 64, PER_PART = CG * PER_CTA;      // pieces
+            float4 *scratch = nullptr;
+            if (PHASE == kGram && parts > 1) {
+                const int first = tiles[t].slot + rank * PER_CTA + (q * (S::NEPI / 4) + half) * PIECES;
+                scratch = reinterpret_cast<float4 *>(prm.dev.parts) + (int64_t)first * 512 + lane;
+                float4 *own = scratch + (int64_t)tiles[t].part * PER_PART * 512;
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p) {
+                    float v[2][32];
+                    read_accumulator(p, v);
+                    if (rows <= 0 || c0 + p * 64 >= here.N) continue;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float *x = &v[i >> 3][4 * (i & 7)];
+                        __stcg(own + p * 512 + 32 * i, make_float4(x[0], x[1], x[2], x[3]));
+                    }
+                }
+                __threadfence();
+                __syncwarp();
+                int arrived = 0;
+                if (lane == 0) arrived = atomicAdd(prm.dev.tickets + first, 1);
+                if (__shfl_sync(0xffffffffu, arrived, 0) != parts - 1) { here = next; continue; }
+                if (lane == 0) prm.dev.tickets[first] = 0;
+                __threadfence();
+            }
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) {
+                const int n0 = c0 + p * 64;
+                const bool live = rows > 0 && n0 < here.N;
+                float v[2][32];
+                if (PHASE == kGram && parts > 1) {
+                    if (!live) continue;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[0][i] = v[1][i] = 0.0f;
+                    for (int part = 0; part < parts; ++part) {
+                        const float4 *from = scratch + (int64_t)part * PER_PART * 512 + p * 512;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float4 x = __ldcg(from + 32 * i);
+                            float *y = &v[i >> 3][4 * (i & 7)];
+                            y[0] += x.x; y[1] += x.y; y[2] += x.z; y[3] += x.w;
+                        }
+                    }
+                } else {
+                    read_accumulator(p, v);
                 }
                 if (PHASE == kLast) {
                     const bool wide = Weights<T>::wide(prm.out, mx);
@@ -698,7 +744,7 @@ cudaError_t launch_product(cudaStream_t st, const Device &dev, Phase phase, int 
     prm.wait_kcycles = wait_kcycles > 0 ? wait_kcycles : WAIT_KCYCLES_DEFAULT;
     prm.test_drop = test_drop;
     auto launch = [&](auto pair, auto solo) {
-        const int runs = phase == kApply ? dev.apply_runs : dev.sym_runs;
+        const int runs = dev.run[phase].runs;
         return dev.pair ? launch_chained(pair, prm, 2 * runs, Shape<2>::THREADS, Shape<2>::SMEM, 2, st)
                         : launch_chained(solo, prm, runs, Shape<1>::THREADS, Shape<1>::SMEM, 1, st);
     };

@@ -32,23 +32,32 @@ struct Matrix {
     float sx;                        // scale of X in half precision
     float scale;                     // of the update
 };
-struct Tile { int32_t matrix, tm, tn; };
+// A tile of a product, or a part of its contraction: stages [k0, k1) of 64 steps.  parts > 1: the parts' sums meet in the
+// plan's scratch from piece `slot` on (part by part), and whoever comes last adds them up.
+struct Tile { int32_t matrix, tm, tn, k0, k1, part, parts, slot; };
 struct Chunk { int32_t matrix, index; };
 
 enum Phase { kGram = 0, kPoly = 1, kApply = 2, kLast = 3 };
 // Tensor maps of a matrix: operands (boxes of 64 x 64) and results (64 columns x 32 rows)
 enum Map { kX0 = 0, kX1, kGramMap, kFactorMap, kPolyMap, kX0Out, kX1Out, kLoOut, kGramOut, kFactorOut, kPolyOut, kMaps };
 
+// The tiles of a phase, in runs, one for each CTA (or pair): run i is tiles [start[i], start[i + 1]).
+struct Run {
+    const Tile *tiles;
+    const int32_t *start;
+    int runs;
+};
+
 struct Device {
     const Matrix *mats;
     const CUtensorMap *maps;         // [matrices][kMaps]
-    const Tile *sym_tiles, *apply_tiles;         // in runs, one for each CTA (or pair)
-    const int32_t *sym_start, *apply_start;      // [runs + 1]
-    int sym_runs, apply_runs;
+    Run run[4];                      // of each phase
     int pair;                        // which tiling the tiles are of
     const Chunk *chunks;
     int n_chunks;
     float *partial;                  // [n_chunks] sums of squares
+    float *parts;                    // sums of parts of a contraction, pieces of 32 rows x 64 columns
+    int32_t *tickets;                // [pieces of a tile's first part] arrivals, zero between launches
 };
 
 // momentum = beta * momentum + g (momentum may be null), u = g + beta * momentum (nesterov) or momentum, sums of squares;

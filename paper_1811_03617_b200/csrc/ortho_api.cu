@@ -21,6 +21,7 @@ struct gvq_ortho {
 namespace {
 
 constexpr size_t kAlign = 256;
+constexpr int kPartStages = 6, kMaxParts = 8;   // a part of a contraction: at least so many stages, at most so many parts
 constexpr int kTileCost = 3;      // what a tile costs beyond its contraction, in stages of 64 steps
 constexpr int kPairTiles = 148;   // fewer 256 x 256 tiles than this: 128 x 64 tiles
 size_t up(size_t n) { return (n + kAlign - 1) & ~(kAlign - 1); }
@@ -73,10 +74,9 @@ bool encode(EncodeTiledFn enc, CUtensorMap *map, void *p, int rows, int cols, in
 
 // Deals tiles to at most `units` CTAs so that their costs come out even (longest first, to whoever has least), and puts
 // each one's tiles together, a matrix's next to each other.  Returns where the runs start.
-template <typename F>
-std::vector<int32_t> deal(std::vector<Tile> &tiles, int units, F contraction)
+std::vector<int32_t> deal(std::vector<Tile> &tiles, int units)
 {
-    auto cost = [&](const Tile &t) { return (contraction(t) + 63) / 64 + kTileCost; };
+    auto cost = [&](const Tile &t) { return t.k1 - t.k0 + kTileCost; };
     std::stable_sort(tiles.begin(), tiles.end(), [&](const Tile &a, const Tile &b) { return cost(a) > cost(b); });
     const int runs = (int)std::min<size_t>(units, tiles.size());
     std::vector<std::vector<Tile>> run(runs);
@@ -96,6 +96,27 @@ std::vector<int32_t> deal(std::vector<Tile> &tiles, int units, F contraction)
         start.push_back((int32_t)tiles.size());
     }
     return start;
+}
+
+// Cuts contractions into parts where there are fewer tiles than CTAs.  `pieces`: of 32 x 64 entries in a tile.
+void split(std::vector<Tile> &tiles, int units, int pieces, int &slots)
+{
+    const int share = std::min(kMaxParts, tiles.empty() ? 1 : units / (int)tiles.size());
+    std::vector<Tile> out;
+    for (const Tile &t : tiles) {
+        const int parts = std::max(1, std::min(share, t.k1 / kPartStages));
+        for (int i = 0; i < parts; ++i) {
+            Tile s = t;
+            s.k0 = (int)((int64_t)t.k1 * i / parts);
+            s.k1 = (int)((int64_t)t.k1 * (i + 1) / parts);
+            s.part = i;
+            s.parts = parts;
+            s.slot = slots;
+            out.push_back(s);
+        }
+        if (parts > 1) slots += parts * pieces;
+    }
+    tiles = out;
 }
 
 // The five steps from X to the result.
@@ -162,44 +183,52 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
             for (int k = 0; k < m.n_chunks; ++k) chunks.push_back({i, k});
         }
         // Which tiling: pairs of CTAs on 256 x 256 tiles where there are enough of them.
+        std::vector<Tile> gram;
         bool pair = false;
         for (int attempt = 0; attempt < 2; ++attempt) {
             pair = attempt == 0;
             const int64_t bm = pair ? 256 : 128, bn = pair ? kPairN : kSoloN;
+            gram.clear();
             sym.clear();
             apply.clear();
             for (int i = 0; i < n; ++i) {
                 const Matrix &m = sz.mats[i];
+                const int kr = (m.r + 63) / 64, kc = (m.c + 63) / 64;
                 // tiles of a symmetric product: those that reach the diagonal or lie right of it
                 for (int tm = 0; tm * bm < m.r; ++tm)
-                    for (int tn = (int)(tm * bm / bn); tn * bn < m.r; ++tn) sym.push_back({i, tm, tn});
+                    for (int tn = (int)(tm * bm / bn); tn * bn < m.r; ++tn) {
+                        gram.push_back({i, tm, tn, 0, kc, 0, 1, 0});
+                        sym.push_back({i, tm, tn, 0, kr, 0, 1, 0});
+                    }
                 for (int tm = 0; tm * bm < m.rows; ++tm)
-                    for (int tn = 0; tn * bn < m.cols; ++tn) apply.push_back({i, tm, tn});
+                    for (int tn = 0; tn * bn < m.cols; ++tn) apply.push_back({i, tm, tn, 0, kr, 0, 1, 0});
             }
             if (pair && (int)apply.size() >= kPairTiles) break;
         }
-        const int units = pair ? ctx->num_sms / 2 : 2 * ctx->num_sms;
-        // (A's contraction is c long, its polynomial's r: one order serves both)
-        const std::vector<int32_t> sym_start = deal(sym, units, [&](const Tile &t) { return sz.mats[t.matrix].c; });
-        const std::vector<int32_t> apply_start = deal(apply, units, [&](const Tile &t) { return sz.mats[t.matrix].r; });
+        const int units = pair ? ctx->num_sms / 2 : ctx->num_sms;
+        int slots = 0;
+        split(gram, units, (pair ? 2 : 1) * 4 * (pair ? kPairN : kSoloN) / 64, slots);
+        const std::vector<int32_t> gram_start = deal(gram, units), sym_start = deal(sym, units), apply_start = deal(apply, units);
 
         gvq_ortho *p = new gvq_ortho();
         p->ctx = ctx;
         p->device = ctx->device;
-        const size_t b_m = up(sizeof(Matrix) * n), b_t = up(sizeof(CUtensorMap) * maps.size()), b_s = up(sizeof(Tile) * sym.size()),
-                     b_a = up(sizeof(Tile) * apply.size()), b_c = up(sizeof(Chunk) * chunks.size()), b_ss = up(sizeof(int32_t) * sym_start.size()), b_as = up(sizeof(int32_t) * apply_start.size()),
-                     b_p = up(sizeof(float) * chunks.size());
-        std::vector<unsigned char> image(b_m + b_t + b_s + b_a + b_c + b_ss + b_as);
-        auto put = [&](size_t at, const void *src, size_t bytes) { if (bytes) std::memcpy(image.data() + at, src, bytes); };
-        put(0, sz.mats.data(), sizeof(Matrix) * n);
-        put(b_m, maps.data(), sizeof(CUtensorMap) * maps.size());
-        put(b_m + b_t, sym.data(), sizeof(Tile) * sym.size());
-        put(b_m + b_t + b_s, apply.data(), sizeof(Tile) * apply.size());
-        put(b_m + b_t + b_s + b_a, chunks.data(), sizeof(Chunk) * chunks.size());
-        put(b_m + b_t + b_s + b_a + b_c, sym_start.data(), sizeof(int32_t) * sym_start.size());
-        put(b_m + b_t + b_s + b_a + b_c + b_ss, apply_start.data(), sizeof(int32_t) * apply_start.size());
+        std::vector<unsigned char> image;
+        auto put = [&](const void *src, size_t bytes) {
+            const size_t at = up(image.size());
+            image.resize(at + bytes);
+            if (bytes) std::memcpy(image.data() + at, src, bytes);
+            return at;
+        };
+        auto table = [&](const auto &v) { return put(v.data(), sizeof(v[0]) * v.size()); };
+        const size_t o_m = table(sz.mats), o_t = table(maps), o_g = table(gram), o_s = table(sym), o_a = table(apply), o_c = table(chunks),
+                     o_gs = table(gram_start), o_ss = table(sym_start), o_as = table(apply_start);
+        const std::vector<int32_t> no_tickets((size_t)slots, 0);
+        const size_t o_k = table(no_tickets);
+        // behind the image: sums of squares, and the parts' sums
+        const size_t o_p = up(image.size()), o_q = o_p + up(sizeof(float) * chunks.size()), all = o_q + (size_t)slots * 8192;
         DeviceGuard guard(ctx->device);
-        cudaError_t e = cudaMalloc(&p->tables, image.size() + b_p + kAlign);
+        cudaError_t e = cudaMalloc(&p->tables, all + kAlign);
         if (e == cudaSuccess) e = cudaMemcpy(p->tables, image.data(), image.size(), cudaMemcpyHostToDevice);
         if (e != cudaSuccess) {
             if (p->tables) cudaFree(p->tables);
@@ -208,16 +237,23 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
         }
         unsigned char *t = static_cast<unsigned char *>(p->tables);
         Device &d = p->dev;
-        d.mats = reinterpret_cast<Matrix *>(t);
-        d.maps = reinterpret_cast<CUtensorMap *>(t + b_m);
-        d.sym_tiles = reinterpret_cast<Tile *>(t + b_m + b_t);
-        d.apply_tiles = reinterpret_cast<Tile *>(t + b_m + b_t + b_s);
-        d.chunks = reinterpret_cast<Chunk *>(t + b_m + b_t + b_s + b_a);
-        d.partial = reinterpret_cast<float *>(t + image.size());
+        d.mats = reinterpret_cast<Matrix *>(t + o_m);
+        d.maps = reinterpret_cast<CUtensorMap *>(t + o_t);
+        auto work = [&](Run &r, size_t tiles, size_t start, const std::vector<int32_t> &s) {
+            r.tiles = reinterpret_cast<Tile *>(t + tiles);
+            r.start = reinterpret_cast<int32_t *>(t + start);
+            r.runs = (int)s.size() - 1;
+        };
+        work(d.run[kGram], o_g, o_gs, gram_start);
+        work(d.run[kPoly], o_s, o_ss, sym_start);
+        work(d.run[kApply], o_a, o_as, apply_start);
+        d.run[kLast] = d.run[kApply];
+        d.chunks = reinterpret_cast<Chunk *>(t + o_c);
+        d.n_chunks = (int)chunks.size();
+        d.tickets = reinterpret_cast<int32_t *>(t + o_k);
+        d.partial = reinterpret_cast<float *>(t + o_p);
+        d.parts = reinterpret_cast<float *>(t + o_q);
         d.pair = pair;
-        d.sym_start = reinterpret_cast<int32_t *>(t + b_m + b_t + b_s + b_a + b_c);
-        d.apply_start = reinterpret_cast<int32_t *>(t + b_m + b_t + b_s + b_a + b_c + b_ss);
-        d.sym_runs = (int)sym_start.size() - 1; d.apply_runs = (int)apply_start.size() - 1; d.n_chunks = (int)chunks.size();
         *out = p;
         return GVQ_OK;
     } catch (const std::bad_alloc &) {
