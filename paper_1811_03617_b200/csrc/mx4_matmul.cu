@@ -305,24 +305,7 @@ template <typename T, int CG, int BN>
 cudaError_t launch_as(cudaStream_t st, int num_sms, const MmParams &prm)
 {
     using S = Shape<CG, BN>;
-    auto kernel = mx4_matmul_kernel<T, CG, BN>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(CG * min(num_sms / CG, prm.tiles_m * prm.tiles_n));
-    cfg.blockDim = dim3(NTHREADS);
-    cfg.dynamicSmemBytes = S::SMEM;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = CG;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = CG > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, prm);
+    return launch_chained(mx4_matmul_kernel<T, CG, BN>, prm, CG * min(num_sms / CG, prm.tiles_m * prm.tiles_n), NTHREADS, S::SMEM, CG, st);
 }
 template <int CG, int BN>
 cudaError_t launch_typed(cudaStream_t st, int num_sms, int dtype, const MmParams &prm)

@@ -6,6 +6,7 @@
 #include "gvq_internal.h"
 #include "mx4.cuh"
 #include "row32.cuh"
+#include "sm100_ptx.cuh"
 
 namespace gvq {
 namespace {
@@ -64,6 +65,8 @@ __global__ void __launch_bounds__(256) mx4_quantize_kernel(const QuantParams prm
     uint32_t *tile = reinterpret_cast<uint32_t *>(smem_q);          // [128][W] + skew, when COLS
     __shared__ __align__(16) uint8_t sc[2][kTileBytes];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    ptx::launch_dependents();
+    ptx::grid_dependency_wait();
     const int rtile = blockIdx.x / prm.ct, ctile = blockIdx.x - rtile * prm.ct;
     const int64_t r0 = (int64_t)rtile * 128, c0 = (int64_t)ctile * 128;
     const T *x = static_cast<const T *>(prm.x);
@@ -177,6 +180,8 @@ struct AggParams {
 template <bool SR, bool OUT>
 __global__ void __launch_bounds__(256) mx4_quantize_aggregate_kernel(const __grid_constant__ AggParams prm)
 {
+    ptx::launch_dependents();
+    ptx::grid_dependency_wait();
     const int t = blockIdx.x, layer = prm.tile_layer[t], row0 = prm.tile_row0[t];
     const int rows = min(kDecompressRows, prm.layer_S[layer] - row0);
     const int d = prm.d, nb = (d + kBlock - 1) / kBlock;
@@ -328,12 +333,7 @@ cudaError_t launch_quantize_as(cudaStream_t st, const QuantParams &prm)
     const unsigned grid = (unsigned)(prm.ct * tiles_of(prm.rows, 128));
     const size_t smem = COLS ? 128 * 128 * sizeof(T) + 128 : 0;
     auto kernel = mx4_quantize_kernel<T, SR, ROWS, COLS>;
-    if (smem > 48 * 1024) {
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-    }
-    kernel<<<grid, 256, smem, st>>>(prm);
-    return cudaGetLastError();
+    return ptx::launch_chained(kernel, prm, (int)grid, 256, smem, 1, st);
 }
 template <typename T, bool SR>
 cudaError_t launch_quantize_forms(cudaStream_t st, const QuantParams &prm)
@@ -388,8 +388,7 @@ cudaError_t launch_mx4_quantize_aggregate(cudaStream_t st, int d, int64_t S, con
         if (e != cudaSuccess) return e;
     }
     auto launch = [&](auto kernel) {
-        kernel<<<tiles.n_tiles, 256, 0, st>>>(prm);
-        return cudaGetLastError();
+        return ptx::launch_chained(kernel, prm, tiles.n_tiles, 256, 0, 1, st);
     };
     if (stochastic) return codes ? launch(mx4_quantize_aggregate_kernel<true, true>) : launch(mx4_quantize_aggregate_kernel<true, false>);
     return codes ? launch(mx4_quantize_aggregate_kernel<false, true>) : launch(mx4_quantize_aggregate_kernel<false, false>);

@@ -696,30 +696,6 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
     if (warp == 1) tmem_dealloc<CG>(tmem, S::TMEM);
 }
 
-template <typename K, typename P>
-cudaError_t launch_chained(K kernel, const P &prm, int grid, int threads, size_t smem, int cluster, cudaStream_t st)
-{
-    if (smem > 48 * 1024) {
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-    }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = cluster;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, prm);
-}
-
 }  // namespace
 
 cudaError_t launch_start(cudaStream_t st, const Device &dev, const ElementArgs &a)

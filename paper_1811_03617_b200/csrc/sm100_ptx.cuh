@@ -307,5 +307,31 @@ __device__ __forceinline__ void tmem_ld32_wait(uint32_t taddr, float (&v)[32])
                  : "r"(taddr) : "memory");
 }
 
+// Host: launches a kernel that begins with launch_dependents() and grid_dependency_wait(), so that its start overlaps the
+// end of the stream's last kernel; cluster: CTAs of a cluster (1: none).
+template <typename K, typename P>
+inline cudaError_t launch_chained(K kernel, const P &prm, int grid, int threads, size_t smem, int cluster, cudaStream_t st)
+{
+    if (smem > 48 * 1024) {
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, prm);
+}
+
 }  // namespace ptx
 }  // namespace gvq

@@ -268,35 +268,64 @@ DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 def _dtype(t: torch.Tensor) -> int:
-    if t.dtype not in DTYPE:
+    d = DTYPE.get(t.dtype)
+    if d is None:
         raise TypeError(f"gvq takes float32, bfloat16 and float16 here, not {t.dtype}")
-    return DTYPE[t.dtype]
+    return d
 
 
 def _rows(t: torch.Tensor, what: str):
     """(rows, cols, leading dimension) of a 2-D tensor whose rows are contiguous."""
-    if t.dim() != 2 or not t.is_cuda:
+    shape = t.shape
+    if len(shape) != 2 or not t.is_cuda:
         raise ValueError(f"{what}: a 2-D CUDA tensor is wanted")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    rows, cols = shape
+    ld, step = t.stride()
+    if cols > 1 and step != 1:
         raise ValueError(f"{what}: the entries of a row have to be contiguous")
-    return t.shape[0], t.shape[1], t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return rows, cols, ld if rows > 1 else cols
 
 
 class Mx4:
     """A matrix [rows][cols] in microscaled 4-bit floating point: device bytes `codes` and `scales` (see gvq.h)."""
 
+    __slots__ = ("rows", "cols", "_codes", "_scales", "_buf", "_n", "_at", "codes_ptr", "scales_ptr")
+
     def __init__(self, rows: int, cols: int, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
                  device=None):
-        self.rows, self.cols = int(rows), int(cols)
-        nc = lib().gvq_mx4_codes_bytes(self.rows, self.cols)
-        ns = lib().gvq_mx4_scales_bytes(self.rows, self.cols)
-        if nc < 0:
+        self.rows, self.cols = rows, cols = int(rows), int(cols)
+        nb = (cols + 31) // 32
+        tiles = ((rows + 127) // 128) * ((nb + 3) // 4)
+        if rows < 1 or cols < 1 or tiles >= 0x7FFFFFFF:
             raise ValueError(f"no 4-bit matrix of {rows} x {cols}")
-        self.codes = torch.empty(nc, dtype=torch.uint8, device=device or "cuda") if codes is None else codes
-        self.scales = torch.empty(ns, dtype=torch.uint8, device=device or "cuda") if scales is None else scales
-        for t, n in ((self.codes, nc), (self.scales, ns)):
+        nc, ns = rows * nb * 16, tiles * 512
+        self._n = (nc, ns)
+        if codes is None and scales is None:       # one allocation for both
+            self._at = (nc + 255) & ~255
+            self._buf = torch.empty(self._at + ns, dtype=torch.uint8, device=device or "cuda")
+            self._codes = self._scales = None
+            self.codes_ptr = self._buf.data_ptr()
+            self.scales_ptr = self.codes_ptr + self._at
+            return
+        if codes is None or scales is None:
+            raise ValueError("codes and scales come together")
+        for t, n in ((codes, nc), (scales, ns)):
             if t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous() or t.numel() < n:
                 raise ValueError(f"a 4-bit matrix of {rows} x {cols} has {nc} bytes of codes and {ns} of scales, contiguous")
+        self._codes, self._scales = codes, scales
+        self.codes_ptr, self.scales_ptr = codes.data_ptr(), scales.data_ptr()
+
+    @property
+    def codes(self) -> torch.Tensor:
+        if self._codes is None:
+            self._codes = self._buf[:self._n[0]]
+        return self._codes
+
+    @property
+    def scales(self) -> torch.Tensor:
+        if self._scales is None:
+            self._scales = self._buf[self._at:self._at + self._n[1]]
+        return self._scales
 
 
 class Context:
@@ -315,12 +344,20 @@ class Context:
         self.M = self.layout.total_entries()
         self.n_layers = len(self.layout.layer_len)
         self._ws = None
+        self._stream_now = self._raw_stream()
 
     def _stream(self):
         return ctypes.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
 
+    def _raw_stream(self) -> int:
+        return torch.cuda.current_stream(self.device).cuda_stream
+
     def _sync_stream(self):
-        _check(lib().gvq_set_stream(self._h, self._stream()), "gvq_set_stream")
+        """Hands the current stream over; only when it is another than at the last call."""
+        now = self._raw_stream()
+        if now != self._stream_now:
+            _check(lib().gvq_set_stream(self._h, now), "gvq_set_stream")
+            self._stream_now = now
 
     def close(self):
         if self._h:
@@ -413,18 +450,25 @@ class Context:
     # ---- microscaled 4-bit floating point ---------------------------------------------------
     def _mx4(self, x, by_rows, by_cols, stochastic, seed, node, out=None, out_t=None):
         rows, cols, ld = _rows(x, "mx4_quantize")
-        if by_rows and out is None:
-            out = Mx4(rows, cols, device=x.device)
-        if by_cols and out_t is None:
-            out_t = Mx4(cols, rows, device=x.device)
-        if (out is not None and (out.rows, out.cols) != (rows, cols)) or \
-                (out_t is not None and (out_t.rows, out_t.cols) != (cols, rows)):
-            raise ValueError("mx4_quantize: the output is of another size")
+        dtype = _dtype(x)
+        c = s = ct = st = None
+        if by_rows:
+            if out is None:
+                out = Mx4(rows, cols, device=x.device)
+            elif out.rows != rows or out.cols != cols:
+                raise ValueError("mx4_quantize: the output is of another size")
+            c, s = out.codes_ptr, out.scales_ptr
+        if by_cols:
+            if out_t is None:
+                out_t = Mx4(cols, rows, device=x.device)
+            elif out_t.rows != cols or out_t.cols != rows:
+                raise ValueError("mx4_quantize: the output is of another size")
+            ct, st = out_t.codes_ptr, out_t.scales_ptr
         self._sync_stream()
-        _check(lib().gvq_mx4_quantize(self._h, x.data_ptr(), _dtype(x), rows, cols, ld, 1 if stochastic else 0, seed, node,
-                                      out.codes.data_ptr() if out else None, out.scales.data_ptr() if out else None,
-                                      out_t.codes.data_ptr() if out_t else None, out_t.scales.data_ptr() if out_t else None),
-               "gvq_mx4_quantize")
+        status = lib().gvq_mx4_quantize(self._h, x.data_ptr(), dtype, rows, cols, ld, 1 if stochastic else 0, seed, node, c, s,
+                                        ct, st)
+        if status:
+            raise GvqError(status, "gvq_mx4_quantize")
         return out, out_t
 
     def mx4_quantize(self, x, stochastic=False, seed=0, node=0, out: Optional[Mx4] = None) -> Mx4:
@@ -443,12 +487,12 @@ class Context:
     def mx4_dequantize(self, q: Mx4, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """gvq_mx4_dequantize: what q stands for, float32 [rows, cols]."""
         if out is None:
-            out = torch.empty((q.rows, q.cols), device=q.codes.device)
+            out = torch.empty((q.rows, q.cols), device=f"cuda:{self.device}")
         rows, cols, ld = _rows(out, "mx4_dequantize")
         if (rows, cols) != (q.rows, q.cols) or out.dtype != torch.float32:
             raise ValueError("mx4_dequantize: a float32 output of the matrix's size is wanted")
         self._sync_stream()
-        _check(lib().gvq_mx4_dequantize(self._h, q.codes.data_ptr(), q.scales.data_ptr(), rows, cols, out.data_ptr(), ld),
+        _check(lib().gvq_mx4_dequantize(self._h, q.codes_ptr, q.scales_ptr, rows, cols, out.data_ptr(), ld),
                "gvq_mx4_dequantize")
         return out
 
@@ -458,9 +502,10 @@ class Context:
         if a.cols != b.cols or (rows, cols) != (a.rows, b.rows):
             raise ValueError(f"mx4_matmul: [{a.rows}, {a.cols}] x [{b.rows}, {b.cols}]^T does not give [{rows}, {cols}]")
         self._sync_stream()
-        _check(lib().gvq_mx4_matmul(self._h, a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(),
-                                    b.scales.data_ptr(), rows, cols, a.cols, out.data_ptr(), _dtype(out), ld),
-               "gvq_mx4_matmul")
+        status = lib().gvq_mx4_matmul(self._h, a.codes_ptr, a.scales_ptr, b.codes_ptr, b.scales_ptr, rows, cols, a.cols,
+                                      out.data_ptr(), _dtype(out), ld)
+        if status:
+            raise GvqError(status, "gvq_mx4_matmul")
         return out
 
     def mx4_slices(self) -> Mx4:
@@ -471,8 +516,8 @@ class Context:
                                out: Optional[Sequence[Mx4]] = None):
         """gvq_mx4_quantize_aggregate; out: one mx4_slices() per node that receives what it would send."""
         self._sync_stream()
-        cp = _ptr_array([q.codes for q in out]) if out is not None else None
-        sp = _ptr_array([q.scales for q in out]) if out is not None else None
+        cp = (ctypes.c_void_p * len(out))(*[q.codes_ptr for q in out]) if out is not None else None
+        sp = (ctypes.c_void_p * len(out))(*[q.scales_ptr for q in out]) if out is not None else None
         _check(lib().gvq_mx4_quantize_aggregate(self._h, _ptr_array(g_nodes), len(g_nodes), node0, 1 if stochastic else 0,
                                                 seed, g_sum.data_ptr() if g_sum is not None else None, cp, sp),
                "gvq_mx4_quantize_aggregate")
@@ -480,8 +525,9 @@ class Context:
     def mx4_dequantize_aggregate(self, q_nodes: Sequence[Mx4], g_nodes_for_tails, g_sum):
         self._sync_stream()
         gp = _ptr_array(g_nodes_for_tails) if g_nodes_for_tails is not None else None
-        _check(lib().gvq_mx4_dequantize_aggregate(self._h, _ptr_array([q.codes for q in q_nodes]),
-                                                  _ptr_array([q.scales for q in q_nodes]), gp, len(q_nodes), g_sum.data_ptr()),
+        cp = (ctypes.c_void_p * len(q_nodes))(*[q.codes_ptr for q in q_nodes])
+        sp = (ctypes.c_void_p * len(q_nodes))(*[q.scales_ptr for q in q_nodes])
+        _check(lib().gvq_mx4_dequantize_aggregate(self._h, cp, sp, gp, len(q_nodes), g_sum.data_ptr()),
                "gvq_mx4_dequantize_aggregate")
 
     def flatten_layer(self, framework, flat, F, D, X):
