@@ -34,12 +34,15 @@ gvq_status gather_nodes(const T *const *src, int N, NodePtrs<const T> &dst, bool
     return GVQ_OK;
 }
 
+// Makes the context's device current, and the caller's again at the end; nothing to do where it is already.
 struct DeviceGuard {
     int prev = -1;
     bool ok = false;
     explicit DeviceGuard(int dev)
     {
-        if (cudaGetDevice(&prev) == cudaSuccess) ok = cudaSetDevice(dev) == cudaSuccess;
+        if (cudaGetDevice(&prev) != cudaSuccess) return;
+        if (prev == dev) { prev = -1; ok = true; }
+        else ok = cudaSetDevice(dev) == cudaSuccess;
     }
     ~DeviceGuard()
     {

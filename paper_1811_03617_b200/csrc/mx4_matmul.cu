@@ -305,7 +305,7 @@ template <typename T, int CG, int BN>
 cudaError_t launch_as(cudaStream_t st, int num_sms, const MmParams &prm)
 {
     using S = Shape<CG, BN>;
-    return launch_chained(mx4_matmul_kernel<T, CG, BN>, prm, CG * min(num_sms / CG, prm.tiles_m * prm.tiles_n), NTHREADS, S::SMEM, CG, st);
+    return launch_chained<mx4_matmul_kernel<T, CG, BN>>(prm, CG * min(num_sms / CG, prm.tiles_m * prm.tiles_n), NTHREADS, S::SMEM, CG, st);
 }
 template <int CG, int BN>
 cudaError_t launch_typed(cudaStream_t st, int num_sms, int dtype, const MmParams &prm)

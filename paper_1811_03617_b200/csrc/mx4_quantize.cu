@@ -332,8 +332,7 @@ cudaError_t launch_quantize_as(cudaStream_t st, const QuantParams &prm)
 {
     const unsigned grid = (unsigned)(prm.ct * tiles_of(prm.rows, 128));
     const size_t smem = COLS ? 128 * 128 * sizeof(T) + 128 : 0;
-    auto kernel = mx4_quantize_kernel<T, SR, ROWS, COLS>;
-    return ptx::launch_chained(kernel, prm, (int)grid, 256, smem, 1, st);
+    return ptx::launch_chained<mx4_quantize_kernel<T, SR, ROWS, COLS>>(prm, (int)grid, 256, smem, 1, st);
 }
 template <typename T, bool SR>
 cudaError_t launch_quantize_forms(cudaStream_t st, const QuantParams &prm)
@@ -387,11 +386,11 @@ cudaError_t launch_mx4_quantize_aggregate(cudaStream_t st, int d, int64_t S, con
         cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
     }
-    auto launch = [&](auto kernel) {
-        return ptx::launch_chained(kernel, prm, tiles.n_tiles, 256, 0, 1, st);
-    };
-    if (stochastic) return codes ? launch(mx4_quantize_aggregate_kernel<true, true>) : launch(mx4_quantize_aggregate_kernel<true, false>);
-    return codes ? launch(mx4_quantize_aggregate_kernel<false, true>) : launch(mx4_quantize_aggregate_kernel<false, false>);
+    const int n = tiles.n_tiles;
+    if (stochastic) return codes ? ptx::launch_chained<mx4_quantize_aggregate_kernel<true, true>>(prm, n, 256, 0, 1, st)
+                                 : ptx::launch_chained<mx4_quantize_aggregate_kernel<true, false>>(prm, n, 256, 0, 1, st);
+    return codes ? ptx::launch_chained<mx4_quantize_aggregate_kernel<false, true>>(prm, n, 256, 0, 1, st)
+                 : ptx::launch_chained<mx4_quantize_aggregate_kernel<false, false>>(prm, n, 256, 0, 1, st);
 }
 
 cudaError_t launch_mx4_dequantize(cudaStream_t st, int num_sms, const NodePtrs<const uint8_t> &codes,

@@ -696,6 +696,13 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
     if (warp == 1) tmem_dealloc<CG>(tmem, S::TMEM);
 }
 
+template <int PHASE, typename T>
+cudaError_t launch_tiling(cudaStream_t st, const ProductParams &prm, int runs)
+{
+    return prm.dev.pair ? launch_chained<product_kernel<PHASE, 2, T>>(prm, 2 * runs, Shape<2>::THREADS, Shape<2>::SMEM, 2, st)
+                        : launch_chained<product_kernel<PHASE, 1, T>>(prm, runs, Shape<1>::THREADS, Shape<1>::SMEM, 1, st);
+}
+
 }  // namespace
 
 cudaError_t launch_start(cudaStream_t st, const Device &dev, const ElementArgs &a)
@@ -704,9 +711,9 @@ cudaError_t launch_start(cudaStream_t st, const Device &dev, const ElementArgs &
     prm.dev = dev;
     prm.a = a;
     prm.mode = !a.momentum ? 0 : a.nesterov ? 2 : 1;
-    cudaError_t e = launch_chained(momentum_kernel, prm, dev.n_chunks, 256, 0, 1, st);
+    cudaError_t e = ptx::launch_chained<momentum_kernel>(prm, dev.n_chunks, 256, 0, 1, st);
     if (e != cudaSuccess) return e;
-    return launch_chained(normalise_kernel, prm, dev.n_chunks, 256, 0, 1, st);
+    return ptx::launch_chained<normalise_kernel>(prm, dev.n_chunks, 256, 0, 1, st);
 }
 
 cudaError_t launch_product(cudaStream_t st, const Device &dev, Phase phase, int step, const OutputArgs *out,
@@ -719,17 +726,13 @@ cudaError_t launch_product(cudaStream_t st, const Device &dev, Phase phase, int 
     prm.error_word = error_word;
     prm.wait_kcycles = wait_kcycles > 0 ? wait_kcycles : WAIT_KCYCLES_DEFAULT;
     prm.test_drop = test_drop;
-    auto launch = [&](auto pair, auto solo) {
-        const int runs = dev.run[phase].runs;
-        return dev.pair ? launch_chained(pair, prm, 2 * runs, Shape<2>::THREADS, Shape<2>::SMEM, 2, st)
-                        : launch_chained(solo, prm, runs, Shape<1>::THREADS, Shape<1>::SMEM, 1, st);
-    };
-    if (phase == kGram) return launch(product_kernel<kGram, 2>, product_kernel<kGram, 1>);
-    if (phase == kPoly) return launch(product_kernel<kPoly, 2>, product_kernel<kPoly, 1>);
-    if (step < kSteps - 1) return launch(product_kernel<kApply, 2>, product_kernel<kApply, 1>);
-    if (out->dtype == GVQ_F32) return launch(product_kernel<kLast, 2, float>, product_kernel<kLast, 1, float>);
-    if (out->dtype == GVQ_BF16) return launch(product_kernel<kLast, 2, __nv_bfloat16>, product_kernel<kLast, 1, __nv_bfloat16>);
-    return launch(product_kernel<kLast, 2, __half>, product_kernel<kLast, 1, __half>);
+    const int runs = dev.run[phase].runs;
+    if (phase == kGram) return launch_tiling<kGram, float>(st, prm, runs);
+    if (phase == kPoly) return launch_tiling<kPoly, float>(st, prm, runs);
+    if (step < kSteps - 1) return launch_tiling<kApply, float>(st, prm, runs);
+    if (out->dtype == GVQ_F32) return launch_tiling<kLast, float>(st, prm, runs);
+    if (out->dtype == GVQ_BF16) return launch_tiling<kLast, __nv_bfloat16>(st, prm, runs);
+    return launch_tiling<kLast, __half>(st, prm, runs);
 }
 
 }  // namespace ortho

@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 namespace gvq {
 namespace ptx {
 
@@ -308,13 +310,21 @@ __device__ __forceinline__ void tmem_ld32_wait(uint32_t taddr, float (&v)[32])
 }
 
 // Host: launches a kernel that begins with launch_dependents() and grid_dependency_wait(), so that its start overlaps the
-// end of the stream's last kernel; cluster: CTAs of a cluster (1: none).
-template <typename K, typename P>
-inline cudaError_t launch_chained(K kernel, const P &prm, int grid, int threads, size_t smem, int cluster, cudaStream_t st)
+// end of the stream's last kernel; cluster: CTAs of a cluster (1: none).  A kernel's shared-memory limit is raised at its
+// first launch on a device.
+template <auto Kernel, typename P>
+cudaError_t launch_chained(const P &prm, int grid, int threads, size_t smem, int cluster, cudaStream_t st)
 {
     if (smem > 48 * 1024) {
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        static std::atomic<uint64_t> raised{0};
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
         if (e != cudaSuccess) return e;
+        if (dev >= 64 || !(raised.load(std::memory_order_relaxed) >> dev & 1)) {
+            e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (e != cudaSuccess) return e;
+            if (dev < 64) raised.fetch_or(1ull << dev, std::memory_order_relaxed);
+        }
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
@@ -330,7 +340,7 @@ inline cudaError_t launch_chained(K kernel, const P &prm, int grid, int threads,
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, prm);
+    return cudaLaunchKernelEx(&cfg, Kernel, prm);
 }
 
 }  // namespace ptx
