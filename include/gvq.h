@@ -539,7 +539,7 @@ gvq_status gvq_mx4_dequantize_aggregate(gvq_ctx *ctx, const uint8_t *const *code
    rounding to w's type once.  A matrix that is zero moves nothing (X = 0); one that holds a NaN or an infinity gives NaN
    or zero for its own layer, as the formula does, and touches no other.
    rows, cols: HOST arrays [n_layers], rows[l] * cols[l] = layer_len[l], or both 0: the layer is left alone; the shorter
-   side is at most 32768.  scales_opt: NULL or HOST [n_layers].  workspace: device, 256-byte aligned,
+   side is at most 32768, the longer one below 2^20.  scales_opt: NULL or HOST [n_layers].  workspace: device, 256-byte aligned,
    gvq_ortho_workspace_bytes() bytes (-1 on bad sizes), owned by the caller and kept while the plan lives; its contents
    carry nothing from one call to the next.  The plan keeps tables in device memory of its own (one allocation at create).
    Its calls use its context's stream, allocate nothing and can be captured; after gvq_destroy(ctx) the plan can only be

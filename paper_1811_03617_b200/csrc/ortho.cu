@@ -62,8 +62,8 @@ __global__ void __launch_bounds__(256) momentum_kernel(const StartParams prm)
     ptx::grid_dependency_wait();
     const Chunk ch = prm.dev.chunks[blockIdx.x];
     const Matrix &mx = prm.dev.mats[ch.matrix];
-    const int64_t total = (int64_t)mx.rows * mx.cols, begin = (int64_t)ch.index * kChunk;
-    const int n = (int)min((int64_t)kChunk, total - begin);
+    const int64_t total = (int64_t)mx.rows * mx.cols, begin = (int64_t)ch.index * prm.dev.chunk;
+    const int n = (int)min((int64_t)prm.dev.chunk, total - begin);
     const float *g = prm.a.g + mx.off + begin;        // 16-byte aligned: layers start at multiples of 4
     float *mo = prm.mode ? prm.a.momentum + mx.off + begin : nullptr;
     float sum = 0.0f;
@@ -124,50 +124,36 @@ __global__ void __launch_bounds__(256) normalise_kernel(const StartParams prm)
 #pragma unroll
     for (int i = 0; i < 8; ++i) s += norm_s[i];
     const float f = mx.sx / ((float)sqrt(s) + kEps);
-    const int64_t total = (int64_t)mx.rows * mx.cols, begin = (int64_t)ch.index * kChunk;
-    const int n = (int)min((int64_t)kChunk, total - begin);
+    const int64_t total = (int64_t)mx.rows * mx.cols, begin = (int64_t)ch.index * prm.dev.chunk;
+    const int n = (int)min((int64_t)prm.dev.chunk, total - begin);
     const float *g = prm.a.g + mx.off + begin;
     const float *mo = prm.mode ? prm.a.momentum + mx.off + begin : nullptr;
+    auto row_of = [&](int64_t at) { return (int64_t)__umul64hi((uint64_t)at << 2, mx.by_cols); };
+    if ((mx.cols & 3) == 0) {       // (so n and every row hold whole quads)
 #pragma unroll 4
-    for (int i = threadIdx.x * 4; i < n; i += 1024) {
-        float gv[4], mv[4] = {0.f, 0.f, 0.f, 0.f};
-        const bool full = i + 4 <= n;
-        if (full) {
-            const float4 q = __ldcs(reinterpret_cast<const float4 *>(g + i));
-            gv[0] = q.x; gv[1] = q.y; gv[2] = q.z; gv[3] = q.w;
-            if (prm.mode) {
-                const float4 m = __ldcs(reinterpret_cast<const float4 *>(mo + i));
-                mv[0] = m.x; mv[1] = m.y; mv[2] = m.z; mv[3] = m.w;
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                gv[e] = i + e < n ? g[i + e] : 0.0f;
-                if (prm.mode && i + e < n) mv[e] = mo[i + e];
-            }
+        for (int i = threadIdx.x * 4; i < n; i += 1024) {
+            const float4 gq = __ldcs(reinterpret_cast<const float4 *>(g + i));
+            const float4 mq = prm.mode ? __ldcs(reinterpret_cast<const float4 *>(mo + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            const float x[4] = {direction(gq.x, mq.x, prm.a.beta, prm.mode) * f, direction(gq.y, mq.y, prm.a.beta, prm.mode) * f,
+                                direction(gq.z, mq.z, prm.a.beta, prm.mode) * f, direction(gq.w, mq.w, prm.a.beta, prm.mode) * f};
+            uint2 hi, lo;
+            hi.x = pack2<__half>(x[0], x[1]);
+            hi.y = pack2<__half>(x[2], x[3]);
+            const float2 a = unpack_half2(hi.x), b = unpack_half2(hi.y);
+            lo.x = pack2<__half>(x[0] - a.x, x[1] - a.y);
+            lo.y = pack2<__half>(x[2] - b.x, x[3] - b.y);
+            const int64_t at = begin + i, row = row_of(at), dst = row * mx.ldx + (at - row * mx.cols);
+            *reinterpret_cast<uint2 *>(mx.x[0] + dst) = hi;
+            *reinterpret_cast<uint2 *>(mx.lo + dst) = lo;
         }
-        __half hi[4], lo[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float x = direction(gv[e], mv[e], prm.a.beta, prm.mode) * f;
-            hi[e] = __float2half_rn(x);
-            lo[e] = __float2half_rn(x - __half2float(hi[e]));
-        }
-        const int64_t at = begin + i;
-        const int64_t row = at / mx.cols;
-        int col = (int)(at - row * mx.cols);
-        int64_t dst = row * mx.ldx + col;
-        if (full && (mx.cols & 3) == 0) {
-            uint2 q;
-            memcpy(&q, hi, 8); *reinterpret_cast<uint2 *>(mx.x[0] + dst) = q;
-            memcpy(&q, lo, 8); *reinterpret_cast<uint2 *>(mx.lo + dst) = q;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (i + e < n) { mx.x[0][dst] = hi[e]; mx.lo[dst] = lo[e]; }
-                ++dst;
-                if (++col == mx.cols) { col = 0; dst += mx.ldx - mx.cols; }
-            }
+    } else {                        // an entry a lane: rows begin anywhere
+#pragma unroll 4
+        for (int i = threadIdx.x; i < n; i += 256) {
+            const float x = direction(__ldcs(g + i), prm.mode ? __ldcs(mo + i) : 0.0f, prm.a.beta, prm.mode) * f;
+            const __half hi = __float2half_rn(x);
+            const int64_t at = begin + i, row = row_of(at), dst = row * mx.ldx + (at - row * mx.cols);
+            mx.x[0][dst] = hi;
+            mx.lo[dst] = __float2half_rn(x - __half2float(hi));
         }
     }
 }
@@ -374,6 +360,7 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CG == 2 ? (int)cluster_rank() : 0;
+    launch_dependents();
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::STAGES; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(d_full + i, 1); mbar_init(d_empty + i, CG * S::NEPI); }
@@ -386,29 +373,48 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
     if (CG == 2) cluster_sync(); else __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    launch_dependents();
-    grid_dependency_wait();      // what the previous launch wrote is visible from here on
     bool failed = false;
-    // this CTA's (pair's) run of tiles
+    // this CTA's (pair's) run of tiles; the plan's tables do not change, so they are read before the wait for the last launch
     constexpr bool APPLY = PHASE == kApply || PHASE == kLast;
     const Tile *tiles = prm.dev.run[PHASE].tiles;
     const int t_begin = prm.dev.run[PHASE].start[blockIdx.x / CG], t_end = prm.dev.run[PHASE].start[blockIdx.x / CG + 1];
 
     if (warp == 0) {
         if (lane == 0) {
-            fence_proxy_async_global();      // what plain stores of the previous launch wrote is read by TMA
-            uint32_t c = 0;
-            for (int t = t_begin; t < t_end && !failed; ++t) {
+            // a tile's geometry, looked up while the one before it is loaded
+            struct Loads {
+                const CUtensorMap *a, *b;
+                int m0, n0, k0, k1, a_left, b_left;
+                bool a_mn, b_mn;
+            };
+            auto loads_of = [&](int t) {
                 const Tile tile = tiles[t];
                 const Work w = work_of<PHASE>(prm.dev.mats[tile.matrix], prm.step);
-                const CUtensorMap *ma = prm.dev.maps + (size_t)tile.matrix * kMaps + w.a_map;
-                const CUtensorMap *mb = prm.dev.maps + (size_t)tile.matrix * kMaps + w.b_map;
+                Loads l;
+                l.a = prm.dev.maps + (size_t)tile.matrix * kMaps + w.a_map;
+                l.b = prm.dev.maps + (size_t)tile.matrix * kMaps + w.b_map;
                 // a pair's columns are split in halves of a multiple of 8 (the last tile's may be narrow)
                 const int half_n = CG == 2 ? min(S::BN, (w.N - tile.tn * S::BN + 15) / 16 * 16) / 2 : 0;
-                const int m0 = tile.tm * 128 * CG + 128 * rank, n0 = tile.tn * S::BN + half_n * rank;
+                l.m0 = tile.tm * 128 * CG + 128 * rank;
+                l.n0 = tile.tn * S::BN + half_n * rank;
                 // steps of the contraction left of the diagonal's block of a symmetric operand's rows
-                const int a_left = w.a_sym ? m0 / S::BLOCK * S::BLOCK : 0, b_left = w.b_sym ? tile.tn * S::BN / S::BLOCK * S::BLOCK : 0;
-                for (int st = tile.k0; st < tile.k1; ++st, ++c) {
+                l.a_left = w.a_sym ? l.m0 / S::BLOCK * S::BLOCK : 0;
+                l.b_left = w.b_sym ? tile.tn * S::BN / S::BLOCK * S::BLOCK : 0;
+                l.a_mn = w.a_mn;
+                l.b_mn = w.b_mn;
+                l.k0 = tile.k0;
+                l.k1 = tile.k1;
+                return l;
+            };
+            Loads l = loads_of(t_begin);
+            asm volatile("prefetch.tensormap [%0];" ::"l"(l.a));
+            asm volatile("prefetch.tensormap [%0];" ::"l"(l.b));
+            grid_dependency_wait();          // what the previous launch wrote is visible from here on
+            fence_proxy_async_global();      // and read by TMA, plain stores included
+            uint32_t c = 0;
+            for (int t = t_begin; t < t_end && !failed; ++t) {
+                const Loads next = loads_of(min(t + 1, t_end - 1));
+                for (int st = l.k0; st < l.k1; ++st, ++c) {
                     const uint32_t s = c % S::STAGES;
                     if (!mbar_poll(empty + s, ((c / S::STAGES) & 1) ^ 1, abort_flag)) { failed = true; break; }
                     if (prm.test_drop && blockIdx.x == 0 && c == 0) continue;   // test hook: this stage never arrives
@@ -421,10 +427,11 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                         else tma_load_2d(to, map, mn ? at : k, mn ? k : at, full + s);
                     };
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) load(dst + i * BOX, ma, w.a_mn || k < a_left, m0 + 64 * i);
+                    for (int i = 0; i < 2; ++i) load(dst + i * BOX, l.a, l.a_mn || k < l.a_left, l.m0 + 64 * i);
 #pragma unroll
-                    for (int i = 0; i < S::NB; ++i) load(dst + S::A_BYTES + i * BOX, mb, w.b_mn || k < b_left, n0 + 64 * i);
+                    for (int i = 0; i < S::NB; ++i) load(dst + S::A_BYTES + i * BOX, l.b, l.b_mn || k < l.b_left, l.n0 + 64 * i);
                 }
+                l = next;
             }
             if (failed && rank == 0) {   // give the copies already in flight a bounded chance to land before the CTA exits
                 for (uint32_t i = c > S::STAGES ? c - S::STAGES : 0; i < c; ++i)
@@ -518,6 +525,7 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
             }
         };
         Place here = place(t_begin);
+        grid_dependency_wait();      // (before anything that another launch writes is read, or written)
         if (PHASE == kApply && read_lo) fetch_lo(here, here.c0);
         if (PHASE == kLast) fetch_weights(here, here.c0);
         uint32_t u = 0, stores = 0;

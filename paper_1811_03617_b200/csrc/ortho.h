@@ -20,13 +20,15 @@ constexpr float kGramScale = 256.0f;
 
 // Tiles of the products (ortho.cu): a pair of CTAs has 256 x kPairN, a CTA alone 128 x kSoloN.
 constexpr int kPairN = 256, kSoloN = 64;
-constexpr int kChunk = 8192;     // entries of a chunk of the element-wise passes
+// Entries of a chunk of the element-wise passes (a multiple of 1024): small plans take shorter ones, to have work for all SMs.
+constexpr int kMinChunk = 1024, kMaxChunk = 8192;
 
 // One matrix [rows][cols] of the flat gradient.  r <= c its shorter and longer side.
 struct Matrix {
     int32_t rows, cols, r, c, tall, ldx, ldr;
     int32_t chunk0, n_chunks;        // its chunks in the element-wise passes
     int64_t off;                     // in the flat buffers
+    uint64_t by_cols;                // floor(2^62 / cols) + 1: n / cols = (4 n * by_cols) >> 64 for n < 2^40, cols < 2^20
     // X (two buffers, in turn), X's low halves; A, b I + c A, P; rows ldx or ldr entries apart
     __half *x[2], *lo, *gram, *factor, *poly;
     float sx;                        // scale of X in half precision
@@ -54,6 +56,7 @@ struct Device {
     Run run[4];                      // of each phase
     int pair;                        // which tiling the tiles are of
     const Chunk *chunks;
+    int chunk;                       // entries of one
     int n_chunks;
     float *partial;                  // [n_chunks] sums of squares
     float *parts;                    // sums of parts of a contraction, pieces of 32 rows x 64 columns

@@ -23,7 +23,10 @@ namespace {
 constexpr size_t kAlign = 256;
 constexpr int kPartStages = 6, kMaxParts = 8;   // a part of a contraction: at least so many stages, at most so many parts
 constexpr int kTileCost = 3;      // what a tile costs beyond its contraction, in stages of 64 steps
-constexpr int kPairTiles = 148;   // fewer 256 x 256 tiles than this: 128 x 64 tiles
+// Pairs of CTAs on 256 x 256 tiles from this many multiply-adds of one X P on, 128 x 64 tiles below.  Measured on either side,
+// us per call: 1280 x 1280 (2.1e9) 231 / 186, twice 512 x 4608 (2.4e9) 245 / 189, 1500 x 1500 (3.4e9) 259 / 275, four
+// 1024 x 1024 (4.3e9) 215 / 265, 2048 x 2048 (8.6e9) 298 / 448.
+constexpr int64_t kPairWork = 3'300'000'000;
 size_t up(size_t n) { return (n + kAlign - 1) & ~(kAlign - 1); }
 int up32(int n) { return (n + 31) & ~31; }     // rows of the work arrays: whole pieces of 32 entries
 
@@ -43,10 +46,11 @@ gvq_status lay_out(int n_layers, const int64_t *off, const int64_t *len, const i
         Matrix m{};
         m.rows = rows[l]; m.cols = cols[l];
         m.r = std::min(m.rows, m.cols); m.c = std::max(m.rows, m.cols);
-        if (m.r > 32768) return GVQ_ERR_SHAPE;                    // r x r products beyond any layer
+        if (m.r > 32768 || m.c >= 1 << 20) return GVQ_ERR_SHAPE;  // beyond any layer
         m.tall = m.rows > m.cols;
         m.ldx = up32(m.cols); m.ldr = up32(m.r);
         m.off = off[l];
+        m.by_cols = ((uint64_t)1 << 62) / (uint64_t)m.cols + 1;
         // entries of X have an rms of 1 / sqrt(r c) at first and 1 / sqrt(c) at last: about 1 / sqrt(r) to 1 when scaled
         m.sx = std::exp2(std::round(0.5f * std::log2((float)m.c)));
         m.scale = scales ? scales[l] : std::sqrt(std::max(1.0f, (float)m.rows / (float)m.cols));
@@ -166,6 +170,9 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
         std::vector<CUtensorMap> maps((size_t)n * kMaps);
         std::vector<Tile> sym, apply;
         std::vector<Chunk> chunks;
+        int64_t entries = 0;
+        for (const Matrix &m : sz.mats) entries += (int64_t)m.rows * m.cols;
+        const int chunk = (int)std::min<int64_t>(kMaxChunk, std::max<int64_t>(kMinChunk, entries / (4 * ctx->num_sms) / kMinChunk * kMinChunk));
         for (int i = 0; i < n; ++i) {
             Matrix &m = sz.mats[i];
             CUtensorMap *mp = &maps[(size_t)i * kMaps];
@@ -179,18 +186,15 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
                 !map(kFactorOut, m.factor, 32, true) || !map(kPolyOut, m.poly, 32, true))
                 return GVQ_ERR_CUDA;
             m.chunk0 = (int)chunks.size();
-            m.n_chunks = (int)(((int64_t)m.rows * m.cols + kChunk - 1) / kChunk);
+            m.n_chunks = (int)(((int64_t)m.rows * m.cols + chunk - 1) / chunk);
             for (int k = 0; k < m.n_chunks; ++k) chunks.push_back({i, k});
         }
-        // Which tiling: pairs of CTAs on 256 x 256 tiles where there are enough of them.
         std::vector<Tile> gram;
-        bool pair = false;
-        for (int attempt = 0; attempt < 2; ++attempt) {
-            pair = attempt == 0;
+        int64_t apply_work = 0;
+        for (const Matrix &m : sz.mats) apply_work += (int64_t)m.r * m.r * m.c;
+        const bool pair = apply_work >= kPairWork;
+        {
             const int64_t bm = pair ? 256 : 128, bn = pair ? kPairN : kSoloN;
-            gram.clear();
-            sym.clear();
-            apply.clear();
             for (int i = 0; i < n; ++i) {
                 const Matrix &m = sz.mats[i];
                 const int kr = (m.r + 63) / 64, kc = (m.c + 63) / 64;
@@ -203,7 +207,6 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
                 for (int tm = 0; tm * bm < m.rows; ++tm)
                     for (int tn = 0; tn * bn < m.cols; ++tn) apply.push_back({i, tm, tn, 0, kr, 0, 1, 0});
             }
-            if (pair && (int)apply.size() >= kPairTiles) break;
         }
         const int units = pair ? ctx->num_sms / 2 : ctx->num_sms;
         int slots = 0;
@@ -254,6 +257,7 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
         d.partial = reinterpret_cast<float *>(t + o_p);
         d.parts = reinterpret_cast<float *>(t + o_q);
         d.pair = pair;
+        d.chunk = chunk;
         *out = p;
         return GVQ_OK;
     } catch (const std::bad_alloc &) {
