@@ -74,23 +74,25 @@ __device__ __forceinline__ uint64_t row_word(uint64_t seed_w, int64_t row)
 {
     return mix64(seed_w ^ (0xD1B54A32D192ED03ull * (uint64_t)(row + 1)));
 }
-// 32 random bits for the columns 2p and 2p + 1 of a row (low and high half).
-__device__ __forceinline__ uint32_t pair_bits(uint64_t h, uint32_t p)
+// The columns 2p and 2p + 1 of a row have the low and the high half of a 32-bit word x ^ (x >> 16); this is x.
+__device__ __forceinline__ uint32_t pair_word(uint64_t h, uint32_t p)
 {
     uint32_t x = (uint32_t)(h >> 32) ^ ((uint32_t)h + 0x9E3779B9u * (p + 1));
     x ^= x >> 16; x *= 0x7FEB352Du;
-    x ^= x >> 15; x *= 0x846CA68Bu;
-    return x ^ (x >> 16);
+    x ^= x >> 15;
+    return x * 0x846CA68Bu;
 }
-// Stochastic rounding of r = |x| / scale to the grid: (floor(65536 r / step) + u) >> 16 steps, u6 = u << 6.
-// For r >= 1 a step is bit 22 of r's float pattern, so u is added 16 places below it and the rest is cut off; below 1,
-// where the grid keeps the step 0.5 of [1, 2), the same is done to r + 1 (rounded toward zero, which keeps every bit
-// that floor(65536 r / step) depends on).
-__device__ __forceinline__ float round_up_or_down(float r, uint32_t u6)
+// Stochastic rounding of r = |x| / scale to the grid: (floor(65536 r / step) + u) >> 16 steps.  For r >= 1 a step is bit 22
+// of r's float pattern, so u is added 16 places below it and the rest is cut off; below 1, where the grid keeps the
+// step 0.5 of [1, 2), the same is done to r + 1 (rounded toward zero, which keeps every bit that floor(65536 r / step)
+// depends on).  Integer and comparison instructions run at half the rate of fp32 arithmetic and are what this costs: the
+// comparison gives 1.0 or 0.0 itself, and the halves of a word are taken from its last mixing step.
+__device__ __forceinline__ float round_up_or_down(float r, uint32_t u)
 {
-    const float c = r < 1.0f ? 1.0f : 0.0f;
+    float c;
+    asm("set.lt.f32.f32 %0, %1, 0f3F800000;" : "=f"(c) : "f"(r));
     const float t = __fadd_rz(r, c);
-    return __uint_as_float((__float_as_uint(t) + u6) & 0xFFC00000u) - c;
+    return __uint_as_float((__float_as_uint(t) + u * 64u) & 0xFFC00000u) - c;
 }
 __device__ __forceinline__ float with_sign(float mag, float x)
 {
@@ -104,9 +106,9 @@ __device__ __forceinline__ void grid8(float (&v)[8], float inv, uint64_t h, uint
     if (SR) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t w = pair_bits(h, p0 + i);
-            v[2 * i] = with_sign(round_up_or_down(fabsf(v[2 * i]) * inv, (w << 6) & 0x3FFFC0u), v[2 * i]);
-            v[2 * i + 1] = with_sign(round_up_or_down(fabsf(v[2 * i + 1]) * inv, (w >> 10) & 0x3FFFC0u), v[2 * i + 1]);
+            const uint32_t x = pair_word(h, p0 + i), y = x >> 16;
+            v[2 * i] = with_sign(round_up_or_down(fabsf(v[2 * i]) * inv, (x ^ y) & 0xFFFFu), v[2 * i]);
+            v[2 * i + 1] = with_sign(round_up_or_down(fabsf(v[2 * i + 1]) * inv, y), v[2 * i + 1]);
         }
     } else {
 #pragma unroll

@@ -108,7 +108,6 @@ gvq_status gvq_mx4_quantize_aggregate(gvq_ctx *ctx, const float *const *g_nodes,
     GVQ_CUDA(ctx, launch_mx4_quantize_aggregate(ctx->stream, ctx->d, ctx->S, ctx->decompress_tiles, ctx->lt, g, N, node0,
                                                 rounding == GVQ_ROUND_STOCHASTIC, seed, g_sum, codes_nodes_opt ? &c : nullptr,
                                                 codes_nodes_opt ? &s : nullptr));
-    if (ctx->has_tails && g_sum) GVQ_CUDA(ctx, launch_tail_sum(ctx->stream, ctx->lt, ctx->d, g, N, g_sum));
     return GVQ_OK;
 }
 

@@ -172,16 +172,29 @@ struct AggParams {
     NodePtrs<const float> g;
     NodePtrs<uint8_t> codes, scales;
     float *out;                 // may be null
+    int n_tiles, n_tails;       // the CTAs after the tiles' sum the tails
+    const int64_t *tail_off;
+    const int32_t *tail_len;
 };
 
 // A quad of lanes takes a block of a slice and goes through the nodes: eight entries a lane, read once, quantized, and
 // what the codes stand for added (fp32, n ascending; code times power of two is exact, so the only rounding is the
-// sum's).  OUT: the codes and scale bytes are wanted.
+// sum's).  OUT: the codes and scale bytes are wanted.  Of four nodes' row words each lane of the quad mixes one.
 template <bool SR, bool OUT>
 __global__ void __launch_bounds__(256) mx4_quantize_aggregate_kernel(const __grid_constant__ AggParams prm)
 {
     ptx::launch_dependents();
     ptx::grid_dependency_wait();
+    if ((int)blockIdx.x >= prm.n_tiles) {
+        const int tail = blockIdx.x - prm.n_tiles, len = prm.tail_len[tail];
+        const int64_t off = prm.tail_off[tail];
+        for (int e = threadIdx.x; e < len; e += 256) {
+            float acc = prm.g.p[0][off + e];
+            for (int n = 1; n < prm.n_nodes; ++n) acc += prm.g.p[n][off + e];
+            prm.out[off + e] = acc;
+        }
+        return;
+    }
     const int t = blockIdx.x, layer = prm.tile_layer[t], row0 = prm.tile_row0[t];
     const int rows = min(kDecompressRows, prm.layer_S[layer] - row0);
     const int d = prm.d, nb = (d + kBlock - 1) / kBlock;
@@ -213,6 +226,8 @@ __global__ void __launch_bounds__(256) mx4_quantize_aggregate_kernel(const __gri
                     if (in1) x[u][1] = __ldcs(src + 1);
                 }
             }
+            uint64_t h_own = 0;
+            if (SR) h_own = row_word(prm.seed_w[min(n0 + lane4, prm.n_nodes - 1)], slice);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (n0 + u >= prm.n_nodes) break;
@@ -223,7 +238,7 @@ __global__ void __launch_bounds__(256) mx4_quantize_aggregate_kernel(const __gri
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] = 0.0f;
                 }
-                const uint64_t h = SR ? row_word(prm.seed_w[n], slice) : 0;
+                const uint64_t h = SR ? __shfl_sync(0xffffffffu, h_own, (threadIdx.x & 28) + u) : 0;
                 grid8<SR>(v, inv_scale(min(s, 253u)), h, (uint32_t)(j >> 1));
                 if (OUT || !SR) {
                     const uint32_t code = codes8(v);
@@ -370,23 +385,26 @@ cudaError_t launch_mx4_quantize_aggregate(cudaStream_t st, int d, int64_t S, con
                                           uint64_t seed, float *out, const NodePtrs<uint8_t> *codes,
                                           const NodePtrs<uint8_t> *scales)
 {
-    if (tiles.n_tiles == 0) return cudaSuccess;
     AggParams prm;
+    prm.n_tiles = tiles.n_tiles;
+    prm.n_tails = out ? lt.n_tails : 0;
+    if (prm.n_tiles + prm.n_tails == 0) return cudaSuccess;
+    prm.tail_off = lt.tail_off; prm.tail_len = lt.tail_len;
     prm.d = d; prm.n_nodes = n_nodes;
+    for (int n = 0; n < n_nodes; ++n) prm.seed_w[n] = seed_word(seed, node0 + (uint32_t)n);
     for (int n = 0; n < GVQ_MAX_NODES; ++n) {
-        prm.seed_w[n] = seed_word(seed, node0 + (uint32_t)n);
         prm.codes.p[n] = codes ? codes->p[n] : nullptr;
         prm.scales.p[n] = scales ? scales->p[n] : nullptr;
     }
     prm.tile_layer = tiles.layer; prm.tile_row0 = tiles.row0; prm.layer_S = lt.S;
     prm.layer_off = lt.off; prm.layer_soff = lt.soff;
     prm.g = g; prm.out = out;
-    if (codes) {
+    if (codes && S > 0) {
         mx4_clear_scale_padding_kernel<<<dim3(32, n_nodes), 256, 0, st>>>(prm.scales, S, (d + kBlock - 1) / kBlock);
         cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
     }
-    const int n = tiles.n_tiles;
+    const int n = prm.n_tiles + prm.n_tails;
     if (stochastic) return codes ? ptx::launch_chained<mx4_quantize_aggregate_kernel<true, true>>(prm, n, 256, 0, 1, st)
                                  : ptx::launch_chained<mx4_quantize_aggregate_kernel<true, false>>(prm, n, 256, 0, 1, st);
     return codes ? ptx::launch_chained<mx4_quantize_aggregate_kernel<false, true>>(prm, n, 256, 0, 1, st)
