@@ -158,7 +158,7 @@ cudaError_t launch_mx4_quantize(cudaStream_t st, const void *x, int dtype, int64
                                 uint8_t *codes_t, uint8_t *scales_t);
 // All nodes' full slices (tiles of kDecompressRows slices) and the sum of what their codes stand for, tails summed as they
 // are; out may be null.
-cudaError_t launch_mx4_quantize_aggregate(cudaStream_t st, int d, int64_t S, const TileTable &tiles, const LayerTables &lt,
+cudaError_t launch_mx4_quantize_aggregate(cudaStream_t st, int num_sms, int d, int64_t S, const TileTable &tiles, const LayerTables &lt,
                                           const NodePtrs<const float> &g, int n_nodes, uint32_t node0, bool stochastic,
                                           uint64_t seed, float *out, const NodePtrs<uint8_t> *codes,
                                           const NodePtrs<uint8_t> *scales);

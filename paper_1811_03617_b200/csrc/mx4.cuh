@@ -115,6 +115,15 @@ __device__ __forceinline__ void grid8(float (&v)[8], float inv, uint64_t h, uint
         for (int i = 0; i < 8; ++i) v[i] *= inv;
     }
 }
+// A block without a value (s = 255) has codes 0.  Kept as a branch: it is hardly ever taken, and eight selects are not free.
+__device__ __forceinline__ void clear_invalid(float (&v)[8], uint32_t s)
+{
+    if (s == 255u) {
+        asm volatile("");
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+    }
+}
 __device__ __forceinline__ float quad_max(float m)
 {
     m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, 1));

@@ -105,7 +105,7 @@ gvq_status gvq_mx4_quantize_aggregate(gvq_ctx *ctx, const float *const *g_nodes,
         if ((st = gather(codes_nodes_opt, N, c)) != GVQ_OK || (st = gather(scales_nodes_opt, N, s)) != GVQ_OK) return st;
     }
     DeviceGuard guard(ctx->device);
-    GVQ_CUDA(ctx, launch_mx4_quantize_aggregate(ctx->stream, ctx->d, ctx->S, ctx->decompress_tiles, ctx->lt, g, N, node0,
+    GVQ_CUDA(ctx, launch_mx4_quantize_aggregate(ctx->stream, ctx->num_sms, ctx->d, ctx->S, ctx->decompress_tiles, ctx->lt, g, N, node0,
                                                 rounding == GVQ_ROUND_STOCHASTIC, seed, g_sum, codes_nodes_opt ? &c : nullptr,
                                                 codes_nodes_opt ? &s : nullptr));
     return GVQ_OK;

@@ -100,10 +100,7 @@ __global__ void __launch_bounds__(256) mx4_quantize_kernel(const QuantParams prm
                 const uint32_t s = scale_byte(amax);
                 uint64_t h = 0;
                 if (SR) h = __shfl_sync(0xffffffffu, h_own, rl & 15);
-                if (s == 255u) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-                }
+                clear_invalid(v, s);
                 grid8<SR>(v, inv_scale(min(s, 253u)), h, (uint32_t)((c0 + cl) >> 1));
                 const int64_t r = r0 + rl, b = (c0 + cl) >> 5;
                 if (r < prm.rows && b < blocks(prm.cols))
@@ -144,7 +141,8 @@ __global__ void __launch_bounds__(256) mx4_quantize_kernel(const QuantParams prm
                 for (int o = 0; o < 4; ++o) {
                     float v[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = s == 255u ? 0.0f : entry(8 * o + e);
+                    for (int e = 0; e < 8; ++e) v[e] = entry(8 * o + e);
+                    clear_invalid(v, s);
                     grid8<SR>(v, inv, h, (uint32_t)((r0 + blk * 32 + 8 * o) >> 1));
                     code[o] = codes8(v);
                 }
@@ -173,6 +171,7 @@ struct AggParams {
     NodePtrs<uint8_t> codes, scales;
     float *out;                 // may be null
     int n_tiles, n_tails;       // the CTAs after the tiles' sum the tails
+    int shares;                 // CTAs that share a tile's rounds, where there are few tiles
     const int64_t *tail_off;
     const int32_t *tail_len;
 };
@@ -181,12 +180,12 @@ struct AggParams {
 // what the codes stand for added (fp32, n ascending; code times power of two is exact, so the only rounding is the
 // sum's).  OUT: the codes and scale bytes are wanted.  Of four nodes' row words each lane of the quad mixes one.
 template <bool SR, bool OUT>
-__global__ void __launch_bounds__(256) mx4_quantize_aggregate_kernel(const __grid_constant__ AggParams prm)
+__global__ void __launch_bounds__(256, 4) mx4_quantize_aggregate_kernel(const __grid_constant__ AggParams prm)
 {
     ptx::launch_dependents();
     ptx::grid_dependency_wait();
-    if ((int)blockIdx.x >= prm.n_tiles) {
-        const int tail = blockIdx.x - prm.n_tiles, len = prm.tail_len[tail];
+    if ((int)blockIdx.x >= prm.n_tiles * prm.shares) {
+        const int tail = blockIdx.x - prm.n_tiles * prm.shares, len = prm.tail_len[tail];
         const int64_t off = prm.tail_off[tail];
         for (int e = threadIdx.x; e < len; e += 256) {
             float acc = prm.g.p[0][off + e];
@@ -195,7 +194,7 @@ __global__ void __launch_bounds__(256) mx4_quantize_aggregate_kernel(const __gri
         }
         return;
     }
-    const int t = blockIdx.x, layer = prm.tile_layer[t], row0 = prm.tile_row0[t];
+    const int t = blockIdx.x / prm.shares, share = blockIdx.x - t * prm.shares, layer = prm.tile_layer[t], row0 = prm.tile_row0[t];
     const int rows = min(kDecompressRows, prm.layer_S[layer] - row0);
     const int d = prm.d, nb = (d + kBlock - 1) / kBlock;
     const int64_t base = prm.layer_off[layer] + (int64_t)row0 * d, slice0 = prm.layer_soff[layer] + row0;
@@ -203,7 +202,7 @@ __global__ void __launch_bounds__(256) mx4_quantize_aggregate_kernel(const __gri
     const int lane4 = threadIdx.x & 3;
     // every thread of a warp makes the same number of rounds: the shuffles below need the whole quad
     const int n_items = rows * nb, rounds = (n_items + 63) / 64;
-    for (int it = 0; it < rounds; ++it) {
+    for (int it = share; it < rounds; it += prm.shares) {
         const int item = it * 64 + (threadIdx.x >> 2);
         const bool in = item < n_items;
         const int row = in ? item / nb : 0, b = in ? item - row * nb : 0;
@@ -234,10 +233,7 @@ __global__ void __launch_bounds__(256) mx4_quantize_aggregate_kernel(const __gri
                 const int n = n0 + u;
                 float v[8] = {x[u][0].x, x[u][0].y, x[u][0].z, x[u][0].w, x[u][1].x, x[u][1].y, x[u][1].z, x[u][1].w};
                 const uint32_t s = scale_byte(quad_max(amax8(v)));
-                if (s == 255u) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-                }
+                if (OUT) clear_invalid(v, s);      // (the sum takes its NaN from the scale)
                 const uint64_t h = SR ? __shfl_sync(0xffffffffu, h_own, (threadIdx.x & 28) + u) : 0;
                 grid8<SR>(v, inv_scale(min(s, 253u)), h, (uint32_t)(j >> 1));
                 if (OUT || !SR) {
@@ -380,7 +376,7 @@ cudaError_t launch_mx4_quantize(cudaStream_t st, const void *x, int dtype, int64
     return launch_quantize_rounding<__half>(st, prm, stochastic);
 }
 
-cudaError_t launch_mx4_quantize_aggregate(cudaStream_t st, int d, int64_t S, const TileTable &tiles, const LayerTables &lt,
+cudaError_t launch_mx4_quantize_aggregate(cudaStream_t st, int num_sms, int d, int64_t S, const TileTable &tiles, const LayerTables &lt,
                                           const NodePtrs<const float> &g, int n_nodes, uint32_t node0, bool stochastic,
                                           uint64_t seed, float *out, const NodePtrs<uint8_t> *codes,
                                           const NodePtrs<uint8_t> *scales)
@@ -404,7 +400,8 @@ cudaError_t launch_mx4_quantize_aggregate(cudaStream_t st, int d, int64_t S, con
         cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
     }
-    const int n = prm.n_tiles + prm.n_tails;
+    prm.shares = tiles.n_tiles > 0 ? max(1, min((d + kBlock - 1) / kBlock, 4 * num_sms / tiles.n_tiles)) : 1;
+    const int n = prm.n_tiles * prm.shares + prm.n_tails;
     if (stochastic) return codes ? ptx::launch_chained<mx4_quantize_aggregate_kernel<true, true>>(prm, n, 256, 0, 1, st)
                                  : ptx::launch_chained<mx4_quantize_aggregate_kernel<true, false>>(prm, n, 256, 0, 1, st);
     return codes ? ptx::launch_chained<mx4_quantize_aggregate_kernel<false, true>>(prm, n, 256, 0, 1, st)
