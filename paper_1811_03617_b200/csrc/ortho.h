@@ -55,6 +55,8 @@ struct Device {
     const CUtensorMap *maps;         // [matrices][kMaps]
     Run run[4];                      // of each phase
     int pair;                        // which tiling the tiles are of
+    int n_mats;
+    int room;                        // all matrices fit one SM, their short sides this room; 0: they do not
     const Chunk *chunks;
     int chunk;                       // entries of one
     int n_chunks;
@@ -81,6 +83,12 @@ struct OutputArgs {
 cudaError_t launch_start(cudaStream_t st, const Device &dev, const ElementArgs &a);
 cudaError_t launch_product(cudaStream_t st, const Device &dev, Phase phase, int step, const OutputArgs *out,
                            int32_t *error_word, int wait_kcycles, int test_drop);
+
+// Matrices that fit one SM (ortho_small.cu): the room their short side takes, 64 or 128; 0: they do not.
+constexpr size_t kSmallSmem = 226 * 1024;
+int small_room(int r, int c);
+cudaError_t launch_small(cudaStream_t st, const Matrix *mats, int n, int room, int blocks, const ElementArgs &in, const OutputArgs &out,
+                         int32_t *error_word, int wait_kcycles, int test_drop);
 
 }  // namespace ortho
 }  // namespace gvq

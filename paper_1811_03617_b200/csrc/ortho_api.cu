@@ -15,6 +15,7 @@ struct gvq_ortho {
     gvq_ctx *ctx = nullptr;
     int device = 0;              // (destroying the plan does not touch the context, which may be gone)
     Device dev{};
+    int small_blocks = 0;        // of 64 entries of the longest side, where all matrices fit one SM
     void *tables = nullptr;      // one device allocation: matrices, tensor maps, tiles, chunks, partial sums
 };
 
@@ -123,14 +124,20 @@ void split(std::vector<Tile> &tiles, int units, int pieces, int &slots)
     tiles = out;
 }
 
-// The five steps from X to the result.
-gvq_status products(gvq_ortho *p, const OutputArgs &out)
+// The whole update: one launch where every matrix fits one SM, otherwise two element-wise ones and three a step.
+gvq_status run(gvq_ortho *p, const ElementArgs &in, const OutputArgs &out)
 {
     gvq_ctx *ctx = p->ctx;
+    DeviceGuard guard(ctx->device);
+    if (p->dev.room > 0) {
+        GVQ_CUDA(ctx, launch_small(ctx->stream, p->dev.mats, p->dev.n_mats, p->dev.room, p->small_blocks, in, out, ctx->error_word,
+                                   ctx->wait_kcycles, ctx->drop_last_load));
+        return GVQ_OK;
+    }
+    GVQ_CUDA(ctx, launch_start(ctx->stream, p->dev, in));
     for (int s = 0; s < kSteps; ++s)
         for (Phase ph : {kGram, kPoly, kApply})
-            GVQ_CUDA(ctx, launch_product(ctx->stream, p->dev, ph, s, &out, ctx->error_word, ctx->wait_kcycles,
-                                         ctx->drop_last_load));
+            GVQ_CUDA(ctx, launch_product(ctx->stream, p->dev, ph, s, &out, ctx->error_word, ctx->wait_kcycles, ctx->drop_last_load));
     return GVQ_OK;
 }
 
@@ -257,6 +264,16 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
         d.partial = reinterpret_cast<float *>(t + o_p);
         d.parts = reinterpret_cast<float *>(t + o_q);
         d.pair = pair;
+        d.n_mats = n;
+        int room = n > 0 ? 64 : 0, longest = 0;
+        for (const Matrix &m : sz.mats) {
+            const int need = small_room(m.r, m.c);
+            room = need == 0 || room == 0 ? 0 : std::max(room, need);
+            longest = std::max(longest, m.c);
+        }
+        p->small_blocks = (longest + 63) / 64;
+        // (one room serves all: a long matrix of few rows next to a short one of many may not fit it)
+        d.room = room > 0 && small_room(room, longest) == room ? room : 0;
         d.chunk = chunk;
         *out = p;
         return GVQ_OK;
@@ -281,9 +298,7 @@ gvq_status gvq_orthogonalize(gvq_ortho *p, const float *g, void *out, int dtype)
     if (static_cast<const void *>(g) == out) return GVQ_ERR_SHAPE;
     if (!aligned16(g) || !aligned16(out)) return GVQ_ERR_ALIGN;
     if (p->dev.n_chunks == 0) return GVQ_OK;
-    DeviceGuard guard(p->ctx->device);
-    GVQ_CUDA(p->ctx, launch_start(p->ctx->stream, p->dev, {g, nullptr, 0.0f, 0}));
-    return products(p, {out, dtype, 0, 0.0f, 0.0f});
+    return run(p, {g, nullptr, 0.0f, 0}, {out, dtype, 0, 0.0f, 0.0f});
 }
 
 gvq_status gvq_ortho_step(gvq_ortho *p, const float *g, float *momentum, float beta, int nesterov, void *w, int dtype, float lr,
@@ -295,9 +310,7 @@ gvq_status gvq_ortho_step(gvq_ortho *p, const float *g, float *momentum, float b
     if (g == momentum || static_cast<const void *>(g) == w || static_cast<void *>(momentum) == w) return GVQ_ERR_SHAPE;
     if (!aligned16(g) || !aligned16(momentum) || !aligned16(w)) return GVQ_ERR_ALIGN;
     if (p->dev.n_chunks == 0) return GVQ_OK;
-    DeviceGuard guard(p->ctx->device);
-    GVQ_CUDA(p->ctx, launch_start(p->ctx->stream, p->dev, {g, momentum, beta, nesterov}));
-    return products(p, {w, dtype, 1, 1.0f - lr * weight_decay, lr});
+    return run(p, {g, momentum, beta, nesterov}, {w, dtype, 1, 1.0f - lr * weight_decay, lr});
 }
 
 }  // extern "C"

@@ -1,0 +1,397 @@
+// The orthogonalised update of matrices that fit one SM, a whole update in one launch, one CTA a matrix.
+//
+// For a small matrix the products take a microsecond and the fifteen launches of ortho.cu 3.3 us each.  Here X stays in
+// shared memory from the gradient to the weights: as a sum of two halves (ortho.cu has the reasons), transposed, the long
+// side as rows: 64 entries of the short side are a row of 128 bytes (with the 128-byte swizzle), a second array holds
+// the next 64.  Then X^T is the K-major operand of X^T P and the MN-major ones of A = X X^T, nothing moves between the products
+// but the accumulators, and a thread that reads one of their rows writes it back as a row:
+//     A      D[R x R]   = sum over the long side             -> A and b I + c A, half precision, shared memory
+//     P      D[R x R]   = A (b I + c A)                      -> P = a I + D in A's place
+//     X^T P  D[128 x R] for every 128 of the long side       -> X = D + a X_lo in place
+// R is the short side's room, 64 or 128.  The unused rows and columns of X are zeros and stay zeros; an MMA's 128 rows
+// may run on into the next array, and those rows of the accumulator are not read.
+//
+// What bounds it is the chain of its steps (MMAs, a wait, accumulator to shared memory, a fence, fifteen times, 1.6 us a
+// step), and beyond that the conversions of X, an entry a lane.
+#include <algorithm>
+
+#include "ortho.h"
+#include "row32.cuh"
+#include "sm100_ptx.cuh"
+
+namespace gvq {
+namespace ortho {
+namespace {
+
+using namespace ptx;
+
+constexpr int NTHREADS = 512, NPART = NTHREADS / 128;     // warps that share a quarter of the accumulator's rows
+
+struct SmallParams {
+    const Matrix *mats;
+    ElementArgs in;
+    OutputArgs out;
+    int mode;                // of the momentum, as in ortho.cu
+    int32_t *error_word;
+    int wait_kcycles, test_drop;
+};
+
+// Byte of entry (i of the long side, j of the short side) in an array of `half`-byte columns of 64 entries.
+__device__ __forceinline__ uint32_t place(int i, int j, uint32_t half)
+{
+    return (uint32_t)(j >> 6) * half + i * 128 + ((((j & 63) >> 3) ^ (i & 7)) << 4) + (j & 7) * 2;
+}
+
+template <int R, typename T>
+__global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallParams prm)
+{
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    __shared__ float sums[NTHREADS / 32];
+    __shared__ uint64_t bar;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int flags[4];                 // abort flag, -, limit of the waits
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const Matrix &mx = prm.mats[blockIdx.x];
+    const int rows = (mx.c + 63) & ~63, tiles = (mx.c + 127) / 128;
+    constexpr uint32_t SQUARE_HALF = R * 128, SQUARE = R / 64 * SQUARE_HALF;
+    const uint32_t half = rows * 128, array = R / 64 * half;
+    unsigned char *gram = smem, *factor = gram + SQUARE, *hi = factor + SQUARE, *lo = hi + array;
+
+    launch_dependents();
+    if (threadIdx.x == 0) {
+        mbar_init(&bar, 1);
+        flags[0] = 0;
+        flags[2] = prm.wait_kcycles;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) tmem_alloc<1>(&tmem_slot, 512);
+    for (uint32_t i = threadIdx.x; i < 2 * array / 16; i += NTHREADS) reinterpret_cast<uint4 *>(hi)[i] = make_uint4(0, 0, 0, 0);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    grid_dependency_wait();
+
+    // u = g + beta * momentum, its bits in the two arrays until the norm is known
+    const int total = mx.rows * mx.cols;
+    const float *g = prm.in.g + mx.off;
+    float *mo = prm.mode ? prm.in.momentum + mx.off : nullptr;
+    float sum = 0.0f;
+    auto at = [&](int e) {
+        const int row = (int)__umul64hi((uint64_t)e << 2, mx.by_cols), col = e - row * mx.cols;
+        return mx.tall ? place(row, col, half) : place(col, row, half);
+    };
+    auto direct = [&](float u, float &m) {
+        if (prm.mode) {
+            m = __fmaf_rn(prm.in.beta, m, u);
+            u = prm.mode == 1 ? m : __fmaf_rn(prm.in.beta, m, u);
+        }
+        sum = __fmaf_rn(u, u, sum);
+        return __float_as_uint(u);
+    };
+    // Four entries of a row at a time where rows hold whole quads.  A tall matrix' row is one here too.  Of a wide one a warp
+    // takes 32 rows x 8 columns, a lane two rows x 4 columns: its words, two rows' entries each, go to different banks.
+    const bool quads = (mx.cols & 3) == 0;
+    const int tall_quads = quads && mx.tall ? total / 4 : 0;
+    const int strips = (mx.rows + 31) / 32, wide_tiles = quads && !mx.tall ? strips * ((mx.cols + 7) / 8) : 0;
+    const int lane_row = 2 * (lane >> 1), lane_col = 4 * (lane & 1);
+    auto load4 = [](const float *from, bool in) { return in ? *reinterpret_cast<const float4 *>(from) : make_float4(0.f, 0.f, 0.f, 0.f); };
+#pragma unroll 6
+    for (int e = threadIdx.x; e < tall_quads; e += NTHREADS) {
+        const float4 x = reinterpret_cast<const float4 *>(g)[e];
+        float4 m = load4(mo + 4 * e, prm.mode != 0);
+        const uint32_t b[4] = {direct(x.x, m.x), direct(x.y, m.y), direct(x.z, m.z), direct(x.w, m.w)};
+        if (prm.mode) reinterpret_cast<float4 *>(mo)[e] = m;
+        const uint32_t p = at(4 * e);
+        *reinterpret_cast<uint2 *>(hi + p) = make_uint2(__byte_perm(b[0], b[1], 0x7632), __byte_perm(b[2], b[3], 0x7632));
+        *reinterpret_cast<uint2 *>(lo + p) = make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410));
+    }
+#pragma unroll 3
+    for (int w = warp; w < wide_tiles; w += NTHREADS / 32) {
+        const int row = 32 * (w % strips) + lane_row, col = 8 * (w / strips) + lane_col;
+        float4 x[2], m[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const bool in = row + h < mx.rows && col < mx.cols;
+            const int e = (row + h) * mx.cols + col;
+            x[h] = load4(g + e, in);
+            m[h] = load4(mo + e, in && prm.mode);
+        }
+        uint32_t b[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            b[h][0] = direct(x[h].x, m[h].x); b[h][1] = direct(x[h].y, m[h].y);
+            b[h][2] = direct(x[h].z, m[h].z); b[h][3] = direct(x[h].w, m[h].w);
+            if (prm.mode && row + h < mx.rows && col < mx.cols) *reinterpret_cast<float4 *>(mo + (row + h) * mx.cols + col) = m[h];
+        }
+        if (row < mx.rows && col < mx.cols) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t p = place(col + i, row, half);
+                *reinterpret_cast<uint32_t *>(hi + p) = __byte_perm(b[0][i], b[1][i], 0x7632);
+                *reinterpret_cast<uint32_t *>(lo + p) = __byte_perm(b[0][i], b[1][i], 0x5410);
+            }
+        }
+    }
+#pragma unroll 8
+    for (int e = threadIdx.x; !quads && e < total; e += NTHREADS) {
+        float m = prm.mode ? mo[e] : 0.0f;
+        const uint32_t b = direct(g[e], m), p = at(e);
+        if (prm.mode) mo[e] = m;
+        *reinterpret_cast<uint16_t *>(hi + p) = (uint16_t)(b >> 16);
+        *reinterpret_cast<uint16_t *>(lo + p) = (uint16_t)b;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) sums[warp] = sum;
+    __syncthreads();
+    sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NTHREADS / 32; ++i) sum += sums[i];
+    const float f = mx.sx / (sqrtf(sum) + kEps);
+    // X = u / |u|: places do not matter here (zeros stay zeros)
+    for (uint32_t i = threadIdx.x; i < array / 16; i += NTHREADS) {
+        uint4 h4 = reinterpret_cast<const uint4 *>(hi)[i], l4 = reinterpret_cast<const uint4 *>(lo)[i];
+        uint32_t h[4] = {h4.x, h4.y, h4.z, h4.w}, l[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float a = __uint_as_float(__byte_perm(l[k], h[k], 0x5410)) * f, b = __uint_as_float(__byte_perm(l[k], h[k], 0x7632)) * f;
+            h[k] = pack2<__half>(a, b);
+            const float2 r = unpack_half2(h[k]);
+            l[k] = pack2<__half>(a - r.x, b - r.y);
+        }
+        reinterpret_cast<uint4 *>(hi)[i] = make_uint4(h[0], h[1], h[2], h[3]);
+        reinterpret_cast<uint4 *>(lo)[i] = make_uint4(l[0], l[1], l[2], l[3]);
+    }
+
+    const int q = warp & 3, part = warp >> 2, m = 32 * q + lane;       // this thread's row of an accumulator
+    const uint32_t lane_base = (uint32_t)(32 * q) << 16;
+    const bool live = 32 * q < R;                                       // in a square result (uniform in a warp)
+    uint32_t phase = 0;
+    bool ok = true;
+    // shared memory written so far is seen by the MMAs; the accumulators have been read
+    auto hand_over = [&]() {
+        fence_proxy_async();
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+    };
+    auto wait = [&]() {
+        if (warp == 0) ok = ok && mbar_poll(&bar, phase & 1, flags);     // (one warp polls, the others wait at the barrier)
+        ++phase;
+        ok = __syncthreads_and(ok);
+        tc_fence_after();
+    };
+    // 16 entries of row m of a square operand from column n on
+    auto put16 = [&](unsigned char *to, int n, const float *v) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            *reinterpret_cast<uint4 *>(to + place(m, n + 8 * i, SQUARE_HALF)) =
+                make_uint4(pack2<__half>(v[8 * i], v[8 * i + 1]), pack2<__half>(v[8 * i + 2], v[8 * i + 3]),
+                           pack2<__half>(v[8 * i + 4], v[8 * i + 5]), pack2<__half>(v[8 * i + 6], v[8 * i + 7]));
+    };
+    const uint32_t a_gram = smem_u32(gram), a_factor = smem_u32(factor), a_hi = smem_u32(hi);
+    // step k of 16 of the short side's contraction in a K-major operand
+    auto along = [](uint32_t base, uint32_t half, int k) { return make_b_desc(base + (k >> 2) * half) + 2 * (k & 3); };
+    constexpr int SQUARE_PIECES = R / 16 / NPART;      // of 16 columns, of a warp
+
+    for (int step = 0; step < kSteps && ok; ++step) {
+        // ---- A, and b I + c A
+        hand_over();
+        if (warp == 0) {
+            constexpr uint32_t idesc = make_idesc_f16(128, R, true, true);
+            if (elect_one()) {
+                // 16 rows of X^T a step.  With R = 64 the second 64 rows of the result repeat the first (chunk distance 0).
+                const uint64_t a = make_mn_desc(a_hi, R == 128 ? half : 0), b = make_mn_desc(a_hi, half);
+                for (int k = 0; k < rows / 16; ++k) tc_mma_f16<1>(tmem, a + k * (16 * 128 / 16), b + k * (16 * 128 / 16), idesc, k != 0);
+                // (test hook: without this the wait below runs out and the kernel gives up)
+                if (!(prm.test_drop && blockIdx.x == 0 && step == 0)) tc_commit(&bar);
+            }
+            __syncwarp();
+        }
+        wait();
+        if (!ok) break;
+        if (live) {
+            const float s = kGramScale / (mx.sx * mx.sx);
+#pragma unroll
+            for (int p = 0; p < SQUARE_PIECES; ++p) {
+                const int n = 16 * (part * SQUARE_PIECES + p);
+                float v[16];
+                tmem_ld16_wait(tmem + lane_base + n, v);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] *= s;
+                put16(gram, n, v);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = v[i] * kC + (n + i == m ? kB * kGramScale : 0.0f);
+                put16(factor, n, v);
+            }
+        }
+        // ---- P
+        hand_over();
+        constexpr uint32_t idesc = make_idesc_f16(128, R, false, false);
+        if (warp == 0) {
+            if (elect_one()) {
+#pragma unroll
+                for (int k = 0; k < R / 16; ++k) tc_mma_f16<1>(tmem, along(a_gram, SQUARE_HALF, k), along(a_factor, SQUARE_HALF, k), idesc, k != 0);
+                tc_commit(&bar);
+            }
+            __syncwarp();
+        }
+        wait();
+        if (!ok) break;
+        if (live) {
+#pragma unroll
+            for (int p = 0; p < SQUARE_PIECES; ++p) {
+                const int n = 16 * (part * SQUARE_PIECES + p);
+                float v[16];
+                tmem_ld16_wait(tmem + lane_base + n, v);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = v[i] * (1.0f / kGramScale) + (n + i == m ? kA * kGramScale : 0.0f);
+                put16(gram, n, v);
+            }
+        }
+        // ---- X^T P, the accumulators of all tiles side by side
+        hand_over();
+        if (warp == 0) {
+            if (elect_one()) {
+                for (int t = 0; t < tiles; ++t)
+#pragma unroll
+                    for (int k = 0; k < R / 16; ++k)
+                        tc_mma_f16<1>(tmem + R * t, along(a_hi + t * (128 * 128), half, k), along(a_gram, SQUARE_HALF, k), idesc, k != 0);
+                tc_commit(&bar);
+            }
+            __syncwarp();
+        }
+        wait();
+        if (!ok) break;
+#pragma unroll 1
+        for (int p = part; p < tiles * (R / 32); p += NPART) {       // 32 columns at a time
+            const int t = p / (R / 32), n = 32 * (p - t * (R / 32)), i = 128 * t + m;
+            float v[32];
+            tmem_ld32_wait(tmem + lane_base + R * t + n, v);
+            if (i >= rows) continue;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const uint32_t o = place(i, n + 8 * c, half);
+                uint4 *l = reinterpret_cast<uint4 *>(lo + o);
+                const uint4 old = *l;
+                const uint32_t w[4] = {old.x, old.y, old.z, old.w};
+                uint32_t nh[4], nl[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float2 x = make_float2(v[8 * c + 2 * e] * (1.0f / kGramScale), v[8 * c + 2 * e + 1] * (1.0f / kGramScale));
+                    if (step < kExactSteps) {
+                        const float2 a = unpack_half2(w[e]);
+                        x.x = __fmaf_rn(kA, a.x, x.x);
+                        x.y = __fmaf_rn(kA, a.y, x.y);
+                    }
+                    nh[e] = pack2<__half>(x.x, x.y);
+                    const float2 r = unpack_half2(nh[e]);
+                    nl[e] = pack2<__half>(x.x - r.x, x.y - r.y);
+                }
+                *reinterpret_cast<uint4 *>(hi + o) = make_uint4(nh[0], nh[1], nh[2], nh[3]);
+                *l = make_uint4(nl[0], nl[1], nl[2], nl[3]);
+            }
+        }
+    }
+    __syncthreads();
+
+    if (ok) {
+        // the result, from both halves
+        T *out = static_cast<T *>(prm.out.ptr) + mx.off;
+        const float k = (prm.out.update ? -prm.out.step * mx.scale : 1.0f) / mx.sx;
+        auto entry = [&](uint32_t p) {
+            return __half2float(*reinterpret_cast<const __half *>(hi + p)) + __half2float(*reinterpret_cast<const __half *>(lo + p));
+        };
+        struct alignas(4 * sizeof(T)) Quad { T v[4]; };
+        auto finish = [&](Quad &o, int i, float x) { o.v[i] = from_f<T>(prm.out.update ? __fmaf_rn(k, x, prm.out.decay * to_f(o.v[i])) : k * x); };
+#pragma unroll 6
+        for (int e = threadIdx.x; e < tall_quads; e += NTHREADS) {
+            Quad o;
+            if (prm.out.update) o = reinterpret_cast<const Quad *>(out)[e];
+            const uint32_t p = at(4 * e);
+            const uint2 h = *reinterpret_cast<const uint2 *>(hi + p), l = *reinterpret_cast<const uint2 *>(lo + p);
+            const float2 h0 = unpack_half2(h.x), h1 = unpack_half2(h.y), l0 = unpack_half2(l.x), l1 = unpack_half2(l.y);
+            finish(o, 0, h0.x + l0.x);
+            finish(o, 1, h0.y + l0.y);
+            finish(o, 2, h1.x + l1.x);
+            finish(o, 3, h1.y + l1.y);
+            reinterpret_cast<Quad *>(out)[e] = o;
+        }
+#pragma unroll 3
+        for (int w = warp; w < wide_tiles; w += NTHREADS / 32) {
+            const int row = 32 * (w % strips) + lane_row, col = 8 * (w / strips) + lane_col;
+            if (row >= mx.rows || col >= mx.cols) continue;
+            const bool two = row + 1 < mx.rows;
+            Quad *to = reinterpret_cast<Quad *>(out + row * mx.cols + col), *to1 = reinterpret_cast<Quad *>(out + (row + 1) * mx.cols + col);
+            Quad o0, o1;
+            if (prm.out.update) {
+                o0 = *to;
+                if (two) o1 = *to1;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t p = place(col + i, row, half);
+                const float2 h = unpack_half2(*reinterpret_cast<const uint32_t *>(hi + p)), l = unpack_half2(*reinterpret_cast<const uint32_t *>(lo + p));
+                finish(o0, i, h.x + l.x);
+                finish(o1, i, h.y + l.y);
+            }
+            *to = o0;
+            if (two) *to1 = o1;
+        }
+#pragma unroll 8
+        for (int e = threadIdx.x; !quads && e < total; e += NTHREADS) {
+            const float x = entry(at(e));
+            out[e] = from_f<T>(prm.out.update ? __fmaf_rn(k, x, prm.out.decay * to_f(out[e])) : k * x);
+        }
+    } else if (threadIdx.x == 0) {
+        atomicExch(prm.error_word, 100);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 0) tmem_dealloc<1>(tmem, 512);
+}
+
+template <int R> size_t small_smem(int blocks) { return (size_t)(R / 64) * 128 * (2 * R + 2 * 64 * blocks) + 1024; }
+
+template <int R, typename T>
+cudaError_t launch_as(cudaStream_t st, const SmallParams &prm, int n, int blocks)
+{
+    // (the launch helper raises a kernel's limit once: the first launch asks for all there is)
+    return launch_chained<ortho_small_kernel<R, T>>(prm, n, NTHREADS, std::max(small_smem<R>(blocks), kSmallSmem), 1, st);
+}
+template <int R>
+cudaError_t launch_typed(cudaStream_t st, const SmallParams &prm, int n, int blocks)
+{
+    if (prm.out.dtype == GVQ_F32) return launch_as<R, float>(st, prm, n, blocks);
+    if (prm.out.dtype == GVQ_BF16) return launch_as<R, __nv_bfloat16>(st, prm, n, blocks);
+    return launch_as<R, __half>(st, prm, n, blocks);
+}
+
+}  // namespace
+
+int small_room(int r, int c)
+{
+    const int blocks = (c + 63) / 64;
+    if (r <= 64 && small_smem<64>(blocks) <= kSmallSmem) return 64;
+    return r <= 128 && small_smem<128>(blocks) <= kSmallSmem ? 128 : 0;
+}
+
+cudaError_t launch_small(cudaStream_t st, const Matrix *mats, int n, int room, int blocks, const ElementArgs &in, const OutputArgs &out,
+                         int32_t *error_word, int wait_kcycles, int test_drop)
+{
+    SmallParams prm;
+    prm.mats = mats;
+    prm.in = in;
+    prm.out = out;
+    prm.mode = !in.momentum ? 0 : in.nesterov ? 2 : 1;
+    prm.error_word = error_word;
+    prm.wait_kcycles = wait_kcycles > 0 ? wait_kcycles : WAIT_KCYCLES_DEFAULT;
+    prm.test_drop = test_drop;
+    return room == 64 ? launch_typed<64>(st, prm, n, blocks) : launch_typed<128>(st, prm, n, blocks);
+}
+
+}  // namespace ortho
+}  // namespace gvq

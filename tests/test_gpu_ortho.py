@@ -89,6 +89,79 @@ def test_orthogonalize_all_shapes_in_one_call(kind):
         assert torch.equal(out[at], again[at])               # the same bits every time
 
 
+# plans whose matrices all fit one SM: both rooms for the short side (64 and 128), both orientations, one block of 64 columns
+# to thirteen, single rows and columns
+SMALL = [[(1, 1), (1, 7), (9, 1), (5, 7), (16, 27), (64, 64), (63, 65), (64, 576), (576, 64), (3, 800), (832, 64), (33, 257)],
+         [(128, 128), (65, 1), (100, 300), (320, 128), (127, 129), (96, 257), (1, 320), (66, 64)], [(64, 64)], [(300, 100)]]
+
+
+@pytest.mark.parametrize("shapes", SMALL)
+@pytest.mark.parametrize("dtype", list(DT))
+def test_small_matrices(shapes, dtype):
+    w, plan = make(shapes)
+    gen = torch.Generator().manual_seed(9)
+    g = torch.randn(w.M, generator=gen)
+    for i, ((m, n), o) in enumerate(zip(shapes, w.layer_off)):
+        if i % 3 == 1:
+            g[o:o + m * n] = kinds(m, n, i, "lowrank").reshape(-1) * 1e-3
+    g = g.cuda()
+    out = torch.full((w.M,), 7.0, dtype=DT[dtype], device="cuda")
+    plan.orthogonalize(g, out)
+    mo = torch.randn(w.M, generator=gen).cuda()
+    mo0 = mo.clone()
+    wt = torch.full((w.M,), 2.0, dtype=DT[dtype], device="cuda")
+    plan.step(g, mo, wt, lr=0.5, weight_decay=0.5, beta=0.5, nesterov=True)
+    plan.ctx.device_status()
+    rest = torch.ones(w.M, dtype=torch.bool, device="cuda")
+    for (m, n), o in zip(shapes, w.layer_off):
+        sl = slice(o, o + m * n)
+        rest[sl] = False
+        want = exact(g[sl].view(m, n)).reshape(-1)
+        err = float((out[sl].double() - want).norm() / want.norm())
+        assert err <= bar(m, n) + 2 * HALF_ULP[DT[dtype]], (m, n, err)
+        mom = 0.5 * mo0[sl].double() + g[sl].double()
+        assert bool(((mo[sl].double() - mom).abs() <= mom.abs() * 2.0 ** -24).all())
+        want = exact((g[sl].double() + 0.5 * mom).view(m, n)).reshape(-1)
+        s = math.sqrt(max(1.0, m / n))
+        new = 0.75 * 2.0 - 0.5 * s * want
+        err = float((wt[sl].double() - new).norm())
+        assert err <= 0.5 * s * float(want.norm()) * bar(m, n) + float(new.norm()) * (2 * HALF_ULP[DT[dtype]] + 2.0 ** -22), (m, n)
+    assert bool((out[rest] == 7.0).all()) and bool((wt[rest] == 2.0).all()) and torch.equal(mo[rest], mo0[rest])
+    again = torch.empty_like(out)
+    plan.orthogonalize(g, again)
+    assert torch.equal(out[~rest], again[~rest])
+
+
+def test_a_small_plan_gives_what_a_larger_one_gives():
+    """The same matrix alone (one SM) and next to one that does not fit (tiles): two summation orders of one algorithm."""
+    w1, one = make([(64, 320)])
+    w2, two = make([(64, 320), (400, 400)])
+    g = torch.randn(w2.M, device="cuda")
+    a, b = torch.empty(w1.M, device="cuda"), torch.empty(w2.M, device="cuda")
+    one.orthogonalize(g[:w1.M].clone(), a)
+    two.orthogonalize(g, b)
+    x, y = a[:64 * 320].double(), b[:64 * 320].double()
+    assert float((x - y).norm() / y.norm()) <= 2 * bar(64, 320)
+
+
+@pytest.mark.parametrize("shape", [(40, 200), (128, 200)])
+def test_small_zero_and_non_finite(shape):
+    m, n = shape
+    w, plan = make([shape] * 3)
+    g = torch.randn(w.M)
+    o = w.layer_off
+    g[o[0]:o[0] + m * n] = 0.0
+    g[o[1] + 5] = float("inf")
+    out = torch.empty(w.M, device="cuda")
+    plan.orthogonalize(g.cuda(), out)
+    plan.ctx.device_status()
+    assert bool((out[o[0]:o[0] + m * n] == 0).all())
+    got = out[o[1]:o[1] + m * n]
+    assert not bool((torch.isfinite(got) & (got != 0)).any())
+    want = exact(g[o[2]:o[2] + m * n].view(m, n))
+    assert float((out[o[2]:o[2] + m * n].view(m, n).cpu().double() - want).norm() / want.norm()) <= bar(m, n)
+
+
 @pytest.mark.parametrize("dtype", list(DT))
 def test_many_large_matrices(dtype):
     """Enough 256 x 256 tiles for pairs of CTAs: wide, tall and square matrices with ragged edges in one plan."""
@@ -231,12 +304,14 @@ def test_step_after_the_exchange_on_one_stream_and_in_a_graph():
         assert torch.equal(mo[o:o + m * n], mo2[o:o + m * n]) and torch.equal(wt[o:o + m * n], wt2[o:o + m * n])
 
 
-def test_a_wait_that_runs_out_is_reported_and_the_plan_recovers():
+@pytest.mark.parametrize("shape", [(300, 400), (60, 100), (1600, 1600)])
+def test_a_wait_that_runs_out_is_reported_and_the_plan_recovers(shape):
     from paper_1811_03617_b200 import gvq
-    w, plan = make([(300, 400)])
+    w, plan = make([shape])
+    n = shape[0] * shape[1]
     g, out = torch.randn(w.M, device="cuda"), torch.empty(w.M, device="cuda")
     plan.orthogonalize(g, out)
-    good = out[:120000].clone()
+    good = out[:n].clone()
     plan.ctx.set_limits(wait_cycles=2_000_000)
     plan.ctx.test_drop_load(True)
     try:
@@ -249,7 +324,7 @@ def test_a_wait_that_runs_out_is_reported_and_the_plan_recovers():
         plan.ctx.set_limits()
     plan.orthogonalize(g, out)
     plan.ctx.device_status()
-    assert torch.equal(out[:120000], good)
+    assert torch.equal(out[:n], good)
 
 
 def test_a_plan_can_be_destroyed_after_its_context():
