@@ -91,46 +91,77 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
         return __float_as_uint(u);
     };
     // Four entries of a row at a time where rows hold whole quads.  A tall matrix' row is one here too.  Of a wide one a warp
-    // takes 32 rows x 8 columns, a lane two rows x 4 columns: its words, two rows' entries each, go to different banks.
+    // takes 8 rows x 32 columns (128 bytes of each), a lane two rows x 4 columns; the two rows' entries of a column make a word
+    // here, and the lanes take their four columns in orders that keep a warp's words in different banks.
     const bool quads = (mx.cols & 3) == 0;
     const int tall_quads = quads && mx.tall ? total / 4 : 0;
-    const int strips = (mx.rows + 31) / 32, wide_tiles = quads && !mx.tall ? strips * ((mx.cols + 7) / 8) : 0;
-    const int lane_row = 2 * (lane >> 1), lane_col = 4 * (lane & 1);
-    auto load4 = [](const float *from, bool in) { return in ? *reinterpret_cast<const float4 *>(from) : make_float4(0.f, 0.f, 0.f, 0.f); };
-#pragma unroll 6
-    for (int e = threadIdx.x; e < tall_quads; e += NTHREADS) {
-        const float4 x = reinterpret_cast<const float4 *>(g)[e];
-        float4 m = load4(mo + 4 * e, prm.mode != 0);
-        const uint32_t b[4] = {direct(x.x, m.x), direct(x.y, m.y), direct(x.z, m.z), direct(x.w, m.w)};
-        if (prm.mode) reinterpret_cast<float4 *>(mo)[e] = m;
-        const uint32_t p = at(4 * e);
-        *reinterpret_cast<uint2 *>(hi + p) = make_uint2(__byte_perm(b[0], b[1], 0x7632), __byte_perm(b[2], b[3], 0x7632));
-        *reinterpret_cast<uint2 *>(lo + p) = make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410));
+    const int strips = (mx.rows + 7) / 8, wide_tiles = quads && !mx.tall ? strips * ((mx.cols + 31) / 32) : 0;
+    const int lane_row = 2 * (lane >> 3), lane_col = 4 * (lane & 7), turn = (lane & 7) >> 1;
+    auto turned = [&](uint32_t (&w)[4]) {      // w[c] = w[(c + turn) % 4]
+        if (turn & 1) { const uint32_t x = w[0]; w[0] = w[1]; w[1] = w[2]; w[2] = w[3]; w[3] = x; }
+        if (turn & 2) { uint32_t x = w[0]; w[0] = w[2]; w[2] = x; x = w[1]; w[1] = w[3]; w[3] = x; }
+    };
+    // Loads are unconditional (entry 0 stands in for what is outside, the gradient for a momentum that is not there), so that a
+    // batch's are issued together, before its first store.
+    const float *mo_or_g = prm.mode ? mo : g;
+    auto load4 = [](const float *from, int e, bool in) { return *reinterpret_cast<const float4 *>(from + (in ? e : 0)); };
+    constexpr int BATCH = 6, TILES = 3;
+    for (int e0 = threadIdx.x; e0 < tall_quads; e0 += BATCH * NTHREADS) {
+        float4 x[BATCH], m[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int e = e0 + i * NTHREADS;
+            x[i] = load4(g, 4 * e, e < tall_quads);
+            m[i] = load4(mo_or_g, 4 * e, e < tall_quads);
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int e = e0 + i * NTHREADS;
+            if (e >= tall_quads) break;
+            const uint32_t b[4] = {direct(x[i].x, m[i].x), direct(x[i].y, m[i].y), direct(x[i].z, m[i].z), direct(x[i].w, m[i].w)};
+            if (prm.mode) reinterpret_cast<float4 *>(mo)[e] = m[i];
+            const uint32_t p = at(4 * e);
+            *reinterpret_cast<uint2 *>(hi + p) = make_uint2(__byte_perm(b[0], b[1], 0x7632), __byte_perm(b[2], b[3], 0x7632));
+            *reinterpret_cast<uint2 *>(lo + p) = make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410));
+        }
     }
-#pragma unroll 3
-    for (int w = warp; w < wide_tiles; w += NTHREADS / 32) {
-        const int row = 32 * (w % strips) + lane_row, col = 8 * (w / strips) + lane_col;
-        float4 x[2], m[2];
+    auto tile_at = [&](int w, int &row, int &col) {
+        row = 8 * (w % strips) + lane_row;
+        col = 32 * (w / strips) + lane_col;
+        return w < wide_tiles && row < mx.rows && col < mx.cols;
+    };
+    for (int w0 = warp; w0 < wide_tiles; w0 += TILES * (NTHREADS / 32)) {
+        float4 x[TILES][2], m[TILES][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const bool in = row + h < mx.rows && col < mx.cols;
-            const int e = (row + h) * mx.cols + col;
-            x[h] = load4(g + e, in);
-            m[h] = load4(mo + e, in && prm.mode);
+        for (int i = 0; i < TILES; ++i) {
+            int row, col;
+            const bool in = tile_at(w0 + i * (NTHREADS / 32), row, col);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int e = (row + h) * mx.cols + col;
+                x[i][h] = load4(g, e, in && row + h < mx.rows);
+                m[i][h] = load4(mo_or_g, e, in && row + h < mx.rows);
+            }
         }
-        uint32_t b[2][4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            b[h][0] = direct(x[h].x, m[h].x); b[h][1] = direct(x[h].y, m[h].y);
-            b[h][2] = direct(x[h].z, m[h].z); b[h][3] = direct(x[h].w, m[h].w);
-            if (prm.mode && row + h < mx.rows && col < mx.cols) *reinterpret_cast<float4 *>(mo + (row + h) * mx.cols + col) = m[h];
-        }
-        if (row < mx.rows && col < mx.cols) {
+        for (int i = 0; i < TILES; ++i) {
+            int row, col;
+            if (!tile_at(w0 + i * (NTHREADS / 32), row, col)) continue;
+            uint32_t b[2][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t p = place(col + i, row, half);
-                *reinterpret_cast<uint32_t *>(hi + p) = __byte_perm(b[0][i], b[1][i], 0x7632);
-                *reinterpret_cast<uint32_t *>(lo + p) = __byte_perm(b[0][i], b[1][i], 0x5410);
+            for (int h = 0; h < 2; ++h) {
+                if (row + h >= mx.rows) x[i][h] = make_float4(0.f, 0.f, 0.f, 0.f), m[i][h] = x[i][h];
+                b[h][0] = direct(x[i][h].x, m[i][h].x); b[h][1] = direct(x[i][h].y, m[i][h].y);
+                b[h][2] = direct(x[i][h].z, m[i][h].z); b[h][3] = direct(x[i][h].w, m[i][h].w);
+                if (prm.mode && row + h < mx.rows) *reinterpret_cast<float4 *>(mo + (row + h) * mx.cols + col) = m[i][h];
+            }
+            turned(b[0]);
+            turned(b[1]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const uint32_t p = place(col + ((c + turn) & 3), row, half);
+                *reinterpret_cast<uint32_t *>(hi + p) = __byte_perm(b[0][c], b[1][c], 0x7632);
+                *reinterpret_cast<uint32_t *>(lo + p) = __byte_perm(b[0][c], b[1][c], 0x5410);
             }
         }
     }
@@ -304,41 +335,64 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
         auto entry = [&](uint32_t p) {
             return __half2float(*reinterpret_cast<const __half *>(hi + p)) + __half2float(*reinterpret_cast<const __half *>(lo + p));
         };
+        auto back = [&](uint32_t (&w)[4]) {        // undoes turned()
+            if (turn & 1) { const uint32_t x = w[3]; w[3] = w[2]; w[2] = w[1]; w[1] = w[0]; w[0] = x; }
+            if (turn & 2) { uint32_t x = w[0]; w[0] = w[2]; w[2] = x; x = w[1]; w[1] = w[3]; w[3] = x; }
+        };
         struct alignas(4 * sizeof(T)) Quad { T v[4]; };
         auto finish = [&](Quad &o, int i, float x) { o.v[i] = from_f<T>(prm.out.update ? __fmaf_rn(k, x, prm.out.decay * to_f(o.v[i])) : k * x); };
-#pragma unroll 6
-        for (int e = threadIdx.x; e < tall_quads; e += NTHREADS) {
-            Quad o;
-            if (prm.out.update) o = reinterpret_cast<const Quad *>(out)[e];
-            const uint32_t p = at(4 * e);
-            const uint2 h = *reinterpret_cast<const uint2 *>(hi + p), l = *reinterpret_cast<const uint2 *>(lo + p);
-            const float2 h0 = unpack_half2(h.x), h1 = unpack_half2(h.y), l0 = unpack_half2(l.x), l1 = unpack_half2(l.y);
-            finish(o, 0, h0.x + l0.x);
-            finish(o, 1, h0.y + l0.y);
-            finish(o, 2, h1.x + l1.x);
-            finish(o, 3, h1.y + l1.y);
-            reinterpret_cast<Quad *>(out)[e] = o;
-        }
-#pragma unroll 3
-        for (int w = warp; w < wide_tiles; w += NTHREADS / 32) {
-            const int row = 32 * (w % strips) + lane_row, col = 8 * (w / strips) + lane_col;
-            if (row >= mx.rows || col >= mx.cols) continue;
-            const bool two = row + 1 < mx.rows;
-            Quad *to = reinterpret_cast<Quad *>(out + row * mx.cols + col), *to1 = reinterpret_cast<Quad *>(out + (row + 1) * mx.cols + col);
-            Quad o0, o1;
-            if (prm.out.update) {
-                o0 = *to;
-                if (two) o1 = *to1;
+        for (int e0 = threadIdx.x; e0 < tall_quads; e0 += BATCH * NTHREADS) {
+            Quad o[BATCH];
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                const int e = e0 + i * NTHREADS;
+                if (prm.out.update) o[i] = reinterpret_cast<const Quad *>(out)[e < tall_quads ? e : 0];
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t p = place(col + i, row, half);
-                const float2 h = unpack_half2(*reinterpret_cast<const uint32_t *>(hi + p)), l = unpack_half2(*reinterpret_cast<const uint32_t *>(lo + p));
-                finish(o0, i, h.x + l.x);
-                finish(o1, i, h.y + l.y);
+            for (int i = 0; i < BATCH; ++i) {
+                const int e = e0 + i * NTHREADS;
+                if (e >= tall_quads) break;
+                const uint32_t p = at(4 * e);
+                const uint2 h = *reinterpret_cast<const uint2 *>(hi + p), l = *reinterpret_cast<const uint2 *>(lo + p);
+                const float2 h0 = unpack_half2(h.x), h1 = unpack_half2(h.y), l0 = unpack_half2(l.x), l1 = unpack_half2(l.y);
+                finish(o[i], 0, h0.x + l0.x);
+                finish(o[i], 1, h0.y + l0.y);
+                finish(o[i], 2, h1.x + l1.x);
+                finish(o[i], 3, h1.y + l1.y);
+                reinterpret_cast<Quad *>(out)[e] = o[i];
             }
-            *to = o0;
-            if (two) *to1 = o1;
+        }
+        for (int w0 = warp; w0 < wide_tiles; w0 += TILES * (NTHREADS / 32)) {
+            Quad o[TILES][2];
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) {
+                int row, col;
+                const bool in = tile_at(w0 + i * (NTHREADS / 32), row, col);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (prm.out.update) o[i][h] = *reinterpret_cast<const Quad *>(out + (in && row + h < mx.rows ? (row + h) * mx.cols + col : 0));
+            }
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) {
+                int row, col;
+                if (!tile_at(w0 + i * (NTHREADS / 32), row, col)) continue;
+                uint32_t x[2][4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const uint32_t p = place(col + ((c + turn) & 3), row, half);
+                    const float2 h = unpack_half2(*reinterpret_cast<const uint32_t *>(hi + p)), l = unpack_half2(*reinterpret_cast<const uint32_t *>(lo + p));
+                    x[0][c] = __float_as_uint(h.x + l.x);
+                    x[1][c] = __float_as_uint(h.y + l.y);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    back(x[h]);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) finish(o[i][h], c, __uint_as_float(x[h][c]));
+                }
+                *reinterpret_cast<Quad *>(out + row * mx.cols + col) = o[i][0];
+                if (row + 1 < mx.rows) *reinterpret_cast<Quad *>(out + (row + 1) * mx.cols + col) = o[i][1];
+            }
         }
 #pragma unroll 8
         for (int e = threadIdx.x; !quads && e < total; e += NTHREADS) {
