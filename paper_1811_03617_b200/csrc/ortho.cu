@@ -176,6 +176,7 @@ __global__ void __launch_bounds__(256) normalise_kernel(const StartParams prm)
 // depend on who that is.
 constexpr int KS = 64;
 constexpr uint32_t BOX = 64 * 128;
+constexpr int kTable = 32;               // tiles of a run whose geometry is looked up ahead
 constexpr uint32_t kStaging = 8192;      // of an epilogue warp: two pieces of 32 rows x 128 bytes
 
 template <int CG> struct Shape {
@@ -186,7 +187,7 @@ template <int CG> struct Shape {
     static constexpr int STAGES = 5;
     static constexpr int NEPI = CG == 2 ? 8 : 4, THREADS = 64 + 32 * NEPI;   // epilogue warps
     static constexpr uint32_t TMEM = 2 * BN;                                 // two accumulators
-    static constexpr size_t SMEM = (size_t)STAGES * STAGE + NEPI * kStaging + 256 + 1024;
+    static constexpr size_t SMEM = (size_t)STAGES * STAGE + NEPI * kStaging + kTable * 48 + 256 + 1024;
 };
 
 struct ProductParams {
@@ -214,19 +215,16 @@ __device__ __forceinline__ Work work_of(const Matrix &m, int step)
                   : Work{m.rows, m.cols, m.r, kPolyMap, x, false, true, true, false};
 }
 
-// The last step's result: out = X, or w = decay w - step scale X, with the weights fetched a piece ahead.
-//   wide     rows start at 16-byte boundaries: a lane has a row, 128 bytes of it at a time, for the arithmetic (as tensor
-//            memory is read), and an eighth of four rows' 128 bytes for the stores
-//   others   32 x 32 entries at a time: a lane has a column, or two neighbouring ones of a 16-bit type whose rows start at
-//            4-byte boundaries, of every row or every other row
+// The last step's result, 32 x 32 entries at a time: out = X, or w = decay w - step scale X, with the weights fetched a piece
+// ahead.
+//   quads    rows hold whole quads of entries: a lane has four entries of every fourth row, eight lanes a row's 32
+//   others   a lane has a column, or two neighbouring ones of a 16-bit type whose rows start at 4-byte boundaries, of every
+//            row or every other row
 template <typename T> struct Weights {
-    static constexpr int WIDE = 128 / (int)sizeof(T);     // columns of a wide piece
     uint32_t w[32];
+    struct alignas(4 * sizeof(T)) Quad { T v[4]; };
 
-    static __device__ __forceinline__ bool wide(const OutputArgs &o, const Matrix &mx)
-    {
-        return (mx.cols * (int64_t)sizeof(T)) % 16 == 0 && (reinterpret_cast<uintptr_t>(static_cast<T *>(o.ptr) + mx.off) & 15u) == 0;
-    }
+    static __device__ __forceinline__ bool quads(const Matrix &mx) { return (mx.cols & 3) == 0; }    // (layers start at quads too)
     static __device__ __forceinline__ bool paired(const OutputArgs &o, const Matrix &mx)
     {
         return sizeof(T) == 2 && (mx.cols & 1) == 0 && (reinterpret_cast<uintptr_t>(static_cast<T *>(o.ptr) + mx.off) & 3u) == 0;
@@ -236,13 +234,19 @@ template <typename T> struct Weights {
     {
         if (!o.update) return;
         const T *at = static_cast<const T *>(o.ptr) + mx.off + (int64_t)m * mx.cols + n;
-        if (wide(o, mx)) {
-            const T *d = at + (int64_t)lane * mx.cols;
+        if (quads(mx)) {
+            const int c = 4 * (lane & 7);
+            const T *d = at + (int64_t)(lane >> 3) * mx.cols + c;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (lane < rows && i * (16 / (int)sizeof(T)) < cols) {
-                    const uint4 q = *reinterpret_cast<const uint4 *>(d + i * (16 / (int)sizeof(T)));
-                    w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
+                if (c < cols && 4 * i + (lane >> 3) < rows) {
+                    if constexpr (sizeof(T) == 2) {
+                        const uint2 x = *reinterpret_cast<const uint2 *>(d + (int64_t)4 * i * mx.cols);
+                        w[2 * i] = x.x; w[2 * i + 1] = x.y;
+                    } else {
+                        const uint4 x = *reinterpret_cast<const uint4 *>(d + (int64_t)4 * i * mx.cols);
+                        w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
+                    }
                 }
             }
         } else if (paired(o, mx)) {
@@ -270,39 +274,25 @@ template <typename T> struct Weights {
         memcpy(&e, &u, 2);
         return to_f(e);
     }
-    // 64 columns of this lane's row (a 32-bit type: the first or last 32 of them), staged and stored
-    __device__ __forceinline__ void finish_wide(const OutputArgs &o, const Matrix &mx, unsigned char *buf, int lane, int m, int n, int rows,
-                                                int cols, float (&a)[32], float (&b)[32])
+    // a piece as stage_swizzled leaves it
+    __device__ __forceinline__ void finish_quads(const OutputArgs &o, const Matrix &mx, const unsigned char *buf, int lane, int m, int n,
+                                                 int rows, int cols)
     {
         const float f = 1.0f / (kGramScale * mx.sx), k = o.update ? -o.step * mx.scale * f : f;
-        if constexpr (sizeof(T) == 2) {
-#pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float(&x)[32] = h ? b : a;
-                    const uint32_t two = w[16 * h + i / 2];
-                    x[i] = o.update ? __fmaf_rn(k, x[i], o.decay * entry(two)) : x[i] * k;
-                    x[i + 1] = o.update ? __fmaf_rn(k, x[i + 1], o.decay * entry(two >> 16)) : x[i + 1] * k;
-                }
-            }
-            __syncwarp();
-            stage_swizzled16<T>(buf, lane, a, b);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) a[i] = o.update ? __fmaf_rn(k, a[i], o.decay * entry(w[i])) : a[i] * k;
-            __syncwarp();
-            stage_swizzled(buf, lane, a);
-        }
-        __syncwarp();
-        const int c = (lane & 7) * (16 / (int)sizeof(T));
-        T *d = static_cast<T *>(o.ptr) + mx.off + (int64_t)m * mx.cols + n + c;
+        const int c = 4 * (lane & 7);
+        T *d = static_cast<T *>(o.ptr) + mx.off + (int64_t)m * mx.cols + n + (int64_t)(lane >> 3) * mx.cols + c;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int r = 4 * i + (lane >> 3);
+            const float4 q = *reinterpret_cast<const float4 *>(buf + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+            float x[4] = {q.x * k, q.y * k, q.z * k, q.w * k};
+            if (o.update) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    x[e] = __fmaf_rn(o.decay, sizeof(T) == 4 ? entry(w[4 * i + e]) : entry(w[2 * i + (e >> 1)] >> (16 * (e & 1))), x[e]);
+            }
             if (r < rows && c < cols)
-                *reinterpret_cast<uint4 *>(d + (int64_t)r * mx.cols) =
-                    *reinterpret_cast<const uint4 *>(buf + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+                *reinterpret_cast<Quad *>(d + (int64_t)4 * i * mx.cols) = Quad{{from_f<T>(x[0]), from_f<T>(x[1]), from_f<T>(x[2]), from_f<T>(x[3])}};
         }
     }
     // a staged piece of 32 x 32
@@ -338,13 +328,16 @@ template <typename T> struct Weights {
     }
 };
 
-__device__ __forceinline__ void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
-// 16 halves of a row (32 bytes, aligned)
-__device__ __forceinline__ void load16(const __half *p, uint32_t (&w)[8])
-{
-    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
-}
+// A tile of the run as the roles need it.  The first kTable ones are looked up before the loops: in them a look-up, two
+// dependent loads that miss L1 behind the tiles' own traffic, took longer than a stage.
+struct Seen {
+    int32_t matrix, m0, n0, M, N, K, k0, k1;
+    uint16_t part, parts;
+    uint16_t a_map, b_map;
+    int32_t slot;
+    bool a_mn, b_mn, a_sym, b_sym;
+};
+static_assert(sizeof(Seen) == 48, "table");
 
 // T: the type of the last step's result (PHASE kLast).
 template <int PHASE, int CG, typename T = float>
@@ -354,9 +347,11 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     unsigned char *staging = smem + (size_t)S::STAGES * S::STAGE;
-    uint64_t *bars = reinterpret_cast<uint64_t *>(staging + S::NEPI * kStaging);
+    Seen *table = reinterpret_cast<Seen *>(staging + S::NEPI * kStaging);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(table + kTable);
     uint64_t *full = bars, *empty = full + S::STAGES, *d_full = empty + S::STAGES, *d_empty = d_full + 2;
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(d_empty + 2);
+    uint64_t *lo_full = d_empty + 2;         // [NEPI] low halves of a warp's pieces have landed
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(lo_full + S::NEPI);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CG == 2 ? (int)cluster_rank() : 0;
@@ -364,56 +359,51 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::STAGES; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(d_full + i, 1); mbar_init(d_empty + i, CG * S::NEPI); }
+        for (int i = 0; i < S::NEPI; ++i) mbar_init(lo_full + i, 1);
         *abort_flag = 0;
         const_cast<int *>(abort_flag)[2] = prm.wait_kcycles;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc<CG>(tmem_slot, S::TMEM);
+    // this CTA's (pair's) run of tiles; the plan's tables do not change, so they are read before the wait for the last launch
+    const Tile *tiles = prm.dev.run[PHASE].tiles;
+    const int t_begin = prm.dev.run[PHASE].start[blockIdx.x / CG], t_end = prm.dev.run[PHASE].start[blockIdx.x / CG + 1];
+    auto look_up = [&](int t) {
+        const Tile tile = tiles[t];
+        const Work w = work_of<PHASE>(prm.dev.mats[tile.matrix], prm.step);
+        Seen s;
+        s.matrix = tile.matrix; s.m0 = tile.tm * 128 * CG; s.n0 = tile.tn * S::BN;
+        s.M = w.M; s.N = w.N; s.K = w.K; s.k0 = tile.k0; s.k1 = tile.k1;
+        s.part = (uint16_t)tile.part; s.parts = (uint16_t)tile.parts; s.slot = tile.slot;
+        s.a_map = (uint16_t)w.a_map; s.b_map = (uint16_t)w.b_map;
+        s.a_mn = w.a_mn; s.b_mn = w.b_mn; s.a_sym = w.a_sym; s.b_sym = w.b_sym;
+        return s;
+    };
+    if ((int)threadIdx.x < min(kTable, t_end - t_begin)) table[threadIdx.x] = look_up(t_begin + threadIdx.x);
+    auto seen = [&](int t) { return t - t_begin < kTable ? table[t - t_begin] : look_up(t); };
     tc_fence_before();
     if (CG == 2) cluster_sync(); else __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     bool failed = false;
-    // this CTA's (pair's) run of tiles; the plan's tables do not change, so they are read before the wait for the last launch
-    constexpr bool APPLY = PHASE == kApply || PHASE == kLast;
-    const Tile *tiles = prm.dev.run[PHASE].tiles;
-    const int t_begin = prm.dev.run[PHASE].start[blockIdx.x / CG], t_end = prm.dev.run[PHASE].start[blockIdx.x / CG + 1];
 
     if (warp == 0) {
         if (lane == 0) {
-            // a tile's geometry, looked up while the one before it is loaded
-            struct Loads {
-                const CUtensorMap *a, *b;
-                int m0, n0, k0, k1, a_left, b_left;
-                bool a_mn, b_mn;
-            };
-            auto loads_of = [&](int t) {
-                const Tile tile = tiles[t];
-                const Work w = work_of<PHASE>(prm.dev.mats[tile.matrix], prm.step);
-                Loads l;
-                l.a = prm.dev.maps + (size_t)tile.matrix * kMaps + w.a_map;
-                l.b = prm.dev.maps + (size_t)tile.matrix * kMaps + w.b_map;
-                // a pair's columns are split in halves of a multiple of 8 (the last tile's may be narrow)
-                const int half_n = CG == 2 ? min(S::BN, (w.N - tile.tn * S::BN + 15) / 16 * 16) / 2 : 0;
-                l.m0 = tile.tm * 128 * CG + 128 * rank;
-                l.n0 = tile.tn * S::BN + half_n * rank;
-                // steps of the contraction left of the diagonal's block of a symmetric operand's rows
-                l.a_left = w.a_sym ? l.m0 / S::BLOCK * S::BLOCK : 0;
-                l.b_left = w.b_sym ? tile.tn * S::BN / S::BLOCK * S::BLOCK : 0;
-                l.a_mn = w.a_mn;
-                l.b_mn = w.b_mn;
-                l.k0 = tile.k0;
-                l.k1 = tile.k1;
-                return l;
-            };
-            Loads l = loads_of(t_begin);
-            asm volatile("prefetch.tensormap [%0];" ::"l"(l.a));
-            asm volatile("prefetch.tensormap [%0];" ::"l"(l.b));
+            Seen l = seen(t_begin);
+            const CUtensorMap *maps = prm.dev.maps + (size_t)l.matrix * kMaps;
+            asm volatile("prefetch.tensormap [%0];" ::"l"(maps + l.a_map));
+            asm volatile("prefetch.tensormap [%0];" ::"l"(maps + l.b_map));
             grid_dependency_wait();          // what the previous launch wrote is visible from here on
             fence_proxy_async_global();      // and read by TMA, plain stores included
             uint32_t c = 0;
             for (int t = t_begin; t < t_end && !failed; ++t) {
-                const Loads next = loads_of(min(t + 1, t_end - 1));
+                const Seen next = seen(min(t + 1, t_end - 1));
+                const CUtensorMap *map_a = prm.dev.maps + (size_t)l.matrix * kMaps + l.a_map, *map_b = prm.dev.maps + (size_t)l.matrix * kMaps + l.b_map;
+                // a pair's columns are split in halves of a multiple of 8 (the last tile's may be narrow)
+                const int half_n = CG == 2 ? min(S::BN, (l.N - l.n0 + 15) / 16 * 16) / 2 : 0;
+                const int m0 = l.m0 + 128 * rank, n0 = l.n0 + half_n * rank;
+                // steps of the contraction left of the diagonal's block of a symmetric operand's rows
+                const int a_left = l.a_sym ? l.m0 / S::BLOCK * S::BLOCK : 0, b_left = l.b_sym ? l.n0 / S::BLOCK * S::BLOCK : 0;
                 for (int st = l.k0; st < l.k1; ++st, ++c) {
                     const uint32_t s = c % S::STAGES;
                     if (!mbar_poll(empty + s, ((c / S::STAGES) & 1) ^ 1, abort_flag)) { failed = true; break; }
@@ -427,9 +417,9 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                         else tma_load_2d(to, map, mn ? at : k, mn ? k : at, full + s);
                     };
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) load(dst + i * BOX, l.a, l.a_mn || k < l.a_left, l.m0 + 64 * i);
+                    for (int i = 0; i < 2; ++i) load(dst + i * BOX, map_a, l.a_mn || k < a_left, m0 + 64 * i);
 #pragma unroll
-                    for (int i = 0; i < S::NB; ++i) load(dst + S::A_BYTES + i * BOX, l.b, l.b_mn || k < l.b_left, l.n0 + 64 * i);
+                    for (int i = 0; i < S::NB; ++i) load(dst + S::A_BYTES + i * BOX, map_b, l.b_mn || k < b_left, n0 + 64 * i);
                 }
                 l = next;
             }
@@ -442,16 +432,14 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
     } else if (warp == 1) {
         uint32_t c = 0, u = 0;
         for (int t = t_begin; rank == 0 && t < t_end && !failed; ++t, ++u) {
-            const Tile tile = tiles[t];
-            const Work w = work_of<PHASE>(prm.dev.mats[tile.matrix], prm.step);
+            const Seen w = seen(t);
             const uint32_t buf = u & 1, d = tmem + buf * S::BN;
-            const int n = min(S::BN, (w.N - tile.tn * S::BN + 15) / 16 * 16);
-            const int a_left = w.a_sym ? tile.tm * 128 * CG / S::BLOCK * S::BLOCK : 0;
-            const int b_left = w.b_sym ? tile.tn * S::BN / S::BLOCK * S::BLOCK : 0;
+            const int n = min(S::BN, (w.N - w.n0 + 15) / 16 * 16);
+            const int a_left = w.a_sym ? w.m0 / S::BLOCK * S::BLOCK : 0, b_left = w.b_sym ? w.n0 / S::BLOCK * S::BLOCK : 0;
             bool ok = mbar_poll(d_empty + buf, ((u >> 1) & 1) ^ 1, abort_flag);
             if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
             tc_fence_after();
-            for (int st = tile.k0; st < tile.k1; ++st, ++c) {
+            for (int st = w.k0; st < w.k1; ++st, ++c) {
                 const uint32_t s = c % S::STAGES;
                 ok = mbar_poll(full + s, (c / S::STAGES) & 1, abort_flag);
                 if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
@@ -467,9 +455,9 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        if (k < n_mma) tc_mma_f16<CG>(d, da + k * ia, db + k * ib, idesc, st > tile.k0 || k > 0);
+                        if (k < n_mma) tc_mma_f16<CG>(d, da + k * ia, db + k * ib, idesc, st > w.k0 || k > 0);
                     if (CG == 2) tc_commit_pair(empty + s); else tc_commit(empty + s);
-                    if (st == tile.k1 - 1) { if (CG == 2) tc_commit_pair(d_full + buf); else tc_commit(d_full + buf); }
+                    if (st == w.k1 - 1) { if (CG == 2) tc_commit_pair(d_full + buf); else tc_commit(d_full + buf); }
                 }
                 __syncwarp();
             }
@@ -481,64 +469,39 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
         constexpr int COLS = S::BN / (S::NEPI / 4), PIECES = COLS / 64;      // of a warp
         const bool read_lo = PHASE == kApply && prm.step < kExactSteps;
         const bool write_lo = PHASE == kApply && prm.step + 1 < kExactSteps;
-        // A tile as this warp sees it: its first row and column, its rows inside the product.
-        struct Place {
-            const Matrix *mx;
-            int m0, c0, rows, N;
-        };
-        auto place = [&](int t) {
-            const Tile tile = tiles[t];
-            const Matrix *mx = prm.dev.mats + tile.matrix;
-            const Work w = work_of<PHASE>(*mx, prm.step);
-            const int m0 = tile.tm * 128 * CG + 128 * rank + 32 * q;
-            return Place{mx, m0, tile.tn * S::BN + half * COLS, min(32, w.M - m0), w.N};
-        };
-        // What the epilogue reads besides the accumulator is asked for a piece ahead, across tiles, and a tile ahead into L2.
-        uint32_t lo[4][8];
-        auto fetch_lo = [&](const Place &at, int n0) {
+        // What the epilogue reads besides the accumulator is on its way before the tile's MMAs are done: X's low halves come
+        // into the staging areas by TMA, where their new values, or X's, take their place; the weights a piece ahead.
+        auto load_lo = [&](const Seen &at) {
+            if (lane == 0) {
+                mbar_arrive_expect_tx(lo_full + warp - 2, PIECES * 4096);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) lo[i][e] = 0;
-                if (lane < at.rows && n0 + 16 * i < at.mx->ldx)
-                    load16(at.mx->lo + (int64_t)(at.m0 + lane) * at.mx->ldx + n0 + 16 * i, lo[i]);
+                for (int p = 0; p < PIECES; ++p)
+                    tma_load_2d(mine + p * 4096, prm.dev.maps + (size_t)at.matrix * kMaps + kLoOut, at.n0 + half * COLS + 64 * p,
+                                at.m0 + 128 * rank + 32 * q, lo_full + warp - 2);
             }
         };
         Weights<T> weights;
-        auto fetch_weights = [&](const Place &at, int n) {
-            const int most = Weights<T>::wide(prm.out, *at.mx) ? Weights<T>::WIDE : 32;
-            weights.fetch(prm.out, *at.mx, lane, at.m0, n, max(at.rows, 0), max(0, min(most, at.N - n)));
+        auto fetch_weights = [&](const Seen &at, int n) {
+            const int m0 = at.m0 + 128 * rank + 32 * q;
+            weights.fetch(prm.out, prm.dev.mats[at.matrix], lane, m0, n, max(0, min(32, at.M - m0)), max(0, min(32, at.N - n)));
         };
-        auto look_ahead = [&](const Place &at) {
-            if (lane >= at.rows) return;
-            if (PHASE == kApply && read_lo) {
-                const __half *row = at.mx->lo + (int64_t)(at.m0 + lane) * at.mx->ldx;
-#pragma unroll
-                for (int c = 0; c < COLS; c += 64)
-                    if (at.c0 + c < at.mx->ldx) prefetch_l2(row + at.c0 + c);
-            }
-            if (PHASE == kLast && prm.out.update) {
-                const T *row = static_cast<const T *>(prm.out.ptr) + at.mx->off + (int64_t)(at.m0 + lane) * at.mx->cols;
-#pragma unroll
-                for (int c = 0; c < COLS; c += 128 / (int)sizeof(T))
-                    if (at.c0 + c < at.N) prefetch_l2(row + at.c0 + c);
-            }
-        };
-        Place here = place(t_begin);
+        Seen here = seen(t_begin);
         grid_dependency_wait();      // (before anything that another launch writes is read, or written)
-        if (PHASE == kApply && read_lo) fetch_lo(here, here.c0);
-        if (PHASE == kLast) fetch_weights(here, here.c0);
+        if (PHASE == kApply && read_lo) load_lo(here);
+        if (PHASE == kLast) fetch_weights(here, here.n0 + half * COLS);
         uint32_t u = 0, stores = 0;
         for (int t = t_begin; t < t_end; ++t, ++u) {
-            const Place next = place(min(t + 1, t_end - 1));
-            const Matrix &mx = *here.mx;
-            const int m0 = here.m0, c0 = here.c0, rows = here.rows;
-            const CUtensorMap *maps = prm.dev.maps + (size_t)tiles[t].matrix * kMaps;
+            const Seen next = seen(min(t + 1, t_end - 1));
+            const Matrix &mx = prm.dev.mats[here.matrix];
+            const int m0 = here.m0 + 128 * rank + 32 * q, c0 = here.n0 + half * COLS;      // first row and column of this warp's pieces
+            const int rows = min(32, here.M - m0);
+            const CUtensorMap *maps = prm.dev.maps + (size_t)here.matrix * kMaps;
             const uint32_t ab = u & 1;
-            if (APPLY && t + 1 < t_end) look_ahead(next);
+            const float sx = mx.sx;
             bool ok = mbar_poll(d_full + ab, (u >> 1) & 1, abort_flag);
             if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
             tc_fence_after();
+            uint32_t new_lo[PIECES][32];
             auto read_accumulator = [&](int p, float (&v)[2][32]) {
                 tmem_ld32_wait(tmem + lane_base + ab * S::BN + half * COLS + p * 64, v[0]);
                 tmem_ld32_wait(tmem + lane_base + ab * S::BN + half * COLS + p * 64 + 32, v[1]);
@@ -549,13 +512,13 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                 }
             };
             // a part of a contraction: this warp's pieces go to scratch, and the last warp to bring its part goes on
-            const int parts = PHASE == kGram ? tiles[t].parts : 1;
+            const int parts = PHASE == kGram ? here.parts : 1;
             constexpr int PER_CTA = 4 * S::BN / 64, PER_PART = CG * PER_CTA;      // pieces
             float4 *scratch = nullptr;
             if (PHASE == kGram && parts > 1) {
-                const int first = tiles[t].slot + rank * PER_CTA + (q * (S::NEPI / 4) + half) * PIECES;
+                const int first = here.slot + rank * PER_CTA + (q * (S::NEPI / 4) + half) * PIECES;
                 scratch = reinterpret_cast<float4 *>(prm.dev.parts) + (int64_t)first * 512 + lane;
-                float4 *own = scratch + (int64_t)tiles[t].part * PER_PART * 512;
+                float4 *own = scratch + (int64_t)here.part * PER_PART * 512;
 #pragma unroll
                 for (int p = 0; p < PIECES; ++p) {
                     float v[2][32];
@@ -597,49 +560,32 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                     read_accumulator(p, v);
                 }
                 if (PHASE == kLast) {
-                    const bool wide = Weights<T>::wide(prm.out, mx);
+                    const bool quads = Weights<T>::quads(mx);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const int n = n0 + 32 * h;
-                        if (sizeof(T) == 2 && wide && h == 1) break;        // the first round took all 64 columns
-                        if (live && n < here.N) {
-                            if (wide) {
-                                weights.finish_wide(prm.out, mx, mine, lane, m0, n, rows, min(Weights<T>::WIDE, here.N - n), v[h], v[h ^ 1]);
+                        const int n = n0 + 32 * h, cols = min(32, here.N - n);
+                        if (live && cols > 0) {
+                            if (quads) {
+                                __syncwarp();
+                                stage_swizzled(mine, lane, v[h]);
+                                __syncwarp();
+                                weights.finish_quads(prm.out, mx, mine, lane, m0, n, rows, cols);
                             } else {
                                 stage_piece(reinterpret_cast<float *>(mine), lane, v[h]);
-                                weights.finish(prm.out, mx, reinterpret_cast<const float *>(mine), lane, m0, n, rows, min(32, here.N - n));
+                                weights.finish(prm.out, mx, reinterpret_cast<const float *>(mine), lane, m0, n, rows, cols);
                             }
                         }
-                        const int after = p * 64 + h * 32 + (wide ? Weights<T>::WIDE : 32);
+                        const int after = p * 64 + h * 32 + 32;
                         if (after < COLS) fetch_weights(here, c0 + after);
-                        else if (t + 1 < t_end) fetch_weights(next, next.c0);
+                        else if (t + 1 < t_end) fetch_weights(next, next.n0 + half * COLS);
                     }
                     continue;
                 }
-                if (PHASE == kApply) {       // X' = P X_hi + a X_lo
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            v[h][i] *= 1.0f / kGramScale;
-                            v[h][i + 1] *= 1.0f / kGramScale;
-                            if (read_lo) {
-                                const float2 l = unpack_half2(lo[2 * h + (i >> 4)][(i & 15) >> 1]);
-                                v[h][i] = __fmaf_rn(kA, l.x, v[h][i]);
-                                v[h][i + 1] = __fmaf_rn(kA, l.y, v[h][i + 1]);
-                            }
-                        }
-                    if (read_lo) {
-                        if (p + 1 < PIECES) fetch_lo(here, n0 + 64);
-                        else if (t + 1 < t_end) fetch_lo(next, next.c0);
-                    }
-                }
-                if (!live) continue;
-                auto store = [&](unsigned char *from, int map) {      // the staged piece, by one lane
+                auto store = [&](unsigned char *from, int map, int n) {      // a staged piece, by one lane
                     fence_proxy_async();
                     __syncwarp();
                     if (lane == 0) {
-                        tma_store_2d(maps + map, n0, m0, from);
+                        tma_store_2d(maps + map, n, m0, from);
                         bulk_commit_group();
                     }
                 };
@@ -648,32 +594,76 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                     __syncwarp();
                     return mine + (stores++ & 1) * 4096;
                 };
-                if (PHASE == kApply) {
-                    unsigned char *to = room();
-                    stage_swizzled16<__half>(to, lane, v[0], v[1]);
-                    store(to, kX0Out + ((prm.step + 1) & 1));
+                if (PHASE == kApply) {       // X' = P X_hi + a X_lo
+                    if (read_lo && p == 0) {
+                        ok = mbar_poll(lo_full + warp - 2, u & 1, abort_flag);
+                        if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            uint4 l = make_uint4(0, 0, 0, 0);
+                            if (read_lo) l = *reinterpret_cast<const uint4 *>(mine + p * 4096 + lane * 128 + (((4 * h + j) ^ (lane & 7)) << 4));
+                            const uint32_t w[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int i = 8 * j + 2 * e;
+                                v[h][i] *= 1.0f / kGramScale;
+                                v[h][i + 1] *= 1.0f / kGramScale;
+                                if (read_lo) {
+                                    const float2 x = unpack_half2(w[e]);
+                                    v[h][i] = __fmaf_rn(kA, x.x, v[h][i]);
+                                    v[h][i + 1] = __fmaf_rn(kA, x.y, v[h][i + 1]);
+                                }
+                            }
+                        }
+                    if (live) {
+                        // (in place: a lane has read its row of the piece)
+                        unsigned char *to = read_lo ? mine + p * 4096 : room();
+                        stage_swizzled16<__half>(to, lane, v[0], v[1]);
+                        store(to, kX0Out + ((prm.step + 1) & 1), n0);
+                    }
                     if (write_lo) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h)
 #pragma unroll
                             for (int i = 0; i < 32; i += 2) {
-                                const float2 f = unpack_half2(pack2<__half>(v[h][i], v[h][i + 1]));
-                                v[h][i] -= f.x;
-                                v[h][i + 1] -= f.y;
+                                const float2 x = unpack_half2(pack2<__half>(v[h][i], v[h][i + 1]));
+                                new_lo[p][16 * h + i / 2] = pack2<__half>(v[h][i] - x.x, v[h][i + 1] - x.y);
                             }
-                        to = room();
-                        stage_swizzled16<__half>(to, lane, v[0], v[1]);
-                        store(to, kLoOut);
+                    }
+                    if (p < PIECES - 1) continue;
+                    // the pieces' new low halves, each once X's store has read its area
+                    if (write_lo) {
+#pragma unroll
+                        for (int r = 0; r < PIECES; ++r) {
+                            if (rows <= 0 || c0 + 64 * r >= here.N) break;
+                            // (the store after the one of this area may still be reading)
+                            if (lane == 0) { if (PIECES == 2 && c0 + 64 < here.N) bulk_wait_group_read<1>(); else bulk_wait_group_read<0>(); }
+                            __syncwarp();
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                *reinterpret_cast<uint4 *>(mine + r * 4096 + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                                    make_uint4(new_lo[r][4 * j], new_lo[r][4 * j + 1], new_lo[r][4 * j + 2], new_lo[r][4 * j + 3]);
+                            store(mine + r * 4096, kLoOut, c0 + 64 * r);
+                        }
+                    }
+                    if (read_lo && t + 1 < t_end) {
+                        if (lane == 0) bulk_wait_group_read<0>();
+                        __syncwarp();
+                        load_lo(next);
                     }
                     continue;
                 }
+                if (!live) continue;
                 // A = X X^T and b I + c A, whose product with A the next launch takes; then P = a I + A (b I + c A)
                 auto put = [&](int map) {
                     unsigned char *to = room();
                     stage_swizzled16<__half>(to, lane, v[0], v[1]);
-                    store(to, map);
+                    store(to, map, n0);
                 };
-                const float f = PHASE == kGram ? kGramScale / (mx.sx * mx.sx) : 1.0f / kGramScale;
+                const float f = PHASE == kGram ? kGramScale / (sx * sx) : 1.0f / kGramScale;
                 const float diagonal = (PHASE == kGram ? kB : kA) * kGramScale;
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
@@ -689,9 +679,12 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                     }
                 if (PHASE == kGram) put(kFactorOut); else put(kPolyOut);
             }
+            if (failed) break;
             here = next;
         }
         if (lane == 0) bulk_wait_group_all();
+        if (failed && read_lo)       // low halves still under way (a bounded chance to land before the CTA exits)
+            for (int it = 0; it < 100000 && !mbar_try_wait(lo_full + warp - 2, u & 1); ++it) {}
     }
 
     if (failed) {
