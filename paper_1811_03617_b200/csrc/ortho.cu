@@ -60,6 +60,8 @@ __global__ void __launch_bounds__(256) momentum_kernel(const StartParams prm)
     __shared__ float scratch[8];
     ptx::launch_dependents();
     ptx::grid_dependency_wait();
+    // (zero already, unless a launch of the last call gave up)
+    for (int i = blockIdx.x * 256 + threadIdx.x; i < prm.dev.n_tickets; i += gridDim.x * 256) prm.dev.tickets[i] = 0;
     const Chunk ch = prm.dev.chunks[blockIdx.x];
     const Matrix &mx = prm.dev.mats[ch.matrix];
     const int64_t total = (int64_t)mx.rows * mx.cols, begin = (int64_t)ch.index * prm.dev.chunk;
@@ -171,9 +173,9 @@ __global__ void __launch_bounds__(256) normalise_kernel(const StartParams prm)
 //   CG = 1  one CTA, tile 128 x 64, for plans without enough large tiles to fill the GPU: four times the CTAs at work, a
 //           quarter of the time a stage.
 // A's contraction is the long side of the matrix and its tiles may be few: there the contraction is split between CTAs
-// (Tile::parts).  The sums of all parts go to scratch in fp32, a warp's piece by piece; of the warps that hold the same
-// piece of a tile the last to arrive adds the parts in their order and goes on with the epilogue, so the result does not
-// depend on who that is.
+// (Tile::parts).  The sums of all parts go to scratch in fp32, piece by piece; of the warps that hold the same piece of a
+// tile the last to arrive adds the parts in their order and goes on with the epilogue, so the result does not depend on
+// who that is.
 constexpr int KS = 64;
 constexpr uint32_t BOX = 64 * 128;
 constexpr int kTable = 32;               // tiles of a run whose geometry is looked up ahead
@@ -502,62 +504,56 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
             if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
             tc_fence_after();
             uint32_t new_lo[PIECES][32];
-            auto read_accumulator = [&](int p, float (&v)[2][32]) {
+            auto read_accumulator = [&](int p, bool last, float (&v)[2][32]) {
                 tmem_ld32_wait(tmem + lane_base + ab * S::BN + half * COLS + p * 64, v[0]);
                 tmem_ld32_wait(tmem + lane_base + ab * S::BN + half * COLS + p * 64 + 32, v[1]);
-                if (p == PIECES - 1) {       // the accumulator is free
+                if (last) {                  // the accumulator is free
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) { if (CG == 2) mbar_arrive_cluster(in_leader(d_empty + ab)); else mbar_arrive(d_empty + ab); }
                 }
             };
-            // a part of a contraction: this warp's pieces go to scratch, and the last warp to bring its part goes on
             const int parts = PHASE == kGram ? here.parts : 1;
-            constexpr int PER_CTA = 4 * S::BN / 64, PER_PART = CG * PER_CTA;      // pieces
-            float4 *scratch = nullptr;
-            if (PHASE == kGram && parts > 1) {
-                const int first = here.slot + rank * PER_CTA + (q * (S::NEPI / 4) + half) * PIECES;
-                scratch = reinterpret_cast<float4 *>(prm.dev.parts) + (int64_t)first * 512 + lane;
-                float4 *own = scratch + (int64_t)here.part * PER_PART * 512;
 #pragma unroll
-                for (int p = 0; p < PIECES; ++p) {
-                    float v[2][32];
-                    read_accumulator(p, v);
-                    if (rows <= 0 || c0 + p * 64 >= here.N) continue;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float *x = &v[i >> 3][4 * (i & 7)];
-                        __stcg(own + p * 512 + 32 * i, make_float4(x[0], x[1], x[2], x[3]));
-                    }
-                }
-                __threadfence();
-                __syncwarp();
-                int arrived = 0;
-                if (lane == 0) arrived = atomicAdd(prm.dev.tickets + first, 1);
-                if (__shfl_sync(0xffffffffu, arrived, 0) != parts - 1) { here = next; continue; }
-                if (lane == 0) prm.dev.tickets[first] = 0;
-                __threadfence();
-            }
-#pragma unroll
-            for (int p = 0; p < PIECES; ++p) {
+            for (int p_ = 0; p_ < PIECES; ++p_) {
+                // (parts take their pieces in different orders, so that the last to bring one is not the last for all)
+                const int p = PHASE == kGram && PIECES == 2 ? p_ ^ (here.part & 1) : p_;
                 const int n0 = c0 + p * 64;
                 const bool live = rows > 0 && n0 < here.N;
                 float v[2][32];
+                read_accumulator(p, p_ == PIECES - 1, v);
                 if (PHASE == kGram && parts > 1) {
                     if (!live) continue;
+                    // a part of a contraction: the piece goes to scratch, and whoever brings its last part adds them up
+                    constexpr int PER_CTA = 4 * S::BN / 64, PER_PART = CG * PER_CTA;      // pieces
+                    const int piece = here.slot + rank * PER_CTA + (q * (S::NEPI / 4) + half) * PIECES + p;
+                    float4 *scratch = reinterpret_cast<float4 *>(prm.dev.parts) + (int64_t)piece * 512 + lane;
+                    float4 *own = scratch + (int64_t)here.part * PER_PART * 512;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float *x = &v[i >> 3][4 * (i & 7)];
+                        __stcg(own + 32 * i, make_float4(x[0], x[1], x[2], x[3]));
+                    }
+                    __threadfence();
+                    __syncwarp();
+                    int arrived = 0;
+                    if (lane == 0) arrived = atomicAdd(prm.dev.tickets + piece, 1);
+                    if (__shfl_sync(0xffffffffu, arrived, 0) != parts - 1) continue;
+                    if (lane == 0) prm.dev.tickets[piece] = 0;
+                    __threadfence();
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[0][i] = v[1][i] = 0.0f;
                     for (int part = 0; part < parts; ++part) {
-                        const float4 *from = scratch + (int64_t)part * PER_PART * 512 + p * 512;
+                        const float4 *from = scratch + (int64_t)part * PER_PART * 512;
+                        float4 x[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) x[i] = __ldcg(from + 32 * i);
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const float4 x = __ldcg(from + 32 * i);
                             float *y = &v[i >> 3][4 * (i & 7)];
-                            y[0] += x.x; y[1] += x.y; y[2] += x.z; y[3] += x.w;
+                            y[0] += x[i].x; y[1] += x[i].y; y[2] += x[i].z; y[3] += x[i].w;
                         }
                     }
-                } else {
-                    read_accumulator(p, v);
                 }
                 if (PHASE == kLast) {
                     const bool quads = Weights<T>::quads(mx);

@@ -62,7 +62,8 @@ struct Device {
     int n_chunks;
     float *partial;                  // [n_chunks] sums of squares
     float *parts;                    // sums of parts of a contraction, pieces of 32 rows x 64 columns
-    int32_t *tickets;                // [pieces of a tile's first part] arrivals, zero between launches
+    int32_t *tickets;                // [n_tickets] arrivals at a piece (of a tile's first part), zero between launches
+    int n_tickets;
 };
 
 // momentum = beta * momentum + g (momentum may be null), u = g + beta * momentum (nesterov) or momentum, sums of squares;

@@ -22,7 +22,7 @@ struct gvq_ortho {
 namespace {
 
 constexpr size_t kAlign = 256;
-constexpr int kPartStages = 6, kMaxParts = 8;   // a part of a contraction: at least so many stages, at most so many parts
+constexpr int kPartStages = 6, kMaxParts = 4;   // a part of a contraction: at least so many stages, at most so many parts
 constexpr int kTileCost = 3;      // what a tile costs beyond its contraction, in stages of 64 steps
 // Pairs of CTAs on 256 x 256 tiles from this many multiply-adds of one X P on, 128 x 64 tiles below.  Measured on either side,
 // us per call: 1280 x 1280 (2.1e9) 231 / 186, twice 512 x 4608 (2.4e9) 245 / 189, 1500 x 1500 (3.4e9) 259 / 275, four
@@ -103,13 +103,15 @@ std::vector<int32_t> deal(std::vector<Tile> &tiles, int units)
     return start;
 }
 
-// Cuts contractions into parts where there are fewer tiles than CTAs.  `pieces`: of 32 x 64 entries in a tile.
+// Cuts contractions that are longer than a CTA's share of all of them.  `pieces`: of 32 x 64 entries in a tile.
 void split(std::vector<Tile> &tiles, int units, int pieces, int &slots)
 {
-    const int share = std::min(kMaxParts, tiles.empty() ? 1 : units / (int)tiles.size());
+    int64_t total = 0;
+    for (const Tile &t : tiles) total += t.k1;
+    const int64_t share = std::max<int64_t>(kPartStages, (total + units - 1) / units);
     std::vector<Tile> out;
     for (const Tile &t : tiles) {
-        const int parts = std::max(1, std::min(share, t.k1 / kPartStages));
+        const int parts = (int)std::min<int64_t>(kMaxParts, (t.k1 + share - 1) / share);
         for (int i = 0; i < parts; ++i) {
             Tile s = t;
             s.k0 = (int)((int64_t)t.k1 * i / parts);
@@ -261,6 +263,7 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
         d.chunks = reinterpret_cast<Chunk *>(t + o_c);
         d.n_chunks = (int)chunks.size();
         d.tickets = reinterpret_cast<int32_t *>(t + o_k);
+        d.n_tickets = slots;
         d.partial = reinterpret_cast<float *>(t + o_p);
         d.parts = reinterpret_cast<float *>(t + o_q);
         d.pair = pair;
