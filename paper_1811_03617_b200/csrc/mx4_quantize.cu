@@ -1,6 +1,7 @@
 // Quantization to microscaled 4-bit floating point, and back (gvq.h, "microscaled 4-bit").
 //
 //  mx4_quantize_kernel            a matrix, along its rows and / or along its columns (the transposed operand), read once
+//  mx4_quantize_rows_kernel       a matrix along its rows only, where they start at 16-byte boundaries
 //  mx4_quantize_aggregate_kernel  every node's slices, and the sum over the nodes of what the codes stand for
 //  mx4_dequantize_kernel          codes back to values, summed over the nodes
 #include "gvq_internal.h"
@@ -50,6 +51,10 @@ struct QuantParams {
     uint8_t *codes_t, *scales_t;   // along the columns
     int vec;                    // rows start at 16-byte boundaries
     int ct;                     // tiles along the columns
+    // of the row kernel: a CTA has rows_per_cta rows of a chunk of columns, chunk_blocks blocks (by_chunk: 2^32 over that, up)
+    int64_t padded_rows;
+    int rows_per_cta, chunks, chunk_blocks;
+    uint32_t by_chunk;
 };
 
 // One CTA: a tile of 128 x 128 entries, which is one tile of scale bytes of either form.  Rows: 16 lanes hold a row's
@@ -160,6 +165,85 @@ __global__ void __launch_bounds__(256) mx4_quantize_kernel(const QuantParams prm
     if (COLS && tid >= 32 && tid < 64)
         reinterpret_cast<uint4 *>(prm.scales_t + ((int64_t)ctile * tiles_of(prm.rows, 128) + rtile) * kTileBytes)[tid - 32] =
             reinterpret_cast<const uint4 *>(sc[1])[tid - 32];
+}
+
+// Max |x| of the entries in four words (NaN and infinity come out as themselves or as a NaN).
+template <typename T>
+__device__ __forceinline__ float amax_words(const uint32_t (&w)[8 * sizeof(T)])
+{
+    constexpr int N = 8 * (int)sizeof(T);
+    if constexpr (sizeof(T) == 4) {
+        float m = fabsf(__uint_as_float(w[0]));
+#pragma unroll
+        for (int i = 1; i < N; ++i) m = max_nan(m, fabsf(__uint_as_float(w[i])));
+        return m;
+    } else {      // patterns without their sign order like the magnitudes, two at a time
+        uint32_t m = w[0] & 0x7FFF7FFFu;
+#pragma unroll
+        for (int i = 1; i < N; ++i) m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
+        const uint16_t top = (uint16_t)max(m & 0xFFFFu, m >> 16);
+        T e;
+        memcpy(&e, &top, 2);
+        return to_f(e);
+    }
+}
+
+// Along the rows only: a lane has a whole block, so that what belongs to a block (its largest entry, its scale, its row's
+// random word) costs a lane once and no shuffles; its 16 bytes of codes lie next to its neighbours'.  With a quad for a
+// block, as in the tile kernel, those were half of 13 instructions an entry, and instructions are what bounds this.
+template <typename T, bool SR>
+__global__ void __launch_bounds__(256) mx4_quantize_rows_kernel(const QuantParams prm)
+{
+    constexpr int W = 8 * (int)sizeof(T);          // words of a block
+    ptx::launch_dependents();
+    ptx::grid_dependency_wait();
+    const int chunk = blockIdx.x % prm.chunks;
+    const int64_t row0 = (int64_t)(blockIdx.x / prm.chunks) * prm.rows_per_cta;
+    const int64_t nb = blocks(prm.cols), kt = tiles_of(nb, kTileBlocks);
+    const int b0 = chunk * prm.chunk_blocks, n_b = (int)min((int64_t)prm.chunk_blocks, kt * kTileBlocks - b0);   // padded
+    const int items = prm.rows_per_cta * n_b;
+    const T *x = static_cast<const T *>(prm.x);
+    for (int it = threadIdx.x; it < items; it += 256) {
+        // (it < 2^16: exact)
+        const int r = n_b == prm.chunk_blocks ? (int)__umulhi((uint32_t)it, prm.by_chunk) : it / n_b;
+        const int64_t row = row0 + r, b = b0 + it - r * n_b;
+        if (row >= prm.padded_rows) break;
+        uint32_t s = 0;
+        if (row < prm.rows && b < nb) {
+            uint32_t w[W];
+            const T *from = x + row * prm.ld + b * kBlock;
+            const int n = (int)min((int64_t)kBlock, prm.cols - b * kBlock);
+            if (n == kBlock) {
+#pragma unroll
+                for (int i = 0; i < W / 4; ++i) {
+                    const uint4 q = __ldcs(reinterpret_cast<const uint4 *>(from) + i);
+                    w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
+                }
+            } else {
+                T e[kBlock];
+#pragma unroll
+                for (int i = 0; i < kBlock; ++i) e[i] = i < n ? from[i] : T(0.0f);
+                memcpy(w, e, sizeof(w));
+            }
+            s = scale_byte(amax_words<T>(w));
+            const float inv = inv_scale(min(s, 253u));
+            const uint64_t h = SR ? row_word(prm.seed_w, row) : 0;
+            uint32_t code[4];
+#pragma unroll
+            for (int o = 0; o < 4; ++o) {
+                float v[8];
+                T e[8];
+                memcpy(e, w + o * (W / 4), sizeof(e));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = to_f(e[i]);
+                clear_invalid(v, s);
+                grid8<SR>(v, inv, h, (uint32_t)(b * 16 + 4 * o));
+                code[o] = codes8(v);
+            }
+            reinterpret_cast<uint4 *>(prm.codes)[row * nb + b] = make_uint4(code[0], code[1], code[2], code[3]);
+        }
+        prm.scales[scale_at(row, b, kt)] = (uint8_t)s;      // (past the matrix: 0)
+    }
 }
 
 struct AggParams {
@@ -348,6 +432,17 @@ cudaError_t launch_quantize_as(cudaStream_t st, const QuantParams &prm)
 template <typename T, bool SR>
 cudaError_t launch_quantize_forms(cudaStream_t st, const QuantParams &prm)
 {
+    if (prm.codes && !prm.codes_t && prm.vec) {
+        QuantParams p = prm;
+        const int64_t padded = tiles_of(blocks(prm.cols), kTileBlocks) * kTileBlocks;
+        p.chunk_blocks = (int)min(padded, (int64_t)1024);
+        p.chunks = (int)tiles_of(padded, 1024);
+        p.by_chunk = (uint32_t)((((uint64_t)1 << 32) + p.chunk_blocks - 1) / p.chunk_blocks);
+        p.rows_per_cta = max(1, 1024 / p.chunk_blocks);
+        p.padded_rows = tiles_of(prm.rows, kTileRows) * kTileRows;
+        const int64_t grid = p.chunks * tiles_of(p.padded_rows, p.rows_per_cta);
+        if (grid <= INT32_MAX) return ptx::launch_chained<mx4_quantize_rows_kernel<T, SR>>(p, (int)grid, 256, 0, 1, st);
+    }
     if (prm.codes && prm.codes_t) return launch_quantize_as<T, SR, true, true>(st, prm);
     if (prm.codes) return launch_quantize_as<T, SR, true, false>(st, prm);
     return launch_quantize_as<T, SR, false, true>(st, prm);
