@@ -57,17 +57,63 @@ struct QuantParams {
     uint32_t by_chunk;
 };
 
-// One CTA: a tile of 128 x 128 entries, which is one tile of scale bytes of either form.  Rows: 16 lanes hold a row's
-// 128 entries (eight each, 16- or 32-byte loads), a quad holds a block.  Columns: the same entries go through shared
-// memory in their own type, and a thread takes 32 entries of a column (two columns of a 16-bit type at a time, so that
-// a word is read once).  The columns' blocks are skewed by eight words per 32 rows, so that the four blocks of eight
-// columns that a warp works on lie in different banks, and a warp's four lanes write 64 bytes of one output row.
+// Max |x| of the entries in four words (NaN and infinity come out as themselves or as a NaN).
+template <typename T>
+__device__ __forceinline__ float amax_words(const uint32_t (&w)[8 * sizeof(T)])
+{
+    constexpr int N = 8 * (int)sizeof(T);
+    if constexpr (sizeof(T) == 4) {
+        float m = fabsf(__uint_as_float(w[0]));
+#pragma unroll
+        for (int i = 1; i < N; ++i) m = max_nan(m, fabsf(__uint_as_float(w[i])));
+        return m;
+    } else {      // patterns without their sign order like the magnitudes, two at a time
+        uint32_t m = w[0] & 0x7FFF7FFFu;
+#pragma unroll
+        for (int i = 1; i < N; ++i) m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
+        const uint16_t top = (uint16_t)max(m & 0xFFFFu, m >> 16);
+        T e;
+        memcpy(&e, &top, 2);
+        return to_f(e);
+    }
+}
+
+// Thirty-two entries that a lane holds in words -> its block's scale byte and 16 bytes of codes.
+template <typename T, bool SR>
+__device__ __forceinline__ uint4 quantize_block(const uint32_t (&w)[8 * sizeof(T)], uint64_t h, uint32_t p0, uint32_t &s)
+{
+    s = scale_byte(amax_words<T>(w));
+    const float inv = inv_scale(min(s, 253u));
+    uint32_t code[4];
+#pragma unroll
+    for (int o = 0; o < 4; ++o) {
+        float v[8];
+        T e[8];
+        memcpy(e, w + o * 2 * sizeof(T), sizeof(e));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = to_f(e[i]);
+        clear_invalid(v, s);
+        grid8<SR>(v, inv, h, p0 + 4 * o);
+        code[o] = codes8(v);
+    }
+    return make_uint4(code[0], code[1], code[2], code[3]);
+}
+
+// One CTA: a tile of 128 x 128 entries, which is one tile of scale bytes of either form, read once (16 lanes have a row,
+// 16 or 32 bytes each).  With COLS it goes through shared memory in its own type, rows 4 words longer than they are so that
+// eight lanes' 16-byte words of eight rows lie in different banks.
+//   ROWS alone   a quad of lanes quantizes a block as it comes
+//   both         a lane takes a row's block from shared memory; the codes go out through shared memory, 64 bytes of a row
+//   COLS         a thread takes 32 entries of a column (two columns of a 16-bit type at a time, so that a word is read once);
+//                another eight words per 32 rows put the four blocks of eight columns that a warp works on in different
+//                banks, and a warp's four lanes write 64 bytes of one output row
 template <typename T, bool SR, bool ROWS, bool COLS>
 __global__ void __launch_bounds__(256) mx4_quantize_kernel(const QuantParams prm)
 {
-    constexpr int W = 128 * (int)sizeof(T) / 4;    // words of a row of the tile
+    constexpr int W = 128 * (int)sizeof(T) / 4, PITCH = W + 4;    // words of a row of the tile
     extern __shared__ uint4 smem_q[];
-    uint32_t *tile = reinterpret_cast<uint32_t *>(smem_q);          // [128][W] + skew, when COLS
+    uint32_t *tile = reinterpret_cast<uint32_t *>(smem_q);          // [128][PITCH] + skew, when COLS
+    uint4 *row_codes = reinterpret_cast<uint4 *>(tile + 128 * PITCH + 32);   // [128][5], when both: four blocks' codes
     __shared__ __align__(16) uint8_t sc[2][kTileBytes];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     ptx::launch_dependents();
@@ -81,7 +127,7 @@ __global__ void __launch_bounds__(256) mx4_quantize_kernel(const QuantParams prm
     const int cl = (lane & 15) * 8;
     const int ncol = (int)min((int64_t)8, prm.cols - (c0 + cl));    // this lane's valid entries (<= 0: none)
     uint64_t h_own = 0;
-    if (ROWS && SR) h_own = row_word(prm.seed_w, r0 + 16 * warp + (lane & 15));
+    if (ROWS && !COLS && SR) h_own = row_word(prm.seed_w, r0 + 16 * warp + (lane & 15));
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
         Raw8<T> raw[4];
@@ -96,9 +142,9 @@ __global__ void __launch_bounds__(256) mx4_quantize_kernel(const QuantParams prm
             if (COLS) {
 #pragma unroll
                 for (int q = 0; q < (int)sizeof(T) / 2; ++q)
-                    *reinterpret_cast<uint4 *>(tile + rl * W + (rl >> 5) * 8 + (lane & 15) * (int)sizeof(T) * 2 + q * 4) = raw[i].q[q];
+                    *reinterpret_cast<uint4 *>(tile + rl * PITCH + (rl >> 5) * 8 + (lane & 15) * (int)sizeof(T) * 2 + q * 4) = raw[i].q[q];
             }
-            if (ROWS) {
+            if (ROWS && !COLS) {
                 float v[8];
                 unpack8(raw[i], v);
                 const float amax = quad_max(amax8(v));
@@ -115,6 +161,21 @@ __global__ void __launch_bounds__(256) mx4_quantize_kernel(const QuantParams prm
         }
     }
     __syncthreads();
+    if (ROWS && COLS) {
+        const int g = warp >> 1, rl = 32 * g + lane;
+        const uint64_t h = SR ? row_word(prm.seed_w, r0 + rl) : 0;
+#pragma unroll 1
+        for (int b = 2 * (warp & 1); b < 2 * (warp & 1) + 2; ++b) {
+            uint32_t w[W / 4], s;
+#pragma unroll
+            for (int i = 0; i < W / 16; ++i) {
+                const uint4 q = *reinterpret_cast<const uint4 *>(tile + rl * PITCH + g * 8 + b * (W / 4) + 4 * i);
+                w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
+            }
+            row_codes[rl * 5 + b] = quantize_block<T, SR>(w, h, (uint32_t)(c0 >> 1) + 16 * b, s);
+            sc[0][(rl & 31) * 16 + g * 4 + b] = (uint8_t)s;
+        }
+    }
     if (COLS) {
         constexpr int PER = 4 / (int)sizeof(T);                 // columns of a word: 1 or 2
         const int blk = lane & 3;
@@ -122,7 +183,7 @@ __global__ void __launch_bounds__(256) mx4_quantize_kernel(const QuantParams prm
         for (int cw = warp * 8 + (lane >> 2); cw < W; cw += 64) {
             uint32_t w[32];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) w[i] = tile[(blk * 32 + i) * W + blk * 8 + cw];
+            for (int i = 0; i < 32; ++i) w[i] = tile[(blk * 32 + i) * PITCH + blk * 8 + cw];
 #pragma unroll
             for (int part = 0; part < PER; ++part) {
                 const int cl2 = cw * PER + part;
@@ -158,6 +219,14 @@ __global__ void __launch_bounds__(256) mx4_quantize_kernel(const QuantParams prm
         }
         __syncthreads();
     }
+    if (ROWS && COLS) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = tid + 256 * i;
+            const int64_t r = r0 + (at >> 2), b = (c0 >> 5) + (at & 3);
+            if (r < prm.rows && b < blocks(prm.cols)) *reinterpret_cast<uint4 *>(prm.codes + r * pitch + b * 16) = row_codes[(at >> 2) * 5 + (at & 3)];
+        }
+    }
     // the tile's scale bytes, whole (entries past the matrix are zeros, whose scale byte is 0)
     if (ROWS && tid < 32)
         reinterpret_cast<uint4 *>(prm.scales + ((int64_t)rtile * prm.ct + ctile) * kTileBytes)[tid] =
@@ -165,27 +234,6 @@ __global__ void __launch_bounds__(256) mx4_quantize_kernel(const QuantParams prm
     if (COLS && tid >= 32 && tid < 64)
         reinterpret_cast<uint4 *>(prm.scales_t + ((int64_t)ctile * tiles_of(prm.rows, 128) + rtile) * kTileBytes)[tid - 32] =
             reinterpret_cast<const uint4 *>(sc[1])[tid - 32];
-}
-
-// Max |x| of the entries in four words (NaN and infinity come out as themselves or as a NaN).
-template <typename T>
-__device__ __forceinline__ float amax_words(const uint32_t (&w)[8 * sizeof(T)])
-{
-    constexpr int N = 8 * (int)sizeof(T);
-    if constexpr (sizeof(T) == 4) {
-        float m = fabsf(__uint_as_float(w[0]));
-#pragma unroll
-        for (int i = 1; i < N; ++i) m = max_nan(m, fabsf(__uint_as_float(w[i])));
-        return m;
-    } else {      // patterns without their sign order like the magnitudes, two at a time
-        uint32_t m = w[0] & 0x7FFF7FFFu;
-#pragma unroll
-        for (int i = 1; i < N; ++i) m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
-        const uint16_t top = (uint16_t)max(m & 0xFFFFu, m >> 16);
-        T e;
-        memcpy(&e, &top, 2);
-        return to_f(e);
-    }
 }
 
 // Along the rows only: a lane has a whole block, so that what belongs to a block (its largest entry, its scale, its row's
@@ -225,22 +273,7 @@ __global__ void __launch_bounds__(256) mx4_quantize_rows_kernel(const QuantParam
                 for (int i = 0; i < kBlock; ++i) e[i] = i < n ? from[i] : T(0.0f);
                 memcpy(w, e, sizeof(w));
             }
-            s = scale_byte(amax_words<T>(w));
-            const float inv = inv_scale(min(s, 253u));
-            const uint64_t h = SR ? row_word(prm.seed_w, row) : 0;
-            uint32_t code[4];
-#pragma unroll
-            for (int o = 0; o < 4; ++o) {
-                float v[8];
-                T e[8];
-                memcpy(e, w + o * (W / 4), sizeof(e));
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = to_f(e[i]);
-                clear_invalid(v, s);
-                grid8<SR>(v, inv, h, (uint32_t)(b * 16 + 4 * o));
-                code[o] = codes8(v);
-            }
-            reinterpret_cast<uint4 *>(prm.codes)[row * nb + b] = make_uint4(code[0], code[1], code[2], code[3]);
+            reinterpret_cast<uint4 *>(prm.codes)[row * nb + b] = quantize_block<T, SR>(w, SR ? row_word(prm.seed_w, row) : 0, (uint32_t)(b * 16), s);
         }
         prm.scales[scale_at(row, b, kt)] = (uint8_t)s;      // (past the matrix: 0)
     }
@@ -426,7 +459,7 @@ template <typename T, bool SR, bool ROWS, bool COLS>
 cudaError_t launch_quantize_as(cudaStream_t st, const QuantParams &prm)
 {
     const unsigned grid = (unsigned)(prm.ct * tiles_of(prm.rows, 128));
-    const size_t smem = COLS ? 128 * 128 * sizeof(T) + 128 : 0;
+    const size_t smem = COLS ? 128 * (128 * sizeof(T) + 16) + 128 + (ROWS ? 128 * 80 : 0) : 0;
     return ptx::launch_chained<mx4_quantize_kernel<T, SR, ROWS, COLS>>(prm, (int)grid, 256, smem, 1, st);
 }
 template <typename T, bool SR>
