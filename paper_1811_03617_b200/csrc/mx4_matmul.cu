@@ -128,31 +128,34 @@ __global__ void __launch_bounds__(NTHREADS, 1) mx4_matmul_kernel(const __grid_co
 
     const int n_tiles = prm.tiles_m * prm.tiles_n;
     const int first = blockIdx.x / CG, stride = gridDim.x / CG;
-    const int64_t k_last = prm.K - (int64_t)(prm.n_stages - 1) * KS;   // entries of the last stage, 1 .. 256
+    const int n_last = (int)((prm.K - (int64_t)(prm.n_stages - 1) * KS + 63) / 64);   // MMAs of a tile's last stage, 1 .. 4
 
     if (warp == 0) {
         // ------------------------------------------------------------------ producer
-        if (lane == 0) {
+        if (elect_one()) {
             fence_proxy_async_global();      // what plain stores of the previous launch wrote is read by TMA
-            uint32_t c = 0;
+            uint32_t c = 0, s = 0, phase = 1;
             for (int tile = first; tile < n_tiles && !failed; tile += stride) {
                 const int tn = tile / prm.tiles_m, tm = tile - tn * prm.tiles_m;
                 const int m0 = tm * 128 * CG + 128 * rank, n0 = tn * BN + BN / CG * rank;
+                const int m_tile = m0 >> 7, n_tile = (tn * BN) >> 7;
                 for (int st = 0; st < prm.n_stages; ++st, ++c) {
-                    const uint32_t s = c % S::STAGES;
-                    if (!mbar_poll(empty + s, ((c / S::STAGES) & 1) ^ 1, abort_flag)) { failed = true; break; }
-                    if (prm.test_drop && blockIdx.x == 0 && c == 0) continue;   // test hook: this stage never arrives
-                    unsigned char *dst = smem + (size_t)s * S::STAGE;
-                    if (rank == 0) mbar_arrive_expect_tx(full + s, CG * S::LOADED);
-                    const uint32_t bar = CG == 2 ? in_leader(full + s) : 0;
-                    auto load = [&](unsigned char *to, const CUtensorMap *map, int x, int y) {
-                        if (CG == 2) tma_load_2d_pair(to, map, x, y, bar); else tma_load_2d(to, map, x, y, full + s);
-                    };
-                    load(dst, &prm.a, st * 128, m0);
-                    load(dst + A_BYTES, &prm.b, st * 128, n0);
-                    // this CTA's rows of A; all of the tile's rows of B, which both CTAs of a pair need
-                    load(dst + A_BYTES + S::B_BYTES, &prm.sa, st * 128, m0 >> 7);
-                    load(dst + A_BYTES + S::B_BYTES + SFA_BYTES, &prm.sb, st * 128, (tn * BN) >> 7);
+                    if (!mbar_poll(empty + s, phase, abort_flag)) { failed = true; break; }
+                    const bool drop = prm.test_drop && blockIdx.x == 0 && c == 0;   // test hook: this stage never arrives
+                    if (!drop) {
+                        unsigned char *dst = smem + s * S::STAGE;
+                        if (rank == 0) mbar_arrive_expect_tx(full + s, CG * S::LOADED);
+                        const uint32_t bar = CG == 2 ? in_leader(full + s) : 0;
+                        auto load = [&](unsigned char *to, const CUtensorMap *map, int x, int y) {
+                            if (CG == 2) tma_load_2d_pair(to, map, x, y, bar); else tma_load_2d(to, map, x, y, full + s);
+                        };
+                        load(dst, &prm.a, st * 128, m0);
+                        load(dst + A_BYTES, &prm.b, st * 128, n0);
+                        // this CTA's rows of A; all of the tile's rows of B, which both CTAs of a pair need
+                        load(dst + A_BYTES + S::B_BYTES, &prm.sa, st * 128, m_tile);
+                        load(dst + A_BYTES + S::B_BYTES + SFA_BYTES, &prm.sb, st * 128, n_tile);
+                    }
+                    if (++s == S::STAGES) { s = 0; phase ^= 1; }
                 }
             }
             if (failed && rank == 0) {   // give the copies already in flight a bounded chance to land before the CTA exits
@@ -160,54 +163,57 @@ __global__ void __launch_bounds__(NTHREADS, 1) mx4_matmul_kernel(const __grid_co
                     for (int it = 0; it < 100000 && !mbar_try_wait(full + i % S::STAGES, (i / S::STAGES) & 1); ++it) {}
             }
         }
-        failed = __shfl_sync(0xffffffffu, failed, 0);
+        failed = __any_sync(0xffffffffu, failed);
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
-        uint32_t c = 0, t = 0;
-        for (int tile = first; rank == 0 && tile < n_tiles && !failed; tile += stride, ++t) {
-            const uint32_t buf = t & 1;
-            const uint32_t d = tmem + buf * S::ACC1;
-            // a narrow tile's rows of B may begin inside their scale tile: 32 rows a column
-            const uint32_t sf_shift = BN < 128 ? ((uint32_t)(tile / prm.tiles_m) * BN & 127u) >> 5 : 0;
-            if (t > 0) {
-                // the tile before this one has been read where the two accumulators overlap (and the one before
-                // that, in this accumulator, entirely: the epilogue takes the tiles in order)
-                bool ok = mbar_poll(d_early + (buf ^ 1), ((t - 1) >> 1) & 1, abort_flag);
-                if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
-                tc_fence_after();
-            }
-            for (int st = 0; st < prm.n_stages; ++st, ++c) {
-                const uint32_t s = c % S::STAGES;
-                bool ok = mbar_poll(full + s, (c / S::STAGES) & 1, abort_flag);
-                if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
-                tc_fence_after();
-                const int64_t left = st == prm.n_stages - 1 ? k_last : KS;
-                const int n_mma = (int)((left + 63) / 64), n_kt = (n_mma + 1) >> 1;
-                const uint32_t base = smem_u32(smem + (size_t)s * S::STAGE);
-                const uint32_t sfa = tmem + S::SF0 + (c & 1) * S::SF_SET, sfb = sfa + 8;
-                if (elect_one()) {
-                    const uint32_t sc = base + A_BYTES + S::B_BYTES;
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        if (k < n_kt) {
-                            copy_scales<CG>(sfa + 4 * k, scales_desc(sc + k * kTileBytes));
-#pragma unroll
-                            for (int r = 0; r < S::NRT; ++r)
-                                copy_scales<CG>(sfb + 4 * (k * S::NRT + r), scales_desc(sc + SFA_BYTES * (1 + r) + k * kTileBytes));
-                        }
-                    }
-                    const uint64_t da = make_b_desc(base), db = make_b_desc(base + A_BYTES);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (k < n_mma)
-                            mma_mxf4<CG>(d, da + k * 2, db + k * 2, idesc_mxf4(128 * CG, BN, k & 1), sfa + 4 * (k >> 1),
-                                         sfb + 4 * S::NRT * (k >> 1) + sf_shift, (st | k) != 0);
-                    if (CG == 2) tc_commit_pair(empty + s); else tc_commit(empty + s);
-                    if (st == prm.n_stages - 1) { if (CG == 2) tc_commit_pair(d_full + buf); else tc_commit(d_full + buf); }
+        // One lane goes through the whole loop: electing it and bringing the warp together again for every stage took 180 of
+        // a stage's 470 clocks, and that bounded narrow products.
+        if (rank == 0 && elect_one()) {
+            uint32_t s = 0, phase = 0, set = 0, t = 0;
+            const uint32_t base0 = smem_u32(smem);
+            const uint64_t a0 = make_b_desc(base0), sc0 = scales_desc(base0 + A_BYTES + S::B_BYTES);
+            for (int tile = first; tile < n_tiles && !failed; tile += stride, ++t) {
+                const uint32_t buf = t & 1;
+                const uint32_t d = tmem + buf * S::ACC1;
+                // a narrow tile's rows of B may begin inside their scale tile: 32 rows a column
+                const uint32_t sf_shift = BN < 128 ? ((uint32_t)(tile / prm.tiles_m) * BN & 127u) >> 5 : 0;
+                if (t > 0) {
+                    // the tile before this one has been read where the two accumulators overlap (and the one before
+                    // that, in this accumulator, entirely: the epilogue takes the tiles in order)
+                    if (!mbar_poll(d_early + (buf ^ 1), ((t - 1) >> 1) & 1, abort_flag)) { failed = true; break; }
+                    tc_fence_after();
                 }
-                __syncwarp();
+                for (int st = 0; st < prm.n_stages; ++st) {
+                    if (!mbar_poll(full + s, phase, abort_flag)) { failed = true; break; }
+                    tc_fence_after();
+                    const bool last = st == prm.n_stages - 1;
+                    const uint32_t sfa = tmem + S::SF0 + set, sfb = sfa + 8;
+                    const uint64_t da = a0 + s * (S::STAGE >> 4), db = da + (A_BYTES >> 4), sc = sc0 + s * (S::STAGE >> 4);
+                    auto issue = [&](int n_mma) {      // (a constant, except in a short last stage)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            if (2 * k < n_mma) {
+                                copy_scales<CG>(sfa + 4 * k, sc + k * (kTileBytes >> 4));
+#pragma unroll
+                                for (int r = 0; r < S::NRT; ++r)
+                                    copy_scales<CG>(sfb + 4 * (k * S::NRT + r), sc + ((SFA_BYTES * (1 + r) + k * kTileBytes) >> 4));
+                            }
+                        }
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (k < n_mma)
+                                mma_mxf4<CG>(d, da + k * 2, db + k * 2, idesc_mxf4(128 * CG, BN, k & 1), sfa + 4 * (k >> 1),
+                                             sfb + 4 * S::NRT * (k >> 1) + sf_shift, (st | k) != 0);
+                    };
+                    if (last && n_last < 4) issue(n_last); else issue(4);
+                    if (CG == 2) tc_commit_pair(empty + s); else tc_commit(empty + s);
+                    if (last) { if (CG == 2) tc_commit_pair(d_full + buf); else tc_commit(d_full + buf); }
+                    set ^= S::SF_SET;
+                    if (++s == S::STAGES) { s = 0; phase ^= 1; }
+                }
             }
         }
+        failed = __any_sync(0xffffffffu, failed);
     } else {
         // ------------------------------------------------------------------ epilogue
         const int q = warp & 3;
