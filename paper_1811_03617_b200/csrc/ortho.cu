@@ -397,7 +397,7 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
             asm volatile("prefetch.tensormap [%0];" ::"l"(maps + l.b_map));
             grid_dependency_wait();          // what the previous launch wrote is visible from here on
             fence_proxy_async_global();      // and read by TMA, plain stores included
-            uint32_t c = 0;
+            uint32_t c = 0, s = 0, phase = 1;
             for (int t = t_begin; t < t_end && !failed; ++t) {
                 const Seen next = seen(min(t + 1, t_end - 1));
                 const CUtensorMap *map_a = prm.dev.maps + (size_t)l.matrix * kMaps + l.a_map, *map_b = prm.dev.maps + (size_t)l.matrix * kMaps + l.b_map;
@@ -407,16 +407,17 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                 // steps of the contraction left of the diagonal's block of a symmetric operand's rows
                 const int a_left = l.a_sym ? l.m0 / S::BLOCK * S::BLOCK : 0, b_left = l.b_sym ? l.n0 / S::BLOCK * S::BLOCK : 0;
                 for (int st = l.k0; st < l.k1; ++st, ++c) {
-                    const uint32_t s = c % S::STAGES;
-                    if (!mbar_poll(empty + s, ((c / S::STAGES) & 1) ^ 1, abort_flag)) { failed = true; break; }
+                    if (!mbar_poll(empty + s, phase, abort_flag)) { failed = true; break; }
+                    unsigned char *dst = smem + s * S::STAGE;
+                    uint64_t *here = full + s;
+                    if (++s == S::STAGES) { s = 0; phase ^= 1; }
                     if (prm.test_drop && blockIdx.x == 0 && c == 0) continue;   // test hook: this stage never arrives
-                    unsigned char *dst = smem + (size_t)s * S::STAGE;
-                    if (rank == 0) mbar_arrive_expect_tx(full + s, CG * S::STAGE);
+                    if (rank == 0) mbar_arrive_expect_tx(here, CG * S::STAGE);
                     const int k = st * KS;
-                    const uint32_t bar = CG == 2 ? in_leader(full + s) : 0;
+                    const uint32_t bar = CG == 2 ? in_leader(here) : 0;
                     auto load = [&](unsigned char *to, const CUtensorMap *map, bool mn, int at) {
                         if (CG == 2) tma_load_2d_pair(to, map, mn ? at : k, mn ? k : at, bar);
-                        else tma_load_2d(to, map, mn ? at : k, mn ? k : at, full + s);
+                        else tma_load_2d(to, map, mn ? at : k, mn ? k : at, here);
                     };
 #pragma unroll
                     for (int i = 0; i < 2; ++i) load(dst + i * BOX, map_a, l.a_mn || k < a_left, m0 + 64 * i);
@@ -432,38 +433,38 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
         }
         failed = __shfl_sync(0xffffffffu, failed, 0);
     } else if (warp == 1) {
-        uint32_t c = 0, u = 0;
-        for (int t = t_begin; rank == 0 && t < t_end && !failed; ++t, ++u) {
-            const Seen w = seen(t);
-            const uint32_t buf = u & 1, d = tmem + buf * S::BN;
-            const int n = min(S::BN, (w.N - w.n0 + 15) / 16 * 16);
-            const int a_left = w.a_sym ? w.m0 / S::BLOCK * S::BLOCK : 0, b_left = w.b_sym ? w.n0 / S::BLOCK * S::BLOCK : 0;
-            bool ok = mbar_poll(d_empty + buf, ((u >> 1) & 1) ^ 1, abort_flag);
-            if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
-            tc_fence_after();
-            for (int st = w.k0; st < w.k1; ++st, ++c) {
-                const uint32_t s = c % S::STAGES;
-                ok = mbar_poll(full + s, (c / S::STAGES) & 1, abort_flag);
-                if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
+        // one lane goes through the whole loop: electing it and bringing the warp together again costs 180 clocks a stage
+        if (rank == 0 && elect_one()) {
+            uint32_t s = 0, phase = 0, u = 0;
+            const uint32_t base0 = smem_u32(smem);
+            for (int t = t_begin; t < t_end && !failed; ++t, ++u) {
+                const Seen w = seen(t);
+                const uint32_t buf = u & 1, d = tmem + buf * S::BN;
+                const int n = min(S::BN, (w.N - w.n0 + 15) / 16 * 16);
+                const int a_left = w.a_sym ? w.m0 / S::BLOCK * S::BLOCK : 0, b_left = w.b_sym ? w.n0 / S::BLOCK * S::BLOCK : 0;
+                if (!mbar_poll(d_empty + buf, ((u >> 1) & 1) ^ 1, abort_flag)) { failed = true; break; }
                 tc_fence_after();
-                const uint32_t base = smem_u32(smem + (size_t)s * S::STAGE);
-                const bool a_mn = w.a_mn || st * KS < a_left, b_mn = w.b_mn || st * KS < b_left;
-                const uint32_t idesc = make_idesc_f16(128 * CG, n, a_mn, b_mn);
-                const uint64_t da = a_mn ? make_mn_desc(base, BOX) : make_b_desc(base);
-                const uint64_t db = b_mn ? make_mn_desc(base + S::A_BYTES, BOX) : make_b_desc(base + S::A_BYTES);
-                // 16 steps of the contraction: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major box
-                const uint32_t ia = a_mn ? 16 * 128 / 16 : 2, ib = b_mn ? 16 * 128 / 16 : 2;
-                const int n_mma = min(4, (w.K - st * KS + 15) / 16);
-                if (elect_one()) {
+                for (int st = w.k0; st < w.k1; ++st) {
+                    if (!mbar_poll(full + s, phase, abort_flag)) { failed = true; break; }
+                    tc_fence_after();
+                    const uint32_t base = base0 + s * S::STAGE;
+                    const bool a_mn = w.a_mn || st * KS < a_left, b_mn = w.b_mn || st * KS < b_left;
+                    const uint32_t idesc = make_idesc_f16(128 * CG, n, a_mn, b_mn);
+                    const uint64_t da = a_mn ? make_mn_desc(base, BOX) : make_b_desc(base);
+                    const uint64_t db = b_mn ? make_mn_desc(base + S::A_BYTES, BOX) : make_b_desc(base + S::A_BYTES);
+                    // 16 steps of the contraction: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major box
+                    const uint32_t ia = a_mn ? 16 * 128 / 16 : 2, ib = b_mn ? 16 * 128 / 16 : 2;
+                    const int n_mma = min(4, (w.K - st * KS + 15) / 16);
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
                         if (k < n_mma) tc_mma_f16<CG>(d, da + k * ia, db + k * ib, idesc, st > w.k0 || k > 0);
                     if (CG == 2) tc_commit_pair(empty + s); else tc_commit(empty + s);
                     if (st == w.k1 - 1) { if (CG == 2) tc_commit_pair(d_full + buf); else tc_commit(d_full + buf); }
+                    if (++s == S::STAGES) { s = 0; phase ^= 1; }
                 }
-                __syncwarp();
             }
         }
+        failed = __any_sync(0xffffffffu, failed);
     } else {
         const int q = warp & 3, half = (warp - 2) >> 2;
         const uint32_t lane_base = (uint32_t)(32 * q) << 16;
