@@ -9,8 +9,10 @@
 //   CG = 2, BN = 256   a pair of CTAs on two SMs: each holds its own 128 rows of A and half of B's rows; the even one issues
 //                      MMAs that read both.  35 KB a stage and SM for 512 clocks of MMAs, where a CTA alone on 128 x 256 would
 //                      load 51 KB -- more than L2 delivers to all SMs at that rate.
-//   CG = 1             one CTA: few rows (of a token, a small batch: they become B, the tile as narrow as they are), or
-//                      products too small to give every SM a large tile.
+//   CG = 1             one CTA, 128 x 64 or narrower: few rows (of a token, a small batch: they become B, the tile as narrow
+//                      as they are), or products too small to give every SM a large tile.  Where the tiles are fewer than
+//                      the SMs, a cluster of up to eight CTAs shares a tile's contraction; each leaves its sums in its shared
+//                      memory, where the stages were, and they add them up across the cluster, always in the same order.
 //   warp 0      producer: per stage TMA loads of both operands' codes (128-byte swizzle, zero fill outside) and scale bytes
 //               (two tiles of 512 bytes, contiguous, for each 128 rows; read as rows of 8-byte words)
 //   warp 1      MMA: copies the stage's scale tiles into tensor memory (each 128 x 4 tile becomes 4 columns), then up
@@ -30,7 +32,7 @@ using mx4::kTileBytes;
 
 constexpr int KS = 256;               // entries of the contraction a stage
 constexpr int NTHREADS = 192;
-constexpr int kPairTiles = 37;        // 256 x 256 tiles from which pairs of CTAs take them
+constexpr int kJoinPitch = 129;        // (a row's words of 16 bytes, eight lanes' of them, lie in different banks)
 constexpr uint32_t A_BYTES = 128 * 128, SFA_BYTES = 2 * kTileBytes;
 
 template <int CG, int BN> struct Shape {
@@ -47,6 +49,7 @@ template <int CG, int BN> struct Shape {
     static constexpr uint32_t STAGING = 8192;                          // of an epilogue warp: two pieces of 4 KB
     static constexpr size_t SMEM = (size_t)STAGE * STAGES + 4 * STAGING + 256 + 1024;
     static_assert(SF0 + 2 * SF_SET <= TMEM, "tensor memory");
+    static_assert(CG == 2 || (size_t)BN / 4 * kJoinPitch * 16 <= (size_t)STAGE * STAGES, "room to join parts");
 };
 
 struct MmParams {
@@ -56,6 +59,7 @@ struct MmParams {
     int tma_out;
     int64_t M, N, K;                  // rows of A, rows of B, contraction
     int tiles_m, tiles_n, n_stages;   // n_stages: of one tile's contraction
+    int parts;                        // CTAs (a cluster) that share a tile's contraction; with more than one, a tile a cluster
     void *out;
     int64_t out_m, out_n;             // strides of the output in entries, one of them 1
     int32_t *error_word;
@@ -94,6 +98,38 @@ __host__ __device__ constexpr uint32_t idesc_mxf4(int m, int n, int half)
            ((uint32_t)(m >> 4) << 24) | ((uint32_t)(2 * half) << 29);
 }
 
+// The CTAs of a cluster of P add up the tile's entries that there are, four columns of a row a thread at a time, the parts in
+// order.  Lanes lie along what is contiguous in the output: the columns, or with B's rows on this side the rows.
+template <typename T, int BN, int P>
+__device__ __forceinline__ void join_parts(const MmParams &prm, const float4 *join, int part, int tm, int tn)
+{
+    const bool by_row = prm.out_n == 1;
+    const int rows = (int)min((int64_t)128, prm.M - (int64_t)tm * 128), cols = (int)min((int64_t)BN, prm.N - (int64_t)tn * BN);
+    const int quads = (cols + 3) / 4, inner = by_row ? quads : rows;
+    uint32_t from[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) from[p] = cluster_address(smem_u32(join), p);
+#pragma unroll 2
+    for (int it = part * NTHREADS + threadIdx.x; it < rows * quads; it += P * NTHREADS) {
+        const int o = it / inner, i = it - o * inner, c4 = by_row ? i : o, r = by_row ? o : i;
+        float4 x[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p) x[p] = load_cluster(from[p] + (c4 * kJoinPitch + r) * 16);
+#pragma unroll
+        for (int p = 1; p < P; ++p) { x[0].x += x[p].x; x[0].y += x[p].y; x[0].z += x[p].z; x[0].w += x[p].w; }
+        const T y[4] = {from_f<T>(x[0].x), from_f<T>(x[0].y), from_f<T>(x[0].z), from_f<T>(x[0].w)};
+        T *out = static_cast<T *>(prm.out) + ((int64_t)tm * 128 + r) * prm.out_m + ((int64_t)tn * BN + c4 * 4) * prm.out_n;
+        if (by_row && prm.tma_out && c4 * 4 + 4 <= cols) {      // (rows at 16-byte boundaries)
+            if (sizeof(T) == 2) { uint2 w; memcpy(&w, y, sizeof(w)); *reinterpret_cast<uint2 *>(out) = w; }
+            else { uint4 w; memcpy(&w, y, sizeof(T) == 4 ? 16 : 8); *reinterpret_cast<uint4 *>(out) = w; }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c4 * 4 + e < cols) out[e * prm.out_n] = y[e];
+        }
+    }
+}
+
 template <typename T, int CG, int BN>
 __global__ void __launch_bounds__(NTHREADS, 1) mx4_matmul_kernel(const __grid_constant__ MmParams prm)
 {
@@ -101,6 +137,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) mx4_matmul_kernel(const __grid_co
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     unsigned char *staging = smem + (size_t)S::STAGE * S::STAGES;
+    float4 *join = reinterpret_cast<float4 *>(smem);       // [BN / 4][kJoinPitch]: four columns of a row
     uint64_t *bars = reinterpret_cast<uint64_t *>(staging + 4 * S::STAGING);
     uint64_t *full = bars, *empty = full + S::STAGES;      // [STAGES]
     uint64_t *d_full = empty + S::STAGES;                  // [2] accumulator complete
@@ -110,6 +147,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) mx4_matmul_kernel(const __grid_co
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CG == 2 ? (int)cluster_rank() : 0;
+    const int parts = CG == 1 ? prm.parts : 1, part = parts > 1 ? (int)cluster_rank() : 0;
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::STAGES; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(d_full + i, 1); mbar_init(d_early + i, 4 * CG); }
@@ -127,7 +165,8 @@ __global__ void __launch_bounds__(NTHREADS, 1) mx4_matmul_kernel(const __grid_co
     bool failed = false;
 
     const int n_tiles = prm.tiles_m * prm.tiles_n;
-    const int first = blockIdx.x / CG, stride = gridDim.x / CG;
+    const int first = blockIdx.x / (CG * parts), stride = gridDim.x / (CG * parts);
+    const int st0 = prm.n_stages * part / parts, st1 = prm.n_stages * (part + 1) / parts;    // this CTA's stages
     const int n_last = (int)((prm.K - (int64_t)(prm.n_stages - 1) * KS + 63) / 64);   // MMAs of a tile's last stage, 1 .. 4
 
     if (warp == 0) {
@@ -139,7 +178,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) mx4_matmul_kernel(const __grid_co
                 const int tn = tile / prm.tiles_m, tm = tile - tn * prm.tiles_m;
                 const int m0 = tm * 128 * CG + 128 * rank, n0 = tn * BN + BN / CG * rank;
                 const int m_tile = m0 >> 7, n_tile = (tn * BN) >> 7;
-                for (int st = 0; st < prm.n_stages; ++st, ++c) {
+                for (int st = st0; st < st1; ++st, ++c) {
                     if (!mbar_poll(empty + s, phase, abort_flag)) { failed = true; break; }
                     const bool drop = prm.test_drop && blockIdx.x == 0 && c == 0;   // test hook: this stage never arrives
                     if (!drop) {
@@ -183,10 +222,10 @@ __global__ void __launch_bounds__(NTHREADS, 1) mx4_matmul_kernel(const __grid_co
                     if (!mbar_poll(d_early + (buf ^ 1), ((t - 1) >> 1) & 1, abort_flag)) { failed = true; break; }
                     tc_fence_after();
                 }
-                for (int st = 0; st < prm.n_stages; ++st) {
+                for (int st = st0; st < st1; ++st) {
                     if (!mbar_poll(full + s, phase, abort_flag)) { failed = true; break; }
                     tc_fence_after();
-                    const bool last = st == prm.n_stages - 1;
+                    const bool last = st == st1 - 1;
                     const uint32_t sfa = tmem + S::SF0 + set, sfb = sfa + 8;
                     const uint64_t da = a0 + s * (S::STAGE >> 4), db = da + (A_BYTES >> 4), sc = sc0 + s * (S::STAGE >> 4);
                     auto issue = [&](int n_mma) {      // (a constant, except in a short last stage)
@@ -203,9 +242,9 @@ __global__ void __launch_bounds__(NTHREADS, 1) mx4_matmul_kernel(const __grid_co
                         for (int k = 0; k < 4; ++k)
                             if (k < n_mma)
                                 mma_mxf4<CG>(d, da + k * 2, db + k * 2, idesc_mxf4(128 * CG, BN, k & 1), sfa + 4 * (k >> 1),
-                                             sfb + 4 * S::NRT * (k >> 1) + sf_shift, (st | k) != 0);
+                                             sfb + 4 * S::NRT * (k >> 1) + sf_shift, st > st0 || k > 0);
                     };
-                    if (last && n_last < 4) issue(n_last); else issue(4);
+                    if (st == prm.n_stages - 1 && n_last < 4) issue(n_last); else issue(4);
                     if (CG == 2) tc_commit_pair(empty + s); else tc_commit(empty + s);
                     if (last) { if (CG == 2) tc_commit_pair(d_full + buf); else tc_commit(d_full + buf); }
                     set ^= S::SF_SET;
@@ -229,6 +268,19 @@ __global__ void __launch_bounds__(NTHREADS, 1) mx4_matmul_kernel(const __grid_co
             if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
             tc_fence_after();
             const uint32_t acc = tmem + lane_base + buf * S::ACC1;
+            if (parts > 1) {           // the stages have been read: what the part has goes into their place
+                if constexpr (CG == 1) {
+#pragma unroll
+                    for (int c = 0; c < BN; c += 16) {
+                        float v[16];
+                        tmem_ld16_wait(acc + c, v);
+#pragma unroll
+                        for (int i = 0; i < 16; i += 4)
+                            join[(c + i) / 4 * kJoinPitch + 32 * q + lane] = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                    }
+                }
+                continue;
+            }
             const int64_t m0 = (int64_t)tm * 128 * CG + 128 * rank + 32 * q;
             const int rows = (int)max((int64_t)0, min((int64_t)32, prm.M - m0));
             // pieces of 64 columns; the first accumulator's last columns are the second one's first: that piece comes first
@@ -297,12 +349,26 @@ __global__ void __launch_bounds__(NTHREADS, 1) mx4_matmul_kernel(const __grid_co
         if (lane == 0) bulk_wait_group_all();
     }
 
+    if constexpr (CG == 1) {
+        if (parts > 1) {
+            __syncwarp();
+            cluster_sync();
+            if (!failed) {
+                const int tn = first / prm.tiles_m, tm = first - tn * prm.tiles_m;
+                if (parts == 2) join_parts<T, BN, 2>(prm, join, part, tm, tn);
+                else if (parts == 4) join_parts<T, BN, 4>(prm, join, part, tm, tn);
+                else join_parts<T, BN, 8>(prm, join, part, tm, tn);
+            }
+        }
+    }
     if (failed) {
         *abort_flag = 1;
         if (lane == 0) atomicExch(prm.error_word, 100 + warp);
     }
     tc_fence_before();
-    if (CG == 2) cluster_sync(); else __syncthreads();     // a pair: the other CTA's barriers and memory are in use until here
+    __syncwarp();
+    // (the other CTAs of a cluster use this one's barriers and memory until here)
+    if (CG == 2 || parts > 1) cluster_sync(); else __syncthreads();
     tc_fence_after();
     if (warp == 1) tmem_dealloc<CG>(tmem, S::TMEM);
 }
@@ -311,7 +377,9 @@ template <typename T, int CG, int BN>
 cudaError_t launch_as(cudaStream_t st, int num_sms, const MmParams &prm)
 {
     using S = Shape<CG, BN>;
-    return launch_chained<mx4_matmul_kernel<T, CG, BN>>(prm, CG * min(num_sms / CG, prm.tiles_m * prm.tiles_n), NTHREADS, S::SMEM, CG, st);
+    const int cluster = CG * prm.parts;
+    return launch_chained<mx4_matmul_kernel<T, CG, BN>>(prm, cluster * min(num_sms / cluster, prm.tiles_m * prm.tiles_n), NTHREADS, S::SMEM,
+                                                        cluster, st);
 }
 template <int CG, int BN>
 cudaError_t launch_typed(cudaStream_t st, int num_sms, int dtype, const MmParams &prm)
@@ -352,15 +420,27 @@ cudaError_t launch_mx4_matmul(cudaStream_t st, int num_sms, EncodeTiledFn enc, c
                               int32_t *error_word, int wait_kcycles, int test_drop)
 {
     MmParams prm;
-    // Few rows of A: B takes the 128-row side of the tile, and the tile is as wide as the few rows need.  Otherwise pairs of
-    // CTAs on 256 x 256 tiles, unless those are too few to occupy the SMs.
-    const bool swap = M <= 64;
-    const bool pair = !swap && mx4::tiles_of(M, 256) * mx4::tiles_of(N, 256) >= kPairTiles;
+    // Few rows of A: B takes the 128-row side of the tile, and the tile is as wide as the few rows need.  Up to 32 rows that
+    // is never slower than 128 x 64 tiles by more than 0.3 us and up to twice as fast (16 x 8192 x 8192 9.8 us against 17.2:
+    // the copies of mostly empty tiles of A are slow); 64 rows cost the epilogue 1.5 us of short stores, which pays where
+    // 128 x 64 tiles would need a second wave (64 x 16384 x 8192 12.0 us against 15.0, 64 x 8192 x 8192 11.5 against 9.9).
+    // Otherwise pairs of CTAs on 256 x 256 tiles where smaller ones would need a second wave (1280 x 1024 x 4096 9.1 us
+    // against 13.1 with them), and smaller ones where they do not (1024 x 1024 x 4096 6.5 us against 9.5 in pairs).
+    const bool waves = mx4::tiles_of(M, 128) * mx4::tiles_of(N, 64) > num_sms;
+    const bool swap = M <= 32 || (M <= 64 && waves), pair = !swap && waves;
     const int BN = pair ? 256 : !swap ? 64 : M <= 16 ? 16 : M <= 32 ? 32 : 64;
     prm.M = swap ? N : M; prm.N = swap ? M : N; prm.K = K;
     prm.tiles_m = (int)mx4::tiles_of(prm.M, pair ? 256 : 128);
     prm.tiles_n = (int)mx4::tiles_of(prm.N, BN);
     prm.n_stages = (int)mx4::tiles_of(K, KS);
+    // Parts of a contraction: as many as there are SMs for (eight CTAs of a cluster find room less easily than four), and at
+    // least 2 stages each of a narrow tile (1 x 2048 x 2048 4.6 -> 3.7 us with 4, 16 x 4096 x 16384 17.1 -> 7.6), 8 of a tile
+    // of 64 columns, whose sums cost 2 us to add up (64 x 2048 x 8192 9.9 -> 6.8 us with 4; 64 x 4096 x 2048 4.6 -> 5.9 with 2).
+    const int min_stages = BN <= 32 ? 2 : 8;
+    prm.parts = 1;
+    while (!pair && prm.parts < 8 && (int64_t)prm.tiles_m * prm.tiles_n * 2 * prm.parts <= (prm.parts < 4 ? num_sms : num_sms * 2 / 3) &&
+           prm.n_stages >= 2 * prm.parts * min_stages)
+        prm.parts *= 2;
     prm.out = out;
     prm.out_m = swap ? 1 : ld; prm.out_n = swap ? ld : 1;
     prm.error_word = error_word;

@@ -98,6 +98,20 @@ __device__ __forceinline__ void tma_load_2d(void *dst, const CUtensorMap *tmap, 
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(smem_u32(dst)), "l"(tmap), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
 }
+// This CTA's shared address `addr` as it is in CTA `cta` of the cluster, and four floats from such an address.
+__device__ __forceinline__ uint32_t cluster_address(uint32_t addr, uint32_t cta)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(cta));
+    return r;
+}
+__device__ __forceinline__ float4 load_cluster(uint32_t cluster_addr)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr) : "memory");
+    return v;
+}
 // Programmatic dependent launch: a kernel launched with the stream-serialization attribute may start while
 // its predecessor in the stream still runs, once every CTA of the predecessor has called launch_dependents
 // (or exited); grid_dependency_wait returns when the predecessor has completed and its writes are visible.

@@ -61,6 +61,17 @@ def test_codes_and_scales_bit_exact(ctx, rows, cols, dtype, stochastic):
     assert np.array_equal(got, v.astype(np.float32).astype(np.float64), equal_nan=True)
 
 
+@pytest.mark.parametrize("stochastic", [False, True])
+@pytest.mark.parametrize("rows,cols", [(3, 33000), (5, 65600), (40000, 8)])
+def test_long_rows_and_columns_bit_exact(ctx, rows, cols, stochastic):
+    """Rows of more than 1024 blocks, which are shared among CTAs, and their padding."""
+    x = torch.randn(rows, cols, generator=torch.Generator().manual_seed(cols)).to(torch.bfloat16)
+    q = ctx.mx4_quantize(x.cuda(), stochastic=stochastic, seed=77, node=1)
+    _check_quantized(q, x, stochastic, 77, 1)
+    qt = ctx.mx4_quantize_transposed(x.cuda(), stochastic=stochastic, seed=77, node=1)
+    _check_quantized(qt, x.t().contiguous(), stochastic, 77, 1)
+
+
 @pytest.mark.parametrize("dtype", list(DT))
 @pytest.mark.parametrize("offset,pad", [(0, 1), (1, 0), (3, 5), (8, 8)])
 def test_strides_and_alignment(ctx, dtype, offset, pad):
@@ -154,6 +165,35 @@ def test_large_product(ctx, m, n, k, dtype, pad):
     again = torch.empty(m, n, dtype=DT[dtype], device="cuda")
     ctx.mx4_matmul(qa, qb, again)
     assert torch.equal(again, buf[:, :n])
+
+
+# Tiles of few rows whose contraction a cluster of CTAs shares (2, 4 and 8 parts, with the few rows on either side of the
+# tile), last stages that are short, rows of the output that do not start at 16-byte boundaries, tiles that stick out.
+@pytest.mark.parametrize("m,n,k,dtype,pad", [
+    (1, 500, 4128, "bf16", 0), (3, 4000, 1100, "f32", 1), (16, 1000, 1283, "f32", 3), (31, 129, 2000, "f16", 1),
+    (32, 2049, 5000, "bf16", 8), (33, 70, 8200, "f32", 0), (64, 1000, 4133, "bf16", 8), (100, 300, 4300, "bf16", 5),
+    (65, 64, 16500, "f32", 4), (128, 61, 17000, "f16", 8), (150, 260, 4224, "bf16", 4)])
+def test_product_of_few_rows_with_a_long_contraction(ctx, m, n, k, dtype, pad):
+    g = torch.Generator(device="cuda").manual_seed(m + n)
+    a = torch.randn(m, k, generator=g, device="cuda") * 2.0 ** torch.randint(-9, 10, (m, 1), generator=g, device="cuda")
+    b = torch.randn(n, k, generator=g, device="cuda")
+    b[:, k // 2:] *= 2.0 ** torch.randint(-3, 4, (n, 1), generator=g, device="cuda")
+    qa, qb = ctx.mx4_quantize(a), ctx.mx4_quantize(b)
+    va, vb = ctx.mx4_dequantize(qa).double(), ctx.mx4_dequantize(qb).double()
+    buf = torch.full((m, n + pad), 3.0, dtype=DT[dtype], device="cuda")
+    ctx.mx4_matmul(qa, qb, buf[:, :n])
+    ctx.device_status()
+    # the bound of the other products: adding up to eight parts loses less than the steps that each part does not take
+    want, mag = va @ vb.T, va.abs() @ vb.abs().T
+    half_ulp = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}[DT[dtype]]
+    bound = mag * (-(-k // 64) + 2) * 2.0 ** -22 + want.abs() * half_ulp + (6e-8 if dtype == "f16" else 0)
+    near = want.abs() + bound < float(torch.finfo(DT[dtype]).max)
+    assert bool(((buf[:, :n].double() - want).abs() <= bound)[near].all())
+    assert bool((buf[:, n:] == 3.0).all())
+    for _ in range(3):
+        again = torch.empty(m, n, dtype=DT[dtype], device="cuda")
+        ctx.mx4_matmul(qa, qb, again)
+        assert torch.equal(again, buf[:, :n])
 
 
 @pytest.mark.parametrize("m", [3, 150])
@@ -335,6 +375,26 @@ def test_a_wait_that_runs_out_is_reported_and_the_context_recovers(ctx):
     a, b = torch.randn(200, 600, device="cuda"), torch.randn(300, 600, device="cuda")
     qa, qb = ctx.mx4_quantize(a), ctx.mx4_quantize(b)
     out = torch.empty(200, 300, device="cuda")
+    good = ctx.mx4_matmul(qa, qb, out).clone()
+    ctx.set_limits(wait_cycles=2_000_000)
+    ctx.test_drop_load(True)
+    try:
+        ctx.mx4_matmul(qa, qb, out)
+        with pytest.raises(gvq.GvqError) as e:
+            ctx.device_status()
+        assert e.value.status == 9
+    finally:
+        ctx.test_drop_load(False)
+        ctx.set_limits()
+    assert torch.equal(ctx.mx4_matmul(qa, qb, out), good)
+    ctx.device_status()
+
+
+@pytest.mark.parametrize("m,n,k", [(16, 500, 4128), (100, 300, 8200)])
+def test_a_part_whose_wait_runs_out_is_reported_and_the_context_recovers(ctx, m, n, k):
+    from paper_1811_03617_b200 import gvq
+    qa, qb = ctx.mx4_quantize(torch.randn(m, k, device="cuda")), ctx.mx4_quantize(torch.randn(n, k, device="cuda"))
+    out = torch.empty(m, n, device="cuda")
     good = ctx.mx4_matmul(qa, qb, out).clone()
     ctx.set_limits(wait_cycles=2_000_000)
     ctx.test_drop_load(True)

@@ -194,6 +194,22 @@ def test_many_large_matrices(dtype):
     assert torch.equal(mo[~rest], g[~rest])
 
 
+@pytest.mark.parametrize("shape", [(8, 900001), (900001, 5)])
+def test_a_matrix_of_very_many_tiles(shape):
+    """More tiles than a CTA keeps the descriptions of."""
+    m, n = shape
+    w, plan = make([shape])
+    u = kinds(m, n, 3, "lowrank")
+    g = torch.zeros(w.M)
+    g[:m * n] = u.reshape(-1)
+    out = torch.empty(w.M, device="cuda")
+    plan.orthogonalize(g.cuda(), out)
+    plan.ctx.device_status()
+    want = exact(u)
+    err = float((out[:m * n].view(m, n).cpu().double() - want).norm() / want.norm())
+    assert err <= bar(m, n) + 2 * HALF_ULP[torch.float32], err
+
+
 def test_singular_values_end_near_one():
     shapes = [(192, 320), (700, 96)]
     w, plan = make(shapes)
