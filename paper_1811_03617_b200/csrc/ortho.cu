@@ -17,7 +17,10 @@
 // 3.4 each (an rms error of 5e-3 in the result for a low-rank gradient over noise, against 1e-3 for a Gaussian one).
 // The a X term carries X forward, so X is kept as a sum of two halves (22 bits) for the first kExactSteps steps; the
 // products take the high half,  X' = (a I + b A + c A^2) X_hi + a X_lo.  After that the steps contract the noise of the large directions, and carrying it exactly
-// would not help.  Measured on the CPU, relative to 64 bits: 0.4e-3 to 1.4e-3 for sides of 256 and more.
+// would not help.  Measured on the CPU, relative to 64 bits: 0.4e-3 to 1.6e-3 for sides of 256 and more.  Where the short side
+// is short, A and P have few entries of like size and their own roundings do not average out: 2e-3 to 4e-3.  Up to kSplitSide
+// A and b I + c A are kept as sums of two halves too, up to kSplitApply P as well, and the products are sums of products of
+// halves (their contractions are short): 0.3e-3 to 1.7e-3.
 #include "ortho.h"
 #include "row32.cuh"
 #include "sm100_ptx.cuh"
@@ -341,8 +344,15 @@ struct Seen {
 };
 static_assert(sizeof(Seen) == 48, "table");
 
-// T: the type of the last step's result (PHASE kLast).
-template <int PHASE, int CG, typename T = float>
+// Stages that take a tile once through its contraction (of products of halves, several follow one another).
+template <int PHASE> __device__ __forceinline__ int stages_of_a_product(const Seen &s)
+{
+    return PHASE == kGram ? s.k1 : min((int)s.k1, (s.K + KS - 1) / KS);
+}
+
+// T: the type of the last step's result (PHASE kLast).  LOW: the plan has matrices whose result has a low half here (kGram,
+// kPoly); without, their code is left out of a kernel whose launches are short.
+template <int PHASE, int CG, typename T = float, bool LOW = false>
 __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __grid_constant__ ProductParams prm)
 {
     using S = Shape<CG>;
@@ -400,29 +410,35 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
             uint32_t c = 0, s = 0, phase = 1;
             for (int t = t_begin; t < t_end && !failed; ++t) {
                 const Seen next = seen(min(t + 1, t_end - 1));
-                const CUtensorMap *map_a = prm.dev.maps + (size_t)l.matrix * kMaps + l.a_map, *map_b = prm.dev.maps + (size_t)l.matrix * kMaps + l.b_map;
+                const CUtensorMap *maps = prm.dev.maps + (size_t)l.matrix * kMaps;
                 // a pair's columns are split in halves of a multiple of 8 (the last tile's may be narrow)
                 const int half_n = CG == 2 ? min(S::BN, (l.N - l.n0 + 15) / 16 * 16) / 2 : 0;
                 const int m0 = l.m0 + 128 * rank, n0 = l.n0 + half_n * rank;
                 // steps of the contraction left of the diagonal's block of a symmetric operand's rows
                 const int a_left = l.a_sym ? l.m0 / S::BLOCK * S::BLOCK : 0, b_left = l.b_sym ? l.n0 / S::BLOCK * S::BLOCK : 0;
-                for (int st = l.k0; st < l.k1; ++st, ++c) {
-                    if (!mbar_poll(empty + s, phase, abort_flag)) { failed = true; break; }
-                    unsigned char *dst = smem + s * S::STAGE;
-                    uint64_t *here = full + s;
-                    if (++s == S::STAGES) { s = 0; phase ^= 1; }
-                    if (prm.test_drop && blockIdx.x == 0 && c == 0) continue;   // test hook: this stage never arrives
-                    if (rank == 0) mbar_arrive_expect_tx(here, CG * S::STAGE);
-                    const int k = st * KS;
-                    const uint32_t bar = CG == 2 ? in_leader(here) : 0;
-                    auto load = [&](unsigned char *to, const CUtensorMap *map, bool mn, int at) {
-                        if (CG == 2) tma_load_2d_pair(to, map, mn ? at : k, mn ? k : at, bar);
-                        else tma_load_2d(to, map, mn ? at : k, mn ? k : at, here);
-                    };
+                const int per = stages_of_a_product<PHASE>(l);
+                for (int first = 0, term = 0; first < l.k1 && !failed; first += per, ++term) {      // products of halves
+                    const CUtensorMap *map_a = maps + l.a_map, *map_b = maps + l.b_map;
+                    if (PHASE == kPoly && term > 0) { map_a = maps + (term == 2 ? kGramLoMap : kGramMap); map_b = maps + (term == 1 ? kFactorLoMap : kFactorMap); }
+                    if (PHASE >= kApply && term > 0) { if (l.a_map == kPolyMap) map_a = maps + kPolyLoMap; else map_b = maps + kPolyLoMap; }
+                    for (int st = first > 0 ? first : l.k0; st < first + per; ++st, ++c) {
+                        if (!mbar_poll(empty + s, phase, abort_flag)) { failed = true; break; }
+                        unsigned char *dst = smem + s * S::STAGE;
+                        uint64_t *here = full + s;
+                        if (++s == S::STAGES) { s = 0; phase ^= 1; }
+                        if (prm.test_drop && blockIdx.x == 0 && c == 0) continue;   // test hook: this stage never arrives
+                        if (rank == 0) mbar_arrive_expect_tx(here, CG * S::STAGE);
+                        const int k = (st - first) * KS;
+                        const uint32_t bar = CG == 2 ? in_leader(here) : 0;
+                        auto load = [&](unsigned char *to, const CUtensorMap *map, bool mn, int at) {
+                            if (CG == 2) tma_load_2d_pair(to, map, mn ? at : k, mn ? k : at, bar);
+                            else tma_load_2d(to, map, mn ? at : k, mn ? k : at, here);
+                        };
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) load(dst + i * BOX, map_a, l.a_mn || k < a_left, m0 + 64 * i);
+                        for (int i = 0; i < 2; ++i) load(dst + i * BOX, map_a, l.a_mn || k < a_left, m0 + 64 * i);
 #pragma unroll
-                    for (int i = 0; i < S::NB; ++i) load(dst + S::A_BYTES + i * BOX, map_b, l.b_mn || k < b_left, n0 + 64 * i);
+                        for (int i = 0; i < S::NB; ++i) load(dst + S::A_BYTES + i * BOX, map_b, l.b_mn || k < b_left, n0 + 64 * i);
+                    }
                 }
                 l = next;
             }
@@ -444,23 +460,26 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                 const int a_left = w.a_sym ? w.m0 / S::BLOCK * S::BLOCK : 0, b_left = w.b_sym ? w.n0 / S::BLOCK * S::BLOCK : 0;
                 if (!mbar_poll(d_empty + buf, ((u >> 1) & 1) ^ 1, abort_flag)) { failed = true; break; }
                 tc_fence_after();
-                for (int st = w.k0; st < w.k1; ++st) {
-                    if (!mbar_poll(full + s, phase, abort_flag)) { failed = true; break; }
-                    tc_fence_after();
-                    const uint32_t base = base0 + s * S::STAGE;
-                    const bool a_mn = w.a_mn || st * KS < a_left, b_mn = w.b_mn || st * KS < b_left;
-                    const uint32_t idesc = make_idesc_f16(128 * CG, n, a_mn, b_mn);
-                    const uint64_t da = a_mn ? make_mn_desc(base, BOX) : make_b_desc(base);
-                    const uint64_t db = b_mn ? make_mn_desc(base + S::A_BYTES, BOX) : make_b_desc(base + S::A_BYTES);
-                    // 16 steps of the contraction: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major box
-                    const uint32_t ia = a_mn ? 16 * 128 / 16 : 2, ib = b_mn ? 16 * 128 / 16 : 2;
-                    const int n_mma = min(4, (w.K - st * KS + 15) / 16);
+                const int per = stages_of_a_product<PHASE>(w);
+                for (int first = 0; first < w.k1 && !failed; first += per) {
+                    for (int st = first > 0 ? first : w.k0; st < first + per; ++st) {
+                        if (!mbar_poll(full + s, phase, abort_flag)) { failed = true; break; }
+                        tc_fence_after();
+                        const uint32_t base = base0 + s * S::STAGE;
+                        const bool a_mn = w.a_mn || (st - first) * KS < a_left, b_mn = w.b_mn || (st - first) * KS < b_left;
+                        const uint32_t idesc = make_idesc_f16(128 * CG, n, a_mn, b_mn);
+                        const uint64_t da = a_mn ? make_mn_desc(base, BOX) : make_b_desc(base);
+                        const uint64_t db = b_mn ? make_mn_desc(base + S::A_BYTES, BOX) : make_b_desc(base + S::A_BYTES);
+                        // 16 steps of the contraction: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major box
+                        const uint32_t ia = a_mn ? 16 * 128 / 16 : 2, ib = b_mn ? 16 * 128 / 16 : 2;
+                        const int n_mma = min(4, (w.K - (st - first) * KS + 15) / 16);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (k < n_mma) tc_mma_f16<CG>(d, da + k * ia, db + k * ib, idesc, st > w.k0 || k > 0);
-                    if (CG == 2) tc_commit_pair(empty + s); else tc_commit(empty + s);
-                    if (st == w.k1 - 1) { if (CG == 2) tc_commit_pair(d_full + buf); else tc_commit(d_full + buf); }
-                    if (++s == S::STAGES) { s = 0; phase ^= 1; }
+                        for (int k = 0; k < 4; ++k)
+                            if (k < n_mma) tc_mma_f16<CG>(d, da + k * ia, db + k * ib, idesc, st > w.k0 || k > 0);
+                        if (CG == 2) tc_commit_pair(empty + s); else tc_commit(empty + s);
+                        if (st == w.k1 - 1) { if (CG == 2) tc_commit_pair(d_full + buf); else tc_commit(d_full + buf); }
+                        if (++s == S::STAGES) { s = 0; phase ^= 1; }
+                    }
                 }
             }
         }
@@ -500,7 +519,8 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
             const int rows = min(32, here.M - m0);
             const CUtensorMap *maps = prm.dev.maps + (size_t)here.matrix * kMaps;
             const uint32_t ab = u & 1;
-            const float sx = mx.sx;
+            const float sx = mx.sx;           // (read here, while the MMAs run)
+            const bool low = LOW && mx.split >= (PHASE == kPoly ? 2 : 1);
             bool ok = mbar_poll(d_full + ab, (u >> 1) & 1, abort_flag);
             if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
             tc_fence_after();
@@ -655,10 +675,24 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                 }
                 if (!live) continue;
                 // A = X X^T and b I + c A, whose product with A the next launch takes; then P = a I + A (b I + c A)
-                auto put = [&](int map) {
+                auto put = [&](int map, int lo_map) {
                     unsigned char *to = room();
                     stage_swizzled16<__half>(to, lane, v[0], v[1]);
                     store(to, map, n0);
+                    if (!LOW || !low) return;
+                    to = room();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float a = v[j >> 2][8 * (j & 3) + 2 * e], b = v[j >> 2][8 * (j & 3) + 2 * e + 1];
+                            const float2 r = unpack_half2(pack2<__half>(a, b));
+                            w[e] = pack2<__half>(a - r.x, b - r.y);
+                        }
+                        *reinterpret_cast<uint4 *>(to + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                    store(to, lo_map, n0);
                 };
                 const float f = PHASE == kGram ? kGramScale / (sx * sx) : 1.0f / kGramScale;
                 const float diagonal = (PHASE == kGram ? kB : kA) * kGramScale;
@@ -666,7 +700,7 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[h][i] *= f;
-                if (PHASE == kGram) put(kGramOut);
+                if (PHASE == kGram) put(kGramOut, kGramLoOut);
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -674,7 +708,7 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                         if (PHASE == kGram) v[h][i] *= kC;
                         if (n0 + 32 * h + i == m0 + lane) v[h][i] += diagonal;
                     }
-                if (PHASE == kGram) put(kFactorOut); else put(kPolyOut);
+                if (PHASE == kGram) put(kFactorOut, kFactorLoOut); else put(kPolyOut, kPolyLoOut);
             }
             if (failed) break;
             here = next;
@@ -694,11 +728,11 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
     if (warp == 1) tmem_dealloc<CG>(tmem, S::TMEM);
 }
 
-template <int PHASE, typename T>
+template <int PHASE, typename T = float, bool LOW = false>
 cudaError_t launch_tiling(cudaStream_t st, const ProductParams &prm, int runs)
 {
-    return prm.dev.pair ? launch_chained<product_kernel<PHASE, 2, T>>(prm, 2 * runs, Shape<2>::THREADS, Shape<2>::SMEM, 2, st)
-                        : launch_chained<product_kernel<PHASE, 1, T>>(prm, runs, Shape<1>::THREADS, Shape<1>::SMEM, 1, st);
+    return prm.dev.pair ? launch_chained<product_kernel<PHASE, 2, T, LOW>>(prm, 2 * runs, Shape<2>::THREADS, Shape<2>::SMEM, 2, st)
+                        : launch_chained<product_kernel<PHASE, 1, T, LOW>>(prm, runs, Shape<1>::THREADS, Shape<1>::SMEM, 1, st);
 }
 
 }  // namespace
@@ -725,9 +759,9 @@ cudaError_t launch_product(cudaStream_t st, const Device &dev, Phase phase, int 
     prm.wait_kcycles = wait_kcycles > 0 ? wait_kcycles : WAIT_KCYCLES_DEFAULT;
     prm.test_drop = test_drop;
     const int runs = dev.run[phase].runs;
-    if (phase == kGram) return launch_tiling<kGram, float>(st, prm, runs);
-    if (phase == kPoly) return launch_tiling<kPoly, float>(st, prm, runs);
-    if (step < kSteps - 1) return launch_tiling<kApply, float>(st, prm, runs);
+    if (phase == kGram) return dev.split > 0 ? launch_tiling<kGram, float, true>(st, prm, runs) : launch_tiling<kGram>(st, prm, runs);
+    if (phase == kPoly) return dev.split > 1 ? launch_tiling<kPoly, float, true>(st, prm, runs) : launch_tiling<kPoly>(st, prm, runs);
+    if (step < kSteps - 1) return launch_tiling<kApply>(st, prm, runs);
     if (out->dtype == GVQ_F32) return launch_tiling<kLast, float>(st, prm, runs);
     if (out->dtype == GVQ_BF16) return launch_tiling<kLast, __nv_bfloat16>(st, prm, runs);
     return launch_tiling<kLast, __half>(st, prm, runs);

@@ -14,6 +14,8 @@ constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr float kEps = 1e-7f;
 // Steps whose X is kept as a sum of two halves (ortho.cu's header has the reason).
 constexpr int kExactSteps = 3;
+// Short sides up to which A and b I + c A, and P, are sums of two halves as well (ortho.cu's header has the reason).
+constexpr int kSplitSide = 128, kSplitApply = 48;
 // Scale of A and of a I + b A + c A^2 in half precision: entries of both are of order 1 (at most 3.5 + 1.2 |b| + 1.44 |c| = 12),
 // those off the diagonal far smaller.
 constexpr float kGramScale = 256.0f;
@@ -31,17 +33,21 @@ struct Matrix {
     uint64_t by_cols;                // floor(2^62 / cols) + 1: n / cols = (4 n * by_cols) >> 64 for n < 2^40, cols < 2^20
     // X (two buffers, in turn), X's low halves; A, b I + c A, P; rows ldx or ldr entries apart
     __half *x[2], *lo, *gram, *factor, *poly;
+    __half *gram_lo, *factor_lo, *poly_lo;      // what the last three lose in half precision 
+    int32_t split;                   // 0: nothing, 1: A and b I + c A are sums of two halves, 2: P too
     float sx;                        // scale of X in half precision
     float scale;                     // of the update
 };
 // A tile of a product, or a part of its contraction: stages [k0, k1) of 64 steps.  parts > 1: the parts' sums meet in the
 // plan's scratch from piece `slot` on (part by part), and whoever comes last adds them up.
+// Stages of products of halves follow one another: hi hi, hi lo and lo hi of A (b I + c A), P_hi X and P_lo X.
 struct Tile { int32_t matrix, tm, tn, k0, k1, part, parts, slot; };
 struct Chunk { int32_t matrix, index; };
 
 enum Phase { kGram = 0, kPoly = 1, kApply = 2, kLast = 3 };
 // Tensor maps of a matrix: operands (boxes of 64 x 64) and results (64 columns x 32 rows)
-enum Map { kX0 = 0, kX1, kGramMap, kFactorMap, kPolyMap, kX0Out, kX1Out, kLoOut, kGramOut, kFactorOut, kPolyOut, kMaps };
+enum Map { kX0 = 0, kX1, kGramMap, kFactorMap, kPolyMap, kX0Out, kX1Out, kLoOut, kGramOut, kFactorOut, kPolyOut,
+           kGramLoMap, kFactorLoMap, kPolyLoMap, kGramLoOut, kFactorLoOut, kPolyLoOut, kMaps };
 
 // The tiles of a phase, in runs, one for each CTA (or pair): run i is tiles [start[i], start[i + 1]).
 struct Run {
@@ -55,6 +61,7 @@ struct Device {
     const CUtensorMap *maps;         // [matrices][kMaps]
     Run run[4];                      // of each phase
     int pair;                        // which tiling the tiles are of
+    int split;                       // the matrices' largest
     int n_mats;
     int room;                        // all matrices fit one SM, their short sides this room; 0: they do not
     const Chunk *chunks;

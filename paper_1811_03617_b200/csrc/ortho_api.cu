@@ -25,9 +25,9 @@ constexpr size_t kAlign = 256;
 constexpr int kPartStages = 6, kMaxParts = 4;   // a part of a contraction: at least so many stages, at most so many parts
 constexpr int kTileCost = 3;      // what a tile costs beyond its contraction, in stages of 64 steps
 // Pairs of CTAs on 256 x 256 tiles from this many multiply-adds of one X P on, 128 x 64 tiles below.  Measured on either side,
-// us per call: 1280 x 1280 (2.1e9) 231 / 186, twice 512 x 4608 (2.4e9) 245 / 189, 1500 x 1500 (3.4e9) 259 / 275, four
-// 1024 x 1024 (4.3e9) 215 / 265, 2048 x 2048 (8.6e9) 298 / 448.
-constexpr int64_t kPairWork = 3'300'000'000;
+// us per call: 1280 x 1280 (2.1e9) 201 / 176, twice 512 x 4608 (2.4e9) 195 / 178, three times (3.6e9) 223 / 222, 1500 x 1500
+// (3.4e9) 285 / 238, four 1024 x 1024 (4.3e9) 252 / 227, 1700 x 1700 (4.9e9) 307 / 315, 2048 x 2048 (8.6e9) 276 / 385.
+constexpr int64_t kPairWork = 4'600'000'000;
 size_t up(size_t n) { return (n + kAlign - 1) & ~(kAlign - 1); }
 int up32(int n) { return (n + 31) & ~31; }     // rows of the work arrays: whole pieces of 32 entries
 
@@ -62,6 +62,9 @@ gvq_status lay_out(int n_layers, const int64_t *off, const int64_t *len, const i
         };
         const size_t nx = (size_t)m.rows * m.ldx, nr = (size_t)m.r * m.ldr;
         m.x[0] = take(nx); m.x[1] = take(nx); m.lo = take(nx); m.gram = take(nr); m.factor = take(nr); m.poly = take(nr);
+        m.split = m.r <= kSplitApply ? 2 : m.r <= kSplitSide ? 1 : 0;
+        if (m.split > 0) { m.gram_lo = take(nr); m.factor_lo = take(nr); }
+        if (m.split > 1) m.poly_lo = take(nr);
         out.mats.push_back(m);
     }
     return GVQ_OK;
@@ -194,6 +197,11 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
                 !map(kX1Out, m.x[1], 32, false) || !map(kLoOut, m.lo, 32, false) || !map(kGramOut, m.gram, 32, true) ||
                 !map(kFactorOut, m.factor, 32, true) || !map(kPolyOut, m.poly, 32, true))
                 return GVQ_ERR_CUDA;
+            if (m.split > 0 && (!map(kGramLoMap, m.gram_lo, 64, true) || !map(kFactorLoMap, m.factor_lo, 64, true) ||
+                                !map(kGramLoOut, m.gram_lo, 32, true) || !map(kFactorLoOut, m.factor_lo, 32, true)))
+                return GVQ_ERR_CUDA;
+            if (m.split > 1 && (!map(kPolyLoMap, m.poly_lo, 64, true) || !map(kPolyLoOut, m.poly_lo, 32, true)))
+                return GVQ_ERR_CUDA;
             m.chunk0 = (int)chunks.size();
             m.n_chunks = (int)(((int64_t)m.rows * m.cols + chunk - 1) / chunk);
             for (int k = 0; k < m.n_chunks; ++k) chunks.push_back({i, k});
@@ -207,14 +215,15 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
             for (int i = 0; i < n; ++i) {
                 const Matrix &m = sz.mats[i];
                 const int kr = (m.r + 63) / 64, kc = (m.c + 63) / 64;
+                const int poly_terms = m.split > 0 ? 3 : 1, apply_terms = m.split > 1 ? 2 : 1;     // products of halves
                 // tiles of a symmetric product: those that reach the diagonal or lie right of it
                 for (int tm = 0; tm * bm < m.r; ++tm)
                     for (int tn = (int)(tm * bm / bn); tn * bn < m.r; ++tn) {
                         gram.push_back({i, tm, tn, 0, kc, 0, 1, 0});
-                        sym.push_back({i, tm, tn, 0, kr, 0, 1, 0});
+                        sym.push_back({i, tm, tn, 0, poly_terms * kr, 0, 1, 0});
                     }
                 for (int tm = 0; tm * bm < m.rows; ++tm)
-                    for (int tn = 0; tn * bn < m.cols; ++tn) apply.push_back({i, tm, tn, 0, kr, 0, 1, 0});
+                    for (int tn = 0; tn * bn < m.cols; ++tn) apply.push_back({i, tm, tn, 0, apply_terms * kr, 0, 1, 0});
             }
         }
         const int units = pair ? ctx->num_sms / 2 : ctx->num_sms;
@@ -267,6 +276,7 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
         d.partial = reinterpret_cast<float *>(t + o_p);
         d.parts = reinterpret_cast<float *>(t + o_q);
         d.pair = pair;
+        for (const Matrix &m : sz.mats) d.split = std::max(d.split, m.split);
         d.n_mats = n;
         int room = n > 0 ? 64 : 0, longest = 0;
         for (const Matrix &m : sz.mats) {

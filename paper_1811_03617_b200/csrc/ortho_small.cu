@@ -5,9 +5,13 @@
 // side as rows: 64 entries of the short side are a row of 128 bytes (with the 128-byte swizzle), a second array holds
 // the next 64.  Then X^T is the K-major operand of X^T P and the MN-major ones of A = X X^T, nothing moves between the products
 // but the accumulators, and a thread that reads one of their rows writes it back as a row:
-//     A      D[R x R]   = sum over the long side             -> A and b I + c A, half precision, shared memory
-//     P      D[R x R]   = A (b I + c A)                      -> P = a I + D in A's place
-//     X^T P  D[128 x R] for every 128 of the long side       -> X = D + a X_lo in place
+//     A      D[R x R]   = sum over the long side             -> A as a sum of two halves, shared memory; in fp32 in registers
+//     A^2    D[R x R]   = A_hi A_hi + A_hi A_lo + A_lo A_hi  -> P = a I + b A + c D as a sum of two halves in A's place
+//     X^T P  D[128 x R] for every 128 of the long side       -> X = X_hi P + a X_lo in place
+// A and P rounded to one half would leave errors of 2e-3 to 4e-3 of the result where the short side is short (their entries
+// are then few and of like size, and the steps amplify what the singular values are off by); with A's low half, and P's up
+// to kSplitApply, it is 0.3e-3 to 1.7e-3.  Where the long side has 64 entries or fewer too, what X loses does not average
+// out either, and its low half takes part in every product.
 // R is the short side's room, 64 or 128.  The unused rows and columns of X are zeros and stay zeros; an MMA's 128 rows
 // may run on into the next array, and those rows of the accumulator are not read.
 //
@@ -56,7 +60,9 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
     const int rows = (mx.c + 63) & ~63, tiles = (mx.c + 127) / 128;
     constexpr uint32_t SQUARE_HALF = R * 128, SQUARE = R / 64 * SQUARE_HALF;
     const uint32_t half = rows * 128, array = R / 64 * half;
-    unsigned char *gram = smem, *factor = gram + SQUARE, *hi = factor + SQUARE, *lo = hi + array;
+    unsigned char *sq = smem, *sq_lo = sq + SQUARE, *hi = sq_lo + SQUARE, *lo = hi + array;     // sq: A, then P
+    const bool full = rows == 64;            // X's low half in every product
+    const bool split_p = full || mx.r <= kSplitApply;
 
     launch_dependents();
     if (threadIdx.x == 0) {
@@ -214,21 +220,31 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
         ok = __syncthreads_and(ok);
         tc_fence_after();
     };
-    // 16 entries of row m of a square operand from column n on
-    auto put16 = [&](unsigned char *to, int n, const float *v) {
+    // 16 entries of row m of the square operand from column n on
+    auto put16 = [&](int n, const float *v) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            *reinterpret_cast<uint4 *>(to + place(m, n + 8 * i, SQUARE_HALF)) =
-                make_uint4(pack2<__half>(v[8 * i], v[8 * i + 1]), pack2<__half>(v[8 * i + 2], v[8 * i + 3]),
-                           pack2<__half>(v[8 * i + 4], v[8 * i + 5]), pack2<__half>(v[8 * i + 6], v[8 * i + 7]));
+        for (int i = 0; i < 2; ++i) {
+            uint32_t h[4], l[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float a = v[8 * i + 2 * e], b = v[8 * i + 2 * e + 1];
+                h[e] = pack2<__half>(a, b);
+                const float2 r = unpack_half2(h[e]);
+                l[e] = pack2<__half>(a - r.x, b - r.y);
+            }
+            const uint32_t p = place(m, n + 8 * i, SQUARE_HALF);
+            *reinterpret_cast<uint4 *>(sq + p) = make_uint4(h[0], h[1], h[2], h[3]);
+            *reinterpret_cast<uint4 *>(sq_lo + p) = make_uint4(l[0], l[1], l[2], l[3]);
+        }
     };
-    const uint32_t a_gram = smem_u32(gram), a_factor = smem_u32(factor), a_hi = smem_u32(hi);
+    const uint32_t a_sq = smem_u32(sq), a_sq_lo = smem_u32(sq_lo), a_hi = smem_u32(hi), a_lo = smem_u32(lo);
     // step k of 16 of the short side's contraction in a K-major operand
     auto along = [](uint32_t base, uint32_t half, int k) { return make_b_desc(base + (k >> 2) * half) + 2 * (k & 3); };
     constexpr int SQUARE_PIECES = R / 16 / NPART;      // of 16 columns, of a warp
 
     for (int step = 0; step < kSteps && ok; ++step) {
-        // ---- A, and b I + c A
+        // ---- A
+        float gram[SQUARE_PIECES][16];      // this thread's entries of it
         hand_over();
         if (warp == 0) {
             constexpr uint32_t idesc = make_idesc_f16(128, R, true, true);
@@ -236,6 +252,14 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
                 // 16 rows of X^T a step.  With R = 64 the second 64 rows of the result repeat the first (chunk distance 0).
                 const uint64_t a = make_mn_desc(a_hi, R == 128 ? half : 0), b = make_mn_desc(a_hi, half);
                 for (int k = 0; k < rows / 16; ++k) tc_mma_f16<1>(tmem, a + k * (16 * 128 / 16), b + k * (16 * 128 / 16), idesc, k != 0);
+                if (full) {
+                    const uint64_t al = make_mn_desc(a_lo, R == 128 ? half : 0), bl = make_mn_desc(a_lo, half);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        tc_mma_f16<1>(tmem, a + k * (16 * 128 / 16), bl + k * (16 * 128 / 16), idesc, 1);
+                        tc_mma_f16<1>(tmem, al + k * (16 * 128 / 16), b + k * (16 * 128 / 16), idesc, 1);
+                    }
+                }
                 // (test hook: without this the wait below runs out and the kernel gives up)
                 if (!(prm.test_drop && blockIdx.x == 0 && step == 0)) tc_commit(&bar);
             }
@@ -248,14 +272,10 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
 #pragma unroll
             for (int p = 0; p < SQUARE_PIECES; ++p) {
                 const int n = 16 * (part * SQUARE_PIECES + p);
-                float v[16];
-                tmem_ld16_wait(tmem + lane_base + n, v);
+                tmem_ld16_wait(tmem + lane_base + n, gram[p]);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] *= s;
-                put16(gram, n, v);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = v[i] * kC + (n + i == m ? kB * kGramScale : 0.0f);
-                put16(factor, n, v);
+                for (int i = 0; i < 16; ++i) gram[p][i] *= s;
+                put16(n, gram[p]);
             }
         }
         // ---- P
@@ -264,7 +284,12 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
         if (warp == 0) {
             if (elect_one()) {
 #pragma unroll
-                for (int k = 0; k < R / 16; ++k) tc_mma_f16<1>(tmem, along(a_gram, SQUARE_HALF, k), along(a_factor, SQUARE_HALF, k), idesc, k != 0);
+                for (int k = 0; k < R / 16; ++k) {
+                    const uint64_t h = along(a_sq, SQUARE_HALF, k), l = along(a_sq_lo, SQUARE_HALF, k);
+                    tc_mma_f16<1>(tmem, h, h, idesc, k != 0);
+                    tc_mma_f16<1>(tmem, h, l, idesc, 1);
+                    tc_mma_f16<1>(tmem, l, h, idesc, 1);
+                }
                 tc_commit(&bar);
             }
             __syncwarp();
@@ -278,8 +303,9 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
                 float v[16];
                 tmem_ld16_wait(tmem + lane_base + n, v);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = v[i] * (1.0f / kGramScale) + (n + i == m ? kA * kGramScale : 0.0f);
-                put16(gram, n, v);
+                for (int i = 0; i < 16; ++i)
+                    v[i] = __fmaf_rn(kB, gram[p][i], v[i] * (kC / kGramScale)) + (n + i == m ? kA * kGramScale : 0.0f);
+                put16(n, v);
             }
         }
         // ---- X^T P, the accumulators of all tiles side by side
@@ -288,8 +314,14 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
             if (elect_one()) {
                 for (int t = 0; t < tiles; ++t)
 #pragma unroll
-                    for (int k = 0; k < R / 16; ++k)
-                        tc_mma_f16<1>(tmem + R * t, along(a_hi + t * (128 * 128), half, k), along(a_gram, SQUARE_HALF, k), idesc, k != 0);
+                    for (int k = 0; k < R / 16; ++k) {
+                        const uint64_t x = along(a_hi + t * (128 * 128), half, k);
+                        tc_mma_f16<1>(tmem + R * t, x, along(a_sq, SQUARE_HALF, k), idesc, k != 0);
+                        if (split_p) tc_mma_f16<1>(tmem + R * t, x, along(a_sq_lo, SQUARE_HALF, k), idesc, 1);
+                    }
+                if (full)
+#pragma unroll
+                    for (int k = 0; k < R / 16; ++k) tc_mma_f16<1>(tmem, along(a_lo, half, k), along(a_sq, SQUARE_HALF, k), idesc, 1);
                 tc_commit(&bar);
             }
             __syncwarp();
@@ -312,7 +344,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float2 x = make_float2(v[8 * c + 2 * e] * (1.0f / kGramScale), v[8 * c + 2 * e + 1] * (1.0f / kGramScale));
-                    if (step < kExactSteps) {
+                    if (step < kExactSteps && !full) {
                         const float2 a = unpack_half2(w[e]);
                         x.x = __fmaf_rn(kA, a.x, x.x);
                         x.y = __fmaf_rn(kA, a.y, x.y);
