@@ -22,7 +22,9 @@ struct gvq_ortho {
 namespace {
 
 constexpr size_t kAlign = 256;
-constexpr int kPartStages = 6, kMaxParts = 4;   // a part of a contraction: at least so many stages, at most so many parts
+// A part of a contraction: at least so many stages, at most so many parts.  (6, 4), (6, 8), (12, 4), (9, 3) in us: 515 x 1027
+// 109.6, 109.4, 112.4, 112.7; twice 512 x 4608 139, 153, 139, 147; the VGG-16-shaped weights 348, 349, 348, 353.
+constexpr int kPartStages = 6, kMaxParts = 4;
 constexpr int kTileCost = 3;      // what a tile costs beyond its contraction, in stages of 64 steps
 // Pairs of CTAs on 256 x 256 tiles from this many multiply-adds of one X P on, 128 x 64 tiles below.  Measured on either side,
 // us per call: 1280 x 1280 (2.1e9) 201 / 176, twice 512 x 4608 (2.4e9) 195 / 178, three times (3.6e9) 223 / 222, 1500 x 1500

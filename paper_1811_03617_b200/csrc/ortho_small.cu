@@ -458,6 +458,8 @@ cudaError_t launch_typed(cudaStream_t st, const SmallParams &prm, int n, int blo
 
 }  // namespace
 
+// Whatever fits is faster here: 64 x 64 14 us against 57 with a launch a product, 100 x 300 50 against 67, 32 matrices of up to
+// 64 x 576 50 against 80.
 int small_room(int r, int c)
 {
     const int blocks = (c + 63) / 64;
