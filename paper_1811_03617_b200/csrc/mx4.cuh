@@ -30,6 +30,12 @@ __device__ __forceinline__ float max_nan(float a, float b)
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
+__device__ __forceinline__ float max_nan(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 // Scale byte of a block from max |x| (NaN and infinity: 255).
 __device__ __forceinline__ uint32_t scale_byte(float amax)
 {
@@ -86,11 +92,11 @@ __device__ __forceinline__ uint32_t pair_word(uint64_t h, uint32_t p)
 // of r's float pattern, so u is added 16 places below it and the rest is cut off; below 1, where the grid keeps the
 // step 0.5 of [1, 2), the same is done to r + 1 (rounded toward zero, which keeps every bit that floor(65536 r / step)
 // depends on).  Integer and comparison instructions run at half the rate of fp32 arithmetic and are what this costs: the
-// comparison gives 1.0 or 0.0 itself, and the halves of a word are taken from its last mixing step.
+// comparison is a multiplication that saturates, and the halves of a word are taken from its last mixing step.
 __device__ __forceinline__ float round_up_or_down(float r, uint32_t u)
 {
-    float c;
-    asm("set.lt.f32.f32 %0, %1, 0f3F800000;" : "=f"(c) : "f"(r));
+    float c;      // 1 below 1, 0 from there on: 2^126 (1 - r), saturated
+    asm("fma.rn.sat.f32 %0, %1, 0fFE800000, 0f7E800000;" : "=f"(c) : "f"(r));
     const float t = __fadd_rz(r, c);
     return __uint_as_float((__float_as_uint(t) + u * 64u) & 0xFFC00000u) - c;
 }
@@ -131,9 +137,9 @@ __device__ __forceinline__ float quad_max(float m)
 }
 __device__ __forceinline__ float amax8(const float (&v)[8])
 {
-    float m = fabsf(v[0]);
+    float m = max_nan(fabsf(v[0]), fabsf(v[1]));
 #pragma unroll
-    for (int i = 1; i < 8; ++i) m = max_nan(m, fabsf(v[i]));
+    for (int i = 2; i < 8; i += 2) m = max_nan(m, fabsf(v[i]), fabsf(v[i + 1]));
     return m;
 }
 

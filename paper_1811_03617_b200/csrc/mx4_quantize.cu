@@ -17,6 +17,12 @@ using namespace mx4;
 // Eight consecutive entries as they lie in memory.
 template <typename T> struct Raw8 { uint4 q[sizeof(T) / 2]; };
 
+// 32 bytes at a 32-byte boundary that are read once.
+__device__ __forceinline__ void load32(const void *p, uint4 &a, uint4 &b)
+{
+    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "l"(p) : "memory");
+}
 template <typename T>
 __device__ __forceinline__ Raw8<T> load8(const T *p, int n, bool vec)
 {
@@ -49,7 +55,7 @@ struct QuantParams {
     uint64_t seed_w;            // mix64 of (seed, node)
     uint8_t *codes, *scales;    // along the rows; null: not wanted
     uint8_t *codes_t, *scales_t;   // along the columns
-    int vec;                    // rows start at 16-byte boundaries
+    int vec;                    // rows start at 16-byte (1) or 32-byte (2) boundaries
     int ct;                     // tiles along the columns
     // of the row kernel: a CTA has rows_per_cta rows of a chunk of columns, chunk_blocks blocks (by_chunk: 2^32 over that, up)
     int64_t padded_rows;
@@ -63,14 +69,14 @@ __device__ __forceinline__ float amax_words(const uint32_t (&w)[8 * sizeof(T)])
 {
     constexpr int N = 8 * (int)sizeof(T);
     if constexpr (sizeof(T) == 4) {
-        float m = fabsf(__uint_as_float(w[0]));
+        float m = max_nan(fabsf(__uint_as_float(w[0])), fabsf(__uint_as_float(w[1])));
 #pragma unroll
-        for (int i = 1; i < N; ++i) m = max_nan(m, fabsf(__uint_as_float(w[i])));
+        for (int i = 2; i < N; i += 2) m = max_nan(m, fabsf(__uint_as_float(w[i])), fabsf(__uint_as_float(w[i + 1])));
         return m;
     } else {      // patterns without their sign order like the magnitudes, two at a time
-        uint32_t m = w[0] & 0x7FFF7FFFu;
+        uint32_t m = __vmaxu2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu);
 #pragma unroll
-        for (int i = 1; i < N; ++i) m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
+        for (int i = 2; i < N; i += 2) m = __vimax3_u16x2(m, w[i] & 0x7FFF7FFFu, w[i + 1] & 0x7FFF7FFFu);
         const uint16_t top = (uint16_t)max(m & 0xFFFFu, m >> 16);
         T e;
         memcpy(&e, &top, 2);
@@ -109,9 +115,9 @@ __device__ __forceinline__ uint4 quantize_block(const uint32_t (&w)[8 * sizeof(T
 //                banks, and a warp's four lanes write 64 bytes of one output row
 // Bound by instructions, 8 to 15 an entry and form, most of them integer ones at half rate (a quad a block in "both" cost 4 us
 // more at the size below).  8192 x 4096 bf16 on the GPU, us, floor in bytes 13 a form and 16 for both: columns 17 nearest and
-// 35 stochastic, both 26 and 52; fp32 (floor 23 and 26) 33, 39, 39 and 57.
+// 28 stochastic, both 26 and 48; fp32 (floor 23 and 26) 34, 40, 39 and 56.
 template <typename T, bool SR, bool ROWS, bool COLS>
-__global__ void __launch_bounds__(256) mx4_quantize_kernel(const QuantParams prm)
+__global__ void __launch_bounds__(256, COLS ? 3 : 4) mx4_quantize_kernel(const QuantParams prm)
 {
     constexpr int W = 128 * (int)sizeof(T) / 4, PITCH = W + 4;    // words of a row of the tile
     extern __shared__ uint4 smem_q[];
@@ -200,7 +206,7 @@ __global__ void __launch_bounds__(256) mx4_quantize_kernel(const QuantParams prm
                 };
                 float amax = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 32; ++i) amax = max_nan(amax, fabsf(entry(i)));
+                for (int i = 0; i < 32; i += 2) amax = max_nan(amax, fabsf(entry(i)), fabsf(entry(i + 1)));
                 const uint32_t s = scale_byte(amax);
                 const float inv = inv_scale(min(s, 253u));
                 uint64_t h = 0;
@@ -242,7 +248,8 @@ __global__ void __launch_bounds__(256) mx4_quantize_kernel(const QuantParams prm
 // Along the rows only: a lane has a whole block, so that what belongs to a block (its largest entry, its scale, its row's
 // random word) costs a lane once and no shuffles; its 16 bytes of codes lie next to its neighbours'.  With a quad for a
 // block, as in the tile kernel, those were half of 13 instructions an entry, and instructions are what bounds this: 8192 x 4096
-// bf16 nearest 14.4 us on the GPU (90 % of the copy rate; the tile kernel 24), stochastic 26.5; fp32 35 and 38.
+// bf16 nearest 13.2 us on the GPU (the copy rate; the tile kernel 24), stochastic 26; fp32 30.6 and 31.8.  Loads of 32 bytes,
+// whole sectors, where rows start at such boundaries; with 16 bytes each sector is asked for twice (14.4, 26.5; 35.4 and 38.3).
 template <typename T, bool SR>
 __global__ void __launch_bounds__(256) mx4_quantize_rows_kernel(const QuantParams prm)
 {
@@ -265,7 +272,15 @@ __global__ void __launch_bounds__(256) mx4_quantize_rows_kernel(const QuantParam
             uint32_t w[W];
             const T *from = x + row * prm.ld + b * kBlock;
             const int n = (int)min((int64_t)kBlock, prm.cols - b * kBlock);
-            if (n == kBlock) {
+            if (n == kBlock && prm.vec == 2) {
+#pragma unroll
+                for (int i = 0; i < W / 8; ++i) {
+                    uint4 q, u;
+                    load32(from + i * 32 / sizeof(T), q, u);
+                    w[8 * i] = q.x; w[8 * i + 1] = q.y; w[8 * i + 2] = q.z; w[8 * i + 3] = q.w;
+                    w[8 * i + 4] = u.x; w[8 * i + 5] = u.y; w[8 * i + 6] = u.z; w[8 * i + 7] = u.w;
+                }
+            } else if (n == kBlock) {
 #pragma unroll
                 for (int i = 0; i < W / 4; ++i) {
                     const uint4 q = __ldcs(reinterpret_cast<const uint4 *>(from) + i);
@@ -504,7 +519,8 @@ cudaError_t launch_mx4_quantize(cudaStream_t st, const void *x, int dtype, int64
     prm.seed_w = seed_word(seed, node);
     prm.codes = codes; prm.scales = scales; prm.codes_t = codes_t; prm.scales_t = scales_t;
     const size_t size = dtype == GVQ_F32 ? 4 : 2;
-    prm.vec = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && (rows == 1 || (ld * size) % 16 == 0);
+    const auto starts_at = [&](unsigned bytes) { return reinterpret_cast<uintptr_t>(x) % bytes == 0 && (rows == 1 || (ld * size) % bytes == 0); };
+    prm.vec = starts_at(32) ? 2 : starts_at(16) ? 1 : 0;
     if (dtype == GVQ_F32) return launch_quantize_rounding<float>(st, prm, stochastic);
     if (dtype == GVQ_BF16) return launch_quantize_rounding<__nv_bfloat16>(st, prm, stochastic);
     return launch_quantize_rounding<__half>(st, prm, stochastic);
