@@ -63,7 +63,6 @@ struct Device {
     int pair;                        // which tiling the tiles are of
     int split;                       // the matrices' largest
     int n_mats;
-    int room;                        // all matrices fit one SM, their short sides this room; 0: they do not
     const Chunk *chunks;
     int chunk;                       // entries of one
     int n_chunks;
@@ -92,10 +91,12 @@ cudaError_t launch_start(cudaStream_t st, const Device &dev, const ElementArgs &
 cudaError_t launch_product(cudaStream_t st, const Device &dev, Phase phase, int step, const OutputArgs *out,
                            int32_t *error_word, int wait_kcycles, int test_drop);
 
-// Matrices that fit one SM (ortho_small.cu): the room their short side takes, 64 or 128; 0: they do not.
+// Matrices that fit an SM or a cluster of them (ortho_small.cu): the room their short side takes, 64 or 128 (0: they do not
+// fit), the CTAs of a matrix and the entries of the long side that each has.
+struct SmallPlan { int room, parts, span; };
 constexpr size_t kSmallSmem = 226 * 1024;
-int small_room(int r, int c);
-cudaError_t launch_small(cudaStream_t st, const Matrix *mats, int n, int room, int blocks, const ElementArgs &in, const OutputArgs &out,
+SmallPlan small_plan(int n, int r, int c, int num_sms);      // n matrices, the largest of their short and of their long sides
+cudaError_t launch_small(cudaStream_t st, const Matrix *mats, int n, const SmallPlan &plan, const ElementArgs &in, const OutputArgs &out,
                          int32_t *error_word, int wait_kcycles, int test_drop);
 
 }  // namespace ortho

@@ -15,7 +15,7 @@ struct gvq_ortho {
     gvq_ctx *ctx = nullptr;
     int device = 0;              // (destroying the plan does not touch the context, which may be gone)
     Device dev{};
-    int small_blocks = 0;        // of 64 entries of the longest side, where all matrices fit one SM
+    SmallPlan small{};           // where all matrices fit an SM or a cluster of them
     void *tables = nullptr;      // one device allocation: matrices, tensor maps, tiles, chunks, partial sums
 };
 
@@ -136,8 +136,8 @@ gvq_status run(gvq_ortho *p, const ElementArgs &in, const OutputArgs &out)
 {
     gvq_ctx *ctx = p->ctx;
     DeviceGuard guard(ctx->device);
-    if (p->dev.room > 0) {
-        GVQ_CUDA(ctx, launch_small(ctx->stream, p->dev.mats, p->dev.n_mats, p->dev.room, p->small_blocks, in, out, ctx->error_word,
+    if (p->small.room > 0) {
+        GVQ_CUDA(ctx, launch_small(ctx->stream, p->dev.mats, p->dev.n_mats, p->small, in, out, ctx->error_word,
                                    ctx->wait_kcycles, ctx->drop_last_load));
         return GVQ_OK;
     }
@@ -280,15 +280,12 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
         d.pair = pair;
         for (const Matrix &m : sz.mats) d.split = std::max(d.split, m.split);
         d.n_mats = n;
-        int room = n > 0 ? 64 : 0, longest = 0;
+        int shorter = 0, longer = 0;
         for (const Matrix &m : sz.mats) {
-            const int need = small_room(m.r, m.c);
-            room = need == 0 || room == 0 ? 0 : std::max(room, need);
-            longest = std::max(longest, m.c);
+            shorter = std::max(shorter, m.r);
+            longer = std::max(longer, m.c);
         }
-        p->small_blocks = (longest + 63) / 64;
-        // (one room serves all: a long matrix of few rows next to a short one of many may not fit it)
-        d.room = room > 0 && small_room(room, longest) == room ? room : 0;
+        p->small = small_plan(n, shorter, longer, ctx->num_sms);
         d.chunk = chunk;
         *out = p;
         return GVQ_OK;

@@ -1,4 +1,7 @@
-// The orthogonalised update of matrices that fit one SM, a whole update in one launch, one CTA a matrix.
+// The orthogonalised update of matrices that fit one SM, or the few of a cluster, a whole update in one launch.
+//
+// A cluster of `parts` CTAs has a matrix, each a span of its long side.  All but A's sum stays in a CTA: the parts' sums meet in
+// shared memory (of the cluster, read by all, each in an order of its own that does not change), and every CTA makes P for itself.
 //
 // For a small matrix the products take a microsecond and the fifteen launches of ortho.cu 3.3 us each.  Here X stays in
 // shared memory from the gradient to the weights: as a sum of two halves (ortho.cu has the reasons), transposed, the long
@@ -36,6 +39,7 @@ struct SmallParams {
     ElementArgs in;
     OutputArgs out;
     int mode;                // of the momentum, as in ortho.cu
+    int parts, span;         // CTAs of a matrix; entries of the long side each has, a multiple of 64
     int32_t *error_word;
     int wait_kcycles, test_drop;
 };
@@ -56,8 +60,14 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
     __shared__ uint32_t tmem_slot;
     __shared__ int flags[4];                 // abort flag, -, limit of the waits
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Matrix &mx = prm.mats[blockIdx.x];
-    const int rows = (mx.c + 63) & ~63, tiles = (mx.c + 127) / 128;
+    __shared__ float shared_sum;             // of the squares, for the cluster
+    __shared__ float shared_ok;
+    const Matrix &mx = prm.mats[blockIdx.x / prm.parts];
+    // this CTA's span of the long side (it may be empty: zeros, which add nothing)
+    const int part_of = blockIdx.x % prm.parts, first = min(part_of * prm.span, mx.c), mine = min(prm.span, mx.c - first);
+    const int my_rows = mx.tall ? mine : mx.rows, my_cols = mx.tall ? mx.cols : mine;
+    const int64_t off = mx.off + (mx.tall ? (int64_t)first * mx.cols : first);
+    const int rows = max(64, (mine + 63) & ~63), tiles = (rows + 127) / 128;
     constexpr uint32_t SQUARE_HALF = R * 128, SQUARE = R / 64 * SQUARE_HALF;
     const uint32_t half = rows * 128, array = R / 64 * half;
     unsigned char *sq = smem, *sq_lo = sq + SQUARE, *hi = sq_lo + SQUARE, *lo = hi + array;     // sq: A, then P
@@ -80,12 +90,15 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
     grid_dependency_wait();
 
     // u = g + beta * momentum, its bits in the two arrays until the norm is known
-    const int total = mx.rows * mx.cols;
-    const float *g = prm.in.g + mx.off;
-    float *mo = prm.mode ? prm.in.momentum + mx.off : nullptr;
+    const int total = my_rows * my_cols;
+    const float *g = prm.in.g + off;
+    float *mo = prm.mode ? prm.in.momentum + off : nullptr;
     float sum = 0.0f;
+    const uint64_t by_cols = my_cols == mx.cols ? mx.by_cols : ((uint64_t)1 << 62) / (uint64_t)max(1, my_cols) + 1;
+    int from = 0;                            // where entry e of this CTA's is in memory, once at(e) has been asked for
     auto at = [&](int e) {
-        const int row = (int)__umul64hi((uint64_t)e << 2, mx.by_cols), col = e - row * mx.cols;
+        const int row = (int)__umul64hi((uint64_t)e << 2, by_cols), col = e - row * my_cols;
+        from = row * mx.cols + col;
         return mx.tall ? place(row, col, half) : place(col, row, half);
     };
     auto direct = [&](float u, float &m) {
@@ -101,7 +114,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
     // here, and the lanes take their four columns in orders that keep a warp's words in different banks.
     const bool quads = (mx.cols & 3) == 0;
     const int tall_quads = quads && mx.tall ? total / 4 : 0;
-    const int strips = (mx.rows + 7) / 8, wide_tiles = quads && !mx.tall ? strips * ((mx.cols + 31) / 32) : 0;
+    const int strips = (my_rows + 7) / 8, wide_tiles = quads && !mx.tall ? strips * ((my_cols + 31) / 32) : 0;
     const int lane_row = 2 * (lane >> 3), lane_col = 4 * (lane & 7), turn = (lane & 7) >> 1;
     auto turned = [&](uint32_t (&w)[4]) {      // w[c] = w[(c + turn) % 4]
         if (turn & 1) { const uint32_t x = w[0]; w[0] = w[1]; w[1] = w[2]; w[2] = w[3]; w[3] = x; }
@@ -134,7 +147,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
     auto tile_at = [&](int w, int &row, int &col) {
         row = 8 * (w % strips) + lane_row;
         col = 32 * (w / strips) + lane_col;
-        return w < wide_tiles && row < mx.rows && col < mx.cols;
+        return w < wide_tiles && row < my_rows && col < my_cols;
     };
     for (int w0 = warp; w0 < wide_tiles; w0 += TILES * (NTHREADS / 32)) {
         float4 x[TILES][2], m[TILES][2];
@@ -145,8 +158,8 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int e = (row + h) * mx.cols + col;
-                x[i][h] = load4(g, e, in && row + h < mx.rows);
-                m[i][h] = load4(mo_or_g, e, in && row + h < mx.rows);
+                x[i][h] = load4(g, e, in && row + h < my_rows);
+                m[i][h] = load4(mo_or_g, e, in && row + h < my_rows);
             }
         }
 #pragma unroll
@@ -156,10 +169,10 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
             uint32_t b[2][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if (row + h >= mx.rows) x[i][h] = make_float4(0.f, 0.f, 0.f, 0.f), m[i][h] = x[i][h];
+                if (row + h >= my_rows) x[i][h] = make_float4(0.f, 0.f, 0.f, 0.f), m[i][h] = x[i][h];
                 b[h][0] = direct(x[i][h].x, m[i][h].x); b[h][1] = direct(x[i][h].y, m[i][h].y);
                 b[h][2] = direct(x[i][h].z, m[i][h].z); b[h][3] = direct(x[i][h].w, m[i][h].w);
-                if (prm.mode && row + h < mx.rows) *reinterpret_cast<float4 *>(mo + (row + h) * mx.cols + col) = m[i][h];
+                if (prm.mode && row + h < my_rows) *reinterpret_cast<float4 *>(mo + (row + h) * mx.cols + col) = m[i][h];
             }
             turned(b[0]);
             turned(b[1]);
@@ -173,9 +186,10 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
     }
 #pragma unroll 8
     for (int e = threadIdx.x; !quads && e < total; e += NTHREADS) {
-        float m = prm.mode ? mo[e] : 0.0f;
-        const uint32_t b = direct(g[e], m), p = at(e);
-        if (prm.mode) mo[e] = m;
+        const uint32_t p = at(e);
+        float m = prm.mode ? mo[from] : 0.0f;
+        const uint32_t b = direct(g[from], m);
+        if (prm.mode) mo[from] = m;
         *reinterpret_cast<uint16_t *>(hi + p) = (uint16_t)(b >> 16);
         *reinterpret_cast<uint16_t *>(lo + p) = (uint16_t)b;
     }
@@ -186,6 +200,13 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
     sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < NTHREADS / 32; ++i) sum += sums[i];
+    if (prm.parts > 1) {
+        if (threadIdx.x == 0) shared_sum = sum;
+        __syncwarp();
+        cluster_sync();
+        sum = 0.0f;
+        for (int p = 0; p < prm.parts; ++p) sum += load_cluster1(cluster_address(smem_u32(&shared_sum), p));
+    }
     const float f = mx.sx / (sqrtf(sum) + kEps);
     // X = u / |u|: places do not matter here (zeros stay zeros)
     for (uint32_t i = threadIdx.x; i < array / 16; i += NTHREADS) {
@@ -242,7 +263,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
     auto along = [](uint32_t base, uint32_t half, int k) { return make_b_desc(base + (k >> 2) * half) + 2 * (k & 3); };
     constexpr int SQUARE_PIECES = R / 16 / NPART;      // of 16 columns, of a warp
 
-    for (int step = 0; step < kSteps && ok; ++step) {
+    for (int step = 0; step < kSteps; ++step) {
         // ---- A
         float gram[SQUARE_PIECES][16];      // this thread's entries of it
         hand_over();
@@ -266,13 +287,64 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
             __syncwarp();
         }
         wait();
-        if (!ok) break;
+        if (prm.parts == 1 && !ok) break;
+        if (live)
+#pragma unroll
+            for (int p = 0; p < SQUARE_PIECES; ++p) tmem_ld16_wait(tmem + lane_base + 16 * (part * SQUARE_PIECES + p), gram[p]);
+        if (prm.parts > 1) {
+            // The parts' sums, in the place of the square operand (nothing reads it now): words of four columns, rows next to
+            // each other.  If one CTA has given up, all do.
+            float4 *join = reinterpret_cast<float4 *>(sq);
+            if (live)
+#pragma unroll
+                for (int p = 0; p < SQUARE_PIECES; ++p)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        join[(4 * (part * SQUARE_PIECES + p) + i) * R + m] =
+                            make_float4(gram[p][4 * i], gram[p][4 * i + 1], gram[p][4 * i + 2], gram[p][4 * i + 3]);
+            if (threadIdx.x == 0) shared_ok = ok ? 1.0f : 0.0f;
+            __syncwarp();
+            cluster_sync();
+            // (each starts from its own, so that they do not all read the same one at a time)
+            const uint32_t join_at = smem_u32(join) + m * 16, ok_at = smem_u32(&shared_ok);
+            constexpr int AHEAD = 3;
+            for (int i0 = 1; i0 < prm.parts; i0 += AHEAD) {
+                uint32_t there[AHEAD];
+                float fine[AHEAD];
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    const int c = part_of + min(i0 + i, prm.parts - 1), peer = c < prm.parts ? c : c - prm.parts;
+                    there[i] = cluster_address(join_at, peer);
+                    fine[i] = load_cluster1(cluster_address(ok_at, peer));
+                }
+#pragma unroll
+                for (int p = 0; p < SQUARE_PIECES; ++p) {
+                    float4 x[AHEAD][4];
+#pragma unroll
+                    for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            x[i][k] = live && i0 + i < prm.parts ? load_cluster(there[i] + (4 * (part * SQUARE_PIECES + p) + k) * R * 16)
+                                                                 : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            gram[p][4 * k] += x[i][k].x; gram[p][4 * k + 1] += x[i][k].y;
+                            gram[p][4 * k + 2] += x[i][k].z; gram[p][4 * k + 3] += x[i][k].w;
+                        }
+                }
+                ok = ok && fine[0] != 0.0f && fine[1] != 0.0f && fine[2] != 0.0f;
+            }
+            __syncwarp();
+            cluster_sync();
+            if (!ok) break;
+        }
         if (live) {
             const float s = kGramScale / (mx.sx * mx.sx);
 #pragma unroll
             for (int p = 0; p < SQUARE_PIECES; ++p) {
                 const int n = 16 * (part * SQUARE_PIECES + p);
-                tmem_ld16_wait(tmem + lane_base + n, gram[p]);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) gram[p][i] *= s;
                 put16(n, gram[p]);
@@ -295,7 +367,10 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
             __syncwarp();
         }
         wait();
-        if (!ok) break;
+        if (!ok) {
+            if (prm.parts > 1) continue;     // (the others hear of it where the parts meet)
+            break;
+        }
         if (live) {
 #pragma unroll
             for (int p = 0; p < SQUARE_PIECES; ++p) {
@@ -327,7 +402,10 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
             __syncwarp();
         }
         wait();
-        if (!ok) break;
+        if (!ok) {
+            if (prm.parts > 1) continue;     // (the others hear of it where the parts meet)
+            break;
+        }
 #pragma unroll 1
         for (int p = part; p < tiles * (R / 32); p += NPART) {       // 32 columns at a time
             const int t = p / (R / 32), n = 32 * (p - t * (R / 32)), i = 128 * t + m;
@@ -362,7 +440,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
 
     if (ok) {
         // the result, from both halves
-        T *out = static_cast<T *>(prm.out.ptr) + mx.off;
+        T *out = static_cast<T *>(prm.out.ptr) + off;
         const float k = (prm.out.update ? -prm.out.step * mx.scale : 1.0f) / mx.sx;
         auto entry = [&](uint32_t p) {
             return __half2float(*reinterpret_cast<const __half *>(hi + p)) + __half2float(*reinterpret_cast<const __half *>(lo + p));
@@ -402,7 +480,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
                 const bool in = tile_at(w0 + i * (NTHREADS / 32), row, col);
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
-                    if (prm.out.update) o[i][h] = *reinterpret_cast<const Quad *>(out + (in && row + h < mx.rows ? (row + h) * mx.cols + col : 0));
+                    if (prm.out.update) o[i][h] = *reinterpret_cast<const Quad *>(out + (in && row + h < my_rows ? (row + h) * mx.cols + col : 0));
             }
 #pragma unroll
             for (int i = 0; i < TILES; ++i) {
@@ -423,13 +501,13 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
                     for (int c = 0; c < 4; ++c) finish(o[i][h], c, __uint_as_float(x[h][c]));
                 }
                 *reinterpret_cast<Quad *>(out + row * mx.cols + col) = o[i][0];
-                if (row + 1 < mx.rows) *reinterpret_cast<Quad *>(out + (row + 1) * mx.cols + col) = o[i][1];
+                if (row + 1 < my_rows) *reinterpret_cast<Quad *>(out + (row + 1) * mx.cols + col) = o[i][1];
             }
         }
 #pragma unroll 8
         for (int e = threadIdx.x; !quads && e < total; e += NTHREADS) {
             const float x = entry(at(e));
-            out[e] = from_f<T>(prm.out.update ? __fmaf_rn(k, x, prm.out.decay * to_f(out[e])) : k * x);
+            out[from] = from_f<T>(prm.out.update ? __fmaf_rn(k, x, prm.out.decay * to_f(out[from])) : k * x);
         }
     } else if (threadIdx.x == 0) {
         atomicExch(prm.error_word, 100);
@@ -443,42 +521,53 @@ __global__ void __launch_bounds__(NTHREADS, 1) ortho_small_kernel(const SmallPar
 template <int R> size_t small_smem(int blocks) { return (size_t)(R / 64) * 128 * (2 * R + 2 * 64 * blocks) + 1024; }
 
 template <int R, typename T>
-cudaError_t launch_as(cudaStream_t st, const SmallParams &prm, int n, int blocks)
+cudaError_t launch_as(cudaStream_t st, const SmallParams &prm, int n)
 {
-    // (the launch helper raises a kernel's limit once: the first launch asks for all there is)
-    return launch_chained<ortho_small_kernel<R, T>>(prm, n, NTHREADS, std::max(small_smem<R>(blocks), kSmallSmem), 1, st);
+    // (the launch helper raises a kernel's limit once: every launch asks for all there is)
+    return launch_chained<ortho_small_kernel<R, T>>(prm, n * prm.parts, NTHREADS, kSmallSmem, prm.parts, st);
 }
 template <int R>
-cudaError_t launch_typed(cudaStream_t st, const SmallParams &prm, int n, int blocks)
+cudaError_t launch_typed(cudaStream_t st, const SmallParams &prm, int n)
 {
-    if (prm.out.dtype == GVQ_F32) return launch_as<R, float>(st, prm, n, blocks);
-    if (prm.out.dtype == GVQ_BF16) return launch_as<R, __nv_bfloat16>(st, prm, n, blocks);
-    return launch_as<R, __half>(st, prm, n, blocks);
+    if (prm.out.dtype == GVQ_F32) return launch_as<R, float>(st, prm, n);
+    if (prm.out.dtype == GVQ_BF16) return launch_as<R, __nv_bfloat16>(st, prm, n);
+    return launch_as<R, __half>(st, prm, n);
 }
 
 }  // namespace
 
-// Whatever fits is faster here: 64 x 64 14 us against 57 with a launch a product, 100 x 300 50 against 67, 32 matrices of up to
-// 64 x 576 50 against 80.
-int small_room(int r, int c)
+// Whatever fits is faster here, in us against a launch a product (ortho.cu): 64 x 64 18 against 57, 100 x 300 49 / 67, 64 x 1500
+// 46 / 79, 20 x 3333 62 / 97, 128 x 512 62 / 84, 128 x 1000 82 / 88, 32 matrices of up to 64 x 576 40 / 80; but not eight parts of
+// a short side of more than 64, whose sums are four times as long (90 x 2400 128 / 99).  As few parts as fit, or up to four of
+// short sides of up to 64 while a part has more than five blocks of the long side: 64 x 576 40 us with one, 38 with two, 37 with
+// four, 47 with eight; 64 x 1500 46 with four, 50 with eight; 100 x 300 49 with one, 58 with two.
+SmallPlan small_plan(int n, int r, int c, int num_sms)
 {
-    const int blocks = (c + 63) / 64;
-    if (r <= 64 && small_smem<64>(blocks) <= kSmallSmem) return 64;
-    return r <= 128 && small_smem<128>(blocks) <= kSmallSmem ? 128 : 0;
+    SmallPlan p{r <= 64 ? 64 : 128, 1, 0};
+    const int blocks = (c + 63) / 64, most = p.room == 64 ? 8 : 4;
+    auto span = [&](int parts) { return (blocks + parts - 1) / parts; };
+    auto fits = [&](int parts) { return (p.room == 64 ? small_smem<64>(span(parts)) : small_smem<128>(span(parts))) <= kSmallSmem; };
+    while (p.parts < most && !fits(p.parts)) p.parts *= 2;
+    if (n == 0 || r > 128 || !fits(p.parts) || (p.parts > 1 && n * p.parts > num_sms)) return SmallPlan{};
+    while (p.room == 64 && p.parts < 4 && n * 2 * p.parts <= num_sms && span(p.parts) > 5) p.parts *= 2;
+    p.span = 64 * span(p.parts);
+    return p;
 }
 
-cudaError_t launch_small(cudaStream_t st, const Matrix *mats, int n, int room, int blocks, const ElementArgs &in, const OutputArgs &out,
+cudaError_t launch_small(cudaStream_t st, const Matrix *mats, int n, const SmallPlan &plan, const ElementArgs &in, const OutputArgs &out,
                          int32_t *error_word, int wait_kcycles, int test_drop)
 {
     SmallParams prm;
     prm.mats = mats;
+    prm.parts = plan.parts;
+    prm.span = plan.span;
     prm.in = in;
     prm.out = out;
     prm.mode = !in.momentum ? 0 : in.nesterov ? 2 : 1;
     prm.error_word = error_word;
     prm.wait_kcycles = wait_kcycles > 0 ? wait_kcycles : WAIT_KCYCLES_DEFAULT;
     prm.test_drop = test_drop;
-    return room == 64 ? launch_typed<64>(st, prm, n, blocks) : launch_typed<128>(st, prm, n, blocks);
+    return plan.room == 64 ? launch_typed<64>(st, prm, n) : launch_typed<128>(st, prm, n);
 }
 
 }  // namespace ortho

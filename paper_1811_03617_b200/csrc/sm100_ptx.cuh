@@ -112,6 +112,12 @@ __device__ __forceinline__ float4 load_cluster(uint32_t cluster_addr)
                  : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr) : "memory");
     return v;
 }
+__device__ __forceinline__ float load_cluster1(uint32_t cluster_addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
+    return v;
+}
 // Programmatic dependent launch: a kernel launched with the stream-serialization attribute may start while
 // its predecessor in the stream still runs, once every CTA of the predecessor has called launch_dependents
 // (or exited); grid_dependency_wait returns when the predecessor has completed and its writes are visible.

@@ -132,6 +132,44 @@ def test_small_matrices(shapes, dtype):
     assert torch.equal(out[~rest], again[~rest])
 
 
+# Plans whose matrices are shared by the CTAs of a cluster: two, four and eight of them, long sides that leave the last ones
+# little or nothing, either orientation, rows of whole quads and others.
+CLUSTER = [[(64, 1500), (64, 1), (7, 100)], [(20, 3333)], [(3333, 50), (50, 65)], [(37, 801), (802, 37), (64, 640)], [(128, 1000), (5, 7), (90, 321)],
+           [(500, 100)], [(63, 5001)]]
+
+
+@pytest.mark.parametrize("shapes", CLUSTER)
+@pytest.mark.parametrize("dtype", list(DT))
+def test_matrices_that_a_cluster_shares(shapes, dtype):
+    w, plan = make(shapes)
+    gen = torch.Generator().manual_seed(5)
+    g = torch.randn(w.M, generator=gen)
+    mo, wt = torch.randn(w.M, generator=gen), torch.randn(w.M, generator=gen).to(DT[dtype])
+    out = torch.full((w.M,), 7.0, dtype=DT[dtype], device="cuda")
+    plan.orthogonalize(g.cuda(), out)
+    dm, dw = mo.cuda(), wt.cuda()
+    plan.step(g.cuda(), dm, dw, lr=0.5, weight_decay=0.1, beta=0.9)
+    plan.ctx.device_status()
+    got, gm, gw = out.cpu(), dm.cpu(), dw.cpu()
+    inside = torch.zeros(w.M, dtype=torch.bool)
+    for (m, n), o in zip(shapes, w.layer_off):
+        at = slice(o, o + m * n)
+        inside[at] = True
+        want = exact(g[at].view(m, n))
+        err = float((got[at].view(m, n).double() - want).norm() / want.norm())
+        assert err <= bar(m, n) + 2 * HALF_ULP[DT[dtype]], (m, n, err)
+        new_m = 0.9 * mo[at].double() + g[at].double()
+        assert float((gm[at].double() - new_m).abs().max()) <= 1e-6
+        want = exact((g[at].double() + 0.9 * new_m).view(m, n)) * math.sqrt(max(1.0, m / n)) * 0.5
+        moved = wt[at].view(m, n).double() * (1 - 0.5 * 0.1) - gw[at].view(m, n).double()
+        slack = 2 * HALF_ULP[DT[dtype]] * float(wt[at].double().norm() + want.norm())
+        assert float((moved - want).norm()) <= (bar(m, n) * float(want.norm()) + slack), (m, n)
+    assert bool((got[~inside] == 7.0).all()) and torch.equal(gm[~inside], mo[~inside]) and torch.equal(gw[~inside], wt[~inside])
+    again = torch.full((w.M,), 7.0, dtype=DT[dtype], device="cuda")
+    plan.orthogonalize(g.cuda(), again)
+    assert torch.equal(again, out)
+
+
 def test_a_small_plan_gives_what_a_larger_one_gives():
     """The same matrix alone (one SM) and next to one that does not fit (tiles): two summation orders of one algorithm."""
     w1, one = make([(64, 320)])
@@ -366,6 +404,29 @@ def test_a_wait_that_runs_out_is_reported_and_the_plan_recovers(shape):
     plan.orthogonalize(g, out)
     plan.ctx.device_status()
     assert torch.equal(out[:n], good)
+
+
+def test_a_cluster_whose_wait_runs_out_is_reported_and_the_plan_recovers():
+    from paper_1811_03617_b200 import gvq
+    shape = (64, 1500)
+    w, plan = make([shape])
+    g = torch.randn(w.M).cuda()
+    good, out = torch.zeros(w.M, device="cuda"), torch.zeros(w.M, device="cuda")
+    plan.orthogonalize(g, good)
+    plan.ctx.device_status()
+    plan.ctx.set_limits(wait_cycles=2_000_000)
+    plan.ctx.test_drop_load(True)
+    try:
+        plan.orthogonalize(g, out)
+        with pytest.raises(gvq.GvqError) as e:
+            plan.ctx.device_status()
+        assert e.value.status == 9
+    finally:
+        plan.ctx.test_drop_load(False)
+        plan.ctx.set_limits()
+    plan.orthogonalize(g, out)
+    plan.ctx.device_status()
+    assert torch.equal(out, good)
 
 
 def test_a_plan_can_be_destroyed_after_its_context():
