@@ -508,7 +508,8 @@ gvq_status gvq_mx4_dequantize(gvq_ctx *ctx, const uint8_t *codes, const uint8_t 
    a: [M][K], b: [N][K] as gvq_mx4_quantize lays them out; out: device, dtype entries, rows ld entries apart (ld >= N),
    aligned to its entries' size.  A linear layer y = x W^T takes x and W along their rows; its gradients
    dx = dy W take dy along its rows and W along its columns, dW = dy^T x both along their columns.
-   Few rows of a (M <= 64, a token or a small batch against kept weights) have a form of their own. */
+   Few rows of a (a token or a small batch against kept weights) have forms of their own; the sum's order depends on the
+   sizes alone, so a call gives the same bits every time. */
 gvq_status gvq_mx4_matmul(gvq_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *b_codes,
                           const uint8_t *b_scales, int64_t M, int64_t N, int64_t K, void *out, int dtype, int64_t ld);
 
@@ -535,7 +536,7 @@ gvq_status gvq_mx4_dequantize_aggregate(gvq_ctx *ctx, const uint8_t *const *code
      w = (1 - lr * weight_decay) w - lr * scale * X          (a, b, c) = (3.4445, -4.7750, 2.0315)
    (the update of the Muon optimiser: every singular value of u is moved to about 1; scale = sqrt(max(1, rows / cols))
    unless given).  The products run on the tensor cores with half-precision operands and fp32 accumulation: X is within
-   about 2e-3 (relative, rms) of its value in exact arithmetic.  Momentum, norms and the weights' sum are fp32, each
+   2.5e-3 (relative, rms; 1.7e-3 where the shorter side is at most 128) of its value in exact arithmetic.  Momentum, norms and the weights' sum are fp32, each
    rounding to w's type once.  A matrix that is zero moves nothing (X = 0); one that holds a NaN or an infinity gives NaN
    or zero for its own layer, as the formula does, and touches no other.
    rows, cols: HOST arrays [n_layers], rows[l] * cols[l] = layer_len[l], or both 0: the layer is left alone; the shorter

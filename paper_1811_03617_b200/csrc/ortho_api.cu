@@ -131,7 +131,7 @@ void split(std::vector<Tile> &tiles, int units, int pieces, int &slots)
     tiles = out;
 }
 
-// The whole update: one launch where every matrix fits one SM, otherwise two element-wise ones and three a step.
+// The whole update: one launch where every matrix fits an SM or a cluster of them, otherwise two element-wise ones and three a step.
 gvq_status run(gvq_ortho *p, const ElementArgs &in, const OutputArgs &out)
 {
     gvq_ctx *ctx = p->ctx;

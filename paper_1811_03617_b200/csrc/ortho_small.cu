@@ -18,8 +18,9 @@
 // R is the short side's room, 64 or 128.  The unused rows and columns of X are zeros and stay zeros; an MMA's 128 rows
 // may run on into the next array, and those rows of the accumulator are not read.
 //
-// What bounds it is the chain of its steps (MMAs, a wait, accumulator to shared memory, a fence, fifteen times, 1.6 us a
-// step), and beyond that the conversions of X, an entry a lane.
+// What bounds it is the chain of its steps (MMAs, a wait, accumulator to shared memory, a fence, fifteen times, 2.5 us a
+// step at 64 x 64), beyond that the conversions of X, an entry a lane, and between CTAs the join of A (1 us a step with four
+// and a short side of 64).
 #include <algorithm>
 
 #include "ortho.h"
