@@ -292,43 +292,51 @@ def _rows(t: torch.Tensor, what: str):
 class Mx4:
     """A matrix [rows][cols] in microscaled 4-bit floating point: device bytes `codes` and `scales` (see gvq.h)."""
 
-    __slots__ = ("rows", "cols", "_codes", "_scales", "_buf", "_n", "_at", "codes_ptr", "scales_ptr")
+    __slots__ = ("rows", "cols", "_codes", "_scales", "_buf", "codes_ptr", "scales_ptr")
 
     def __init__(self, rows: int, cols: int, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
                  device=None):
-        self.rows, self.cols = rows, cols = int(rows), int(cols)
+        rows, cols = int(rows), int(cols)
         nb = (cols + 31) // 32
         tiles = ((rows + 127) // 128) * ((nb + 3) // 4)
         if rows < 1 or cols < 1 or tiles >= 0x7FFFFFFF:
             raise ValueError(f"no 4-bit matrix of {rows} x {cols}")
-        nc, ns = rows * nb * 16, tiles * 512
-        self._n = (nc, ns)
+        self.rows, self.cols = rows, cols
         if codes is None and scales is None:       # one allocation for both
-            self._at = (nc + 255) & ~255
-            self._buf = torch.empty(self._at + ns, dtype=torch.uint8, device=device or "cuda")
-            self._codes = self._scales = None
-            self.codes_ptr = self._buf.data_ptr()
-            self.scales_ptr = self.codes_ptr + self._at
+            at = (rows * nb * 16 + 255) & ~255
+            self._buf = buf = torch.empty(at + tiles * 512, dtype=torch.uint8, device=device or "cuda")
+            self._codes = None
+            self.codes_ptr = p = buf.data_ptr()
+            self.scales_ptr = p + at
             return
         if codes is None or scales is None:
             raise ValueError("codes and scales come together")
+        nc, ns = self._sizes()
         for t, n in ((codes, nc), (scales, ns)):
             if t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous() or t.numel() < n:
                 raise ValueError(f"a 4-bit matrix of {rows} x {cols} has {nc} bytes of codes and {ns} of scales, contiguous")
         self._codes, self._scales = codes, scales
         self.codes_ptr, self.scales_ptr = codes.data_ptr(), scales.data_ptr()
 
+    def _sizes(self):
+        """Bytes of codes and of scales."""
+        nb = (self.cols + 31) // 32
+        return self.rows * nb * 16, ((self.rows + 127) // 128) * ((nb + 3) // 4) * 512
+
+    def _views(self):
+        if self._codes is None:
+            nc, ns = self._sizes()
+            at = self.scales_ptr - self.codes_ptr
+            self._codes, self._scales = self._buf[:nc], self._buf[at:at + ns]
+        return self._codes, self._scales
+
     @property
     def codes(self) -> torch.Tensor:
-        if self._codes is None:
-            self._codes = self._buf[:self._n[0]]
-        return self._codes
+        return self._views()[0]
 
     @property
     def scales(self) -> torch.Tensor:
-        if self._scales is None:
-            self._scales = self._buf[self._at:self._at + self._n[1]]
-        return self._scales
+        return self._views()[1]
 
 
 class Context:
