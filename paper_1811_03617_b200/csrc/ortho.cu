@@ -189,8 +189,10 @@ template <int CG> struct Shape {
     static constexpr int BN = CG == 2 ? kPairN : kSoloN;                     // columns of a tile
     static constexpr int BLOCK = 128 * CG;                                   // of the diagonal of a symmetric result
     static constexpr int NB = CG == 2 ? 2 : BN / 64;                        // boxes of B a CTA loads
-    static constexpr uint32_t A_BYTES = 2 * BOX, STAGE = A_BYTES + NB * BOX;
-    static constexpr int STAGES = 5;
+    static constexpr uint32_t A_BYTES = 2 * BOX, BYTES = A_BYTES + NB * BOX;    // of KS steps of the contraction
+    // Of a CTA alone they come two at a time: its four small MMAs take 128 clocks, waiting for them and reporting them 160.
+    static constexpr int PER_STAGE = CG == 2 ? 1 : 2, STAGES = CG == 2 ? 5 : 4;
+    static constexpr uint32_t STAGE = PER_STAGE * BYTES;
     static constexpr int NEPI = CG == 2 ? 8 : 4, THREADS = 64 + 32 * NEPI;   // epilogue warps
     static constexpr uint32_t TMEM = 2 * BN;                                 // two accumulators
     static constexpr size_t SMEM = (size_t)STAGES * STAGE + NEPI * kStaging + kTable * 48 + 256 + 1024;
@@ -422,23 +424,29 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                     const CUtensorMap *map_a = maps + l.a_map, *map_b = maps + l.b_map;
                     if (PHASE == kPoly && term > 0) { map_a = maps + (term == 2 ? kGramLoMap : kGramMap); map_b = maps + (term == 1 ? kFactorLoMap : kFactorMap); }
                     if (PHASE >= kApply && term > 0) { if (l.a_map == kPolyMap) map_a = maps + kPolyLoMap; else map_b = maps + kPolyLoMap; }
-                    for (int st = first > 0 ? first : l.k0; st < first + per; ++st, ++c) {
+                    for (int st = first > 0 ? first : l.k0; st < first + per; st += S::PER_STAGE, ++c) {
                         if (!mbar_poll(empty + s, phase, abort_flag)) { failed = true; break; }
                         unsigned char *dst = smem + s * S::STAGE;
                         uint64_t *here = full + s;
                         if (++s == S::STAGES) { s = 0; phase ^= 1; }
                         if (prm.test_drop && blockIdx.x == 0 && c == 0) continue;   // test hook: this stage never arrives
-                        if (rank == 0) mbar_arrive_expect_tx(here, CG * S::STAGE);
-                        const int k = (st - first) * KS;
+                        const int blocks = min(S::PER_STAGE, first + per - st);
+                        if (rank == 0) mbar_arrive_expect_tx(here, CG * S::BYTES * blocks);
                         const uint32_t bar = CG == 2 ? in_leader(here) : 0;
-                        auto load = [&](unsigned char *to, const CUtensorMap *map, bool mn, int at) {
-                            if (CG == 2) tma_load_2d_pair(to, map, mn ? at : k, mn ? k : at, bar);
-                            else tma_load_2d(to, map, mn ? at : k, mn ? k : at, here);
-                        };
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) load(dst + i * BOX, map_a, l.a_mn || k < a_left, m0 + 64 * i);
+                        for (int j = 0; j < S::PER_STAGE; ++j) {
+                            if (j >= blocks) break;
+                            const int k = (st + j - first) * KS;
+                            auto load = [&](unsigned char *to, const CUtensorMap *map, bool mn, int at) {
+                                if (CG == 2) tma_load_2d_pair(to, map, mn ? at : k, mn ? k : at, bar);
+                                else tma_load_2d(to, map, mn ? at : k, mn ? k : at, here);
+                            };
 #pragma unroll
-                        for (int i = 0; i < S::NB; ++i) load(dst + S::A_BYTES + i * BOX, map_b, l.b_mn || k < b_left, n0 + 64 * i);
+                            for (int i = 0; i < 2; ++i) load(dst + j * S::BYTES + i * BOX, map_a, l.a_mn || k < a_left, m0 + 64 * i);
+#pragma unroll
+                            for (int i = 0; i < S::NB; ++i)
+                                load(dst + j * S::BYTES + S::A_BYTES + i * BOX, map_b, l.b_mn || k < b_left, n0 + 64 * i);
+                        }
                     }
                 }
                 l = next;
@@ -463,22 +471,27 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                 tc_fence_after();
                 const int per = stages_of_a_product<PHASE>(w);
                 for (int first = 0; first < w.k1 && !failed; first += per) {
-                    for (int st = first > 0 ? first : w.k0; st < first + per; ++st) {
+                    for (int st = first > 0 ? first : w.k0; st < first + per; st += S::PER_STAGE) {
                         if (!mbar_poll(full + s, phase, abort_flag)) { failed = true; break; }
                         tc_fence_after();
-                        const uint32_t base = base0 + s * S::STAGE;
-                        const bool a_mn = w.a_mn || (st - first) * KS < a_left, b_mn = w.b_mn || (st - first) * KS < b_left;
-                        const uint32_t idesc = make_idesc_f16(128 * CG, n, a_mn, b_mn);
-                        const uint64_t da = a_mn ? make_mn_desc(base, BOX) : make_b_desc(base);
-                        const uint64_t db = b_mn ? make_mn_desc(base + S::A_BYTES, BOX) : make_b_desc(base + S::A_BYTES);
-                        // 16 steps of the contraction: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major box
-                        const uint32_t ia = a_mn ? 16 * 128 / 16 : 2, ib = b_mn ? 16 * 128 / 16 : 2;
-                        const int n_mma = min(4, (w.K - (st - first) * KS + 15) / 16);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (k < n_mma) tc_mma_f16<CG>(d, da + k * ia, db + k * ib, idesc, st > w.k0 || k > 0);
+                        for (int j = 0; j < S::PER_STAGE; ++j) {
+                            const int k0 = (st + j - first) * KS;
+                            if (j > 0 && st + j >= first + per) break;
+                            const uint32_t base = base0 + s * S::STAGE + j * S::BYTES;
+                            const bool a_mn = w.a_mn || k0 < a_left, b_mn = w.b_mn || k0 < b_left;
+                            const uint32_t idesc = make_idesc_f16(128 * CG, n, a_mn, b_mn);
+                            const uint64_t da = a_mn ? make_mn_desc(base, BOX) : make_b_desc(base);
+                            const uint64_t db = b_mn ? make_mn_desc(base + S::A_BYTES, BOX) : make_b_desc(base + S::A_BYTES);
+                            // 16 steps of the contraction: 32 bytes of a K-major row, 16 rows of 128 bytes of an MN-major box
+                            const uint32_t ia = a_mn ? 16 * 128 / 16 : 2, ib = b_mn ? 16 * 128 / 16 : 2;
+                            const int n_mma = min(4, (w.K - k0 + 15) / 16);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                if (k < n_mma) tc_mma_f16<CG>(d, da + k * ia, db + k * ib, idesc, st + j > w.k0 || k > 0);
+                        }
                         if (CG == 2) tc_commit_pair(empty + s); else tc_commit(empty + s);
-                        if (st == w.k1 - 1) { if (CG == 2) tc_commit_pair(d_full + buf); else tc_commit(d_full + buf); }
+                        if (first + per >= w.k1 && st + S::PER_STAGE >= w.k1) { if (CG == 2) tc_commit_pair(d_full + buf); else tc_commit(d_full + buf); }
                         if (++s == S::STAGES) { s = 0; phase ^= 1; }
                     }
                 }
