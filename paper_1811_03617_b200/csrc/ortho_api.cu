@@ -27,9 +27,10 @@ constexpr size_t kAlign = 256;
 constexpr int kPartStages = 6, kMaxParts = 4;
 constexpr int kTileCost = 3;      // what a tile costs beyond its contraction, in stages of 64 steps
 // Pairs of CTAs on 256 x 256 tiles from this many multiply-adds of one X P on, 128 x 64 tiles below.  Measured on either side,
-// us per call: 1280 x 1280 (2.1e9) 201 / 176, twice 512 x 4608 (2.4e9) 195 / 178, three times (3.6e9) 223 / 222, 1500 x 1500
-// (3.4e9) 285 / 238, four 1024 x 1024 (4.3e9) 252 / 227, 1700 x 1700 (4.9e9) 307 / 315, 2048 x 2048 (8.6e9) 276 / 385.
-constexpr int64_t kPairWork = 4'600'000'000;
+// us per call in pairs / alone: 1500 x 1500 (3.4e9) 285 / 215, four 512 x 4608 (4.8e9) 242 / 249, 1700 x 1700 (4.9e9) 306 / 283,
+// five 1024 x 1024 (5.4e9) 295 / 252, 1850 x 1850 (6.3e9) 267 / 275, six 1024 x 1024 (6.4e9) 305 / 274, six 512 x 4608 (7.2e9)
+// 295 / 315, eight 1024 x 1024 (8.6e9) 306 / 334, 2048 x 2048 (8.6e9) 279 / 317.
+constexpr int64_t kPairWork = 6'800'000'000;
 size_t up(size_t n) { return (n + kAlign - 1) & ~(kAlign - 1); }
 int up32(int n) { return (n + 31) & ~31; }     // rows of the work arrays: whole pieces of 32 entries
 

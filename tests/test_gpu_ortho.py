@@ -406,6 +406,11 @@ def test_a_wait_that_runs_out_is_reported_and_the_plan_recovers(shape):
     assert torch.equal(out[:n], good)
 
 
+def test_a_wait_of_a_pair_that_runs_out_is_reported_and_the_plan_recovers():
+    """The same with tiles of CTA pairs."""
+    test_a_wait_that_runs_out_is_reported_and_the_plan_recovers((2000, 2000))
+
+
 def test_a_cluster_whose_wait_runs_out_is_reported_and_the_plan_recovers():
     from paper_1811_03617_b200 import gvq
     shape = (64, 1500)
