@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(256) normalise_kernel(const StartParams prm)
 }
 
 // ---- the products ------------------------------------------------------------------------------------
-// Persistent CTAs (or pairs of CTAs), 64 steps of the contraction a stage.  Every operand comes in boxes of 64 x 64 entries
+// Persistent CTAs (or pairs of CTAs), 64 steps of the contraction a stage (a CTA alone: 128).  Every operand comes in boxes of 64 x 64 entries
 // (8 KB, 128-byte swizzle, zero fill outside), the same tensor map for either major:
 //   K-major   box = 64 steps x 64 rows     MN-major   box = 64 entries across x 64 steps
 //   warp 0      producer      warp 1  MMA      then the epilogue's warps (lane quarter warp % 4; a pair's CTA has eight, half

@@ -22,8 +22,8 @@ struct gvq_ortho {
 namespace {
 
 constexpr size_t kAlign = 256;
-// A part of a contraction: at least so many stages, at most so many parts.  (6, 4), (6, 8), (12, 4), (9, 3) in us: 515 x 1027
-// 109.6, 109.4, 112.4, 112.7; twice 512 x 4608 139, 153, 139, 147; the VGG-16-shaped weights 348, 349, 348, 353.
+// A part of a contraction: at least so many stages, at most so many parts.  Against (6, 4), time with (6, 8), (12, 4), (9, 3):
+// 515 x 1027 +0, +3, +3 %; twice 512 x 4608 +10, +0, +6 %; the VGG-16-shaped weights +0, +0, +1 %.
 constexpr int kPartStages = 6, kMaxParts = 4;
 constexpr int kTileCost = 3;      // what a tile costs beyond its contraction, in stages of 64 steps
 // Pairs of CTAs on 256 x 256 tiles from this many multiply-adds of one X P on, 128 x 64 tiles below.  Measured on either side,
