@@ -521,6 +521,29 @@ class Context:
             raise GvqError(status, "gvq_mx4_matmul")
         return out
 
+    def _flat(self, t: torch.Tensor, what: str):
+        if not t.is_cuda or not t.is_contiguous() or t.numel() < self.M:
+            raise ValueError(f"{what}: a contiguous CUDA tensor of {self.M} entries is wanted")
+        return t.data_ptr()
+
+    def _flat_fp32(self, t: torch.Tensor, what: str):
+        if t.dtype != torch.float32:
+            raise TypeError(f"{what}: float32 is wanted, not {t.dtype}")
+        return self._flat(t, what)
+
+    def _flats(self, tensors, what: str):
+        return (ctypes.c_void_p * len(tensors))(*[self._flat_fp32(t, what) for t in tensors])
+
+    def _slices(self, q_nodes: Sequence[Mx4], n: int, what: str):
+        """(codes, scales) of one [S][d] matrix per node, as host arrays."""
+        if len(q_nodes) != n:
+            raise ValueError(f"{what}: one 4-bit matrix per node is wanted ({n}), not {len(q_nodes)}")
+        for q in q_nodes:
+            if q.rows != self.S or q.cols != self.d:
+                raise ValueError(f"{what}: a node's slices are {self.S} x {self.d}, not {q.rows} x {q.cols}")
+        vpn = ctypes.c_void_p * n
+        return vpn(*[q.codes_ptr for q in q_nodes]), vpn(*[q.scales_ptr for q in q_nodes])
+
     def mx4_slices(self) -> Mx4:
         """Room for one node's quantized slices, a matrix [S][d]."""
         return Mx4(self.S, self.d, device=f"cuda:{self.device}")
@@ -528,20 +551,24 @@ class Context:
     def mx4_quantize_aggregate(self, g_nodes, g_sum, stochastic=True, seed=0, node0=0,
                                out: Optional[Sequence[Mx4]] = None):
         """gvq_mx4_quantize_aggregate; out: one mx4_slices() per node that receives what it would send."""
+        what = "gvq_mx4_quantize_aggregate"
+        n = len(g_nodes)
+        cp, sp = self._slices(out, n, what) if out is not None else (None, None)
+        gp, total = self._flats(g_nodes, what), self._flat_fp32(g_sum, what) if g_sum is not None else None
         self._sync_stream()
-        cp = (ctypes.c_void_p * len(out))(*[q.codes_ptr for q in out]) if out is not None else None
-        sp = (ctypes.c_void_p * len(out))(*[q.scales_ptr for q in out]) if out is not None else None
-        _check(lib().gvq_mx4_quantize_aggregate(self._h, _ptr_array(g_nodes), len(g_nodes), node0, 1 if stochastic else 0,
-                                                seed, g_sum.data_ptr() if g_sum is not None else None, cp, sp),
-               "gvq_mx4_quantize_aggregate")
+        _check(lib().gvq_mx4_quantize_aggregate(self._h, gp, n, node0, 1 if stochastic else 0, seed, total, cp, sp), what)
 
     def mx4_dequantize_aggregate(self, q_nodes: Sequence[Mx4], g_nodes_for_tails, g_sum):
+        """gvq_mx4_dequantize_aggregate; g_nodes_for_tails: the same nodes' gradients, or None for a layout without tails."""
+        what = "gvq_mx4_dequantize_aggregate"
+        n = len(q_nodes)
+        cp, sp = self._slices(q_nodes, n, what)
+        if g_nodes_for_tails is not None and len(g_nodes_for_tails) != n:
+            raise ValueError(f"{what}: one gradient per node is wanted ({n}), not {len(g_nodes_for_tails)}")
+        gp = self._flats(g_nodes_for_tails, what) if g_nodes_for_tails is not None else None
+        total = self._flat_fp32(g_sum, what)
         self._sync_stream()
-        gp = _ptr_array(g_nodes_for_tails) if g_nodes_for_tails is not None else None
-        cp = (ctypes.c_void_p * len(q_nodes))(*[q.codes_ptr for q in q_nodes])
-        sp = (ctypes.c_void_p * len(q_nodes))(*[q.scales_ptr for q in q_nodes])
-        _check(lib().gvq_mx4_dequantize_aggregate(self._h, cp, sp, gp, len(q_nodes), g_sum.data_ptr()),
-               "gvq_mx4_dequantize_aggregate")
+        _check(lib().gvq_mx4_dequantize_aggregate(self._h, cp, sp, gp, n, total), what)
 
     def flatten_layer(self, framework, flat, F, D, X):
         self._sync_stream()
@@ -711,23 +738,14 @@ class OrthoPlan:
         except Exception:
             pass
 
-    def _flat(self, t: torch.Tensor, what: str):
-        if not t.is_cuda or not t.is_contiguous() or t.numel() < self.ctx.M:
-            raise ValueError(f"{what}: a contiguous CUDA tensor of {self.ctx.M} entries is wanted")
-        return t.data_ptr()
-
-    def _fp32(self, t: torch.Tensor, what: str):
-        if t.dtype != torch.float32:
-            raise TypeError(f"{what}: float32 is wanted, not {t.dtype}")
-        return self._flat(t, what)
-
     def step(self, g, momentum, w, lr: float, weight_decay: float = 0.0, beta: float = 0.95, nesterov: bool = True):
         """gvq_ortho_step on flat buffers: momentum and w are updated in place."""
         self.ctx._sync_stream()
-        _check(lib().gvq_ortho_step(self._h, self._fp32(g, "g"), self._fp32(momentum, "momentum"), beta, 1 if nesterov else 0,
-                                    self._flat(w, "w"), _dtype(w), lr, weight_decay), "gvq_ortho_step")
+        _check(lib().gvq_ortho_step(self._h, self.ctx._flat_fp32(g, "g"), self.ctx._flat_fp32(momentum, "momentum"), beta,
+                                    1 if nesterov else 0, self.ctx._flat(w, "w"), _dtype(w), lr, weight_decay), "gvq_ortho_step")
 
     def orthogonalize(self, g, out):
         """gvq_orthogonalize: the plan's matrices of the flat buffer g, orthogonalised, into `out`."""
         self.ctx._sync_stream()
-        _check(lib().gvq_orthogonalize(self._h, self._fp32(g, "g"), self._flat(out, "out"), _dtype(out)), "gvq_orthogonalize")
+        _check(lib().gvq_orthogonalize(self._h, self.ctx._flat_fp32(g, "g"), self.ctx._flat(out, "out"), _dtype(out)),
+               "gvq_orthogonalize")

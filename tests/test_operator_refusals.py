@@ -1,0 +1,102 @@
+"""What the binding of the 4-bit exchange and of the orthogonalised update refuses before anything reaches the library.
+Host only: the library is a stand-in that counts calls, and no pointer is followed."""
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+
+class Library:
+    """Counts the calls of every entry point; all succeed."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, args))
+            return 0
+        return call
+
+    def names(self):
+        return [n for n, _ in self.calls if n != "gvq_set_stream"]
+
+
+class Device(SimpleNamespace):
+    """A CUDA tensor as far as the binding looks at one."""
+
+    def __init__(self, numel, dtype=torch.float32, contiguous=True, cuda=True):
+        super().__init__(dtype=dtype, is_cuda=cuda)
+        self._n, self._c = numel, contiguous
+
+    def numel(self):
+        return self._n
+
+    def is_contiguous(self):
+        return self._c
+
+    def data_ptr(self):
+        return 4096
+
+    def get_device(self):
+        return 0 if self.is_cuda else -1
+
+
+def matrix(rows, cols):
+    return SimpleNamespace(rows=rows, cols=cols, codes_ptr=256, scales_ptr=512, device=0)
+
+
+@pytest.fixture
+def made(monkeypatch):
+    """(context of 100 slices of 16 and a tail of 8, stand-in library)"""
+    from paper_1811_03617_b200 import gvq
+    ctx = object.__new__(gvq.Context)
+    ctx._h, ctx.device, ctx.S, ctx.d, ctx.M, ctx.n_layers = 1, 0, 100, 16, 1608, 1
+    ctx._stream_now = 0
+    ctx._raw_stream = lambda: 0
+    fake = Library()
+    monkeypatch.setattr(gvq, "lib", lambda: fake)
+    yield ctx, fake
+    ctx._h = None        # nothing to destroy
+
+
+def test_exchange_takes_one_matrix_of_slices_per_node(made):
+    ctx, fake = made
+    g = [Device(1608) for _ in range(3)]
+    total, q = Device(1608), [matrix(100, 16) for _ in range(3)]
+    ctx.mx4_quantize_aggregate(g, total, out=q)
+    ctx.mx4_quantize_aggregate(g, None, out=q)
+    ctx.mx4_quantize_aggregate(g, total)
+    assert fake.names() == ["gvq_mx4_quantize_aggregate"] * 3
+    for bad in (q[:2], q + q[:1], [], q[:2] + [matrix(99, 16)], q[:2] + [matrix(100, 8)], [matrix(16, 100)] * 3):
+        with pytest.raises(ValueError):
+            ctx.mx4_quantize_aggregate(g, total, out=bad)
+    assert len(fake.names()) == 3
+
+
+def test_exchange_takes_flat_float32_gradients(made):
+    ctx, fake = made
+    good = Device(1608)
+    for bad, error in ((Device(1607), ValueError), (Device(1608, contiguous=False), ValueError),
+                       (Device(1608, cuda=False), ValueError), (Device(1608, torch.bfloat16), TypeError)):
+        with pytest.raises(error):
+            ctx.mx4_quantize_aggregate([good, bad], good)
+        with pytest.raises(error):
+            ctx.mx4_quantize_aggregate([good, good], bad)
+        with pytest.raises(error):
+            ctx.mx4_dequantize_aggregate([matrix(100, 16)] * 2, [good, bad], good)
+        with pytest.raises(error):
+            ctx.mx4_dequantize_aggregate([matrix(100, 16)] * 2, [good, good], bad)
+    assert fake.names() == []
+
+
+def test_receiver_takes_the_slices_and_the_gradients_of_the_same_nodes(made):
+    ctx, fake = made
+    g, total, q = [Device(1608)] * 2, Device(1608), [matrix(100, 16)] * 2
+    ctx.mx4_dequantize_aggregate(q, g, total)
+    ctx.mx4_dequantize_aggregate(q, None, total)
+    assert fake.names() == ["gvq_mx4_dequantize_aggregate"] * 2
+    for bad_q, bad_g in ((q[:1], g), (q + q, g), (q, g[:1]), (q, g + g), ([matrix(100, 16), matrix(50, 32)], g), ([matrix(101, 16)] * 2, g)):
+        with pytest.raises(ValueError):
+            ctx.mx4_dequantize_aggregate(bad_q, bad_g, total)
+    assert len(fake.names()) == 2
