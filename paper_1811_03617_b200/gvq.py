@@ -738,14 +738,20 @@ class OrthoPlan:
         except Exception:
             pass
 
+    def _ready(self, what: str):
+        """The plan's calls use its context, which may have been closed before it: the library cannot tell."""
+        if not self._h or not self.ctx._h:
+            raise GvqError(1, what)
+        self.ctx._sync_stream()
+
     def step(self, g, momentum, w, lr: float, weight_decay: float = 0.0, beta: float = 0.95, nesterov: bool = True):
         """gvq_ortho_step on flat buffers: momentum and w are updated in place."""
-        self.ctx._sync_stream()
+        self._ready("gvq_ortho_step")
         _check(lib().gvq_ortho_step(self._h, self.ctx._flat_fp32(g, "g"), self.ctx._flat_fp32(momentum, "momentum"), beta,
                                     1 if nesterov else 0, self.ctx._flat(w, "w"), _dtype(w), lr, weight_decay), "gvq_ortho_step")
 
     def orthogonalize(self, g, out):
         """gvq_orthogonalize: the plan's matrices of the flat buffer g, orthogonalised, into `out`."""
-        self.ctx._sync_stream()
+        self._ready("gvq_orthogonalize")
         _check(lib().gvq_orthogonalize(self._h, self.ctx._flat_fp32(g, "g"), self.ctx._flat(out, "out"), _dtype(out)),
                "gvq_orthogonalize")

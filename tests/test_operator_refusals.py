@@ -12,6 +12,9 @@ class Library:
     def __init__(self):
         self.calls = []
 
+    def gvq_status_string(self, status):
+        return b"refused"
+
     def __getattr__(self, name):
         def call(*args):
             self.calls.append((name, args))
@@ -100,3 +103,22 @@ def test_receiver_takes_the_slices_and_the_gradients_of_the_same_nodes(made):
         with pytest.raises(ValueError):
             ctx.mx4_dequantize_aggregate(bad_q, bad_g, total)
     assert len(fake.names()) == 2
+
+
+@pytest.mark.parametrize("closed", ["context", "plan"])
+def test_a_plan_is_not_used_after_its_context_or_itself_was_closed(made, closed):
+    from paper_1811_03617_b200 import gvq
+    ctx, fake = made
+    plan = object.__new__(gvq.OrthoPlan)
+    plan.ctx, plan._h = ctx, 2
+    g, mo, w = Device(1608), Device(1608), Device(1608)
+    plan.step(g, mo, w, lr=0.1)
+    plan.orthogonalize(g, w)
+    assert fake.names() == ["gvq_ortho_step", "gvq_orthogonalize"]
+    (ctx if closed == "context" else plan).close()
+    for call in (lambda: plan.step(g, mo, w, lr=0.1), lambda: plan.orthogonalize(g, w)):
+        with pytest.raises(gvq.GvqError) as e:
+            call()
+        assert e.value.status == 1
+    assert not [n for n in fake.names()[2:] if n in ("gvq_ortho_step", "gvq_orthogonalize")]
+    plan._h = None
