@@ -355,7 +355,6 @@ class Context:
         self.M = self.layout.total_entries()
         self.n_layers = len(self.layout.layer_len)
         self._ws = None
-        self._stream_now = self._raw_stream()
 
     def _stream(self):
         return ctypes.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
@@ -366,11 +365,11 @@ class Context:
         return torch.cuda.current_stream(self.device).cuda_stream
 
     def _sync_stream(self):
-        """Hands the current stream over; only when it is another than at the last call."""
-        now = self._raw_stream()
-        if now != self._stream_now:
-            _check(lib().gvq_set_stream(self._h, now), "gvq_set_stream")
-            self._stream_now = now
+        """Hands the current stream over.  The library knows which one it has; a copy of that kept here would go stale when
+        somebody else sets it."""
+        status = lib().gvq_set_stream(self._h, self._raw_stream())
+        if status:
+            raise GvqError(status, "gvq_set_stream")
 
     def close(self):
         if self._h:

@@ -55,7 +55,6 @@ def made(monkeypatch):
     from paper_1811_03617_b200 import gvq
     ctx = object.__new__(gvq.Context)
     ctx._h, ctx.device, ctx.S, ctx.d, ctx.M, ctx.n_layers = 1, 0, 100, 16, 1608, 1
-    ctx._stream_now = 0
     ctx._raw_stream = lambda: 0
     fake = Library()
     monkeypatch.setattr(gvq, "lib", lambda: fake)
@@ -122,3 +121,19 @@ def test_a_plan_is_not_used_after_its_context_or_itself_was_closed(made, closed)
         assert e.value.status == 1
     assert not [n for n in fake.names()[2:] if n in ("gvq_ortho_step", "gvq_orthogonalize")]
     plan._h = None
+
+
+def test_a_stream_that_somebody_else_set_does_not_stay(made):
+    """gvq_set_stream is public: a call made through the binding goes to torch's current stream all the same."""
+    from paper_1811_03617_b200 import gvq
+    ctx, fake = made
+
+    def stream_of_the_library():
+        return [args[1] for name, args in fake.calls if name == "gvq_set_stream"][-1]
+    ctx.mx4_quantize_aggregate([Device(1608)], Device(1608))
+    gvq.lib().gvq_set_stream(ctx._h, 77)
+    ctx.mx4_quantize_aggregate([Device(1608)], Device(1608))
+    assert stream_of_the_library() == 0
+    ctx._raw_stream = lambda: 5
+    ctx.mx4_quantize_aggregate([Device(1608)], Device(1608))
+    assert stream_of_the_library() == 5
