@@ -34,6 +34,20 @@ gvq_status gather_nodes(const T *const *src, int N, NodePtrs<const T> &dst, bool
     return GVQ_OK;
 }
 
+// The tables of a context or a plan, from pageable memory, and zeroed counters: on the device when the call returns.  cudaMemcpy
+// alone promises that the source has been read and cudaMemset nothing, and a stream that does not wait for the default one (every
+// side stream of torch) would not be ordered behind either.
+inline cudaError_t upload(void *dst, const void *src, size_t bytes)
+{
+    const cudaError_t e = cudaMemcpy(dst, src, bytes, cudaMemcpyHostToDevice);
+    return e != cudaSuccess ? e : cudaStreamSynchronize(cudaStreamLegacy);
+}
+inline cudaError_t clear(void *dst, size_t bytes)
+{
+    const cudaError_t e = cudaMemset(dst, 0, bytes);
+    return e != cudaSuccess ? e : cudaStreamSynchronize(cudaStreamLegacy);
+}
+
 // Makes the context's device current, and the caller's again at the end; nothing to do where it is already.
 struct DeviceGuard {
     int prev = -1;

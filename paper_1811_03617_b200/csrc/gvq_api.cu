@@ -457,7 +457,7 @@ gvq_status gvq_create(gvq_ctx **out, const gvq_layout *layout, int device, void 
         o_t[i][2] = put(hts[i]->first.data(), hts[i]->first.size() * 4);
     }
     e = cudaMalloc(&ctx->table_block, image.size());
-    if (e == cudaSuccess) e = cudaMemcpy(ctx->table_block, image.data(), image.size(), cudaMemcpyHostToDevice);
+    if (e == cudaSuccess) e = upload(ctx->table_block, image.data(), image.size());
     if (e != cudaSuccess) {
         if (ctx->table_block) cudaFree(ctx->table_block);
         delete ctx;
@@ -490,7 +490,7 @@ gvq_status gvq_create(gvq_ctx **out, const gvq_layout *layout, int device, void 
             if (e == cudaSuccess) {
                 ctx->tc_partial = (float *)((char *)ctx->tmaps_dev + map_bytes);
                 ctx->tc_tile_counter = (int32_t *)((char *)ctx->tmaps_dev + map_bytes + part_bytes);
-                e = cudaMemset(ctx->tc_tile_counter, 0, cnt_bytes);
+                e = clear(ctx->tc_tile_counter, cnt_bytes);
             }
             if (e != cudaSuccess) {
                 cudaFree(ctx->table_block);

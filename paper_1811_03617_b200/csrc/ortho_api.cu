@@ -253,7 +253,7 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
         const size_t o_p = up(image.size()), o_q = o_p + up(sizeof(float) * chunks.size()), all = o_q + (size_t)slots * 8192;
         DeviceGuard guard(ctx->device);
         cudaError_t e = cudaMalloc(&p->tables, all + kAlign);
-        if (e == cudaSuccess) e = cudaMemcpy(p->tables, image.data(), image.size(), cudaMemcpyHostToDevice);
+        if (e == cudaSuccess) e = upload(p->tables, image.data(), image.size());
         if (e != cudaSuccess) {
             if (p->tables) cudaFree(p->tables);
             delete p;

@@ -23,3 +23,24 @@ def test_a_plan_whose_context_is_closed_refuses_its_calls():
         plan.orthogonalize(g, w)
     with pytest.raises(gvq.GvqError):
         gvq.OrthoPlan(ctx, [64, 120], [64, 400])
+
+
+@pytest.mark.parametrize("shapes", [[(64, 576)] * 6, [(300, 400), (129, 1000)], [(1024, 1024)] * 7])
+def test_a_plan_made_on_a_side_stream_is_ready_for_it_at_once(shapes):
+    """Tables are on the device when the calls that make them return: a side stream does not wait for the default one."""
+    from paper_1811_03617_b200 import gvq
+    lens = [m * n for m, n in shapes]
+    off = [sum(lens[:i]) for i in range(len(lens))]
+    g = torch.randn(sum(lens), device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            ctx = gvq.Context(gvq.HostLayout(64, 4, off, lens))
+            plan = gvq.OrthoPlan(ctx, [m for m, _ in shapes], [n for _, n in shapes])
+            first = torch.empty(ctx.M, device="cuda")
+            plan.orthogonalize(g, first)
+            torch.cuda.synchronize()
+            later = torch.empty(ctx.M, device="cuda")
+            plan.orthogonalize(g, later)
+            ctx.device_status()
+        assert torch.equal(first, later)
