@@ -267,6 +267,7 @@ class Schedule:
 # the handle alone, without a Stream object around it (a tenth of the time), where this torch has it
 _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
+_F32 = torch.float32
 DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
@@ -277,11 +278,11 @@ def _dtype(t: torch.Tensor) -> int:
     return d
 
 
-def _rows(t: torch.Tensor, what: str):
-    """(rows, cols, leading dimension) of a 2-D tensor whose rows are contiguous."""
+def _rows(t: torch.Tensor, device: int, what: str):
+    """(rows, cols, leading dimension) of a 2-D tensor on that CUDA device whose rows are contiguous."""
     shape = t.shape
-    if len(shape) != 2 or not t.is_cuda:
-        raise ValueError(f"{what}: a 2-D CUDA tensor is wanted")
+    if len(shape) != 2 or t.get_device() != device:
+        raise ValueError(f"{what}: a 2-D tensor on cuda:{device} is wanted")
     rows, cols = shape
     ld, step = t.stride()
     if cols > 1 and step != 1:
@@ -292,7 +293,7 @@ def _rows(t: torch.Tensor, what: str):
 class Mx4:
     """A matrix [rows][cols] in microscaled 4-bit floating point: device bytes `codes` and `scales` (see gvq.h)."""
 
-    __slots__ = ("rows", "cols", "_codes", "_scales", "_buf", "codes_ptr", "scales_ptr")
+    __slots__ = ("rows", "cols", "device", "_codes", "_scales", "_buf", "codes_ptr", "scales_ptr")
 
     def __init__(self, rows: int, cols: int, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
                  device=None):
@@ -306,6 +307,7 @@ class Mx4:
             at = (rows * nb * 16 + 255) & ~255
             self._buf = buf = torch.empty(at + tiles * 512, dtype=torch.uint8, device=device or "cuda")
             self._codes = None
+            self.device = buf.get_device()
             self.codes_ptr = p = buf.data_ptr()
             self.scales_ptr = p + at
             return
@@ -315,6 +317,9 @@ class Mx4:
         for t, n in ((codes, nc), (scales, ns)):
             if t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous() or t.numel() < n:
                 raise ValueError(f"a 4-bit matrix of {rows} x {cols} has {nc} bytes of codes and {ns} of scales, contiguous")
+        self.device = codes.get_device()
+        if scales.get_device() != self.device:
+            raise ValueError("codes and scales are on one device")
         self._codes, self._scales = codes, scales
         self.codes_ptr, self.scales_ptr = codes.data_ptr(), scales.data_ptr()
 
@@ -461,20 +466,20 @@ class Context:
 
     # ---- microscaled 4-bit floating point ---------------------------------------------------
     def _mx4(self, x, by_rows, by_cols, stochastic, seed, node, out=None, out_t=None):
-        rows, cols, ld = _rows(x, "mx4_quantize")
+        rows, cols, ld = _rows(x, self.device, "mx4_quantize")
         dtype = _dtype(x)
         c = s = ct = st = None
         if by_rows:
             if out is None:
                 out = Mx4(rows, cols, device=x.device)
-            elif out.rows != rows or out.cols != cols:
-                raise ValueError("mx4_quantize: the output is of another size")
+            elif out.rows != rows or out.cols != cols or out.device != self.device:
+                raise ValueError("mx4_quantize: the output is of another size or on another device")
             c, s = out.codes_ptr, out.scales_ptr
         if by_cols:
             if out_t is None:
                 out_t = Mx4(cols, rows, device=x.device)
-            elif out_t.rows != cols or out_t.cols != rows:
-                raise ValueError("mx4_quantize: the output is of another size")
+            elif out_t.rows != cols or out_t.cols != rows or out_t.device != self.device:
+                raise ValueError("mx4_quantize: the output is of another size or on another device")
             ct, st = out_t.codes_ptr, out_t.scales_ptr
         self._sync_stream()
         status = lib().gvq_mx4_quantize(self._h, x.data_ptr(), dtype, rows, cols, ld, 1 if stochastic else 0, seed, node, c, s,
@@ -500,9 +505,9 @@ class Context:
         """gvq_mx4_dequantize: what q stands for, float32 [rows, cols]."""
         if out is None:
             out = torch.empty((q.rows, q.cols), device=f"cuda:{self.device}")
-        rows, cols, ld = _rows(out, "mx4_dequantize")
-        if (rows, cols) != (q.rows, q.cols) or out.dtype != torch.float32:
-            raise ValueError("mx4_dequantize: a float32 output of the matrix's size is wanted")
+        rows, cols, ld = _rows(out, self.device, "mx4_dequantize")
+        if (rows, cols) != (q.rows, q.cols) or out.dtype != torch.float32 or q.device != self.device:
+            raise ValueError("mx4_dequantize: a float32 output of the matrix's size, on its device, is wanted")
         self._sync_stream()
         _check(lib().gvq_mx4_dequantize(self._h, q.codes_ptr, q.scales_ptr, rows, cols, out.data_ptr(), ld),
                "gvq_mx4_dequantize")
@@ -510,9 +515,11 @@ class Context:
 
     def mx4_matmul(self, a: Mx4, b: Mx4, out: torch.Tensor) -> torch.Tensor:
         """gvq_mx4_matmul: out [a.rows, b.rows] = a b^T; out is float32, bfloat16 or float16."""
-        rows, cols, ld = _rows(out, "mx4_matmul")
+        rows, cols, ld = _rows(out, self.device, "mx4_matmul")
         if a.cols != b.cols or (rows, cols) != (a.rows, b.rows):
             raise ValueError(f"mx4_matmul: [{a.rows}, {a.cols}] x [{b.rows}, {b.cols}]^T does not give [{rows}, {cols}]")
+        if a.device != self.device or b.device != self.device:
+            raise ValueError(f"mx4_matmul: operands on cuda:{a.device} and cuda:{b.device}, the context on cuda:{self.device}")
         self._sync_stream()
         status = lib().gvq_mx4_matmul(self._h, a.codes_ptr, a.scales_ptr, b.codes_ptr, b.scales_ptr, rows, cols, a.cols,
                                       out.data_ptr(), _dtype(out), ld)
@@ -521,25 +528,30 @@ class Context:
         return out
 
     def _flat(self, t: torch.Tensor, what: str):
-        if not t.is_cuda or not t.is_contiguous() or t.numel() < self.M:
-            raise ValueError(f"{what}: a contiguous CUDA tensor of {self.M} entries is wanted")
+        if t.get_device() != self.device or not t.is_contiguous() or t.numel() < self.M:
+            raise ValueError(f"{what}: a contiguous tensor of {self.M} entries on cuda:{self.device} is wanted")
         return t.data_ptr()
 
     def _flat_fp32(self, t: torch.Tensor, what: str):
-        if t.dtype != torch.float32:
+        if t.dtype is not _F32:
             raise TypeError(f"{what}: float32 is wanted, not {t.dtype}")
         return self._flat(t, what)
 
     def _flats(self, tensors, what: str):
-        return (ctypes.c_void_p * len(tensors))(*[self._flat_fp32(t, what) for t in tensors])
+        M, device = self.M, self.device
+        for t in tensors:
+            if t.dtype is not _F32 or t.get_device() != device or t.numel() < M or not t.is_contiguous():
+                self._flat_fp32(t, what)
+        return _ptr_array(tensors)
 
     def _slices(self, q_nodes: Sequence[Mx4], n: int, what: str):
         """(codes, scales) of one [S][d] matrix per node, as host arrays."""
         if len(q_nodes) != n:
             raise ValueError(f"{what}: one 4-bit matrix per node is wanted ({n}), not {len(q_nodes)}")
         for q in q_nodes:
-            if q.rows != self.S or q.cols != self.d:
-                raise ValueError(f"{what}: a node's slices are {self.S} x {self.d}, not {q.rows} x {q.cols}")
+            if q.rows != self.S or q.cols != self.d or q.device != self.device:
+                raise ValueError(f"{what}: a node's slices are {self.S} x {self.d} on cuda:{self.device}, "
+                                 f"not {q.rows} x {q.cols} on cuda:{q.device}")
         vpn = ctypes.c_void_p * n
         return vpn(*[q.codes_ptr for q in q_nodes]), vpn(*[q.scales_ptr for q in q_nodes])
 

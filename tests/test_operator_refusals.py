@@ -28,9 +28,9 @@ class Library:
 class Device(SimpleNamespace):
     """A CUDA tensor as far as the binding looks at one."""
 
-    def __init__(self, numel, dtype=torch.float32, contiguous=True, cuda=True):
-        super().__init__(dtype=dtype, is_cuda=cuda)
-        self._n, self._c = numel, contiguous
+    def __init__(self, numel, dtype=torch.float32, contiguous=True, cuda=True, device=0, shape=None):
+        super().__init__(dtype=dtype, is_cuda=cuda, shape=shape or (numel,), device=f"cuda:{device}")
+        self._n, self._c, self._device = numel, contiguous, device
 
     def numel(self):
         return self._n
@@ -42,11 +42,14 @@ class Device(SimpleNamespace):
         return 4096
 
     def get_device(self):
-        return 0 if self.is_cuda else -1
+        return self._device if self.is_cuda else -1
+
+    def stride(self):
+        return self.shape[1], 1
 
 
-def matrix(rows, cols):
-    return SimpleNamespace(rows=rows, cols=cols, codes_ptr=256, scales_ptr=512, device=0)
+def matrix(rows, cols, device=0):
+    return SimpleNamespace(rows=rows, cols=cols, codes_ptr=256, scales_ptr=512, device=device)
 
 
 @pytest.fixture
@@ -137,3 +140,27 @@ def test_a_stream_that_somebody_else_set_does_not_stay(made):
     ctx._raw_stream = lambda: 5
     ctx.mx4_quantize_aggregate([Device(1608)], Device(1608))
     assert stream_of_the_library() == 5
+
+
+def test_operands_are_on_the_context_s_device(made):
+    """What lies on another device would be read or written through a pointer that this one may not follow."""
+    ctx, fake = made
+    here, there = Device(12800, shape=(100, 128)), Device(12800, shape=(100, 128), device=1)
+    out = Device(10000, shape=(100, 100))
+    q, q_t, far, far_t = matrix(100, 128), matrix(128, 100), matrix(100, 128, 1), matrix(128, 100, 1)
+    ctx.mx4_quantize_both(here, out=q, out_t=q_t)
+    ctx.mx4_dequantize(q, here)
+    ctx.mx4_matmul(q, q, out)
+    assert len(fake.names()) == 3
+    flat, flat_there = Device(1608), Device(1608, device=1)
+    for call in (lambda: ctx.mx4_quantize(there), lambda: ctx.mx4_quantize(here, out=far),
+                 lambda: ctx.mx4_quantize_transposed(here, out=far_t), lambda: ctx.mx4_dequantize(far, here),
+                 lambda: ctx.mx4_dequantize(q, there), lambda: ctx.mx4_matmul(far, q, out), lambda: ctx.mx4_matmul(q, far, out),
+                 lambda: ctx.mx4_matmul(q, q, Device(10000, shape=(100, 100), device=1)),
+                 lambda: ctx.mx4_quantize_aggregate([flat, flat_there], flat),
+                 lambda: ctx.mx4_quantize_aggregate([flat], flat_there),
+                 lambda: ctx.mx4_quantize_aggregate([flat], flat, out=[matrix(100, 16, 1)]),
+                 lambda: ctx.mx4_dequantize_aggregate([matrix(100, 16, 1)], None, flat)):
+        with pytest.raises(ValueError):
+            call()
+    assert len(fake.names()) == 3
