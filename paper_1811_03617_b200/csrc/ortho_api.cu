@@ -2,8 +2,9 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <exception>
 #include <functional>
-#include <new>
+#include <memory>
 
 #include "api_util.h"
 #include "ortho.h"
@@ -158,9 +159,13 @@ extern "C" {
 int64_t gvq_ortho_workspace_bytes(const gvq_layout *layout, const int32_t *rows, const int32_t *cols)
 {
     if (!rows || !cols || gvq_layout_check(layout) != GVQ_OK) return -1;
-    Sizes s;
-    if (lay_out(layout->n_layers, layout->layer_off, layout->layer_len, rows, cols, nullptr, nullptr, s) != GVQ_OK) return -1;
-    return (int64_t)s.bytes;
+    try {
+        Sizes s;
+        if (lay_out(layout->n_layers, layout->layer_off, layout->layer_len, rows, cols, nullptr, nullptr, s) != GVQ_OK) return -1;
+        return (int64_t)s.bytes;
+    } catch (const std::exception &) {       // no host memory
+        return -1;
+    }
 }
 
 gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, const int32_t *cols, const float *scales_opt,
@@ -234,7 +239,7 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
         split(gram, units, (pair ? 2 : 1) * 4 * (pair ? kPairN : kSoloN) / 64, slots);
         const std::vector<int32_t> gram_start = deal(gram, units), sym_start = deal(sym, units), apply_start = deal(apply, units);
 
-        gvq_ortho *p = new gvq_ortho();
+        std::unique_ptr<gvq_ortho> p(new gvq_ortho());
         p->ctx = ctx;
         p->device = ctx->device;
         std::vector<unsigned char> image;
@@ -256,7 +261,6 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
         if (e == cudaSuccess) e = upload(p->tables, image.data(), image.size());
         if (e != cudaSuccess) {
             if (p->tables) cudaFree(p->tables);
-            delete p;
             return cuda_fail(ctx, e);
         }
         unsigned char *t = static_cast<unsigned char *>(p->tables);
@@ -288,9 +292,9 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
         }
         p->small = small_plan(n, shorter, longer, ctx->num_sms);
         d.chunk = chunk;
-        *out = p;
+        *out = p.release();
         return GVQ_OK;
-    } catch (const std::bad_alloc &) {
+    } catch (const std::exception &) {       // no host memory
         return GVQ_ERR_CUDA;
     }
 }

@@ -87,3 +87,28 @@ def test_reference_random_numbers_look_uniform():
     assert abs(u.mean() - 0.5) < 5 * (1 / 12 / n) ** 0.5
     assert abs(np.corrcoef(u[:, 0::2].ravel(), u[:, 1::2].ravel())[0, 1]) < 5 / (n / 2) ** 0.5
     assert abs(np.corrcoef(u[:-1].ravel(), u[1:].ravel())[0, 1]) < 5 / n ** 0.5
+
+
+def test_running_out_of_host_memory_is_an_error_code():
+    """No exception leaves a C entry: 4 million layers under a limit of the address space that their tables exceed."""
+    import subprocess
+    import sys
+    from pathlib import Path
+    code = """
+import ctypes, resource
+import numpy as np
+from paper_1811_03617_b200 import gvq
+L, n = gvq.lib(), 4_000_000
+off, length, rows = np.arange(n, dtype=np.int64) * 4, np.full(n, 4, dtype=np.int64), np.full(n, 2, dtype=np.int32)
+p = lambda a, t: a.ctypes.data_as(ctypes.POINTER(t))
+layout = gvq._Layout(64, 4, n, p(off, ctypes.c_int64), p(length, ctypes.c_int64))
+need = lambda: L.gvq_ortho_workspace_bytes(ctypes.byref(layout), p(rows, ctypes.c_int32), p(rows, ctypes.c_int32))
+held = int(open('/proc/self/statm').read().split()[0]) * resource.getpagesize()
+resource.setrlimit(resource.RLIMIT_AS, (held + (200 << 20), resource.RLIM_INFINITY))
+less = need()
+resource.setrlimit(resource.RLIMIT_AS, (resource.RLIM_INFINITY, resource.RLIM_INFINITY))
+print('less', less, 'enough', need() > 0)
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=Path(__file__).resolve().parent.parent)
+    assert r.returncode == 0, r.stderr[-500:]
+    assert r.stdout.split() == ["less", "-1", "enough", "True"]
