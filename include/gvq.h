@@ -535,10 +535,17 @@ gvq_status gvq_mx4_dequantize_aggregate(gvq_ctx *ctx, const uint8_t *const *code
      X = u / (|u|_F + 1e-7);            five times, on the shorter side:  A = X X^T,  X = a X + (b A + c A^2) X
      w = (1 - lr * weight_decay) w - lr * scale * X          (a, b, c) = (3.4445, -4.7750, 2.0315)
    (the update of the Muon optimiser: every singular value of u is moved to about 1; scale = sqrt(max(1, rows / cols))
-   unless given).  The products run on the tensor cores with half-precision operands and fp32 accumulation: X is within
-   2.5e-3 (relative, rms; 1.7e-3 where the shorter side is at most 128) of its value in exact arithmetic.  Momentum, norms and the weights' sum are fp32, each
-   rounding to w's type once.  A matrix that is zero moves nothing (X = 0); one that holds a NaN or an infinity gives NaN
-   or zero for its own layer, as the formula does, and touches no other.
+   unless given).  The products run on the tensor cores with half-precision operands and fp32 accumulation.  X is within
+     3.2e-3  of its value in exact arithmetic (relative, rms) for sums of rank-one terms of random factors, any number of
+             them, over noise of any size, shorter side 8 or more;
+     4e-3    for other matrices of random entries, equal or decaying singular values among them;
+     1.5e-2  where roundings do not average out: few nonzero rows or columns, entries that are all alike (constants,
+             signs, identities);
+     2e-4    whatever the entries, where the longer side is at most 64 and every matrix of the plan fits an SM (shorter side
+             up to 64 and longer up to 832, or up to 128 and 320)
+   as long as |u|_F is at least 1e-10 and its square within fp32's range (a larger one counts as an infinity).  Momentum,
+   norms and the weights' sum are fp32, each rounding to w's type once.  A matrix that is zero moves nothing (X = 0); one
+   that holds a NaN or an infinity gives NaN or zero for its own layer, as the formula does, and touches no other.
    rows, cols: HOST arrays [n_layers], rows[l] * cols[l] = layer_len[l], or both 0: the layer is left alone; the shorter
    side is at most 32768, the longer one below 2^20.  scales_opt: NULL or HOST [n_layers].  workspace: device, 256-byte aligned,
    gvq_ortho_workspace_bytes() bytes (-1 on bad sizes), owned by the caller and kept while the plan lives; its contents

@@ -8,19 +8,26 @@
 // with X^T X and X B; the tensor core reads an operand K-major or MN-major, so X is one row-major array for all of:
 //     wide   A = X X^T   both operands K-major       X' = B X   B K-major (symmetric), X MN-major
 //     tall   A = X^T X   both operands MN-major      X' = X B   both K-major
-// A, b I + c A and P are symmetric: only tiles that touch or lie right of the diagonal are computed and stored; an operand
-// tile left of it is read as the transposed tile, in the other major.
+// A and P = a I + b A + c A^2 are symmetric: only tiles that touch or lie right of the diagonal are computed and stored; an operand
+// tile left of it is read as the transposed tile, in the other major.  P is made of what is symmetric exactly, A A and A:
+// as A (b I + c A), its second factor rounded, its two sides differed (errors of 3.3e-3 instead of 2.7e-3 at 1024 x 1024).
 //
 // Precision.  The products take half-precision operands (11 significant bits; bf16 would leave 8) and accumulate in
 // fp32.  Powers of two keep the operands in range.  X in half precision alone would lose what matters most: rounding X
-// adds noise to every direction alike, and the first steps amplify the small singular directions, noise included, by
+// adds noise to every direction alike, and the steps amplify the small singular directions, noise included, by
 // 3.4 each (an rms error of 5e-3 in the result for a low-rank gradient over noise, against 1e-3 for a Gaussian one).
 // The a X term carries X forward, so X is kept as a sum of two halves (22 bits) for the first kExactSteps steps; the
-// products take the high half,  X' = (a I + b A + c A^2) X_hi + a X_lo.  After that the steps contract the noise of the large directions, and carrying it exactly
-// would not help.  Measured on the CPU, relative to 64 bits: 0.4e-3 to 1.6e-3 for sides of 256 and more.  Where the short side
-// is short, A and P have few entries of like size and their own roundings do not average out: 2e-3 to 4e-3.  Up to kSplitSide
-// A and b I + c A are kept as sums of two halves too, up to kSplitApply P as well, and the products are sums of products of
-// halves (their contractions are short): 0.3e-3 to 1.7e-3.
+// products take the high half,  X' = (a I + b A + c A^2) X_hi + a X_lo.  With three such steps instead of four, gradients of
+// low rank were off by 3.3e-3 to 3.6e-3, with four by 1.9e-3 to 2.9e-3; in the last one the large directions, whose noise a step
+// contracts, would get more back than they lose (Gaussian 2.1e-3 -> 2.2e-3).  Where the short side is short, A and P have few
+// entries of like size and their own roundings do not average out.  Up to kSplitSide A is kept as a sum of two halves too, up
+// to kSplitApply P as well, and the products are sums of products of halves (their contractions are short).
+// Relative rms errors against 64 bits, shapes from 8 x 12 to 2000 x 2000 and 512 x 4608:
+//   sums of rank-one terms of random factors, any number, over noise of any size    0.3e-3 to 2.9e-3
+//   equal or decaying singular values                                              0.5e-3 to 3.6e-3
+//   random entries in a few rows or columns, zeros elsewhere                        up to 5e-3
+//   entries that are all alike: constants, signs, (partial) identities               up to 9.2e-3
+// The last two are what is left of half-precision operands: roundings that do not average out, of X itself among them.
 #include "ortho.h"
 #include "row32.cuh"
 #include "sm100_ptx.cuh"
@@ -218,7 +225,7 @@ __device__ __forceinline__ Work work_of(const Matrix &m, int step)
 {
     const int x = step & 1;
     if (PHASE == kGram) return {m.r, m.r, m.c, x, x, m.tall != 0, m.tall != 0, false, false};
-    if (PHASE == kPoly) return {m.r, m.r, m.r, kGramMap, kFactorMap, false, false, true, true};
+    if (PHASE == kPoly) return {m.r, m.r, m.r, kGramMap, kGramMap, false, false, true, true};
     return m.tall ? Work{m.rows, m.cols, m.r, x, kPolyMap, false, false, false, true}
                   : Work{m.rows, m.cols, m.r, kPolyMap, x, false, true, true, false};
 }
@@ -353,8 +360,8 @@ template <int PHASE> __device__ __forceinline__ int stages_of_a_product(const Se
     return PHASE == kGram ? s.k1 : min((int)s.k1, (s.K + KS - 1) / KS);
 }
 
-// T: the type of the last step's result (PHASE kLast).  LOW: the plan has matrices whose result has a low half here (kGram,
-// kPoly); without, their code is left out of a kernel whose launches are short.
+// T: the type of the last step's result (PHASE kLast).  LOW: the plan has matrices whose A has a low half (kGram, kPoly);
+// without, the code for them is left out of a kernel whose launches are short.
 template <int PHASE, int CG, typename T = float, bool LOW = false>
 __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __grid_constant__ ProductParams prm)
 {
@@ -365,8 +372,8 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
     Seen *table = reinterpret_cast<Seen *>(staging + S::NEPI * kStaging);
     uint64_t *bars = reinterpret_cast<uint64_t *>(table + kTable);
     uint64_t *full = bars, *empty = full + S::STAGES, *d_full = empty + S::STAGES, *d_empty = d_full + 2;
-    uint64_t *lo_full = d_empty + 2;         // [NEPI] low halves of a warp's pieces have landed
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(lo_full + S::NEPI);
+    uint64_t *fetched = d_empty + 2;         // [NEPI] what a warp's epilogue reads has landed
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(fetched + S::NEPI);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CG == 2 ? (int)cluster_rank() : 0;
@@ -374,7 +381,7 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::STAGES; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(d_full + i, 1); mbar_init(d_empty + i, CG * S::NEPI); }
-        for (int i = 0; i < S::NEPI; ++i) mbar_init(lo_full + i, 1);
+        for (int i = 0; i < S::NEPI; ++i) mbar_init(fetched + i, 1);
         *abort_flag = 0;
         const_cast<int *>(abort_flag)[2] = prm.wait_kcycles;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -422,7 +429,7 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                 const int per = stages_of_a_product<PHASE>(l);
                 for (int first = 0, term = 0; first < l.k1 && !failed; first += per, ++term) {      // products of halves
                     const CUtensorMap *map_a = maps + l.a_map, *map_b = maps + l.b_map;
-                    if (PHASE == kPoly && term > 0) { map_a = maps + (term == 2 ? kGramLoMap : kGramMap); map_b = maps + (term == 1 ? kFactorLoMap : kFactorMap); }
+                    if (PHASE == kPoly && term > 0) { if (term == 1) map_b = maps + kGramLoMap; else map_a = maps + kGramLoMap; }
                     if (PHASE >= kApply && term > 0) { if (l.a_map == kPolyMap) map_a = maps + kPolyLoMap; else map_b = maps + kPolyLoMap; }
                     for (int st = first > 0 ? first : l.k0; st < first + per; st += S::PER_STAGE, ++c) {
                         if (!mbar_poll(empty + s, phase, abort_flag)) { failed = true; break; }
@@ -503,17 +510,17 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
         const uint32_t lane_base = (uint32_t)(32 * q) << 16;
         unsigned char *mine = staging + (warp - 2) * kStaging;
         constexpr int COLS = S::BN / (S::NEPI / 4), PIECES = COLS / 64;      // of a warp
-        const bool read_lo = PHASE == kApply && prm.step < kExactSteps;
-        const bool write_lo = PHASE == kApply && prm.step + 1 < kExactSteps;
-        // What the epilogue reads besides the accumulator is on its way before the tile's MMAs are done: X's low halves come
-        // into the staging areas by TMA, where their new values, or X's, take their place; the weights a piece ahead.
-        auto load_lo = [&](const Seen &at) {
+        constexpr bool FETCH = PHASE == kPoly || PHASE == kApply;
+        const bool write_lo = PHASE == kApply && prm.step + 1 < kExactSteps;      // (every step of this phase reads them)
+        // What the epilogue reads besides the accumulator is on its way before the tile's MMAs are done: A or X's low halves come
+        // into the staging areas by TMA, where the results take their place; the weights a piece ahead.
+        auto fetch = [&](const Seen &at) {
             if (lane == 0) {
-                mbar_arrive_expect_tx(lo_full + warp - 2, PIECES * 4096);
+                mbar_arrive_expect_tx(fetched + warp - 2, PIECES * 4096);
 #pragma unroll
                 for (int p = 0; p < PIECES; ++p)
-                    tma_load_2d(mine + p * 4096, prm.dev.maps + (size_t)at.matrix * kMaps + kLoOut, at.n0 + half * COLS + 64 * p,
-                                at.m0 + 128 * rank + 32 * q, lo_full + warp - 2);
+                    tma_load_2d(mine + p * 4096, prm.dev.maps + (size_t)at.matrix * kMaps + (PHASE == kPoly ? kGramOut : kLoOut),
+                                at.n0 + half * COLS + 64 * p, at.m0 + 128 * rank + 32 * q, fetched + warp - 2);
             }
         };
         Weights<T> weights;
@@ -523,7 +530,7 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
         };
         Seen here = seen(t_begin);
         grid_dependency_wait();      // (before anything that another launch writes is read, or written)
-        if (PHASE == kApply && read_lo) load_lo(here);
+        if (FETCH) fetch(here);
         if (PHASE == kLast) fetch_weights(here, here.n0 + half * COLS);
         uint32_t u = 0, stores = 0;
         for (int t = t_begin; t < t_end; ++t, ++u) {
@@ -534,7 +541,7 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
             const CUtensorMap *maps = prm.dev.maps + (size_t)here.matrix * kMaps;
             const uint32_t ab = u & 1;
             const float sx = mx.sx;           // (read here, while the MMAs run)
-            const bool low = LOW && mx.split >= (PHASE == kPoly ? 2 : 1);
+            const bool low = LOW && mx.split > 0;
             bool ok = mbar_poll(d_full + ab, (u >> 1) & 1, abort_flag);
             if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
             tc_fence_after();
@@ -625,33 +632,48 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                     __syncwarp();
                     return mine + (stores++ & 1) * 4096;
                 };
-                if (PHASE == kApply) {       // X' = P X_hi + a X_lo
-                    if (read_lo && p == 0) {
-                        ok = mbar_poll(lo_full + warp - 2, u & 1, abort_flag);
-                        if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
+                if (FETCH && p == 0) {
+                    ok = mbar_poll(fetched + warp - 2, u & 1, abort_flag);
+                    if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
+                }
+                auto fetch_next = [&]() {      // once the tile's stores have read their areas
+                    if (t + 1 == t_end) return;
+                    if (lane == 0) bulk_wait_group_read<0>();
+                    __syncwarp();
+                    fetch(next);
+                };
+                // the low halves of what a lane holds of a piece, as it is staged
+                auto stage_low = [&](unsigned char *to) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float a = v[j >> 2][8 * (j & 3) + 2 * e], b = v[j >> 2][8 * (j & 3) + 2 * e + 1];
+                            const float2 r = unpack_half2(pack2<__half>(a, b));
+                            w[e] = pack2<__half>(a - r.x, b - r.y);
+                        }
+                        *reinterpret_cast<uint4 *>(to + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
+                };
+                if (PHASE == kApply) {       // X' = P X_hi + a X_lo
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            uint4 l = make_uint4(0, 0, 0, 0);
-                            if (read_lo) l = *reinterpret_cast<const uint4 *>(mine + p * 4096 + lane * 128 + (((4 * h + j) ^ (lane & 7)) << 4));
+                            const uint4 l = *reinterpret_cast<const uint4 *>(mine + p * 4096 + lane * 128 + (((4 * h + j) ^ (lane & 7)) << 4));
                             const uint32_t w[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 const int i = 8 * j + 2 * e;
-                                v[h][i] *= 1.0f / kGramScale;
-                                v[h][i + 1] *= 1.0f / kGramScale;
-                                if (read_lo) {
-                                    const float2 x = unpack_half2(w[e]);
-                                    v[h][i] = __fmaf_rn(kA, x.x, v[h][i]);
-                                    v[h][i + 1] = __fmaf_rn(kA, x.y, v[h][i + 1]);
-                                }
+                                const float2 x = unpack_half2(w[e]);
+                                v[h][i] = __fmaf_rn(kA, x.x, v[h][i] * (1.0f / kGramScale));
+                                v[h][i + 1] = __fmaf_rn(kA, x.y, v[h][i + 1] * (1.0f / kGramScale));
                             }
                         }
                     if (live) {
                         // (in place: a lane has read its row of the piece)
-                        unsigned char *to = read_lo ? mine + p * 4096 : room();
+                        unsigned char *to = mine + p * 4096;
                         stage_swizzled16<__half>(to, lane, v[0], v[1]);
                         store(to, kX0Out + ((prm.step + 1) & 1), n0);
                     }
@@ -680,56 +702,67 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                             store(mine + r * 4096, kLoOut, c0 + 64 * r);
                         }
                     }
-                    if (read_lo && t + 1 < t_end) {
-                        if (lane == 0) bulk_wait_group_read<0>();
-                        __syncwarp();
-                        load_lo(next);
-                    }
+                    fetch_next();
                     continue;
                 }
-                if (!live) continue;
-                // A = X X^T and b I + c A, whose product with A the next launch takes; then P = a I + A (b I + c A)
-                auto put = [&](int map, int lo_map) {
+                if (PHASE == kPoly) {        // P = a I + b A + c A^2
+                    if (live) {
+                        unsigned char *to = mine + p * 4096;
+                        const __half *lows = low && lane < rows ? mx.gram_lo + (int64_t)(m0 + lane) * mx.ldr + n0 : nullptr;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const uint4 hi = *reinterpret_cast<const uint4 *>(to + lane * 128 + ((j ^ (lane & 7)) << 4));
+                            const uint32_t w[4] = {hi.x, hi.y, hi.z, hi.w};
+                            uint4 lo = make_uint4(0, 0, 0, 0);       // (rows are ldr entries, a multiple of 32, long)
+                            if (LOW && lows && n0 + 8 * j < mx.ldr) lo = *reinterpret_cast<const uint4 *>(lows + 8 * j);
+                            const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w};
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const float2 x = unpack_half2(w[e >> 1]);
+                                float a = e & 1 ? x.y : x.x;
+                                if (LOW) {
+                                    const float2 y = unpack_half2(l[e >> 1]);
+                                    a += e & 1 ? y.y : y.x;
+                                }
+                                float &r = v[j >> 2][8 * (j & 3) + e];
+                                r = __fmaf_rn(kB, a, r * (kC / kGramScale));
+                                if (n0 + 8 * j + e == m0 + lane) r += kA * kGramScale;
+                            }
+                        }
+                        stage_swizzled16<__half>(to, lane, v[0], v[1]);       // (in place: a lane has read its row of the piece)
+                        store(to, kPolyOut, n0);
+                        // P's low halves: only of short sides that the first piece holds, so that the other area is free
+                        static_assert(kSplitApply <= 64, "a piece");
+                        if (LOW && mx.split > 1) {
+                            stage_low(mine + 4096);
+                            store(mine + 4096, kPolyLoOut, n0);
+                        }
+                    }
+                    if (p == PIECES - 1) fetch_next();
+                    continue;
+                }
+                if (PHASE == kGram && live) {       // A = X X^T
+                    const float f = kGramScale / (sx * sx);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[h][i] *= f;
                     unsigned char *to = room();
                     stage_swizzled16<__half>(to, lane, v[0], v[1]);
-                    store(to, map, n0);
-                    if (!LOW || !low) return;
-                    to = room();
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        uint32_t w[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float a = v[j >> 2][8 * (j & 3) + 2 * e], b = v[j >> 2][8 * (j & 3) + 2 * e + 1];
-                            const float2 r = unpack_half2(pack2<__half>(a, b));
-                            w[e] = pack2<__half>(a - r.x, b - r.y);
-                        }
-                        *reinterpret_cast<uint4 *>(to + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    store(to, kGramOut, n0);
+                    if (LOW && low) {
+                        to = room();
+                        stage_low(to);
+                        store(to, kGramLoOut, n0);
                     }
-                    store(to, lo_map, n0);
-                };
-                const float f = PHASE == kGram ? kGramScale / (sx * sx) : 1.0f / kGramScale;
-                const float diagonal = (PHASE == kGram ? kB : kA) * kGramScale;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[h][i] *= f;
-                if (PHASE == kGram) put(kGramOut, kGramLoOut);
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        if (PHASE == kGram) v[h][i] *= kC;
-                        if (n0 + 32 * h + i == m0 + lane) v[h][i] += diagonal;
-                    }
-                if (PHASE == kGram) put(kFactorOut, kFactorLoOut); else put(kPolyOut, kPolyLoOut);
+                }
             }
             if (failed) break;
             here = next;
         }
         if (lane == 0) bulk_wait_group_all();
-        if (failed && read_lo)       // low halves still under way (a bounded chance to land before the CTA exits)
-            for (int it = 0; it < 100000 && !mbar_try_wait(lo_full + warp - 2, u & 1); ++it) {}
+        if (FETCH && failed)         // what is still under way gets a bounded chance to land before the CTA exits
+            for (int it = 0; it < 100000 && !mbar_try_wait(fetched + warp - 2, u & 1); ++it) {}
     }
 
     if (failed) {
@@ -765,6 +798,7 @@ cudaError_t launch_start(cudaStream_t st, const Device &dev, const ElementArgs &
 cudaError_t launch_product(cudaStream_t st, const Device &dev, Phase phase, int step, const OutputArgs *out,
                            int32_t *error_word, int wait_kcycles, int test_drop)
 {
+    static_assert(kExactSteps == kSteps - 1, "every product with an X that is not the last result reads its low half");
     ProductParams prm;
     prm.dev = dev;
     prm.out = out ? *out : OutputArgs{};
@@ -774,7 +808,7 @@ cudaError_t launch_product(cudaStream_t st, const Device &dev, Phase phase, int 
     prm.test_drop = test_drop;
     const int runs = dev.run[phase].runs;
     if (phase == kGram) return dev.split > 0 ? launch_tiling<kGram, float, true>(st, prm, runs) : launch_tiling<kGram>(st, prm, runs);
-    if (phase == kPoly) return dev.split > 1 ? launch_tiling<kPoly, float, true>(st, prm, runs) : launch_tiling<kPoly>(st, prm, runs);
+    if (phase == kPoly) return dev.split > 0 ? launch_tiling<kPoly, float, true>(st, prm, runs) : launch_tiling<kPoly>(st, prm, runs);
     if (step < kSteps - 1) return launch_tiling<kApply>(st, prm, runs);
     if (out->dtype == GVQ_F32) return launch_tiling<kLast, float>(st, prm, runs);
     if (out->dtype == GVQ_BF16) return launch_tiling<kLast, __nv_bfloat16>(st, prm, runs);

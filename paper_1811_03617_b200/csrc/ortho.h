@@ -12,9 +12,9 @@ constexpr int kSteps = 5;
 // five steps (Jordan's choice for the Muon optimiser: slope 3.44 at zero, values end in [0.7, 1.2]).
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr float kEps = 1e-7f;
-// Steps whose X is kept as a sum of two halves (ortho.cu's header has the reason).
-constexpr int kExactSteps = 3;
-// Short sides up to which A and b I + c A, and P, are sums of two halves as well (ortho.cu's header has the reason).
+// Steps whose X is kept as a sum of two halves: all but the last (ortho.cu's header has the reason).
+constexpr int kExactSteps = kSteps - 1;
+// Short sides up to which A, and P, are sums of two halves as well (ortho.cu's header has the reason).
 constexpr int kSplitSide = 128, kSplitApply = 48;
 // Scale of A and of a I + b A + c A^2 in half precision: entries of both are of order 1 (at most 3.5 + 1.2 |b| + 1.44 |c| = 12),
 // those off the diagonal far smaller.
@@ -31,23 +31,23 @@ struct Matrix {
     int32_t chunk0, n_chunks;        // its chunks in the element-wise passes
     int64_t off;                     // in the flat buffers
     uint64_t by_cols;                // floor(2^62 / cols) + 1: n / cols = (4 n * by_cols) >> 64 for n < 2^40, cols < 2^20
-    // X (two buffers, in turn), X's low halves; A, b I + c A, P; rows ldx or ldr entries apart
-    __half *x[2], *lo, *gram, *factor, *poly;
-    __half *gram_lo, *factor_lo, *poly_lo;      // what the last three lose in half precision 
-    int32_t split;                   // 0: nothing, 1: A and b I + c A are sums of two halves, 2: P too
+    // X (two buffers, in turn), X's low halves; A, P; rows ldx or ldr entries apart
+    __half *x[2], *lo, *gram, *poly;
+    __half *gram_lo, *poly_lo;       // what the last two lose in half precision
+    int32_t split;                   // 0: nothing, 1: A is a sum of two halves, 2: P too
     float sx;                        // scale of X in half precision
     float scale;                     // of the update
 };
 // A tile of a product, or a part of its contraction: stages [k0, k1) of 64 steps.  parts > 1: the parts' sums meet in the
 // plan's scratch from piece `slot` on (part by part), and whoever comes last adds them up.
-// Stages of products of halves follow one another: hi hi, hi lo and lo hi of A (b I + c A), P_hi X and P_lo X.
+// Stages of products of halves follow one another: hi hi, hi lo and lo hi of A^2, P_hi X and P_lo X.
 struct Tile { int32_t matrix, tm, tn, k0, k1, part, parts, slot; };
 struct Chunk { int32_t matrix, index; };
 
 enum Phase { kGram = 0, kPoly = 1, kApply = 2, kLast = 3 };
 // Tensor maps of a matrix: operands (boxes of 64 x 64) and results (64 columns x 32 rows)
-enum Map { kX0 = 0, kX1, kGramMap, kFactorMap, kPolyMap, kX0Out, kX1Out, kLoOut, kGramOut, kFactorOut, kPolyOut,
-           kGramLoMap, kFactorLoMap, kPolyLoMap, kGramLoOut, kFactorLoOut, kPolyLoOut, kMaps };
+enum Map { kX0 = 0, kX1, kGramMap, kPolyMap, kX0Out, kX1Out, kLoOut, kGramOut, kPolyOut, kGramLoMap, kPolyLoMap,
+           kGramLoOut, kPolyLoOut, kMaps };
 
 // The tiles of a phase, in runs, one for each CTA (or pair): run i is tiles [start[i], start[i + 1]).
 struct Run {

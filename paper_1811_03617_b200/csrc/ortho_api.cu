@@ -65,9 +65,9 @@ gvq_status lay_out(int n_layers, const int64_t *off, const int64_t *len, const i
             return p;
         };
         const size_t nx = (size_t)m.rows * m.ldx, nr = (size_t)m.r * m.ldr;
-        m.x[0] = take(nx); m.x[1] = take(nx); m.lo = take(nx); m.gram = take(nr); m.factor = take(nr); m.poly = take(nr);
+        m.x[0] = take(nx); m.x[1] = take(nx); m.lo = take(nx); m.gram = take(nr); m.poly = take(nr);
         m.split = m.r <= kSplitApply ? 2 : m.r <= kSplitSide ? 1 : 0;
-        if (m.split > 0) { m.gram_lo = take(nr); m.factor_lo = take(nr); }
+        if (m.split > 0) m.gram_lo = take(nr);
         if (m.split > 1) m.poly_lo = take(nr);
         out.mats.push_back(m);
     }
@@ -201,15 +201,11 @@ gvq_status gvq_ortho_create(gvq_ortho **out, gvq_ctx *ctx, const int32_t *rows, 
                               square ? m.ldr : m.ldx, box_rows);
             };
             if (!map(kX0, m.x[0], 64, false) || !map(kX1, m.x[1], 64, false) || !map(kGramMap, m.gram, 64, true) ||
-                !map(kFactorMap, m.factor, 64, true) || !map(kPolyMap, m.poly, 64, true) || !map(kX0Out, m.x[0], 32, false) ||
-                !map(kX1Out, m.x[1], 32, false) || !map(kLoOut, m.lo, 32, false) || !map(kGramOut, m.gram, 32, true) ||
-                !map(kFactorOut, m.factor, 32, true) || !map(kPolyOut, m.poly, 32, true))
+                !map(kPolyMap, m.poly, 64, true) || !map(kX0Out, m.x[0], 32, false) || !map(kX1Out, m.x[1], 32, false) ||
+                !map(kLoOut, m.lo, 32, false) || !map(kGramOut, m.gram, 32, true) || !map(kPolyOut, m.poly, 32, true))
                 return GVQ_ERR_CUDA;
-            if (m.split > 0 && (!map(kGramLoMap, m.gram_lo, 64, true) || !map(kFactorLoMap, m.factor_lo, 64, true) ||
-                                !map(kGramLoOut, m.gram_lo, 32, true) || !map(kFactorLoOut, m.factor_lo, 32, true)))
-                return GVQ_ERR_CUDA;
-            if (m.split > 1 && (!map(kPolyLoMap, m.poly_lo, 64, true) || !map(kPolyLoOut, m.poly_lo, 32, true)))
-                return GVQ_ERR_CUDA;
+            if (m.split > 0 && (!map(kGramLoMap, m.gram_lo, 64, true) || !map(kGramLoOut, m.gram_lo, 32, true))) return GVQ_ERR_CUDA;
+            if (m.split > 1 && (!map(kPolyLoMap, m.poly_lo, 64, true) || !map(kPolyLoOut, m.poly_lo, 32, true))) return GVQ_ERR_CUDA;
             m.chunk0 = (int)chunks.size();
             m.n_chunks = (int)(((int64_t)m.rows * m.cols + chunk - 1) / chunk);
             for (int k = 0; k < m.n_chunks; ++k) chunks.push_back({i, k});

@@ -13,8 +13,8 @@
 //     X^T P  D[128 x R] for every 128 of the long side       -> X = X_hi P + a X_lo in place
 // A and P rounded to one half would leave errors of 2e-3 to 4e-3 of the result where the short side is short (their entries
 // are then few and of like size, and the steps amplify what the singular values are off by); with A's low half, and P's up
-// to kSplitApply, it is 0.3e-3 to 1.7e-3.  Where the long side has 64 entries or fewer too, what X loses does not average
-// out either, and its low half takes part in every product.
+// to kSplitApply, it is what ortho.cu's header lists, at most 2.6e-3 for gradients of random factors.  Where the long side has 64
+// entries or fewer too, what X loses does not average out either; its low half takes part in every product, and about 1e-4 is left.
 // R is the short side's room, 64 or 128.  The unused rows and columns of X are zeros and stay zeros; an MMA's 128 rows
 // may run on into the next array, and those rows of the accumulator are not read.
 //
