@@ -530,7 +530,10 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
         };
         Seen here = seen(t_begin);
         grid_dependency_wait();      // (before anything that another launch writes is read, or written)
-        if (FETCH) fetch(here);
+        if (FETCH) {
+            if (PHASE == kApply) fence_proxy_async_global();      // (X's first low halves were written by plain stores)
+            fetch(here);
+        }
         if (PHASE == kLast) fetch_weights(here, here.n0 + half * COLS);
         uint32_t u = 0, stores = 0;
         for (int t = t_begin; t < t_end; ++t, ++u) {
