@@ -534,8 +534,10 @@ gvq_status gvq_mx4_dequantize_aggregate(gvq_ctx *ctx, const uint8_t *const *code
      momentum = beta * momentum + g;    u = g + beta * momentum (nesterov != 0) or momentum
      X = u / (|u|_F + 1e-7);            five times, on the shorter side:  A = X X^T,  X = a X + (b A + c A^2) X
      w = (1 - lr * weight_decay) w - lr * scale * X          (a, b, c) = (3.4445, -4.7750, 2.0315)
-   (the update of the Muon optimiser: every singular value of u is moved to about 1; scale = sqrt(max(1, rows / cols))
-   unless given).  The products run on the tensor cores with half-precision operands and fp32 accumulation.  X is within
+   (the update of the Muon optimiser: every singular value of u is moved to about 1.  scale, unless scales_opt gives it, is
+   sqrt(max(1, rows / cols)), that optimiser's factor for a matrix whose rows are the layer's outputs, W[out][in].  In
+   gvq_flatten_layer's order a layer is [inputs][filters]: there the factor is sqrt(max(1, cols / rows)), to be given in
+   scales_opt.)  The products run on the tensor cores with half-precision operands and fp32 accumulation.  X is within
      3.2e-3  of its value in exact arithmetic (relative, rms) for sums of rank-one terms of random factors, any number of
              them, over noise of any size, shorter side 8 or more;
      4e-3    for other matrices of random entries, equal or decaying singular values among them;

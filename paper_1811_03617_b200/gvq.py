@@ -8,6 +8,7 @@ fallback: if the shared library is missing or a call fails, an exception is rais
 from __future__ import annotations
 
 import ctypes
+import math
 from pathlib import Path
 from typing import Optional, Sequence
 
@@ -721,13 +722,25 @@ class Context:
 
 
 class OrthoPlan:
-    """gvq_ortho: the orthogonalised update of a context's layers that are matrices, rows[l] x cols[l] (0, 0: not one)."""
+    """gvq_ortho: the orthogonalised update of a context's layers that are matrices, rows[l] x cols[l] (0, 0: not one).
 
-    def __init__(self, ctx: Context, rows: Sequence[int], cols: Sequence[int], scales: Optional[Sequence[float]] = None):
+    scales: the update's factor of each layer.  None: sqrt(max(1, outputs / inputs)), a layer's outputs being its rows
+    (W[out][in]), or its columns where `flattened` says that layers are in gvq_flatten_layer's order, [inputs][filters]
+    (one truth value for all layers or one for each)."""
+
+    def __init__(self, ctx: Context, rows: Sequence[int], cols: Sequence[int], scales: Optional[Sequence[float]] = None,
+                 flattened=False):
         self._h = ctypes.c_void_p()
         n = ctx.n_layers
         if len(rows) != n or len(cols) != n or (scales is not None and len(scales) != n):
             raise ValueError(f"OrthoPlan: one entry per layer is wanted ({n})")
+        if scales is None and flattened is not False:
+            order = [bool(flattened)] * n if isinstance(flattened, (bool, int)) else list(flattened)
+            if len(order) != n:
+                raise ValueError(f"OrthoPlan: one entry per layer is wanted ({n})")
+            scales = [math.sqrt(max(1.0, (v / u if f else u / v) if u and v else 1.0)) for u, v, f in zip(rows, cols, order)]
+        elif flattened is not False:
+            raise ValueError("OrthoPlan: scales are given, so the layers' order has no use")
         self.ctx = ctx                       # the plan uses its stream and must not outlive it
         r, c = (ctypes.c_int32 * n)(*[int(v) for v in rows]), (ctypes.c_int32 * n)(*[int(v) for v in cols])
         nbytes = lib().gvq_ortho_workspace_bytes(ctypes.byref(ctx.layout.c), r, c)

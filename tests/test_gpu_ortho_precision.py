@@ -112,3 +112,22 @@ def test_errors_stay_within_the_bound_for_small_and_large_gradients(shapes, norm
     plan.orthogonalize(u.view(-1), out)
     want = exact(u)
     assert float((out.view(r, c).double() - want).norm() / want.norm()) <= FACTORS
+
+
+@pytest.mark.parametrize("outputs,inputs", [(192, 64), (64, 576), (300, 129)])
+def test_a_layer_in_flatten_order_moves_as_its_transpose(outputs, inputs):
+    """[outputs][inputs] by default and [inputs][filters] with `flattened`: the same update of the same layer."""
+    from paper_1811_03617_b200 import gvq
+    gen = torch.Generator(device="cuda").manual_seed(outputs)
+    g, w = (torch.randn((outputs, inputs), generator=gen, device="cuda") for _ in range(2))
+    moved = []
+    for flat in (False, True):
+        ctx = gvq.Context(gvq.HostLayout(64, 4, [0], [outputs * inputs]))
+        shape = (inputs, outputs) if flat else (outputs, inputs)
+        plan = gvq.OrthoPlan(ctx, [shape[0]], [shape[1]], flattened=flat)
+        gf, wf = [(x.t() if flat else x).contiguous().view(-1) for x in (g, w)]
+        plan.step(gf, torch.zeros_like(gf), wf, lr=0.5, beta=0.0, nesterov=False)
+        moved.append((wf.view(shape).t() if flat else wf.view(shape)) - w)
+    assert float((moved[0] - moved[1]).norm() / moved[0].norm()) <= 2 * FACTORS
+    want = -0.5 * max(1.0, outputs / inputs) ** 0.5 * (exact(g) if outputs <= inputs else exact(g.t()).t())
+    assert float((moved[1].double() - want).norm() / want.norm()) <= FACTORS + 1e-6

@@ -164,3 +164,26 @@ def test_operands_are_on_the_context_s_device(made):
         with pytest.raises(ValueError):
             call()
     assert len(fake.names()) == 3
+
+
+def test_scales_of_layers_in_flatten_order(made, monkeypatch):
+    """[inputs][filters]: the factor grows with the columns.  Otherwise the library's default, rows over columns, is left alone."""
+    from paper_1811_03617_b200 import gvq
+    ctx, fake = made
+    ctx.n_layers = 4
+    ctx.layout = SimpleNamespace(c=gvq._Layout())
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: Device(256))
+
+    def scales(**kw):
+        plan = gvq.OrthoPlan(ctx, [64, 16, 0, 10], [16, 64, 0, 10], **kw)
+        plan._h = None
+        got = [args for name, args in fake.calls if name == "gvq_ortho_create"][-1][4]
+        return None if got is None else list(got)
+    assert scales() is None
+    assert scales(flattened=True) == [1.0, 2.0, 1.0, 1.0]
+    assert scales(flattened=[True, False, True, False]) == [1.0, 1.0, 1.0, 1.0]
+    assert scales(flattened=[False, True, False, True]) == [2.0, 2.0, 1.0, 1.0]
+    assert scales(scales=[3.0, 1.0, 1.0, 0.5]) == [3.0, 1.0, 1.0, 0.5]
+    for bad in (dict(flattened=[True]), dict(flattened=True, scales=[1.0] * 4)):
+        with pytest.raises(ValueError):
+            scales(**bad)
