@@ -125,7 +125,7 @@ def test_a_layer_in_flatten_order_moves_as_its_transpose(outputs, inputs):
         ctx = gvq.Context(gvq.HostLayout(64, 4, [0], [outputs * inputs]))
         shape = (inputs, outputs) if flat else (outputs, inputs)
         plan = gvq.OrthoPlan(ctx, [shape[0]], [shape[1]], flattened=flat)
-        gf, wf = [(x.t() if flat else x).contiguous().view(-1) for x in (g, w)]
+        gf, wf = [(x.t() if flat else x).clone(memory_format=torch.contiguous_format).view(-1) for x in (g, w)]
         plan.step(gf, torch.zeros_like(gf), wf, lr=0.5, beta=0.0, nesterov=False)
         moved.append((wf.view(shape).t() if flat else wf.view(shape)) - w)
     assert float((moved[0] - moved[1]).norm() / moved[0].norm()) <= 2 * FACTORS
