@@ -523,6 +523,17 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                                 at.n0 + half * COLS + 64 * p, at.m0 + 128 * rank + 32 * q, fetched + warp - 2);
             }
         };
+        // A's low halves, a lane's row of a piece, by plain loads a piece ahead (short sides only; rows of ldr entries, a multiple of 32)
+        uint4 lows[8];
+        auto fetch_lows = [&](const Seen &at, int n) {
+            const Matrix &m = prm.dev.mats[at.matrix];
+            const int row = at.m0 + 128 * rank + 32 * q + lane;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                lows[j] = make_uint4(0, 0, 0, 0);
+                if (m.split > 0 && row < at.M && n + 8 * j < m.ldr) lows[j] = *reinterpret_cast<const uint4 *>(m.gram_lo + (int64_t)row * m.ldr + n + 8 * j);
+            }
+        };
         Weights<T> weights;
         auto fetch_weights = [&](const Seen &at, int n) {
             const int m0 = at.m0 + 128 * rank + 32 * q;
@@ -534,6 +545,7 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
             if (PHASE == kApply) fence_proxy_async_global();      // (X's first low halves were written by plain stores)
             fetch(here);
         }
+        if (PHASE == kPoly && LOW) fetch_lows(here, here.n0 + half * COLS);
         if (PHASE == kLast) fetch_weights(here, here.n0 + half * COLS);
         uint32_t u = 0, stores = 0;
         for (int t = t_begin; t < t_end; ++t, ++u) {
@@ -711,14 +723,11 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                 if (PHASE == kPoly) {        // P = a I + b A + c A^2
                     if (live) {
                         unsigned char *to = mine + p * 4096;
-                        const __half *lows = low && lane < rows ? mx.gram_lo + (int64_t)(m0 + lane) * mx.ldr + n0 : nullptr;
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             const uint4 hi = *reinterpret_cast<const uint4 *>(to + lane * 128 + ((j ^ (lane & 7)) << 4));
                             const uint32_t w[4] = {hi.x, hi.y, hi.z, hi.w};
-                            uint4 lo = make_uint4(0, 0, 0, 0);       // (rows are ldr entries, a multiple of 32, long)
-                            if (LOW && lows && n0 + 8 * j < mx.ldr) lo = *reinterpret_cast<const uint4 *>(lows + 8 * j);
-                            const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w};
+                            const uint32_t l[4] = {lows[j].x, lows[j].y, lows[j].z, lows[j].w};
 #pragma unroll
                             for (int e = 0; e < 8; ++e) {
                                 const float2 x = unpack_half2(w[e >> 1]);
@@ -732,6 +741,7 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                                 if (n0 + 8 * j + e == m0 + lane) r += kA * kGramScale;
                             }
                         }
+                        if (LOW && p + 1 < PIECES) fetch_lows(here, n0 + 64);
                         stage_swizzled16<__half>(to, lane, v[0], v[1]);       // (in place: a lane has read its row of the piece)
                         store(to, kPolyOut, n0);
                         // P's low halves: only of short sides that the first piece holds, so that the other area is free
@@ -741,7 +751,10 @@ __global__ void __launch_bounds__(Shape<CG>::THREADS, 1) product_kernel(const __
                             store(mine + 4096, kPolyLoOut, n0);
                         }
                     }
-                    if (p == PIECES - 1) fetch_next();
+                    if (p == PIECES - 1) {
+                        if (LOW && t + 1 < t_end) fetch_lows(next, next.n0 + half * COLS);
+                        fetch_next();
+                    }
                     continue;
                 }
                 if (PHASE == kGram && live) {       // A = X X^T
