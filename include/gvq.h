@@ -144,6 +144,7 @@ gvq_status gvq_select_k(const float *evals, int d, double lambda_loss, int32_t *
    room for the TMA descriptors of up to 128 gradient buffers and of one history buffer, two
    partial tiles per SM and a counter per tile for the tensor-core projection.  These are the
    only device allocations the library makes, apart from what gvq_host_prepare adds when asked
+   and the tables of a gvq_ortho_create
    (on the host, the first call with a new node count keeps that count's work split: a few
    hundred integers). */
 gvq_status gvq_create(gvq_ctx **out, const gvq_layout *layout, int device, void *cuda_stream);

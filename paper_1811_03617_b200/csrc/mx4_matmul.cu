@@ -21,7 +21,7 @@
 // Accumulators alternate between two column ranges.  Every mbarrier wait is bounded.
 //
 // Measured on the GPU: 8192 x 16384 x 4096 to bf16 202 us (5.4 PFLOP/s, 82 % of four times the measured bf16 rate, under the
-// power cap), 4096 x 4096 x 8192 49 us (5.6); what a large product waits for is the loads of its operands from L2 (without the
+// power cap), 4096 x 4096 x 8192 50 us (5.4); what a large product waits for is the loads of its operands from L2 (without the
 // MMAs 8192 x 8192 x 8192 takes 162 of its 182 us).  Few rows are bound by a stage's fixed cost in the two issuing lanes, 0.22 us:
 // 16 x 4096 x 16384 16.3 us with a CTA a tile, 7.6 us (4.4 TB/s of codes from L2) with four.
 #include "gvq_internal.h"

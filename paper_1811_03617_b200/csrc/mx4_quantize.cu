@@ -114,8 +114,9 @@ __device__ __forceinline__ uint4 quantize_block(const uint32_t (&w)[8 * sizeof(T
 //                another eight words per 32 rows put the four blocks of eight columns that a warp works on in different
 //                banks, and a warp's four lanes write 64 bytes of one output row
 // Bound by instructions, 8 to 15 an entry and form, most of them integer ones at half rate (a quad a block in "both" cost 4 us
-// more at the size below).  8192 x 4096 bf16 on the GPU, us, floor in bytes 13 a form and 16 for both: columns 17 nearest and
-// 28 stochastic, both 26 and 48; fp32 (floor 23 and 26) 34, 40, 39 and 56.
+// more at the size below).  8192 x 4096 bf16 on the GPU, inputs from memory, us, floor in bytes 13 a form and 16 for both:
+// columns 19.5 nearest and 29.5 stochastic, both 27 and 49; fp32 (floor 23 and 26) 34, 39, 41 and 57.
+// (Of fp32 both ways two CTAs fit an SM; held to the registers of three it takes 57.0 us stochastic, to those of two 58.3.)
 template <typename T, bool SR, bool ROWS, bool COLS>
 __global__ void __launch_bounds__(256, COLS ? 3 : 4) mx4_quantize_kernel(const QuantParams prm)
 {
@@ -248,8 +249,9 @@ __global__ void __launch_bounds__(256, COLS ? 3 : 4) mx4_quantize_kernel(const Q
 // Along the rows only: a lane has a whole block, so that what belongs to a block (its largest entry, its scale, its row's
 // random word) costs a lane once and no shuffles; its 16 bytes of codes lie next to its neighbours'.  With a quad for a
 // block, as in the tile kernel, those were half of 13 instructions an entry, and instructions are what bounds this: 8192 x 4096
-// bf16 nearest 13.2 us on the GPU (the copy rate; the tile kernel 24), stochastic 26; fp32 30.6 and 31.8.  Loads of 32 bytes,
-// whole sectors, where rows start at such boundaries; with 16 bytes each sector is asked for twice (14.4, 26.5; 35.4 and 38.3).
+// bf16 nearest 16.6 us on the GPU (floor 13; 13.4 of an input that L2 still holds), stochastic 26; fp32 30.5 and 29.5 (floor 23).
+// Loads of 32 bytes, whole sectors, where rows start at such boundaries; with 16 bytes each sector is asked for twice (17.3, 26.3;
+// 36 and 38).
 template <typename T, bool SR>
 __global__ void __launch_bounds__(256) mx4_quantize_rows_kernel(const QuantParams prm)
 {
@@ -315,8 +317,9 @@ struct AggParams {
 // A quad of lanes takes a block of a slice and goes through the nodes: eight entries a lane, read once, quantized, and
 // what the codes stand for added (fp32, n ascending; code times power of two is exact, so the only rounding is the
 // sum's).  OUT: the codes and scale bytes are wanted.  Of four nodes' row words each lane of the quad mixes one.
-// Bound by instructions, a third of them the random words': 14.7 million entries of 16 nodes, stochastic, 190 us on the GPU, 80 %
-// of what copying the same bytes takes (153 us).  One launch for slices and tails: a small layout's 3.3 us are its launch.
+// Bound by instructions, a third of them the random words': 14.7 million entries of 16 nodes, stochastic, 188 us a call in a long
+// loop (copying the same bytes: 153), 205 in a burst of three, whose first call's way to the GPU is in it.  Nearest 171.  With the
+// codes, 125 MB more, 250 and 224.  One launch for slices and tails: a small layout's 3.1 us are its launch.
 template <bool SR, bool OUT>
 __global__ void __launch_bounds__(256, 4) mx4_quantize_aggregate_kernel(const __grid_constant__ AggParams prm)
 {
@@ -431,7 +434,9 @@ struct DeqParams {
     int vec;
 };
 
-// A lane takes eight entries of a row, one after the other every node's: four code bytes and the block's scale byte.
+// A lane takes eight entries of a row, one after the other every node's: four code bytes and the block's scale byte.  8192 x 4096
+// 33 us (floor 23); the sum of 16 nodes' 14.7 million entries 123 us (floor 28): bound by the index arithmetic in 64 bits and by
+// four-byte loads.
 template <bool LAYOUT>
 __global__ void __launch_bounds__(256) mx4_dequantize_kernel(const __grid_constant__ DeqParams prm)
 {

@@ -24,13 +24,13 @@ namespace {
 
 constexpr size_t kAlign = 256;
 // A part of a contraction: at least so many stages, at most so many parts.  Against (6, 4), time with (6, 8), (12, 4), (9, 3):
-// 515 x 1027 +0, +3, +3 %; twice 512 x 4608 +10, +0, +6 %; the VGG-16-shaped weights +0, +0, +1 %.
+// 515 x 1027 +0, +2, +2 %; twice 512 x 4608 +0, +0, -8 %; the VGG-16-shaped weights +0, +0, +2 %.
 constexpr int kPartStages = 6, kMaxParts = 4;
 constexpr int kTileCost = 3;      // what a tile costs beyond its contraction, in stages of 64 steps
 // Pairs of CTAs on 256 x 256 tiles from this many multiply-adds of one X P on, 128 x 64 tiles below.  Measured on either side,
-// us per call in pairs / alone: 1500 x 1500 (3.4e9) 285 / 215, four 512 x 4608 (4.8e9) 242 / 249, 1700 x 1700 (4.9e9) 306 / 283,
-// five 1024 x 1024 (5.4e9) 295 / 252, 1850 x 1850 (6.3e9) 267 / 275, six 1024 x 1024 (6.4e9) 305 / 274, six 512 x 4608 (7.2e9)
-// 295 / 315, eight 1024 x 1024 (8.6e9) 306 / 334, 2048 x 2048 (8.6e9) 279 / 317.
+// us per step of bf16 weights in pairs / alone: 1500 x 1500 (3.4e9) 284 / 217, four 512 x 4608 (4.8e9) 262 / 272, 1700 x 1700
+// (4.9e9) 306 / 287, five 1024 x 1024 (5.4e9) 307 / 265, 1850 x 1850 (6.3e9) 277 / 282, six 1024 x 1024 (6.4e9) 317 / 290,
+// six 512 x 4608 (7.2e9) 337 / 354, eight 1024 x 1024 (8.6e9) 316 / 350, 2048 x 2048 (8.6e9) 288 / 326.
 constexpr int64_t kPairWork = 6'800'000'000;
 size_t up(size_t n) { return (n + kAlign - 1) & ~(kAlign - 1); }
 int up32(int n) { return (n + 31) & ~31; }     // rows of the work arrays: whole pieces of 32 entries

@@ -537,11 +537,12 @@ cudaError_t launch_typed(cudaStream_t st, const SmallParams &prm, int n)
 
 }  // namespace
 
-// Whatever fits is faster here, in us against a launch a product (ortho.cu): 64 x 64 18 against 57, 100 x 300 49 / 67, 64 x 1500
-// 46 / 79, 20 x 3333 62 / 97, 128 x 512 62 / 84, 128 x 1000 82 / 88, 32 matrices of up to 64 x 576 40 / 80; but not eight parts of
-// a short side of more than 64, whose sums are four times as long (90 x 2400 128 / 99).  As few parts as fit, or up to four of
-// short sides of up to 64 while a part has more than five blocks of the long side: 64 x 576 40 us with one, 38 with two, 37 with
-// four, 47 with eight; 64 x 1500 46 with four, 50 with eight; 100 x 300 49 with one, 58 with two.
+// Whatever fits is faster here, in us a step of bf16 weights against a launch a product (ortho.cu): 64 x 64 19 against 62,
+// 100 x 300 55 / 77, 64 x 1500 50 / 88, 20 x 3333 66 / 98, 128 x 512 65 / 86, 128 x 1000 87 / 95, 32 matrices of up to 64 x 576
+// 44 / 93; but not eight parts of a short side of more than 64, whose sums are four times as long (90 x 2400 128 / 98).  As few
+// parts as fit, or up to four of short sides of up to 64 while a part has more than five blocks of the long side (the
+// orthogonalisation alone): 64 x 576 40 us with one, 38 with two, 37 with four, 47 with eight; 64 x 1500 46 with four, 50 with
+// eight; 100 x 300 49 with one, 58 with two.
 SmallPlan small_plan(int n, int r, int c, int num_sms)
 {
     SmallPlan p{r <= 64 ? 64 : 128, 1, 0};
