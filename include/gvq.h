@@ -529,6 +529,79 @@ gvq_status gvq_mx4_dequantize_aggregate(gvq_ctx *ctx, const uint8_t *const *code
                                         const uint8_t *const *scales_nodes, const float *const *g_nodes_for_tails, int N,
                                         float *g_sum);
 
+/* ---- 8-bit integers ------------------------------------------------------------------------------------
+   Where four bits lose too much: a matrix in 8-bit integers with one scale a row (a token of the activations, an output
+   channel of the weights), multiplied on the integer tensor path.
+
+   Format.  A matrix [rows][cols] is quantized along its rows: with a = max(max |x|, 2^-100) over a row and r the largest
+   float with r * a <= 127, scale = a / 127 (rounded to float), and an entry stands for code * scale, |code| <= 127.
+     nearest:     code = x * r to the nearest whole number, ties to even (rounded once, from the exact product);
+     stochastic:  code = (floor(16384 x r) + u) >> 14, u = the upper 14 of the 16 bits that the 4-bit format takes for (seed,
+                  node, row, column).  Unbiased to 2^-14 of a step.
+   A row that holds a NaN or an infinity has scale NaN and codes 0 and stands for NaN.
+   codes:  device bytes [rows][16 * ceil(cols / 16)], rows padded by zeros; scales: device float [rows], 4-byte aligned.
+   "Along the columns" means the same of the transposed matrix [cols][rows], as above.
+   Sizes: rows, cols >= 1, below 2^31 - 1024; ceil(rows / 128) * ceil(cols / 128) < 2^31. */
+
+/* Bytes of the codes of a quantized matrix [rows][cols], and of the scratch that quantizing it along its columns takes;
+   -1 on bad sizes. */
+int64_t gvq_i8_codes_bytes(int64_t rows, int64_t cols);
+int64_t gvq_i8_scratch_bytes(int64_t rows, int64_t cols);
+
+/* Quantizes a matrix along its rows (codes, scales) and / or along its columns (codes_t, scales_t).  A pair may be NULL, not
+   both.  x: device, entries of type dtype, rows ld entries apart (ld >= cols; x aligned to its entries' size only -- rows
+   that start at 16-byte boundaries are read faster).  scratch: device, 4-byte aligned, gvq_i8_scratch_bytes(rows, cols);
+   for the rows alone it may be NULL (0 bytes).  Its contents carry nothing from one call to the next. */
+gvq_status gvq_i8_quantize(gvq_ctx *ctx, const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, int rounding,
+                           uint64_t seed, uint32_t node, int8_t *codes, float *scales, int8_t *codes_t, float *scales_t,
+                           void *scratch, size_t scratch_bytes);
+/* What a quantized matrix stands for.  out: device fp32, rows ld floats apart. */
+gvq_status gvq_i8_dequantize(gvq_ctx *ctx, const int8_t *codes, const float *scales, int64_t rows, int64_t cols, float *out,
+                             int64_t ld);
+
+/* The product of two quantized matrices, both quantized along the contraction:
+     out[m][n] = (sum over k < K of a[m][k] * b[n][k]) * a_scale[m] * b_scale[n]
+   The sum of codes is exact (32-bit integers; K <= 131072), the scales are applied in fp32, the result is rounded once to
+   dtype.  a: [M][K], b: [N][K]; out: device, dtype entries, rows ld entries apart (ld >= N), aligned to its entries' size.
+   A linear layer's three products and few rows of a: as for the 4-bit format. */
+gvq_status gvq_i8_matmul(gvq_ctx *ctx, const int8_t *a_codes, const float *a_scales, const int8_t *b_codes, const float *b_scales,
+                         int64_t M, int64_t N, int64_t K, void *out, int dtype, int64_t ld);
+
+/* ---- the gated block ---------------------------------------------------------------------------------------
+   The gated feed-forward block of a network, up to its last projection (any of the products here):
+     g = x Wg^T,  u = x Wu^T,  h = act(g) * u            x: [M][K], Wg and Wu: [F][K], h: [M][F]
+   Both products, the activation and their product are one kernel; sums are fp32, g and u are not rounded on the way to h.
+     act:  silu g / (1 + e^-g);  gelu g (1 + erf(g / sqrt 2)) / 2;  gelu_tanh, its approximation
+           g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2;  relu;  sigmoid 1 / (1 + e^-g)
+   dtype is GVQ_BF16 or GVQ_F16 and is that of all matrices but the weights' gradients.  Every matrix has rows that are its
+   ld_... entries apart and is aligned to its entries' size.  TMA reads rows that start at 16-byte boundaries (ld a multiple
+   of 8): where x or a weight matrix has others, a copy that has is made in the workspace first.
+   workspace: device, 16-byte aligned, gvq_gated_workspace_bytes() bytes: aligned != 0 where every one of x, w_gate and w_up
+   that the call reads has such rows; 0 bytes (NULL) for a forward pass then.  Its contents carry nothing from one call to the
+   next; calls that run at the same time (graphs replayed on two streams) need one each. */
+typedef enum { GVQ_SILU = 0, GVQ_GELU = 1, GVQ_GELU_TANH = 2, GVQ_RELU = 3, GVQ_SIGMOID = 4 } gvq_activation;
+
+int64_t gvq_gated_workspace_bytes(int64_t M, int64_t F, int64_t K, int backward, int aligned);
+/* gate_opt, up_opt: both NULL, or [M][F] that receive g and u (rounded to dtype) for the backward pass. */
+gvq_status gvq_gated_forward(gvq_ctx *ctx, const void *x, int64_t ldx, const void *w_gate, int64_t ld_gate, const void *w_up, int64_t ld_up,
+                             int dtype, int64_t M, int64_t F, int64_t K, int activation, void *h, int64_t ldh, void *gate_opt,
+                             int64_t ld_gate_out, void *up_opt, int64_t ld_up_out, void *workspace, size_t workspace_bytes);
+/* Gradients from dh and what the forward pass kept:
+     dg = dh * u * act'(g),  du = dh * act(g)            (rounded to dtype: they are operands of the products below)
+     dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x     (fp32 sums, rounded once)
+   dx_opt: [M][K]; dw_gate_opt, dw_up_opt: [F][K] of type dw_dtype (GVQ_F32: views of a flat gradient).  Any of the three may be
+   NULL, not all; w_gate and w_up are read for dx only, x for the weights' gradients only.  Gradients are overwritten. */
+gvq_status gvq_gated_backward(gvq_ctx *ctx, const void *dh, int64_t ld_dh, const void *gate, int64_t ld_gate_in, const void *up,
+                              int64_t ld_up_in, const void *x, int64_t ldx, const void *w_gate, int64_t ld_gate, const void *w_up,
+                              int64_t ld_up, int dtype, int64_t M, int64_t F, int64_t K, int activation, void *dx_opt, int64_t ld_dx,
+                              void *dw_gate_opt, int64_t ld_dw_gate, void *dw_up_opt, int64_t ld_dw_up, int dw_dtype, void *workspace,
+                              size_t workspace_bytes);
+/* The block's output from 8-bit integers (tokens and both matrices as gvq_i8_quantize lays them out; K <= 131072): the sums of
+   codes are exact, scales and activation fp32, h rounded once to dtype (any of the three). */
+gvq_status gvq_i8_gated(gvq_ctx *ctx, const int8_t *a_codes, const float *a_scales, const int8_t *gate_codes, const float *gate_scales,
+                        const int8_t *up_codes, const float *up_scales, int64_t M, int64_t F, int64_t K, int activation, void *out, int dtype,
+                        int64_t ld);
+
 /* ---- the orthogonalised update ------------------------------------------------------------------------
    What an aggregated gradient is for.  A plan holds the layers of the context's layout that are matrices (row-major
    [rows][cols] where the layer lies in a flat buffer) and updates all of them in one call:

@@ -1,0 +1,181 @@
+// Backward pass of the gated block (gvq.h, "the gated block"):
+//   dg = dh u act'(g),  du = dh act(g)             gated_slopes_kernel
+//   dx = dg Wg + du Wu                             one product whose contraction has two segments
+//   dWg = dg^T x,  dWu = du^T x                    one launch of two products that have x in common
+// and the copies of operands whose rows do not start at 16-byte boundaries, which TMA cannot address.
+#include "product.cuh"
+
+namespace gvq {
+namespace {
+
+using namespace product;
+
+struct SlopeParams {
+    const void *dh, *g, *u;
+    int64_t ld_dh, ld_g, ld_u;
+    void *dg, *du;             // rows ld_out entries apart, starting at 16-byte boundaries
+    int64_t rows, cols, ld_out;
+    int chunks;                // groups of eight columns of a row
+    int vec;                   // all rows start at 16-byte boundaries
+};
+
+template <typename T>
+__device__ __forceinline__ void load_eight(const void *p, int64_t at, int n, bool vec, float (&v)[8])
+{
+    T e[8];
+    const T *from = static_cast<const T *>(p) + at;
+    if (vec && n >= 8) {
+        const uint4 q = __ldcs(reinterpret_cast<const uint4 *>(from));
+        memcpy(e, &q, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = i < n ? from[i] : T(0.0f);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = to_f(e[i]);
+}
+
+// Eight entries a thread, each read and written once.
+template <typename T, int ACT>
+__global__ void __launch_bounds__(256) gated_slopes_kernel(const SlopeParams prm)
+{
+    launch_dependents();
+    grid_dependency_wait();
+    const int64_t total = prm.rows * prm.chunks;
+    for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < total; it += (int64_t)gridDim.x * 256) {
+        const int64_t r = it / prm.chunks;
+        const int c = (int)(it - r * prm.chunks) * 8, n = (int)min((int64_t)8, prm.cols - c);
+        float dh[8], g[8], u[8];
+        load_eight<T>(prm.dh, r * prm.ld_dh + c, n, prm.vec, dh);
+        load_eight<T>(prm.g, r * prm.ld_g + c, n, prm.vec, g);
+        load_eight<T>(prm.u, r * prm.ld_u + c, n, prm.vec, u);
+        uint32_t dg[4], du[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 a = activation_and_slope<ACT>(g[2 * i]), b = activation_and_slope<ACT>(g[2 * i + 1]);
+            dg[i] = pack2<T>(dh[2 * i] * u[2 * i] * a.y, dh[2 * i + 1] * u[2 * i + 1] * b.y);
+            du[i] = pack2<T>(dh[2 * i] * a.x, dh[2 * i + 1] * b.x);
+        }
+        const int64_t at = r * prm.ld_out + c;      // (rows are padded to eight entries)
+        *reinterpret_cast<uint4 *>(static_cast<T *>(prm.dg) + at) = make_uint4(dg[0], dg[1], dg[2], dg[3]);
+        *reinterpret_cast<uint4 *>(static_cast<T *>(prm.du) + at) = make_uint4(du[0], du[1], du[2], du[3]);
+    }
+}
+
+__global__ void __launch_bounds__(256) align_rows_kernel(const uint16_t *from, int64_t ld, uint16_t *to, int64_t ld_to, int64_t rows, int chunks,
+                                                         int64_t cols)
+{
+    launch_dependents();
+    grid_dependency_wait();
+    const int64_t total = rows * chunks;
+    for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < total; it += (int64_t)gridDim.x * 256) {
+        const int64_t r = it / chunks;
+        const int c = (int)(it - r * chunks) * 8;
+        uint16_t e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = c + i < cols ? from[r * ld + c + i] : (uint16_t)0;
+        uint4 q;
+        memcpy(&q, e, 16);
+        *reinterpret_cast<uint4 *>(to + r * ld_to + c) = q;
+    }
+}
+
+Params start(const Launch &l, int dtype, int out_dtype)
+{
+    Params prm = {};
+    prm.dtype = out_dtype;
+    prm.bf16 = dtype == GVQ_BF16;
+    prm.error_word = l.error_word;
+    prm.wait_kcycles = l.wait_kcycles > 0 ? l.wait_kcycles : WAIT_KCYCLES_DEFAULT;
+    prm.test_drop = l.test_drop;
+    return prm;
+}
+
+int grid_of(int num_sms, int64_t items)
+{
+    const int64_t blocks = (items + 255) / 256, most = (int64_t)num_sms * 16;
+    return (int)(blocks < most ? blocks : most);
+}
+
+template <typename T>
+cudaError_t launch_slopes_as(const Launch &l, const SlopeParams &prm, int act)
+{
+    const int grid = grid_of(l.num_sms, prm.rows * prm.chunks);
+    switch (act) {
+    case GVQ_SILU: return launch_chained<gated_slopes_kernel<T, GVQ_SILU>>(prm, grid, 256, 0, 1, l.stream);
+    case GVQ_GELU: return launch_chained<gated_slopes_kernel<T, GVQ_GELU>>(prm, grid, 256, 0, 1, l.stream);
+    case GVQ_GELU_TANH: return launch_chained<gated_slopes_kernel<T, GVQ_GELU_TANH>>(prm, grid, 256, 0, 1, l.stream);
+    case GVQ_RELU: return launch_chained<gated_slopes_kernel<T, GVQ_RELU>>(prm, grid, 256, 0, 1, l.stream);
+    default: return launch_chained<gated_slopes_kernel<T, GVQ_SIGMOID>>(prm, grid, 256, 0, 1, l.stream);
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_align_rows(const Launch &l, const void *from, int64_t ld, void *to, int64_t ld_to, int64_t rows, int64_t cols)
+{
+    const int chunks = (int)((cols + 7) / 8);
+    align_rows_kernel<<<grid_of(l.num_sms, rows * chunks), 256, 0, l.stream>>>(static_cast<const uint16_t *>(from), ld,
+                                                                               static_cast<uint16_t *>(to), ld_to, rows, chunks, cols);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_gated_slopes(const Launch &l, const void *dh, int64_t ld_dh, const void *g, int64_t ld_g, const void *u, int64_t ld_u,
+                                int dtype, int64_t rows, int64_t cols, int act, void *dg, void *du, int64_t ld_out)
+{
+    auto aligned = [](const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % 8 == 0; };
+    SlopeParams prm = {dh, g, u, ld_dh, ld_g, ld_u, dg, du, rows, cols, ld_out, (int)((cols + 7) / 8),
+                       aligned(dh, ld_dh) && aligned(g, ld_g) && aligned(u, ld_u)};
+    return dtype == GVQ_BF16 ? launch_slopes_as<__nv_bfloat16>(l, prm, act) : launch_slopes_as<__half>(l, prm, act);
+}
+
+cudaError_t launch_gated_dx(const Launch &l, const void *dg, const void *du, int64_t ld_d, const void *gate, int64_t ld_gate, const void *up,
+                            int64_t ld_up, int dtype, int64_t M, int64_t F, int64_t K, void *dx, int64_t ld)
+{
+    Params prm = start(l, dtype, dtype);
+    const Cut c = cut(l.num_sms, M, K, 64);
+    prm.M = c.swapped ? K : M;
+    prm.N = c.swapped ? M : K;
+    divide(prm, l.num_sms, c, k16, c.bn, F, 2, 1);
+    // the weights are MN-major here: boxes of 64 of a row's entries by 64 rows
+    CUtensorMap *map_w = c.swapped ? prm.a : prm.b, *map_d = c.swapped ? prm.b : prm.a;
+    const int box_d = c.swapped ? c.bn : 128;
+    if (!encode(l.encode, map_w, k16, gate, F, K, ld_gate, 64) || !encode(l.encode, map_w + 1, k16, up, F, K, ld_up, 64) ||
+        !encode(l.encode, map_d, k16, dg, M, F, ld_d, box_d) || !encode(l.encode, map_d + 1, k16, du, M, F, ld_d, box_d))
+        return cudaErrorInvalidValue;
+    set_output(l.encode, prm, 0, dx, dtype, M, K, ld);
+    if (c.cg == 2) return launch<k16, 2, 256, 1, false, true, false>(l.stream, l.num_sms, prm);
+    if (!c.swapped) return launch<k16, 1, 64, 1, false, true, false>(l.stream, l.num_sms, prm);
+    switch (c.bn) {
+    case 16: return launch<k16, 1, 16, 1, true, false, false>(l.stream, l.num_sms, prm);
+    case 32: return launch<k16, 1, 32, 1, true, false, false>(l.stream, l.num_sms, prm);
+    default: return launch<k16, 1, 64, 1, true, false, false>(l.stream, l.num_sms, prm);
+    }
+}
+
+cudaError_t launch_gated_dw(const Launch &l, const void *dg, const void *du, int64_t ld_d, const void *x, int64_t ldx, int dtype, int64_t M,
+                            int64_t F, int64_t K, void *dw_gate, int64_t ld_dw_gate, void *dw_up, int64_t ld_dw_up, int out_dtype)
+{
+    Params prm = start(l, dtype, out_dtype);
+    prm.M = F;
+    prm.N = K;
+    // (one of the two may not be wanted)
+    const void *d[2] = {dw_gate ? dg : du, du};
+    void *out[2] = {dw_gate ? dw_gate : dw_up, dw_up};
+    const int64_t ld[2] = {dw_gate ? ld_dw_gate : ld_dw_up, ld_dw_up};
+    const int halves = dw_gate && dw_up ? 2 : 1;
+    Cut c;
+    c.swapped = false;
+    c.cg = (int64_t)halves * tiles_of(F, 128) * tiles_of(K, 64) > l.num_sms ? 2 : 1;
+    c.bn = c.cg == 2 ? 256 : 64;
+    divide(prm, l.num_sms, c, k16, c.bn, M, 1, halves);
+    if (!encode(l.encode, &prm.b[0], k16, x, M, K, ldx, 64)) return cudaErrorInvalidValue;
+    for (int i = 0; i < halves; ++i) {
+        if (!encode(l.encode, &prm.a[i], k16, d[i], M, F, ld_d, 64)) return cudaErrorInvalidValue;
+        set_output(l.encode, prm, i, out[i], out_dtype, F, K, ld[i]);
+    }
+    if (c.cg == 2) return launch<k16, 2, 256, 1, true, true, false>(l.stream, l.num_sms, prm);
+    return launch<k16, 1, 64, 1, true, true, false>(l.stream, l.num_sms, prm);
+}
+
+}  // namespace gvq

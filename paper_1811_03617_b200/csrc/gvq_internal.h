@@ -170,6 +170,38 @@ cudaError_t launch_mx4_matmul(cudaStream_t st, int num_sms, EncodeTiledFn enc, c
                               const uint8_t *sb, int64_t M, int64_t N, int64_t K, void *out, int dtype, int64_t ld,
                               int32_t *error_word, int wait_kcycles, int test_drop);
 
+// What a product's launch takes from its context.
+struct Launch {
+    cudaStream_t stream;
+    int num_sms;
+    EncodeTiledFn encode;
+    int32_t *error_word;
+    int wait_kcycles, test_drop;
+};
+// 8-bit integers (i8_quantize.cu, product_i8.cu).  A null pair of outputs is not written; at least one pair is given.
+// scratch: i8_scratch_bytes of the matrix, where it is quantized along its columns.
+int64_t i8_scratch_bytes(int64_t rows, int64_t cols);
+cudaError_t launch_i8_quantize(cudaStream_t st, const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, bool stochastic,
+                               uint64_t seed, uint32_t node, int8_t *codes, float *scales, int8_t *codes_t, float *scales_t, void *scratch);
+cudaError_t launch_i8_dequantize(cudaStream_t st, int num_sms, const int8_t *codes, const float *scales, int64_t rows, int64_t cols,
+                                 float *out, int64_t ld);
+cudaError_t launch_i8_matmul(const Launch &l, const int8_t *a, const float *sa, const int8_t *b, const float *sb, int64_t M, int64_t N,
+                             int64_t K, void *out, int dtype, int64_t ld);
+cudaError_t launch_i8_gated(const Launch &l, const int8_t *a, const float *sa, const int8_t *gate, const float *s_gate, const int8_t *up,
+                            const float *s_up, int64_t M, int64_t F, int64_t K, int act, void *out, int dtype, int64_t ld);
+// The gated block (gated_product.cu, gated_gradient.cu).  Operands' rows start at 16-byte boundaries, apart from those of
+// launch_gated_slopes and launch_align_rows, which write such rows.  g and u, or one of the weights' gradients, may be null.
+cudaError_t launch_gated(const Launch &l, const void *x, int64_t ldx, const void *gate, int64_t ld_gate, const void *up, int64_t ld_up,
+                         int dtype, int64_t M, int64_t F, int64_t K, int act, void *h, int64_t ldh, void *g, int64_t ldg, void *u,
+                         int64_t ldu);
+cudaError_t launch_align_rows(const Launch &l, const void *from, int64_t ld, void *to, int64_t ld_to, int64_t rows, int64_t cols);
+cudaError_t launch_gated_slopes(const Launch &l, const void *dh, int64_t ld_dh, const void *g, int64_t ld_g, const void *u, int64_t ld_u,
+                                int dtype, int64_t rows, int64_t cols, int act, void *dg, void *du, int64_t ld_out);
+cudaError_t launch_gated_dx(const Launch &l, const void *dg, const void *du, int64_t ld_d, const void *gate, int64_t ld_gate, const void *up,
+                            int64_t ld_up, int dtype, int64_t M, int64_t F, int64_t K, void *dx, int64_t ld);
+cudaError_t launch_gated_dw(const Launch &l, const void *dg, const void *du, int64_t ld_d, const void *x, int64_t ldx, int dtype, int64_t M,
+                            int64_t F, int64_t K, void *dw_gate, int64_t ld_dw_gate, void *dw_up, int64_t ld_dw_up, int out_dtype);
+
 // Basis fit.  Workspace layout is private to fit_basis.cu.
 size_t fit_workspace_bytes(int d, int n_layers, int n_fit_tiles);
 struct FitArgs {

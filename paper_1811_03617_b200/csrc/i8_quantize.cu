@@ -1,0 +1,409 @@
+// Quantization to 8-bit integers with a scale a row, and back (gvq.h, "8-bit integers").
+//
+//  i8_rows_kernel     along the rows, read once: a row stays in the registers of the threads that share it
+//  i8_max_kernel      largest magnitudes of columns (and rows) over blocks of the matrix
+//  i8_tile_kernel     along the columns, or both ways, from those: a tile goes through shared memory
+//  i8_dequantize_kernel
+//
+// With a = max(max |x|, 2^-100) and r the largest float with r a <= 127, a code is x r to the nearest whole number, rounded from
+// the exact product: one fused multiply-add to 1.5 * 2^23 leaves it in the low bits, two's complement.  Stochastic rounding adds 14
+// random bits below floor(2^14 x r), which the same instruction leaves there when it rounds down (2^14 * 127 < 2^22).
+#include "gvq_internal.h"
+#include "mx4.cuh"
+#include "row32.cuh"
+#include "sm100_ptx.cuh"
+
+namespace gvq {
+namespace {
+
+constexpr float kMagic = 12582912.0f;               // 1.5 * 2^23: its pattern's low 22 bits are 0
+constexpr int kMaxCols = 256, kMinBlockRows = 256;  // a block of i8_max_kernel
+constexpr int kMaxBlocks = 64;                      // most blocks along the rows
+
+__host__ __device__ inline int64_t pitch_of(int64_t cols) { return (cols + 15) / 16 * 16; }
+__host__ __device__ inline int64_t block_rows(int64_t rows)
+{
+    const int64_t per = (rows + kMaxBlocks - 1) / kMaxBlocks;
+    return per < kMinBlockRows ? kMinBlockRows : (per + 127) / 128 * 128;
+}
+
+// A row's factor and scale from the pattern of its largest magnitude.  A row that holds a NaN or an infinity has factor 0,
+// and the caller's entries are replaced by 0.
+struct RowScale { float r, scale; };
+__device__ __forceinline__ RowScale row_scale(uint32_t top)
+{
+    RowScale s;
+    if (top >= 0x7F800000u) { s.r = 0.0f; s.scale = __uint_as_float(0x7FC00000u); return s; }
+    const float a = fmaxf(__uint_as_float(top), 7.888609052210118e-31f);      // 2^-100
+    s.r = __fdiv_rd(127.0f, a);
+    s.scale = __fdiv_rn(a, 127.0f);
+    return s;
+}
+// Eight codes.  `r` is the row's factor, times 2^14 for stochastic rounding; p0: column pair of the first entry.
+template <bool SR>
+__device__ __forceinline__ uint2 codes_of(const float (&v)[8], float r, uint64_t h, uint32_t p0)
+{
+    uint32_t c[8];
+    if (SR) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = mx4::pair_word(h, p0 + i), y = x >> 16;
+            c[2 * i] = (__float_as_uint(__fmaf_rd(v[2 * i], r, kMagic)) + (((x ^ y) & 0xFFFFu) >> 2)) >> 14;
+            c[2 * i + 1] = (__float_as_uint(__fmaf_rd(v[2 * i + 1], r, kMagic)) + (y >> 2)) >> 14;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = __float_as_uint(__fmaf_rn(v[i], r, kMagic));
+    }
+    uint2 q;
+    q.x = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+    q.y = __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410);
+    return q;
+}
+
+// Eight consecutive entries as they lie in memory; past the n-th: 0.
+template <typename T> struct Raw8 { uint4 q[sizeof(T) / 2]; };
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8(const T *p, int n, bool vec)
+{
+    Raw8<T> r;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.q[i] = make_uint4(0, 0, 0, 0);
+    if (n >= 8 && vec) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.q[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+    } else if (n > 0) {
+        T e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = i < n ? p[i] : T(0.0f);
+        memcpy(&r, e, sizeof(r));
+    }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void unpack8(const Raw8<T> &r, float (&v)[8])
+{
+    T e[8];
+    memcpy(e, &r, sizeof(r));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = to_f(e[i]);
+}
+// Pattern of the largest magnitude: patterns without their sign order like the magnitudes, infinity and NaN above all.
+template <typename T>
+__device__ __forceinline__ uint32_t top8(const Raw8<T> &r)
+{
+    if constexpr (sizeof(T) == 4) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            m = max(m, max(r.q[i].x & 0x7FFFFFFFu, r.q[i].y & 0x7FFFFFFFu));
+            m = max(m, max(r.q[i].z & 0x7FFFFFFFu, r.q[i].w & 0x7FFFFFFFu));
+        }
+        return m;
+    } else {      // two at a time
+        const uint32_t m = __vmaxu2(__vmaxu2(r.q[0].x & 0x7FFF7FFFu, r.q[0].y & 0x7FFF7FFFu), __vmaxu2(r.q[0].z & 0x7FFF7FFFu, r.q[0].w & 0x7FFF7FFFu));
+        const uint16_t top = (uint16_t)max(m & 0xFFFFu, m >> 16);
+        T e;
+        memcpy(&e, &top, 2);
+        return __float_as_uint(to_f(e));
+    }
+}
+
+struct QuantParams {
+    const void *x;
+    int64_t rows, cols, ld;
+    uint64_t seed_w;            // mix64 of (seed, node)
+    int8_t *codes, *codes_t;    // along the rows, along the columns; null: not wanted
+    float *scales, *scales_t;
+    uint32_t *col_top, *row_top;   // [blocks along the rows][cols], [blocks along the columns][rows]: patterns of magnitudes
+    int64_t block_rows;
+    int row_blocks, col_blocks;
+    int vec;                    // rows start at 16-byte boundaries
+    int ct;                     // tiles along the columns
+};
+
+// G threads share a row, KEEP groups of eight entries a thread in registers; longer rows are read again from L2.
+template <typename T, bool SR, int G>
+__global__ void __launch_bounds__(G < 256 ? 256 : G) i8_rows_kernel(const QuantParams prm)
+{
+    constexpr int KEEP = 4, NT = G < 256 ? 256 : G, ROWS = NT / G;
+    __shared__ uint32_t tops[NT / 32];
+    ptx::launch_dependents();
+    ptx::grid_dependency_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, in_row = threadIdx.x % G;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / G;
+    const bool there = row < prm.rows;
+    const T *x = static_cast<const T *>(prm.x) + (there ? row : 0) * prm.ld;
+    const int64_t pitch = pitch_of(prm.cols), groups = there ? pitch / 8 : 0;
+    auto load = [&](int64_t at) { return load8(x + at * 8, (int)min((int64_t)8, prm.cols - at * 8), prm.vec); };
+    Raw8<T> kept[KEEP];
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) {
+        const int64_t at = in_row + i * G;
+        if (at < groups) kept[i] = load(at);
+    }
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i)
+        if (in_row + i * G < groups) top = max(top, top8(kept[i]));
+    for (int64_t at = in_row + KEEP * G; at < groups; at += G) top = max(top, top8(load(at)));
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (G > 32) {
+        if (lane == 0) tops[warp] = top;
+        __syncthreads();
+        constexpr int WARPS = G / 32;
+        top = 0;
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) top = max(top, tops[warp / WARPS * WARPS + i]);
+    }
+    const RowScale s = row_scale(top);
+    const bool fine = top < 0x7F800000u;
+    const uint64_t h = SR ? mx4::row_word(prm.seed_w, row) : 0;
+    const float r = SR ? s.r * 16384.0f : s.r;
+    auto write = [&](int64_t at, const Raw8<T> &raw) {
+        float v[8];
+        unpack8(raw, v);
+        *reinterpret_cast<uint2 *>(prm.codes + row * pitch + at * 8) = fine ? codes_of<SR>(v, r, h, (uint32_t)(at * 4)) : make_uint2(0, 0);
+    };
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i)
+        if (in_row + i * G < groups) write(in_row + i * G, kept[i]);
+    for (int64_t at = in_row + KEEP * G; at < groups; at += G) write(at, load(at));
+    if (there && in_row == 0) prm.scales[row] = s.scale;
+}
+
+// A CTA: block_rows rows x 256 columns; a warp goes along rows, a lane has eight columns.
+template <typename T, bool ROWS>
+__global__ void __launch_bounds__(256) i8_max_kernel(const QuantParams prm)
+{
+    __shared__ uint32_t tops[8][kMaxCols];
+    ptx::launch_dependents();
+    ptx::grid_dependency_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int cb = blockIdx.x % prm.col_blocks, rb = blockIdx.x / prm.col_blocks;
+    const int64_t c0 = (int64_t)cb * kMaxCols, c = c0 + lane * 8;
+    const int64_t r0 = (int64_t)rb * prm.block_rows, r1 = min(prm.rows, r0 + prm.block_rows);
+    const int n = (int)max((int64_t)0, min((int64_t)8, prm.cols - c));
+    const T *x = static_cast<const T *>(prm.x);
+    uint32_t m[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m[i] = 0;
+    constexpr int U = 4;
+    for (int64_t r = r0 + warp; r < r1; r += 8 * U) {
+        Raw8<T> raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = load8(x + (r + 8 * u) * prm.ld + c, r + 8 * u < r1 ? n : 0, prm.vec);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float v[8];
+            unpack8(raw[u], v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m[i] = max(m[i], __float_as_uint(v[i]) & 0x7FFFFFFFu);
+            if (ROWS) {
+                const uint32_t t = __reduce_max_sync(0xffffffffu, top8(raw[u]));
+                if (lane == 0 && r + 8 * u < r1) prm.row_top[(int64_t)cb * prm.rows + r + 8 * u] = t;
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) tops[warp][lane * 8 + i] = m[i];
+    __syncthreads();
+    uint32_t t = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) t = max(t, tops[w][threadIdx.x]);
+    if (c0 + threadIdx.x < prm.cols) prm.col_top[(int64_t)rb * prm.cols + c0 + threadIdx.x] = t;
+}
+
+// A CTA: a tile of 128 x 128 entries.  It lies in shared memory in its own type, rows 4 words longer than they are and another 4
+// words on every 16 rows, so that eight lanes' 16-byte words of eight rows, and the words of 4 columns in 8 runs of 16 rows, lie in
+// different banks.  A thread takes 16 entries of a column (of two columns of a 16-bit type, so that a word is read once): eight
+// lanes write 128 bytes of an output row.
+template <typename T, bool SR, bool ROWS>
+__global__ void __launch_bounds__(256) i8_tile_kernel(const QuantParams prm)
+{
+    constexpr int W = 128 * (int)sizeof(T) / 4, PITCH = W + 4;    // words of a row of the tile
+    extern __shared__ uint4 smem_q[];
+    uint32_t *tile = reinterpret_cast<uint32_t *>(smem_q);
+    __shared__ RowScale of_col[128], of_row[128];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    ptx::launch_dependents();
+    ptx::grid_dependency_wait();
+    const int rtile = blockIdx.x / prm.ct, ctile = blockIdx.x - rtile * prm.ct;
+    const int64_t r0 = (int64_t)rtile * 128, c0 = (int64_t)ctile * 128;
+    const T *x = static_cast<const T *>(prm.x);
+    auto at = [&](int row) { return tile + row * PITCH + (row >> 4) * 4; };
+
+    // warp w, iteration it: rows 16 w + 2 it + (lane >> 4)
+    const int cl = (lane & 15) * 8;
+    const int ncol = (int)min((int64_t)8, prm.cols - (c0 + cl));    // this lane's valid entries (<= 0: none)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        Raw8<T> raw[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t r = r0 + 16 * warp + 2 * (4 * half + i) + (lane >> 4);
+            raw[i] = load8(x + r * prm.ld + c0 + cl, r < prm.rows ? ncol : 0, prm.vec);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t *to = at(16 * warp + 2 * (4 * half + i) + (lane >> 4)) + (lane & 15) * (int)sizeof(T) * 2;
+#pragma unroll
+            for (int q = 0; q < (int)sizeof(T) / 2; ++q) *reinterpret_cast<uint4 *>(to + q * 4) = raw[i].q[q];
+        }
+    }
+    if (tid < 128) {
+        uint32_t top = 0;
+        if (c0 + tid < prm.cols)
+            for (int b = 0; b < prm.row_blocks; ++b) top = max(top, __ldg(prm.col_top + (int64_t)b * prm.cols + c0 + tid));
+        const RowScale s = row_scale(top);
+        of_col[tid] = s;
+        if (rtile == 0 && c0 + tid < prm.cols) prm.scales_t[c0 + tid] = s.scale;
+    } else if (ROWS) {
+        const int64_t r = r0 + tid - 128;
+        uint32_t top = 0;
+        if (r < prm.rows)
+            for (int b = 0; b < prm.col_blocks; ++b) top = max(top, __ldg(prm.row_top + (int64_t)b * prm.rows + r));
+        const RowScale s = row_scale(top);
+        of_row[tid - 128] = s;
+        if (ctile == 0 && r < prm.rows) prm.scales[r] = s.scale;
+    }
+    __syncthreads();
+    if (ROWS) {
+        const int64_t pitch = pitch_of(prm.cols);
+#pragma unroll 1
+        for (int it = 0; it < 4; ++it) {
+            const int item = it * 256 + tid, row = item >> 3, b = item & 7;
+            const int64_t r = r0 + row, c = c0 + b * 16;
+            if (r >= prm.rows || c >= pitch) continue;
+            const uint32_t *from = at(row) + b * 4 * (int)sizeof(T);
+            const RowScale s = of_row[row];
+            const uint64_t h = SR ? mx4::row_word(prm.seed_w, r) : 0;
+            uint2 q[2];
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+                Raw8<T> raw;
+#pragma unroll
+                for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw.q[i] = *reinterpret_cast<const uint4 *>(from + (o * (int)sizeof(T) / 2 + i) * 4);
+                float v[8];
+                unpack8(raw, v);
+                q[o] = s.scale == s.scale ? codes_of<SR>(v, SR ? s.r * 16384.0f : s.r, h, (uint32_t)((c + 8 * o) >> 1)) : make_uint2(0, 0);
+            }
+            *reinterpret_cast<uint4 *>(prm.codes + r * pitch + c) = make_uint4(q[0].x, q[0].y, q[1].x, q[1].y);
+        }
+    }
+    constexpr int PER = 4 / (int)sizeof(T);                 // columns of a word: 1 or 2
+    const int64_t pitch_t = pitch_of(prm.rows);
+    const int blk = lane & 7;
+#pragma unroll 1
+    for (int cw = warp * 4 + (lane >> 3); cw < W; cw += 32) {
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = at(blk * 16 + i)[cw];
+#pragma unroll
+        for (int part = 0; part < PER; ++part) {
+            const int col = cw * PER + part;
+            const int64_t c = c0 + col, r = r0 + blk * 16;
+            if (c >= prm.cols || r >= pitch_t) continue;
+            const RowScale s = of_col[col];
+            const uint64_t h = SR ? mx4::row_word(prm.seed_w, c) : 0;
+            uint2 q[2];
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t word = w[8 * o + e];
+                    if (sizeof(T) == 4) v[e] = __uint_as_float(word);
+                    else {
+                        T t;
+                        const uint16_t u = (uint16_t)(part ? word >> 16 : word & 0xFFFFu);
+                        memcpy(&t, &u, sizeof(t) < 2 ? sizeof(t) : 2);
+                        v[e] = to_f(t);
+                    }
+                }
+                q[o] = s.scale == s.scale ? codes_of<SR>(v, SR ? s.r * 16384.0f : s.r, h, (uint32_t)((r + 8 * o) >> 1)) : make_uint2(0, 0);
+            }
+            *reinterpret_cast<uint4 *>(prm.codes_t + c * pitch_t + r) = make_uint4(q[0].x, q[0].y, q[1].x, q[1].y);
+        }
+    }
+}
+
+__global__ void __launch_bounds__(256) i8_dequantize_kernel(const int8_t *codes, const float *scales, int64_t rows, int64_t cols, float *out,
+                                                            int64_t ld)
+{
+    ptx::launch_dependents();
+    ptx::grid_dependency_wait();
+    const int64_t pitch = pitch_of(cols), quads = (cols + 3) / 4, total = rows * quads;
+    for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < total; it += (int64_t)gridDim.x * 256) {
+        const int64_t r = it / quads, c = (it - r * quads) * 4;
+        const char4 q = *reinterpret_cast<const char4 *>(codes + r * pitch + c);
+        const float s = scales[r], v[4] = {q.x * s, q.y * s, q.z * s, q.w * s};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + i < cols) out[r * ld + c + i] = v[i];
+    }
+}
+
+template <typename T, bool SR>
+cudaError_t quantize_rows(cudaStream_t st, const QuantParams &prm)
+{
+    // a row's threads: as few as keep it in registers, where there are rows enough
+    auto grid = [&](int rows) { return (int)((prm.rows + rows - 1) / rows); };
+    if (prm.cols <= 1024) return ptx::launch_chained<i8_rows_kernel<T, SR, 32>>(prm, grid(8), 256, 0, 1, st);
+    if (prm.cols <= 4096 && prm.rows > 512) return ptx::launch_chained<i8_rows_kernel<T, SR, 128>>(prm, grid(2), 256, 0, 1, st);
+    if (prm.cols <= 8192) return ptx::launch_chained<i8_rows_kernel<T, SR, 256>>(prm, grid(1), 256, 0, 1, st);
+    return ptx::launch_chained<i8_rows_kernel<T, SR, 1024>>(prm, grid(1), 1024, 0, 1, st);
+}
+
+template <typename T, bool SR>
+cudaError_t quantize_as(cudaStream_t st, QuantParams prm)
+{
+    if (!prm.codes_t) return quantize_rows<T, SR>(st, prm);
+    const int blocks = prm.row_blocks * prm.col_blocks;
+    cudaError_t e = prm.codes ? ptx::launch_chained<i8_max_kernel<T, true>>(prm, blocks, 256, 0, 1, st)
+                              : ptx::launch_chained<i8_max_kernel<T, false>>(prm, blocks, 256, 0, 1, st);
+    if (e != cudaSuccess) return e;
+    const int tiles = (int)(mx4::tiles_of(pitch_of(prm.rows), 128) * prm.ct);
+    const size_t smem = (128 * (128 * sizeof(T) / 4 + 4) + 32) * 4;
+    return prm.codes ? ptx::launch_chained<i8_tile_kernel<T, SR, true>>(prm, tiles, 256, smem, 1, st)
+                     : ptx::launch_chained<i8_tile_kernel<T, SR, false>>(prm, tiles, 256, smem, 1, st);
+}
+
+}  // namespace
+
+int64_t i8_scratch_bytes(int64_t rows, int64_t cols)
+{
+    const int64_t rb = (rows + block_rows(rows) - 1) / block_rows(rows), cb = (cols + kMaxCols - 1) / kMaxCols;
+    return (rb * cols + cb * rows) * 4;
+}
+
+cudaError_t launch_i8_quantize(cudaStream_t st, const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, bool stochastic,
+                               uint64_t seed, uint32_t node, int8_t *codes, float *scales, int8_t *codes_t, float *scales_t, void *scratch)
+{
+    QuantParams prm = {};
+    prm.x = x;
+    prm.rows = rows; prm.cols = cols; prm.ld = ld;
+    prm.seed_w = mx4::seed_word(seed, node);
+    prm.codes = codes; prm.codes_t = codes_t;
+    prm.scales = scales; prm.scales_t = scales_t;
+    prm.block_rows = block_rows(rows);
+    prm.row_blocks = (int)((rows + prm.block_rows - 1) / prm.block_rows);
+    prm.col_blocks = (int)((cols + kMaxCols - 1) / kMaxCols);
+    prm.col_top = static_cast<uint32_t *>(scratch);
+    prm.row_top = prm.col_top + (int64_t)prm.row_blocks * cols;
+    prm.vec = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && ld * (dtype == GVQ_F32 ? 4 : 2) % 16 == 0;
+    prm.ct = (int)mx4::tiles_of(pitch_of(cols), 128);
+    if (dtype == GVQ_F32) return stochastic ? quantize_as<float, true>(st, prm) : quantize_as<float, false>(st, prm);
+    if (dtype == GVQ_BF16) return stochastic ? quantize_as<__nv_bfloat16, true>(st, prm) : quantize_as<__nv_bfloat16, false>(st, prm);
+    return stochastic ? quantize_as<__half, true>(st, prm) : quantize_as<__half, false>(st, prm);
+}
+
+cudaError_t launch_i8_dequantize(cudaStream_t st, int num_sms, const int8_t *codes, const float *scales, int64_t rows, int64_t cols,
+                                 float *out, int64_t ld)
+{
+    const int64_t blocks = (rows * ((cols + 3) / 4) + 255) / 256, most = (int64_t)num_sms * 16;
+    i8_dequantize_kernel<<<(int)(blocks < most ? blocks : most), 256, 0, st>>>(codes, scales, rows, cols, out, ld);
+    return cudaGetLastError();
+}
+
+}  // namespace gvq

@@ -104,6 +104,20 @@ def lib() -> ctypes.CDLL:
         L.gvq_mx4_matmul.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, vp, i32, i64]
         L.gvq_mx4_quantize_aggregate.argtypes = [vp, vp, i32, u32, i32, u64, vp, vp, vp]
         L.gvq_mx4_dequantize_aggregate.argtypes = [vp, vp, vp, vp, i32, vp]
+        sz = ctypes.c_size_t
+        L.gvq_i8_codes_bytes.restype = i64
+        L.gvq_i8_codes_bytes.argtypes = [i64, i64]
+        L.gvq_i8_scratch_bytes.restype = i64
+        L.gvq_i8_scratch_bytes.argtypes = [i64, i64]
+        L.gvq_i8_quantize.argtypes = [vp, vp, i32, i64, i64, i64, i32, u64, u32, vp, vp, vp, vp, vp, sz]
+        L.gvq_i8_dequantize.argtypes = [vp, vp, vp, i64, i64, vp, i64]
+        L.gvq_i8_matmul.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, vp, i32, i64]
+        L.gvq_i8_gated.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i32, vp, i32, i64]
+        L.gvq_gated_workspace_bytes.restype = i64
+        L.gvq_gated_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+        L.gvq_gated_forward.argtypes = [vp, vp, i64, vp, i64, vp, i64, i32, i64, i64, i64, i32, vp, i64, vp, i64, vp, i64, vp, sz]
+        L.gvq_gated_backward.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i32, i64, i64, i64, i32, vp, i64, vp, i64,
+                                         vp, i64, i32, vp, sz]
         i32p = ctypes.POINTER(ctypes.c_int32)
         L.gvq_ortho_workspace_bytes.restype = i64
         L.gvq_ortho_workspace_bytes.argtypes = [LP, i32p, i32p]
@@ -345,6 +359,64 @@ class Mx4:
         return self._views()[1]
 
 
+class I8:
+    """A matrix [rows][cols] in 8-bit integers with a scale a row: device `codes` (int8 [rows, 16 * ceil(cols / 16)]) and `scales`
+    (float32 [rows]); see gvq.h."""
+
+    __slots__ = ("rows", "cols", "device", "_codes", "_scales", "_buf", "codes_ptr", "scales_ptr")
+
+    def __init__(self, rows: int, cols: int, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                 device=None):
+        rows, cols = int(rows), int(cols)
+        if rows < 1 or cols < 1 or max(rows, cols) > 0x7FFFFFFF - 1024 or ((rows + 127) // 128) * ((cols + 127) // 128) >= 0x7FFFFFFF:
+            raise ValueError(f"no 8-bit matrix of {rows} x {cols}")
+        self.rows, self.cols = rows, cols
+        pitch = (cols + 15) & ~15
+        if codes is None and scales is None:       # one allocation for both
+            at = (rows * pitch + 255) & ~255
+            self._buf = buf = torch.empty(at + 4 * rows, dtype=torch.int8, device=device or "cuda")
+            self._codes = None
+            self.device = buf.get_device()
+            self.codes_ptr = p = buf.data_ptr()
+            self.scales_ptr = p + at
+            return
+        if codes is None or scales is None:
+            raise ValueError("codes and scales come together")
+        for t, n, dtype in ((codes, rows * pitch, torch.int8), (scales, rows, _F32)):
+            if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.numel() != n:
+                raise ValueError(f"an 8-bit matrix of {rows} x {cols} has int8 codes [{rows}, {pitch}] and float32 scales [{rows}], contiguous")
+        self.device = codes.get_device()
+        if scales.get_device() != self.device:
+            raise ValueError("codes and scales are on one device")
+        self._codes, self._scales = codes, scales
+        self.codes_ptr, self.scales_ptr = codes.data_ptr(), scales.data_ptr()
+
+    def _views(self):
+        if self._codes is None:
+            pitch, at = (self.cols + 15) & ~15, self.scales_ptr - self.codes_ptr
+            self._codes = self._buf[:self.rows * pitch].view(self.rows, pitch)
+            self._scales = self._buf[at:at + 4 * self.rows].view(_F32)
+        return self._codes, self._scales
+
+    @property
+    def codes(self) -> torch.Tensor:
+        return self._views()[0]
+
+    @property
+    def scales(self) -> torch.Tensor:
+        return self._views()[1]
+
+
+ACTIVATION = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
+
+
+def _activation(name: str) -> int:
+    a = ACTIVATION.get(name)
+    if a is None:
+        raise ValueError(f"activation {name!r}: one of {', '.join(ACTIVATION)} is wanted")
+    return a
+
+
 class Context:
     """gvq_ctx for one layout on one CUDA device."""
 
@@ -526,6 +598,180 @@ class Context:
                                       out.data_ptr(), _dtype(out), ld)
         if status:
             raise GvqError(status, "gvq_mx4_matmul")
+        return out
+
+    # ---- 8-bit integers ---------------------------------------------------------------------
+    def _i8(self, x, by_rows, by_cols, stochastic, seed, node, out=None, out_t=None):
+        rows, cols, ld = _rows(x, self.device, "i8_quantize")
+        dtype = _dtype(x)
+        c = s = ct = st = scratch = None
+        n_scratch = 0
+        if by_rows:
+            if out is None:
+                out = I8(rows, cols, device=x.device)
+            elif out.rows != rows or out.cols != cols or out.device != self.device:
+                raise ValueError("i8_quantize: the output is of another size or on another device")
+            c, s = out.codes_ptr, out.scales_ptr
+        if by_cols:
+            if out_t is None:
+                out_t = I8(cols, rows, device=x.device)
+            elif out_t.rows != cols or out_t.cols != rows or out_t.device != self.device:
+                raise ValueError("i8_quantize: the output is of another size or on another device")
+            ct, st = out_t.codes_ptr, out_t.scales_ptr
+            n_scratch = lib().gvq_i8_scratch_bytes(rows, cols)
+            if n_scratch < 0:
+                raise ValueError(f"no 8-bit matrix of {rows} x {cols}")
+            kept = torch.empty(n_scratch, dtype=torch.uint8, device=x.device)
+            scratch = kept.data_ptr()
+        self._sync_stream()
+        status = lib().gvq_i8_quantize(self._h, x.data_ptr(), dtype, rows, cols, ld, 1 if stochastic else 0, seed, node, c, s, ct, st,
+                                       scratch, n_scratch)
+        if status:
+            raise GvqError(status, "gvq_i8_quantize")
+        return out, out_t
+
+    def i8_quantize(self, x, stochastic=False, seed=0, node=0, out: Optional[I8] = None) -> I8:
+        """gvq_i8_quantize along the rows of x [rows, cols]."""
+        return self._i8(x, True, False, stochastic, seed, node, out=out)[0]
+
+    def i8_quantize_transposed(self, x, stochastic=False, seed=0, node=0, out: Optional[I8] = None) -> I8:
+        """gvq_i8_quantize along the columns of x: the quantized [cols, rows] matrix."""
+        return self._i8(x, False, True, stochastic, seed, node, out_t=out)[1]
+
+    def i8_quantize_both(self, x, stochastic=False, seed=0, node=0, out: Optional[I8] = None, out_t: Optional[I8] = None):
+        """gvq_i8_quantize along the rows and along the columns: (by rows, by columns)."""
+        return self._i8(x, True, True, stochastic, seed, node, out, out_t)
+
+    def i8_dequantize(self, q: I8, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """gvq_i8_dequantize: what q stands for, float32 [rows, cols]."""
+        if out is None:
+            out = torch.empty((q.rows, q.cols), device=f"cuda:{self.device}")
+        rows, cols, ld = _rows(out, self.device, "i8_dequantize")
+        if (rows, cols) != (q.rows, q.cols) or out.dtype != torch.float32 or q.device != self.device:
+            raise ValueError("i8_dequantize: a float32 output of the matrix's size, on its device, is wanted")
+        self._sync_stream()
+        _check(lib().gvq_i8_dequantize(self._h, q.codes_ptr, q.scales_ptr, rows, cols, out.data_ptr(), ld), "gvq_i8_dequantize")
+        return out
+
+    def i8_matmul(self, a: I8, b: I8, out: torch.Tensor) -> torch.Tensor:
+        """gvq_i8_matmul: out [a.rows, b.rows] = a b^T; out is float32, bfloat16 or float16."""
+        rows, cols, ld = _rows(out, self.device, "i8_matmul")
+        if a.cols != b.cols or (rows, cols) != (a.rows, b.rows):
+            raise ValueError(f"i8_matmul: [{a.rows}, {a.cols}] x [{b.rows}, {b.cols}]^T does not give [{rows}, {cols}]")
+        if a.device != self.device or b.device != self.device:
+            raise ValueError(f"i8_matmul: operands on cuda:{a.device} and cuda:{b.device}, the context on cuda:{self.device}")
+        self._sync_stream()
+        status = lib().gvq_i8_matmul(self._h, a.codes_ptr, a.scales_ptr, b.codes_ptr, b.scales_ptr, rows, cols, a.cols, out.data_ptr(),
+                                     _dtype(out), ld)
+        if status:
+            raise GvqError(status, "gvq_i8_matmul")
+        return out
+
+    # ---- the gated block --------------------------------------------------------------------
+    def _halves(self, what: str, like: torch.Tensor, *wanted):
+        """Leading dimensions of 16-bit matrices of the sizes given: (tensor, rows, cols) each; None goes through."""
+        if like.dtype is not torch.bfloat16 and like.dtype is not torch.float16:
+            raise TypeError(f"{what}: bfloat16 and float16 are taken, not {like.dtype}")
+        lds = []
+        for t, rows, cols in wanted:
+            if t is None:
+                lds.append(0)
+                continue
+            r, c, ld = _rows(t, self.device, what)
+            if t.dtype is not like.dtype:
+                raise TypeError(f"{what}: the matrices are of one type, not {like.dtype} and {t.dtype}")
+            if (r, c) != (rows, cols):
+                raise ValueError(f"{what}: a matrix of {rows} x {cols} is wanted, not {r} x {c}")
+            lds.append(ld)
+        return lds
+
+    def _gated_workspace(self, what: str, M: int, F: int, K: int, backward: bool, read):
+        """(tensor or None, address, bytes) for a call that reads the matrices `read`, (tensor, leading dimension) each."""
+        aligned = all(t is None or (t.data_ptr() % 16 == 0 and (t.shape[0] == 1 or ld % 8 == 0)) for t, ld in read)
+        n = lib().gvq_gated_workspace_bytes(M, F, K, 1 if backward else 0, 1 if aligned else 0)
+        if n < 0:
+            raise GvqError(2, what)
+        if n == 0:
+            return None, None, 0
+        ws = torch.empty(n, dtype=torch.uint8, device=f"cuda:{self.device}")
+        return ws, ws.data_ptr(), n
+
+    def gated_forward(self, x, w_gate, w_up, out, act: str = "silu", gate: Optional[torch.Tensor] = None,
+                      up: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """gvq_gated_forward: out [M, F] = act(x w_gate^T) * (x w_up^T); bfloat16 or float16 throughout.  gate, up: [M, F] that receive
+        both projections for gated_backward."""
+        what = "gated_forward"
+        a = _activation(act)
+        M, K, _ = _rows(x, self.device, what)
+        F = w_gate.shape[0]
+        if (gate is None) != (up is None):
+            raise ValueError(f"{what}: both projections are kept, or neither")
+        ldx, lg, lu, lh, lgo, luo = self._halves(what, x, (x, M, K), (w_gate, F, K), (w_up, F, K), (out, M, F), (gate, M, F), (up, M, F))
+        ws, at, n = self._gated_workspace(what, M, F, K, False, ((x, ldx), (w_gate, lg), (w_up, lu)))
+        self._sync_stream()
+        status = lib().gvq_gated_forward(self._h, x.data_ptr(), ldx, w_gate.data_ptr(), lg, w_up.data_ptr(), lu, DTYPE[x.dtype], M, F, K, a,
+                                         out.data_ptr(), lh, gate.data_ptr() if gate is not None else None, lgo,
+                                         up.data_ptr() if up is not None else None, luo, at, n)
+        if status:
+            raise GvqError(status, "gvq_gated_forward")
+        return out
+
+    def gated_backward(self, dh, gate, up, x, w_gate, w_up, act: str = "silu", dx: Optional[torch.Tensor] = None,
+                       dw_gate: Optional[torch.Tensor] = None, dw_up: Optional[torch.Tensor] = None) -> None:
+        """gvq_gated_backward: the gradients that are given room for.  dx [M, K] is of the operands' type; dw_gate, dw_up [F, K] are
+        float32, bfloat16 or float16, of one type.  x may be None where neither is wanted, the weights where dx is not."""
+        what = "gated_backward"
+        a = _activation(act)
+        M, F, _ = _rows(dh, self.device, what)
+        dws = [t for t in (dw_gate, dw_up) if t is not None]
+        if dx is None and not dws:
+            raise ValueError(f"{what}: no gradient is wanted")
+        if (dws and x is None) or (dx is not None and (w_gate is None or w_up is None)):
+            raise ValueError(f"{what}: x is needed for the weights' gradients, the weights for dx")
+        if not dws:
+            x = None
+        if dx is None:
+            w_gate = w_up = None
+        K = (dws[0] if dws else dx).shape[-1]
+        ldh, lgi, lui, ldx, lg, lu, ldd = self._halves(what, dh, (dh, M, F), (gate, M, F), (up, M, F), (x, M, K), (w_gate, F, K), (w_up, F, K),
+                                                       (dx, M, K))
+        lds = []
+        for t in (dw_gate, dw_up):
+            if t is None:
+                lds.append(0)
+                continue
+            r, c, ld = _rows(t, self.device, what)
+            if (r, c) != (F, K):
+                raise ValueError(f"{what}: a gradient of {F} x {K} is wanted, not {r} x {c}")
+            if t.dtype is not dws[0].dtype:
+                raise TypeError(f"{what}: both weights' gradients are of one type")
+            lds.append(ld)
+        dw_dtype = _dtype(dws[0]) if dws else 0
+        ws, at, n = self._gated_workspace(what, M, F, K, True, ((x, ldx), (w_gate, lg), (w_up, lu)))
+        self._sync_stream()
+
+        def ptr(t):
+            return t.data_ptr() if t is not None else None
+        status = lib().gvq_gated_backward(self._h, dh.data_ptr(), ldh, gate.data_ptr(), lgi, up.data_ptr(), lui, ptr(x), ldx, ptr(w_gate), lg,
+                                          ptr(w_up), lu, DTYPE[dh.dtype], M, F, K, a, ptr(dx), ldd, ptr(dw_gate), lds[0], ptr(dw_up), lds[1],
+                                          dw_dtype, at, n)
+        if status:
+            raise GvqError(status, "gvq_gated_backward")
+
+    def i8_gated(self, a: I8, w_gate: I8, w_up: I8, out: torch.Tensor, act: str = "silu") -> torch.Tensor:
+        """gvq_i8_gated: out [a.rows, w_gate.rows] = act(a w_gate^T) * (a w_up^T); out is float32, bfloat16 or float16."""
+        code = _activation(act)
+        rows, cols, ld = _rows(out, self.device, "i8_gated")
+        if w_gate.cols != a.cols or w_up.cols != a.cols or w_gate.rows != w_up.rows or (rows, cols) != (a.rows, w_gate.rows):
+            raise ValueError(f"i8_gated: [{a.rows}, {a.cols}] x [{w_gate.rows}, {w_gate.cols}]^T and [{w_up.rows}, {w_up.cols}]^T do not give "
+                             f"[{rows}, {cols}]")
+        if not a.device == w_gate.device == w_up.device == self.device:
+            raise ValueError(f"i8_gated: operands on another device than the context's, cuda:{self.device}")
+        self._sync_stream()
+        status = lib().gvq_i8_gated(self._h, a.codes_ptr, a.scales_ptr, w_gate.codes_ptr, w_gate.scales_ptr, w_up.codes_ptr, w_up.scales_ptr,
+                                    rows, cols, a.cols, code, out.data_ptr(), _dtype(out), ld)
+        if status:
+            raise GvqError(status, "gvq_i8_gated")
         return out
 
     def _flat(self, t: torch.Tensor, what: str):
