@@ -543,15 +543,15 @@ gvq_status gvq_mx4_dequantize_aggregate(gvq_ctx *ctx, const uint8_t *const *code
    "Along the columns" means the same of the transposed matrix [cols][rows], as above.
    Sizes: rows, cols >= 1, below 2^31 - 1024; ceil(rows / 128) * ceil(cols / 128) < 2^31. */
 
-/* Bytes of the codes of a quantized matrix [rows][cols], and of the scratch that quantizing it along its columns takes;
-   -1 on bad sizes. */
+/* Bytes of the codes of a quantized matrix [rows][cols], and of the scratch that quantizing it along its columns takes
+   (0 up to 3072 rows); -1 on bad sizes. */
 int64_t gvq_i8_codes_bytes(int64_t rows, int64_t cols);
 int64_t gvq_i8_scratch_bytes(int64_t rows, int64_t cols);
 
 /* Quantizes a matrix along its rows (codes, scales) and / or along its columns (codes_t, scales_t).  A pair may be NULL, not
    both.  x: device, entries of type dtype, rows ld entries apart (ld >= cols; x aligned to its entries' size only -- rows
-   that start at 16-byte boundaries are read faster).  scratch: device, 4-byte aligned, gvq_i8_scratch_bytes(rows, cols);
-   for the rows alone it may be NULL (0 bytes).  Its contents carry nothing from one call to the next. */
+   that start at 16-byte boundaries are read faster).  scratch: device, 4-byte aligned, gvq_i8_scratch_bytes(rows, cols)
+   bytes where codes_t is wanted; NULL where that is 0 or it is not.  Its contents carry nothing from one call to the next. */
 gvq_status gvq_i8_quantize(gvq_ctx *ctx, const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, int rounding,
                            uint64_t seed, uint32_t node, int8_t *codes, float *scales, int8_t *codes_t, float *scales_t,
                            void *scratch, size_t scratch_bytes);

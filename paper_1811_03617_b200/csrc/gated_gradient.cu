@@ -3,6 +3,7 @@
 //   dx = dg Wg + du Wu                             one product whose contraction has two segments
 //   dWg = dg^T x,  dWu = du^T x                    one launch of two products that have x in common
 // and the copies of operands whose rows do not start at 16-byte boundaries, which TMA cannot address.
+#include "load8.cuh"
 #include "product.cuh"
 
 namespace gvq {
@@ -10,34 +11,47 @@ namespace {
 
 using namespace product;
 
+// The copies, eight entries a thread at a time; rows of a copy are padded to eight entries by zeros.
+__device__ __forceinline__ void copy_rows(const RowCopies &c)
+{
+    for (int k = 0; k < c.n; ++k) {
+        const int64_t total = c.rows[k] * c.chunks[k];
+        for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < total; it += (int64_t)gridDim.x * 256) {
+            const int64_t r = it / c.chunks[k], at = (it - r * c.chunks[k]) * 8;
+            const int n = (int)min((int64_t)8, c.cols[k] - at);
+            *reinterpret_cast<uint4 *>(c.to[k] + r * c.chunks[k] * 8 + at) = load8<false>(c.from[k] + r * c.ld[k] + at, n).q[0];
+        }
+    }
+}
+__global__ void __launch_bounds__(256) align_rows_kernel(const __grid_constant__ RowCopies copies)
+{
+    launch_dependents();
+    grid_dependency_wait();
+    copy_rows(copies);
+}
+
 struct SlopeParams {
     const void *dh, *g, *u;
     int64_t ld_dh, ld_g, ld_u;
     void *dg, *du;             // rows ld_out entries apart, starting at 16-byte boundaries
     int64_t rows, cols, ld_out;
     int chunks;                // groups of eight columns of a row
-    int vec;                   // all rows start at 16-byte boundaries
+    RowCopies copies;          // done on the way: the products after this launch read them
 };
 
-template <typename T>
-__device__ __forceinline__ void load_eight(const void *p, int64_t at, int n, bool vec, float (&v)[8])
+template <typename T, bool VEC>
+__device__ __forceinline__ void load_eight(const void *p, int64_t at, int n, float (&v)[8])
 {
+    const Raw8<uint16_t> q = load8<VEC>(static_cast<const uint16_t *>(p) + at, n);
     T e[8];
-    const T *from = static_cast<const T *>(p) + at;
-    if (vec && n >= 8) {
-        const uint4 q = __ldcs(reinterpret_cast<const uint4 *>(from));
-        memcpy(e, &q, 16);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = i < n ? from[i] : T(0.0f);
-    }
+    memcpy(e, &q, 16);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = to_f(e[i]);
 }
 
 // Eight entries a thread, each read and written once.
-template <typename T, int ACT>
-__global__ void __launch_bounds__(256) gated_slopes_kernel(const SlopeParams prm)
+template <typename T, int ACT, bool VEC>
+__global__ void __launch_bounds__(256) gated_slopes_kernel(const __grid_constant__ SlopeParams prm)
 {
     launch_dependents();
     grid_dependency_wait();
@@ -46,9 +60,9 @@ __global__ void __launch_bounds__(256) gated_slopes_kernel(const SlopeParams prm
         const int64_t r = it / prm.chunks;
         const int c = (int)(it - r * prm.chunks) * 8, n = (int)min((int64_t)8, prm.cols - c);
         float dh[8], g[8], u[8];
-        load_eight<T>(prm.dh, r * prm.ld_dh + c, n, prm.vec, dh);
-        load_eight<T>(prm.g, r * prm.ld_g + c, n, prm.vec, g);
-        load_eight<T>(prm.u, r * prm.ld_u + c, n, prm.vec, u);
+        load_eight<T, VEC>(prm.dh, r * prm.ld_dh + c, n, dh);
+        load_eight<T, VEC>(prm.g, r * prm.ld_g + c, n, g);
+        load_eight<T, VEC>(prm.u, r * prm.ld_u + c, n, u);
         uint32_t dg[4], du[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -60,24 +74,7 @@ __global__ void __launch_bounds__(256) gated_slopes_kernel(const SlopeParams prm
         *reinterpret_cast<uint4 *>(static_cast<T *>(prm.dg) + at) = make_uint4(dg[0], dg[1], dg[2], dg[3]);
         *reinterpret_cast<uint4 *>(static_cast<T *>(prm.du) + at) = make_uint4(du[0], du[1], du[2], du[3]);
     }
-}
-
-__global__ void __launch_bounds__(256) align_rows_kernel(const uint16_t *from, int64_t ld, uint16_t *to, int64_t ld_to, int64_t rows, int chunks,
-                                                         int64_t cols)
-{
-    launch_dependents();
-    grid_dependency_wait();
-    const int64_t total = rows * chunks;
-    for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < total; it += (int64_t)gridDim.x * 256) {
-        const int64_t r = it / chunks;
-        const int c = (int)(it - r * chunks) * 8;
-        uint16_t e[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = c + i < cols ? from[r * ld + c + i] : (uint16_t)0;
-        uint4 q;
-        memcpy(&q, e, 16);
-        *reinterpret_cast<uint4 *>(to + r * ld_to + c) = q;
-    }
+    copy_rows(prm.copies);
 }
 
 Params start(const Launch &l, int dtype, int out_dtype)
@@ -97,59 +94,65 @@ int grid_of(int num_sms, int64_t items)
     return (int)(blocks < most ? blocks : most);
 }
 
-template <typename T>
+template <typename T, bool VEC>
 cudaError_t launch_slopes_as(const Launch &l, const SlopeParams &prm, int act)
 {
     const int grid = grid_of(l.num_sms, prm.rows * prm.chunks);
     switch (act) {
-    case GVQ_SILU: return launch_chained<gated_slopes_kernel<T, GVQ_SILU>>(prm, grid, 256, 0, 1, l.stream);
-    case GVQ_GELU: return launch_chained<gated_slopes_kernel<T, GVQ_GELU>>(prm, grid, 256, 0, 1, l.stream);
-    case GVQ_GELU_TANH: return launch_chained<gated_slopes_kernel<T, GVQ_GELU_TANH>>(prm, grid, 256, 0, 1, l.stream);
-    case GVQ_RELU: return launch_chained<gated_slopes_kernel<T, GVQ_RELU>>(prm, grid, 256, 0, 1, l.stream);
-    default: return launch_chained<gated_slopes_kernel<T, GVQ_SIGMOID>>(prm, grid, 256, 0, 1, l.stream);
+    case GVQ_SILU: return launch_chained<gated_slopes_kernel<T, GVQ_SILU, VEC>>(prm, grid, 256, 0, 1, l.stream);
+    case GVQ_GELU: return launch_chained<gated_slopes_kernel<T, GVQ_GELU, VEC>>(prm, grid, 256, 0, 1, l.stream);
+    case GVQ_GELU_TANH: return launch_chained<gated_slopes_kernel<T, GVQ_GELU_TANH, VEC>>(prm, grid, 256, 0, 1, l.stream);
+    case GVQ_RELU: return launch_chained<gated_slopes_kernel<T, GVQ_RELU, VEC>>(prm, grid, 256, 0, 1, l.stream);
+    default: return launch_chained<gated_slopes_kernel<T, GVQ_SIGMOID, VEC>>(prm, grid, 256, 0, 1, l.stream);
     }
 }
 
 }  // namespace
 
-cudaError_t launch_align_rows(const Launch &l, const void *from, int64_t ld, void *to, int64_t ld_to, int64_t rows, int64_t cols)
+cudaError_t launch_align_rows(const Launch &l, const RowCopies &copies)
 {
-    const int chunks = (int)((cols + 7) / 8);
-    align_rows_kernel<<<grid_of(l.num_sms, rows * chunks), 256, 0, l.stream>>>(static_cast<const uint16_t *>(from), ld,
-                                                                               static_cast<uint16_t *>(to), ld_to, rows, chunks, cols);
-    return cudaGetLastError();
+    int64_t items = 0;
+    for (int k = 0; k < copies.n; ++k) items = items > copies.rows[k] * copies.chunks[k] ? items : copies.rows[k] * copies.chunks[k];
+    return launch_chained<align_rows_kernel>(copies, grid_of(l.num_sms, items), 256, 0, 1, l.stream);
 }
 
 cudaError_t launch_gated_slopes(const Launch &l, const void *dh, int64_t ld_dh, const void *g, int64_t ld_g, const void *u, int64_t ld_u,
-                                int dtype, int64_t rows, int64_t cols, int act, void *dg, void *du, int64_t ld_out)
+                                int dtype, int64_t rows, int64_t cols, int act, void *dg, void *du, int64_t ld_out, const RowCopies &copies)
 {
     auto aligned = [](const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % 8 == 0; };
-    SlopeParams prm = {dh, g, u, ld_dh, ld_g, ld_u, dg, du, rows, cols, ld_out, (int)((cols + 7) / 8),
-                       aligned(dh, ld_dh) && aligned(g, ld_g) && aligned(u, ld_u)};
-    return dtype == GVQ_BF16 ? launch_slopes_as<__nv_bfloat16>(l, prm, act) : launch_slopes_as<__half>(l, prm, act);
+    const SlopeParams prm = {dh, g, u, ld_dh, ld_g, ld_u, dg, du, rows, cols, ld_out, (int)((cols + 7) / 8), copies};
+    if (aligned(dh, ld_dh) && aligned(g, ld_g) && aligned(u, ld_u))      // all rows start at 16-byte boundaries
+        return dtype == GVQ_BF16 ? launch_slopes_as<__nv_bfloat16, true>(l, prm, act) : launch_slopes_as<__half, true>(l, prm, act);
+    return dtype == GVQ_BF16 ? launch_slopes_as<__nv_bfloat16, false>(l, prm, act) : launch_slopes_as<__half, false>(l, prm, act);
 }
 
 cudaError_t launch_gated_dx(const Launch &l, const void *dg, const void *du, int64_t ld_d, const void *gate, int64_t ld_gate, const void *up,
                             int64_t ld_up, int dtype, int64_t M, int64_t F, int64_t K, void *dx, int64_t ld)
 {
     Params prm = start(l, dtype, dtype);
-    const Cut c = cut(l.num_sms, M, K, 64);
-    prm.M = c.swapped ? K : M;
-    prm.N = c.swapped ? M : K;
-    divide(prm, l.num_sms, c, k16, c.bn, F, 2, 1);
+    const Cut c = cut(l.num_sms, M, K, false, 2 * stages_of(F, k16), 64);
+    prm.M = c.few ? K : M;
+    prm.N = c.few ? M : K;
+    divide(prm, c, k16, false, F, 2, 1);
     // the weights are MN-major here: boxes of 64 of a row's entries by 64 rows
-    CUtensorMap *map_w = c.swapped ? prm.a : prm.b, *map_d = c.swapped ? prm.b : prm.a;
-    const int box_d = c.swapped ? c.bn : 128;
+    CUtensorMap *map_w = c.few ? prm.a : prm.b, *map_d = c.few ? prm.b : prm.a;
+    const int box_d = c.few ? c.bn : 128;
     if (!encode(l.encode, map_w, k16, gate, F, K, ld_gate, 64) || !encode(l.encode, map_w + 1, k16, up, F, K, ld_up, 64) ||
         !encode(l.encode, map_d, k16, dg, M, F, ld_d, box_d) || !encode(l.encode, map_d + 1, k16, du, M, F, ld_d, box_d))
         return cudaErrorInvalidValue;
-    set_output(l.encode, prm, 0, dx, dtype, M, K, ld);
-    if (c.cg == 2) return launch<k16, 2, 256, 1, false, true, false>(l.stream, l.num_sms, prm);
-    if (!c.swapped) return launch<k16, 1, 64, 1, false, true, false>(l.stream, l.num_sms, prm);
+    set_output(prm, 0, dx, dtype, ld);
+    const cudaStream_t st = l.stream;
+    if (c.few) {
+        switch (c.bn) {
+        case 16: return launch<k16, 1, 16, true, true, false, false>(st, l.num_sms, prm);
+        case 32: return launch<k16, 1, 32, true, true, false, false>(st, l.num_sms, prm);
+        default: return launch<k16, 1, 64, true, true, false, false>(st, l.num_sms, prm);
+        }
+    }
     switch (c.bn) {
-    case 16: return launch<k16, 1, 16, 1, true, false, false>(l.stream, l.num_sms, prm);
-    case 32: return launch<k16, 1, 32, 1, true, false, false>(l.stream, l.num_sms, prm);
-    default: return launch<k16, 1, 64, 1, true, false, false>(l.stream, l.num_sms, prm);
+    case 256: return launch<k16, 2, 256, false, false, true, false>(st, l.num_sms, prm);
+    case 128: return launch<k16, 2, 128, false, false, true, false>(st, l.num_sms, prm);
+    default: return launch<k16, 1, 64, false, false, true, false>(st, l.num_sms, prm);
     }
 }
 
@@ -164,18 +167,18 @@ cudaError_t launch_gated_dw(const Launch &l, const void *dg, const void *du, int
     void *out[2] = {dw_gate ? dw_gate : dw_up, dw_up};
     const int64_t ld[2] = {dw_gate ? ld_dw_gate : ld_dw_up, ld_dw_up};
     const int halves = dw_gate && dw_up ? 2 : 1;
-    Cut c;
-    c.swapped = false;
-    c.cg = (int64_t)halves * tiles_of(F, 128) * tiles_of(K, 64) > l.num_sms ? 2 : 1;
-    c.bn = c.cg == 2 ? 256 : 64;
-    divide(prm, l.num_sms, c, k16, c.bn, M, 1, halves);
+    const Cut c = cut_tiles(l.num_sms, F, K, false, stages_of(M, k16), halves);
+    divide(prm, c, k16, false, M, 1, halves);
     if (!encode(l.encode, &prm.b[0], k16, x, M, K, ldx, 64)) return cudaErrorInvalidValue;
     for (int i = 0; i < halves; ++i) {
         if (!encode(l.encode, &prm.a[i], k16, d[i], M, F, ld_d, 64)) return cudaErrorInvalidValue;
-        set_output(l.encode, prm, i, out[i], out_dtype, F, K, ld[i]);
+        set_output(prm, i, out[i], out_dtype, ld[i]);
     }
-    if (c.cg == 2) return launch<k16, 2, 256, 1, true, true, false>(l.stream, l.num_sms, prm);
-    return launch<k16, 1, 64, 1, true, true, false>(l.stream, l.num_sms, prm);
+    switch (c.bn) {
+    case 256: return launch<k16, 2, 256, false, true, true, false>(l.stream, l.num_sms, prm);
+    case 128: return launch<k16, 2, 128, false, true, true, false>(l.stream, l.num_sms, prm);
+    default: return launch<k16, 1, 64, false, true, true, false>(l.stream, l.num_sms, prm);
+    }
 }
 
 }  // namespace gvq

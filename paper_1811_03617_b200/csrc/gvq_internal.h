@@ -190,13 +190,21 @@ cudaError_t launch_i8_matmul(const Launch &l, const int8_t *a, const float *sa, 
 cudaError_t launch_i8_gated(const Launch &l, const int8_t *a, const float *sa, const int8_t *gate, const float *s_gate, const int8_t *up,
                             const float *s_up, int64_t M, int64_t F, int64_t K, int act, void *out, int dtype, int64_t ld);
 // The gated block (gated_product.cu, gated_gradient.cu).  Operands' rows start at 16-byte boundaries, apart from those of
-// launch_gated_slopes and launch_align_rows, which write such rows.  g and u, or one of the weights' gradients, may be null.
+// launch_gated_slopes and of copies, which write such rows.  g and u, or one of the weights' gradients, may be null.
 cudaError_t launch_gated(const Launch &l, const void *x, int64_t ldx, const void *gate, int64_t ld_gate, const void *up, int64_t ld_up,
                          int dtype, int64_t M, int64_t F, int64_t K, int act, void *h, int64_t ldh, void *g, int64_t ldg, void *u,
                          int64_t ldu);
-cudaError_t launch_align_rows(const Launch &l, const void *from, int64_t ld, void *to, int64_t ld_to, int64_t rows, int64_t cols);
+// Copies of 16-bit matrices whose rows start at 16-byte boundaries (eight entries, `chunks` of them a row).
+struct RowCopies {
+    int n;
+    const uint16_t *from[3];
+    uint16_t *to[3];
+    int64_t ld[3], rows[3], cols[3];
+    int chunks[3];
+};
+cudaError_t launch_align_rows(const Launch &l, const RowCopies &copies);
 cudaError_t launch_gated_slopes(const Launch &l, const void *dh, int64_t ld_dh, const void *g, int64_t ld_g, const void *u, int64_t ld_u,
-                                int dtype, int64_t rows, int64_t cols, int act, void *dg, void *du, int64_t ld_out);
+                                int dtype, int64_t rows, int64_t cols, int act, void *dg, void *du, int64_t ld_out, const RowCopies &copies);
 cudaError_t launch_gated_dx(const Launch &l, const void *dg, const void *du, int64_t ld_d, const void *gate, int64_t ld_gate, const void *up,
                             int64_t ld_up, int dtype, int64_t M, int64_t F, int64_t K, void *dx, int64_t ld);
 cudaError_t launch_gated_dw(const Launch &l, const void *dg, const void *du, int64_t ld_d, const void *x, int64_t ldx, int dtype, int64_t M,

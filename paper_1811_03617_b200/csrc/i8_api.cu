@@ -32,22 +32,28 @@ bool rows_aligned(const void *p, int64_t rows, int64_t ld) { return aligned16(p)
 int64_t ld_of(int64_t rows, int64_t cols, int64_t ld) { return rows == 1 ? padded(cols, 8) : ld; }
 
 struct Operand { const void *p; int64_t rows, cols, ld; };
-// Operands whose rows do not start at 16-byte boundaries, copied to `at`; each gets its place.
-gvq_status align_operands(gvq_ctx *ctx, const Launch &l, Operand *ops, int n, char *at)
+// Operands whose rows do not start at 16-byte boundaries get copies at `at`, which the caller has made.
+RowCopies align_operands(Operand *ops, int n, char *at)
 {
+    RowCopies c = {};
     for (int i = 0; i < n; ++i) {
         Operand &o = ops[i];
         if (!o.p) continue;
         if (!rows_aligned(o.p, o.rows, o.ld)) {
-            const int64_t ld = padded(o.cols, 8);
-            GVQ_CUDA(ctx, launch_align_rows(l, o.p, o.ld, at, ld, o.rows, o.cols));
+            const int k = c.n++;
+            c.from[k] = static_cast<const uint16_t *>(o.p);
+            c.to[k] = reinterpret_cast<uint16_t *>(at);
+            c.ld[k] = o.ld;
+            c.rows[k] = o.rows;
+            c.cols[k] = o.cols;
+            c.chunks[k] = (int)(padded(o.cols, 8) / 8);
             o.p = at;
-            o.ld = ld;
+            o.ld = padded(o.cols, 8);
             at += bytes_of(o.rows, o.cols);
         }
         o.ld = ld_of(o.rows, o.cols, o.ld);
     }
-    return GVQ_OK;
+    return c;
 }
 bool all_aligned(const Operand *ops, int n)
 {
@@ -73,7 +79,8 @@ gvq_status gvq_i8_quantize(gvq_ctx *ctx, const void *x, int dtype, int64_t rows,
     if (rounding != GVQ_ROUND_NEAREST && rounding != GVQ_ROUND_STOCHASTIC) return GVQ_ERR_SHAPE;
     if (!entry_aligned(x, dtype) || !aligned16(codes) || !aligned4(scales) || !aligned16(codes_t) || !aligned4(scales_t) || !aligned4(scratch))
         return GVQ_ERR_ALIGN;
-    if (codes_t && (!scratch || scratch_bytes < (size_t)i8_scratch_bytes(rows, cols))) return GVQ_ERR_WORKSPACE;
+    const size_t need = codes_t ? (size_t)i8_scratch_bytes(rows, cols) : 0;
+    if (need && (!scratch || scratch_bytes < need)) return GVQ_ERR_WORKSPACE;
     DeviceGuard guard(ctx->device);
     GVQ_CUDA(ctx, launch_i8_quantize(ctx->stream, x, dtype, rows, cols, ld, rounding == GVQ_ROUND_STOCHASTIC, seed, node, codes, scales,
                                      codes_t, scales_t, scratch));
@@ -144,8 +151,8 @@ gvq_status gvq_gated_forward(gvq_ctx *ctx, const void *x, int64_t ldx, const voi
     if (!ctx->encode_fn) return GVQ_ERR_UNSUPPORTED;
     DeviceGuard guard(ctx->device);
     const Launch l = launch_of(ctx);
-    const gvq_status s = align_operands(ctx, l, ops, 3, static_cast<char *>(workspace));
-    if (s != GVQ_OK) return s;
+    const RowCopies copies = align_operands(ops, 3, static_cast<char *>(workspace));
+    if (copies.n) GVQ_CUDA(ctx, launch_align_rows(l, copies));
     GVQ_CUDA(ctx, launch_gated(l, ops[0].p, ops[0].ld, ops[1].p, ops[1].ld, ops[2].p, ops[2].ld, dtype, M, F, K, activation, h, ldh, gate_opt,
                                ld_gate_out, up_opt, ld_up_out));
     return GVQ_OK;
@@ -172,10 +179,9 @@ gvq_status gvq_gated_backward(gvq_ctx *ctx, const void *dh, int64_t ld_dh, const
     DeviceGuard guard(ctx->device);
     const Launch l = launch_of(ctx);
     char *at = static_cast<char *>(workspace), *dg = at, *du = at + bytes_of(M, F);
-    const gvq_status s = align_operands(ctx, l, ops, 3, at + 2 * bytes_of(M, F));
-    if (s != GVQ_OK) return s;
+    const RowCopies copies = align_operands(ops, 3, at + 2 * bytes_of(M, F));
     const int64_t ld_d = padded(F, 8);
-    GVQ_CUDA(ctx, launch_gated_slopes(l, dh, ld_dh, gate, ld_gate_in, up, ld_up_in, dtype, M, F, activation, dg, du, ld_d));
+    GVQ_CUDA(ctx, launch_gated_slopes(l, dh, ld_dh, gate, ld_gate_in, up, ld_up_in, dtype, M, F, activation, dg, du, ld_d, copies));
     if (dx_opt)
         GVQ_CUDA(ctx, launch_gated_dx(l, dg, du, ld_d, ops[1].p, ops[1].ld, ops[2].p, ops[2].ld, dtype, M, F, K, dx_opt, ld_dx));
     if (dw)

@@ -1,14 +1,15 @@
 // Quantization to 8-bit integers with a scale a row, and back (gvq.h, "8-bit integers").
 //
 //  i8_rows_kernel     along the rows, read once: a row stays in the registers of the threads that share it
-//  i8_max_kernel      largest magnitudes of columns (and rows) over blocks of the matrix
-//  i8_tile_kernel     along the columns, or both ways, from those: a tile goes through shared memory
+//  i8_strip_kernel    along the columns, read once: a strip of columns stays in the shared memory of a cluster
+//  i8_max_kernel, i8_tile_kernel   along columns too long for that: largest magnitudes first, then tile by tile
 //  i8_dequantize_kernel
 //
 // With a = max(max |x|, 2^-100) and r the largest float with r a <= 127, a code is x r to the nearest whole number, rounded from
 // the exact product: one fused multiply-add to 1.5 * 2^23 leaves it in the low bits, two's complement.  Stochastic rounding adds 14
 // random bits below floor(2^14 x r), which the same instruction leaves there when it rounds down (2^14 * 127 < 2^22).
 #include "gvq_internal.h"
+#include "load8.cuh"
 #include "mx4.cuh"
 #include "row32.cuh"
 #include "sm100_ptx.cuh"
@@ -17,15 +18,12 @@ namespace gvq {
 namespace {
 
 constexpr float kMagic = 12582912.0f;               // 1.5 * 2^23: its pattern's low 22 bits are 0
-constexpr int kMaxCols = 256, kMinBlockRows = 256;  // a block of i8_max_kernel
-constexpr int kMaxBlocks = 64;                      // most blocks along the rows
+constexpr int kMaxRows = 512;      // of a CTA of i8_max_kernel
+// i8_strip_kernel: CTAs of a cluster, threads, words from row to row, most rows of a CTA (109 KB of shared memory)
+constexpr int kCluster = 4, kStripThreads = 512, kStripPitch = 36, kStripRows = 768;
 
 __host__ __device__ inline int64_t pitch_of(int64_t cols) { return (cols + 15) / 16 * 16; }
-__host__ __device__ inline int64_t block_rows(int64_t rows)
-{
-    const int64_t per = (rows + kMaxBlocks - 1) / kMaxBlocks;
-    return per < kMinBlockRows ? kMinBlockRows : (per + 127) / 128 * 128;
-}
+inline int64_t row_blocks(int64_t rows) { return (rows + kMaxRows - 1) / kMaxRows; }
 
 // A row's factor and scale from the pattern of its largest magnitude.  A row that holds a NaN or an infinity has factor 0,
 // and the caller's entries are replaced by 0.
@@ -61,25 +59,6 @@ __device__ __forceinline__ uint2 codes_of(const float (&v)[8], float r, uint64_t
     return q;
 }
 
-// Eight consecutive entries as they lie in memory; past the n-th: 0.
-template <typename T> struct Raw8 { uint4 q[sizeof(T) / 2]; };
-template <typename T>
-__device__ __forceinline__ Raw8<T> load8(const T *p, int n, bool vec)
-{
-    Raw8<T> r;
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.q[i] = make_uint4(0, 0, 0, 0);
-    if (n >= 8 && vec) {
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.q[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
-    } else if (n > 0) {
-        T e[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = i < n ? p[i] : T(0.0f);
-        memcpy(&r, e, sizeof(r));
-    }
-    return r;
-}
 template <typename T>
 __device__ __forceinline__ void unpack8(const Raw8<T> &r, float (&v)[8])
 {
@@ -115,15 +94,14 @@ struct QuantParams {
     uint64_t seed_w;            // mix64 of (seed, node)
     int8_t *codes, *codes_t;    // along the rows, along the columns; null: not wanted
     float *scales, *scales_t;
-    uint32_t *col_top, *row_top;   // [blocks along the rows][cols], [blocks along the columns][rows]: patterns of magnitudes
-    int64_t block_rows;
-    int row_blocks, col_blocks;
-    int vec;                    // rows start at 16-byte boundaries
+    int cluster, rows_per;      // of i8_strip_kernel: CTAs that share a strip, rows of a CTA (a multiple of 16)
+    uint32_t *col_top;          // [row_blocks][cols]: patterns of magnitudes
+    int row_blocks;             // CTAs along the rows of i8_max_kernel
     int ct;                     // tiles along the columns
 };
 
 // G threads share a row, KEEP groups of eight entries a thread in registers; longer rows are read again from L2.
-template <typename T, bool SR, int G>
+template <typename T, bool SR, int G, bool VEC>
 __global__ void __launch_bounds__(G < 256 ? 256 : G) i8_rows_kernel(const QuantParams prm)
 {
     constexpr int KEEP = 4, NT = G < 256 ? 256 : G, ROWS = NT / G;
@@ -135,7 +113,7 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G) i8_rows_kernel(const QuantP
     const bool there = row < prm.rows;
     const T *x = static_cast<const T *>(prm.x) + (there ? row : 0) * prm.ld;
     const int64_t pitch = pitch_of(prm.cols), groups = there ? pitch / 8 : 0;
-    auto load = [&](int64_t at) { return load8(x + at * 8, (int)min((int64_t)8, prm.cols - at * 8), prm.vec); };
+    auto load = [&](int64_t at) { return load8<VEC>(x + at * 8, (int)min((int64_t)8, prm.cols - at * 8)); };
     Raw8<T> kept[KEEP];
     uint32_t top = 0;
 #pragma unroll
@@ -172,65 +150,226 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G) i8_rows_kernel(const QuantP
     if (there && in_row == 0) prm.scales[row] = s.scale;
 }
 
-// A CTA: block_rows rows x 256 columns; a warp goes along rows, a lane has eight columns.
-template <typename T, bool ROWS>
-__global__ void __launch_bounds__(256) i8_max_kernel(const QuantParams prm)
-{
-    __shared__ uint32_t tops[8][kMaxCols];
-    ptx::launch_dependents();
-    ptx::grid_dependency_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int cb = blockIdx.x % prm.col_blocks, rb = blockIdx.x / prm.col_blocks;
-    const int64_t c0 = (int64_t)cb * kMaxCols, c = c0 + lane * 8;
-    const int64_t r0 = (int64_t)rb * prm.block_rows, r1 = min(prm.rows, r0 + prm.block_rows);
-    const int n = (int)max((int64_t)0, min((int64_t)8, prm.cols - c));
-    const T *x = static_cast<const T *>(prm.x);
-    uint32_t m[8];
+// Largest magnitudes of eight columns over rows, as patterns: kept as they come, two columns of a 16-bit type a word.
+template <typename T> struct Tops8 {
+    static constexpr int N = 2 * (int)sizeof(T);
+    uint32_t m[N];
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m[i] = 0;
-    constexpr int U = 4;
-    for (int64_t r = r0 + warp; r < r1; r += 8 * U) {
-        Raw8<T> raw[U];
+        for (int i = 0; i < N; ++i) m[i] = 0;
+    }
+    __device__ __forceinline__ void add(const Raw8<T> &r)
+    {
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = load8(x + (r + 8 * u) * prm.ld + c, r + 8 * u < r1 ? n : 0, prm.vec);
+        for (int i = 0; i < N; ++i) {
+            const uint4 q = r.q[i / 4];
+            const uint32_t w = i % 4 == 0 ? q.x : i % 4 == 1 ? q.y : i % 4 == 2 ? q.z : q.w;
+            m[i] = sizeof(T) == 4 ? max(m[i], w & 0x7FFFFFFFu) : __vmaxu2(m[i], w & 0x7FFF7FFFu);
+        }
+    }
+    __device__ __forceinline__ void across(int lanes)      // of the lanes that are `lanes` apart (a power of two, a constant)
+    {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float v[8];
-            unpack8(raw[u], v);
+        for (int d = 16; d >= lanes; d >>= 1) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m[i] = max(m[i], __float_as_uint(v[i]) & 0x7FFFFFFFu);
-            if (ROWS) {
-                const uint32_t t = __reduce_max_sync(0xffffffffu, top8(raw[u]));
-                if (lane == 0 && r + 8 * u < r1) prm.row_top[(int64_t)cb * prm.rows + r + 8 * u] = t;
+            for (int i = 0; i < N; ++i) {
+                const uint32_t o = __shfl_xor_sync(0xffffffffu, m[i], d);
+                m[i] = sizeof(T) == 4 ? max(m[i], o) : __vmaxu2(m[i], o);
             }
         }
     }
+    __device__ __forceinline__ uint32_t column(int i) const      // (a constant)
+    {
+        if (sizeof(T) == 4) return m[i % N];
+        const uint16_t u = (uint16_t)(i & 1 ? m[i / 2 % N] >> 16 : m[i / 2 % N] & 0xFFFFu);
+        T e;
+        memcpy(&e, &u, sizeof(e) < 2 ? sizeof(e) : 2);
+        return __float_as_uint(to_f(e));
+    }
+};
+
+// Sixteen rows from r on of column c, whose entries are the `part`-th of the words: a 16-byte piece of the output's row c.
+template <typename T, bool SR>
+__device__ __forceinline__ void column_run(const QuantParams &prm, const uint32_t (&w)[16], int part, const RowScale &s, int64_t c, int64_t r,
+                                           int64_t pitch_t)
+{
+    if (c >= prm.cols) return;
+    const uint64_t h = SR ? mx4::row_word(prm.seed_w, c) : 0;
+    uint2 q[2];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) tops[warp][lane * 8 + i] = m[i];
-    __syncthreads();
-    uint32_t t = 0;
+    for (int o = 0; o < 2; ++o) {
+        float v[8];
 #pragma unroll
-    for (int w = 0; w < 8; ++w) t = max(t, tops[w][threadIdx.x]);
-    if (c0 + threadIdx.x < prm.cols) prm.col_top[(int64_t)rb * prm.cols + c0 + threadIdx.x] = t;
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t word = w[8 * o + e];
+            if (sizeof(T) == 4) v[e] = __uint_as_float(word);
+            else {
+                T t;
+                const uint16_t u = (uint16_t)(part ? word >> 16 : word & 0xFFFFu);
+                memcpy(&t, &u, sizeof(t) < 2 ? sizeof(t) : 2);
+                v[e] = to_f(t);
+            }
+        }
+        q[o] = s.scale == s.scale ? codes_of<SR>(v, SR ? s.r * 16384.0f : s.r, h, (uint32_t)((r + 8 * o) >> 1)) : make_uint2(0, 0);
+    }
+    *reinterpret_cast<uint4 *>(prm.codes_t + c * pitch_t + r) = make_uint4(q[0].x, q[0].y, q[1].x, q[1].y);
 }
 
-// A CTA: a tile of 128 x 128 entries.  It lies in shared memory in its own type, rows 4 words longer than they are and another 4
-// words on every 16 rows, so that eight lanes' 16-byte words of eight rows, and the words of 4 columns in 8 runs of 16 rows, lie in
-// different banks.  A thread takes 16 entries of a column (of two columns of a 16-bit type, so that a word is read once): eight
-// lanes write 128 bytes of an output row.
-template <typename T, bool SR, bool ROWS>
+// A cluster of up to four CTAs has a strip of 128 bytes of every row, rows_per rows a CTA (all of its columns' entries): it is read once
+// into shared memory, the columns' largest magnitudes go round the cluster, and a thread takes 16 entries of a column (of two columns
+// of a 16-bit type, so that a word is read once); eight lanes write 128 bytes of an output row.  Rows lie 4 words further apart than
+// they are long and another 4 words on every 16 rows, so that eight lanes' 16-byte words, and the words of 4 columns in 8 runs of 16
+// rows, lie in different banks.
+template <typename T, bool SR, bool VEC>
+__global__ void __launch_bounds__(kStripThreads) i8_strip_kernel(const QuantParams prm)
+{
+    constexpr int SC = 128 / (int)sizeof(T), L = SC / 8, RP = kStripThreads / L, WARPS = kStripThreads / 32;   // columns, lanes a row, rows a pass
+    extern __shared__ uint4 smem_q[];
+    uint32_t *tile = reinterpret_cast<uint32_t *>(smem_q);
+    __shared__ uint32_t tops[WARPS][SC], of_cta[SC];
+    __shared__ RowScale of_col[SC];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    ptx::launch_dependents();
+    ptx::grid_dependency_wait();
+    const int cluster = prm.cluster, rank = blockIdx.x % cluster;
+    const int64_t c0 = (int64_t)(blockIdx.x / cluster) * SC, r0 = (int64_t)rank * prm.rows_per;
+    const T *x = static_cast<const T *>(prm.x);
+    auto at = [&](int row) { return tile + row * kStripPitch + (row >> 4) * 4; };
+
+    const int g = tid % L, n = (int)max((int64_t)0, min((int64_t)8, prm.cols - (c0 + g * 8)));
+    Tops8<T> m;
+    m.clear();
+    constexpr int U = 16 / (int)sizeof(T);
+    for (int p = tid / L; p < prm.rows_per; p += RP * U) {
+        Raw8<T> raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t r = r0 + p + u * RP;
+            raw[u] = load8<VEC>(x + r * prm.ld + c0 + g * 8, r < prm.rows && p + u * RP < prm.rows_per ? n : 0);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            m.add(raw[u]);
+            if (p + u * RP < prm.rows_per) {
+#pragma unroll
+                for (int q = 0; q < (int)sizeof(T) / 2; ++q)
+                    *reinterpret_cast<uint4 *>(at(p + u * RP) + g * (int)sizeof(T) * 2 + q * 4) = raw[u].q[q];
+            }
+        }
+    }
+    __syncwarp();
+    m.across(L);
+    if (lane < L) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) tops[warp][lane * 8 + i] = m.column(i);
+    }
+    __syncthreads();
+    if (tid < SC) {
+        uint32_t t = 0;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) t = max(t, tops[w][tid]);
+        of_cta[tid] = t;
+    }
+    if (cluster > 1) ptx::cluster_sync_any(); else __syncthreads();
+    if (tid < SC) {
+        uint32_t t = of_cta[tid];
+        if (cluster > 1) {
+            const uint32_t from = ptx::smem_u32(of_cta + tid);
+            t = 0;
+#pragma unroll
+            for (int i = 0; i < kCluster; ++i)
+                if (i < cluster) t = max(t, __float_as_uint(ptx::load_cluster1(ptx::cluster_address(from, i))));
+        }
+        const RowScale s = row_scale(t);
+        of_col[tid] = s;
+        if (rank == 0 && c0 + tid < prm.cols) prm.scales_t[c0 + tid] = s.scale;
+    }
+    __syncthreads();
+    const int64_t pitch_t = pitch_of(prm.rows);
+    constexpr int PER = 4 / (int)sizeof(T);                 // columns of a word: 1 or 2
+    const int runs = prm.rows_per / 16, items = (runs + 7) / 8 * 8;    // groups of eight runs, times eight groups of four words
+    for (int it = warp; it < items; it += WARPS) {
+        const int blk = it / 8 * 8 + (lane & 7), cw = it % 8 * 4 + (lane >> 3);
+        const int64_t r = r0 + blk * 16;
+        if (blk < runs && r < pitch_t) {
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = at(blk * 16 + i)[cw];
+#pragma unroll
+            for (int part = 0; part < PER; ++part)
+                column_run<T, SR>(prm, w, part, of_col[cw * PER + part], c0 + cw * PER + part, r, pitch_t);
+        }
+    }
+    if (cluster > 1) ptx::cluster_sync_any();      // (its neighbours have read this CTA's maxima)
+}
+
+// A CTA: kMaxRows rows of a strip of 128 bytes.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) i8_max_kernel(const QuantParams prm)
+{
+    constexpr int SC = 128 / (int)sizeof(T), L = SC / 8, RP = 256 / L;      // columns, lanes a row, rows a pass
+    __shared__ uint32_t tops[8][SC];
+    ptx::launch_dependents();
+    ptx::grid_dependency_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = threadIdx.x % L;
+    const int strips = (int)((prm.cols + SC - 1) / SC), rb = blockIdx.x / strips;
+    const int64_t c0 = (int64_t)(blockIdx.x - rb * strips) * SC;
+    const int64_t r0 = (int64_t)rb * kMaxRows, r1 = min(prm.rows, r0 + kMaxRows);
+    const int n = (int)max((int64_t)0, min((int64_t)8, prm.cols - (c0 + g * 8)));
+    const T *x = static_cast<const T *>(prm.x) + c0 + g * 8;
+    Tops8<T> m;
+    m.clear();
+    constexpr int U = 16 / (int)sizeof(T);
+    for (int64_t r = r0 + threadIdx.x / L; r < r1; r += RP * U) {
+        Raw8<T> raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = load8<VEC>(x + (r + u * RP) * prm.ld, r + u * RP < r1 ? n : 0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) m.add(raw[u]);
+    }
+    __syncwarp();
+    m.across(L);
+    if (lane < L) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) tops[warp][lane * 8 + i] = m.column(i);
+    }
+    __syncthreads();
+    if (threadIdx.x < SC && c0 + threadIdx.x < prm.cols) {
+        uint32_t t = 0;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) t = max(t, tops[w][threadIdx.x]);
+        prm.col_top[(int64_t)rb * prm.cols + c0 + threadIdx.x] = t;
+    }
+}
+
+// A CTA: a tile of 128 x 128 entries, from the end: what i8_max_kernel has read last is in L2.  Shared memory and what follows as above.
+template <typename T, bool SR, bool VEC>
 __global__ void __launch_bounds__(256) i8_tile_kernel(const QuantParams prm)
 {
     constexpr int W = 128 * (int)sizeof(T) / 4, PITCH = W + 4;    // words of a row of the tile
     extern __shared__ uint4 smem_q[];
     uint32_t *tile = reinterpret_cast<uint32_t *>(smem_q);
-    __shared__ RowScale of_col[128], of_row[128];
+    __shared__ RowScale of_col[128];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     ptx::launch_dependents();
     ptx::grid_dependency_wait();
-    const int rtile = blockIdx.x / prm.ct, ctile = blockIdx.x - rtile * prm.ct;
+    const int tile_at = gridDim.x - 1 - blockIdx.x, rtile = tile_at / prm.ct, ctile = tile_at - rtile * prm.ct;
     const int64_t r0 = (int64_t)rtile * 128, c0 = (int64_t)ctile * 128;
     const T *x = static_cast<const T *>(prm.x);
+    uint32_t top = 0;
+    if (tid < 128 && c0 + tid < prm.cols) {
+        const uint32_t *from = prm.col_top + c0 + tid;
+        int b = 0;
+        for (; b + 8 <= prm.row_blocks; b += 8) {
+            uint32_t t[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[i] = __ldcg(from + (int64_t)(b + i) * prm.cols);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = max(top, t[i]);
+        }
+        for (; b < prm.row_blocks; ++b) top = max(top, __ldcg(from + (int64_t)b * prm.cols));
+    }
     auto at = [&](int row) { return tile + row * PITCH + (row >> 4) * 4; };
 
     // warp w, iteration it: rows 16 w + 2 it + (lane >> 4)
@@ -242,7 +381,7 @@ __global__ void __launch_bounds__(256) i8_tile_kernel(const QuantParams prm)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int64_t r = r0 + 16 * warp + 2 * (4 * half + i) + (lane >> 4);
-            raw[i] = load8(x + r * prm.ld + c0 + cl, r < prm.rows ? ncol : 0, prm.vec);
+            raw[i] = load8<VEC>(x + r * prm.ld + c0 + cl, r < prm.rows ? ncol : 0);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -252,45 +391,11 @@ __global__ void __launch_bounds__(256) i8_tile_kernel(const QuantParams prm)
         }
     }
     if (tid < 128) {
-        uint32_t top = 0;
-        if (c0 + tid < prm.cols)
-            for (int b = 0; b < prm.row_blocks; ++b) top = max(top, __ldg(prm.col_top + (int64_t)b * prm.cols + c0 + tid));
         const RowScale s = row_scale(top);
         of_col[tid] = s;
         if (rtile == 0 && c0 + tid < prm.cols) prm.scales_t[c0 + tid] = s.scale;
-    } else if (ROWS) {
-        const int64_t r = r0 + tid - 128;
-        uint32_t top = 0;
-        if (r < prm.rows)
-            for (int b = 0; b < prm.col_blocks; ++b) top = max(top, __ldg(prm.row_top + (int64_t)b * prm.rows + r));
-        const RowScale s = row_scale(top);
-        of_row[tid - 128] = s;
-        if (ctile == 0 && r < prm.rows) prm.scales[r] = s.scale;
     }
     __syncthreads();
-    if (ROWS) {
-        const int64_t pitch = pitch_of(prm.cols);
-#pragma unroll 1
-        for (int it = 0; it < 4; ++it) {
-            const int item = it * 256 + tid, row = item >> 3, b = item & 7;
-            const int64_t r = r0 + row, c = c0 + b * 16;
-            if (r >= prm.rows || c >= pitch) continue;
-            const uint32_t *from = at(row) + b * 4 * (int)sizeof(T);
-            const RowScale s = of_row[row];
-            const uint64_t h = SR ? mx4::row_word(prm.seed_w, r) : 0;
-            uint2 q[2];
-#pragma unroll
-            for (int o = 0; o < 2; ++o) {
-                Raw8<T> raw;
-#pragma unroll
-                for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw.q[i] = *reinterpret_cast<const uint4 *>(from + (o * (int)sizeof(T) / 2 + i) * 4);
-                float v[8];
-                unpack8(raw, v);
-                q[o] = s.scale == s.scale ? codes_of<SR>(v, SR ? s.r * 16384.0f : s.r, h, (uint32_t)((c + 8 * o) >> 1)) : make_uint2(0, 0);
-            }
-            *reinterpret_cast<uint4 *>(prm.codes + r * pitch + c) = make_uint4(q[0].x, q[0].y, q[1].x, q[1].y);
-        }
-    }
     constexpr int PER = 4 / (int)sizeof(T);                 // columns of a word: 1 or 2
     const int64_t pitch_t = pitch_of(prm.rows);
     const int blk = lane & 7;
@@ -299,31 +404,10 @@ __global__ void __launch_bounds__(256) i8_tile_kernel(const QuantParams prm)
         uint32_t w[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) w[i] = at(blk * 16 + i)[cw];
+        if (r0 + blk * 16 < pitch_t) {
 #pragma unroll
-        for (int part = 0; part < PER; ++part) {
-            const int col = cw * PER + part;
-            const int64_t c = c0 + col, r = r0 + blk * 16;
-            if (c >= prm.cols || r >= pitch_t) continue;
-            const RowScale s = of_col[col];
-            const uint64_t h = SR ? mx4::row_word(prm.seed_w, c) : 0;
-            uint2 q[2];
-#pragma unroll
-            for (int o = 0; o < 2; ++o) {
-                float v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t word = w[8 * o + e];
-                    if (sizeof(T) == 4) v[e] = __uint_as_float(word);
-                    else {
-                        T t;
-                        const uint16_t u = (uint16_t)(part ? word >> 16 : word & 0xFFFFu);
-                        memcpy(&t, &u, sizeof(t) < 2 ? sizeof(t) : 2);
-                        v[e] = to_f(t);
-                    }
-                }
-                q[o] = s.scale == s.scale ? codes_of<SR>(v, SR ? s.r * 16384.0f : s.r, h, (uint32_t)((r + 8 * o) >> 1)) : make_uint2(0, 0);
-            }
-            *reinterpret_cast<uint4 *>(prm.codes_t + c * pitch_t + r) = make_uint4(q[0].x, q[0].y, q[1].x, q[1].y);
+            for (int part = 0; part < PER; ++part)
+                column_run<T, SR>(prm, w, part, of_col[cw * PER + part], c0 + cw * PER + part, r0 + blk * 16, pitch_t);
         }
     }
 }
@@ -344,38 +428,51 @@ __global__ void __launch_bounds__(256) i8_dequantize_kernel(const int8_t *codes,
     }
 }
 
-template <typename T, bool SR>
+template <typename T, bool SR, bool VEC>
 cudaError_t quantize_rows(cudaStream_t st, const QuantParams &prm)
 {
     // a row's threads: as few as keep it in registers, where there are rows enough
     auto grid = [&](int rows) { return (int)((prm.rows + rows - 1) / rows); };
-    if (prm.cols <= 1024) return ptx::launch_chained<i8_rows_kernel<T, SR, 32>>(prm, grid(8), 256, 0, 1, st);
-    if (prm.cols <= 4096 && prm.rows > 512) return ptx::launch_chained<i8_rows_kernel<T, SR, 128>>(prm, grid(2), 256, 0, 1, st);
-    if (prm.cols <= 8192) return ptx::launch_chained<i8_rows_kernel<T, SR, 256>>(prm, grid(1), 256, 0, 1, st);
-    return ptx::launch_chained<i8_rows_kernel<T, SR, 1024>>(prm, grid(1), 1024, 0, 1, st);
+    if (prm.cols <= 1024) return ptx::launch_chained<i8_rows_kernel<T, SR, 32, VEC>>(prm, grid(8), 256, 0, 1, st);
+    if (prm.cols <= 4096 && prm.rows > 512) return ptx::launch_chained<i8_rows_kernel<T, SR, 128, VEC>>(prm, grid(2), 256, 0, 1, st);
+    if (prm.cols <= 8192) return ptx::launch_chained<i8_rows_kernel<T, SR, 256, VEC>>(prm, grid(1), 256, 0, 1, st);
+    return ptx::launch_chained<i8_rows_kernel<T, SR, 1024, VEC>>(prm, grid(1), 1024, 0, 1, st);
 }
-
-template <typename T, bool SR>
-cudaError_t quantize_as(cudaStream_t st, QuantParams prm)
+template <typename T, bool SR, bool VEC>
+cudaError_t quantize_cols(cudaStream_t st, QuantParams prm)
 {
-    if (!prm.codes_t) return quantize_rows<T, SR>(st, prm);
-    const int blocks = prm.row_blocks * prm.col_blocks;
-    cudaError_t e = prm.codes ? ptx::launch_chained<i8_max_kernel<T, true>>(prm, blocks, 256, 0, 1, st)
-                              : ptx::launch_chained<i8_max_kernel<T, false>>(prm, blocks, 256, 0, 1, st);
+    constexpr int SC = 128 / (int)sizeof(T);
+    const int64_t strips = (prm.cols + SC - 1) / SC;
+    int cluster = 1;      // more CTAs where a strip does not fit one, or where there are SMs for them and 128 rows each
+    auto per = [&] { return (prm.rows + 16 * cluster - 1) / (16 * cluster) * 16; };
+    while (cluster < kCluster && (per() > kStripRows || (strips * cluster < 128 && per() > 128))) cluster *= 2;
+    if (per() <= kStripRows) {
+        prm.cluster = cluster;
+        prm.rows_per = (int)per();
+        const size_t smem = (size_t)(prm.rows_per * kStripPitch + prm.rows_per / 16 * 4) * 4;
+        return ptx::launch_chained<i8_strip_kernel<T, SR, VEC>>(prm, (int)(strips * cluster), kStripThreads, smem, cluster, st);
+    }
+    const cudaError_t e = ptx::launch_chained<i8_max_kernel<T, VEC>>(prm, (int)(prm.row_blocks * strips), 256, 0, 1, st);
     if (e != cudaSuccess) return e;
     const int tiles = (int)(mx4::tiles_of(pitch_of(prm.rows), 128) * prm.ct);
     const size_t smem = (128 * (128 * sizeof(T) / 4 + 4) + 32) * 4;
-    return prm.codes ? ptx::launch_chained<i8_tile_kernel<T, SR, true>>(prm, tiles, 256, smem, 1, st)
-                     : ptx::launch_chained<i8_tile_kernel<T, SR, false>>(prm, tiles, 256, smem, 1, st);
+    return ptx::launch_chained<i8_tile_kernel<T, SR, VEC>>(prm, tiles, 256, smem, 1, st);
+}
+
+template <typename T, bool SR>
+cudaError_t quantize_as(cudaStream_t st, const QuantParams &prm, bool vec)
+{
+    if (prm.codes) {
+        const cudaError_t e = vec ? quantize_rows<T, SR, true>(st, prm) : quantize_rows<T, SR, false>(st, prm);
+        if (e != cudaSuccess) return e;
+    }
+    if (!prm.codes_t) return cudaSuccess;
+    return vec ? quantize_cols<T, SR, true>(st, prm) : quantize_cols<T, SR, false>(st, prm);
 }
 
 }  // namespace
 
-int64_t i8_scratch_bytes(int64_t rows, int64_t cols)
-{
-    const int64_t rb = (rows + block_rows(rows) - 1) / block_rows(rows), cb = (cols + kMaxCols - 1) / kMaxCols;
-    return (rb * cols + cb * rows) * 4;
-}
+int64_t i8_scratch_bytes(int64_t rows, int64_t cols) { return rows <= kCluster * kStripRows ? 0 : row_blocks(rows) * cols * 4; }
 
 cudaError_t launch_i8_quantize(cudaStream_t st, const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, bool stochastic,
                                uint64_t seed, uint32_t node, int8_t *codes, float *scales, int8_t *codes_t, float *scales_t, void *scratch)
@@ -386,16 +483,13 @@ cudaError_t launch_i8_quantize(cudaStream_t st, const void *x, int dtype, int64_
     prm.seed_w = mx4::seed_word(seed, node);
     prm.codes = codes; prm.codes_t = codes_t;
     prm.scales = scales; prm.scales_t = scales_t;
-    prm.block_rows = block_rows(rows);
-    prm.row_blocks = (int)((rows + prm.block_rows - 1) / prm.block_rows);
-    prm.col_blocks = (int)((cols + kMaxCols - 1) / kMaxCols);
+    prm.row_blocks = (int)row_blocks(rows);
     prm.col_top = static_cast<uint32_t *>(scratch);
-    prm.row_top = prm.col_top + (int64_t)prm.row_blocks * cols;
-    prm.vec = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && ld * (dtype == GVQ_F32 ? 4 : 2) % 16 == 0;
+    const bool vec = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && ld * (dtype == GVQ_F32 ? 4 : 2) % 16 == 0;
     prm.ct = (int)mx4::tiles_of(pitch_of(cols), 128);
-    if (dtype == GVQ_F32) return stochastic ? quantize_as<float, true>(st, prm) : quantize_as<float, false>(st, prm);
-    if (dtype == GVQ_BF16) return stochastic ? quantize_as<__nv_bfloat16, true>(st, prm) : quantize_as<__nv_bfloat16, false>(st, prm);
-    return stochastic ? quantize_as<__half, true>(st, prm) : quantize_as<__half, false>(st, prm);
+    if (dtype == GVQ_F32) return stochastic ? quantize_as<float, true>(st, prm, vec) : quantize_as<float, false>(st, prm, vec);
+    if (dtype == GVQ_BF16) return stochastic ? quantize_as<__nv_bfloat16, true>(st, prm, vec) : quantize_as<__nv_bfloat16, false>(st, prm, vec);
+    return stochastic ? quantize_as<__half, true>(st, prm, vec) : quantize_as<__half, false>(st, prm, vec);
 }
 
 cudaError_t launch_i8_dequantize(cudaStream_t st, int num_sms, const int8_t *codes, const float *scales, int64_t rows, int64_t cols,

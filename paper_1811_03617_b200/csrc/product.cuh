@@ -5,18 +5,20 @@
 // Operands come by TMA (128-byte swizzle, zero fill outside), K-major (a row of the contraction is contiguous) or MN-major (a
 // row across it is; 16-bit types only).  A stage is 128 bytes of contraction of either: 64 entries of 16 bits or 128 of 8, four
 // MMAs.  Tiles are CG * 128 rows of A x BN rows of B.
-//   CG = 2, BN = 256   a pair of CTAs on two SMs; each holds its own 128 rows of A and half of B's rows, the even one issues
-//                      MMAs that read both: 64 bytes a clock and SM from L2, half of what a CTA alone on 128 x 128 would ask for.
+//   CG = 2, BN = 256, 128   a pair of CTAs on two SMs; each holds its own 128 rows of A and half of B's rows, the even one issues
+//                      MMAs that read both: 64 (96) bytes a clock and SM from L2, where a CTA alone on 128 x 128 would ask for 128.
 //                      Gated: B's first half are rows of the gate's weights (the even CTA's), the second of the other
-//                      projection's, so that the accumulator holds both values of 128 outputs.
+//                      projection's, so that the accumulator holds both values of an output.
 //   CG = 1, BN = 64    one CTA: products too small to give every SM a large tile.  Gated: 32 rows of either matrix.
-//   CG = 1, NA tiles   few rows (tokens): they become B, the tile as narrow as they are (BN = 16, 32 or 64) against NA * 128 rows
-//                      of weights; gated: NA = 2, a tile of either matrix.
+//   CG = 1, FEW        few rows (tokens): they become B, the tile as narrow as they are (BN = 16, 32 or 64) against rows_a rows
+//                      of weights, as many as spread them evenly over the SMs (the MMA takes 128; what the others hold is not
+//                      looked at).  Gated: rows_a rows of either matrix, one below the other, so that a step of the contraction is
+//                      one MMA; the two sums of an output meet in shared memory.
 // Where CG = 1 leaves SMs without a tile, a cluster of up to eight CTAs shares a tile's contraction; each leaves its sums in its
-// shared memory, where the stages were, and they add them up across the cluster, always in the same order.
+// shared memory, and they add them up across the cluster, always in the same order.
 //   warp 0      producer, one lane
 //   warp 1      MMA issuer, one lane (the order of issue is the order of execution)
-//   warps 2-5   epilogue: accumulator -> registers -> staging -> output along its rows
+//   warps 2-9   epilogue: accumulator -> registers -> staging -> output along its rows
 // Accumulators alternate between two column ranges of tensor memory.  Every mbarrier wait is bounded.
 #pragma once
 #include "activation.cuh"
@@ -29,7 +31,8 @@ namespace product {
 
 using namespace ptx;
 
-constexpr int NTHREADS = 192;
+constexpr int NTHREADS = 320;
+constexpr int kHalves = 2;             // epilogue warps that share a quarter of the tile's rows, every other 32 columns each
 constexpr int kJoinPitch = 129;        // (a row's words of 16 bytes, eight lanes' of them, lie in different banks)
 constexpr int kBox = 8192;             // an MN-major box: 64 entries (128 bytes) x 64 steps of the contraction
 constexpr uint32_t A_BYTES = 128 * 128;
@@ -38,33 +41,36 @@ enum { k16 = 0, kI8 = 1 };             // kinds of operands
 
 struct Params {
     CUtensorMap a[2], b[2];            // see the producer
-    CUtensorMap o[3];                  // outputs, boxes of 128 bytes x 32 rows (where tma_out says so)
     int64_t M, N;                      // rows of A (of one half), rows of B, as far as there are outputs
     int tiles_m, tiles_n;              // tiles_m: of both halves
     int half_tiles;                    // tiles_m of one half: two products with B in common are one, A's and the outputs' halves apart
     int n_stages, seg_stages, n_last;  // stages of a tile's contraction, of its first segment; MMAs of a segment's last stage
     int parts;                         // CTAs (a cluster) that share a tile's contraction; with more than one, a tile a cluster
     int group;                         // tiles along M that are gone through before the next along N
-    int swapped;                       // rows of A run along the output's rows
+    int rows_a, stages;                // FEW: rows of a matrix that a tile has (a multiple of 8); stages that there is room for
     void *out[3];                      // the product of either half; or the block's output, its gate and its other projection
     int64_t ld[3];
-    int tma_out;                       // a bit an output
+    int align[3];                      // bytes at whose multiples the outputs' rows start: 32, 16 or less
     int dtype, act, bf16;              // outputs' type; activation; operands' type, of 16 bits
     const float *scale_m[2], *scale_n[2];   // of 8-bit operands
     int32_t *error_word;
     int wait_kcycles, test_drop;
 };
 
-template <int CG, int BN, int NA> struct Shape {
-    static constexpr uint32_t B_BYTES = BN / CG * 128;
-    static constexpr uint32_t LOADED = NA * A_BYTES + B_BYTES, STAGE = LOADED;
-    static constexpr int STAGES = CG == 2 ? 6 : (int)(200 * 1024 / STAGE) < 8 ? (int)(200 * 1024 / STAGE) : 8;
-    static constexpr uint32_t ACC = NA * BN;                          // columns of an accumulator
-    static constexpr uint32_t TMEM = 2 * ACC <= 32 ? 32 : 2 * ACC <= 64 ? 64 : 2 * ACC <= 128 ? 128 : 2 * ACC <= 256 ? 256 : 512;
-    static constexpr uint32_t STAGING = CG == 2 || (BN == 64 && NA == 1) ? 8192 : 1024;   // of an epilogue warp; a few rows have no use for it
-    static constexpr size_t SMEM = (size_t)STAGE * STAGES + 4 * STAGING + 256 + 1024;
-    static_assert(STAGE % 1024 == 0 && 2 * ACC <= TMEM && SMEM <= 232448, "room");
-    static_assert(CG == 2 || (size_t)ACC / 4 * kJoinPitch * 16 <= (size_t)STAGE * STAGES, "room to join parts");
+template <int CG, int BN, bool FEW> struct Shape {
+    static constexpr uint32_t B_BYTES = BN / CG * 128, LOADED = A_BYTES + B_BYTES;
+    static constexpr uint32_t ROOM = FEW ? 168 * 1024 : 200 * 1024;   // for the stages
+    static constexpr int MOST = 16, STAGES = FEW ? MOST : (int)(ROOM / LOADED) < 8 ? (int)(ROOM / LOADED) : 8;
+    // sums on their way to other threads: of few rows behind the stages (and behind what the MMA reads past the last of them, 128 rows
+    // of A that may be fewer), else where the stages were
+    static constexpr uint32_t JOIN = BN / 4 * kJoinPitch * 16, JOIN_AT = FEW ? ROOM + A_BYTES : 0;
+    static constexpr uint32_t ALL = FEW ? (JOIN_AT + JOIN + 1023) / 1024 * 1024 : STAGES * LOADED;
+    static constexpr uint32_t TMEM = 2 * BN <= 32 ? 32 : 2 * BN <= 64 ? 64 : 2 * BN <= 128 ? 128 : 2 * BN <= 256 ? 256 : 512;
+    // of an epilogue warp: 16 rows of a piece (tiles of few rows have no use for it), and its columns' scales
+    static constexpr uint32_t PIECE = FEW ? 0 : 16 * 128, STAGING = PIECE + 512;
+    static constexpr size_t SMEM = (size_t)ALL + 4 * kHalves * STAGING + 512 + 1024;
+    static_assert(LOADED % 1024 == 0 && SMEM <= 232448, "room");
+    static_assert(CG == 2 || JOIN_AT + JOIN <= ALL, "room to join parts");
 };
 
 template <int CG>
@@ -108,15 +114,67 @@ __device__ __forceinline__ void store_four(void *out, int dtype, int64_t at, int
             if (e < n) store_one(out, dtype, at + e * step, x[e]);
     }
 }
-// 32 columns of a 64-column piece of a 16-bit type, as a TMA store reads it (see stage_swizzled16).
-__device__ __forceinline__ void stage_half16(unsigned char *buf, int lane, int half, int dtype, const float (&v)[32])
+// A lane's 32 columns of a row, which starts at a 16-byte boundary: whole 32-byte sectors where it starts at such a boundary.
+__device__ __forceinline__ void store32(void *p, int align, const uint32_t (&w)[8])
 {
+    if (align == 32)
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                     ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+    else {
+        static_cast<uint4 *>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        static_cast<uint4 *>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
+__device__ __forceinline__ void store_row(void *out, int dtype, int align, int64_t at, const float (&v)[32])
+{
+    uint32_t w[8];
+    if (dtype == GVQ_F32) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        uint32_t w[4];
+        for (int j = 0; j < 4; ++j) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = pack_as(dtype, v[8 * j + 2 * i], v[8 * j + 2 * i + 1]);
-        *reinterpret_cast<uint4 *>(buf + lane * 128 + (((4 * half + j) ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[8 * j + i]);
+            store32(static_cast<float *>(out) + at + 8 * j, align, w);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = pack_as(dtype, v[16 * j + 2 * i], v[16 * j + 2 * i + 1]);
+            store32(static_cast<uint16_t *>(out) + at + 16 * j, align, w);
+        }
+    }
+}
+// Rows that start anywhere: 16 of them at a time go through shared memory (16-byte chunk j of row r at place j ^ (r % 8)) and out along
+// the rows, two entries a lane of a 16-bit type where rows start at 4-byte boundaries.
+__device__ __forceinline__ void store_rows(unsigned char *buf, int lane, int dtype, void *out, int64_t at, int64_t ld, int rows, int cols,
+                                           const float (&v)[32])
+{
+    auto word = [&](int r, int c) { return buf + r * 128 + (((c >> 2) ^ (r & 7)) << 4) + (c & 3) * 4; };
+    const bool pairs = dtype != GVQ_F32 && (ld & 1) == 0 && (reinterpret_cast<uintptr_t>(static_cast<uint16_t *>(out) + at) & 3u) == 0;
+#pragma unroll 1
+    for (int r0 = 0; r0 < rows; r0 += 16) {
+        __syncwarp();
+        if ((lane & 16) == r0) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                *reinterpret_cast<float4 *>(word(lane & 15, 4 * j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        }
+        __syncwarp();
+        const int n = min(16, rows - r0);
+        const int64_t from = at + r0 * ld;
+        if (pairs) {
+            const int c = (lane & 15) * 2;
+#pragma unroll 4
+            for (int r = lane >> 4; r < n; r += 2) {
+                const float2 x = *reinterpret_cast<const float2 *>(word(r, c));
+                if (c + 1 < cols) *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(out) + from + r * ld + c) = pack_as(dtype, x.x, x.y);
+                else if (c < cols) store_one(out, dtype, from + r * ld + c, x.x);
+            }
+        } else {
+#pragma unroll 4
+            for (int r = 0; r < n; ++r)
+                if (lane < cols) store_one(out, dtype, from + r * ld + lane, *reinterpret_cast<const float *>(word(r, lane)));
+        }
     }
 }
 
@@ -130,88 +188,99 @@ __device__ __forceinline__ void place(const Params &prm, int tile, int &tm, int 
     tm = g * prm.group + r - tn * m;
 }
 
-// The CTAs of a cluster of P add up a tile's entries, four columns of a row a thread at a time, the parts in order, and do what
-// the epilogue does with them.  Lanes lie along what is contiguous in the output.
-template <int KIND, int BN, int NA, bool GATED, int P>
-__device__ __forceinline__ void join_parts(const Params &prm, const float4 *join, int part, int tm, int tn)
+// Sums that lie in the shared memory of the P CTAs of a cluster (of this one): added up, four columns of a row a thread at a time, the
+// parts in order, and then what the epilogue does with them.  Lanes lie along what is contiguous in the output.  tid: this thread's
+// place among the `threads` that do this in each CTA, whole warps.
+template <int KIND, int BN, bool FEW, bool GATED, int P>
+__device__ __forceinline__ void join_parts(const Params &prm, const float4 *join, int part, int tm, int tn, int tid, int threads)
 {
-    constexpr int HN = GATED && NA == 1 ? BN / 2 : BN;
-    const int half = tm >= prm.half_tiles, hm = tm - half * prm.half_tiles;
-    const int64_t m0 = (int64_t)hm * 128, n0 = (int64_t)tn * HN;
-    const int rows = (int)min((int64_t)128, prm.M - m0), cols = (int)min((int64_t)HN, prm.N - n0);
-    const int quads = (cols + 3) / 4, inner = prm.swapped ? rows : quads;
+    constexpr int HN = GATED && !FEW ? BN / 2 : BN;
+    const int half = tm >= prm.half_tiles, hm = tm - half * prm.half_tiles, per = FEW ? prm.rows_a : 128;
+    const int64_t m0 = (int64_t)hm * per, n0 = (int64_t)tn * HN;
+    const int rows = (int)min((int64_t)per, prm.M - m0), cols = (int)min((int64_t)HN, prm.N - n0);
+    const int quads = (cols + 3) / 4, inner = FEW ? rows : quads, total = rows * quads;
     uint32_t from[P];
+    if constexpr (P > 1) {
 #pragma unroll
-    for (int p = 0; p < P; ++p) from[p] = cluster_address(smem_u32(join), p);
-    auto sum = [&](int c4, int r, float (&y)[4]) {
-        float4 x[P];
-#pragma unroll
-        for (int p = 0; p < P; ++p) x[p] = load_cluster(from[p] + (c4 * kJoinPitch + r) * 16);
-        if constexpr (KIND == kI8) {
-            int s[4] = {0, 0, 0, 0};
-#pragma unroll
-            for (int p = 0; p < P; ++p) {
-                s[0] += __float_as_int(x[p].x); s[1] += __float_as_int(x[p].y);
-                s[2] += __float_as_int(x[p].z); s[3] += __float_as_int(x[p].w);
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = __int2float_rn(s[e]);
-        } else {
-#pragma unroll
-            for (int p = 1; p < P; ++p) { x[0].x += x[p].x; x[0].y += x[p].y; x[0].z += x[p].z; x[0].w += x[p].w; }
-            y[0] = x[0].x; y[1] = x[0].y; y[2] = x[0].z; y[3] = x[0].w;
-        }
-    };
-#pragma unroll 2
-    for (int it = part * NTHREADS + threadIdx.x; it < rows * quads; it += P * NTHREADS) {
-        const int o = it / inner, i = it - o * inner, c4 = prm.swapped ? o : i, r = prm.swapped ? i : o;
+        for (int p = 0; p < P; ++p) from[p] = cluster_address(smem_u32(join), p);
+    }
+    auto one = [&](int it) {
+        const int o = it / inner, i = it - o * inner, c4 = FEW ? o : i, r = FEW ? i : o;
         const int n = cols - c4 * 4;
         const int64_t m = m0 + r, col = n0 + c4 * 4;
-        auto scaled = [&](int which, float (&y)[4]) {
-            sum(c4 + which * (NA == 1 ? HN : BN) / 4, r, y);
-            if constexpr (KIND == kI8) {
-                const float sm = prm.scale_m[NA == 2 ? which : 0][m];
-                const float *sn = prm.scale_n[GATED && NA == 1 ? which : 0] + col;
+        auto value = [&](int which, float (&y)[4]) {
+            const int at = (c4 + (FEW ? 0 : which * HN / 4)) * kJoinPitch + r + (FEW ? which * prm.rows_a : 0);
+            float4 x[P];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = e < n ? y[e] * sm * sn[e] : 0.0f;
+            for (int p = 0; p < P; ++p) x[p] = P > 1 ? load_cluster(from[p] + at * 16) : join[at];
+            if constexpr (KIND == kI8) {
+                int s[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    s[0] += __float_as_int(x[p].x); s[1] += __float_as_int(x[p].y);
+                    s[2] += __float_as_int(x[p].z); s[3] += __float_as_int(x[p].w);
+                }
+                const float sm = prm.scale_m[FEW ? which : 0][m];
+                const float *sn = prm.scale_n[FEW ? 0 : which] + col;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = e < n ? __int2float_rn(s[e]) * sm * sn[e] : 0.0f;
+            } else {
+#pragma unroll
+                for (int p = 1; p < P; ++p) { x[0].x += x[p].x; x[0].y += x[p].y; x[0].z += x[p].z; x[0].w += x[p].w; }
+                y[0] = x[0].x; y[1] = x[0].y; y[2] = x[0].z; y[3] = x[0].w;
             }
         };
         auto store = [&](int k, const float (&y)[4]) {
             const int64_t ld = prm.ld[k];
-            store_four(prm.out[k], prm.dtype, prm.swapped ? m + col * ld : m * ld + col, prm.swapped ? ld : 1, y, n,
-                       !prm.swapped && (prm.tma_out >> k & 1));
+            store_four(prm.out[k], prm.dtype, FEW ? m + col * ld : m * ld + col, FEW ? ld : 1, y, n, !FEW && prm.align[k] >= 16);
         };
         if constexpr (GATED) {
             float g[4], u[4], h[4];
-            scaled(0, g);
-            scaled(1, u);
+            value(0, g);
+            value(1, u);
 #pragma unroll
             for (int e = 0; e < 4; ++e) h[e] = activation(prm.act, g[e]) * u[e];
             store(0, h);
             if (prm.out[1]) { store(1, g); store(2, u); }
         } else {
             float y[4];
-            scaled(0, y);
+            value(0, y);
             store(half, y);
         }
+    };
+    // (a warp's lanes go round together: what follows are barriers and a dealloc that its lanes take as one)
+#pragma unroll 1
+    for (int it0 = part * threads + (tid & ~31); it0 < total; it0 += P * threads) {
+        const int it = it0 + (tid & 31);
+        if (it < total) one(it);
+        __syncwarp();
     }
 }
+// The epilogue's warps alone: all of them have come here, and whether `ok` held for all.
+__device__ __forceinline__ bool epilogue_and(bool ok)
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)ok), "n"(32 * 4 * kHalves) : "memory");
+    return r != 0;
+}
 
-template <int KIND, int CG, int BN, int NA, bool A_MN, bool B_MN, bool GATED>
+template <int KIND, int CG, int BN, bool FEW, bool A_MN, bool B_MN, bool GATED>
 __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_constant__ Params prm)
 {
-    using S = Shape<CG, BN, NA>;
+    using S = Shape<CG, BN, FEW>;
     constexpr int KS = KIND == kI8 ? 128 : 64;                        // entries of the contraction a stage
-    constexpr bool SIDE = GATED && NA == 1;                           // both matrices lie side by side in B
+    constexpr bool SIDE = GATED && !FEW;                              // both matrices lie side by side in B
     constexpr int HN = SIDE ? BN / 2 : BN;                            // columns of the output a tile has
-    constexpr int UP = NA == 2 ? BN : HN;                             // accumulator columns from the gate to the other projection
     constexpr int BL = BN / CG;                                       // rows of B that this CTA holds
-    static_assert(!(KIND == kI8 && (A_MN || B_MN)) && (!B_MN || BL % 64 == 0) && (NA == 1 || (CG == 1 && GATED)), "forms");
+    static_assert(!(KIND == kI8 && (A_MN || B_MN)) && (!B_MN || BL % 64 == 0) && !(FEW && (CG == 2 || B_MN)) && !(GATED && A_MN), "forms");
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    unsigned char *staging = smem + (size_t)S::STAGE * S::STAGES;
-    float4 *join = reinterpret_cast<float4 *>(smem);                  // [ACC / 4][kJoinPitch]: four columns of a row
-    uint64_t *bars = reinterpret_cast<uint64_t *>(staging + 4 * S::STAGING);
+    unsigned char *staging = smem + S::ALL;
+    float4 *join = reinterpret_cast<float4 *>(smem + S::JOIN_AT);     // [BN / 4][kJoinPitch]: four columns of a row
+    uint64_t *bars = reinterpret_cast<uint64_t *>(staging + 4 * kHalves * S::STAGING);
+    const uint32_t a_bytes = FEW ? prm.rows_a * 128 : A_BYTES, stage_bytes = (FEW && GATED ? 2 : 1) * a_bytes + S::B_BYTES;
+    const uint32_t n_stage = FEW ? prm.stages : S::STAGES;
     uint64_t *full = bars, *empty = full + S::STAGES;                 // [STAGES]
     uint64_t *d_full = empty + S::STAGES;                             // [2] accumulator complete
     uint64_t *d_empty = d_full + 2;                                   // [2] accumulator read
@@ -223,23 +292,36 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
     const int parts = CG == 1 ? prm.parts : 1, part = parts > 1 ? (int)cluster_rank() : 0;
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::STAGES; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(d_full + i, 1); mbar_init(d_empty + i, 4 * CG); }
+        for (int i = 0; i < 2; ++i) { mbar_init(d_full + i, 1); mbar_init(d_empty + i, 4 * kHalves * CG); }
         *abort_flag = 0;
         const_cast<int *>(abort_flag)[2] = prm.wait_kcycles;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc<CG>(tmem_slot, S::TMEM);
     tc_fence_before();
-    if (CG == 2) cluster_sync(); else __syncthreads();
+    if (CG == 2) cluster_sync_any(); else __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     launch_dependents();
-    grid_dependency_wait();      // what earlier launches wrote is visible from here on
-    bool failed = false;
-
     const int n_tiles = prm.tiles_m * prm.tiles_n;
     const int first = blockIdx.x / (CG * parts), stride = gridDim.x / (CG * parts);
     const int st0 = prm.n_stages * part / parts, st1 = prm.n_stages * (part + 1) / parts;    // this CTA's stages
+    if constexpr (FEW) {
+        // weights on their way to L2 while the launch before this one ends (nothing is read yet that it may write)
+        if (warp == 0 && elect_one()) {
+            int tm, tn;
+            place(prm, first, tm, tn);
+            for (int st = st0; st < min(st1, st0 + (int)n_stage); ++st) {
+                const int seg = st >= prm.seg_stages, k = (st - seg * prm.seg_stages) * KS, m0 = tm * prm.rows_a;
+                prefetch_2d(prm.a + seg, A_MN ? m0 : k, A_MN ? k : m0);
+                if (A_MN && a_bytes > kBox) prefetch_2d(prm.a + seg, m0 + 64, k);
+                if (GATED) prefetch_2d(prm.a + 1, k, m0);
+            }
+        }
+        __syncwarp();
+    }
+    grid_dependency_wait();      // what earlier launches wrote is visible from here on
+    bool failed = false;
 
     if (warp == 0) {
         // ------------------------------------------------------------------ producer
@@ -250,7 +332,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
                 int tm, tn;
                 place(prm, tile, tm, tn);
                 const int half = tm >= prm.half_tiles;
-                const int m0 = (tm - half * prm.half_tiles) * 128 * CG + 128 * rank;
+                const int m0 = (tm - half * prm.half_tiles) * (FEW ? prm.rows_a : 128 * CG) + 128 * rank;
                 const int n0 = SIDE ? tn * HN : tn * BN + BL * rank;
                 for (int st = st0; st < st1; ++st, ++c) {
                     if (!mbar_poll(empty + s, phase, abort_flag)) { failed = true; break; }
@@ -259,19 +341,16 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
                         // a contraction of two segments has a map of either operand for each; two halves one of A
                         const int seg = st >= prm.seg_stages;
                         const int k = (st - seg * prm.seg_stages) * KS;
-                        unsigned char *dst = smem + s * S::STAGE, *dst_b = dst + NA * A_BYTES;
-                        if (rank == 0) mbar_arrive_expect_tx(full + s, CG * S::LOADED);
+                        unsigned char *dst = smem + s * stage_bytes, *dst_b = dst + stage_bytes - S::B_BYTES;
+                        if (rank == 0) mbar_arrive_expect_tx(full + s, CG * stage_bytes);
                         const uint32_t bar = CG == 2 ? in_leader(full + s) : 0;
                         auto load = [&](unsigned char *to, const CUtensorMap *map, bool mn, int at) {
                             if (CG == 2) tma_load_2d_pair(to, map, mn ? at : k, mn ? k : at, bar);
                             else tma_load_2d(to, map, mn ? at : k, mn ? k : at, full + s);
                         };
-#pragma unroll
-                        for (int i = 0; i < NA; ++i) {
-                            const CUtensorMap *map = prm.a + (NA == 2 ? i : half + seg);
-                            load(dst + i * A_BYTES, map, A_MN, m0);
-                            if (A_MN) load(dst + i * A_BYTES + kBox, map, A_MN, m0 + 64);
-                        }
+                        load(dst, prm.a + half + seg, A_MN, m0);
+                        if (A_MN && (!FEW || a_bytes > kBox)) load(dst + kBox, prm.a + half + seg, A_MN, m0 + 64);
+                        if (FEW && GATED) load(dst + a_bytes, prm.a + 1, A_MN, m0);
                         if constexpr (SIDE && CG == 2) load(dst_b, prm.b + rank, false, n0);
                         else if constexpr (SIDE) {
                             load(dst_b, prm.b, false, n0);
@@ -281,12 +360,12 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
                             for (int i = 0; i < BL / 64; ++i) load(dst_b + i * kBox, prm.b + seg, true, n0 + 64 * i);
                         } else load(dst_b, prm.b + seg, false, n0);
                     }
-                    if (++s == S::STAGES) { s = 0; phase ^= 1; }
+                    if (++s == n_stage) { s = 0; phase ^= 1; }
                 }
             }
             if (failed && rank == 0) {   // give the copies already in flight a bounded chance to land before the CTA exits
-                for (uint32_t i = c > S::STAGES ? c - S::STAGES : 0; i < c; ++i)
-                    for (int it = 0; it < 100000 && !mbar_try_wait(full + i % S::STAGES, (i / S::STAGES) & 1); ++it) {}
+                for (uint32_t i = c > n_stage ? c - n_stage : 0; i < c; ++i)
+                    for (int it = 0; it < 100000 && !mbar_try_wait(full + i % n_stage, (i / n_stage) & 1); ++it) {}
             }
         }
         failed = __any_sync(0xffffffffu, failed);
@@ -296,13 +375,14 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
             uint32_t s = 0, phase = 0, t = 0;
             const uint32_t base = smem_u32(smem);
             const uint64_t a0 = A_MN ? make_mn_desc(base, kBox) : make_b_desc(base);
-            const uint64_t b0 = B_MN ? make_mn_desc(base + NA * A_BYTES, kBox) : make_b_desc(base + NA * A_BYTES);
+            const uint64_t b0 = B_MN ? make_mn_desc(base + stage_bytes - S::B_BYTES, kBox)
+                                     : make_b_desc(base + stage_bytes - S::B_BYTES);
             // 32 bytes of a K-major row, or 16 rows of 128 bytes of an MN-major box
             constexpr uint32_t IA = A_MN ? 16 * 128 / 16 : 2, IB = B_MN ? 16 * 128 / 16 : 2;
             const uint32_t idesc = KIND == kI8 ? idesc_i8(128 * CG, BN)
                                                : make_idesc_f16(128 * CG, BN, A_MN, B_MN) | (prm.bf16 ? (1u << 7) | (1u << 10) : 0u);
             for (int tile = first; tile < n_tiles && !failed; tile += stride, ++t) {
-                const uint32_t buf = t & 1, d = tmem + buf * S::ACC;
+                const uint32_t buf = t & 1, d = tmem + buf * BN;
                 if (t > 1) {
                     if (!mbar_poll(d_empty + buf, ((t >> 1) - 1) & 1, abort_flag)) { failed = true; break; }
                     tc_fence_after();
@@ -310,184 +390,154 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
                 for (int st = st0; st < st1; ++st) {
                     if (!mbar_poll(full + s, phase, abort_flag)) { failed = true; break; }
                     tc_fence_after();
-                    const uint64_t da = a0 + s * (S::STAGE >> 4), db = b0 + s * (S::STAGE >> 4);
+                    const uint64_t da = a0 + s * (stage_bytes >> 4), db = b0 + s * (stage_bytes >> 4);
                     auto issue = [&](int n_mma) {      // (a constant, except in a short last stage)
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
                             if (k < n_mma) {
-#pragma unroll
-                                for (int i = 0; i < NA; ++i) {
-                                    const uint64_t ak = da + i * (A_BYTES >> 4) + k * IA, bk = db + k * IB;
-                                    if (KIND == kI8) mma_i8<CG>(d + i * BN, ak, bk, idesc, st > st0 || k > 0);
-                                    else tc_mma_f16<CG>(d + i * BN, ak, bk, idesc, st > st0 || k > 0);
-                                }
+                                if (KIND == kI8) mma_i8<CG>(d, da + k * IA, db + k * IB, idesc, st > st0 || k > 0);
+                                else tc_mma_f16<CG>(d, da + k * IA, db + k * IB, idesc, st > st0 || k > 0);
                             }
                     };
                     if (prm.n_last < 4 && (st == prm.n_stages - 1 || st == prm.seg_stages - 1)) issue(prm.n_last); else issue(4);
                     if (CG == 2) tc_commit_pair(empty + s); else tc_commit(empty + s);
                     if (st == st1 - 1) { if (CG == 2) tc_commit_pair(d_full + buf); else tc_commit(d_full + buf); }
-                    if (++s == S::STAGES) { s = 0; phase ^= 1; }
+                    if (++s == n_stage) { s = 0; phase ^= 1; }
                 }
             }
         }
         failed = __any_sync(0xffffffffu, failed);
     } else {
         // ------------------------------------------------------------------ epilogue
-        const int q = warp & 3;
+        const int q = warp & 3, side = (warp - 2) >> 2;      // a quarter of the rows; pieces of 32 columns side, side + 2, ...
         const uint32_t lane_base = (uint32_t)(32 * q) << 16;
         unsigned char *mine = staging + (warp - 2) * S::STAGING;
-        float *piece_buf = reinterpret_cast<float *>(mine);
-        uint32_t t = 0, stores = 0;
+        float *scales = reinterpret_cast<float *>(mine + S::PIECE);      // of the columns: [matrix][piece][32]
+        uint32_t t = 0;
         const int dtype = prm.dtype;
+        constexpr int PW = HN < 32 ? HN : 32, NP = HN / PW;  // columns of a piece, pieces of a tile
         for (int tile = first; tile < n_tiles; tile += stride, ++t) {
             int tm, tn;
             place(prm, tile, tm, tn);
             const int half = tm >= prm.half_tiles;
-            const int64_t m0 = (int64_t)(tm - half * prm.half_tiles) * 128 * CG + 128 * rank + 32 * q, n0 = (int64_t)tn * HN;
-            const int rows = (int)max((int64_t)0, min((int64_t)32, prm.M - m0));
-            // 8-bit operands: the scale of this lane's row, and of every 32nd column from this lane's on (of either matrix)
-            constexpr int NS = KIND == kI8 ? (HN + 31) / 32 : 1;
-            float sm[NA], sn[SIDE ? 2 : 1][NS];
-            if constexpr (KIND == kI8) {
-                if (parts == 1) {
+            const int64_t m0 = (int64_t)(tm - half * prm.half_tiles) * (FEW ? prm.rows_a : 128 * CG) + 128 * rank + 32 * q, n0 = (int64_t)tn * HN;
+            const int rows = (int)max((int64_t)0, min((int64_t)(FEW ? min(32, prm.rows_a - 32 * q) : 32), prm.M - m0));
+            // 8-bit operands: the scale of this lane's row, and those of the columns, which every lane reads
+            constexpr int NS = (NP + kHalves - 1) / kHalves;
+            float sm = 0.0f;
+            if constexpr (KIND == kI8 && !(FEW && GATED)) {
+                if (lane < rows) sm = __ldg(prm.scale_m[0] + m0 + lane);
 #pragma unroll
-                    for (int i = 0; i < NA; ++i) sm[i] = lane < rows ? __ldg(prm.scale_m[i] + m0 + lane) : 0.0f;
+                for (int i = 0; i < (SIDE ? 2 : 1); ++i)
 #pragma unroll
-                    for (int i = 0; i < (SIDE ? 2 : 1); ++i)
-#pragma unroll
-                        for (int j = 0; j < NS; ++j)
-                            sn[i][j] = n0 + 32 * j + lane < prm.N ? __ldg(prm.scale_n[i] + n0 + 32 * j + lane) : 0.0f;
-                }
+                    for (int j = 0; j < NS; ++j) {
+                        const int64_t n = n0 + 32 * (kHalves * j + side) + lane;
+                        scales[(i * NS + j) * 32 + lane] = n < prm.N ? __ldg(prm.scale_n[i] + n) : 0.0f;
+                    }
+                __syncwarp();
             }
             const uint32_t buf = t & 1;
             bool ok = mbar_poll(d_full + buf, (t >> 1) & 1, abort_flag);
-            if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
+            // (those that go on to wait for one another below have to agree)
+            ok = FEW && GATED && parts == 1 ? epilogue_and(ok) : __all_sync(0xffffffffu, ok);
+            if (!ok) { failed = true; break; }
             tc_fence_after();
-            const uint32_t acc = tmem + lane_base + buf * S::ACC;
-            if (parts > 1) {           // the stages have been read: what the part has goes into their place
+            const uint32_t acc = tmem + lane_base + buf * BN;
+            if (parts > 1 || (FEW && GATED)) {           // sums that other threads take up
                 if constexpr (CG == 1) {
 #pragma unroll 1
-                    for (int c = 0; c < (int)S::ACC; c += 16) {
+                    for (int c = 16 * side; c < BN; c += 16 * kHalves) {
                         float v[16];
                         tmem_ld16_wait(acc + c, v);
 #pragma unroll
                         for (int i = 0; i < 16; i += 4)
                             join[(c + i) / 4 * kJoinPitch + 32 * q + lane] = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
                     }
+                    if constexpr (FEW && GATED) {
+                        if (parts == 1) {
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(d_empty + buf);
+                            epilogue_and(true);
+                            join_parts<KIND, BN, FEW, GATED, 1>(prm, join, 0, tm, tn, threadIdx.x - 64, 32 * 4 * kHalves);
+                            epilogue_and(true);      // (the next tile's sums take their place)
+                        }
+                    }
                 }
                 continue;
             }
-            // 32 columns of one matrix's sums; `j`: c / 32, a constant where it indexes registers
-            auto sums = [&](int which, int c, int j, float (&v)[32]) {
-                if constexpr (BN >= 32) tmem_ld32_wait(acc + (GATED ? which * UP : 0) + c, v);
+            // the sums of one matrix's piece p = 2 j + side
+            auto sums = [&](int which, int j, float (&v)[32]) {
+                const uint32_t from = acc + (SIDE ? which * HN : 0) + 32 * (kHalves * j + side);
+                if constexpr (PW == 32) tmem_ld32_wait(from, v);
                 else {
                     float w[16];
-                    tmem_ld16_wait(acc + (GATED ? which * UP : 0), w);
+                    tmem_ld16_wait(from, w);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = i < 16 ? w[i] : 0.0f;
                 }
                 if constexpr (KIND == kI8) {
-                    float mine_n = 0.0f;
+                    const float4 *of = reinterpret_cast<const float4 *>(scales + ((SIDE ? which : 0) * NS + j) * 32);
 #pragma unroll
-                    for (int x = 0; x < NS; ++x)
-                        if (x == j) mine_n = sn[SIDE ? which : 0][x];
-                    const float mine_m = sm[NA == 2 ? which : 0];
-#pragma unroll
-                    for (int i = 0; i < (BN >= 32 ? 32 : 16); ++i)
-                        v[i] = __int2float_rn(__float_as_int(v[i])) * mine_m * __shfl_sync(0xffffffffu, mine_n, i);
+                    for (int i = 0; i < PW; i += 4) {
+                        const float4 x = of[i / 4];
+                        v[i] = __int2float_rn(__float_as_int(v[i])) * sm * x.x;
+                        v[i + 1] = __int2float_rn(__float_as_int(v[i + 1])) * sm * x.y;
+                        v[i + 2] = __int2float_rn(__float_as_int(v[i + 2])) * sm * x.z;
+                        v[i + 3] = __int2float_rn(__float_as_int(v[i + 3])) * sm * x.w;
+                    }
                 }
             };
-            // output `o` (0: the product, or the block's; 1, 2: its projections)
-            auto values = [&](int o, int c, int j, float (&v)[32]) {
-                if constexpr (GATED) {
-                    if (o > 0) { sums(o - 1, c, j, v); return; }
-                    float u[32];
-                    sums(0, c, j, v);
-                    sums(1, c, j, u);
-                    activate(prm.act, v, u);
-                } else sums(0, c, j, v);
-            };
-            const int n_out = GATED && prm.out[1] ? 3 : 1;
-            constexpr int PW = HN < 64 ? HN : 64;                      // columns of a piece
-            constexpr int NP = HN / PW;
+            const int n_out = SIDE && prm.out[1] ? 3 : 1;
 #pragma unroll 1
             for (int oi = 0; oi < n_out; ++oi) {
-                const int o = n_out - 1 - oi;                          // (the block's output last)
-                const int slot = GATED ? o : half;
+                const int o = n_out - 1 - oi;                          // 0: the product, or the block's; 1, 2: its projections, first
+                const int slot = SIDE ? o : half;
                 void *out = prm.out[slot];
                 const int64_t ld = prm.ld[slot];
-                const bool tma = prm.tma_out >> slot & 1;
+                const int align = prm.align[slot];
 #pragma unroll 1
-                for (int p = 0; p < NP; ++p) {
-                    const int64_t n = n0 + p * PW;
-                    const bool wanted = rows > 0 && n < prm.N;
-                    // (a tiled store writes whole 16-byte chunks: past the last column where that does not end at one)
-                    const bool by_tma = PW == 64 && tma && (n + 64 <= prm.N || prm.N * (dtype == GVQ_F32 ? 4 : 2) % 16 == 0);
-                    unsigned char *to = dtype != GVQ_F32 && by_tma ? mine + (stores & 1) * 4096 : mine;
+                for (int j = 0; kHalves * j + side < NP; ++j) {
+                    const int64_t n = n0 + 32 * (kHalves * j + side);
+                    const int cols = (int)min((int64_t)PW, prm.N - n);
+                    if (rows <= 0 || cols <= 0) break;
+                    float v[32];
+                    if constexpr (SIDE) {
+                        if (o > 0) sums(o - 1, j, v);
+                        else {
+                            float u[32];
+                            sums(0, j, v);
+                            sums(1, j, u);
+                            activate(prm.act, v, u);
+                        }
+                    } else sums(0, j, v);
+                    if constexpr (FEW) {       // rows of A run along the output's rows: a warp's lanes do too
+                        if (lane < rows) {
 #pragma unroll
-                    for (int h = 0; h < (PW + 31) / 32; ++h) {
-                        float v[32];
-                        values(o, p * PW + 32 * h, p * (PW / 32) + h, v);
-                        if (oi == n_out - 1 && p == NP - 1 && h == (PW + 31) / 32 - 1) {
-                            tc_fence_before();
-                            __syncwarp();
-                            if (lane == 0) { if (CG == 2) mbar_arrive_cluster(in_leader(d_empty + buf)); else mbar_arrive(d_empty + buf); }
+                            for (int i = 0; i < PW; ++i)
+                                if (i < cols) store_one(out, dtype, m0 + lane + (n + i) * ld, v[i]);
                         }
-                        const int cols = (int)min((int64_t)min(PW, 32), prm.N - n - 32 * h);
-                        if (!wanted || cols <= 0) continue;
-                        if (by_tma) {
-                            // rows of 128 bytes, swizzled, stored by the copy engine: what the pieces cost in shared-memory
-                            // bandwidth is taken from the MMAs, so they pass through it in the output's type and once
-                            if (h == 0) {
-                                if (lane == 0) { if (dtype != GVQ_F32) bulk_wait_group_read<1>(); else bulk_wait_group_read<0>(); }
-                                __syncwarp();
-                            }
-                            if (dtype == GVQ_F32) stage_swizzled(to + 4096 * h, lane, v);
-                            else stage_half16(to, lane, h, dtype, v);
-                        } else if (prm.swapped) {       // rows of A run along the output's rows: a warp's lanes do too
-                            if (lane < rows) {
-#pragma unroll
-                                for (int i = 0; i < 32; ++i)
-                                    if (i < cols) store_one(out, dtype, m0 + lane + (n + 32 * h + i) * ld, v[i]);
-                            }
-                        } else {
-                            if (lane == 0) bulk_wait_group_read<0>();      // the staging area may still be on its way out
-                            __syncwarp();
-                            if constexpr (S::STAGING >= 32 * kPiecePitch * 4) {
-                                stage_piece(piece_buf, lane, v);
-                                const int64_t at = m0 * ld + n + 32 * h;
-                                if (dtype == GVQ_F32) store_piece(piece_buf, lane, static_cast<float *>(out) + at, ld, rows, cols);
-                                else if (dtype == GVQ_BF16) store_piece(piece_buf, lane, static_cast<__nv_bfloat16 *>(out) + at, ld, rows, cols);
-                                else store_piece(piece_buf, lane, static_cast<__half *>(out) + at, ld, rows, cols);
-                            }
-                        }
-                    }
-                    if (by_tma && wanted) {
-                        fence_proxy_async();
-                        __syncwarp();
-                        if (lane == 0) {
-                            tma_store_2d(prm.o + slot, (int)n, (int)m0, to);
-                            if (dtype == GVQ_F32 && n + 32 < prm.N) tma_store_2d(prm.o + slot, (int)n + 32, (int)m0, to + 4096);
-                            bulk_commit_group();
-                        }
-                        ++stores;
-                    }
+                    } else if (align >= 16 && cols == 32) {
+                        if (lane < rows) store_row(out, dtype, align, (m0 + lane) * ld + n, v);
+                    } else
+                        store_rows(mine, lane, dtype, out, m0 * ld + n, ld, rows, cols, v);
                 }
             }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) { if (CG == 2) mbar_arrive_cluster(in_leader(d_empty + buf)); else mbar_arrive(d_empty + buf); }
         }
-        if (lane == 0) bulk_wait_group_all();
     }
 
     if constexpr (CG == 1) {
         if (parts > 1) {
-            __syncwarp();
-            cluster_sync();
+            cluster_sync_any();
             if (!failed) {
                 int tm, tn;
                 place(prm, first, tm, tn);
-                if (parts == 2) join_parts<KIND, BN, NA, GATED, 2>(prm, join, part, tm, tn);
-                else if (parts == 4) join_parts<KIND, BN, NA, GATED, 4>(prm, join, part, tm, tn);
-                else join_parts<KIND, BN, NA, GATED, 8>(prm, join, part, tm, tn);
+                if (parts == 2) join_parts<KIND, BN, FEW, GATED, 2>(prm, join, part, tm, tn, threadIdx.x, NTHREADS);
+                else if (parts == 4) join_parts<KIND, BN, FEW, GATED, 4>(prm, join, part, tm, tn, threadIdx.x, NTHREADS);
+                else join_parts<KIND, BN, FEW, GATED, 8>(prm, join, part, tm, tn, threadIdx.x, NTHREADS);
             }
         }
     }
@@ -498,27 +548,22 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
     tc_fence_before();
     __syncwarp();
     // (the other CTAs of a cluster use this one's barriers and memory until here)
-    if (CG == 2 || parts > 1) cluster_sync(); else __syncthreads();
+    if (CG == 2 || parts > 1) cluster_sync_any(); else __syncthreads();
     tc_fence_after();
+    __syncwarp();
     if (warp == 1) tmem_dealloc<CG>(tmem, S::TMEM);
 }
 
 // ---------------------------------------------------------------------------------------------------- host side
 inline int tiles_of(int64_t n, int per) { return (int)((n + per - 1) / per); }
 
-// How a product M x N (rows of tokens x outputs) is cut up.
-struct Cut {
-    bool swapped;      // the rows of tokens are B
-    int cg, bn;
-};
-
-template <int KIND, int CG, int BN, int NA, bool A_MN, bool B_MN, bool GATED>
+template <int KIND, int CG, int BN, bool FEW, bool A_MN, bool B_MN, bool GATED>
 cudaError_t launch(cudaStream_t st, int num_sms, const Params &prm)
 {
-    using S = Shape<CG, BN, NA>;
+    using S = Shape<CG, BN, FEW>;
     const int cluster = CG * prm.parts;
     const int64_t tiles = (int64_t)prm.tiles_m * prm.tiles_n;
-    return launch_chained<product_kernel<KIND, CG, BN, NA, A_MN, B_MN, GATED>>(
+    return launch_chained<product_kernel<KIND, CG, BN, FEW, A_MN, B_MN, GATED>>(
         prm, cluster * (int)(tiles < num_sms / cluster ? tiles : num_sms / cluster), NTHREADS, S::SMEM, cluster, st);
 }
 
@@ -536,55 +581,102 @@ inline bool encode(EncodeTiledFn enc, CUtensorMap *map, int kind, const void *p,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Output `slot` [M][N], rows ld entries apart: by TMA where its rows start at 16-byte boundaries.
-inline void set_output(EncodeTiledFn enc, Params &prm, int slot, void *out, int dtype, int64_t M, int64_t N, int64_t ld)
+// Output `slot`, rows ld entries apart.
+inline void set_output(Params &prm, int slot, void *out, int dtype, int64_t ld)
 {
     prm.out[slot] = out;
     prm.ld[slot] = ld;
-    const size_t size = dtype == GVQ_F32 ? 4 : 2;
-    if (prm.swapped || !out || (reinterpret_cast<uintptr_t>(out) & 15u) != 0 || (M > 1 && ld * size % 16 != 0)) return;
-    cuuint64_t dims[2] = {(cuuint64_t)N, (cuuint64_t)M};
-    cuuint64_t strides[1] = {(cuuint64_t)((M > 1 ? ld : (N * size + 15) / 16 * 16 / size) * size)};
-    cuuint32_t box[2] = {(cuuint32_t)(128 / size), 32}, estr[2] = {1, 1};
-    const CUtensorMapDataType type = dtype == GVQ_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
-                                     : dtype == GVQ_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    if (enc(&prm.o[slot], type, 2, out, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-            CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS)
-        prm.tma_out |= 1 << slot;      // (strides of 2^40 bytes and more are not taken)
+    const uint64_t at = reinterpret_cast<uintptr_t>(out) | (uint64_t)(ld * (dtype == GVQ_F32 ? 4 : 2));
+    prm.align[slot] = at % 32 == 0 ? 32 : at % 16 == 0 ? 16 : 1;
 }
 
-// Few rows of tokens: the weights take the 128-row side of the tile, and the tile is as wide as the few rows need.  Otherwise
-// pairs of CTAs on 256 x 256 tiles where smaller ones would need a second wave.  `n_small`: columns of the output a 64-column
-// tile has.
-inline Cut cut(int num_sms, int64_t M, int64_t N, int n_small)
+// How a product of M rows of tokens and N outputs is cut up.
+struct Cut {
+    bool few;          // the tokens are B: A and B, M and N change places
+    int cg, bn;        // of the kernel
+    int rows_a, parts;
+};
+
+// Parts of a contraction of n stages where a CTA has a tile alone: as many as there are SMs for, of `least` stages at least.  Clusters
+// of four fill 128 of 148 SMs and those of eight fewer (the SMs of a cluster lie together); one more than fit takes a wave of its
+// own (8 x 2048 x 1024 gated in 37 clusters of four 14 us, in 32 of them 8).
+inline int parts_of(int num_sms, int64_t tiles, int n, int least)
 {
-    const bool waves = (int64_t)tiles_of(M, 128) * tiles_of(N, n_small) > num_sms;
-    Cut c;
-    c.swapped = M <= 32 || (M <= 64 && waves);
-    c.cg = !c.swapped && waves ? 2 : 1;
-    c.bn = c.cg == 2 ? 256 : !c.swapped ? 64 : M <= 16 ? 16 : M <= 32 ? 32 : 64;
-    return c;
+    int parts = 1;
+    while (parts < 8 && tiles * 2 * parts <= (parts == 1 ? num_sms : parts == 2 ? num_sms * 7 / 8 : num_sms * 2 / 3) &&
+           n >= 2 * parts * least)
+        parts *= 2;
+    return parts;
 }
+// What bringing parts together takes, in microseconds.
+inline double join_cost(int parts) { return parts > 1 ? 1.2 + 0.3 * parts : 0.0; }
+
+// Tiles: of the forms, the one with the least time in microseconds by what was measured: a tile's stages, its epilogue where that
+// takes longer than another tile's stages, and once what a launch, the pipeline's start and the last epilogue take.
+inline Cut cut_tiles(int num_sms, int64_t M, int64_t N, bool gated, int n, int halves)
+{
+    static const struct { int cg, bn; double stage, epilogue, once; } forms[3] = {
+        {2, 256, 0.29, 3.6, 6.2}, {2, 128, 0.21, 2.6, 4.7}, {1, 64, 0.21, 1.4, 3.8}};
+    Cut best = {};
+    double least = 0;
+    for (const auto &f : forms) {
+        const int64_t tiles = (int64_t)halves * tiles_of(M, 128 * f.cg) * tiles_of(N, f.bn / (gated ? 2 : 1));
+        const int slots = num_sms / f.cg;
+        const int most = f.cg == 1 ? parts_of(num_sms, tiles, n, 4) : 1;
+        for (int parts = 1; parts <= most; parts *= 2) {
+            const double own = f.stage * ((n + parts - 1) / parts), more = own > f.epilogue ? own : f.epilogue;
+            const double t = f.once + own + join_cost(parts) + more * (double)((tiles * parts + slots - 1) / slots - 1);
+            if (!best.cg || t < least) { best = {false, f.cg, f.bn, 128, parts}; least = t; }
+        }
+    }
+    return best;
+}
+
+// Few tokens: the weights' rows are spread over the SMs, step rows at a time.  A stage takes its bytes' time or, where they are few, that
+// of its four MMAs.
+inline Cut cut_few(int num_sms, int64_t M, int64_t N, bool gated, int n, int step)
+{
+    const int na = gated ? 2 : 1;
+    Cut best = {};
+    best.few = true;
+    best.cg = 1;
+    best.bn = M <= 16 ? 16 : M <= 32 ? 32 : 64;
+    double least = 0;
+    for (int rows = step; rows * na <= 128; rows += step) {
+        const int64_t tiles = (int64_t)tiles_of(N, rows) * tiles_of(M, best.bn);
+        const int most = parts_of(num_sms, tiles, n, 2);
+        const double bytes = rows * na * 128 / 44e3, stage = bytes > 0.21 ? bytes : 0.21;
+        for (int parts = 1; parts <= most; parts *= 2) {
+            const double t = stage * ((n + parts - 1) / parts) * (double)((tiles * parts + num_sms - 1) / num_sms) + join_cost(parts);
+            if (!best.rows_a || t <= least) { best.rows_a = rows; best.parts = parts; least = t; }
+        }
+    }
+    return best;
+}
+
+// n: stages of the contraction; step: of rows_a.
+inline Cut cut(int num_sms, int64_t M, int64_t N, bool gated, int n, int step = 8)
+{
+    return M <= 64 ? cut_few(num_sms, M, N, gated, n, step) : cut_tiles(num_sms, M, N, gated, n, 1);
+}
+inline int stages_of(int64_t K, int kind) { return tiles_of(K, kind == kI8 ? 128 : 64); }
 
 // Fills in how the product is gone through.  out_n: columns of the output a tile has; K: of a segment of the contraction.
-inline void divide(Params &prm, int num_sms, const Cut &c, int kind, int out_n, int64_t K, int segments, int halves)
+inline void divide(Params &prm, const Cut &c, int kind, bool gated, int64_t K, int segments, int halves)
 {
     const int ks = kind == kI8 ? 128 : 64;
-    prm.half_tiles = tiles_of(prm.M, 128 * c.cg);
+    prm.rows_a = c.few ? c.rows_a : 128;
+    prm.half_tiles = tiles_of(prm.M, c.few ? c.rows_a : 128 * c.cg);
     prm.tiles_m = prm.half_tiles * halves;
-    if (halves == 1) prm.half_tiles = prm.tiles_m;
-    prm.tiles_n = tiles_of(prm.N, out_n);
+    prm.tiles_n = tiles_of(prm.N, gated && !c.few ? c.bn / 2 : c.bn);
     prm.seg_stages = tiles_of(K, ks);
     prm.n_stages = prm.seg_stages * segments;
     prm.n_last = (int)((K - (int64_t)(prm.seg_stages - 1) * ks + ks / 4 - 1) / (ks / 4));
     prm.group = prm.tiles_m < 8 ? prm.tiles_m : 8;
-    prm.swapped = c.swapped;
-    // Parts of a contraction: as many as there are SMs for, of a few stages each.
-    const int min_stages = c.bn <= 32 ? 2 : 8;
-    prm.parts = 1;
-    while (c.cg == 1 && prm.parts < 8 && (int64_t)prm.tiles_m * prm.tiles_n * 2 * prm.parts <= (prm.parts < 4 ? num_sms : num_sms * 2 / 3) &&
-           prm.n_stages >= 2 * prm.parts * min_stages)
-        prm.parts *= 2;
+    prm.parts = c.parts;
+    if (halves == 1) prm.half_tiles = prm.tiles_m;
+    const int stage = (gated ? 2 : 1) * c.rows_a * 128 + c.bn * 128, room = Shape<1, 16, true>::ROOM / stage;
+    prm.stages = room < Shape<1, 16, true>::MOST ? room : Shape<1, 16, true>::MOST;      // (of few rows)
 }
 
 }  // namespace product

@@ -27,21 +27,28 @@ cudaError_t launch_i8_matmul(const Launch &l, const int8_t *a, const float *sa, 
                              int64_t K, void *out, int dtype, int64_t ld)
 {
     Params prm = start(l, dtype);
-    const Cut c = cut(l.num_sms, M, N, 64);
-    prm.M = c.swapped ? N : M;
-    prm.N = c.swapped ? M : N;
-    divide(prm, l.num_sms, c, kI8, c.bn, K, 1, 1);
-    prm.scale_m[0] = c.swapped ? sb : sa;
-    prm.scale_n[0] = c.swapped ? sa : sb;
-    if (!encode_codes(l.encode, &prm.a[0], c.swapped ? b : a, prm.M, K, 128) ||
-        !encode_codes(l.encode, &prm.b[0], c.swapped ? a : b, prm.N, K, c.bn / c.cg))
+    const Cut c = cut(l.num_sms, M, N, false, stages_of(K, kI8));
+    prm.M = c.few ? N : M;
+    prm.N = c.few ? M : N;
+    divide(prm, c, kI8, false, K, 1, 1);
+    prm.scale_m[0] = c.few ? sb : sa;
+    prm.scale_n[0] = c.few ? sa : sb;
+    if (!encode_codes(l.encode, &prm.a[0], c.few ? b : a, prm.M, K, prm.rows_a) ||
+        !encode_codes(l.encode, &prm.b[0], c.few ? a : b, prm.N, K, c.bn / c.cg))
         return cudaErrorInvalidValue;
-    set_output(l.encode, prm, 0, out, dtype, M, N, ld);
-    if (c.cg == 2) return launch<kI8, 2, 256, 1, false, false, false>(l.stream, l.num_sms, prm);
+    set_output(prm, 0, out, dtype, ld);
+    const cudaStream_t st = l.stream;
+    if (c.few) {
+        switch (c.bn) {
+        case 16: return launch<kI8, 1, 16, true, false, false, false>(st, l.num_sms, prm);
+        case 32: return launch<kI8, 1, 32, true, false, false, false>(st, l.num_sms, prm);
+        default: return launch<kI8, 1, 64, true, false, false, false>(st, l.num_sms, prm);
+        }
+    }
     switch (c.bn) {
-    case 16: return launch<kI8, 1, 16, 1, false, false, false>(l.stream, l.num_sms, prm);
-    case 32: return launch<kI8, 1, 32, 1, false, false, false>(l.stream, l.num_sms, prm);
-    default: return launch<kI8, 1, 64, 1, false, false, false>(l.stream, l.num_sms, prm);
+    case 256: return launch<kI8, 2, 256, false, false, false, false>(st, l.num_sms, prm);
+    case 128: return launch<kI8, 2, 128, false, false, false, false>(st, l.num_sms, prm);
+    default: return launch<kI8, 1, 64, false, false, false, false>(st, l.num_sms, prm);
     }
 }
 
@@ -50,26 +57,32 @@ cudaError_t launch_i8_gated(const Launch &l, const int8_t *a, const float *sa, c
 {
     Params prm = start(l, dtype);
     prm.act = act;
-    const Cut c = cut(l.num_sms, M, F, 32);
-    prm.M = c.swapped ? F : M;
-    prm.N = c.swapped ? M : F;
-    divide(prm, l.num_sms, c, kI8, c.swapped ? c.bn : c.bn / 2, K, 1, 1);
+    const Cut c = cut(l.num_sms, M, F, true, stages_of(K, kI8));
+    prm.M = c.few ? F : M;
+    prm.N = c.few ? M : F;
+    divide(prm, c, kI8, true, K, 1, 1);
     const int8_t *w[2] = {gate, up};
     const float *sw[2] = {s_gate, s_up};
-    CUtensorMap *map_w = c.swapped ? prm.a : prm.b;
+    CUtensorMap *map_w = c.few ? prm.a : prm.b;
     for (int i = 0; i < 2; ++i) {
-        (c.swapped ? prm.scale_m : prm.scale_n)[i] = sw[i];
-        if (!encode_codes(l.encode, map_w + i, w[i], F, K, c.swapped || c.cg == 2 ? 128 : 32)) return cudaErrorInvalidValue;
+        (c.few ? prm.scale_m : prm.scale_n)[i] = sw[i];
+        if (!encode_codes(l.encode, map_w + i, w[i], F, K, c.few ? prm.rows_a : c.bn / 2)) return cudaErrorInvalidValue;
     }
-    (c.swapped ? prm.scale_n : prm.scale_m)[0] = sa;
-    if (!encode_codes(l.encode, c.swapped ? prm.b : prm.a, a, M, K, c.swapped ? c.bn : 128)) return cudaErrorInvalidValue;
-    set_output(l.encode, prm, 0, out, dtype, M, F, ld);
-    if (c.cg == 2) return launch<kI8, 2, 256, 1, false, false, true>(l.stream, l.num_sms, prm);
-    if (!c.swapped) return launch<kI8, 1, 64, 1, false, false, true>(l.stream, l.num_sms, prm);
+    (c.few ? prm.scale_n : prm.scale_m)[0] = sa;
+    if (!encode_codes(l.encode, c.few ? prm.b : prm.a, a, M, K, c.few ? c.bn : 128)) return cudaErrorInvalidValue;
+    set_output(prm, 0, out, dtype, ld);
+    const cudaStream_t st = l.stream;
+    if (c.few) {
+        switch (c.bn) {
+        case 16: return launch<kI8, 1, 16, true, false, false, true>(st, l.num_sms, prm);
+        case 32: return launch<kI8, 1, 32, true, false, false, true>(st, l.num_sms, prm);
+        default: return launch<kI8, 1, 64, true, false, false, true>(st, l.num_sms, prm);
+        }
+    }
     switch (c.bn) {
-    case 16: return launch<kI8, 1, 16, 2, false, false, true>(l.stream, l.num_sms, prm);
-    case 32: return launch<kI8, 1, 32, 2, false, false, true>(l.stream, l.num_sms, prm);
-    default: return launch<kI8, 1, 64, 2, false, false, true>(l.stream, l.num_sms, prm);
+    case 256: return launch<kI8, 2, 256, false, false, false, true>(st, l.num_sms, prm);
+    case 128: return launch<kI8, 2, 128, false, false, false, true>(st, l.num_sms, prm);
+    default: return launch<kI8, 1, 64, false, false, false, true>(st, l.num_sms, prm);
     }
 }
 

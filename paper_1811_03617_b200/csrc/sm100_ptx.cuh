@@ -98,6 +98,11 @@ __device__ __forceinline__ void tma_load_2d(void *dst, const CUtensorMap *tmap, 
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(smem_u32(dst)), "l"(tmap), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
 }
+// The same box to L2 alone.
+__device__ __forceinline__ void prefetch_2d(const CUtensorMap *tmap, int x, int y)
+{
+    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(tmap), "r"(x), "r"(y) : "memory");
+}
 // This CTA's shared address `addr` as it is in CTA `cta` of the cluster, and four floats from such an address.
 __device__ __forceinline__ uint32_t cluster_address(uint32_t addr, uint32_t cta)
 {
@@ -167,6 +172,14 @@ __device__ __forceinline__ uint32_t cluster_rank()
 __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The same from warps whose lanes may have come apart: the aligned form counts a warp that reaches it in pieces more than once, and a
+// CTA then ends while its neighbours still read its shared memory.
+__device__ __forceinline__ void cluster_sync_any()
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+    __syncwarp();
 }
 // Address of the same shared variable in the CTA of rank 0.
 __device__ __forceinline__ uint32_t in_leader(const void *p)
@@ -330,20 +343,20 @@ __device__ __forceinline__ void tmem_ld32_wait(uint32_t taddr, float (&v)[32])
 }
 
 // Host: launches a kernel that begins with launch_dependents() and grid_dependency_wait(), so that its start overlaps the
-// end of the stream's last kernel; cluster: CTAs of a cluster (1: none).  A kernel's shared-memory limit is raised at its
-// first launch on a device.
+// end of the stream's last kernel; cluster: CTAs of a cluster (1: none).  A kernel's shared-memory limit on a device is raised at the
+// first launch that needs more than any before it.
 template <auto Kernel, typename P>
 cudaError_t launch_chained(const P &prm, int grid, int threads, size_t smem, int cluster, cudaStream_t st)
 {
     if (smem > 48 * 1024) {
-        static std::atomic<uint64_t> raised{0};
+        static std::atomic<int> raised[64];
         int dev = 0;
         cudaError_t e = cudaGetDevice(&dev);
         if (e != cudaSuccess) return e;
-        if (dev >= 64 || !(raised.load(std::memory_order_relaxed) >> dev & 1)) {
+        if (dev >= 64 || raised[dev].load(std::memory_order_relaxed) < (int)smem) {
             e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
             if (e != cudaSuccess) return e;
-            if (dev < 64) raised.fetch_or(1ull << dev, std::memory_order_relaxed);
+            if (dev < 64) raised[dev].store((int)smem, std::memory_order_relaxed);
         }
     }
     cudaLaunchConfig_t cfg = {};

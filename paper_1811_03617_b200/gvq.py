@@ -621,8 +621,9 @@ class Context:
             n_scratch = lib().gvq_i8_scratch_bytes(rows, cols)
             if n_scratch < 0:
                 raise ValueError(f"no 8-bit matrix of {rows} x {cols}")
-            kept = torch.empty(n_scratch, dtype=torch.uint8, device=x.device)
-            scratch = kept.data_ptr()
+            if n_scratch:
+                kept = torch.empty(n_scratch, dtype=torch.uint8, device=x.device)
+                scratch = kept.data_ptr()
         self._sync_stream()
         status = lib().gvq_i8_quantize(self._h, x.data_ptr(), dtype, rows, cols, ld, 1 if stochastic else 0, seed, node, c, s, ct, st,
                                        scratch, n_scratch)
