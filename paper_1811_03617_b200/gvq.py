@@ -368,34 +368,37 @@ class I8:
     def __init__(self, rows: int, cols: int, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
                  device=None):
         rows, cols = int(rows), int(cols)
-        if rows < 1 or cols < 1 or max(rows, cols) > 0x7FFFFFFF - 1024 or ((rows + 127) // 128) * ((cols + 127) // 128) >= 0x7FFFFFFF:
+        if rows < 1 or cols < 1 or rows > _MOST or cols > _MOST or ((rows + 127) >> 7) * ((cols + 127) >> 7) >= 0x7FFFFFFF:
             raise ValueError(f"no 8-bit matrix of {rows} x {cols}")
-        self.rows, self.cols = rows, cols
-        pitch = (cols + 15) & ~15
-        if codes is None and scales is None:       # one allocation for both
-            at = (rows * pitch + 255) & ~255
-            self._buf = buf = torch.empty(at + 4 * rows, dtype=torch.int8, device=device or "cuda")
-            self._codes = None
-            self.device = buf.get_device()
-            self.codes_ptr = p = buf.data_ptr()
-            self.scales_ptr = p + at
+        if codes is None and scales is None:
+            self._room(rows, cols, torch.empty(_i8_bytes(rows, cols), dtype=torch.int8, device=device or "cuda"))
             return
         if codes is None or scales is None:
             raise ValueError("codes and scales come together")
-        for t, n, dtype in ((codes, rows * pitch, torch.int8), (scales, rows, _F32)):
-            if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.numel() != n:
-                raise ValueError(f"an 8-bit matrix of {rows} x {cols} has int8 codes [{rows}, {pitch}] and float32 scales [{rows}], contiguous")
+        self.rows, self.cols = rows, cols
+        n = rows * ((cols + 15) & ~15)
+        if not (codes.dtype is torch.int8 and scales.dtype is _F32 and codes.is_cuda and scales.is_cuda and codes.numel() == n and
+                scales.numel() == rows and codes.is_contiguous() and scales.is_contiguous()):
+            raise ValueError(f"an 8-bit matrix of {rows} x {cols} has int8 codes [{rows}, {n // rows}] and float32 scales [{rows}], contiguous")
         self.device = codes.get_device()
         if scales.get_device() != self.device:
             raise ValueError("codes and scales are on one device")
         self._codes, self._scales = codes, scales
         self.codes_ptr, self.scales_ptr = codes.data_ptr(), scales.data_ptr()
 
+    def _room(self, rows, cols, buf):
+        """Codes and scales in one allocation of at least _i8_bytes()."""
+        self.rows, self.cols, self._buf, self._codes = rows, cols, buf, None
+        self.device = buf.get_device()
+        self.codes_ptr = p = buf.data_ptr()
+        self.scales_ptr = p + ((rows * ((cols + 15) & ~15) + 255) & ~255)
+
     def _views(self):
         if self._codes is None:
+            buf = self._buf.view(torch.int8)
             pitch, at = (self.cols + 15) & ~15, self.scales_ptr - self.codes_ptr
-            self._codes = self._buf[:self.rows * pitch].view(self.rows, pitch)
-            self._scales = self._buf[at:at + 4 * self.rows].view(_F32)
+            self._codes = buf[:self.rows * pitch].view(self.rows, pitch)
+            self._scales = buf[at:at + 4 * self.rows].view(_F32)
         return self._codes, self._scales
 
     @property
@@ -407,6 +410,21 @@ class I8:
         return self._views()[1]
 
 
+_MOST = 0x7FFFFFFF - 1024      # rows, columns
+
+
+def _i8_bytes(rows: int, cols: int) -> int:
+    return ((rows * ((cols + 15) & ~15) + 255) & ~255) + 4 * rows
+
+
+def _i8_like(x: torch.Tensor, rows: int, cols: int) -> I8:
+    """Room for a matrix on x's device (sizes that the library refuses are refused by it); of x's type, whose new_empty is the quickest."""
+    q = I8.__new__(I8)
+    n, size = _i8_bytes(rows, cols), x.element_size()
+    q._room(rows, cols, x.new_empty((n + size - 1) // size))
+    return q
+
+
 ACTIVATION = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
 
 
@@ -415,6 +433,14 @@ def _activation(name: str) -> int:
     if a is None:
         raise ValueError(f"activation {name!r}: one of {', '.join(ACTIVATION)} is wanted")
     return a
+
+
+def _half_type(t: torch.Tensor, what: str) -> int:
+    if t.dtype is torch.bfloat16:
+        return 1
+    if t.dtype is torch.float16:
+        return 2
+    raise TypeError(f"{what}: bfloat16 and float16 are taken, not {t.dtype}")
 
 
 class Context:
@@ -602,31 +628,33 @@ class Context:
 
     # ---- 8-bit integers ---------------------------------------------------------------------
     def _i8(self, x, by_rows, by_cols, stochastic, seed, node, out=None, out_t=None):
-        rows, cols, ld = _rows(x, self.device, "i8_quantize")
-        dtype = _dtype(x)
+        device = self.device
+        rows, cols, ld = _rows(x, device, "i8_quantize")
+        dtype = DTYPE.get(x.dtype)
+        if dtype is None:
+            _dtype(x)
         c = s = ct = st = scratch = None
         n_scratch = 0
         if by_rows:
             if out is None:
-                out = I8(rows, cols, device=x.device)
-            elif out.rows != rows or out.cols != cols or out.device != self.device:
+                out = _i8_like(x, rows, cols)
+            elif out.rows != rows or out.cols != cols or out.device != device:
                 raise ValueError("i8_quantize: the output is of another size or on another device")
             c, s = out.codes_ptr, out.scales_ptr
+        L = lib()
         if by_cols:
             if out_t is None:
-                out_t = I8(cols, rows, device=x.device)
-            elif out_t.rows != cols or out_t.cols != rows or out_t.device != self.device:
+                out_t = _i8_like(x, cols, rows)
+            elif out_t.rows != cols or out_t.cols != rows or out_t.device != device:
                 raise ValueError("i8_quantize: the output is of another size or on another device")
             ct, st = out_t.codes_ptr, out_t.scales_ptr
-            n_scratch = lib().gvq_i8_scratch_bytes(rows, cols)
-            if n_scratch < 0:
-                raise ValueError(f"no 8-bit matrix of {rows} x {cols}")
-            if n_scratch:
+            n_scratch = L.gvq_i8_scratch_bytes(rows, cols)
+            if n_scratch > 0:
                 kept = torch.empty(n_scratch, dtype=torch.uint8, device=x.device)
                 scratch = kept.data_ptr()
         self._sync_stream()
-        status = lib().gvq_i8_quantize(self._h, x.data_ptr(), dtype, rows, cols, ld, 1 if stochastic else 0, seed, node, c, s, ct, st,
-                                       scratch, n_scratch)
+        status = L.gvq_i8_quantize(self._h, x.data_ptr(), dtype, rows, cols, ld, 1 if stochastic else 0, seed, node, c, s, ct, st,
+                                   scratch, n_scratch)
         if status:
             raise GvqError(status, "gvq_i8_quantize")
         return out, out_t
@@ -656,63 +684,63 @@ class Context:
 
     def i8_matmul(self, a: I8, b: I8, out: torch.Tensor) -> torch.Tensor:
         """gvq_i8_matmul: out [a.rows, b.rows] = a b^T; out is float32, bfloat16 or float16."""
-        rows, cols, ld = _rows(out, self.device, "i8_matmul")
-        if a.cols != b.cols or (rows, cols) != (a.rows, b.rows):
+        device, k = self.device, a.cols
+        rows, cols, ld = _rows(out, device, "i8_matmul")
+        if k != b.cols or rows != a.rows or cols != b.rows:
             raise ValueError(f"i8_matmul: [{a.rows}, {a.cols}] x [{b.rows}, {b.cols}]^T does not give [{rows}, {cols}]")
-        if a.device != self.device or b.device != self.device:
+        if a.device != device or b.device != device:
             raise ValueError(f"i8_matmul: operands on cuda:{a.device} and cuda:{b.device}, the context on cuda:{self.device}")
         self._sync_stream()
-        status = lib().gvq_i8_matmul(self._h, a.codes_ptr, a.scales_ptr, b.codes_ptr, b.scales_ptr, rows, cols, a.cols, out.data_ptr(),
+        status = lib().gvq_i8_matmul(self._h, a.codes_ptr, a.scales_ptr, b.codes_ptr, b.scales_ptr, rows, cols, k, out.data_ptr(),
                                      _dtype(out), ld)
         if status:
             raise GvqError(status, "gvq_i8_matmul")
         return out
 
     # ---- the gated block --------------------------------------------------------------------
-    def _halves(self, what: str, like: torch.Tensor, *wanted):
-        """Leading dimensions of 16-bit matrices of the sizes given: (tensor, rows, cols) each; None goes through."""
-        if like.dtype is not torch.bfloat16 and like.dtype is not torch.float16:
-            raise TypeError(f"{what}: bfloat16 and float16 are taken, not {like.dtype}")
-        lds = []
-        for t, rows, cols in wanted:
-            if t is None:
-                lds.append(0)
-                continue
-            r, c, ld = _rows(t, self.device, what)
-            if t.dtype is not like.dtype:
-                raise TypeError(f"{what}: the matrices are of one type, not {like.dtype} and {t.dtype}")
-            if (r, c) != (rows, cols):
-                raise ValueError(f"{what}: a matrix of {rows} x {cols} is wanted, not {r} x {c}")
-            lds.append(ld)
-        return lds
+    def _half(self, what: str, t: torch.Tensor, like, rows: int, cols: int) -> int:
+        """Leading dimension of a 16-bit matrix of the size and type given."""
+        r, c, ld = _rows(t, self.device, what)
+        if t.dtype is not like:
+            raise TypeError(f"{what}: the matrices are of one type, not {like} and {t.dtype}")
+        if r != rows or c != cols:
+            raise ValueError(f"{what}: a matrix of {rows} x {cols} is wanted, not {r} x {c}")
+        return ld
 
-    def _gated_workspace(self, what: str, M: int, F: int, K: int, backward: bool, read):
-        """(tensor or None, address, bytes) for a call that reads the matrices `read`, (tensor, leading dimension) each."""
-        aligned = all(t is None or (t.data_ptr() % 16 == 0 and (t.shape[0] == 1 or ld % 8 == 0)) for t, ld in read)
+    def _gated_workspace(self, what: str, M: int, F: int, K: int, backward: bool, aligned: bool):
+        """(tensor or None, address, bytes); aligned: the rows of x and the weights, as far as they are read, start at 16-byte boundaries."""
+        if aligned and not backward:
+            return None, None, 0
         n = lib().gvq_gated_workspace_bytes(M, F, K, 1 if backward else 0, 1 if aligned else 0)
         if n < 0:
             raise GvqError(2, what)
-        if n == 0:
-            return None, None, 0
-        ws = torch.empty(n, dtype=torch.uint8, device=f"cuda:{self.device}")
+        ws = torch.empty(n, dtype=torch.uint8, device=self._torch_device())
         return ws, ws.data_ptr(), n
+
+    def _torch_device(self):
+        return torch.device("cuda", self.device)
 
     def gated_forward(self, x, w_gate, w_up, out, act: str = "silu", gate: Optional[torch.Tensor] = None,
                       up: Optional[torch.Tensor] = None) -> torch.Tensor:
         """gvq_gated_forward: out [M, F] = act(x w_gate^T) * (x w_up^T); bfloat16 or float16 throughout.  gate, up: [M, F] that receive
         both projections for gated_backward."""
         what = "gated_forward"
-        a = _activation(act)
-        M, K, _ = _rows(x, self.device, what)
+        a, half = _activation(act), self._half
+        M, K, ldx = _rows(x, self.device, what)
+        like, dtype = x.dtype, _half_type(x, what)
         F = w_gate.shape[0]
-        if (gate is None) != (up is None):
+        lg = half(what, w_gate, like, F, K)
+        lu, lh = half(what, w_up, like, F, K), half(what, out, like, M, F)
+        kept = (None, 0, None, 0)
+        if gate is not None and up is not None:
+            kept = (gate.data_ptr(), half(what, gate, like, M, F), up.data_ptr(), half(what, up, like, M, F))
+        elif gate is not None or up is not None:
             raise ValueError(f"{what}: both projections are kept, or neither")
-        ldx, lg, lu, lh, lgo, luo = self._halves(what, x, (x, M, K), (w_gate, F, K), (w_up, F, K), (out, M, F), (gate, M, F), (up, M, F))
-        ws, at, n = self._gated_workspace(what, M, F, K, False, ((x, ldx), (w_gate, lg), (w_up, lu)))
+        px, pg, pu = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr()
+        aligned = not ((px | pg | pu) & 15 or (M > 1 and ldx & 7) or (F > 1 and (lg | lu) & 7))
+        ws, at, n = self._gated_workspace(what, M, F, K, False, aligned)
         self._sync_stream()
-        status = lib().gvq_gated_forward(self._h, x.data_ptr(), ldx, w_gate.data_ptr(), lg, w_up.data_ptr(), lu, DTYPE[x.dtype], M, F, K, a,
-                                         out.data_ptr(), lh, gate.data_ptr() if gate is not None else None, lgo,
-                                         up.data_ptr() if up is not None else None, luo, at, n)
+        status = lib().gvq_gated_forward(self._h, px, ldx, pg, lg, pu, lu, dtype, M, F, K, a, out.data_ptr(), lh, *kept, at, n)
         if status:
             raise GvqError(status, "gvq_gated_forward")
         return out
@@ -722,40 +750,34 @@ class Context:
         """gvq_gated_backward: the gradients that are given room for.  dx [M, K] is of the operands' type; dw_gate, dw_up [F, K] are
         float32, bfloat16 or float16, of one type.  x may be None where neither is wanted, the weights where dx is not."""
         what = "gated_backward"
-        a = _activation(act)
-        M, F, _ = _rows(dh, self.device, what)
-        dws = [t for t in (dw_gate, dw_up) if t is not None]
-        if dx is None and not dws:
+        a, half = _activation(act), self._half
+        M, F, ldh = _rows(dh, self.device, what)
+        like, dtype = dh.dtype, _half_type(dh, what)
+        lgi, lui = half(what, gate, like, M, F), half(what, up, like, M, F)
+        dw = dw_gate if dw_gate is not None else dw_up
+        if dx is None and dw is None:
             raise ValueError(f"{what}: no gradient is wanted")
-        if (dws and x is None) or (dx is not None and (w_gate is None or w_up is None)):
+        if (dw is not None and x is None) or (dx is not None and (w_gate is None or w_up is None)):
             raise ValueError(f"{what}: x is needed for the weights' gradients, the weights for dx")
-        if not dws:
-            x = None
-        if dx is None:
-            w_gate = w_up = None
-        K = (dws[0] if dws else dx).shape[-1]
-        ldh, lgi, lui, ldx, lg, lu, ldd = self._halves(what, dh, (dh, M, F), (gate, M, F), (up, M, F), (x, M, K), (w_gate, F, K), (w_up, F, K),
-                                                       (dx, M, K))
-        lds = []
-        for t in (dw_gate, dw_up):
-            if t is None:
-                lds.append(0)
-                continue
-            r, c, ld = _rows(t, self.device, what)
-            if (r, c) != (F, K):
-                raise ValueError(f"{what}: a gradient of {F} x {K} is wanted, not {r} x {c}")
-            if t.dtype is not dws[0].dtype:
-                raise TypeError(f"{what}: both weights' gradients are of one type")
-            lds.append(ld)
-        dw_dtype = _dtype(dws[0]) if dws else 0
-        ws, at, n = self._gated_workspace(what, M, F, K, True, ((x, ldx), (w_gate, lg), (w_up, lu)))
+        K = (dx if dx is not None else dw).shape[-1]
+        px = pg = pu = pdx = pdg = pdu = None
+        ldx = lg = lu = ldd = ldg = ldu = dw_dtype = odd = 0
+        if dx is not None:
+            lg, lu, ldd = half(what, w_gate, like, F, K), half(what, w_up, like, F, K), half(what, dx, like, M, K)
+            pg, pu, pdx = w_gate.data_ptr(), w_up.data_ptr(), dx.data_ptr()
+            odd = (pg | pu) & 15 | (F > 1 and (lg | lu) & 7)
+        if dw is not None:
+            ldx, dw_dtype = half(what, x, like, M, K), _dtype(dw)
+            px = x.data_ptr()
+            odd |= px & 15 | (M > 1 and ldx & 7)
+            if dw_gate is not None:
+                ldg, pdg = half(what, dw_gate, dw.dtype, F, K), dw_gate.data_ptr()
+            if dw_up is not None:
+                ldu, pdu = half(what, dw_up, dw.dtype, F, K), dw_up.data_ptr()
+        ws, at, n = self._gated_workspace(what, M, F, K, True, not odd)
         self._sync_stream()
-
-        def ptr(t):
-            return t.data_ptr() if t is not None else None
-        status = lib().gvq_gated_backward(self._h, dh.data_ptr(), ldh, gate.data_ptr(), lgi, up.data_ptr(), lui, ptr(x), ldx, ptr(w_gate), lg,
-                                          ptr(w_up), lu, DTYPE[dh.dtype], M, F, K, a, ptr(dx), ldd, ptr(dw_gate), lds[0], ptr(dw_up), lds[1],
-                                          dw_dtype, at, n)
+        status = lib().gvq_gated_backward(self._h, dh.data_ptr(), ldh, gate.data_ptr(), lgi, up.data_ptr(), lui, px, ldx, pg, lg, pu, lu,
+                                          dtype, M, F, K, a, pdx, ldd, pdg, ldg, pdu, ldu, dw_dtype, at, n)
         if status:
             raise GvqError(status, "gvq_gated_backward")
 
