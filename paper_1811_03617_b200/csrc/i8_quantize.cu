@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(kStripThreads) i8_strip_kernel(const QuantPara
         for (int w = 0; w < WARPS; ++w) t = max(t, tops[w][tid]);
         of_cta[tid] = t;
     }
-    if (cluster > 1) ptx::cluster_sync_any(); else __syncthreads();
+    if (cluster > 1) ptx::cluster_sync(); else __syncthreads();
     if (tid < SC) {
         uint32_t t = of_cta[tid];
         if (cluster > 1) {
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(kStripThreads) i8_strip_kernel(const QuantPara
                 column_run<T, SR>(prm, w, part, of_col[cw * PER + part], c0 + cw * PER + part, r, pitch_t);
         }
     }
-    if (cluster > 1) ptx::cluster_sync_any();      // (its neighbours have read this CTA's maxima)
+    if (cluster > 1) ptx::cluster_sync();      // (its neighbours have read this CTA's maxima)
 }
 
 // A CTA: kMaxRows rows of a strip of 128 bytes.

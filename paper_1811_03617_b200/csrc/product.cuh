@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
     }
     if (warp == 1) tmem_alloc<CG>(tmem_slot, S::TMEM);
     tc_fence_before();
-    if (CG == 2) cluster_sync_any(); else __syncthreads();
+    if (CG == 2) cluster_sync(); else __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     launch_dependents();
@@ -531,7 +531,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
 
     if constexpr (CG == 1) {
         if (parts > 1) {
-            cluster_sync_any();
+            cluster_sync();
             if (!failed) {
                 int tm, tn;
                 place(prm, first, tm, tn);
@@ -548,7 +548,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
     tc_fence_before();
     __syncwarp();
     // (the other CTAs of a cluster use this one's barriers and memory until here)
-    if (CG == 2 || parts > 1) cluster_sync_any(); else __syncthreads();
+    if (CG == 2 || parts > 1) cluster_sync(); else __syncthreads();
     tc_fence_after();
     __syncwarp();
     if (warp == 1) tmem_dealloc<CG>(tmem, S::TMEM);

@@ -168,14 +168,10 @@ __device__ __forceinline__ uint32_t cluster_rank()
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
-// All threads of both CTAs (a hardware barrier, like __syncthreads).
+// All threads of a cluster (a hardware barrier, like __syncthreads).  Not the aligned form: that one counts a warp whose lanes reach it
+// in pieces, as they may after a loop of different lengths, more than once, and a CTA then ends while its neighbours still read its
+// shared memory (an illegal address where 144 items were joined by 320 threads).
 __device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// The same from warps whose lanes may have come apart: the aligned form counts a warp that reaches it in pieces more than once, and a
-// CTA then ends while its neighbours still read its shared memory.
-__device__ __forceinline__ void cluster_sync_any()
 {
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
