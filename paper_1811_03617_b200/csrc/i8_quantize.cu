@@ -343,6 +343,11 @@ __global__ void __launch_bounds__(256) i8_max_kernel(const QuantParams prm)
     }
 }
 
+// 16 bytes to shared memory without a register, zeros after the first `bytes` of them.
+__device__ __forceinline__ void copy16(void *to, const void *from, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(to)), "l"(from), "r"(bytes) : "memory");
+}
 // A CTA: a tile of 128 x 128 entries, from the end: what i8_max_kernel has read last is in L2.  Shared memory and what follows as above.
 template <typename T, bool SR, bool VEC>
 __global__ void __launch_bounds__(256) i8_tile_kernel(const QuantParams prm)
@@ -357,6 +362,29 @@ __global__ void __launch_bounds__(256) i8_tile_kernel(const QuantParams prm)
     const int tile_at = gridDim.x - 1 - blockIdx.x, rtile = tile_at / prm.ct, ctile = tile_at - rtile * prm.ct;
     const int64_t r0 = (int64_t)rtile * 128, c0 = (int64_t)ctile * 128;
     const T *x = static_cast<const T *>(prm.x);
+    auto at = [&](int row) { return tile + row * PITCH + (row >> 4) * 4; };
+
+    // warp w, iteration it: rows 16 w + 2 it + (lane >> 4); copies that need no registers, all of them on their way at once
+    const int cl = (lane & 15) * 8;
+    const int ncol = (int)max((int64_t)0, min((int64_t)8, prm.cols - (c0 + cl)));    // this lane's valid entries
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int row = 16 * warp + 2 * i + (lane >> 4);
+        uint32_t *to = at(row) + (lane & 15) * (int)sizeof(T) * 2;
+        const int64_t r = r0 + row;
+        if constexpr (VEC) {
+#pragma unroll
+            for (int q = 0; q < (int)sizeof(T) / 2; ++q) {
+                const int bytes = r < prm.rows ? max(0, min(16, ncol * (int)sizeof(T) - 16 * q)) : 0;
+                // (where nothing is read the address is x's own)
+                copy16(to + q * 4, bytes ? reinterpret_cast<const char *>(x + r * prm.ld + c0 + cl) + 16 * q : prm.x, bytes);
+            }
+        } else {
+            const Raw8<T> raw = load8<false>(x + r * prm.ld + c0 + cl, r < prm.rows ? ncol : 0);
+#pragma unroll
+            for (int q = 0; q < (int)sizeof(T) / 2; ++q) *reinterpret_cast<uint4 *>(to + q * 4) = raw.q[q];
+        }
+    }
     uint32_t top = 0;
     if (tid < 128 && c0 + tid < prm.cols) {
         const uint32_t *from = prm.col_top + c0 + tid;
@@ -370,31 +398,12 @@ __global__ void __launch_bounds__(256) i8_tile_kernel(const QuantParams prm)
         }
         for (; b < prm.row_blocks; ++b) top = max(top, __ldcg(from + (int64_t)b * prm.cols));
     }
-    auto at = [&](int row) { return tile + row * PITCH + (row >> 4) * 4; };
-
-    // warp w, iteration it: rows 16 w + 2 it + (lane >> 4)
-    const int cl = (lane & 15) * 8;
-    const int ncol = (int)min((int64_t)8, prm.cols - (c0 + cl));    // this lane's valid entries (<= 0: none)
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        Raw8<T> raw[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t r = r0 + 16 * warp + 2 * (4 * half + i) + (lane >> 4);
-            raw[i] = load8<VEC>(x + r * prm.ld + c0 + cl, r < prm.rows ? ncol : 0);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t *to = at(16 * warp + 2 * (4 * half + i) + (lane >> 4)) + (lane & 15) * (int)sizeof(T) * 2;
-#pragma unroll
-            for (int q = 0; q < (int)sizeof(T) / 2; ++q) *reinterpret_cast<uint4 *>(to + q * 4) = raw[i].q[q];
-        }
-    }
     if (tid < 128) {
         const RowScale s = row_scale(top);
         of_col[tid] = s;
         if (rtile == 0 && c0 + tid < prm.cols) prm.scales_t[c0 + tid] = s.scale;
     }
+    if (VEC) asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
     constexpr int PER = 4 / (int)sizeof(T);                 // columns of a word: 1 or 2
     const int64_t pitch_t = pitch_of(prm.rows);

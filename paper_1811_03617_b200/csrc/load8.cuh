@@ -15,6 +15,12 @@ __device__ __forceinline__ Raw8<T> load8(const T *p, int n)
     constexpr int G = (int)sizeof(T) / 2, W = 4 * G;      // 16-byte words, words of the result
     Raw8<T> r;
     if (VEC && n >= 8) {
+        if (sizeof(T) == 4 && (reinterpret_cast<uintptr_t>(p) & 31) == 0) {      // a whole sector (two halves ask for it twice)
+            asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(r.q[0].x), "=r"(r.q[0].y), "=r"(r.q[0].z), "=r"(r.q[0].w), "=r"(r.q[G - 1].x), "=r"(r.q[G - 1].y),
+                           "=r"(r.q[G - 1].z), "=r"(r.q[G - 1].w) : "l"(p));
+            return r;
+        }
 #pragma unroll
         for (int i = 0; i < G; ++i) r.q[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
         return r;
