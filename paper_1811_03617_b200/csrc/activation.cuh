@@ -4,16 +4,23 @@
 
 namespace gvq {
 
-// 1 / (1 + e^-x), by the hardware's exponential and reciprocal (two units of the last place each): 0 where e^-x overflows.  The
-// argument's rounding moves e^-x by 2^-23 |x| of itself, and the result by at most a quarter of that.  With expf and a
-// division the epilogue of 128 x 128 outputs took ... us, with these ....
+// e^x and 1 / x by the hardware's units (two units of the last place each), subnormal results 0: without that, e^x takes three
+// more instructions, and instructions are what bounds the epilogue of a short contraction.  The argument's rounding moves e^x by
+// 2^-23 |x| of itself.
+__device__ __forceinline__ float exp_approx(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * 1.4426950408889634f));
+    return r;
+}
 __device__ __forceinline__ float reciprocal(float x)
 {
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ float logistic(float x) { return reciprocal(1.0f + __expf(-x)); }
+// 1 / (1 + e^-x): 0 where e^-x overflows, off by at most a quarter of what e^-x is of itself.
+__device__ __forceinline__ float logistic(float x) { return reciprocal(1.0f + exp_approx(-x)); }
 constexpr float kTanhScale = 1.5957691216057308f, kTanhCubic = 0.044715f;      // 2 sqrt(2 / pi)
 
 template <int ACT>

@@ -431,7 +431,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
                 for (int i = 0; i < (SIDE ? 2 : 1); ++i)
 #pragma unroll
                     for (int j = 0; j < NS; ++j) {
-                        const int64_t n = n0 + 32 * (kHalves * j + side) + lane;
+                        const int64_t n = n0 + 32 * (NS * side + j) + lane;
                         scales[(i * NS + j) * 32 + lane] = n < prm.N ? __ldg(prm.scale_n[i] + n) : 0.0f;
                     }
                 __syncwarp();
@@ -468,7 +468,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
             }
             // the sums of one matrix's piece p = 2 j + side
             auto sums = [&](int which, int j, float (&v)[32]) {
-                const uint32_t from = acc + (SIDE ? which * HN : 0) + 32 * (kHalves * j + side);
+                const uint32_t from = acc + (SIDE ? which * HN : 0) + 32 * (NS * side + j);
                 if constexpr (PW == 32) tmem_ld32_wait(from, v);
                 else {
                     float w[16];
@@ -488,40 +488,39 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
                     }
                 }
             };
-            const int n_out = SIDE && prm.out[1] ? 3 : 1;
-#pragma unroll 1
-            for (int oi = 0; oi < n_out; ++oi) {
-                const int o = n_out - 1 - oi;                          // 0: the product, or the block's; 1, 2: its projections, first
-                const int slot = SIDE ? o : half;
+            // a piece to output `slot`
+            auto store = [&](int slot, int64_t n, int cols, const float (&v)[32]) {
                 void *out = prm.out[slot];
                 const int64_t ld = prm.ld[slot];
                 const int align = prm.align[slot];
-#pragma unroll 1
-                for (int j = 0; kHalves * j + side < NP; ++j) {
-                    const int64_t n = n0 + 32 * (kHalves * j + side);
-                    const int cols = (int)min((int64_t)PW, prm.N - n);
-                    if (rows <= 0 || cols <= 0) break;
-                    float v[32];
-                    if constexpr (SIDE) {
-                        if (o > 0) sums(o - 1, j, v);
-                        else {
-                            float u[32];
-                            sums(0, j, v);
-                            sums(1, j, u);
-                            activate(prm.act, v, u);
-                        }
-                    } else sums(0, j, v);
-                    if constexpr (FEW) {       // rows of A run along the output's rows: a warp's lanes do too
-                        if (lane < rows) {
+                if constexpr (FEW) {       // rows of A run along the output's rows: a warp's lanes do too
+                    if (lane < rows) {
 #pragma unroll
-                            for (int i = 0; i < PW; ++i)
-                                if (i < cols) store_one(out, dtype, m0 + lane + (n + i) * ld, v[i]);
-                        }
-                    } else if (align >= 16 && cols == 32) {
-                        if (lane < rows) store_row(out, dtype, align, (m0 + lane) * ld + n, v);
-                    } else
-                        store_rows(mine, lane, dtype, out, m0 * ld + n, ld, rows, cols, v);
-                }
+                        for (int i = 0; i < PW; ++i)
+                            if (i < cols) store_one(out, dtype, m0 + lane + (n + i) * ld, v[i]);
+                    }
+                } else if (align >= 16 && cols == 32) {
+                    if (lane < rows) store_row(out, dtype, align, (m0 + lane) * ld + n, v);
+                } else
+                    store_rows(mine, lane, dtype, out, m0 * ld + n, ld, rows, cols, v);
+            };
+#pragma unroll 1
+            for (int j = 0; j < NS && NS * side + j < NP; ++j) {
+                const int64_t n = n0 + 32 * (NS * side + j);
+                const int cols = (int)min((int64_t)PW, prm.N - n);
+                if (rows <= 0 || cols <= 0) break;
+                float v[32];
+                sums(0, j, v);
+                if constexpr (SIDE) {
+                    float u[32];
+                    sums(1, j, u);
+                    if (prm.out[1]) {
+                        store(1, n, cols, v);
+                        store(2, n, cols, u);
+                    }
+                    activate(prm.act, v, u);
+                    store(0, n, cols, v);
+                } else store(half, n, cols, v);
             }
             tc_fence_before();
             __syncwarp();
