@@ -1,4 +1,5 @@
-"""Thin ctypes binding of libgvq.so: argument marshalling only.
+"""Thin ctypes binding of libgvq.so: argument marshalling only.  Calls that a step makes once per product (8-bit matrices, the gated block)
+have a shorter way through _binding.so, which takes what is plainly right; everything else goes through here, and errors are raised here.
 
 Every function here has the name and the meaning of the C entry point it calls
 (see include/gvq.h); tensors are torch CUDA tensors used purely as device
@@ -8,6 +9,7 @@ fallback: if the shared library is missing or a call fails, an exception is rais
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import math
 from pathlib import Path
 from typing import Optional, Sequence
@@ -16,7 +18,9 @@ import torch
 
 _PKG = Path(__file__).resolve().parent
 LIB_PATH = _PKG / "libgvq.so"
+BINDING_PATH = _PKG / "_binding.so"
 _lib = None
+_short = None      # the module _binding.so, once the library is loaded
 
 MAX_NODES = 64
 
@@ -38,12 +42,13 @@ class _Layout(ctypes.Structure):
 
 
 def lib() -> ctypes.CDLL:
-    """Loads libgvq.so (once).  Raises if it has not been built."""
-    global _lib
+    """Loads libgvq.so and _binding.so (once).  Raises if they have not been built."""
+    global _lib, _short
     if _lib is None:
-        if not LIB_PATH.exists():
-            raise RuntimeError(f"{LIB_PATH} is missing: run `python -m paper_1811_03617_b200.build` "
-                               "(there is no fallback implementation)")
+        for path in (LIB_PATH, BINDING_PATH):
+            if not path.exists():
+                raise RuntimeError(f"{path} is missing: run `python -m paper_1811_03617_b200.build` "
+                                   "(there is no fallback implementation)")
         L = ctypes.CDLL(str(LIB_PATH))
         vp, i32, i64, u64, u32 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_uint64, ctypes.c_uint32
         LP = ctypes.POINTER(_Layout)
@@ -144,7 +149,13 @@ def lib() -> ctypes.CDLL:
         L.gvq_schedule_nodes_over.argtypes = [vp]
         L.gvq_schedule_step.argtypes = [vp, vp, i32, ctypes.POINTER(i32)]
         L.gvq_schedule_counters.argtypes = [vp, ctypes.POINTER(i64), ctypes.POINTER(i64), ctypes.POINTER(i64)]
-        _lib = L
+        spec = importlib.util.spec_from_file_location(f"{__package__}._binding", BINDING_PATH)
+        short = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(short)
+        entries = ("gvq_set_stream", "gvq_i8_scratch_bytes", "gvq_i8_quantize", "gvq_i8_matmul", "gvq_i8_gated", "gvq_gated_workspace_bytes",
+                   "gvq_gated_forward", "gvq_gated_backward")
+        short.bind(*[ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in entries], I8)
+        _lib, _short = L, short
     return _lib
 
 
@@ -446,6 +457,8 @@ def _half_type(t: torch.Tensor, what: str) -> int:
 class Context:
     """gvq_ctx for one layout on one CUDA device."""
 
+    _address = 0        # of the handle, for the short way; 0: none
+
     def __init__(self, layout, device: Optional[int] = None):
         self.layout = layout if isinstance(layout, HostLayout) else HostLayout.of(layout)
         if not torch.cuda.is_available():
@@ -454,6 +467,7 @@ class Context:
         self._h = ctypes.c_void_p()
         st = lib().gvq_create(ctypes.byref(self._h), ctypes.byref(self.layout.c), self.device, self._stream())
         _check(st, "gvq_create")
+        self._address = self._h.value
         self.d, self.k = self.layout.d, self.layout.k
         self.S = self.layout.total_slices()
         self.M = self.layout.total_entries()
@@ -477,6 +491,7 @@ class Context:
 
     def close(self):
         if self._h:
+            self._address = 0
             lib().gvq_destroy(self._h)
             self._h = ctypes.c_void_p()
 
@@ -661,14 +676,26 @@ class Context:
 
     def i8_quantize(self, x, stochastic=False, seed=0, node=0, out: Optional[I8] = None) -> I8:
         """gvq_i8_quantize along the rows of x [rows, cols]."""
+        if out is None and _short is not None:
+            q = _short.i8_quantize(self._address, self.device, x, True, False, stochastic, seed, node)
+            if q is not None:
+                return q
         return self._i8(x, True, False, stochastic, seed, node, out=out)[0]
 
     def i8_quantize_transposed(self, x, stochastic=False, seed=0, node=0, out: Optional[I8] = None) -> I8:
         """gvq_i8_quantize along the columns of x: the quantized [cols, rows] matrix."""
+        if out is None and _short is not None:
+            q = _short.i8_quantize(self._address, self.device, x, False, True, stochastic, seed, node)
+            if q is not None:
+                return q
         return self._i8(x, False, True, stochastic, seed, node, out_t=out)[1]
 
     def i8_quantize_both(self, x, stochastic=False, seed=0, node=0, out: Optional[I8] = None, out_t: Optional[I8] = None):
         """gvq_i8_quantize along the rows and along the columns: (by rows, by columns)."""
+        if out is None and out_t is None and _short is not None:
+            q = _short.i8_quantize(self._address, self.device, x, True, True, stochastic, seed, node)
+            if q is not None:
+                return q
         return self._i8(x, True, True, stochastic, seed, node, out, out_t)
 
     def i8_dequantize(self, q: I8, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -684,6 +711,8 @@ class Context:
 
     def i8_matmul(self, a: I8, b: I8, out: torch.Tensor) -> torch.Tensor:
         """gvq_i8_matmul: out [a.rows, b.rows] = a b^T; out is float32, bfloat16 or float16."""
+        if _short is not None and _short.i8_matmul(self._address, self.device, a, b, out):
+            return out
         device, k = self.device, a.cols
         rows, cols, ld = _rows(out, device, "i8_matmul")
         if k != b.cols or rows != a.rows or cols != b.rows:
@@ -724,6 +753,8 @@ class Context:
                       up: Optional[torch.Tensor] = None) -> torch.Tensor:
         """gvq_gated_forward: out [M, F] = act(x w_gate^T) * (x w_up^T); bfloat16 or float16 throughout.  gate, up: [M, F] that receive
         both projections for gated_backward."""
+        if _short is not None and _short.gated_forward(self._address, self.device, x, w_gate, w_up, out, ACTIVATION.get(act, -1), gate, up):
+            return out
         what = "gated_forward"
         a, half = _activation(act), self._half
         M, K, ldx = _rows(x, self.device, what)
@@ -749,6 +780,9 @@ class Context:
                        dw_gate: Optional[torch.Tensor] = None, dw_up: Optional[torch.Tensor] = None) -> None:
         """gvq_gated_backward: the gradients that are given room for.  dx [M, K] is of the operands' type; dw_gate, dw_up [F, K] are
         float32, bfloat16 or float16, of one type.  x may be None where neither is wanted, the weights where dx is not."""
+        if _short is not None and _short.gated_backward(self._address, self.device, dh, gate, up, x, w_gate, w_up, ACTIVATION.get(act, -1), dx,
+                                                        dw_gate, dw_up):
+            return
         what = "gated_backward"
         a, half = _activation(act), self._half
         M, F, ldh = _rows(dh, self.device, what)
@@ -783,6 +817,8 @@ class Context:
 
     def i8_gated(self, a: I8, w_gate: I8, w_up: I8, out: torch.Tensor, act: str = "silu") -> torch.Tensor:
         """gvq_i8_gated: out [a.rows, w_gate.rows] = act(a w_gate^T) * (a w_up^T); out is float32, bfloat16 or float16."""
+        if _short is not None and _short.i8_gated(self._address, self.device, a, w_gate, w_up, out, ACTIVATION.get(act, -1)):
+            return out
         code = _activation(act)
         rows, cols, ld = _rows(out, self.device, "i8_gated")
         if w_gate.cols != a.cols or w_up.cols != a.cols or w_gate.rows != w_up.rows or (rows, cols) != (a.rows, w_gate.rows):

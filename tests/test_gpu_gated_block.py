@@ -197,3 +197,61 @@ def test_refusals(ctx):
         gvq.I8(64, 64, codes=torch.empty(3, dtype=torch.int8, device="cuda"), scales=torch.empty(64, device="cuda"))
     with pytest.raises(ValueError):
         gvq.I8(64, 64, codes=torch.empty(64, 64, dtype=torch.int8, device="cuda"))
+
+
+def test_both_ways_of_the_binding_give_the_same_bits(ctx, monkeypatch):
+    """The long way, which the short one leaves to whatever is not plainly right, makes the same calls."""
+    from paper_1811_03617_b200 import gvq
+
+    def everything():
+        gen = torch.Generator(device="cuda").manual_seed(0)
+        x, wg, wu, dh = (torch.randn(r, c, generator=gen, device="cuda").bfloat16() for r, c in ((70, 129), (200, 129), (200, 129), (70, 200)))
+        out = []
+        for kw in (dict(), dict(stochastic=True, seed=2 ** 64 - 3, node=5)):
+            both = ctx.i8_quantize_both(x, **kw)
+            out += [t for q in (*both, ctx.i8_quantize(x, **kw), ctx.i8_quantize_transposed(x, **kw)) for t in (q.codes, q.scales)]
+        q, g, u = ctx.i8_quantize(x), ctx.i8_quantize(wg), ctx.i8_quantize(wu)
+        assert (q.rows, q.cols, q.device) == (70, 129, 0) and q.codes.dtype is torch.int8 and q.codes.shape == (70, 144) and q.scales.shape == (70,)
+        out.append(ctx.i8_matmul(q, g, torch.empty(70, 200, device="cuda")))
+        out.append(ctx.i8_gated(q, g, u, torch.empty(70, 200, device="cuda"), act="gelu"))
+        h, gate, up = (torch.empty(70, 200, dtype=torch.bfloat16, device="cuda") for _ in range(3))
+        out += [ctx.gated_forward(x, wg, wu, h, act="gelu_tanh", gate=gate, up=up), gate, up]
+        dx, dg, du = torch.empty_like(x), torch.empty(200, 129, device="cuda"), torch.empty(200, 129, device="cuda")
+        ctx.gated_backward(dh, gate, up, x, wg, wu, act="gelu_tanh", dx=dx, dw_gate=dg, dw_up=du)
+        du2 = torch.empty_like(du)
+        ctx.gated_backward(dh, gate, up, x, None, None, act="gelu_tanh", dw_up=du2)
+        return out + [dx, dg, du, du2]
+    short = everything()
+    assert gvq._short is not None
+    monkeypatch.setattr(gvq, "_short", None)
+    for a, b in zip(short, everything()):
+        assert torch.equal(a, b)
+
+
+def test_the_short_way_leaves_errors_to_the_long_one(ctx):
+    from paper_1811_03617_b200 import gvq
+    x, q = torch.zeros(64, 64, device="cuda"), gvq.I8(64, 64)
+    h, bf = ctx._address, x.bfloat16()
+    s = gvq._short
+    assert s.i8_quantize(h, 0, x, True, False, False, 0, 0) is not None
+    for args in ((0, 0, x), (h, 0, x[0]), (h, 0, x.t()[:, ::2]), (h, 0, x.double()), (h, 0, x.cpu()), (h, 0, None), (h, 0, x[:0]), (h, 0, x.expand(64, 64)[:1, :0])):
+        assert s.i8_quantize(*args, True, False, False, 0, 0) is None
+    assert s.i8_quantize(h, 0, x, True, False, False, "1", 0) is None and s.i8_quantize(h, 0, x) is None
+    assert s.i8_quantize(h, 0, x[:1].expand(64, 64), True, True, False, 0, 0) is None          # rows 0 entries apart
+    assert not s.i8_matmul(h, 0, q, q, x.double()) and not s.i8_matmul(h, 0, q, gvq.I8(64, 32), x) and not s.i8_matmul(h, 0, q, object(), x)
+    assert not s.i8_matmul(h, 0, gvq.I8.__new__(gvq.I8), q, x) and not s.i8_matmul(0, 0, q, q, x)
+    assert not s.i8_gated(h, 0, q, q, q, x, -1) and not s.i8_gated(h, 0, q, q, gvq.I8(32, 64), x, 0)
+    assert not s.gated_forward(h, 0, x, x, x, x, 0, None, None) and not s.gated_forward(h, 0, bf, bf, bf, x, 0, None, None)
+    assert not s.gated_forward(h, 0, bf, bf, bf, bf, 0, bf, None) and not s.gated_forward(h, 0, bf, bf[:, :32], bf, bf, 0, None, None)
+    assert not s.gated_backward(h, 0, bf, bf, bf, bf, bf, bf, 0, None, None, None)
+    assert not s.gated_backward(h, 0, bf, bf, bf, None, bf, bf, 0, None, x, None) and not s.gated_backward(h, 0, bf, bf, bf, bf, None, bf, 0, bf, None, None)
+    assert not s.gated_backward(h, 0, bf, bf, bf, bf, bf, bf, 0, None, x, bf) and not s.gated_backward(h, 0, bf, bf, bf, bf, bf, bf, 9, bf, None, None)
+    ctx.device_status()
+    with pytest.raises(ValueError):
+        ctx.i8_matmul(q, gvq.I8(64, 32), x)
+    with pytest.raises(gvq.GvqError):
+        ctx.i8_quantize(x[:1].expand(64, 64))
+    closed = gvq.Context(gvq.HostLayout(4, 4, [0], [4]))
+    closed.close()
+    with pytest.raises(gvq.GvqError):
+        closed.i8_quantize(x)
