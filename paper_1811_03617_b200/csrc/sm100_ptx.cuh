@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <mutex>
 
 namespace gvq {
 namespace ptx {
@@ -350,9 +351,13 @@ cudaError_t launch_chained(const P &prm, int grid, int threads, size_t smem, int
         cudaError_t e = cudaGetDevice(&dev);
         if (e != cudaSuccess) return e;
         if (dev >= 64 || raised[dev].load(std::memory_order_relaxed) < (int)smem) {
-            e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-            if (e != cudaSuccess) return e;
-            if (dev < 64) raised[dev].store((int)smem, std::memory_order_relaxed);
+            static std::mutex one_at_a_time;      // (another thread's smaller limit must not come after this one's)
+            const std::lock_guard<std::mutex> hold(one_at_a_time);
+            if (dev >= 64 || raised[dev].load(std::memory_order_relaxed) < (int)smem) {
+                e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+                if (e != cudaSuccess) return e;
+                if (dev < 64) raised[dev].store((int)smem, std::memory_order_relaxed);
+            }
         }
     }
     cudaLaunchConfig_t cfg = {};

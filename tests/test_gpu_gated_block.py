@@ -255,3 +255,27 @@ def test_the_short_way_leaves_errors_to_the_long_one(ctx):
     closed.close()
     with pytest.raises(gvq.GvqError):
         closed.i8_quantize(x)
+
+
+def test_threads_quantize_columns_of_different_lengths_at_once():
+    """Strips of different sizes in shared memory, whose limit the first launches raise, from threads with a context each."""
+    import threading
+    from paper_1811_03617_b200 import gvq
+    rows, got = (450, 900, 1500, 2900), {}
+    xs = {r: torch.randn(r, 130, generator=torch.Generator().manual_seed(r)).half() for r in rows}
+
+    def work(r):
+        ctx, x = gvq.Context(gvq.HostLayout(4, 4, [0], [4])), xs[r].cuda()
+        with torch.cuda.stream(torch.cuda.Stream()):
+            x.record_stream(torch.cuda.current_stream())
+            torch.cuda.current_stream().wait_stream(torch.cuda.default_stream())
+            q = [ctx.i8_quantize_transposed(x) for _ in range(5)][-1]
+            got[r] = q.codes.cpu(), q.scales.cpu()
+    threads = [threading.Thread(target=work, args=(r,)) for r in rows]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for r in rows:
+        codes, scales, _ = R.quantize(xs[r].t().contiguous())
+        assert torch.equal(got[r][0], codes) and torch.equal(got[r][1], scales)
