@@ -540,11 +540,13 @@ gvq_status gvq_mx4_dequantize_aggregate(gvq_ctx *ctx, const uint8_t *const *code
                   node, row, column).  Unbiased to 2^-14 of a step.
    A row that holds a NaN or an infinity has scale NaN and codes 0 and stands for NaN.
    codes:  device bytes [rows][16 * ceil(cols / 16)], rows padded by zeros; scales: device float [rows], 4-byte aligned.
+   Codes and scales made elsewhere are taken too: codes of -127 to 127 (what -128 gives is not defined: the longest sums of it
+   overflow), whatever lies in the padding.
    "Along the columns" means the same of the transposed matrix [cols][rows], as above.
    Sizes: rows, cols >= 1, below 2^31 - 1024; ceil(rows / 128) * ceil(cols / 128) < 2^31. */
 
 /* Bytes of the codes of a quantized matrix [rows][cols], and of the scratch that quantizing it along its columns takes
-   (0 up to 3072 rows); -1 on bad sizes. */
+   (0 where a strip of columns fits the shared memory of four SMs); -1 on bad sizes. */
 int64_t gvq_i8_codes_bytes(int64_t rows, int64_t cols);
 int64_t gvq_i8_scratch_bytes(int64_t rows, int64_t cols);
 
@@ -562,7 +564,8 @@ gvq_status gvq_i8_dequantize(gvq_ctx *ctx, const int8_t *codes, const float *sca
 /* The product of two quantized matrices, both quantized along the contraction:
      out[m][n] = (sum over k < K of a[m][k] * b[n][k]) * a_scale[m] * b_scale[n]
    The sum of codes is exact (32-bit integers; K <= 131072), the scales are applied in fp32, the result is rounded once to
-   dtype.  a: [M][K], b: [N][K]; out: device, dtype entries, rows ld entries apart (ld >= N), aligned to its entries' size.
+   dtype.  a: [M][K], b: [N][K]; out: device, dtype entries, rows ld entries apart (ld >= N), aligned to its entries' size,
+   apart from the operands.
    A linear layer's three products and few rows of a: as for the 4-bit format. */
 gvq_status gvq_i8_matmul(gvq_ctx *ctx, const int8_t *a_codes, const float *a_scales, const int8_t *b_codes, const float *b_scales,
                          int64_t M, int64_t N, int64_t K, void *out, int dtype, int64_t ld);
@@ -578,7 +581,8 @@ gvq_status gvq_i8_matmul(gvq_ctx *ctx, const int8_t *a_codes, const float *a_sca
    of 8): where x or a weight matrix has others, a copy that has is made in the workspace first.
    workspace: device, 16-byte aligned, gvq_gated_workspace_bytes() bytes: aligned != 0 where every one of x, w_gate and w_up
    that the call reads has such rows; 0 bytes (NULL) for a forward pass then.  Its contents carry nothing from one call to the
-   next; calls that run at the same time (graphs replayed on two streams) need one each. */
+   next; calls that run at the same time (graphs replayed on two streams) need one each.
+   Outputs lie apart from one another, from the workspace and from what the call reads. */
 typedef enum { GVQ_SILU = 0, GVQ_GELU = 1, GVQ_GELU_TANH = 2, GVQ_RELU = 3, GVQ_SIGMOID = 4 } gvq_activation;
 
 int64_t gvq_gated_workspace_bytes(int64_t M, int64_t F, int64_t K, int backward, int aligned);

@@ -19,8 +19,8 @@ namespace {
 
 constexpr float kMagic = 12582912.0f;               // 1.5 * 2^23: its pattern's low 22 bits are 0
 constexpr int kMaxRows = 512;      // of a CTA of i8_max_kernel
-// i8_strip_kernel: CTAs of a cluster, threads, words from row to row, most rows of a CTA (109 KB of shared memory)
-constexpr int kCluster = 4, kStripThreads = 512, kStripPitch = 36, kStripRows = 768;
+// i8_strip_kernel: CTAs of a cluster, threads, words from row to row, most rows of a CTA (106 KB of shared memory: two CTAs an SM)
+constexpr int kCluster = 4, kStripThreads = 512, kStripPitch = 36, kStripRows = 752;
 
 __host__ __device__ inline int64_t pitch_of(int64_t cols) { return (cols + 15) / 16 * 16; }
 inline int64_t row_blocks(int64_t rows) { return (rows + kMaxRows - 1) / kMaxRows; }

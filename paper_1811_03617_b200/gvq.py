@@ -382,7 +382,7 @@ class I8:
         if rows < 1 or cols < 1 or rows > _MOST or cols > _MOST or ((rows + 127) >> 7) * ((cols + 127) >> 7) >= 0x7FFFFFFF:
             raise ValueError(f"no 8-bit matrix of {rows} x {cols}")
         if codes is None and scales is None:
-            self._room(rows, cols, torch.empty(_i8_bytes(rows, cols), dtype=torch.int8, device=device or "cuda"))
+            self._room(rows, cols, torch.empty(_i8_bytes(rows, cols), dtype=torch.int8, device="cuda" if device is None else device))
             return
         if codes is None or scales is None:
             raise ValueError("codes and scales come together")

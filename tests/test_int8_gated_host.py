@@ -24,7 +24,7 @@ def test_sizes(gvq):
     for rows, cols in ((1, 1), (1, 16), (7, 33), (515, 1083), (4096, 16384)):
         assert L.gvq_i8_codes_bytes(rows, cols) == rows * -(-cols // 16) * 16
         assert L.gvq_i8_scratch_bytes(rows, cols) >= 0
-    assert L.gvq_i8_scratch_bytes(3072, 10 ** 6) == 0 and L.gvq_i8_scratch_bytes(3073, 10) > 0
+    assert L.gvq_i8_scratch_bytes(2900, 10 ** 6) == 0 and L.gvq_i8_scratch_bytes(3200, 10) > 0
     for rows, cols in ((0, 1), (1, 0), (-1, 5), (1 << 31, 1), (1, (1 << 31) - 1000), (1 << 30, 1 << 30)):
         assert L.gvq_i8_codes_bytes(rows, cols) == -1 and L.gvq_i8_scratch_bytes(rows, cols) == -1
         with pytest.raises(ValueError):
