@@ -1,7 +1,8 @@
 // Backward pass of the gated block (gvq.h, "the gated block"):
 //   dg = dh u act'(g),  du = dh act(g)             gated_slopes_kernel
 //   dx = dg Wg + du Wu                             one product whose contraction has two segments
-//   dWg = dg^T x,  dWu = du^T x                    one launch of two products that have x in common
+//   dWg = dg^T x,  dWu = du^T x                    one product of two halves that have x in common
+// in one launch for the slopes and one or two for the products,
 // and the copies of operands whose rows do not start at 16-byte boundaries, which TMA cannot address.
 #include "load8.cuh"
 #include "product.cuh"
@@ -94,10 +95,18 @@ int grid_of(int num_sms, int64_t items)
     return (int)(blocks < most ? blocks : most);
 }
 
+int64_t items_of(const RowCopies &c)      // of the largest
+{
+    int64_t items = 0;
+    for (int k = 0; k < c.n; ++k) items = items > c.rows[k] * c.chunks[k] ? items : c.rows[k] * c.chunks[k];
+    return items;
+}
+
 template <typename T, bool VEC>
 cudaError_t launch_slopes_as(const Launch &l, const SlopeParams &prm, int act)
 {
-    const int grid = grid_of(l.num_sms, prm.rows * prm.chunks);
+    const int64_t slopes = prm.rows * prm.chunks, copies = items_of(prm.copies);
+    const int grid = grid_of(l.num_sms, slopes > copies ? slopes : copies);
     switch (act) {
     case GVQ_SILU: return launch_chained<gated_slopes_kernel<T, GVQ_SILU, VEC>>(prm, grid, 256, 0, 1, l.stream);
     case GVQ_GELU: return launch_chained<gated_slopes_kernel<T, GVQ_GELU, VEC>>(prm, grid, 256, 0, 1, l.stream);
@@ -111,9 +120,7 @@ cudaError_t launch_slopes_as(const Launch &l, const SlopeParams &prm, int act)
 
 cudaError_t launch_align_rows(const Launch &l, const RowCopies &copies)
 {
-    int64_t items = 0;
-    for (int k = 0; k < copies.n; ++k) items = items > copies.rows[k] * copies.chunks[k] ? items : copies.rows[k] * copies.chunks[k];
-    return launch_chained<align_rows_kernel>(copies, grid_of(l.num_sms, items), 256, 0, 1, l.stream);
+    return launch_chained<align_rows_kernel>(copies, grid_of(l.num_sms, items_of(copies)), 256, 0, 1, l.stream);
 }
 
 cudaError_t launch_gated_slopes(const Launch &l, const void *dh, int64_t ld_dh, const void *g, int64_t ld_g, const void *u, int64_t ld_u,
@@ -126,21 +133,46 @@ cudaError_t launch_gated_slopes(const Launch &l, const void *dh, int64_t ld_dh, 
     return dtype == GVQ_BF16 ? launch_slopes_as<__nv_bfloat16, false>(l, prm, act) : launch_slopes_as<__half, false>(l, prm, act);
 }
 
-cudaError_t launch_gated_dx(const Launch &l, const void *dg, const void *du, int64_t ld_d, const void *gate, int64_t ld_gate, const void *up,
-                            int64_t ld_up, int dtype, int64_t M, int64_t F, int64_t K, void *dx, int64_t ld)
+namespace {
+
+// dx = dg Wg + du Wu: a contraction of two segments.  The weights are MN-major here: boxes of 64 of a row's entries by 64 rows.
+bool dx_problem(Params &prm, const Launch &l, const Cut &c, const GatedGrads &g)
 {
-    Params prm = start(l, dtype, dtype);
-    const Cut c = cut(l.num_sms, M, K, false, 2 * stages_of(F, k16), 64);
-    prm.M = c.few ? K : M;
-    prm.N = c.few ? M : K;
-    divide(prm, c, k16, false, F, 2, 1);
-    // the weights are MN-major here: boxes of 64 of a row's entries by 64 rows
+    prm = start(l, g.dtype, g.dtype);
+    prm.M = c.few ? g.K : g.M;
+    prm.N = c.few ? g.M : g.K;
+    divide(prm, c, k16, false, g.F, 2, 1);
     CUtensorMap *map_w = c.few ? prm.a : prm.b, *map_d = c.few ? prm.b : prm.a;
     const int box_d = c.few ? c.bn : 128;
-    if (!encode(l.encode, map_w, k16, gate, F, K, ld_gate, 64) || !encode(l.encode, map_w + 1, k16, up, F, K, ld_up, 64) ||
-        !encode(l.encode, map_d, k16, dg, M, F, ld_d, box_d) || !encode(l.encode, map_d + 1, k16, du, M, F, ld_d, box_d))
-        return cudaErrorInvalidValue;
-    set_output(prm, 0, dx, dtype, ld);
+    set_output(prm, 0, g.dx, g.dtype, g.ld_dx);
+    return encode(l.encode, map_w, k16, g.w[0], g.F, g.K, g.ld_w[0], 64) && encode(l.encode, map_w + 1, k16, g.w[1], g.F, g.K, g.ld_w[1], 64) &&
+           encode(l.encode, map_d, k16, g.d[0], g.M, g.F, g.ld_d, box_d) && encode(l.encode, map_d + 1, k16, g.d[1], g.M, g.F, g.ld_d, box_d);
+}
+// dWg = dg^T x, dWu = du^T x, or the one of them that is wanted: two halves of a product, both operands MN-major.
+int halves_of(const GatedGrads &g) { return g.dw[0] && g.dw[1] ? 2 : 1; }
+bool dw_problem(Params &prm, const Launch &l, const Cut &c, const GatedGrads &g)
+{
+    const int halves = halves_of(g);
+    prm = start(l, g.dtype, g.dw_dtype);
+    prm.M = g.F;
+    prm.N = g.K;
+    prm.a_mn = 1;
+    divide(prm, c, k16, false, g.M, 1, halves);
+    bool ok = encode(l.encode, &prm.b[0], k16, g.x, g.M, g.K, g.ldx, 64);
+    for (int i = 0; i < halves; ++i) {
+        const int which = g.dw[0] ? i : 1;
+        ok = ok && encode(l.encode, &prm.a[i], k16, g.d[which], g.M, g.F, g.ld_d, 64);
+        set_output(prm, i, g.dw[which], g.dw_dtype, g.ld_dw[which]);
+    }
+    return ok;
+}
+Cut cut_dx(const Launch &l, const GatedGrads &g) { return cut(l.num_sms, g.M, g.K, false, 2 * stages_of(g.F, k16), 64); }
+Cut cut_dw(const Launch &l, const GatedGrads &g) { return cut_tiles(l.num_sms, g.F, g.K, false, stages_of(g.M, k16), halves_of(g)); }
+
+cudaError_t launch_dx(const Launch &l, const Cut &c, const GatedGrads &g)
+{
+    Params prm;
+    if (!dx_problem(prm, l, c, g)) return cudaErrorInvalidValue;
     const cudaStream_t st = l.stream;
     if (c.few) {
         switch (c.bn) {
@@ -155,30 +187,47 @@ cudaError_t launch_gated_dx(const Launch &l, const void *dg, const void *du, int
     default: return launch<k16, 1, 64, false, false, true, false>(st, l.num_sms, prm);
     }
 }
-
-cudaError_t launch_gated_dw(const Launch &l, const void *dg, const void *du, int64_t ld_d, const void *x, int64_t ldx, int dtype, int64_t M,
-                            int64_t F, int64_t K, void *dw_gate, int64_t ld_dw_gate, void *dw_up, int64_t ld_dw_up, int out_dtype)
+cudaError_t launch_dw(const Launch &l, const Cut &c, const GatedGrads &g)
 {
-    Params prm = start(l, dtype, out_dtype);
-    prm.M = F;
-    prm.N = K;
-    // (one of the two may not be wanted)
-    const void *d[2] = {dw_gate ? dg : du, du};
-    void *out[2] = {dw_gate ? dw_gate : dw_up, dw_up};
-    const int64_t ld[2] = {dw_gate ? ld_dw_gate : ld_dw_up, ld_dw_up};
-    const int halves = dw_gate && dw_up ? 2 : 1;
-    const Cut c = cut_tiles(l.num_sms, F, K, false, stages_of(M, k16), halves);
-    divide(prm, c, k16, false, M, 1, halves);
-    if (!encode(l.encode, &prm.b[0], k16, x, M, K, ldx, 64)) return cudaErrorInvalidValue;
-    for (int i = 0; i < halves; ++i) {
-        if (!encode(l.encode, &prm.a[i], k16, d[i], M, F, ld_d, 64)) return cudaErrorInvalidValue;
-        set_output(prm, i, out[i], out_dtype, ld[i]);
-    }
+    Params prm;
+    if (!dw_problem(prm, l, c, g)) return cudaErrorInvalidValue;
     switch (c.bn) {
     case 256: return launch<k16, 2, 256, false, true, true, false>(l.stream, l.num_sms, prm);
     case 128: return launch<k16, 2, 128, false, true, true, false>(l.stream, l.num_sms, prm);
     default: return launch<k16, 1, 64, false, true, true, false>(l.stream, l.num_sms, prm);
     }
+}
+
+}  // namespace
+
+// Neither product needs the other: where one of them, or its last round of tiles, would leave SMs idle, they share a launch, each on
+// SMs of its own.
+cudaError_t launch_gated_products(const Launch &l, const GatedGrads &g)
+{
+    const bool dw = g.dw[0] || g.dw[1];
+    Cut cx = {}, cw = {};
+    if (g.dx) cx = cut_dx(l, g);
+    if (dw) cw = cut_dw(l, g);
+    if (g.dx && dw && !cx.few) {
+        const Extent e[2] = {{g.M, g.K, 2 * stages_of(g.F, k16), 1}, {g.F, g.K, stages_of(g.M, k16), halves_of(g)}};
+        const PairCut c = cut_pair(l.num_sms, e);
+        // (the second of two launches starts while the first ends)
+        if (c.time && c.time < 0.98 * (cx.time + cw.time - 1.5)) {
+            Pair pair;
+            if (!dx_problem(pair.p[0], l, c.c[0], g) || !dw_problem(pair.p[1], l, c.c[1], g)) return cudaErrorInvalidValue;
+            pair.blocks = c.blocks[0];
+            switch (c.c[0].bn) {
+            case 256: return launch_pair<k16, 2, 256, true>(l.stream, pair, c.blocks);
+            case 128: return launch_pair<k16, 2, 128, true>(l.stream, pair, c.blocks);
+            default: return launch_pair<k16, 1, 64, true>(l.stream, pair, c.blocks);
+            }
+        }
+    }
+    if (g.dx) {
+        const cudaError_t e = launch_dx(l, cx, g);
+        if (e != cudaSuccess || !dw) return e;
+    }
+    return launch_dw(l, cw, g);
 }
 
 }  // namespace gvq

@@ -205,10 +205,16 @@ struct RowCopies {
 cudaError_t launch_align_rows(const Launch &l, const RowCopies &copies);
 cudaError_t launch_gated_slopes(const Launch &l, const void *dh, int64_t ld_dh, const void *g, int64_t ld_g, const void *u, int64_t ld_u,
                                 int dtype, int64_t rows, int64_t cols, int act, void *dg, void *du, int64_t ld_out, const RowCopies &copies);
-cudaError_t launch_gated_dx(const Launch &l, const void *dg, const void *du, int64_t ld_d, const void *gate, int64_t ld_gate, const void *up,
-                            int64_t ld_up, int dtype, int64_t M, int64_t F, int64_t K, void *dx, int64_t ld);
-cudaError_t launch_gated_dw(const Launch &l, const void *dg, const void *du, int64_t ld_d, const void *x, int64_t ldx, int dtype, int64_t M,
-                            int64_t F, int64_t K, void *dw_gate, int64_t ld_dw_gate, void *dw_up, int64_t ld_dw_up, int out_dtype);
+// The products of a backward pass.  d, w, dw: the gate's and the other projection's; dx or dw null: not wanted.
+struct GatedGrads {
+    const void *d[2], *w[2], *x;
+    int64_t ld_d, ld_w[2], ldx;
+    int dtype, dw_dtype;
+    int64_t M, F, K;
+    void *dx, *dw[2];
+    int64_t ld_dx, ld_dw[2];
+};
+cudaError_t launch_gated_products(const Launch &l, const GatedGrads &g);
 
 // Basis fit.  Workspace layout is private to fit_basis.cu.
 size_t fit_workspace_bytes(int d, int n_layers, int n_fit_tiles);

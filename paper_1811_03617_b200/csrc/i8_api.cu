@@ -182,11 +182,9 @@ gvq_status gvq_gated_backward(gvq_ctx *ctx, const void *dh, int64_t ld_dh, const
     const RowCopies copies = align_operands(ops, 3, at + 2 * bytes_of(M, F));
     const int64_t ld_d = padded(F, 8);
     GVQ_CUDA(ctx, launch_gated_slopes(l, dh, ld_dh, gate, ld_gate_in, up, ld_up_in, dtype, M, F, activation, dg, du, ld_d, copies));
-    if (dx_opt)
-        GVQ_CUDA(ctx, launch_gated_dx(l, dg, du, ld_d, ops[1].p, ops[1].ld, ops[2].p, ops[2].ld, dtype, M, F, K, dx_opt, ld_dx));
-    if (dw)
-        GVQ_CUDA(ctx, launch_gated_dw(l, dg, du, ld_d, ops[0].p, ops[0].ld, dtype, M, F, K, dw_gate_opt, ld_dw_gate, dw_up_opt, ld_dw_up,
-                                      dw_dtype));
+    const GatedGrads g = {{dg, du}, {ops[1].p, ops[2].p}, ops[0].p, ld_d, {ops[1].ld, ops[2].ld}, ops[0].ld, dtype, dw_dtype, M, F, K,
+                          dx_opt, {dw_gate_opt, dw_up_opt}, ld_dx, {ld_dw_gate, ld_dw_up}};
+    GVQ_CUDA(ctx, launch_gated_products(l, g));
     return GVQ_OK;
 }
 

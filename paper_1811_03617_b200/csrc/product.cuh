@@ -26,6 +26,8 @@
 #include "row32.cuh"
 #include "sm100_ptx.cuh"
 
+#include <type_traits>
+
 namespace gvq {
 namespace product {
 
@@ -55,6 +57,12 @@ struct Params {
     const float *scale_m[2], *scale_n[2];   // of 8-bit operands
     int32_t *error_word;
     int wait_kcycles, test_drop;
+    int a_mn;                          // of two problems in a launch: this one's A is MN-major
+};
+// Two products of the same form in one launch, each on CTAs of its own.
+struct Pair {
+    Params p[2];
+    int blocks;                        // CTAs of the first
 };
 
 template <int CG, int BN, bool FEW> struct Shape {
@@ -265,15 +273,23 @@ __device__ __forceinline__ bool epilogue_and(bool ok)
     return r != 0;
 }
 
-template <int KIND, int CG, int BN, bool FEW, bool A_MN, bool B_MN, bool GATED>
-__global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_constant__ Params prm)
+template <int KIND, int CG, int BN, bool FEW, bool A_MN, bool B_MN, bool GATED, bool PAIR = false>
+__global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_constant__ std::conditional_t<PAIR, Pair, Params> all)
 {
     using S = Shape<CG, BN, FEW>;
     constexpr int KS = KIND == kI8 ? 128 : 64;                        // entries of the contraction a stage
     constexpr bool SIDE = GATED && !FEW;                              // both matrices lie side by side in B
     constexpr int HN = SIDE ? BN / 2 : BN;                            // columns of the output a tile has
     constexpr int BL = BN / CG;                                       // rows of B that this CTA holds
-    static_assert(!(KIND == kI8 && (A_MN || B_MN)) && (!B_MN || BL % 64 == 0) && !(FEW && (CG == 2 || B_MN)) && !(GATED && A_MN), "forms");
+    static_assert(!(KIND == kI8 && (A_MN || B_MN)) && (!B_MN || BL % 64 == 0) && !(FEW && (CG == 2 || B_MN || PAIR)) && !(GATED && A_MN), "forms");
+    int block = blockIdx.x, blocks = gridDim.x, which = 0;
+    if constexpr (PAIR) {
+        which = block >= all.blocks;
+        blocks = which ? blocks - all.blocks : all.blocks;
+        if (which) block -= all.blocks;
+    }
+    const Params &prm = [&]() -> const Params & { if constexpr (PAIR) return all.p[which]; else return all; }();
+    const bool a_mn = PAIR ? prm.a_mn : A_MN;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     unsigned char *staging = smem + S::ALL;
@@ -304,7 +320,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
     const uint32_t tmem = *tmem_slot;
     launch_dependents();
     const int n_tiles = prm.tiles_m * prm.tiles_n;
-    const int first = blockIdx.x / (CG * parts), stride = gridDim.x / (CG * parts);
+    const int first = block / (CG * parts), stride = blocks / (CG * parts);
     const int st0 = prm.n_stages * part / parts, st1 = prm.n_stages * (part + 1) / parts;    // this CTA's stages
     if constexpr (FEW) {
         // weights on their way to L2 while the launch before this one ends (nothing is read yet that it may write)
@@ -348,9 +364,9 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
                             if (CG == 2) tma_load_2d_pair(to, map, mn ? at : k, mn ? k : at, bar);
                             else tma_load_2d(to, map, mn ? at : k, mn ? k : at, full + s);
                         };
-                        load(dst, prm.a + half + seg, A_MN, m0);
-                        if (A_MN && (!FEW || a_bytes > kBox)) load(dst + kBox, prm.a + half + seg, A_MN, m0 + 64);
-                        if (FEW && GATED) load(dst + a_bytes, prm.a + 1, A_MN, m0);
+                        load(dst, prm.a + half + seg, a_mn, m0);
+                        if (a_mn && (!FEW || a_bytes > kBox)) load(dst + kBox, prm.a + half + seg, true, m0 + 64);
+                        if (FEW && GATED) load(dst + a_bytes, prm.a + 1, false, m0);
                         if constexpr (SIDE && CG == 2) load(dst_b, prm.b + rank, false, n0);
                         else if constexpr (SIDE) {
                             load(dst_b, prm.b, false, n0);
@@ -374,13 +390,14 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
         if (rank == 0 && elect_one()) {
             uint32_t s = 0, phase = 0, t = 0;
             const uint32_t base = smem_u32(smem);
-            const uint64_t a0 = A_MN ? make_mn_desc(base, kBox) : make_b_desc(base);
+            const uint64_t a0 = a_mn ? make_mn_desc(base, kBox) : make_b_desc(base);
             const uint64_t b0 = B_MN ? make_mn_desc(base + stage_bytes - S::B_BYTES, kBox)
                                      : make_b_desc(base + stage_bytes - S::B_BYTES);
             // 32 bytes of a K-major row, or 16 rows of 128 bytes of an MN-major box
-            constexpr uint32_t IA = A_MN ? 16 * 128 / 16 : 2, IB = B_MN ? 16 * 128 / 16 : 2;
+            const uint32_t IA = a_mn ? 16 * 128 / 16 : 2;
+            constexpr uint32_t IB = B_MN ? 16 * 128 / 16 : 2;
             const uint32_t idesc = KIND == kI8 ? idesc_i8(128 * CG, BN)
-                                               : make_idesc_f16(128 * CG, BN, A_MN, B_MN) | (prm.bf16 ? (1u << 7) | (1u << 10) : 0u);
+                                               : make_idesc_f16(128 * CG, BN, a_mn, B_MN) | (prm.bf16 ? (1u << 7) | (1u << 10) : 0u);
             for (int tile = first; tile < n_tiles && !failed; tile += stride, ++t) {
                 const uint32_t buf = t & 1, d = tmem + buf * BN;
                 if (t > 1) {
@@ -566,6 +583,15 @@ cudaError_t launch(cudaStream_t st, int num_sms, const Params &prm)
         prm, cluster * (int)(tiles < num_sms / cluster ? tiles : num_sms / cluster), NTHREADS, S::SMEM, cluster, st);
 }
 
+template <int KIND, int CG, int BN, bool B_MN>
+cudaError_t launch_pair(cudaStream_t st, const Pair &pair, const int (&blocks)[2])
+{
+    using S = Shape<CG, BN, false>;
+    const int parts = pair.p[0].parts > pair.p[1].parts ? pair.p[0].parts : pair.p[1].parts;
+    return launch_chained<product_kernel<KIND, CG, BN, false, false, B_MN, false, true>>(pair, blocks[0] + blocks[1], NTHREADS, S::SMEM,
+                                                                                     CG * parts, st);
+}
+
 // A matrix [rows][cols] of 16-bit or 8-bit entries, rows ld entries apart and starting at 16-byte boundaries: boxes of 128 bytes of
 // a row by `box_rows` rows.
 inline bool encode(EncodeTiledFn enc, CUtensorMap *map, int kind, const void *p, int64_t rows, int64_t cols, int64_t ld, int box_rows)
@@ -594,6 +620,7 @@ struct Cut {
     bool few;          // the tokens are B: A and B, M and N change places
     int cg, bn;        // of the kernel
     int rows_a, parts;
+    double time;       // expected, in microseconds
 };
 
 // Parts of a contraction of n stages where a CTA has a tile alone: as many as there are SMs for, of `least` stages at least.  Clusters
@@ -612,20 +639,63 @@ inline double join_cost(int parts) { return parts > 1 ? 1.2 + 0.3 * parts : 0.0;
 
 // Tiles: of the forms, the one with the least time in microseconds by what was measured: a tile's stages, its epilogue where that
 // takes longer than another tile's stages, and once what a launch, the pipeline's start and the last epilogue take.
+struct Form { int cg, bn; double stage, epilogue, once; };
+static const Form kForms[3] = {{2, 256, 0.29, 3.6, 6.2}, {2, 128, 0.21, 2.6, 4.7}, {1, 64, 0.21, 1.4, 3.8}};
 inline Cut cut_tiles(int num_sms, int64_t M, int64_t N, bool gated, int n, int halves)
 {
-    static const struct { int cg, bn; double stage, epilogue, once; } forms[3] = {
-        {2, 256, 0.29, 3.6, 6.2}, {2, 128, 0.21, 2.6, 4.7}, {1, 64, 0.21, 1.4, 3.8}};
     Cut best = {};
-    double least = 0;
-    for (const auto &f : forms) {
+    for (const Form &f : kForms) {
         const int64_t tiles = (int64_t)halves * tiles_of(M, 128 * f.cg) * tiles_of(N, f.bn / (gated ? 2 : 1));
         const int slots = num_sms / f.cg;
         const int most = f.cg == 1 ? parts_of(num_sms, tiles, n, 4) : 1;
         for (int parts = 1; parts <= most; parts *= 2) {
             const double own = f.stage * ((n + parts - 1) / parts), more = own > f.epilogue ? own : f.epilogue;
             const double t = f.once + own + join_cost(parts) + more * (double)((tiles * parts + slots - 1) / slots - 1);
-            if (!best.cg || t < least) { best = {false, f.cg, f.bn, 128, parts}; least = t; }
+            if (!best.cg || t < best.time) best = {false, f.cg, f.bn, 128, parts, t};
+        }
+    }
+    return best;
+}
+
+// Two products in one launch: each on SMs of its own, that both end at about the same time.
+struct PairCut {
+    Cut c[2];
+    int blocks[2];
+    double time;
+};
+struct Extent { int64_t M, N; int n, halves; };      // of a product; n: stages of its contraction
+inline PairCut cut_pair(int num_sms, const Extent (&e)[2])
+{
+    PairCut best = {};
+    for (const Form &f : kForms) {
+        int64_t tiles[2];
+        double own[2], more[2];
+        for (int i = 0; i < 2; ++i) tiles[i] = (int64_t)e[i].halves * tiles_of(e[i].M, 128 * f.cg) * tiles_of(e[i].N, f.bn);
+        // parts of the one's contraction and of the other's: one, or as many as a cluster has CTAs
+        for (int cluster = 1; cluster <= (f.cg == 1 ? 8 : 1); cluster *= 2) {
+            const int slots = (cluster <= 2 ? num_sms : cluster == 4 ? num_sms * 7 / 8 : num_sms * 2 / 3) / (f.cg * cluster) * cluster;
+            for (int which = cluster == 1 ? 0 : 1; which < (cluster == 1 ? 1 : 4); ++which) {      // (bit i: of product i)
+                const int parts[2] = {which & 1 ? cluster : 1, which & 2 ? cluster : 1};
+                bool fits = true;
+                for (int i = 0; i < 2; ++i) {
+                    fits = fits && (parts[i] == 1 || (e[i].n >= 4 * parts[i] && tiles[i] * parts[i] < slots));
+                    own[i] = f.stage * ((e[i].n + parts[i] - 1) / parts[i]) + join_cost(parts[i]);
+                    more[i] = own[i] > f.epilogue ? own[i] : f.epilogue;
+                }
+                // rounds of the first's tiles; past eight of them two launches are as good
+                for (int rounds = 1; fits && rounds <= (parts[0] > 1 ? 1 : 8) && rounds <= tiles[0]; ++rounds) {
+                    const int64_t first = ((tiles[0] * parts[0] + rounds - 1) / rounds + cluster - 1) / cluster * cluster;
+                    if (first >= slots) continue;
+                    const int64_t need = (tiles[1] * parts[1] + cluster - 1) / cluster * cluster, second = need < slots - first ? need : slots - first;
+                    if (parts[1] > 1 && second < need) continue;
+                    const double a = own[0] + more[0] * (rounds - 1);
+                    const double b = own[1] + more[1] * (double)((tiles[1] * parts[1] + second - 1) / second - 1);
+                    const double t = f.once + (a > b ? a : b);
+                    if (!best.time || t < best.time)
+                        best = {{{false, f.cg, f.bn, 128, parts[0], t}, {false, f.cg, f.bn, 128, parts[1], t}},
+                                {(int)first * f.cg, (int)second * f.cg}, t};
+                }
+            }
         }
     }
     return best;
