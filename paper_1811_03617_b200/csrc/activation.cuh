@@ -44,13 +44,14 @@ __device__ __forceinline__ float activation(int act, float x)
     }
 }
 // v = act(v) * u
-template <int ACT>
-__device__ __forceinline__ void activate_as(float (&v)[32], const float (&u)[32])
+template <int ACT, int N>
+__device__ __forceinline__ void activate_as(float (&v)[N], const float (&u)[N])
 {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = activation_of<ACT>(v[i]) * u[i];
+    for (int i = 0; i < N; ++i) v[i] = activation_of<ACT>(v[i]) * u[i];
 }
-__device__ __forceinline__ void activate(int act, float (&v)[32], const float (&u)[32])
+template <int N>
+__device__ __forceinline__ void activate(int act, float (&v)[N], const float (&u)[N])
 {
     switch (act) {
     case GVQ_SILU: activate_as<GVQ_SILU>(v, u); break;

@@ -36,6 +36,7 @@ using namespace ptx;
 constexpr int NTHREADS = 320;
 constexpr int kHalves = 2;             // epilogue warps that share a quarter of the tile's rows, every other 32 columns each
 constexpr int kJoinPitch = 129;        // (a row's words of 16 bytes, eight lanes' of them, lie in different banks)
+constexpr int kWindow = 12;            // words of a lane's sector of shared memory: 8, and 4 that spread the lanes over the banks
 constexpr int kBox = 8192;             // an MN-major box: 64 entries (128 bytes) x 64 steps of the contraction
 constexpr uint32_t A_BYTES = 128 * 128;
 
@@ -74,8 +75,8 @@ template <int CG, int BN, bool FEW> struct Shape {
     static constexpr uint32_t JOIN = BN / 4 * kJoinPitch * 16, JOIN_AT = FEW ? ROOM + A_BYTES : 0;
     static constexpr uint32_t ALL = FEW ? (JOIN_AT + JOIN + 1023) / 1024 * 1024 : STAGES * LOADED;
     static constexpr uint32_t TMEM = 2 * BN <= 32 ? 32 : 2 * BN <= 64 ? 64 : 2 * BN <= 128 ? 128 : 2 * BN <= 256 ? 256 : 512;
-    // of an epilogue warp: 16 rows of a piece (tiles of few rows have no use for it), and its columns' scales
-    static constexpr uint32_t PIECE = FEW ? 0 : 16 * 128, STAGING = PIECE + 512;
+    // of an epilogue warp: a sector a lane (tiles of few rows have no use for them), and its columns' scales
+    static constexpr uint32_t PIECE = FEW ? 0 : 32 * kWindow * 4, STAGING = PIECE + 512;
     static constexpr size_t SMEM = (size_t)ALL + 4 * kHalves * STAGING + 512 + 1024;
     static_assert(LOADED % 1024 == 0 && SMEM <= 232448, "room");
     static_assert(CG == 2 || JOIN_AT + JOIN <= ALL, "room to join parts");
@@ -122,18 +123,13 @@ __device__ __forceinline__ void store_four(void *out, int dtype, int64_t at, int
             if (e < n) store_one(out, dtype, at + e * step, x[e]);
     }
 }
-// A lane's 32 columns of a row, which starts at a 16-byte boundary: whole 32-byte sectors where it starts at such a boundary.
-__device__ __forceinline__ void store32(void *p, int align, const uint32_t (&w)[8])
+// A sector of 32 bytes; a lane's 32 columns of a row that starts at one.
+__device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8])
 {
-    if (align == 32)
-        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                     ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
-    else {
-        static_cast<uint4 *>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        static_cast<uint4 *>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-    }
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
 }
-__device__ __forceinline__ void store_row(void *out, int dtype, int align, int64_t at, const float (&v)[32])
+__device__ __forceinline__ void store_row(void *out, int dtype, int64_t at, const float (&v)[32])
 {
     uint32_t w[8];
     if (dtype == GVQ_F32) {
@@ -141,49 +137,104 @@ __device__ __forceinline__ void store_row(void *out, int dtype, int align, int64
         for (int j = 0; j < 4; ++j) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[8 * j + i]);
-            store32(static_cast<float *>(out) + at + 8 * j, align, w);
+            store32(static_cast<float *>(out) + at + 8 * j, w);
         }
     } else {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = pack_as(dtype, v[16 * j + 2 * i], v[16 * j + 2 * i + 1]);
-            store32(static_cast<uint16_t *>(out) + at + 16 * j, align, w);
+            store32(static_cast<uint16_t *>(out) + at + 16 * j, w);
         }
     }
 }
-// Rows that start anywhere: 16 of them at a time go through shared memory (16-byte chunk j of row r at place j ^ (r % 8)) and out along
-// the rows, two entries a lane of a 16-bit type where rows start at 4-byte boundaries.
-__device__ __forceinline__ void store_rows(unsigned char *buf, int lane, int dtype, void *out, int64_t at, int64_t ld, int rows, int cols,
-                                           const float (&v)[32])
+// Bytes lo to hi of a sector at `from` (shared memory) to the same places from `to` on; both are even.
+__device__ __forceinline__ void store_bytes(char *to, const uint32_t *from, int lo, int hi)
 {
-    auto word = [&](int r, int c) { return buf + r * 128 + (((c >> 2) ^ (r & 7)) << 4) + (c & 3) * 4; };
-    const bool pairs = dtype != GVQ_F32 && (ld & 1) == 0 && (reinterpret_cast<uintptr_t>(static_cast<uint16_t *>(out) + at) & 3u) == 0;
+    auto move = [&](auto unit) {
+        using U = decltype(unit);
+        *reinterpret_cast<U *>(to + lo) = *reinterpret_cast<const U *>(reinterpret_cast<const char *>(from) + lo);
+        lo += (int)sizeof(U);
+    };
+    if ((lo & 2) && lo + 2 <= hi) move(uint16_t{});
+    if ((lo & 4) && lo + 4 <= hi) move(uint32_t{});
+    if ((lo & 8) && lo + 8 <= hi) move(uint2{});
+    if (hi - lo >= 16) move(uint4{});
+    if (hi - lo >= 8) move(uint2{});
+    if (hi - lo >= 4) move(uint32_t{});
+    if (hi - lo >= 2) move(uint16_t{});
+}
+// `cols` columns of a warp's rows, which start anywhere; value(c, x) gives the lane's 16 entries from column c on.  L2 takes a 32-byte
+// sector in parts at a fraction of the rate at which it takes it whole, so only whole ones are written but for a row's first and last
+// of the strip: 64 bytes at a time are shifted in registers by the row's offset within a sector (by 16, 8, 4 and 2 bytes), and what
+// they begin of the next sector waits.
+template <typename F>
+__device__ __forceinline__ void store_strip(uint32_t *win, int lane, int dtype, void *out, int64_t at, int64_t ld, int rows, int cols, F value)
+{
+    const int size = dtype == GVQ_F32 ? 4 : 2, bytes = cols * size;
+    char *to = static_cast<char *>(out) + (at + lane * ld) * size;
+    const int phase = (int)(reinterpret_cast<uintptr_t>(to) & 31u), words = phase >> 2;
+    to -= phase;
+    const uint32_t shift = phase & 2 ? 16 : 0;
+    const bool fine = __any_sync(0xffffffffu, phase & 15);
+    uint32_t kept[7] = {}, last = 0;      // words of a sector that is not whole, the word before the next
+    auto sector = [&](int place, const uint32_t (&x)[8]) {
+        const int lo = max(0, phase - place), hi = min(32, phase + bytes - place);
+        if (lane >= rows || lo >= hi) return;
+        if (lo == 0 && hi == 32) store32(to + place, x);
+        else {
+            uint32_t *own = win + lane * kWindow;
+            *reinterpret_cast<uint4 *>(own) = make_uint4(x[0], x[1], x[2], x[3]);
+            *reinterpret_cast<uint4 *>(own + 4) = make_uint4(x[4], x[5], x[6], x[7]);
+            store_bytes(to + place, own, lo, hi);
+        }
+    };
+    int place = 0;
 #pragma unroll 1
-    for (int r0 = 0; r0 < rows; r0 += 16) {
-        __syncwarp();
-        if ((lane & 16) == r0) {
+    for (int c = 0; c < cols; c += 64 / size, place += 64) {
+        uint32_t y[23], x[8];
+        float v[16];
+        __syncwarp();      // (sums are read by a warp's lanes together)
+        value(c, v);
+        if (size == 4) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                *reinterpret_cast<float4 *>(word(lane & 15, 4 * j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-        }
-        __syncwarp();
-        const int n = min(16, rows - r0);
-        const int64_t from = at + r0 * ld;
-        if (pairs) {
-            const int c = (lane & 15) * 2;
-#pragma unroll 4
-            for (int r = lane >> 4; r < n; r += 2) {
-                const float2 x = *reinterpret_cast<const float2 *>(word(r, c));
-                if (c + 1 < cols) *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(out) + from + r * ld + c) = pack_as(dtype, x.x, x.y);
-                else if (c < cols) store_one(out, dtype, from + r * ld + c, x.x);
-            }
+            for (int k = 0; k < 16; ++k) y[k] = __float_as_uint(v[k]);
         } else {
-#pragma unroll 4
-            for (int r = 0; r < n; ++r)
-                if (lane < cols) store_one(out, dtype, from + r * ld + lane, *reinterpret_cast<const float *>(word(r, lane)));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) y[k] = pack_as(dtype, v[2 * k], v[2 * k + 1]);
+            value(c + 16, v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) y[8 + k] = pack_as(dtype, v[2 * k], v[2 * k + 1]);
         }
+#pragma unroll
+        for (int k = 16; k < 23; ++k) y[k] = 0;
+        auto up = [&](int d) {
+            const bool by = phase & (4 * d);
+#pragma unroll
+            for (int k = 22; k >= 0; --k) y[k] = by ? (k >= d ? y[k - d] : 0u) : y[k];
+        };
+        if (fine) {
+            const uint32_t before = last;
+            last = y[15];
+#pragma unroll
+            for (int k = 15; k >= 0; --k) y[k] = __funnelshift_l(k ? y[k - 1] : before, y[k], shift);
+            up(1);
+            up(2);
+        }
+        up(4);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = k < 7 && k < words ? kept[k < 7 ? k : 0] : y[k];
+        sector(place, x);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = y[8 + k];
+        sector(place + 32, x);
+#pragma unroll
+        for (int k = 0; k < 7; ++k) kept[k] = y[16 + k];
     }
+    uint32_t x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = k < 7 && k < words ? kept[k < 7 ? k : 0] : last >> 16;      // (of an odd row, an entry that is left)
+    sector(place, x);
 }
 
 // A tile's place: tiles go through groups of `group` tiles along M, so that the operands of the tiles at work at a time lie
@@ -505,39 +556,76 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
                     }
                 }
             };
-            // a piece to output `slot`
-            auto store = [&](int slot, int64_t n, int cols, const float (&v)[32]) {
-                void *out = prm.out[slot];
-                const int64_t ld = prm.ld[slot];
-                const int align = prm.align[slot];
-                if constexpr (FEW) {       // rows of A run along the output's rows: a warp's lanes do too
+            if constexpr (FEW) {       // rows of A run along the output's rows: a warp's lanes do too
+#pragma unroll 1
+                for (int j = 0; j < NS && NS * side + j < NP; ++j) {
+                    const int64_t n = n0 + 32 * (NS * side + j);
+                    const int cols = (int)min((int64_t)PW, prm.N - n);
+                    if (rows <= 0 || cols <= 0) break;
+                    float v[32];
+                    __syncwarp();
+                    sums(0, j, v);
                     if (lane < rows) {
 #pragma unroll
                         for (int i = 0; i < PW; ++i)
-                            if (i < cols) store_one(out, dtype, m0 + lane + (n + i) * ld, v[i]);
+                            if (i < cols) store_one(prm.out[half], dtype, m0 + lane + (n + i) * prm.ld[half], v[i]);
                     }
-                } else if (align >= 16 && cols == 32) {
-                    if (lane < rows) store_row(out, dtype, align, (m0 + lane) * ld + n, v);
-                } else
-                    store_rows(mine, lane, dtype, out, m0 * ld + n, ld, rows, cols, v);
-            };
+                }
+            } else {
+                // this warp's columns, side by side
+                const int64_t n = n0 + 32 * NS * side;
+                const int cols = (int)min((int64_t)32 * min(NS, NP - NS * side), prm.N - n);
+                const bool all = SIDE && prm.out[1];
+                const bool direct = prm.align[half] == 32 && (!all || (prm.align[1] == 32 && prm.align[2] == 32));
+                if (rows > 0 && cols > 0) {
+                    int j = 0;
+                    if (direct) {
 #pragma unroll 1
-            for (int j = 0; j < NS && NS * side + j < NP; ++j) {
-                const int64_t n = n0 + 32 * (NS * side + j);
-                const int cols = (int)min((int64_t)PW, prm.N - n);
-                if (rows <= 0 || cols <= 0) break;
-                float v[32];
-                sums(0, j, v);
-                if constexpr (SIDE) {
-                    float u[32];
-                    sums(1, j, u);
-                    if (prm.out[1]) {
-                        store(1, n, cols, v);
-                        store(2, n, cols, u);
+                        for (; 32 * (j + 1) <= cols; ++j) {
+                            float v[32];
+                            __syncwarp();
+                            sums(0, j, v);
+                            auto store = [&](int slot, const float (&x)[32]) {
+                                if (lane < rows) store_row(prm.out[slot], dtype, (m0 + lane) * prm.ld[slot] + n + 32 * j, x);
+                            };
+                            if constexpr (SIDE) {
+                                float u[32];
+                                sums(1, j, u);
+                                if (all) {
+                                    store(1, v);
+                                    store(2, u);
+                                }
+                                activate(prm.act, v, u);
+                                store(0, v);
+                            } else store(half, v);
+                        }
                     }
-                    activate(prm.act, v, u);
-                    store(0, n, cols, v);
-                } else store(half, n, cols, v);
+                    const int left = cols - 32 * j;
+                    if (left > 0) {
+                        // 16 sums of one matrix from column c of the strip on
+                        auto sixteen = [&](int which, int c, float (&x)[16]) {
+                            tmem_ld16_wait(acc + (SIDE ? which * HN : 0) + 32 * NS * side + c, x);
+                            if constexpr (KIND == kI8) {
+                                const float *of = scales + (SIDE ? which : 0) * NS * 32 + c;
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) x[i] = __int2float_rn(__float_as_int(x[i])) * sm * of[i];
+                            }
+                        };
+#pragma unroll 1
+                        for (int slot = all ? 2 : half; slot >= (SIDE ? 0 : half); --slot)
+                            store_strip(reinterpret_cast<uint32_t *>(mine), lane, dtype, prm.out[slot], m0 * prm.ld[slot] + n + 32 * j,
+                                        prm.ld[slot], rows, left, [&](int c, float (&x)[16]) {
+                                            sixteen(SIDE && slot == 2 ? 1 : 0, 32 * j + c, x);
+                                            if constexpr (SIDE) {
+                                                if (slot == 0) {
+                                                    float u[16];
+                                                    sixteen(1, 32 * j + c, u);
+                                                    activate(prm.act, x, u);
+                                                }
+                                            }
+                                        });
+                    }
+                }
             }
             tc_fence_before();
             __syncwarp();
