@@ -12,22 +12,6 @@ namespace {
 
 using namespace product;
 
-// f(row, chunk) of every chunk of eight entries of `rows` rows of `chunks` of them, the grid's threads side by side.  One division a
-// thread: what a step adds is the same for all.
-template <typename F>
-__device__ __forceinline__ void for_chunks(int64_t rows, uint32_t chunks, F f)
-{
-    const uint32_t first = blockIdx.x * 256 + threadIdx.x, step = gridDim.x * 256, dr = step / chunks, dc = step - dr * chunks;
-    int64_t r = first / chunks;
-    uint32_t c = first - (uint32_t)r * chunks;
-    while (r < rows) {
-        f(r, (int)c);
-        r += dr;
-        c += dc;
-        if (c >= chunks) { c -= chunks; ++r; }
-    }
-}
-
 // The copies, eight entries a thread at a time; rows of a copy are padded to eight entries by zeros.
 __device__ __forceinline__ void copy_rows(const RowCopies &k)
 {

@@ -5,6 +5,12 @@
 //  i8_max_kernel, i8_tile_kernel   along columns too long for that: largest magnitudes first, then tile by tile
 //  i8_dequantize_kernel
 //
+// Measured, from memory, in us (the bytes at the copy rate): rows of 8192 x 4096 bf16 20.0 nearest, 28 stochastic (15.4), fp32 28 and 32
+// (25.7); columns of 2048 x 4096 bf16 in strips 9.9 and 12.6 (3.8); columns of 8192 x 4096 bf16, read twice, 30 and 41 (15.4), fp32
+// 60 and 70 (25.7); 777 x 1083 rows 3.3, columns 6.5 (0.4).  Of large ones instructions take as long as memory: of the nearest codes
+// the conversions, maxima and packing, of the stochastic ones the random words, 10 integer instructions for two entries.  Small ones
+// are a launch and the way to memory and back.
+//
 // With a = max(max |x|, 2^-100) and r the largest float with r a <= 127, a code is x r to the nearest whole number, rounded from
 // the exact product: one fused multiply-add to 1.5 * 2^23 leaves it in the low bits, two's complement.  Stochastic rounding adds 14
 // random bits below floor(2^14 x r), which the same instruction leaves there when it rounds down (2^14 * 127 < 2^22).
@@ -421,30 +427,39 @@ __global__ void __launch_bounds__(256) i8_tile_kernel(const QuantParams prm)
     }
 }
 
+// Four entries a thread.  8192 x 4096 in 34 us, where the bytes take 26 at the copy rate.
+template <bool VEC>
 __global__ void __launch_bounds__(256) i8_dequantize_kernel(const int8_t *codes, const float *scales, int64_t rows, int64_t cols, float *out,
                                                             int64_t ld)
 {
     ptx::launch_dependents();
     ptx::grid_dependency_wait();
-    const int64_t pitch = pitch_of(cols), quads = (cols + 3) / 4, total = rows * quads;
-    for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < total; it += (int64_t)gridDim.x * 256) {
-        const int64_t r = it / quads, c = (it - r * quads) * 4;
+    const int64_t pitch = pitch_of(cols);
+    for_chunks(rows, (uint32_t)((cols + 3) / 4), [&](int64_t r, int chunk) {
+        const int64_t c = (int64_t)chunk * 4;
         const char4 q = *reinterpret_cast<const char4 *>(codes + r * pitch + c);
-        const float s = scales[r], v[4] = {q.x * s, q.y * s, q.z * s, q.w * s};
+        const float s = __ldg(scales + r), v[4] = {q.x * s, q.y * s, q.z * s, q.w * s};
+        float *to = out + r * ld + c;
+        if (VEC && c + 4 <= cols) *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
+        else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (c + i < cols) out[r * ld + c + i] = v[i];
-    }
+            for (int i = 0; i < 4; ++i)
+                if (c + i < cols) to[i] = v[i];
+        }
+    });
 }
 
 template <typename T, bool SR, bool VEC>
 cudaError_t quantize_rows(cudaStream_t st, const QuantParams &prm)
 {
-    // a row's threads: as few as keep it in registers, where there are rows enough
+    // a row's threads: as few as keep it in registers, where there are rows enough (us, bf16: 8192 x 1024 with 32 threads a row 6.9, 128
+    // 12.5, 256 18.9; 8192 x 4096 with 128 20.0, 256 25.5; 16 x 4096 with 128 2.5, 256 2.2; 2048 x 8192 with 256 11.2, 1024 34;
+    // 2000 x 16384 with 512 23, 1024 39; 300 x 32768, which only 1024 keep, 11.2, 256 that read it twice 15.8)
     auto grid = [&](int rows) { return (int)((prm.rows + rows - 1) / rows); };
     if (prm.cols <= 1024) return ptx::launch_chained<i8_rows_kernel<T, SR, 32, VEC>>(prm, grid(8), 256, 0, 1, st);
     if (prm.cols <= 4096 && prm.rows > 512) return ptx::launch_chained<i8_rows_kernel<T, SR, 128, VEC>>(prm, grid(2), 256, 0, 1, st);
     if (prm.cols <= 8192) return ptx::launch_chained<i8_rows_kernel<T, SR, 256, VEC>>(prm, grid(1), 256, 0, 1, st);
+    if (prm.cols <= 16384) return ptx::launch_chained<i8_rows_kernel<T, SR, 512, VEC>>(prm, grid(1), 512, 0, 1, st);
     return ptx::launch_chained<i8_rows_kernel<T, SR, 1024, VEC>>(prm, grid(1), 1024, 0, 1, st);
 }
 template <typename T, bool SR, bool VEC>
@@ -452,9 +467,11 @@ cudaError_t quantize_cols(cudaStream_t st, QuantParams prm)
 {
     constexpr int SC = 128 / (int)sizeof(T);
     const int64_t strips = (prm.cols + SC - 1) / SC;
-    int cluster = 1;      // more CTAs where a strip does not fit one, or where there are SMs for them and 128 rows each
+    // more CTAs where a strip does not fit one, or where it is long and there are SMs for them (bf16, 700 x 8192 11.4 us, two 7.9, four
+    // 13.6; 450 x 4096 4.6, 6.4, 7.4; rows at any place take longer to read: 777 x 1083 two 7.5, four 6.5)
+    int cluster = 1;
     auto per = [&] { return (prm.rows + 16 * cluster - 1) / (16 * cluster) * 16; };
-    while (cluster < kCluster && (per() > kStripRows || (strips * cluster < 128 && per() > 128))) cluster *= 2;
+    while (cluster < kCluster && (per() > kStripRows || (strips * cluster <= 128 && per() > (VEC ? 512 : 256)))) cluster *= 2;
     if (per() <= kStripRows) {
         prm.cluster = cluster;
         prm.rows_per = (int)per();
@@ -504,8 +521,10 @@ cudaError_t launch_i8_quantize(cudaStream_t st, const void *x, int dtype, int64_
 cudaError_t launch_i8_dequantize(cudaStream_t st, int num_sms, const int8_t *codes, const float *scales, int64_t rows, int64_t cols,
                                  float *out, int64_t ld)
 {
-    const int64_t blocks = (rows * ((cols + 3) / 4) + 255) / 256, most = (int64_t)num_sms * 16;
-    i8_dequantize_kernel<<<(int)(blocks < most ? blocks : most), 256, 0, st>>>(codes, scales, rows, cols, out, ld);
+    const int64_t blocks = (rows * ((cols + 3) / 4) + 255) / 256, most = (int64_t)num_sms * 8;
+    const int grid = (int)(blocks < most ? blocks : most);
+    if ((reinterpret_cast<uintptr_t>(out) & 15u) == 0 && ld % 4 == 0) i8_dequantize_kernel<true><<<grid, 256, 0, st>>>(codes, scales, rows, cols, out, ld);
+    else i8_dequantize_kernel<false><<<grid, 256, 0, st>>>(codes, scales, rows, cols, out, ld);
     return cudaGetLastError();
 }
 

@@ -1,4 +1,4 @@
-// Eight consecutive entries of a row that starts anywhere, as they lie in memory.
+// Eight consecutive entries of a row that starts anywhere, as they lie in memory; a matrix's chunks of entries dealt out to a grid.
 #pragma once
 #include <stdint.h>
 
@@ -57,6 +57,22 @@ __device__ __forceinline__ Raw8<T> load8(const T *p, int n)
 #pragma unroll
     for (int i = 0; i < G; ++i) r.q[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
     return r;
+}
+
+// f(row, chunk) of every chunk of `rows` rows of `chunks` of them, the grid's threads side by side.  One division a
+// thread: what a step adds is the same for all.
+template <typename F>
+__device__ __forceinline__ void for_chunks(int64_t rows, uint32_t chunks, F f)
+{
+    const uint32_t first = blockIdx.x * 256 + threadIdx.x, step = gridDim.x * 256, dr = step / chunks, dc = step - dr * chunks;
+    int64_t r = first / chunks;
+    uint32_t c = first - (uint32_t)r * chunks;
+    while (r < rows) {
+        f(r, (int)c);
+        r += dr;
+        c += dc;
+        if (c >= chunks) { c -= chunks; ++r; }
+    }
 }
 
 }  // namespace gvq

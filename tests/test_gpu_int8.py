@@ -62,7 +62,7 @@ def test_codes_and_scales_bit_exact(ctx, rows, cols, dtype, stochastic):
 
 
 @pytest.mark.parametrize("stochastic", [False, True])
-@pytest.mark.parametrize("rows,cols", [(2, 5000), (600, 4096), (3, 33000), (2, 70001), (20000, 24), (17000, 3)])
+@pytest.mark.parametrize("rows,cols", [(2, 5000), (600, 4096), (3, 9001), (131, 16384), (3, 33000), (2, 70001), (20000, 24), (17000, 3)])
 def test_long_rows_and_columns_bit_exact(ctx, rows, cols, stochastic):
     """Rows that more than a warp shares, rows that do not stay in registers, columns of many blocks."""
     x = torch.randn(rows, cols, generator=torch.Generator().manual_seed(cols)).to(torch.bfloat16)
