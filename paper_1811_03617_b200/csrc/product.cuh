@@ -732,7 +732,9 @@ inline int parts_of(int num_sms, int64_t tiles, int n, int least)
 inline double join_cost(int parts) { return parts > 1 ? 1.2 + 0.3 * parts : 0.0; }
 
 // Tiles: of the forms, the one with the least time in microseconds by what was measured: a tile's stages, its epilogue where that
-// takes longer than another tile's stages, and once what a launch, the pipeline's start and the last epilogue take.
+// takes longer than another tile's stages, and once what a launch, the pipeline's start and the last epilogue take.  (In 8 bits, us, with
+// 256, 128 and 64 columns: 777 x 515 x 1083 9.5, 7.7, 6.5; 512 x 4096 x 4096 16.2, 12.3, 17.4; 2048 x 8192 x 4096 47, 53, 94;
+// 8192 x 16384 x 4096 344, 424, 705; 300 x 300 x 8192 24, 17, 16, with four parts of 64 columns 9.2.)
 struct Form { int cg, bn; double stage, epilogue, once; };
 static const Form kForms[3] = {{2, 256, 0.29, 3.6, 6.2}, {2, 128, 0.21, 2.6, 4.7}, {1, 64, 0.21, 1.4, 3.8}};
 inline Cut cut_tiles(int num_sms, int64_t M, int64_t N, bool gated, int n, int halves)
@@ -797,8 +799,9 @@ inline PairCut cut_pair(int num_sms, const Extent (&e)[2])
     return best;
 }
 
-// Few tokens: the weights' rows are spread over the SMs, step rows at a time (16 tokens, 4096 -> 16384 in 8 bits: 112 rows on 147 SMs
-// 14 us, 128 rows on 128 24).  A stage takes its bytes' time or, where they are few, that of its four MMAs.
+// Few tokens: the weights' rows are spread over the SMs, step rows at a time.  A stage takes its bytes' time or, where they are few, that
+// of its four MMAs.  (In 8 bits, us: 16 x 4096 -> 16384 with 112 rows a tile 17.4, 96 21.7, 64 20.4, 32 31.9; 1 x 2048 -> 1000 with 96
+// rows 6.4, of four parts 4.8, of eight 5.2; 40 x 4096 -> 4096 with 64 rows 11.5, of two parts 9.2.)
 inline Cut cut_few(int num_sms, int64_t M, int64_t N, bool gated, int n, int step)
 {
     const int na = gated ? 2 : 1;
