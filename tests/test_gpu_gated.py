@@ -320,3 +320,45 @@ def test_a_wait_that_runs_out_is_reported_and_the_context_recovers(ctx, M, F, K)
         ctx.set_limits()
     assert torch.equal(ctx.gated_forward(x, wg, wu, h), good)
     ctx.device_status()
+
+
+# dx and the weights' gradients in one launch: an SM a tile, some with a shared contraction, pairs of SMs with 128 and 256 columns
+@pytest.mark.parametrize("M,F,K,dtype,dw,pad,opad", [
+    (150, 200, 136, "bf16", "bf16", 0, 0), (100, 2500, 90, "f16", "f32", 3, 1), (300, 520, 264, "bf16", "f16", 0, 2), (1100, 700, 700, "f16", "f16", 1, 0),
+    (1100, 704, 720, "bf16", "f32", 0, 8), (2100, 1030, 1000, "bf16", "bf16", 0, 0), (600, 600, 2101, "f16", "f32", 0, 3), (520, 1029, 2050, "bf16", "bf16", 0, 6)])
+def test_backward_in_one_launch(ctx, M, F, K, dtype, dw, pad, opad):
+    _backward(ctx, M, F, K, dtype, "gelu", pad, dw=dw, opad=opad)
+    _backward(ctx, M, F, K, dtype, "relu", pad, dw=dw, opad=opad, which=("dx", "dw_up"))
+
+
+@pytest.mark.parametrize("M,F,K", [(150, 200, 136), (300, 520, 264), (600, 600, 2104), (20, 300, 200)])
+def test_a_wait_of_the_backward_pass_that_runs_out(ctx, M, F, K):
+    from paper_1811_03617_b200 import gvq
+    x, wg, wu, dh, g, u = (torch.randn(r, c, device="cuda").bfloat16() for r, c in ((M, K), (F, K), (F, K), (M, F), (M, F), (M, F)))
+    out = {"dx": torch.empty_like(x), "dw_gate": torch.empty_like(wg), "dw_up": torch.empty_like(wu)}
+    ctx.gated_backward(dh, g, u, x, wg, wu, **out)
+    good = [t.clone() for t in out.values()]
+    ctx.set_limits(wait_cycles=2_000_000)
+    ctx.test_drop_load(True)
+    try:
+        ctx.gated_backward(dh, g, u, x, wg, wu, **out)
+        with pytest.raises(gvq.GvqError) as e:
+            ctx.device_status()
+        assert e.value.status == 9
+    finally:
+        ctx.test_drop_load(False)
+        ctx.set_limits()
+    ctx.gated_backward(dh, g, u, x, wg, wu, **out)
+    ctx.device_status()
+    for a, b in zip(good, out.values()):
+        assert torch.equal(a, b)
+
+
+# outputs whose rows start anywhere in a sector, of every width of a strip's last piece
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("hpad", [0, 1, 2, 5, 8, 16])
+def test_outputs_at_any_place(ctx, dtype, hpad):
+    for F in (1, 15, 30, 31, 47, 64, 66, 97, 129, 250):
+        _forward(ctx, 140, F, 40, dtype, "silu", hpad=hpad)
+    for F in (1029, 1040):
+        _forward(ctx, 2100, F, 24, dtype, "gelu", hpad=hpad)

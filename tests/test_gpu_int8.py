@@ -282,3 +282,23 @@ def test_a_wait_that_runs_out_is_reported_and_the_context_recovers(ctx, m, n, k)
         ctx.set_limits()
     assert torch.equal(ctx.i8_matmul(qa, qb, out), good)
     ctx.device_status()
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_outputs_at_any_place(ctx, dtype):
+    """Every offset within a sector and every width of a strip's last piece, exactly: sums of whole numbers below 2^8."""
+    t = DT[dtype]
+    for m, n in ((130, 1), (130, 2), (130, 13), (130, 31), (130, 33), (260, 63), (260, 200), (2100, 1031), (2100, 1048)):
+        k = 16
+        g = torch.Generator().manual_seed(n)
+        a, b = (torch.randint(-3, 4, (r, k), generator=g, dtype=torch.int8).cuda() for r in (m, n))
+        from paper_1811_03617_b200 import gvq
+        qa, qb = gvq.I8(m, k, a, torch.ones(m, device="cuda")), gvq.I8(n, k, b, torch.ones(n, device="cuda"))
+        want = (a.double() @ b.double().T).to(t)
+        for offset, pad in ((0, 0), (1, 0), (0, 1), (3, 2), (8, 8), (5, 16), (2, 4), (16, 7)):
+            buf = torch.full((offset + m * (n + pad) + 64,), 77.0, dtype=t, device="cuda")
+            out = torch.as_strided(buf, (m, n), (n + pad, 1), offset)
+            ctx.i8_matmul(qa, qb, out)
+            assert torch.equal(out, want), (m, n, offset, pad)
+            out.fill_(77.0)
+            assert bool((buf == 77.0).all()), (m, n, offset, pad)
