@@ -56,13 +56,17 @@ def build(force: bool = False, verbose: bool = False) -> Path:
     tmp_binding = BINDING.with_suffix(f".so.tmp{os.getpid()}")
     binding = subprocess.Popen(_binding_command(tmp_binding))
     try:
-        subprocess.run(cmd, check=True)
+        try:
+            subprocess.run(cmd, check=True)
+        finally:
+            status = binding.wait()
+        if status:
+            raise subprocess.CalledProcessError(status, binding.args)
+        os.replace(tmp, LIB)
+        os.replace(tmp_binding, BINDING)
     finally:
-        status = binding.wait()
-    if status:
-        raise subprocess.CalledProcessError(status, binding.args)
-    os.replace(tmp, LIB)
-    os.replace(tmp_binding, BINDING)
+        for path in (tmp, tmp_binding):      # (what a failure leaves)
+            path.unlink(missing_ok=True)
     return LIB
 
 

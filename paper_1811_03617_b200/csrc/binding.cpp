@@ -112,6 +112,18 @@ struct Ref {
     ~Ref() { Py_XDECREF(o); }
     PyObject *take() { return std::exchange(o, nullptr); }
 };
+// An object whose slots are these; what it held before is given up.
+void fill(PyObject *o, int64_t rows, int64_t cols, int device, PyObject *codes, PyObject *scales, PyObject *buf, const void *codes_at,
+          const void *scales_at)
+{
+    PyObject *v[kSlots] = {PyLong_FromLongLong(rows), PyLong_FromLongLong(cols), PyLong_FromLong(device), Py_NewRef(codes), Py_NewRef(scales), buf,
+                           PyLong_FromVoidPtr(const_cast<void *>(codes_at)), PyLong_FromVoidPtr(const_cast<void *>(scales_at))};
+    for (int i = 0; i < kSlots; ++i) {
+        PyObject *old = std::exchange(slot(o, i), v[i]);
+        Py_XDECREF(old);
+    }
+}
+
 // Room for a matrix, codes and scales in one allocation.
 PyObject *new_quantized(int64_t rows, int64_t cols, int device, Quantized &q)
 {
@@ -120,14 +132,7 @@ PyObject *new_quantized(int64_t rows, int64_t cols, int device, Quantized &q)
     q = {rows, cols, static_cast<int8_t *>(buf.data_ptr()), reinterpret_cast<float *>(static_cast<char *>(buf.data_ptr()) + at)};
     PyObject *o = i8_type->tp_alloc(i8_type, 0);
     if (!o) return nullptr;
-    slot(o, kRows) = PyLong_FromLongLong(rows);
-    slot(o, kCols) = PyLong_FromLongLong(cols);
-    slot(o, kDevice) = PyLong_FromLong(device);
-    slot(o, kCodes) = Py_NewRef(Py_None);
-    slot(o, kScales) = Py_NewRef(Py_None);
-    slot(o, kBuf) = THPVariable_Wrap(std::move(buf));
-    slot(o, kCodesPtr) = PyLong_FromVoidPtr(q.codes);
-    slot(o, kScalesPtr) = PyLong_FromVoidPtr(q.scales);
+    fill(o, rows, cols, device, Py_None, Py_None, THPVariable_Wrap(std::move(buf)), q.codes, q.scales);
     return o;
 }
 
@@ -172,6 +177,27 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
     Py_XINCREF(type);
     i8_type = type;
     return Py_NewRef(Py_None);
+}
+
+// i8_fill(matrix, rows, columns, codes, scales): whether the matrix is now of these codes and scales
+PyObject *i8_fill(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 5 || Py_TYPE(args[0]) != i8_type || !PyLong_CheckExact(args[1]) || !PyLong_CheckExact(args[2]) || !THPVariable_Check(args[3]) ||
+            !THPVariable_Check(args[4]))
+            return nullptr;
+        const int64_t rows = PyLong_AsLongLong(args[1]), cols = PyLong_AsLongLong(args[2]);
+        if (rows < 1 || cols < 1 || rows > INT32_MAX - 1024 || cols > INT32_MAX - 1024 || (rows + 127) / 128 >= INT32_MAX / ((cols + 127) / 128))
+            return nullptr;
+        const at::Tensor &codes = THPVariable_Unpack(args[3]), &scales = THPVariable_Unpack(args[4]);
+        for (const at::Tensor *t : {&codes, &scales})
+            if (t->layout() != at::kStrided || !t->is_cuda() || !t->is_contiguous() || t->is_neg()) return nullptr;
+        if (codes.scalar_type() != at::kChar || scales.scalar_type() != at::kFloat || codes.numel() != rows * ((cols + 15) / 16 * 16) ||
+            scales.numel() != rows || codes.get_device() != scales.get_device())
+            return nullptr;
+        fill(args[0], rows, cols, codes.get_device(), args[3], args[4], nullptr, codes.data_ptr(), scales.data_ptr());
+        return truth(true);
+    });
 }
 
 // i8_quantize(handle, device, x, by rows, by columns, stochastic, seed, node): the matrix or matrices, or None
@@ -295,9 +321,9 @@ PyMethodDef method(const char *name)
 {
     return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)), METH_FASTCALL, nullptr};
 }
-PyMethodDef methods[] = {method<bind>("bind"),           method<i8_quantize>("i8_quantize"),     method<i8_matmul>("i8_matmul"),
-                         method<i8_gated>("i8_gated"),   method<gated_forward>("gated_forward"), method<gated_backward>("gated_backward"),
-                         {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {method<bind>("bind"),           method<i8_fill>("i8_fill"),             method<i8_quantize>("i8_quantize"),
+                         method<i8_matmul>("i8_matmul"), method<i8_gated>("i8_gated"),           method<gated_forward>("gated_forward"),
+                         method<gated_backward>("gated_backward"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

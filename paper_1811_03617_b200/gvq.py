@@ -378,6 +378,8 @@ class I8:
 
     def __init__(self, rows: int, cols: int, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
                  device=None):
+        if codes is not None and _short is not None and _short.i8_fill(self, rows, cols, codes, scales):
+            return
         rows, cols = int(rows), int(cols)
         if rows < 1 or cols < 1 or rows > _MOST or cols > _MOST or ((rows + 127) >> 7) * ((cols + 127) >> 7) >= 0x7FFFFFFF:
             raise ValueError(f"no 8-bit matrix of {rows} x {cols}")

@@ -211,6 +211,9 @@ def test_both_ways_of_the_binding_give_the_same_bits(ctx, monkeypatch):
             both = ctx.i8_quantize_both(x, **kw)
             out += [t for q in (*both, ctx.i8_quantize(x, **kw), ctx.i8_quantize_transposed(x, **kw)) for t in (q.codes, q.scales)]
         q, g, u = ctx.i8_quantize(x), ctx.i8_quantize(wg), ctx.i8_quantize(wu)
+        kept = gvq.I8(g.rows, g.cols, g.codes, g.scales)
+        assert kept.codes is g.codes and kept.scales is g.scales and (kept.rows, kept.cols, kept.device) == (200, 129, 0)
+        out.append(ctx.i8_matmul(q, kept, torch.empty(70, 200, device="cuda")))
         assert (q.rows, q.cols, q.device) == (70, 129, 0) and q.codes.dtype is torch.int8 and q.codes.shape == (70, 144) and q.scales.shape == (70,)
         out.append(ctx.i8_matmul(q, g, torch.empty(70, 200, device="cuda")))
         out.append(ctx.i8_gated(q, g, u, torch.empty(70, 200, device="cuda"), act="gelu"))
@@ -246,6 +249,15 @@ def test_the_short_way_leaves_errors_to_the_long_one(ctx):
     assert not s.gated_backward(h, 0, bf, bf, bf, bf, bf, bf, 0, None, None, None)
     assert not s.gated_backward(h, 0, bf, bf, bf, None, bf, bf, 0, None, x, None) and not s.gated_backward(h, 0, bf, bf, bf, bf, None, bf, 0, bf, None, None)
     assert not s.gated_backward(h, 0, bf, bf, bf, bf, bf, bf, 0, None, x, bf) and not s.gated_backward(h, 0, bf, bf, bf, bf, bf, bf, 9, bf, None, None)
+    c, w = torch.zeros(64, 64, dtype=torch.int8, device="cuda"), torch.ones(64, device="cuda")
+    for args in ((q, 64, 64, c, w[:32]), (q, 64, 64, c.t(), w[::2]), (q, 64, 60, c.cpu(), w), (q, 64, 64, c.byte(), w), (q, 64, 64, c, w.double()), (q, 0, 64, c, w),
+                 (q, 64, 1 << 40, c, w), (q, 64.0, 64, c, w), (q, 64, 64, c, None), (object(), 64, 64, c, w), (q, 64, 80, c, w)):
+        assert not s.i8_fill(*args)
+    assert q.codes is not c and s.i8_fill(q, 64, 64, c, w) and q.codes is c and q.scales is w
+    for args in ((64, 64, c, w[:32]), (64, 64, c, None), (64, 80, c, w), (64, 64, c.byte(), w)):
+        with pytest.raises(ValueError):
+            gvq.I8(*args)
+    assert gvq.I8(64.0, 64, c, w).rows == 64
     ctx.device_status()
     with pytest.raises(ValueError):
         ctx.i8_matmul(q, gvq.I8(64, 32), x)
