@@ -2,12 +2,13 @@
 //
 //  i8_rows_kernel     along the rows, read once: a row stays in the registers of the threads that share it
 //  i8_strip_kernel    along the columns, read once: a strip of columns stays in the shared memory of a cluster
+//  i8_both_kernel     both of these in one launch
 //  i8_max_kernel, i8_tile_kernel   along columns too long for that: largest magnitudes first, then tile by tile
 //  i8_dequantize_kernel
 //
 // Measured, from memory, in us (the bytes at the copy rate): rows of 8192 x 4096 bf16 20.0 nearest, 28 stochastic (15.4), fp32 28 and 32
 // (25.7); columns of 2048 x 4096 bf16 in strips 9.9 and 12.6 (3.8); columns of 8192 x 4096 bf16, read twice, 30 and 41 (15.4), fp32
-// 60 and 70 (25.7); 777 x 1083 rows 3.3, columns 6.5 (0.4).  Of large ones instructions take as long as memory: of the nearest codes
+// 60 and 70 (25.7); 777 x 1083 rows 3.3, columns 6.5, both 8.1 (0.4).  Of large ones instructions take as long as memory: of the nearest codes
 // the conversions, maxima and packing, of the stochastic ones the random words, 10 integer instructions for two entries.  Small ones
 // are a launch and the way to memory and back.
 //
@@ -27,6 +28,10 @@ constexpr float kMagic = 12582912.0f;               // 1.5 * 2^23: its pattern's
 constexpr int kMaxRows = 512;      // of a CTA of i8_max_kernel
 // i8_strip_kernel: CTAs of a cluster, threads, words from row to row, most rows of a CTA (106 KB of shared memory: two CTAs an SM)
 constexpr int kCluster = 4, kStripThreads = 512, kStripPitch = 36, kStripRows = 752;
+// i8_both_kernel: up to so many CTAs one at a time has an SM (us, bf16, one, two, a launch each: 512 x 4096, 192 CTAs, 5.2, 6.0, 9.2; 2048 x
+// 1024, 192, 6.2, 7.9, 10.2; 777 x 1083, 263, 8.1, 9.9, 9.2; 1000 x 4096, 378, 11.3, 9.2, 12.1; 2048 x 2048, 640, 14.3, 9.7, 13.2), and
+// so many are made in one launch at all (2048 x 4096, 768, 22.3, 15.1, 15.1; 1000 x 8192, 1256, 24.2, 16.4, 14.3).
+constexpr int64_t kFewBlocks = 296, kBothBlocks = 768;
 
 __host__ __device__ inline int64_t pitch_of(int64_t cols) { return (cols + 15) / 16 * 16; }
 inline int64_t row_blocks(int64_t rows) { return (rows + kMaxRows - 1) / kMaxRows; }
@@ -100,22 +105,21 @@ struct QuantParams {
     uint64_t seed_w;            // mix64 of (seed, node)
     int8_t *codes, *codes_t;    // along the rows, along the columns; null: not wanted
     float *scales, *scales_t;
-    int cluster, rows_per;      // of i8_strip_kernel: CTAs that share a strip, rows of a CTA (a multiple of 16)
+    int cluster, rows_per;      // of strips: CTAs that share one, rows of a CTA (a multiple of 16)
+    int strip_blocks;           // of i8_both_kernel: CTAs for strips
     uint32_t *col_top;          // [row_blocks][cols]: patterns of magnitudes
     int row_blocks;             // CTAs along the rows of i8_max_kernel
     int ct;                     // tiles along the columns
 };
 
-// G threads share a row, KEEP groups of eight entries a thread in registers; longer rows are read again from L2.
-template <typename T, bool SR, int G, bool VEC>
-__global__ void __launch_bounds__(G < 256 ? 256 : G) i8_rows_kernel(const QuantParams prm)
+// A CTA of NT threads: G of them share a row, KEEP groups of eight entries a thread in registers; longer rows are read again from L2.
+template <typename T, bool SR, int G, int NT, bool VEC>
+__device__ __forceinline__ void quantize_rows_of(const QuantParams &prm, uint32_t block)
 {
-    constexpr int KEEP = 4, NT = G < 256 ? 256 : G, ROWS = NT / G;
+    constexpr int KEEP = 4, ROWS = NT / G;
     __shared__ uint32_t tops[NT / 32];
-    ptx::launch_dependents();
-    ptx::grid_dependency_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, in_row = threadIdx.x % G;
-    const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / G;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, in_row = ROWS == 1 ? threadIdx.x : threadIdx.x % G;
+    const int64_t row = (int64_t)block * ROWS + (ROWS == 1 ? 0 : threadIdx.x / G);
     const bool there = row < prm.rows;
     const T *x = static_cast<const T *>(prm.x) + (there ? row : 0) * prm.ld;
     const int64_t pitch = pitch_of(prm.cols), groups = there ? pitch / 8 : 0;
@@ -138,7 +142,7 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G) i8_rows_kernel(const QuantP
         constexpr int WARPS = G / 32;
         top = 0;
 #pragma unroll
-        for (int i = 0; i < WARPS; ++i) top = max(top, tops[warp / WARPS * WARPS + i]);
+        for (int i = 0; i < WARPS; ++i) top = max(top, tops[(ROWS == 1 ? 0 : warp / WARPS * WARPS) + i]);
     }
     const RowScale s = row_scale(top);
     const bool fine = top < 0x7F800000u;
@@ -154,6 +158,13 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G) i8_rows_kernel(const QuantP
         if (in_row + i * G < groups) write(in_row + i * G, kept[i]);
     for (int64_t at = in_row + KEEP * G; at < groups; at += G) write(at, load(at));
     if (there && in_row == 0) prm.scales[row] = s.scale;
+}
+template <typename T, bool SR, int G, bool VEC>
+__global__ void __launch_bounds__(G < 256 ? 256 : G) i8_rows_kernel(const QuantParams prm)
+{
+    ptx::launch_dependents();
+    ptx::grid_dependency_wait();
+    quantize_rows_of<T, SR, G, (G < 256 ? 256 : G), VEC>(prm, blockIdx.x);
 }
 
 // Largest magnitudes of eight columns over rows, as patterns: kept as they come, two columns of a 16-bit type a word.
@@ -228,7 +239,7 @@ __device__ __forceinline__ void column_run(const QuantParams &prm, const uint32_
 // they are long and another 4 words on every 16 rows, so that eight lanes' 16-byte words, and the words of 4 columns in 8 runs of 16
 // rows, lie in different banks.
 template <typename T, bool SR, bool VEC>
-__global__ void __launch_bounds__(kStripThreads) i8_strip_kernel(const QuantParams prm)
+__device__ __forceinline__ void quantize_strip(const QuantParams &prm, uint32_t block)
 {
     constexpr int SC = 128 / (int)sizeof(T), L = SC / 8, RP = kStripThreads / L, WARPS = kStripThreads / 32;   // columns, lanes a row, rows a pass
     extern __shared__ uint4 smem_q[];
@@ -236,10 +247,8 @@ __global__ void __launch_bounds__(kStripThreads) i8_strip_kernel(const QuantPara
     __shared__ uint32_t tops[WARPS][SC], of_cta[SC];
     __shared__ RowScale of_col[SC];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    ptx::launch_dependents();
-    ptx::grid_dependency_wait();
-    const int cluster = prm.cluster, rank = blockIdx.x % cluster;
-    const int64_t c0 = (int64_t)(blockIdx.x / cluster) * SC, r0 = (int64_t)rank * prm.rows_per;
+    const int cluster = prm.cluster, rank = block % cluster;
+    const int64_t c0 = (int64_t)(block / cluster) * SC, r0 = (int64_t)rank * prm.rows_per;
     const T *x = static_cast<const T *>(prm.x);
     auto at = [&](int row) { return tile + row * kStripPitch + (row >> 4) * 4; };
 
@@ -308,6 +317,26 @@ __global__ void __launch_bounds__(kStripThreads) i8_strip_kernel(const QuantPara
         }
     }
     if (cluster > 1) ptx::cluster_sync();      // (its neighbours have read this CTA's maxima)
+}
+template <typename T, bool SR, bool VEC>
+__global__ void __launch_bounds__(kStripThreads) i8_strip_kernel(const QuantParams prm)
+{
+    ptx::launch_dependents();
+    ptx::grid_dependency_wait();
+    quantize_strip<T, SR, VEC>(prm, blockIdx.x);
+}
+// Both in one launch, which a small matrix waits for as long as for its data: the strips first, rows on CTAs of the same size.  AT_ONCE:
+// CTAs of an SM; two have 64 registers a thread and spill some.
+template <typename T, bool SR, bool VEC, int AT_ONCE>
+__global__ void __launch_bounds__(kStripThreads, AT_ONCE) i8_both_kernel(const QuantParams prm)
+{
+    ptx::launch_dependents();
+    ptx::grid_dependency_wait();
+    const int block = (int)blockIdx.x - prm.strip_blocks;
+    if (block < 0) quantize_strip<T, SR, VEC>(prm, blockIdx.x);
+    else if (prm.cols <= 1024) quantize_rows_of<T, SR, 32, kStripThreads, VEC>(prm, block);
+    else if (prm.cols <= 4096) quantize_rows_of<T, SR, 128, kStripThreads, VEC>(prm, block);
+    else quantize_rows_of<T, SR, kStripThreads, kStripThreads, VEC>(prm, block);
 }
 
 // A CTA: kMaxRows rows of a strip of 128 bytes.
@@ -462,8 +491,9 @@ cudaError_t quantize_rows(cudaStream_t st, const QuantParams &prm)
     if (prm.cols <= 16384) return ptx::launch_chained<i8_rows_kernel<T, SR, 512, VEC>>(prm, grid(1), 512, 0, 1, st);
     return ptx::launch_chained<i8_rows_kernel<T, SR, 1024, VEC>>(prm, grid(1), 1024, 0, 1, st);
 }
-template <typename T, bool SR, bool VEC>
-cudaError_t quantize_cols(cudaStream_t st, QuantParams prm)
+// Sets how a matrix's columns are quantized in strips, whether they are.
+template <typename T, bool VEC>
+bool cut_strips(QuantParams &prm)
 {
     constexpr int SC = 128 / (int)sizeof(T);
     const int64_t strips = (prm.cols + SC - 1) / SC;
@@ -472,28 +502,51 @@ cudaError_t quantize_cols(cudaStream_t st, QuantParams prm)
     int cluster = 1;
     auto per = [&] { return (prm.rows + 16 * cluster - 1) / (16 * cluster) * 16; };
     while (cluster < kCluster && (per() > kStripRows || (strips * cluster <= 128 && per() > (VEC ? 512 : 256)))) cluster *= 2;
-    if (per() <= kStripRows) {
-        prm.cluster = cluster;
-        prm.rows_per = (int)per();
-        const size_t smem = (size_t)(prm.rows_per * kStripPitch + prm.rows_per / 16 * 4) * 4;
-        return ptx::launch_chained<i8_strip_kernel<T, SR, VEC>>(prm, (int)(strips * cluster), kStripThreads, smem, cluster, st);
-    }
-    const cudaError_t e = ptx::launch_chained<i8_max_kernel<T, VEC>>(prm, (int)(prm.row_blocks * strips), 256, 0, 1, st);
+    if (per() > kStripRows) return false;
+    prm.cluster = cluster;
+    prm.rows_per = (int)per();
+    prm.strip_blocks = (int)(strips * cluster);
+    return true;
+}
+inline size_t strip_smem(const QuantParams &prm) { return (size_t)(prm.rows_per * kStripPitch + prm.rows_per / 16 * 4) * 4; }
+
+template <typename T, bool SR, bool VEC>
+cudaError_t quantize_cols(cudaStream_t st, QuantParams prm)
+{
+    constexpr int SC = 128 / (int)sizeof(T);
+    if (cut_strips<T, VEC>(prm))
+        return ptx::launch_chained<i8_strip_kernel<T, SR, VEC>>(prm, prm.strip_blocks, kStripThreads, strip_smem(prm), prm.cluster, st);
+    const cudaError_t e = ptx::launch_chained<i8_max_kernel<T, VEC>>(prm, (int)(prm.row_blocks * ((prm.cols + SC - 1) / SC)), 256, 0, 1, st);
     if (e != cudaSuccess) return e;
     const int tiles = (int)(mx4::tiles_of(pitch_of(prm.rows), 128) * prm.ct);
     const size_t smem = (128 * (128 * sizeof(T) / 4 + 4) + 32) * 4;
     return ptx::launch_chained<i8_tile_kernel<T, SR, VEC>>(prm, tiles, 256, smem, 1, st);
 }
 
+template <typename T, bool SR, bool VEC>
+cudaError_t quantize_as(cudaStream_t st, QuantParams prm)
+{
+    if (prm.codes && prm.codes_t && cut_strips<T, VEC>(prm)) {
+        const int rows = prm.cols <= 1024 ? kStripThreads / 32 : prm.cols <= 4096 ? kStripThreads / 128 : 1;      // of a CTA
+        const int64_t blocks = prm.strip_blocks + (prm.rows + rows - 1) / rows;
+        if (blocks <= kBothBlocks) {
+            const int grid = (int)((blocks + prm.cluster - 1) / prm.cluster * prm.cluster);
+            if (blocks <= kFewBlocks)
+                return ptx::launch_chained<i8_both_kernel<T, SR, VEC, 1>>(prm, grid, kStripThreads, strip_smem(prm), prm.cluster, st);
+            return ptx::launch_chained<i8_both_kernel<T, SR, VEC, 2>>(prm, grid, kStripThreads, strip_smem(prm), prm.cluster, st);
+        }
+    }
+    if (prm.codes) {
+        const cudaError_t e = quantize_rows<T, SR, VEC>(st, prm);
+        if (e != cudaSuccess) return e;
+    }
+    return prm.codes_t ? quantize_cols<T, SR, VEC>(st, prm) : cudaSuccess;
+}
+
 template <typename T, bool SR>
 cudaError_t quantize_as(cudaStream_t st, const QuantParams &prm, bool vec)
 {
-    if (prm.codes) {
-        const cudaError_t e = vec ? quantize_rows<T, SR, true>(st, prm) : quantize_rows<T, SR, false>(st, prm);
-        if (e != cudaSuccess) return e;
-    }
-    if (!prm.codes_t) return cudaSuccess;
-    return vec ? quantize_cols<T, SR, true>(st, prm) : quantize_cols<T, SR, false>(st, prm);
+    return vec ? quantize_as<T, SR, true>(st, prm) : quantize_as<T, SR, false>(st, prm);
 }
 
 }  // namespace

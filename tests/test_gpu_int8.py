@@ -41,7 +41,7 @@ def _check(q, x, stochastic=False, seed=0, node=0):
     assert torch.equal(q.codes.cpu(), codes)
 
 
-SIZES = [(1, 1), (1, 15), (3, 16), (7, 64), (128, 128), (129, 130), (33, 515), (260, 77), (9, 1024), (10, 1040), (520, 2100)]
+SIZES = [(1, 1), (1, 15), (3, 16), (7, 64), (128, 128), (129, 130), (33, 515), (260, 77), (9, 1024), (10, 1040), (520, 2100), (1000, 4095), (2500, 1001)]
 
 
 @pytest.mark.parametrize("stochastic", [False, True])
