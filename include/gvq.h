@@ -591,7 +591,8 @@ gvq_status gvq_gated_forward(gvq_ctx *ctx, const void *x, int64_t ldx, const voi
                              int dtype, int64_t M, int64_t F, int64_t K, int activation, void *h, int64_t ldh, void *gate_opt,
                              int64_t ld_gate_out, void *up_opt, int64_t ld_up_out, void *workspace, size_t workspace_bytes);
 /* Gradients from dh and what the forward pass kept:
-     dg = dh * u * act'(g),  du = dh * act(g)            (rounded to dtype: they are operands of the products below)
+     dg = dh * u * act'(g),  du = dh * act(g)            (rounded to dtype: they are operands of the products below; up to
+                                                         M * F * K = 2^26 what the rounding left is multiplied too)
      dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x     (fp32 sums, rounded once)
    dx_opt: [M][K]; dw_gate_opt, dw_up_opt: [F][K] of type dw_dtype (GVQ_F32: views of a flat gradient).  Any of the three may be
    NULL, not all; w_gate and w_up are read for dx only, x for the weights' gradients only.  Gradients are overwritten. */

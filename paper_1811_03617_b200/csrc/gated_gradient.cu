@@ -4,6 +4,8 @@
 //   dWg = dg^T x,  dWu = du^T x                    one product of two halves that have x in common
 // in one launch for the slopes and one or two for the products,
 // and the copies of operands whose rows do not start at 16-byte boundaries, which TMA cannot address.
+#include <float.h>
+
 #include "load8.cuh"
 #include "product.cuh"
 
@@ -32,7 +34,7 @@ __global__ void __launch_bounds__(256) align_rows_kernel(const __grid_constant__
 struct SlopeParams {
     const void *dh, *g, *u;
     int64_t ld_dh, ld_g, ld_u;
-    void *dg, *du;             // rows ld_out entries apart, starting at 16-byte boundaries
+    void *d[4];                // dg, du and what rounding them left (or null); rows ld_out entries apart, starting at 16-byte boundaries
     int64_t rows, cols, ld_out;
     int chunks;                // groups of eight columns of a row
     RowCopies copies;          // done on the way: the products after this launch read them
@@ -62,16 +64,31 @@ __global__ void __launch_bounds__(256, kResident) gated_slopes_kernel(const __gr
         load_eight<T, VEC>(prm.dh, r * prm.ld_dh + c, n, dh);
         load_eight<T, VEC>(prm.g, r * prm.ld_g + c, n, g);
         load_eight<T, VEC>(prm.u, r * prm.ld_u + c, n, u);
-        uint32_t dg[4], du[4];
+        float d[2][8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 a = activation_and_slope<ACT>(g[2 * i]), b = activation_and_slope<ACT>(g[2 * i + 1]);
-            dg[i] = pack2<T>(dh[2 * i] * u[2 * i] * a.y, dh[2 * i + 1] * u[2 * i + 1] * b.y);
-            du[i] = pack2<T>(dh[2 * i] * a.x, dh[2 * i + 1] * b.x);
+        for (int i = 0; i < 8; ++i) {
+            const float2 a = activation_and_slope<ACT>(g[i]);
+            d[0][i] = dh[i] * u[i] * a.y;
+            d[1][i] = dh[i] * a.x;
         }
         const int64_t at = r * prm.ld_out + c;      // (rows are padded to eight entries)
-        *reinterpret_cast<uint4 *>(static_cast<T *>(prm.dg) + at) = make_uint4(dg[0], dg[1], dg[2], dg[3]);
-        *reinterpret_cast<uint4 *>(static_cast<T *>(prm.du) + at) = make_uint4(du[0], du[1], du[2], du[3]);
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = pack2<T>(d[which][2 * i], d[which][2 * i + 1]);
+            *reinterpret_cast<uint4 *>(static_cast<T *>(prm.d[which]) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+            if (prm.d[2]) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    T e[2];
+                    memcpy(e, &w[i], 4);
+                    auto rest = [](float x, float of) { return fabsf(x - of) <= FLT_MAX ? x - of : 0.0f; };      // (none of an infinity or a NaN)
+                    w[i] = pack2<T>(rest(d[which][2 * i], to_f(e[0])), rest(d[which][2 * i + 1], to_f(e[1])));
+                }
+                *reinterpret_cast<uint4 *>(static_cast<T *>(prm.d[2 + which]) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
     });
     copy_rows(prm.copies);
 }
@@ -122,10 +139,10 @@ cudaError_t launch_align_rows(const Launch &l, const RowCopies &copies)
 }
 
 cudaError_t launch_gated_slopes(const Launch &l, const void *dh, int64_t ld_dh, const void *g, int64_t ld_g, const void *u, int64_t ld_u,
-                                int dtype, int64_t rows, int64_t cols, int act, void *dg, void *du, int64_t ld_out, const RowCopies &copies)
+                                int dtype, int64_t rows, int64_t cols, int act, void *const (&d)[4], int64_t ld_out, const RowCopies &copies)
 {
     auto aligned = [](const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % 8 == 0; };
-    const SlopeParams prm = {dh, g, u, ld_dh, ld_g, ld_u, dg, du, rows, cols, ld_out, (int)((cols + 7) / 8), copies};
+    const SlopeParams prm = {dh, g, u, ld_dh, ld_g, ld_u, {d[0], d[1], d[2], d[3]}, rows, cols, ld_out, (int)((cols + 7) / 8), copies};
     if (aligned(dh, ld_dh) && aligned(g, ld_g) && aligned(u, ld_u))      // all rows start at 16-byte boundaries
         return dtype == GVQ_BF16 ? launch_slopes_as<__nv_bfloat16, true>(l, prm, act) : launch_slopes_as<__half, true>(l, prm, act);
     return dtype == GVQ_BF16 ? launch_slopes_as<__nv_bfloat16, false>(l, prm, act) : launch_slopes_as<__half, false>(l, prm, act);
@@ -133,39 +150,49 @@ cudaError_t launch_gated_slopes(const Launch &l, const void *dh, int64_t ld_dh, 
 
 namespace {
 
-// dx = dg Wg + du Wu: a contraction of two segments.  The weights are MN-major here: boxes of 64 of a row's entries by 64 rows.
+// Halves that dg and du have: one, or two where what rounding left of them is multiplied too.
+int precise(const GatedGrads &g) { return g.d[2] ? 2 : 1; }
+// dx = dg Wg + du Wu: a contraction of two segments (four).  The weights are MN-major here: boxes of 64 of a row's entries by 64 rows.
 bool dx_problem(Params &prm, const Launch &l, const Cut &c, const GatedGrads &g)
 {
     prm = start(l, g.dtype, g.dtype);
     prm.M = c.few ? g.K : g.M;
     prm.N = c.few ? g.M : g.K;
-    divide(prm, c, k16, false, g.F, 2, 1);
+    const int segments = 2 * precise(g);
+    divide(prm, c, k16, false, g.F, segments, 1);
     CUtensorMap *map_w = c.few ? prm.a : prm.b, *map_d = c.few ? prm.b : prm.a;
     const int box_d = c.few ? c.bn : 128;
     set_output(prm, 0, g.dx, g.dtype, g.ld_dx);
-    return encode(l.encode, map_w, k16, g.w[0], g.F, g.K, g.ld_w[0], 64) && encode(l.encode, map_w + 1, k16, g.w[1], g.F, g.K, g.ld_w[1], 64) &&
-           encode(l.encode, map_d, k16, g.d[0], g.M, g.F, g.ld_d, box_d) && encode(l.encode, map_d + 1, k16, g.d[1], g.M, g.F, g.ld_d, box_d);
+    bool ok = true;
+    for (int i = 0; i < segments; ++i) {
+        ok = ok && encode(l.encode, map_d + i, k16, g.d[i], g.M, g.F, g.ld_d, box_d);
+        if (i < 2) ok = ok && encode(l.encode, map_w + i, k16, g.w[i], g.F, g.K, g.ld_w[i], 64);
+        else map_w[i] = map_w[i - 2];
+    }
+    return ok;
 }
 // dWg = dg^T x, dWu = du^T x, or the one of them that is wanted: two halves of a product, both operands MN-major.
 int halves_of(const GatedGrads &g) { return g.dw[0] && g.dw[1] ? 2 : 1; }
 bool dw_problem(Params &prm, const Launch &l, const Cut &c, const GatedGrads &g)
 {
-    const int halves = halves_of(g);
+    const int halves = halves_of(g), segments = precise(g);
     prm = start(l, g.dtype, g.dw_dtype);
     prm.M = g.F;
     prm.N = g.K;
     prm.a_mn = 1;
-    divide(prm, c, k16, false, g.M, 1, halves);
+    divide(prm, c, k16, false, g.M, segments, halves);
     bool ok = encode(l.encode, &prm.b[0], k16, g.x, g.M, g.K, g.ldx, 64);
+    prm.b[1] = prm.b[0];
     for (int i = 0; i < halves; ++i) {
         const int which = g.dw[0] ? i : 1;
-        ok = ok && encode(l.encode, &prm.a[i], k16, g.d[which], g.M, g.F, g.ld_d, 64);
+        for (int seg = 0; seg < segments; ++seg)
+            ok = ok && encode(l.encode, &prm.a[i * segments + seg], k16, g.d[2 * seg + which], g.M, g.F, g.ld_d, 64);
         set_output(prm, i, g.dw[which], g.dw_dtype, g.ld_dw[which]);
     }
     return ok;
 }
-Cut cut_dx(const Launch &l, const GatedGrads &g) { return cut(l.num_sms, g.M, g.K, false, 2 * stages_of(g.F, k16), 64); }
-Cut cut_dw(const Launch &l, const GatedGrads &g) { return cut_tiles(l.num_sms, g.F, g.K, false, stages_of(g.M, k16), halves_of(g)); }
+Cut cut_dx(const Launch &l, const GatedGrads &g) { return cut(l.num_sms, g.M, g.K, false, 2 * precise(g) * stages_of(g.F, k16), 64); }
+Cut cut_dw(const Launch &l, const GatedGrads &g) { return cut_tiles(l.num_sms, g.F, g.K, false, precise(g) * stages_of(g.M, k16), halves_of(g)); }
 
 cudaError_t launch_dx(const Launch &l, const Cut &c, const GatedGrads &g)
 {
@@ -207,7 +234,7 @@ cudaError_t launch_gated_products(const Launch &l, const GatedGrads &g)
     if (g.dx) cx = cut_dx(l, g);
     if (dw) cw = cut_dw(l, g);
     if (g.dx && dw && !cx.few) {
-        const Extent e[2] = {{g.M, g.K, 2 * stages_of(g.F, k16), 1}, {g.F, g.K, stages_of(g.M, k16), halves_of(g)}};
+        const Extent e[2] = {{g.M, g.K, 2 * precise(g) * stages_of(g.F, k16), 1}, {g.F, g.K, precise(g) * stages_of(g.M, k16), halves_of(g)}};
         const PairCut c = cut_pair(l.num_sms, e);
         // (the second of two launches starts while the first ends)
         if (c.time && c.time < 0.98 * (cx.time + cw.time - 1.5)) {

@@ -203,11 +203,12 @@ struct RowCopies {
     int chunks[3];
 };
 cudaError_t launch_align_rows(const Launch &l, const RowCopies &copies);
+// d: dg and du, and what rounding them left (null: not wanted).
 cudaError_t launch_gated_slopes(const Launch &l, const void *dh, int64_t ld_dh, const void *g, int64_t ld_g, const void *u, int64_t ld_u,
-                                int dtype, int64_t rows, int64_t cols, int act, void *dg, void *du, int64_t ld_out, const RowCopies &copies);
-// The products of a backward pass.  d, w, dw: the gate's and the other projection's; dx or dw null: not wanted.
+                                int dtype, int64_t rows, int64_t cols, int act, void *const (&d)[4], int64_t ld_out, const RowCopies &copies);
+// The products of a backward pass.  w, dw: the gate's and the other projection's; d: as above; dx or dw null: not wanted.
 struct GatedGrads {
-    const void *d[2], *w[2], *x;
+    const void *d[4], *w[2], *x;
     int64_t ld_d, ld_w[2], ldx;
     int dtype, dw_dtype;
     int64_t M, F, K;

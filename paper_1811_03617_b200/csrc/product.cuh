@@ -49,11 +49,12 @@ constexpr uint32_t A_BYTES = 128 * 128;
 enum { k16 = 0, kI8 = 1 };             // kinds of operands
 
 struct Params {
-    CUtensorMap a[2], b[2];            // see the producer
+    CUtensorMap a[4], b[4];            // see the producer
     int64_t M, N;                      // rows of A (of one half), rows of B, as far as there are outputs
     int tiles_m, tiles_n;              // tiles_m: of both halves
     int half_tiles;                    // tiles_m of one half: two products with B in common are one, A's and the outputs' halves apart
-    int n_stages, seg_stages, n_last;  // stages of a tile's contraction, of its first segment; MMAs of a segment's last stage
+    int n_stages, seg_stages, segments;     // stages of a tile's contraction, of one of its segments (all alike), segments
+    int n_last;                        // MMAs of a segment's last stage
     int parts;                         // CTAs (a cluster) that share a tile's contraction; with more than one, a tile a cluster
     int group;                         // tiles along M that are gone through before the next along N
     int rows_a, stages;                // FEW: rows of a matrix that a tile has (a multiple of 8); stages that there is room for
@@ -253,6 +254,12 @@ __device__ __forceinline__ void place(const Params &prm, int tile, int &tm, int 
     tm = g * prm.group + r - tn * m;
 }
 
+// The segment of a stage.
+__device__ __forceinline__ int segment_of(const Params &prm, int st)
+{
+    return (st >= prm.seg_stages) + (st >= 2 * prm.seg_stages) + (st >= 3 * prm.seg_stages);
+}
+
 // Sums that lie in the shared memory of the P CTAs of a cluster (of this one): added up, four columns of a row a thread at a time, the
 // parts in order, and then what the epilogue does with them.  Lanes lie along what is contiguous in the output.  tid: this thread's
 // place among the `threads` that do this in each CTA, whole warps.
@@ -385,7 +392,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
             int tm, tn;
             place(prm, first, tm, tn);
             for (int st = st0; st < min(st1, st0 + (int)n_stage); ++st) {
-                const int seg = st >= prm.seg_stages, k = (st - seg * prm.seg_stages) * KS, m0 = tm * prm.rows_a;
+                const int seg = segment_of(prm, st), k = (st - seg * prm.seg_stages) * KS, m0 = tm * prm.rows_a;
                 prefetch_2d(prm.a + seg, A_MN ? m0 : k, A_MN ? k : m0);
                 if (A_MN && a_bytes > kBox) prefetch_2d(prm.a + seg, m0 + 64, k);
                 if (GATED) prefetch_2d(prm.a + 1, k, m0);
@@ -411,8 +418,9 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
                     if (!mbar_poll(empty + s, phase, abort_flag)) { failed = true; break; }
                     const bool drop = prm.test_drop && blockIdx.x == 0 && c == 0;   // test hook: this stage never arrives
                     if (!drop) {
-                        // a contraction of two segments has a map of either operand for each; two halves one of A
-                        const int seg = st >= prm.seg_stages;
+                        // a contraction of segments has a map of either operand for each; two halves have their own of A
+                        const int seg = segment_of(prm, st);
+                        const CUtensorMap *map_a = prm.a + half * prm.segments + seg;
                         const int k = (st - seg * prm.seg_stages) * KS;
                         unsigned char *dst = smem + s * stage_bytes, *dst_b = dst + stage_bytes - S::B_BYTES;
                         if (rank == 0) mbar_arrive_expect_tx(full + s, CG * stage_bytes);
@@ -421,8 +429,8 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
                             if (CG == 2) tma_load_2d_pair(to, map, mn ? at : k, mn ? k : at, bar);
                             else tma_load_2d(to, map, mn ? at : k, mn ? k : at, full + s);
                         };
-                        load(dst, prm.a + half + seg, a_mn, m0);
-                        if (a_mn && (!FEW || a_bytes > kBox)) load(dst + kBox, prm.a + half + seg, true, m0 + 64);
+                        load(dst, map_a, a_mn, m0);
+                        if (a_mn && (!FEW || a_bytes > kBox)) load(dst + kBox, map_a, true, m0 + 64);
                         if (FEW && GATED) load(dst + a_bytes, prm.a + 1, false, m0);
                         if constexpr (SIDE && CG == 2) load(dst_b, prm.b + rank, false, n0);
                         else if constexpr (SIDE) {
@@ -461,6 +469,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
                     if (!mbar_poll(d_empty + buf, ((t >> 1) - 1) & 1, abort_flag)) { failed = true; break; }
                     tc_fence_after();
                 }
+                int left = prm.seg_stages - (st0 - segment_of(prm, st0) * prm.seg_stages);      // stages of the segment
                 for (int st = st0; st < st1; ++st) {
                     if (!mbar_poll(full + s, phase, abort_flag)) { failed = true; break; }
                     tc_fence_after();
@@ -473,7 +482,10 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
                                 else tc_mma_f16<CG>(d, da + k * IA, db + k * IB, idesc, st > st0 || k > 0);
                             }
                     };
-                    if (prm.n_last < 4 && (st == prm.n_stages - 1 || st == prm.seg_stages - 1)) issue(prm.n_last); else issue(4);
+                    if (--left == 0) {
+                        left = prm.seg_stages;
+                        issue(prm.n_last);
+                    } else issue(4);
                     if (CG == 2) tc_commit_pair(empty + s); else tc_commit(empty + s);
                     if (st == st1 - 1) { if (CG == 2) tc_commit_pair(d_full + buf); else tc_commit(d_full + buf); }
                     if (++s == n_stage) { s = 0; phase ^= 1; }
@@ -838,6 +850,7 @@ inline void divide(Params &prm, const Cut &c, int kind, bool gated, int64_t K, i
     prm.tiles_m = prm.half_tiles * halves;
     prm.tiles_n = tiles_of(prm.N, gated && !c.few ? c.bn / 2 : c.bn);
     prm.seg_stages = tiles_of(K, ks);
+    prm.segments = segments;
     prm.n_stages = prm.seg_stages * segments;
     prm.n_last = (int)((K - (int64_t)(prm.seg_stages - 1) * ks + ks / 4 - 1) / (ks / 4));
     prm.group = prm.tiles_m < 8 ? prm.tiles_m : 8;

@@ -362,3 +362,34 @@ def test_outputs_at_any_place(ctx, dtype, hpad):
         _forward(ctx, 140, F, 40, dtype, "silu", hpad=hpad)
     for F in (1029, 1040):
         _forward(ctx, 2100, F, 24, dtype, "gelu", hpad=hpad)
+
+
+@pytest.mark.parametrize("M,F,K,dtype,name", [
+    (1, 40, 24, "bf16", "silu"), (20, 300, 130, "f16", "gelu"), (64, 200, 700, "bf16", "relu"), (90, 50, 46, "f16", "silu"), (300, 333, 165, "bf16", "gelu_tanh"),
+    (1400, 50, 46, "f16", "gelu"), (400, 600, 250, "bf16", "sigmoid"), (250, 2100, 100, "f16", "relu")])
+def test_short_products_do_not_round_the_slopes(ctx, M, F, K, dtype, name):
+    """Up to 2^26 multiply-adds dg and du are two halves each: what is off by half a step of dtype above is off by half a step of half
+    a step, and with fp16 by no more than half its smallest step."""
+    t = DT[dtype]
+    g = torch.Generator(device="cuda").manual_seed(M + F + K)
+    x, wg, wu = (_rows(g, r, K, t, 0, s) for r, s in ((M, 1.0), (F, 1 / math.sqrt(K)), (F, 1 / math.sqrt(K))))
+    gate, up, dh = (_rows(g, M, F, t, 0) for _ in range(3))
+    out = {"dx": torch.empty(M, K, device="cuda", dtype=t), "dw_gate": torch.empty(F, K, device="cuda"), "dw_up": torch.empty(F, K, device="cuda")}
+    ctx.gated_backward(dh, gate, up, x, wg, wu, act=name, **out)
+    ctx.device_status()
+    a, slope = act(name, gate.double())
+    dg, du = dh.double() * up.double() * slope, dh.double() * a
+    eg = (dh.double() * up.double()).abs() * 2.0 ** -19 * (1 + gate.double().abs()) + dg.abs() * HALF[t] ** 2 + TINY[t]
+    eu = dh.double().abs() * 2.0 ** -20 * (1 + gate.double().abs()) + du.abs() * HALF[t] ** 2 + TINY[t]
+    x, wg, wu = x.double(), wg.double(), wu.double()
+    want = {"dx": dg @ wg + du @ wu, "dw_gate": dg.T @ x, "dw_up": du.T @ x}
+    mag = {"dx": dg.abs() @ wg.abs() + du.abs() @ wu.abs(), "dw_gate": dg.abs().T @ x.abs(), "dw_up": du.abs().T @ x.abs()}
+    err = {"dx": eg @ wg.abs() + eu @ wu.abs(), "dw_gate": eg.T @ x.abs(), "dw_up": eu.T @ x.abs()}
+    for k, got in out.items():
+        e = err[k] + 1.01 * _lost(mag[k], 2 * (2 * F + 64) if k == "dx" else 2 * (M + 64))
+        _near(got, want[k], e + (want[k].abs() + e) * HALF[got.dtype] + TINY[got.dtype], got.dtype)
+    if M == 1:      # an infinite slope stays one, and its row's alone
+        dh[0, 3] = float("inf")
+        ctx.gated_backward(dh, gate, up, x.to(t), None, None, act=name, dw_gate=out["dw_gate"], dw_up=out["dw_up"])
+        other = torch.arange(F, device="cuda") != 3
+        assert bool(torch.isfinite(out["dw_up"][other]).all()) and bool(torch.isinf(out["dw_up"][3]).all())
