@@ -345,7 +345,7 @@ __device__ __forceinline__ void tmem_ld32_wait(uint32_t taddr, float (&v)[32])
 template <auto Kernel, typename P>
 cudaError_t launch_chained(const P &prm, int grid, int threads, size_t smem, int cluster, cudaStream_t st)
 {
-    if (smem > 48 * 1024) {
+    if (smem > 0) {      // (48 KB without it hold the kernel's own arrays too)
         static std::atomic<int> raised[64];
         int dev = 0;
         cudaError_t e = cudaGetDevice(&dev);

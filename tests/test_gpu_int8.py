@@ -92,6 +92,22 @@ def test_strides_and_alignment(ctx, dtype, offset, pad):
     assert torch.equal(torch.nan_to_num(out[:, :cols]), torch.nan_to_num(ctx.i8_dequantize(q)))
 
 
+@pytest.mark.parametrize("rows,both", [(310, True), (320, False), (336, True)])
+def test_first_call_of_a_process_with_nearly_48_kb_of_shared_memory(rows, both):
+    """The strips' shared memory and the kernel's own arrays are together more than a kernel has without asking."""
+    import subprocess
+    import sys
+    from pathlib import Path
+    code = f"""import torch
+from paper_1811_03617_b200 import gvq
+ctx = gvq.Context(gvq.HostLayout(4, 4, [0], [4]))
+x = torch.randn({rows}, 200, device="cuda", dtype=torch.bfloat16)
+q = ctx.i8_quantize_both(x)[1] if {both} else ctx.i8_quantize_transposed(x)
+assert torch.equal(q.codes, ctx.i8_quantize(x.t().contiguous()).codes)
+"""
+    subprocess.run([sys.executable, "-c", code], check=True, cwd=Path(__file__).resolve().parent.parent, timeout=300)
+
+
 def test_stochastic_rounding_is_unbiased(ctx):
     """4096 roundings of one step have a standard error of at most step / 2 / 64; five of them, the 2^-14 of a step that u
     leaves, and what rounding the scale and the factor to 24 bits moves 127 steps by."""
