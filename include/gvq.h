@@ -594,6 +594,9 @@ gvq_status gvq_gated_forward(gvq_ctx *ctx, const void *x, int64_t ldx, const voi
      dg = dh * u * act'(g),  du = dh * act(g)            (rounded to dtype: they are operands of the products below; up to
                                                          M * F * K = 2^26 what the rounding left is multiplied too)
      dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x     (fp32 sums, rounded once)
+   In half precision dg and du are held times a power of two that brings the largest finite entry of both to 2^15 .. 2^16 (or half of that),
+   and the sums are multiplied by its reciprocal: entries of any size up to fp32's range are products' operands, and those down to 2^-29
+   of the largest keep 11 bits.
    dx_opt: [M][K]; dw_gate_opt, dw_up_opt: [F][K] of type dw_dtype (GVQ_F32: views of a flat gradient).  Any of the three may be
    NULL, not all; w_gate and w_up are read for dx only, x for the weights' gradients only.  Gradients are overwritten. */
 gvq_status gvq_gated_backward(gvq_ctx *ctx, const void *dh, int64_t ld_dh, const void *gate, int64_t ld_gate_in, const void *up,

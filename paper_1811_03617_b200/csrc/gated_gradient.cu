@@ -1,8 +1,8 @@
 // Backward pass of the gated block (gvq.h, "the gated block"):
-//   dg = dh u act'(g),  du = dh act(g)             gated_slopes_kernel
+//   dg = dh u act'(g),  du = dh act(g)             gated_slopes_kernel; in half precision gated_tops_kernel before it
 //   dx = dg Wg + du Wu                             one product whose contraction has two segments
 //   dWg = dg^T x,  dWu = du^T x                    one product of two halves that have x in common
-// in one launch for the slopes and one or two for the products,
+// in one launch for the slopes (two in half precision) and one or two for the products,
 // and the copies of operands whose rows do not start at 16-byte boundaries, which TMA cannot address.
 #include <float.h>
 
@@ -38,6 +38,9 @@ struct SlopeParams {
     int64_t rows, cols, ld_out;
     int chunks;                // groups of eight columns of a row
     RowCopies copies;          // done on the way: the products after this launch read them
+    uint16_t *tops;            // half precision: of each CTA of gated_tops_kernel, see there
+    int n_tops;
+    float *unscale;            // half precision: what makes the products of dg and du as they are held those of dg and du
 };
 
 template <typename T, bool VEC>
@@ -50,6 +53,71 @@ __device__ __forceinline__ void load_eight(const void *p, int64_t at, int n, flo
     for (int i = 0; i < 8; ++i) v[i] = to_f(e[i]);
 }
 
+// Eight entries of dg and of du from column `chunk * 8` of row r on.
+template <typename T, int ACT, bool VEC>
+__device__ __forceinline__ void slopes_at(const SlopeParams &prm, int64_t r, int chunk, float (&d)[2][8])
+{
+    const int64_t c = (int64_t)chunk * 8;
+    const int n = (int)min((int64_t)8, prm.cols - c);
+    float dh[8], g[8], u[8];
+    load_eight<T, VEC>(prm.dh, r * prm.ld_dh + c, n, dh);
+    load_eight<T, VEC>(prm.g, r * prm.ld_g + c, n, g);
+    load_eight<T, VEC>(prm.u, r * prm.ld_u + c, n, u);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float2 a = activation_and_slope<ACT>(g[i]);
+        d[0][i] = dh[i] * u[i] * a.y;
+        d[1][i] = dh[i] * a.x;
+    }
+}
+__device__ __forceinline__ uint32_t block_max(uint32_t v)      // 256 threads
+{
+    __shared__ uint32_t of_warp[8];
+    v = __reduce_max_sync(0xffffffffu, v);
+    if ((threadIdx.x & 31) == 0) of_warp[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = of_warp[threadIdx.x & 7];
+    return __reduce_max_sync(0xffffffffu, v);
+}
+
+// Half precision has 5 bits of exponent: dg and du of tokens with small gradients would be among its subnormal numbers (1e-6 in steps of
+// 6e-8), and those past 65504 infinite, although fp32 sums and the weights' gradients in fp32 hold them.  So they are held times a power of
+// two, the largest finite entry of both between 2^15 and 2^16, and the products' epilogues undo it (exactly): entries down to 2^-29 of the
+// largest keep their 11 bits.  The largest has to be known before the first is rounded, so inputs are read once more (all gradients in
+// fp16, us, with and without: 100 x 100 x 100 18.5, 15.8; 777 x 1029 x 515 28.7, 24.6; 2048 x 2048 x 1024 49.1, 40.7; 8192 x 8192 x 512 403, 315).
+// A bfloat16 has fp32's exponents and needs none of this.
+// A CTA leaves its entries' largest exponent, as fp32 has it; one more where times a power of two up to 2^16 it would round past 65504.
+constexpr int kMostTops = 1024;
+template <typename T, int ACT, bool VEC>
+__global__ void __launch_bounds__(256) gated_tops_kernel(const __grid_constant__ SlopeParams prm)
+{
+    launch_dependents();
+    grid_dependency_wait();
+    uint32_t top = 0;
+    for_chunks(prm.rows, prm.chunks, [&](int64_t r, int chunk) {
+        float d[2][8];
+        slopes_at<T, ACT, VEC>(prm, r, chunk, d);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t m = __float_as_uint(d[i / 8][i % 8]) & 0x7FFFFFFFu;
+            top = max(top, m < 0x7F800000u ? m : 0u);
+        }
+    });
+    __syncwarp();
+    top = block_max(top);
+    if (threadIdx.x == 0) prm.tops[blockIdx.x] = (uint16_t)((top >> 23) + ((top & 0x7FFFFFu) > 0x7FE000u));
+}
+// The power of two, and its reciprocal for the products.
+__device__ __forceinline__ float half_scale(const SlopeParams &prm)
+{
+    uint32_t top = 0;
+    for (int i = threadIdx.x; i < prm.n_tops; i += 256) top = max(top, (uint32_t)__ldcg(prm.tops + i));
+    __syncwarp();
+    const int e = min(126, 15 + 127 - (int)block_max(top));      // (both are normal numbers)
+    if (blockIdx.x == 0 && threadIdx.x == 0) *prm.unscale = __uint_as_float((uint32_t)(127 - e) << 23);
+    return __uint_as_float((uint32_t)(127 + e) << 23);
+}
+
 // Eight entries a thread, each read and written once: 8192 x 8192 in 106 us, where the bytes take 103 at the copy rate.
 constexpr int kResident = 6;      // CTAs of an SM: the grid is as many as there is room for at once (16 an SM: 109 us)
 template <typename T, int ACT, bool VEC>
@@ -57,24 +125,19 @@ __global__ void __launch_bounds__(256, kResident) gated_slopes_kernel(const __gr
 {
     launch_dependents();
     grid_dependency_wait();
+    float scale = 1.0f;
+    if constexpr (std::is_same_v<T, __half>) scale = half_scale(prm);
     for_chunks(prm.rows, prm.chunks, [&](int64_t r, int chunk) {
-        const int64_t c = (int64_t)chunk * 8;
-        const int n = (int)min((int64_t)8, prm.cols - c);
-        float dh[8], g[8], u[8];
-        load_eight<T, VEC>(prm.dh, r * prm.ld_dh + c, n, dh);
-        load_eight<T, VEC>(prm.g, r * prm.ld_g + c, n, g);
-        load_eight<T, VEC>(prm.u, r * prm.ld_u + c, n, u);
         float d[2][8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2 a = activation_and_slope<ACT>(g[i]);
-            d[0][i] = dh[i] * u[i] * a.y;
-            d[1][i] = dh[i] * a.x;
-        }
-        const int64_t at = r * prm.ld_out + c;      // (rows are padded to eight entries)
+        slopes_at<T, ACT, VEC>(prm, r, chunk, d);
+        const int64_t at = r * prm.ld_out + (int64_t)chunk * 8;      // (rows are padded to eight entries)
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
             uint32_t w[4];
+            if constexpr (std::is_same_v<T, __half>) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[which][i] *= scale;
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = pack2<T>(d[which][2 * i], d[which][2 * i + 1]);
             *reinterpret_cast<uint4 *>(static_cast<T *>(prm.d[which]) + at) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -93,11 +156,12 @@ __global__ void __launch_bounds__(256, kResident) gated_slopes_kernel(const __gr
     copy_rows(prm.copies);
 }
 
-Params start(const Launch &l, int dtype, int out_dtype)
+Params start(const Launch &l, const GatedGrads &g, int out_dtype)
 {
     Params prm = {};
     prm.dtype = out_dtype;
-    prm.bf16 = dtype == GVQ_BF16;
+    prm.bf16 = g.dtype == GVQ_BF16;
+    prm.unscale = g.unscale;
     prm.error_word = l.error_word;
     prm.wait_kcycles = l.wait_kcycles > 0 ? l.wait_kcycles : WAIT_KCYCLES_DEFAULT;
     prm.test_drop = l.test_drop;
@@ -117,17 +181,28 @@ int64_t items_of(const RowCopies &c)      // of the largest
     return items;
 }
 
-template <typename T, bool VEC>
-cudaError_t launch_slopes_as(const Launch &l, const SlopeParams &prm, int act)
+template <typename T, int ACT, bool VEC>
+cudaError_t launch_slopes_of(const Launch &l, SlopeParams &prm)
 {
     const int64_t slopes = prm.rows * prm.chunks, copies = items_of(prm.copies);
+    if constexpr (std::is_same_v<T, __half>) {
+        const int grid = grid_of(l.num_sms, slopes, kResident);
+        prm.n_tops = grid < kMostTops ? grid : kMostTops;
+        const cudaError_t e = launch_chained<gated_tops_kernel<T, ACT, VEC>>(prm, prm.n_tops, 256, 0, 1, l.stream);
+        if (e != cudaSuccess) return e;
+    }
     const int grid = grid_of(l.num_sms, slopes > copies ? slopes : copies, kResident);
+    return launch_chained<gated_slopes_kernel<T, ACT, VEC>>(prm, grid, 256, 0, 1, l.stream);
+}
+template <typename T, bool VEC>
+cudaError_t launch_slopes_as(const Launch &l, SlopeParams &prm, int act)
+{
     switch (act) {
-    case GVQ_SILU: return launch_chained<gated_slopes_kernel<T, GVQ_SILU, VEC>>(prm, grid, 256, 0, 1, l.stream);
-    case GVQ_GELU: return launch_chained<gated_slopes_kernel<T, GVQ_GELU, VEC>>(prm, grid, 256, 0, 1, l.stream);
-    case GVQ_GELU_TANH: return launch_chained<gated_slopes_kernel<T, GVQ_GELU_TANH, VEC>>(prm, grid, 256, 0, 1, l.stream);
-    case GVQ_RELU: return launch_chained<gated_slopes_kernel<T, GVQ_RELU, VEC>>(prm, grid, 256, 0, 1, l.stream);
-    default: return launch_chained<gated_slopes_kernel<T, GVQ_SIGMOID, VEC>>(prm, grid, 256, 0, 1, l.stream);
+    case GVQ_SILU: return launch_slopes_of<T, GVQ_SILU, VEC>(l, prm);
+    case GVQ_GELU: return launch_slopes_of<T, GVQ_GELU, VEC>(l, prm);
+    case GVQ_GELU_TANH: return launch_slopes_of<T, GVQ_GELU_TANH, VEC>(l, prm);
+    case GVQ_RELU: return launch_slopes_of<T, GVQ_RELU, VEC>(l, prm);
+    default: return launch_slopes_of<T, GVQ_SIGMOID, VEC>(l, prm);
     }
 }
 
@@ -138,14 +213,17 @@ cudaError_t launch_align_rows(const Launch &l, const RowCopies &copies)
     return launch_chained<align_rows_kernel>(copies, grid_of(l.num_sms, items_of(copies), kResident), 256, 0, 1, l.stream);
 }
 
+static_assert(kGatedRoom >= kMostTops * sizeof(uint16_t) + sizeof(float) && kGatedRoom % 256 == 0, "the workspace's room");
+
 cudaError_t launch_gated_slopes(const Launch &l, const void *dh, int64_t ld_dh, const void *g, int64_t ld_g, const void *u, int64_t ld_u,
-                                int dtype, int64_t rows, int64_t cols, int act, void *const (&d)[4], int64_t ld_out, const RowCopies &copies)
+                                int act, const GatedGrads &of, void *room, const RowCopies &copies)
 {
     auto aligned = [](const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % 8 == 0; };
-    const SlopeParams prm = {dh, g, u, ld_dh, ld_g, ld_u, {d[0], d[1], d[2], d[3]}, rows, cols, ld_out, (int)((cols + 7) / 8), copies};
-    if (aligned(dh, ld_dh) && aligned(g, ld_g) && aligned(u, ld_u))      // all rows start at 16-byte boundaries
-        return dtype == GVQ_BF16 ? launch_slopes_as<__nv_bfloat16, true>(l, prm, act) : launch_slopes_as<__half, true>(l, prm, act);
-    return dtype == GVQ_BF16 ? launch_slopes_as<__nv_bfloat16, false>(l, prm, act) : launch_slopes_as<__half, false>(l, prm, act);
+    SlopeParams prm = {dh, g, u, ld_dh, ld_g, ld_u, {of.d[0], of.d[1], of.d[2], of.d[3]}, of.M, of.F, of.ld_d, (int)((of.F + 7) / 8), copies,
+                       static_cast<uint16_t *>(room), 0, of.unscale};
+    const bool vec = aligned(dh, ld_dh) && aligned(g, ld_g) && aligned(u, ld_u);      // all rows start at 16-byte boundaries
+    if (of.dtype == GVQ_BF16) return vec ? launch_slopes_as<__nv_bfloat16, true>(l, prm, act) : launch_slopes_as<__nv_bfloat16, false>(l, prm, act);
+    return vec ? launch_slopes_as<__half, true>(l, prm, act) : launch_slopes_as<__half, false>(l, prm, act);
 }
 
 namespace {
@@ -155,7 +233,7 @@ int precise(const GatedGrads &g) { return g.d[2] ? 2 : 1; }
 // dx = dg Wg + du Wu: a contraction of two segments (four).  The weights are MN-major here: boxes of 64 of a row's entries by 64 rows.
 bool dx_problem(Params &prm, const Launch &l, const Cut &c, const GatedGrads &g)
 {
-    prm = start(l, g.dtype, g.dtype);
+    prm = start(l, g, g.dtype);
     prm.M = c.few ? g.K : g.M;
     prm.N = c.few ? g.M : g.K;
     const int segments = 2 * precise(g);
@@ -176,7 +254,7 @@ int halves_of(const GatedGrads &g) { return g.dw[0] && g.dw[1] ? 2 : 1; }
 bool dw_problem(Params &prm, const Launch &l, const Cut &c, const GatedGrads &g)
 {
     const int halves = halves_of(g), segments = precise(g);
-    prm = start(l, g.dtype, g.dw_dtype);
+    prm = start(l, g, g.dw_dtype);
     prm.M = g.F;
     prm.N = g.K;
     prm.a_mn = 1;

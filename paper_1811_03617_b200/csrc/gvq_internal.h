@@ -203,18 +203,22 @@ struct RowCopies {
     int chunks[3];
 };
 cudaError_t launch_align_rows(const Launch &l, const RowCopies &copies);
-// d: dg and du, and what rounding them left (null: not wanted).
-cudaError_t launch_gated_slopes(const Launch &l, const void *dh, int64_t ld_dh, const void *g, int64_t ld_g, const void *u, int64_t ld_u,
-                                int dtype, int64_t rows, int64_t cols, int act, void *const (&d)[4], int64_t ld_out, const RowCopies &copies);
-// The products of a backward pass.  w, dw: the gate's and the other projection's; d: as above; dx or dw null: not wanted.
+// A backward pass.  d: dg and du, and what rounding them left (null: not wanted), rows ld_d entries apart; w, dw: the gate's and the
+// other projection's; dx or dw null: not wanted.
 struct GatedGrads {
-    const void *d[4], *w[2], *x;
+    void *d[4];
+    const void *w[2], *x;
     int64_t ld_d, ld_w[2], ldx;
     int dtype, dw_dtype;
     int64_t M, F, K;
     void *dx, *dw[2];
     int64_t ld_dx, ld_dw[2];
+    float *unscale;            // half precision: the factor of the products of what d holds (device memory; null otherwise)
 };
+// room: kGatedRoom bytes of workspace, whose last four are the factor's.
+constexpr int64_t kGatedRoom = 2304;
+cudaError_t launch_gated_slopes(const Launch &l, const void *dh, int64_t ld_dh, const void *g, int64_t ld_g, const void *u, int64_t ld_u,
+                                int act, const GatedGrads &of, void *room, const RowCopies &copies);
 cudaError_t launch_gated_products(const Launch &l, const GatedGrads &g);
 
 // Basis fit.  Workspace layout is private to fit_basis.cu.

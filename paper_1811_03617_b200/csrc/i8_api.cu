@@ -24,7 +24,7 @@ Launch launch_of(const gvq_ctx *ctx)
     return {ctx->stream, ctx->num_sms, (EncodeTiledFn)ctx->encode_fn, ctx->error_word, ctx->wait_kcycles, ctx->drop_last_load};
 }
 
-// The gated block's workspace: dg and du of a backward pass, then copies of operands whose rows TMA cannot address.
+// The gated block's workspace: dg and du of a backward pass and what holding them in half precision takes, then copies of operands whose rows TMA cannot address.
 int64_t padded(int64_t n, int per) { return (n + per - 1) / per * per; }
 // Matrices of a backward pass: dg and du, and where the products are short what rounding them left.  It is there that few outputs carry a
 // gradient's norm, so that roundings do not average: of 99 thousand blocks' gradients with M, F and K spread over 65..8192, 33..8192 and
@@ -138,7 +138,7 @@ gvq_status gvq_i8_gated(gvq_ctx *ctx, const int8_t *a_codes, const float *a_scal
 int64_t gvq_gated_workspace_bytes(int64_t M, int64_t F, int64_t K, int backward, int aligned)
 {
     if (!sizes_ok(M, F) || !sizes_ok(M, K) || !sizes_ok(F, K)) return -1;
-    return (backward ? slopes_of(M, F, K) * bytes_of(M, F) : 0) + (aligned ? 0 : bytes_of(M, K) + 2 * bytes_of(F, K));
+    return (backward ? slopes_of(M, F, K) * bytes_of(M, F) + kGatedRoom : 0) + (aligned ? 0 : bytes_of(M, K) + 2 * bytes_of(F, K));
 }
 
 gvq_status gvq_gated_forward(gvq_ctx *ctx, const void *x, int64_t ldx, const void *w_gate, int64_t ld_gate, const void *w_up, int64_t ld_up,
@@ -188,13 +188,13 @@ gvq_status gvq_gated_backward(gvq_ctx *ctx, const void *dh, int64_t ld_dh, const
     const Launch l = launch_of(ctx);
     char *at = static_cast<char *>(workspace);
     const int n = slopes_of(M, F, K);
-    void *d[4] = {};
-    for (int i = 0; i < n; ++i) d[i] = at + i * bytes_of(M, F);
-    const RowCopies copies = align_operands(ops, 3, at + n * bytes_of(M, F));
-    const int64_t ld_d = padded(F, 8);
-    GVQ_CUDA(ctx, launch_gated_slopes(l, dh, ld_dh, gate, ld_gate_in, up, ld_up_in, dtype, M, F, activation, d, ld_d, copies));
-    const GatedGrads g = {{d[0], d[1], d[2], d[3]}, {ops[1].p, ops[2].p}, ops[0].p, ld_d, {ops[1].ld, ops[2].ld}, ops[0].ld, dtype, dw_dtype, M, F, K,
-                          dx_opt, {dw_gate_opt, dw_up_opt}, ld_dx, {ld_dw_gate, ld_dw_up}};
+    char *room = at + n * bytes_of(M, F);
+    const RowCopies copies = align_operands(ops, 3, room + kGatedRoom);
+    GatedGrads g = {{}, {ops[1].p, ops[2].p}, ops[0].p, padded(F, 8), {ops[1].ld, ops[2].ld}, ops[0].ld, dtype, dw_dtype, M, F, K,
+                    dx_opt, {dw_gate_opt, dw_up_opt}, ld_dx, {ld_dw_gate, ld_dw_up},
+                    dtype == GVQ_F16 ? reinterpret_cast<float *>(room + kGatedRoom) - 1 : nullptr};
+    for (int i = 0; i < n; ++i) g.d[i] = at + i * bytes_of(M, F);
+    GVQ_CUDA(ctx, launch_gated_slopes(l, dh, ld_dh, gate, ld_gate_in, up, ld_up_in, activation, g, room, copies));
     GVQ_CUDA(ctx, launch_gated_products(l, g));
     return GVQ_OK;
 }

@@ -63,6 +63,7 @@ struct Params {
     int align[3];                      // bytes at whose multiples the outputs' rows start: 32, 16 or less
     int dtype, act, bf16;              // outputs' type; activation; operands' type, of 16 bits
     const float *scale_m[2], *scale_n[2];   // of 8-bit operands
+    const float *unscale;              // of 16-bit operands that are held times a power of two: the sums' factor; null: 1
     int32_t *error_word;
     int wait_kcycles, test_drop;
     int a_mn;                          // of two problems in a launch: this one's A is MN-major
@@ -299,7 +300,8 @@ __device__ __forceinline__ void join_parts(const Params &prm, const float4 *join
             } else {
 #pragma unroll
                 for (int p = 1; p < P; ++p) { x[0].x += x[p].x; x[0].y += x[p].y; x[0].z += x[p].z; x[0].w += x[p].w; }
-                y[0] = x[0].x; y[1] = x[0].y; y[2] = x[0].z; y[3] = x[0].w;
+                const float f = !GATED && prm.unscale ? __ldcg(prm.unscale) : 1.0f;
+                y[0] = x[0].x * f; y[1] = x[0].y * f; y[2] = x[0].z * f; y[3] = x[0].w * f;
             }
         };
         auto store = [&](int k, const float (&y)[4]) {
@@ -502,6 +504,8 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
         uint32_t t = 0;
         const int dtype = prm.dtype;
         constexpr int PW = HN < 32 ? HN : 32, NP = HN / PW;  // columns of a piece, pieces of a tile
+        constexpr bool SCALED = KIND == k16 && !GATED;
+        const float unscale = SCALED && prm.unscale ? __ldcg(prm.unscale) : 1.0f;
         for (int tile = first; tile < n_tiles; tile += stride, ++t) {
             int tm, tn;
             place(prm, tile, tm, tn);
@@ -573,6 +577,10 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
                         v[i + 3] = __int2float_rn(__float_as_int(v[i + 3])) * sm * x.w;
                     }
                 }
+                if constexpr (SCALED) {
+#pragma unroll
+                    for (int i = 0; i < PW; ++i) v[i] *= unscale;
+                }
             };
             if constexpr (FEW) {       // rows of A run along the output's rows: a warp's lanes do too
 #pragma unroll 1
@@ -627,6 +635,10 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
                                 const float *of = scales + (SIDE ? which : 0) * NS * 32 + c;
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) x[i] = __int2float_rn(__float_as_int(x[i])) * sm * of[i];
+                            }
+                            if constexpr (SCALED) {
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) x[i] *= unscale;
                             }
                         };
 #pragma unroll 1

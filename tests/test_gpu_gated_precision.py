@@ -1,0 +1,138 @@
+"""How exact the gated block's gradients are where it is easily lost."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+BF, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+HALF = {BF: 2.0 ** -8, F16: 2.0 ** -11, F32: 2.0 ** -24}      # half a step, relative
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_1811_03617_b200 import gvq
+    return gvq.Context(gvq.HostLayout(4, 4, [0], [4]))
+
+
+def act(name, g):
+    """(activation, derivative) in 64 bits, without differences of nearly equal numbers."""
+    if name == "relu":
+        return g * (g > 0), (g > 0).double()
+    if name == "gelu":
+        cdf = 0.5 * torch.special.erfc(-g / math.sqrt(2))
+        return g * cdf, cdf + g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+    if name == "gelu_tanh":
+        c = 2 * math.sqrt(2 / math.pi)
+        z = c * (g + 0.044715 * g ** 3)
+        s = torch.sigmoid(z)
+        return g * s, s + g * s * torch.sigmoid(-z) * c * (1 + 3 * 0.044715 * g * g)
+    s, r = torch.sigmoid(g), torch.sigmoid(-g)
+    return (s, s * r) if name == "sigmoid" else (g * s, s + g * s * r)
+
+
+# sizes on both sides of 2^26 multiply-adds; one token, few, tiles, one launch for all gradients, pairs of SMs, rows at any place
+SIZES = [(1, 300, 264), (20, 333, 165), (300, 333, 165), (700, 520, 264), (64, 2056, 1032), (1300, 1029, 520)]
+
+
+def _gradients(ctx, M, F, K, dtype, name, dh_size, up_size=1.0, **kw):
+    """Outputs, and for each (wanted value, sum of magnitudes, what errors of dg and du relative to themselves make of it)."""
+    gen = torch.Generator(device="cuda").manual_seed(M + F + K)
+
+    def made(rows, cols, size=1.0):
+        return (torch.randn(rows, cols, generator=gen, device="cuda") * size).to(dtype)
+    x, wg, wu = made(M, K), made(F, K, 1 / math.sqrt(K)), made(F, K, 1 / math.sqrt(K))
+    gate, up, dh = made(M, F), made(M, F, up_size), made(M, F) * 1.0
+    dh = (dh.float() * dh_size).to(dtype)
+    out = {"dx": torch.empty(M, K, device="cuda", dtype=dtype), "dw_gate": torch.empty(F, K, device="cuda"), "dw_up": torch.empty(F, K, device="cuda")}
+    ctx.gated_backward(dh, gate, up, x, wg, wu, act=name, **out, **kw)
+    ctx.device_status()
+    a, slope = act(name, gate.double())
+    dhu = dh.double() * up.double()
+    dg, du = dhu * slope, dh.double() * a
+    x, wg, wu = x.double(), wg.double(), wu.double()
+    want = {"dx": dg @ wg + du @ wu, "dw_gate": dg.T @ x, "dw_up": du.T @ x}
+
+    def spread(eg, eu):
+        return {"dx": eg @ wg.abs() + eu @ wu.abs(), "dw_gate": eg.T @ x.abs(), "dw_up": eu.T @ x.abs()}
+    top = max(float(dg.abs().max()), float(du.abs().max()))
+    # fp32: the activation 16 half steps of max(1, |g|), its slope twice that (of dh u, as |slope| < 1.13)
+    fp32 = (dhu.abs() * 2.0 ** -19 * (1 + gate.double().abs()), dh.double().abs() * 2.0 ** -20 * (1 + gate.double().abs()))
+    return out, want, spread(dg.abs(), du.abs()), spread(*fp32), spread(torch.ones_like(dg) * top, torch.ones_like(dg) * top)
+
+
+def _check(out, want, mag, fp32, top, M, F, dtype, operand, names):
+    """operand: what rounding leaves of dg and du, relative; half precision: half its smallest step, 2^-25, where the largest
+    entry is held as 2^15 to 2^16, or half of that where it overflows."""
+    for k in names:
+        got, t = out[k], out[k].dtype
+        steps = (2 * 2 * F if k == "dx" else 2 * M) // 16 + 8      # of 16 terms, each of which may lose 2^-22 of the sum of magnitudes
+        e = mag[k] * (operand + steps * 2.0 ** -22) + fp32[k] + (top[k] * 2.0 ** -39 if dtype == F16 else 0)
+        tiny = 2.0 ** -25 if t == F16 else 0.0
+        bound = e + (want[k].abs() + e) * HALF[t] + tiny
+        assert bool(torch.isfinite(got).all()), k
+        off = (got.double() - want[k]).abs() / bound
+        assert float(off.max()) <= 1, (k, float(off.max()))
+
+
+@pytest.mark.parametrize("M,F,K", SIZES)
+@pytest.mark.parametrize("dh_size", [1.0, 1e-4, 2e-6])
+def test_small_gradients_in_half_precision_keep_their_digits(ctx, M, F, K, dh_size):
+    """dg and du of 1e-6 are among half precision's subnormal numbers, whose steps are 6e-8: they are held at another power of two."""
+    r = _gradients(ctx, M, F, K, F16, "silu", dh_size)
+    _check(*r, M, F, F16, HALF[F16], ("dx", "dw_gate", "dw_up"))
+
+
+@pytest.mark.parametrize("M,F,K", SIZES)
+def test_large_gradients_in_half_precision_do_not_overflow(ctx, M, F, K):
+    """dh u act'(g) of a million is past half precision; the weights' gradients in fp32 hold its products."""
+    r = _gradients(ctx, M, F, K, F16, "gelu_tanh", 300.0, 3000.0)
+    _check(*r, M, F, F16, HALF[F16], ("dw_gate", "dw_up"))
+
+
+def test_infinities_and_zeros_in_half_precision(ctx):
+    """The power of two is that of the finite entries: a row with an infinity makes its own results infinite or NaN, and the other tokens'
+    have the bits that they have without it; of gradients that are all 0 everything is 0."""
+    M, F, K = 300, 333, 168
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x, wg, wu, gate, up, dh = (torch.randn(r, c, generator=gen, device="cuda").half() for r, c in ((M, K), (F, K), (F, K), (M, F), (M, F), (M, F)))
+    dh *= 1e-3
+    dh[7] = 0
+
+    def gradients():
+        out = {"dx": torch.empty(M, K, device="cuda", dtype=F16), "dw_gate": torch.empty(F, K, device="cuda"), "dw_up": torch.empty(F, K, device="cuda")}
+        ctx.gated_backward(dh, gate, up, x, wg, wu, act="silu", **out)
+        ctx.device_status()
+        return out
+    want = gradients()
+    dh[7, 5], gate[7, 5] = float("inf"), 1.0
+    got = gradients()
+    others = torch.arange(M, device="cuda") != 7
+    assert torch.equal(got["dx"][others], want["dx"][others]) and not bool(torch.isfinite(got["dx"][7]).any())
+    columns = torch.arange(F, device="cuda") != 5
+    for k in ("dw_gate", "dw_up"):
+        assert torch.equal(got[k][columns], want[k][columns]) and not bool(torch.isfinite(got[k][5]).any())
+    dh.zero_()
+    assert all(bool((t == 0).all()) for t in gradients().values())
+
+
+@pytest.mark.parametrize("M,F,K", [(20, 333, 165), (300, 520, 264), (1300, 1029, 520)])
+def test_a_captured_backward_pass_takes_its_power_of_two_from_its_own_inputs(ctx, M, F, K):
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x, wg, wu, gate, up, dh = (torch.randn(r, c, generator=gen, device="cuda").half() for r, c in ((M, K), (F, K), (F, K), (M, F), (M, F), (M, F)))
+
+    def room():
+        return {"dx": torch.empty_like(x), "dw_gate": torch.empty(F, K, device="cuda"), "dw_up": torch.empty(F, K, device="cuda")}
+    captured, eager = room(), room()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.gated_backward(dh, gate, up, x, wg, wu, **captured)
+    for size in (1.0, 2.0 ** -18, 2.0 ** 10):
+        dh.copy_(torch.randn(M, F, generator=gen, device="cuda") * size)
+        graph.replay()
+        ctx.gated_backward(dh, gate, up, x, wg, wu, **eager)
+        torch.cuda.synchronize()
+        for k in eager:
+            assert torch.equal(captured[k], eager[k]) and bool((eager[k] != 0).any())
