@@ -423,6 +423,13 @@ class I8:
         return self._views()[1]
 
 
+def _formats(what: str, other, *matrices) -> None:
+    """4-bit and 8-bit matrices look alike but for their sizes in bytes: one of the other format is refused."""
+    for q in matrices:
+        if isinstance(q, other):
+            raise TypeError(f"{what}: a {'4' if other is Mx4 else '8'}-bit matrix where one of the other format is wanted")
+
+
 _MOST = 0x7FFFFFFF - 1024      # rows, columns
 
 
@@ -582,6 +589,7 @@ class Context:
 
     # ---- microscaled 4-bit floating point ---------------------------------------------------
     def _mx4(self, x, by_rows, by_cols, stochastic, seed, node, out=None, out_t=None):
+        _formats("mx4_quantize", I8, out, out_t)
         rows, cols, ld = _rows(x, self.device, "mx4_quantize")
         dtype = _dtype(x)
         c = s = ct = st = None
@@ -619,6 +627,7 @@ class Context:
 
     def mx4_dequantize(self, q: Mx4, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """gvq_mx4_dequantize: what q stands for, float32 [rows, cols]."""
+        _formats("mx4_dequantize", I8, q)
         if out is None:
             out = torch.empty((q.rows, q.cols), device=f"cuda:{self.device}")
         rows, cols, ld = _rows(out, self.device, "mx4_dequantize")
@@ -631,6 +640,7 @@ class Context:
 
     def mx4_matmul(self, a: Mx4, b: Mx4, out: torch.Tensor) -> torch.Tensor:
         """gvq_mx4_matmul: out [a.rows, b.rows] = a b^T; out is float32, bfloat16 or float16."""
+        _formats("mx4_matmul", I8, a, b)
         rows, cols, ld = _rows(out, self.device, "mx4_matmul")
         if a.cols != b.cols or (rows, cols) != (a.rows, b.rows):
             raise ValueError(f"mx4_matmul: [{a.rows}, {a.cols}] x [{b.rows}, {b.cols}]^T does not give [{rows}, {cols}]")
@@ -646,6 +656,7 @@ class Context:
     # ---- 8-bit integers ---------------------------------------------------------------------
     def _i8(self, x, by_rows, by_cols, stochastic, seed, node, out=None, out_t=None):
         device = self.device
+        _formats("i8_quantize", Mx4, out, out_t)
         rows, cols, ld = _rows(x, device, "i8_quantize")
         dtype = DTYPE.get(x.dtype)
         if dtype is None:
@@ -702,6 +713,7 @@ class Context:
 
     def i8_dequantize(self, q: I8, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """gvq_i8_dequantize: what q stands for, float32 [rows, cols]."""
+        _formats("i8_dequantize", Mx4, q)
         if out is None:
             out = torch.empty((q.rows, q.cols), device=f"cuda:{self.device}")
         rows, cols, ld = _rows(out, self.device, "i8_dequantize")
@@ -716,6 +728,7 @@ class Context:
         if _short is not None and _short.i8_matmul(self._address, self.device, a, b, out):
             return out
         device, k = self.device, a.cols
+        _formats("i8_matmul", Mx4, a, b)
         rows, cols, ld = _rows(out, device, "i8_matmul")
         if k != b.cols or rows != a.rows or cols != b.rows:
             raise ValueError(f"i8_matmul: [{a.rows}, {a.cols}] x [{b.rows}, {b.cols}]^T does not give [{rows}, {cols}]")
@@ -822,6 +835,7 @@ class Context:
         if _short is not None and _short.i8_gated(self._address, self.device, a, w_gate, w_up, out, ACTIVATION.get(act, -1)):
             return out
         code = _activation(act)
+        _formats("i8_gated", Mx4, a, w_gate, w_up)
         rows, cols, ld = _rows(out, self.device, "i8_gated")
         if w_gate.cols != a.cols or w_up.cols != a.cols or w_gate.rows != w_up.rows or (rows, cols) != (a.rows, w_gate.rows):
             raise ValueError(f"i8_gated: [{a.rows}, {a.cols}] x [{w_gate.rows}, {w_gate.cols}]^T and [{w_up.rows}, {w_up.cols}]^T do not give "
@@ -856,6 +870,7 @@ class Context:
         """(codes, scales) of one [S][d] matrix per node, as host arrays."""
         if len(q_nodes) != n:
             raise ValueError(f"{what}: one 4-bit matrix per node is wanted ({n}), not {len(q_nodes)}")
+        _formats(what, I8, *q_nodes)
         for q in q_nodes:
             if q.rows != self.S or q.cols != self.d or q.device != self.device:
                 raise ValueError(f"{what}: a node's slices are {self.S} x {self.d} on cuda:{self.device}, "
