@@ -101,8 +101,11 @@ __device__ __forceinline__ float2 activation_and_slope(float x)
         const float t = s * (1.0f - s);      // (0 where the square below may overflow)
         return make_float2(x * s, s + (t > 0.0f ? x * t * kTanhScale * (1.0f + 3.0f * kTanhCubic * x * x) : t));
     }
+    if (ACT == GVQ_SIGMOID) {      // with t = e^-|x|, t / (1 + t)^2: s (1 - s) has no digit left at 16
+        const float t = exp_approx(-fabsf(x)), s = reciprocal(1.0f + t);
+        return make_float2(x < 0.0f ? t * s : s, t * s * s);
+    }
     const float s = logistic(x);
-    if (ACT == GVQ_SIGMOID) return make_float2(s, s * (1.0f - s));
     return make_float2(x * s, s + x * s * (1.0f - s));
 }
 

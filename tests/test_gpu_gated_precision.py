@@ -32,6 +32,32 @@ def act(name, g):
     return (s, s * r) if name == "sigmoid" else (g * s, s + g * s * r)
 
 
+def _of_one_token(ctx, g, name):
+    """(du, dg) of gates g with dh = u = 1, as the kernels form them: one token, x = 1, so that the weights' gradients in fp32 are du and
+    dg themselves, of which what rounding to 16 bits leaves is multiplied too (2^26 multiply-adds are far off)."""
+    n = len(g)
+    gate, ones = g.view(1, n), torch.ones(1, n, dtype=g.dtype, device="cuda")
+    dw = [torch.empty(n, 1, device="cuda") for _ in range(2)]
+    ctx.gated_backward(ones, gate, ones, torch.ones(1, 1, dtype=g.dtype, device="cuda"), None, None, act=name, dw_gate=dw[0], dw_up=dw[1])
+    ctx.device_status()
+    return dw[1][:, 0].double(), dw[0][:, 0].double()
+
+
+@pytest.mark.parametrize("dtype", [BF, F16])
+def test_sigmoid_keeps_its_digits_where_it_saturates(ctx, dtype):
+    """Relative errors: two halves of dg 2^-16 or 2^-22 of it; the exponential's argument has three roundings (the constant, the product,
+    the unit's), each 2^-24 of |g|, and what follows is a few steps of fp32, 2^-20 with room."""
+    g = torch.linspace(0.25, 30 if dtype == BF else 12, 300, device="cuda").to(dtype)
+    g = torch.cat([g, -g])
+    value, slope = act("sigmoid", g.double())
+    for got, want in zip(_of_one_token(ctx, g, "sigmoid"), (value, slope)):
+        bound = HALF[dtype] ** 2 + 3 * g.double().abs() * 2.0 ** -24 + 2.0 ** -20
+        if dtype == F16:      # (half of half precision's smallest step, 2^-25, where the largest entry, 1 here, is held as 2^15, or 32752 where that overflows)
+            bound = bound + 2.0 ** -39 / want
+        off = ((got - want).abs() / want / bound)
+        assert float(off.max()) <= 1, (float(off.max()), float(g[off.argmax()]))
+
+
 # sizes on both sides of 2^26 multiply-adds; one token, few, tiles, one launch for all gradients, pairs of SMs, rows at any place
 SIZES = [(1, 300, 264), (20, 333, 165), (300, 333, 165), (700, 520, 264), (64, 2056, 1032), (1300, 1029, 520)]
 
