@@ -26,8 +26,9 @@ __device__ __forceinline__ float logistic(float x) { return reciprocal(1.0f + ex
 constexpr float kTanhScale = 1.5957691216057308f, kTanhCubic = 0.044715f;      // 2 sqrt(2 / pi)
 // The normal distribution's cdf is erfc(-x / sqrt 2) / 2, and its density has the exponential that erfc has as a factor: with
 // z = |x| / sqrt 2 and t = 1 / (1 + z / 2), erfc z = t e^(p(t) - z^2) by the rational fit of Press, Flannery, Teukolsky and Vetterling's
-// "Numerical Recipes" (off by 1.2e-7 of itself at most; with fp32's arguments 10^-6 from -3 on, 10^-5 at -14, where a 16-bit result's
-// half step is 5 * 10^-4).  A third of the instructions of erfcf and expf: slopes of 8192 x 8192 in 112 us, not 176.
+// "Numerical Recipes" (off by 1.2e-7 of itself at most; with fp32's exponents, whose roundings grow with z^2, 7 * 10^-7 down to x = -3 and
+// 10^-5 down to -12.9, where a 16-bit result's half step is 5 * 10^-4 at least; below that the cdf is subnormal in fp32, and 0 here).
+// A third of the instructions of erfcf and expf: slopes of 8192 x 8192 in 112 us, not 176.
 struct Normal { float p, z2; };      // exponents of 2: of t e^p, and of the density
 __device__ __forceinline__ float normal_terms(float x, Normal &n)
 {

@@ -58,6 +58,21 @@ def test_sigmoid_keeps_its_digits_where_it_saturates(ctx, dtype):
         assert float(off.max()) <= 1, (float(off.max()), float(g[off.argmax()]))
 
 
+def test_the_tail_of_gelu_keeps_its_digits(ctx):
+    """Relative errors from -3 to -12: the fit 1.2e-7; exponents g^2 / 2, four roundings of 2^-24 of it; the fit's polynomial, whose ten steps
+    sum to less than 8, 80 roundings of 2^-25; two halves of a bfloat16.  The derivative is cdf - |g| density, the second at least 9 times
+    the first, so that nothing cancels (twice the bound covers both terms' errors)."""
+    g = torch.linspace(-3, -12, 400, device="cuda").to(BF)
+    value, slope = act("gelu", g.double())
+    bound = 1.2e-7 + g.double() ** 2 / 2 * 4 * 2.0 ** -24 + 80 * 2.0 ** -25 + 2.0 ** -16
+    for got, want, times in zip(_of_one_token(ctx, g, "gelu"), (value, slope), (1, 2)):
+        off = ((got - want) / want).abs() / (times * bound)
+        assert float(off.max()) <= 1, (float(off.max()), float(g[off.argmax()]))
+    # past where the density is a normal number: nothing, and nothing wrong
+    for far in _of_one_token(ctx, torch.tensor([-14.0, -20.0, -1e4, -3e38], device="cuda").to(BF), "gelu"):
+        assert bool((far.abs() < 2.0 ** -120).all())
+
+
 # sizes on both sides of 2^26 multiply-adds; one token, few, tiles, one launch for all gradients, pairs of SMs, rows at any place
 SIZES = [(1, 300, 264), (20, 333, 165), (300, 333, 165), (700, 520, 264), (64, 2056, 1032), (1300, 1029, 520)]
 
