@@ -261,6 +261,15 @@ __device__ __forceinline__ int segment_of(const Params &prm, int st)
     return (st >= prm.seg_stages) + (st >= 2 * prm.seg_stages) + (st >= 3 * prm.seg_stages);
 }
 
+// A sum of codes times its scales, of A's row and of B's: the tokens' before the weights', so that a token's results have the same bits in
+// every form.
+template <bool FEW>
+__device__ __forceinline__ float scaled(int sum, float of_a, float of_b)
+{
+    const float x = __int2float_rn(sum);
+    return FEW ? x * of_b * of_a : x * of_a * of_b;
+}
+
 // Sums that lie in the shared memory of the P CTAs of a cluster (of this one): added up, four columns of a row a thread at a time, the
 // parts in order, and then what the epilogue does with them.  Lanes lie along what is contiguous in the output.  tid: this thread's
 // place among the `threads` that do this in each CTA, whole warps.
@@ -296,7 +305,7 @@ __device__ __forceinline__ void join_parts(const Params &prm, const float4 *join
                 const float sm = prm.scale_m[FEW ? which : 0][m];
                 const float *sn = prm.scale_n[FEW ? 0 : which] + col;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = e < n ? __int2float_rn(s[e]) * sm * sn[e] : 0.0f;
+                for (int e = 0; e < 4; ++e) y[e] = e < n ? scaled<FEW>(s[e], sm, sn[e]) : 0.0f;
             } else {
 #pragma unroll
                 for (int p = 1; p < P; ++p) { x[0].x += x[p].x; x[0].y += x[p].y; x[0].z += x[p].z; x[0].w += x[p].w; }
@@ -571,10 +580,10 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
 #pragma unroll
                     for (int i = 0; i < PW; i += 4) {
                         const float4 x = of[i / 4];
-                        v[i] = __int2float_rn(__float_as_int(v[i])) * sm * x.x;
-                        v[i + 1] = __int2float_rn(__float_as_int(v[i + 1])) * sm * x.y;
-                        v[i + 2] = __int2float_rn(__float_as_int(v[i + 2])) * sm * x.z;
-                        v[i + 3] = __int2float_rn(__float_as_int(v[i + 3])) * sm * x.w;
+                        v[i] = scaled<FEW>(__float_as_int(v[i]), sm, x.x);
+                        v[i + 1] = scaled<FEW>(__float_as_int(v[i + 1]), sm, x.y);
+                        v[i + 2] = scaled<FEW>(__float_as_int(v[i + 2]), sm, x.z);
+                        v[i + 3] = scaled<FEW>(__float_as_int(v[i + 3]), sm, x.w);
                     }
                 }
                 if constexpr (SCALED) {
@@ -634,7 +643,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
                             if constexpr (KIND == kI8) {
                                 const float *of = scales + (SIDE ? which : 0) * NS * 32 + c;
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) x[i] = __int2float_rn(__float_as_int(x[i])) * sm * of[i];
+                                for (int i = 0; i < 16; ++i) x[i] = scaled<FEW>(__float_as_int(x[i]), sm, of[i]);
                             }
                             if constexpr (SCALED) {
 #pragma unroll
