@@ -563,9 +563,9 @@ gvq_status gvq_i8_dequantize(gvq_ctx *ctx, const int8_t *codes, const float *sca
 
 /* The product of two quantized matrices, both quantized along the contraction:
      out[m][n] = (sum over k < K of a[m][k] * b[n][k]) * a_scale[m] * b_scale[n]
-   The sum of codes is exact (32-bit integers; K <= 131072), the scales are applied in fp32, a's first, so that a row of a has
-   the same results among any number of rows, the result is rounded once to dtype.  a: [M][K], b: [N][K]; out: device, dtype entries, rows ld entries apart (ld >= N), aligned to its entries' size,
-   apart from the operands.
+   The sum of codes is exact (32-bit integers; K <= 131072), the scales are applied in fp32, a's first (a row of a has the same
+   results among any number of rows), the result is rounded once to dtype.  a: [M][K], b: [N][K]; out: device, dtype entries, rows
+   ld entries apart (ld >= N), aligned to its entries' size, apart from the operands.
    A linear layer's three products and few rows of a: as for the 4-bit format. */
 gvq_status gvq_i8_matmul(gvq_ctx *ctx, const int8_t *a_codes, const float *a_scales, const int8_t *b_codes, const float *b_scales,
                          int64_t M, int64_t N, int64_t K, void *out, int dtype, int64_t ld);

@@ -3,6 +3,9 @@
 // dealt with here: the function says so by returning None or False, and gvq.py goes its own way, which names what is wrong.  With small
 // operands the host's part is the whole of a call's time: i8_quantize 7.5 us through ctypes, i8_matmul 5.2, of which 2.2 and 2.8 are the
 // launch's.
+// Arguments are unpacked with the interpreter's lock, and the call and its allocations run without it: a launch waits where the stream's
+// queue is full, which may be emptied by another Python thread alone (a host function in the stream), and an allocation may wait for
+// the device.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -36,17 +39,26 @@ Py_ssize_t slot_at[kSlots];
 
 PyObject *&slot(PyObject *o, int i) { return *reinterpret_cast<PyObject **>(reinterpret_cast<char *>(o) + slot_at[i]); }
 
+// Without the interpreter's lock from here to the end of the block.
+struct Unlocked {
+    PyThreadState *state = PyEval_SaveThread();
+    Unlocked() = default;
+    Unlocked(const Unlocked &) = delete;
+    ~Unlocked() { PyEval_RestoreThread(state); }
+};
+
 struct Context {
     gvq_ctx *h;
     int device;
+    // The context's stream becomes torch's current one.
+    bool ready() const { return entry.set_stream(h, c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream()) == GVQ_OK; }
 };
-// A context's handle and device; its stream becomes torch's current one.
+// A context's handle and device.
 bool open(PyObject *handle, PyObject *device, Context &c)
 {
     c.h = static_cast<gvq_ctx *>(PyLong_AsVoidPtr(handle));
-    if (!c.h || !entry.set_stream) return false;
     c.device = (int)PyLong_AsLong(device);
-    return entry.set_stream(c.h, c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)c.device).stream()) == GVQ_OK;
+    return c.h && entry.set_stream && !PyErr_Occurred();
 }
 
 struct Matrix {
@@ -124,15 +136,18 @@ void fill(PyObject *o, int64_t rows, int64_t cols, int device, PyObject *codes, 
     }
 }
 
-// Room for a matrix, codes and scales in one allocation.
-PyObject *new_quantized(int64_t rows, int64_t cols, int device, Quantized &q)
+// Room for a matrix, codes and scales in one allocation; the object of such a matrix.
+at::Tensor room_for(int64_t rows, int64_t cols, int device, Quantized &q)
 {
     const int64_t at = (rows * ((cols + 15) / 16 * 16) + 255) / 256 * 256;
     at::Tensor buf = room(at + 4 * rows, device);
     q = {rows, cols, static_cast<int8_t *>(buf.data_ptr()), reinterpret_cast<float *>(static_cast<char *>(buf.data_ptr()) + at)};
+    return buf;
+}
+PyObject *new_quantized(const Quantized &q, int device, at::Tensor &&buf)
+{
     PyObject *o = i8_type->tp_alloc(i8_type, 0);
-    if (!o) return nullptr;
-    fill(o, rows, cols, device, Py_None, Py_None, THPVariable_Wrap(std::move(buf)), q.codes, q.scales);
+    if (o) fill(o, q.rows, q.cols, device, Py_None, Py_None, THPVariable_Wrap(std::move(buf)), q.codes, q.scales);
     return o;
 }
 
@@ -152,6 +167,17 @@ PyObject *guarded(F f)
     return r ? r : Py_NewRef(Py_None);
 }
 PyObject *truth(bool b) { return Py_NewRef(b ? Py_True : Py_False); }
+// What f, which touches no Python object, says.
+template <typename F>
+PyObject *without_lock(F f)
+{
+    bool done;
+    {
+        Unlocked unlocked;
+        done = f();
+    }
+    return truth(done);
+}
 
 // bind(addresses of the entry points in the order above, the class of quantized matrices)
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
@@ -213,15 +239,23 @@ PyObject *i8_quantize(PyObject *, PyObject *const *args, Py_ssize_t n)
         const uint32_t node = (uint32_t)PyLong_AsUnsignedLongMask(args[7]);
         if (PyErr_Occurred() || x.rows > INT32_MAX - 1024 || x.cols > INT32_MAX - 1024) return nullptr;
         Quantized q = {}, t = {};
+        at::Tensor buf, buf_t;
+        {
+            Unlocked unlocked;
+            if (!c.ready()) return nullptr;
+            if (by_rows) buf = room_for(x.rows, x.cols, c.device, q);
+            if (by_cols) buf_t = room_for(x.cols, x.rows, c.device, t);
+            const int64_t bytes = by_cols ? entry.i8_scratch_bytes(x.rows, x.cols) : 0;
+            at::Tensor scratch;
+            if (bytes > 0) scratch = room(bytes, c.device);
+            if (bytes < 0 || entry.i8_quantize(c.h, x.p, x.dtype, x.rows, x.cols, x.ld, stochastic, seed, node, q.codes, q.scales, t.codes, t.scales,
+                                               bytes > 0 ? scratch.data_ptr() : nullptr, (size_t)bytes) != GVQ_OK)
+                return nullptr;
+        }
         Ref out, out_t;
-        if (by_rows) out = Ref(new_quantized(x.rows, x.cols, c.device, q));
-        if (by_cols) out_t = Ref(new_quantized(x.cols, x.rows, c.device, t));
-        const int64_t bytes = by_cols ? entry.i8_scratch_bytes(x.rows, x.cols) : 0;
-        at::Tensor scratch;
-        if (bytes > 0) scratch = room(bytes, c.device);
-        if (bytes < 0 || entry.i8_quantize(c.h, x.p, x.dtype, x.rows, x.cols, x.ld, stochastic, seed, node, q.codes, q.scales, t.codes, t.scales,
-                                           bytes > 0 ? scratch.data_ptr() : nullptr, (size_t)bytes) != GVQ_OK)
-            return nullptr;
+        if (by_rows) out = Ref(new_quantized(q, c.device, std::move(buf)));
+        if (by_cols) out_t = Ref(new_quantized(t, c.device, std::move(buf_t)));
+        if ((by_rows && !out.o) || (by_cols && !out_t.o)) return nullptr;
         return by_rows && by_cols ? PyTuple_Pack(2, out.o, out_t.o) : by_rows ? out.take() : out_t.take();
     });
 }
@@ -236,7 +270,9 @@ PyObject *i8_matmul(PyObject *, PyObject *const *args, Py_ssize_t n)
         if (n != 5 || !open(args[0], args[1], c) || !quantized(args[2], c.device, a) || !quantized(args[3], c.device, b) ||
             !matrix(args[4], c.device, out) || a.cols != b.cols || out.rows != a.rows || out.cols != b.rows)
             return nullptr;
-        return truth(entry.i8_matmul(c.h, a.codes, a.scales, b.codes, b.scales, a.rows, b.rows, a.cols, out.p, out.dtype, out.ld) == GVQ_OK);
+        return without_lock([&] {
+            return c.ready() && entry.i8_matmul(c.h, a.codes, a.scales, b.codes, b.scales, a.rows, b.rows, a.cols, out.p, out.dtype, out.ld) == GVQ_OK;
+        });
     });
 }
 
@@ -251,8 +287,12 @@ PyObject *i8_gated(PyObject *, PyObject *const *args, Py_ssize_t n)
             !quantized(args[4], c.device, u) || !matrix(args[5], c.device, out) || a.cols != g.cols || a.cols != u.cols || g.rows != u.rows ||
             out.rows != a.rows || out.cols != g.rows)
             return nullptr;
-        return truth(entry.i8_gated(c.h, a.codes, a.scales, g.codes, g.scales, u.codes, u.scales, a.rows, g.rows, a.cols, (int)PyLong_AsLong(args[6]),
-                                    out.p, out.dtype, out.ld) == GVQ_OK);
+        const int act = (int)PyLong_AsLong(args[6]);
+        if (PyErr_Occurred()) return nullptr;
+        return without_lock([&] {
+            return c.ready() && entry.i8_gated(c.h, a.codes, a.scales, g.codes, g.scales, u.codes, u.scales, a.rows, g.rows, a.cols, act, out.p,
+                                               out.dtype, out.ld) == GVQ_OK;
+        });
     });
 }
 
@@ -268,12 +308,16 @@ PyObject *gated_forward(PyObject *, PyObject *const *args, Py_ssize_t n)
             return nullptr;
         if (args[7] != Py_None && (!matrix(args[7], c.device, g, h.rows, h.cols, x.dtype) || !matrix(args[8], c.device, u, h.rows, h.cols, x.dtype)))
             return nullptr;
-        const int64_t bytes = aligned(x) && aligned(wg) && aligned(wu) ? 0 : entry.gated_workspace_bytes(x.rows, wg.rows, x.cols, 0, 0);
-        if (bytes < 0) return nullptr;
-        at::Tensor ws;
-        if (bytes > 0) ws = room(bytes, c.device);
-        return truth(entry.gated_forward(c.h, x.p, x.ld, wg.p, wg.ld, wu.p, wu.ld, x.dtype, x.rows, wg.rows, x.cols, (int)PyLong_AsLong(args[6]), h.p,
-                                         h.ld, g.p, g.ld, u.p, u.ld, bytes > 0 ? ws.data_ptr() : nullptr, (size_t)bytes) == GVQ_OK);
+        const int act = (int)PyLong_AsLong(args[6]);
+        if (PyErr_Occurred()) return nullptr;
+        return without_lock([&] {
+            const int64_t bytes = aligned(x) && aligned(wg) && aligned(wu) ? 0 : entry.gated_workspace_bytes(x.rows, wg.rows, x.cols, 0, 0);
+            if (bytes < 0 || !c.ready()) return false;
+            at::Tensor ws;
+            if (bytes > 0) ws = room(bytes, c.device);
+            return entry.gated_forward(c.h, x.p, x.ld, wg.p, wg.ld, wu.p, wu.ld, x.dtype, x.rows, wg.rows, x.cols, act, h.p, h.ld, g.p, g.ld, u.p, u.ld,
+                                       bytes > 0 ? ws.data_ptr() : nullptr, (size_t)bytes) == GVQ_OK;
+        });
     });
 }
 
@@ -307,12 +351,15 @@ PyObject *gated_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
             plain = plain && aligned(x);
         }
         if (!K) return nullptr;
-        const int64_t bytes = entry.gated_workspace_bytes(M, F, K, 1, plain);
-        if (bytes < 0) return nullptr;
-        const at::Tensor ws = room(bytes, c.device);
-        return truth(entry.gated_backward(c.h, dh.p, dh.ld, g.p, g.ld, u.p, u.ld, x.p, x.ld, wg.p, wg.ld, wu.p, wu.ld, dh.dtype, M, F, K,
-                                          (int)PyLong_AsLong(args[8]), dx.p, dx.ld, dg.p, dg.ld, du.p, du.ld, want_g ? dg.dtype : du.dtype,
-                                          ws.data_ptr(), (size_t)bytes) == GVQ_OK);
+        const int act = (int)PyLong_AsLong(args[8]);
+        if (PyErr_Occurred()) return nullptr;
+        return without_lock([&] {
+            const int64_t bytes = entry.gated_workspace_bytes(M, F, K, 1, plain);
+            if (bytes < 0 || !c.ready()) return false;
+            const at::Tensor ws = room(bytes, c.device);
+            return entry.gated_backward(c.h, dh.p, dh.ld, g.p, g.ld, u.p, u.ld, x.p, x.ld, wg.p, wg.ld, wu.p, wu.ld, dh.dtype, M, F, K, act, dx.p, dx.ld,
+                                        dg.p, dg.ld, du.p, du.ld, want_g ? dg.dtype : du.dtype, ws.data_ptr(), (size_t)bytes) == GVQ_OK;
+        });
     });
 }
 
