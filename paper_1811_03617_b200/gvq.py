@@ -1,5 +1,6 @@
 """Thin ctypes binding of libgvq.so: argument marshalling only.  Calls that a step makes once per product (8-bit matrices, the gated block)
-have a shorter way through _binding.so, which takes what is plainly right; everything else goes through here, and errors are raised here.
+have a shorter way through the module of binding.cpp, which takes what is plainly right; everything else goes through here, and errors are
+raised here.
 
 Every function here has the name and the meaning of the C entry point it calls
 (see include/gvq.h); tensors are torch CUDA tensors used purely as device
@@ -11,16 +12,18 @@ from __future__ import annotations
 import ctypes
 import importlib.util
 import math
+import warnings
 from pathlib import Path
 from typing import Optional, Sequence
 
 import torch
 
+from . import build as _build
+
 _PKG = Path(__file__).resolve().parent
 LIB_PATH = _PKG / "libgvq.so"
-BINDING_PATH = _PKG / "_binding.so"
 _lib = None
-_short = None      # the module _binding.so, once the library is loaded
+_short = None      # the module of binding.cpp, once the library is loaded, where it has been built for this Python and this torch
 
 MAX_NODES = 64
 
@@ -41,14 +44,33 @@ class _Layout(ctypes.Structure):
                 ("layer_off", ctypes.POINTER(ctypes.c_int64)), ("layer_len", ctypes.POINTER(ctypes.c_int64))]
 
 
+_ENTRIES = ("gvq_set_stream", "gvq_i8_scratch_bytes", "gvq_i8_quantize", "gvq_i8_matmul", "gvq_i8_gated", "gvq_gated_workspace_bytes",
+            "gvq_gated_forward", "gvq_gated_backward")
+
+
+def _load_short(L):
+    """The module of binding.cpp, bound to the library, or None: calls then take some microseconds more."""
+    path = _build.binding_path()
+    try:
+        if not path.exists():
+            raise ImportError(f"{path} is missing: run `python -m paper_1811_03617_b200.build`")
+        spec = importlib.util.spec_from_file_location(f"{__package__}._binding", path)
+        short = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(short)
+        short.bind(*[ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in _ENTRIES], I8)
+        return short
+    except ImportError as e:
+        warnings.warn(f"gvq: the library is called through ctypes ({e})", RuntimeWarning, stacklevel=3)
+        return None
+
+
 def lib() -> ctypes.CDLL:
-    """Loads libgvq.so and _binding.so (once).  Raises if they have not been built."""
+    """Loads libgvq.so, and the short way to it where there is one (once).  Raises if the library has not been built."""
     global _lib, _short
     if _lib is None:
-        for path in (LIB_PATH, BINDING_PATH):
-            if not path.exists():
-                raise RuntimeError(f"{path} is missing: run `python -m paper_1811_03617_b200.build` "
-                                   "(there is no fallback implementation)")
+        if not LIB_PATH.exists():
+            raise RuntimeError(f"{LIB_PATH} is missing: run `python -m paper_1811_03617_b200.build` "
+                               "(there is no fallback implementation)")
         L = ctypes.CDLL(str(LIB_PATH))
         vp, i32, i64, u64, u32 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_uint64, ctypes.c_uint32
         LP = ctypes.POINTER(_Layout)
@@ -149,13 +171,7 @@ def lib() -> ctypes.CDLL:
         L.gvq_schedule_nodes_over.argtypes = [vp]
         L.gvq_schedule_step.argtypes = [vp, vp, i32, ctypes.POINTER(i32)]
         L.gvq_schedule_counters.argtypes = [vp, ctypes.POINTER(i64), ctypes.POINTER(i64), ctypes.POINTER(i64)]
-        spec = importlib.util.spec_from_file_location(f"{__package__}._binding", BINDING_PATH)
-        short = importlib.util.module_from_spec(spec)
-        spec.loader.exec_module(short)
-        entries = ("gvq_set_stream", "gvq_i8_scratch_bytes", "gvq_i8_quantize", "gvq_i8_matmul", "gvq_i8_gated", "gvq_gated_workspace_bytes",
-                   "gvq_gated_forward", "gvq_gated_backward")
-        short.bind(*[ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in entries], I8)
-        _lib, _short = L, short
+        _lib, _short = L, _load_short(L)
     return _lib
 
 
