@@ -584,6 +584,11 @@ gvq_status gvq_i8_matmul(gvq_ctx *ctx, const int8_t *a_codes, const float *a_sca
    next; calls that run at the same time (graphs replayed on two streams) need one each.
    Outputs lie apart from one another, from the workspace and from what the call reads. */
 typedef enum { GVQ_SILU = 0, GVQ_GELU = 1, GVQ_GELU_TANH = 2, GVQ_RELU = 3, GVQ_SIGMOID = 4 } gvq_activation;
+/* How exact the operands dg and du of a backward pass's products are, or'ed to its `activation` and to the `backward` (1) of
+   gvq_gated_workspace_bytes(), the same to both: one 16-bit number each; two, the second what rounding the first left, for twice the
+   multiplications; or by the size of the call, two up to M * F * K = 2^26 and one beyond.  Gradients of one accuracy at every size, and a
+   workspace that is enough for every smaller call, need one of the first two. */
+typedef enum { GVQ_SLOPES_BY_SIZE = 0, GVQ_SLOPES_ROUNDED = 0x100, GVQ_SLOPES_PRECISE = 0x200 } gvq_gated_slopes;
 
 int64_t gvq_gated_workspace_bytes(int64_t M, int64_t F, int64_t K, int backward, int aligned);
 /* gate_opt, up_opt: both NULL, or [M][F] that receive g and u (rounded to dtype) for the backward pass. */
@@ -591,8 +596,7 @@ gvq_status gvq_gated_forward(gvq_ctx *ctx, const void *x, int64_t ldx, const voi
                              int dtype, int64_t M, int64_t F, int64_t K, int activation, void *h, int64_t ldh, void *gate_opt,
                              int64_t ld_gate_out, void *up_opt, int64_t ld_up_out, void *workspace, size_t workspace_bytes);
 /* Gradients from dh and what the forward pass kept:
-     dg = dh * u * act'(g),  du = dh * act(g)            (rounded to dtype: they are operands of the products below; up to
-                                                         M * F * K = 2^26 what the rounding left is multiplied too)
+     dg = dh * u * act'(g),  du = dh * act(g)            (one or two numbers of dtype each: gvq_gated_slopes)
      dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x     (fp32 sums, rounded once)
    In half precision dg and du are held times a power of two that brings the largest finite entry of both to 2^15 .. 2^16 (or half of that),
    and the sums are multiplied by its reciprocal: entries of any size up to fp32's range are products' operands, and those down to 2^-29

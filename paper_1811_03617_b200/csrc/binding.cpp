@@ -352,9 +352,9 @@ PyObject *gated_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
         }
         if (!K) return nullptr;
         const int act = (int)PyLong_AsLong(args[8]);
-        if (PyErr_Occurred()) return nullptr;
+        if (act < 0 || PyErr_Occurred()) return nullptr;
         return without_lock([&] {
-            const int64_t bytes = entry.gated_workspace_bytes(M, F, K, 1, plain);
+            const int64_t bytes = entry.gated_workspace_bytes(M, F, K, 1 | (act & (GVQ_SLOPES_ROUNDED | GVQ_SLOPES_PRECISE)), plain);
             if (bytes < 0 || !c.ready()) return false;
             const at::Tensor ws = room(bytes, c.device);
             return entry.gated_backward(c.h, dh.p, dh.ld, g.p, g.ld, u.p, u.ld, x.p, x.ld, wg.p, wg.ld, wu.p, wu.ld, dh.dtype, M, F, K, act, dx.p, dx.ld,

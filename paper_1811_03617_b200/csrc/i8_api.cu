@@ -26,14 +26,19 @@ Launch launch_of(const gvq_ctx *ctx)
 
 // The gated block's workspace: dg and du of a backward pass and what holding them in half precision takes, then copies of operands whose rows TMA cannot address.
 int64_t padded(int64_t n, int per) { return (n + per - 1) / per * per; }
-// Matrices of a backward pass: dg and du, and where the products are short what rounding them left.  It is there that few outputs carry a
-// gradient's norm, so that roundings do not average: of 99 thousand blocks' gradients with M, F and K spread over 65..8192, 33..8192 and
-// 33..4096, 5 % were further from 64 bits than 1.5 times a 16-bit result's own rounding, the worst 3.3 times (1.41 in the mean); with
-// the low halves up to 2^26 multiply-adds 0.4 %, the worst 1.7.  And there they cost least (us, dx and both weights' gradients, with and without: 100 x 100
-// x 100 10.6, 9.0; 150 x 400 x 200 9.1, 7.2; 386 x 380 x 464 13.9, 12.4; the call from Python takes 10), while beyond they double the
-// tensor pipe's time.
+// Matrices of a backward pass: dg and du, and where they are held in two halves what rounding them left.  Rounded, they add as much to a
+// gradient's error as rounding a 16-bit gradient does: sqrt 2 of that in all where both average, but few outputs may carry a gradient's norm
+// where products are short (of 99 thousand blocks' gradients with M, F and K spread over 65..8192, 33..8192 and 33..4096, the worst
+// 3.3 times, 5 % more than 1.5 times; with the low halves up to 2^26 multiply-adds 1.7 times and 0.4 %).  There the low halves cost least
+// (us, dx and both weights' gradients, with and without: 100 x 100 x 100 10.6, 9.0; 150 x 400 x 200 9.1, 7.2; 386 x 380 x 464 13.9, 12.4; the
+// call from Python takes 10); with more multiply-adds they double the tensor pipe's time.  Where a caller does not say, the size does.
 constexpr int64_t kShort = 1 << 26;
-int slopes_of(int64_t M, int64_t F, int64_t K) { return M * F <= kShort / K ? 4 : 2; }
+constexpr int kSlopes = GVQ_SLOPES_ROUNDED | GVQ_SLOPES_PRECISE;
+bool slopes_ok(int mode) { return (mode & kSlopes) != kSlopes; }
+int slopes_of(int64_t M, int64_t F, int64_t K, int mode)
+{
+    return mode & GVQ_SLOPES_PRECISE ? 4 : mode & GVQ_SLOPES_ROUNDED ? 2 : M * F <= kShort / K ? 4 : 2;
+}
 int64_t bytes_of(int64_t rows, int64_t cols) { return padded(rows * padded(cols, 8) * 2, 256); }
 bool rows_aligned(const void *p, int64_t rows, int64_t ld) { return aligned16(p) && (rows == 1 || ld % 8 == 0); }
 // A row that is alone may have any leading dimension: one that a tensor map takes.
@@ -137,8 +142,8 @@ gvq_status gvq_i8_gated(gvq_ctx *ctx, const int8_t *a_codes, const float *a_scal
 
 int64_t gvq_gated_workspace_bytes(int64_t M, int64_t F, int64_t K, int backward, int aligned)
 {
-    if (!sizes_ok(M, F) || !sizes_ok(M, K) || !sizes_ok(F, K)) return -1;
-    return (backward ? slopes_of(M, F, K) * bytes_of(M, F) + kGatedRoom : 0) + (aligned ? 0 : bytes_of(M, K) + 2 * bytes_of(F, K));
+    if (!sizes_ok(M, F) || !sizes_ok(M, K) || !sizes_ok(F, K) || !slopes_ok(backward)) return -1;
+    return (backward ? slopes_of(M, F, K, backward) * bytes_of(M, F) + kGatedRoom : 0) + (aligned ? 0 : bytes_of(M, K) + 2 * bytes_of(F, K));
 }
 
 gvq_status gvq_gated_forward(gvq_ctx *ctx, const void *x, int64_t ldx, const void *w_gate, int64_t ld_gate, const void *w_up, int64_t ld_up,
@@ -173,8 +178,10 @@ gvq_status gvq_gated_backward(gvq_ctx *ctx, const void *dh, int64_t ld_dh, const
                               size_t workspace_bytes)
 {
     const bool dw = dw_gate_opt || dw_up_opt;
+    const int slopes = activation & kSlopes;
+    activation &= ~kSlopes;
     if (!ctx || !dh || !gate || !up || (!dx_opt && !dw) || (dx_opt && (!w_gate || !w_up)) || (dw && !x)) return GVQ_ERR_NULL;
-    if (!sizes_ok(M, F) || !sizes_ok(M, K) || !sizes_ok(F, K) || !half_ok(dtype) || (dw && !dtype_ok(dw_dtype)) || !act_ok(activation) ||
+    if (!sizes_ok(M, F) || !sizes_ok(M, K) || !sizes_ok(F, K) || !half_ok(dtype) || (dw && !dtype_ok(dw_dtype)) || !act_ok(activation) || !slopes_ok(slopes) ||
         ld_dh < F || ld_gate_in < F || ld_up_in < F || (dw && ldx < K) || (dx_opt && (ld_gate < K || ld_up < K || ld_dx < K)) ||
         (dw_gate_opt && ld_dw_gate < K) || (dw_up_opt && ld_dw_up < K))
         return GVQ_ERR_SHAPE;
@@ -182,12 +189,12 @@ gvq_status gvq_gated_backward(gvq_ctx *ctx, const void *dh, int64_t ld_dh, const
         if (!entry_aligned(p, dtype)) return GVQ_ERR_ALIGN;
     if (!entry_aligned(dw_gate_opt, dw_dtype) || !entry_aligned(dw_up_opt, dw_dtype) || !aligned16(workspace)) return GVQ_ERR_ALIGN;
     Operand ops[3] = {{dw ? x : nullptr, M, K, ldx}, {dx_opt ? w_gate : nullptr, F, K, ld_gate}, {dx_opt ? w_up : nullptr, F, K, ld_up}};
-    if (!workspace || workspace_bytes < (size_t)gvq_gated_workspace_bytes(M, F, K, 1, all_aligned(ops, 3))) return GVQ_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < (size_t)gvq_gated_workspace_bytes(M, F, K, 1 | slopes, all_aligned(ops, 3))) return GVQ_ERR_WORKSPACE;
     if (!ctx->encode_fn) return GVQ_ERR_UNSUPPORTED;
     DeviceGuard guard(ctx->device);
     const Launch l = launch_of(ctx);
     char *at = static_cast<char *>(workspace);
-    const int n = slopes_of(M, F, K);
+    const int n = slopes_of(M, F, K, slopes);
     char *room = at + n * bytes_of(M, F);
     const RowCopies copies = align_operands(ops, 3, room + kGatedRoom);
     GatedGrads g = {{}, {ops[1].p, ops[2].p}, ops[0].p, padded(F, 8), {ops[1].ld, ops[2].ld}, ops[0].ld, dtype, dw_dtype, M, F, K,

@@ -471,6 +471,9 @@ def _activation(name: str) -> int:
     return a
 
 
+SLOPES = {None: 0, False: 0x100, True: 0x200}      # gvq_gated_slopes
+
+
 def _half_type(t: torch.Tensor, what: str) -> int:
     if t.dtype is torch.bfloat16:
         return 1
@@ -767,11 +770,12 @@ class Context:
             raise ValueError(f"{what}: a matrix of {rows} x {cols} is wanted, not {r} x {c}")
         return ld
 
-    def _gated_workspace(self, what: str, M: int, F: int, K: int, backward: bool, aligned: bool):
-        """(tensor or None, address, bytes); aligned: the rows of x and the weights, as far as they are read, start at 16-byte boundaries."""
+    def _gated_workspace(self, what: str, M: int, F: int, K: int, backward: int, aligned: bool):
+        """(tensor or None, address, bytes); backward: 0, or 1 and gvq_gated_slopes; aligned: the rows of x and the weights, as far as they
+        are read, start at 16-byte boundaries."""
         if aligned and not backward:
             return None, None, 0
-        n = lib().gvq_gated_workspace_bytes(M, F, K, 1 if backward else 0, 1 if aligned else 0)
+        n = lib().gvq_gated_workspace_bytes(M, F, K, backward, 1 if aligned else 0)
         if n < 0:
             raise GvqError(2, what)
         ws = torch.empty(n, dtype=torch.uint8, device=self._torch_device())
@@ -800,7 +804,7 @@ class Context:
             raise ValueError(f"{what}: both projections are kept, or neither")
         px, pg, pu = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr()
         aligned = not ((px | pg | pu) & 15 or (M > 1 and ldx & 7) or (F > 1 and (lg | lu) & 7))
-        ws, at, n = self._gated_workspace(what, M, F, K, False, aligned)
+        ws, at, n = self._gated_workspace(what, M, F, K, 0, aligned)
         self._sync_stream()
         status = lib().gvq_gated_forward(self._h, px, ldx, pg, lg, pu, lu, dtype, M, F, K, a, out.data_ptr(), lh, *kept, at, n)
         if status:
@@ -808,14 +812,18 @@ class Context:
         return out
 
     def gated_backward(self, dh, gate, up, x, w_gate, w_up, act: str = "silu", dx: Optional[torch.Tensor] = None,
-                       dw_gate: Optional[torch.Tensor] = None, dw_up: Optional[torch.Tensor] = None) -> None:
+                       dw_gate: Optional[torch.Tensor] = None, dw_up: Optional[torch.Tensor] = None, precise: Optional[bool] = None) -> None:
         """gvq_gated_backward: the gradients that are given room for.  dx [M, K] is of the operands' type; dw_gate, dw_up [F, K] are
-        float32, bfloat16 or float16, of one type.  x may be None where neither is wanted, the weights where dx is not."""
-        if _short is not None and _short.gated_backward(self._address, self.device, dh, gate, up, x, w_gate, w_up, ACTIVATION.get(act, -1), dx,
-                                                        dw_gate, dw_up):
-            return
+        float32, bfloat16 or float16, of one type.  x may be None where neither is wanted, the weights where dx is not.  precise: whether dg
+        and du keep what rounding them to 16 bits leaves, for twice the multiplications; None: up to M F K = 2^26."""
         what = "gated_backward"
-        a, half = _activation(act), self._half
+        slopes = SLOPES.get(precise)
+        if slopes is None:
+            raise ValueError(f"{what}: precise is True, False or None")
+        if _short is not None and _short.gated_backward(self._address, self.device, dh, gate, up, x, w_gate, w_up, ACTIVATION.get(act, -1) | slopes,
+                                                        dx, dw_gate, dw_up):
+            return
+        a, half = _activation(act) | slopes, self._half
         M, F, ldh = _rows(dh, self.device, what)
         like, dtype = dh.dtype, _half_type(dh, what)
         lgi, lui = half(what, gate, like, M, F), half(what, up, like, M, F)
@@ -839,7 +847,7 @@ class Context:
                 ldg, pdg = half(what, dw_gate, dw.dtype, F, K), dw_gate.data_ptr()
             if dw_up is not None:
                 ldu, pdu = half(what, dw_up, dw.dtype, F, K), dw_up.data_ptr()
-        ws, at, n = self._gated_workspace(what, M, F, K, True, not odd)
+        ws, at, n = self._gated_workspace(what, M, F, K, 1 | slopes, not odd)
         self._sync_stream()
         status = lib().gvq_gated_backward(self._h, dh.data_ptr(), ldh, gate.data_ptr(), lgi, up.data_ptr(), lui, px, ldx, pg, lg, pu, lu,
                                           dtype, M, F, K, a, pdx, ldd, pdg, ldg, pdu, ldu, dw_dtype, at, n)

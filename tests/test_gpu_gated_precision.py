@@ -177,3 +177,30 @@ def test_a_captured_backward_pass_takes_its_power_of_two_from_its_own_inputs(ctx
         torch.cuda.synchronize()
         for k in eager:
             assert torch.equal(captured[k], eager[k]) and bool((eager[k] != 0).any())
+
+
+# on both sides of 2^26 multiply-adds
+@pytest.mark.parametrize("M,F,K", SIZES + [(64, 2056, 511), (64, 2056, 510), (2100, 1030, 1000)])
+@pytest.mark.parametrize("dtype", [BF, F16])
+def test_the_caller_says_how_exact_the_products_operands_are(ctx, M, F, K, dtype):
+    """precise: what is off by half a step of dg and du is off by half a step of half a step, at every size."""
+    names = ("dx", "dw_gate", "dw_up")
+    exact, rounded, auto = (_gradients(ctx, M, F, K, dtype, "silu", 1.0, precise=p) for p in (True, False, None))
+    _check(*exact, M, F, dtype, HALF[dtype] ** 2, names)
+    _check(*rounded, M, F, dtype, HALF[dtype], names)
+    for k in names:
+        assert torch.equal(auto[0][k], (exact if M * F * K <= 2 ** 26 else rounded)[0][k])
+    if dtype == BF and M > 1:      # (of these sums of roundings fp32 keeps far more)
+        want = rounded[1]["dw_gate"]
+        off = [float((r[0]["dw_gate"].double() - want).norm() / want.norm()) for r in (exact, rounded)]
+        assert off[0] < 2.0 ** -14 and off[1] > 2.0 ** -11
+
+
+@pytest.mark.parametrize("precise", [True, False, None])
+def test_both_ways_of_the_binding_take_what_the_caller_says(ctx, precise, monkeypatch):
+    from paper_1811_03617_b200 import gvq
+    assert gvq._short is not None
+    short = _gradients(ctx, 700, 520, 264, BF, "gelu", 1.0, precise=precise)[0]
+    monkeypatch.setattr(gvq, "_short", None)
+    for k, t in _gradients(ctx, 700, 520, 264, BF, "gelu", 1.0, precise=precise)[0].items():
+        assert torch.equal(t, short[k])
