@@ -74,6 +74,9 @@ struct Pair {
     int blocks;                        // CTAs of the first
 };
 
+__device__ __forceinline__ const Params &params_of(const Params &p, int) { return p; }
+__device__ __forceinline__ const Params &params_of(const Pair &p, int which) { return p.p[which]; }
+
 template <int CG, int BN, bool FEW> struct Shape {
     static constexpr uint32_t B_BYTES = BN / CG * 128, LOADED = A_BYTES + B_BYTES;
     static constexpr uint32_t ROOM = FEW ? 168 * 1024 : 200 * 1024;   // for the stages
@@ -363,7 +366,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) product_kernel(const __grid_const
         blocks = which ? blocks - all.blocks : all.blocks;
         if (which) block -= all.blocks;
     }
-    const Params &prm = [&]() -> const Params & { if constexpr (PAIR) return all.p[which]; else return all; }();
+    const Params &prm = params_of(all, which);
     const bool a_mn = PAIR ? prm.a_mn : A_MN;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
