@@ -204,3 +204,29 @@ def test_both_ways_of_the_binding_take_what_the_caller_says(ctx, precise, monkey
     monkeypatch.setattr(gvq, "_short", None)
     for k, t in _gradients(ctx, 700, 520, 264, BF, "gelu", 1.0, precise=precise)[0].items():
         assert torch.equal(t, short[k])
+
+
+def test_gradients_along_themselves_are_the_differences_of_a_loss(ctx):
+    """L = sum(dh * h) in 64 bits, each input moved along its own gradient, so that all terms have one sign: the quotient of differences is
+    off by step^2 times a third derivative (1e-8 of it), and a gradient's length by less than its roundings: gate, up, dg, du and the
+    gradient itself to 2^-8 each at most, as they average out, and 1 % covers them.  1.1 times a gradient would be ten times that off."""
+    M, F, K = 70, 96, 80
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x, wg, wu, dh = ((torch.randn(r, c, generator=g, device="cuda") * s).to(BF) for r, c, s in
+                     ((M, K, 1.0), (F, K, 0.125), (F, K, 0.125), (M, F, 1.0)))
+    for name in ("silu", "gelu", "gelu_tanh", "relu", "sigmoid"):
+        h, gate, up, dx = (torch.empty(r, c, dtype=BF, device="cuda") for r, c in ((M, F), (M, F), (M, F), (M, K)))
+        ctx.gated_forward(x, wg, wu, h, act=name, gate=gate, up=up)
+        dwg, dwu = torch.empty(F, K, device="cuda"), torch.empty(F, K, device="cuda")
+        ctx.gated_backward(dh, gate, up, x, wg, wu, act=name, dx=dx, dw_gate=dwg, dw_up=dwu)
+
+        def loss(x, wg, wu):
+            return float((dh.double() * act(name, x @ wg.T)[0] * (x @ wu.T)).sum())
+        ins = [t.double() for t in (x, wg, wu)]
+        for j, grad in enumerate((dx, dwg, dwu)):
+            norm = float(grad.double().norm())
+            d = grad.double() / norm
+            e = 1e-4
+            moved = [[t + (s * e * d if i == j else 0) for i, t in enumerate(ins)] for s in (1, -1)]
+            want = (loss(*moved[0]) - loss(*moved[1])) / (2 * e)
+            assert abs(norm - want) <= 0.01 * want, (name, j, norm, want)
