@@ -7,7 +7,7 @@
 //  i8_dequantize_kernel
 //
 // Measured, from memory, in us (the bytes at the copy rate): rows of 8192 x 4096 bf16 20.0 nearest, 28 stochastic (15.4), fp32 28 and 32
-// (25.7); columns of 2048 x 4096 bf16 in strips 9.9 and 12.6 (3.8); columns of 8192 x 4096 bf16, read twice, 30 and 41 (15.4), fp32
+// (25.7); columns of 2048 x 4096 bf16 in strips 9.9 and 12.6 (3.8); columns of 8192 x 4096 bf16, gone through twice, 30 and 41 (15.4), fp32
 // 60 and 70 (25.7); 777 x 1083 rows 3.3, columns 6.5, both 8.1 (0.4).  Of large ones instructions take as long as memory: of the nearest codes
 // the conversions, maxima and packing, of the stochastic ones the random words, 10 integer instructions for two entries.  Small ones
 // are a launch and the way to memory and back.
@@ -383,7 +383,7 @@ __device__ __forceinline__ void copy16(void *to, const void *from, int bytes)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(to)), "l"(from), "r"(bytes) : "memory");
 }
-// A CTA: a tile of 128 x 128 entries, from the end: what i8_max_kernel has read last is in L2.  Shared memory and what follows as above.
+// A CTA: a tile of 128 x 128 entries, from the end: what i8_max_kernel has read last is in L2 (of 8192 x 4096 bf16 a fifth comes from memory again).  Shared memory and what follows as above.
 template <typename T, bool SR, bool VEC>
 __global__ void __launch_bounds__(256) i8_tile_kernel(const QuantParams prm)
 {
