@@ -5,7 +5,7 @@
 // launch's.
 // Arguments are unpacked with the interpreter's lock, and the call and its allocations run without it: a launch waits where the stream's
 // queue is full, which may be emptied by another Python thread alone (a host function in the stream), and an allocation may wait for
-// the device.
+// the device.  Calls of one context take turns: its stream is set for each.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -14,6 +14,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <mutex>
 #include <utility>
 
 #include "gvq.h"
@@ -52,6 +53,12 @@ struct Context {
     int device;
     // The context's stream becomes torch's current one.
     bool ready() const { return entry.set_stream(h, c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream()) == GVQ_OK; }
+    // What its calls take in turn, without the interpreter's lock; contexts may share one.
+    std::mutex &turn() const
+    {
+        static std::mutex turns[16];
+        return turns[(reinterpret_cast<uintptr_t>(h) >> 6) % 16];
+    }
 };
 // A context's handle and device.
 bool open(PyObject *handle, PyObject *device, Context &c)
@@ -167,14 +174,15 @@ PyObject *guarded(F f)
     return r ? r : Py_NewRef(Py_None);
 }
 PyObject *truth(bool b) { return Py_NewRef(b ? Py_True : Py_False); }
-// What f, which touches no Python object, says.
+// What f, a call of the context that touches no Python object, says.
 template <typename F>
-PyObject *without_lock(F f)
+PyObject *without_lock(const Context &c, F f)
 {
     bool done;
     {
         Unlocked unlocked;
-        done = f();
+        const std::lock_guard<std::mutex> hold(c.turn());
+        done = c.ready() && f();
     }
     return truth(done);
 }
@@ -242,6 +250,7 @@ PyObject *i8_quantize(PyObject *, PyObject *const *args, Py_ssize_t n)
         at::Tensor buf, buf_t;
         {
             Unlocked unlocked;
+            const std::lock_guard<std::mutex> hold(c.turn());
             if (!c.ready()) return nullptr;
             if (by_rows) buf = room_for(x.rows, x.cols, c.device, q);
             if (by_cols) buf_t = room_for(x.cols, x.rows, c.device, t);
@@ -270,8 +279,8 @@ PyObject *i8_matmul(PyObject *, PyObject *const *args, Py_ssize_t n)
         if (n != 5 || !open(args[0], args[1], c) || !quantized(args[2], c.device, a) || !quantized(args[3], c.device, b) ||
             !matrix(args[4], c.device, out) || a.cols != b.cols || out.rows != a.rows || out.cols != b.rows)
             return nullptr;
-        return without_lock([&] {
-            return c.ready() && entry.i8_matmul(c.h, a.codes, a.scales, b.codes, b.scales, a.rows, b.rows, a.cols, out.p, out.dtype, out.ld) == GVQ_OK;
+        return without_lock(c, [&] {
+            return entry.i8_matmul(c.h, a.codes, a.scales, b.codes, b.scales, a.rows, b.rows, a.cols, out.p, out.dtype, out.ld) == GVQ_OK;
         });
     });
 }
@@ -289,8 +298,8 @@ PyObject *i8_gated(PyObject *, PyObject *const *args, Py_ssize_t n)
             return nullptr;
         const int act = (int)PyLong_AsLong(args[6]);
         if (PyErr_Occurred()) return nullptr;
-        return without_lock([&] {
-            return c.ready() && entry.i8_gated(c.h, a.codes, a.scales, g.codes, g.scales, u.codes, u.scales, a.rows, g.rows, a.cols, act, out.p,
+        return without_lock(c, [&] {
+            return entry.i8_gated(c.h, a.codes, a.scales, g.codes, g.scales, u.codes, u.scales, a.rows, g.rows, a.cols, act, out.p,
                                                out.dtype, out.ld) == GVQ_OK;
         });
     });
@@ -310,9 +319,9 @@ PyObject *gated_forward(PyObject *, PyObject *const *args, Py_ssize_t n)
             return nullptr;
         const int act = (int)PyLong_AsLong(args[6]);
         if (PyErr_Occurred()) return nullptr;
-        return without_lock([&] {
+        return without_lock(c, [&] {
             const int64_t bytes = aligned(x) && aligned(wg) && aligned(wu) ? 0 : entry.gated_workspace_bytes(x.rows, wg.rows, x.cols, 0, 0);
-            if (bytes < 0 || !c.ready()) return false;
+            if (bytes < 0) return false;
             at::Tensor ws;
             if (bytes > 0) ws = room(bytes, c.device);
             return entry.gated_forward(c.h, x.p, x.ld, wg.p, wg.ld, wu.p, wu.ld, x.dtype, x.rows, wg.rows, x.cols, act, h.p, h.ld, g.p, g.ld, u.p, u.ld,
@@ -353,9 +362,9 @@ PyObject *gated_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
         if (!K) return nullptr;
         const int act = (int)PyLong_AsLong(args[8]);
         if (act < 0 || PyErr_Occurred()) return nullptr;
-        return without_lock([&] {
+        return without_lock(c, [&] {
             const int64_t bytes = entry.gated_workspace_bytes(M, F, K, 1 | (act & (GVQ_SLOPES_ROUNDED | GVQ_SLOPES_PRECISE)), plain);
-            if (bytes < 0 || !c.ready()) return false;
+            if (bytes < 0) return false;
             const at::Tensor ws = room(bytes, c.device);
             return entry.gated_backward(c.h, dh.p, dh.ld, g.p, g.ld, u.p, u.ld, x.p, x.ld, wg.p, wg.ld, wu.p, wu.ld, dh.dtype, M, F, K, act, dx.p, dx.ld,
                                         dg.p, dg.ld, du.p, du.ld, want_g ? dg.dtype : du.dtype, ws.data_ptr(), (size_t)bytes) == GVQ_OK;

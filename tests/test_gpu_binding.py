@@ -46,3 +46,29 @@ def test_other_threads_run_while_a_call_waits(call):
     assert max(gaps) < 0.15 and len(gaps) > 50
     assert gvq.I8(64, 64).rows == 64 and ctx.i8_quantize(x).rows == 64
     ctx.device_status()
+
+
+def test_threads_may_share_a_context():
+    """Calls of one context take turns, each on its own thread's stream: what a stream has written before a call is what the call reads."""
+    from paper_1811_03617_b200 import gvq
+    ctx, wrong = gvq.Context(gvq.HostLayout(4, 4, [0], [4])), []
+    w = ctx.i8_quantize(torch.eye(512, device="cuda"))
+    want = ctx.i8_matmul(ctx.i8_quantize(torch.ones(64, 512, device="cuda")), w, torch.empty(64, 512, device="cuda"))
+    torch.cuda.synchronize()
+
+    def work(k):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            x, y = torch.empty(64, 512, device="cuda"), torch.empty(64, 512, device="cuda")
+            for i in range(200):
+                x.zero_()
+                x.add_(float(2 ** ((i + k) % 7)))
+                ctx.i8_matmul(ctx.i8_quantize(x), w, y)
+                if not torch.equal(y, want * 2.0 ** ((i + k) % 7)):
+                    wrong.append((k, i))
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    ctx.device_status()
+    assert not wrong
