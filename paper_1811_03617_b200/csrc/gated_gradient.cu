@@ -84,7 +84,8 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v)      // 256 threads
 // 6e-8), and those past 65504 infinite, although fp32 sums and the weights' gradients in fp32 hold them.  So they are held times a power of
 // two, the largest finite entry of both between 2^15 and 2^16, and the products' epilogues undo it (exactly): entries down to 2^-29 of the
 // largest keep their 11 bits.  The largest has to be known before the first is rounded, so inputs are read once more (all gradients in
-// fp16, us, with and without: 100 x 100 x 100 18.5, 15.8; 777 x 1029 x 515 28.7, 24.6; 2048 x 2048 x 1024 49.1, 40.7; 8192 x 8192 x 512 403, 315).
+// fp16, us, with and without: 100 x 100 x 100 12, 9.7; 777 x 1029 x 515 25, 19; 2048 x 2048 x 1024 40, 31; 8192 x 8192 x 512 434, 338).  Two or
+// three chunks of a thread on their way at a time are no faster (777 x 1029 x 515 26 and 28).
 // A bfloat16 has fp32's exponents and needs none of this.
 // A CTA leaves its entries' largest exponent, as fp32 has it; one more where times a power of two up to 2^16 it would round past 65504.
 constexpr int kMostTops = 1024;
